@@ -267,10 +267,101 @@ int fem_bwd_f32(const float *q, const float *k, const float *v, const float *bet
                 int B, int H, int T, int d, int causal, void *stream);
 
 /*
+ * The paged key/value cache of a serving program, and the read over it.  The
+ * paper has no counterpart of the paging; the read is fem_decode's, for any
+ * number of new tokens of many sequences of different lengths at once.
+ *
+ * A cache is caller-owned device memory in pages of page_size positions:
+ *   k, v         : [num_pages, H, page_size, d], contiguous, 16-byte aligned
+ *   k_exp, v_exp : uint8 [num_pages, H, page_size] (FEM_CACHE_E4M3), else NULL
+ *   page_size    : 16, 32, 64, 128 or 256
+ *   d            : a multiple of 16 up to 256
+ * Formats:
+ *   FEM_CACHE_BF16  bf16 elements
+ *   FEM_CACHE_E4M3  8-bit e4m3 codes with one power-of-two scale 2^e per
+ *                   (token, head) row, e the smallest with max |x| <= 448 2^e
+ *                   (e >= -100), stored as the byte e + 127; a row that holds an
+ *                   infinity or NaN gets the byte 255 and reads back as NaN.  The
+ *                   value code * 2^e is a bf16 number exactly.
+ *   FEM_CACHE_F32   float32 elements
+ * Sequence s's position i lives in page block_table[s * max_pages + i /
+ * page_size], row i % page_size; table entries past a sequence's length are not
+ * read.  Slots, tables, offsets and lengths are device arrays and are not
+ * inspected on the host.  An entry that points outside its buffers is left out
+ * (a key that is not there, a row not written, a gathered row of zeros) and
+ * recorded: fem_check_device_error() then returns FEM_ERR_INVALID_ARG.
+ */
+typedef enum { FEM_CACHE_BF16 = 0, FEM_CACHE_E4M3 = 1, FEM_CACHE_F32 = 2 } fem_cache_format;
+
+typedef struct {
+    void *k, *v;
+    void *k_exp, *v_exp;
+    int format; /* fem_cache_format */
+    int num_pages, H, page_size, d;
+} fem_paged_cache;
+
+/*
+ * fem_cache_write -- puts N tokens' keys and values into the cache.
+ *   k, v  : device, [N, H, d] bf16 (FEM_CACHE_F32: float32), d fastest; token
+ *           and head strides in elements, so both may be views of one
+ *           projection's output; 16-byte aligned, strides multiples of 16 bytes
+ *   slots : device, int64 [N]: page * page_size + row of each token; negative:
+ *           the token is left out (padding).  Which of two tokens with one slot
+ *           stays is not defined.
+ * N = 0 does nothing.
+ */
+int fem_cache_write(const fem_paged_cache *cache, const void *k, const void *v, int64_t k_stride_n,
+                    int64_t k_stride_h, int64_t v_stride_n, int64_t v_stride_h, const int64_t *slots, int N,
+                    void *stream);
+
+/*
+ * fem_cache_gather -- reads stretches of cached sequences back.
+ *   starts       : device, int32 [S]: first position of sequence s's stretch
+ *   offsets      : device, int32 [S + 1], ascending from 0: its rows of the output
+ *   k_out, v_out : device, [total, H, d] bf16 (FEM_CACHE_F32: float32), 16-byte
+ *                  aligned; total = offsets[S] as the host knows it
+ * total = 0 does nothing.
+ */
+int fem_cache_gather(const fem_paged_cache *cache, const int *block_table, int max_pages, const int *starts,
+                     const int *offsets, int S, void *k_out, void *v_out, int total, void *stream);
+
+/*
+ * fem_paged_read -- the read of new tokens over the cache that already holds
+ * their own keys and values.  Sequence s has the query rows q_offsets[s] ..
+ * q_offsets[s + 1] - 1 (n of them) and ctx_lens[s] cached positions, the last n
+ * of which are the new tokens' own.  Row t of n sees the positions
+ * i < ctx - n + t + 1 (causal) or every i < ctx:
+ *
+ *   s_i = q . k_i / sqrt(d),  o_j = (1/beta_j) log sum_i softmax(s)_i exp(beta_j v_ij),
+ *   lse = LSE_i s_i;  beta_j = 0, or beta NULL: o_j = sum_i softmax(s)_i v_ij
+ *
+ * A row that sees no position gives o = 0 and lse = -infinity.
+ *   q         : device, [N, Hq, d] bf16 (FEM_CACHE_F32: float32), strides as in
+ *               fem_cache_write; Hq a multiple of the cache's H, and query heads
+ *               g Hq/H .. (g+1) Hq/H - 1 read key/value head g
+ *   beta      : device, float32 [H, d], or NULL: it belongs to the values, so
+ *               the query heads of a group share it
+ *   q_offsets : device, int32 [S + 1], ascending;  ctx_lens: device, int32 [S]
+ *   max_q     : host, at least the largest n (a bound that chooses how rows are
+ *               split over the GPU; n above it is still read correctly)
+ *   out       : device, [N, Hq, d], contiguous, q's type (bf16 or float32)
+ *   lse       : device, float32 [N, Hq], or NULL
+ * Rows that no sequence owns are not written.  N = 0 does nothing.  Accuracy:
+ * scores, softmax statistics and sums in fp32; FEM_CACHE_F32 and head dimensions
+ * other than 64 and 128 are exact to fp32 rounding.
+ */
+int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride_n, int64_t q_stride_h,
+                   const float *beta, const int *q_offsets, const int *ctx_lens, const int *block_table,
+                   int max_pages, int S, int N, int Hq, int max_q, int causal, void *out, float *lse,
+                   void *stream);
+
+/*
  * fem_check_device_error -- synchronises `stream`, then returns FEM_OK, or
  * FEM_ERR_TIMEOUT if any kernel of this library on the current device gave up
  * on a bounded wait since the last check (the word is cleared), or
- * FEM_ERR_CUDA if the synchronisation failed.
+ * FEM_ERR_INVALID_ARG if none did but a paged-cache call met a slot, page or
+ * row range outside its buffers (the word is cleared), or FEM_ERR_CUDA if the
+ * synchronisation failed.
  */
 int fem_check_device_error(void *stream);
 

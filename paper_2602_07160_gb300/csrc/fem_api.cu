@@ -11,6 +11,7 @@
 #include <cudaTypedefs.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdlib>
 #include <cstring>
 #include <mutex>
@@ -19,6 +20,7 @@
 #include "fem.h"
 #include "fem_chunks.h"
 #include "fem_launch.h"
+#include "fem_paged.cuh"
 
 namespace fem {
 namespace {
@@ -750,9 +752,104 @@ int fem_check_device_error(void *stream) {
   if (word) {
     const unsigned zero = 0;
     if (cudaMemcpy(ds->err, &zero, sizeof(zero), cudaMemcpyHostToDevice) != cudaSuccess) return FEM_ERR_CUDA;
-    return FEM_ERR_TIMEOUT;
+    return (word & ~kErrPageRange) ? FEM_ERR_TIMEOUT : FEM_ERR_INVALID_ARG;
   }
   return FEM_OK;
+}
+
+// The cache's pointers and sizes, as the kernels take them.
+static int cache_view(const fem_paged_cache *c, PagedCacheView *out) {
+  if (!c || !c->k || !c->v) return FEM_ERR_INVALID_ARG;
+  if (c->format != FEM_CACHE_BF16 && c->format != FEM_CACHE_E4M3 && c->format != FEM_CACHE_F32)
+    return FEM_ERR_INVALID_ARG;
+  if (c->num_pages <= 0 || c->H <= 0 || c->page_size <= 0 || c->d <= 0) return FEM_ERR_INVALID_ARG;
+  if (!aligned16(c->k) || !aligned16(c->v)) return FEM_ERR_INVALID_ARG;
+  if (c->format == FEM_CACHE_E4M3 ? (!c->k_exp || !c->v_exp) : (c->k_exp || c->v_exp)) return FEM_ERR_INVALID_ARG;
+  int shift = 4;
+  while (shift <= 8 && (1 << shift) != c->page_size) ++shift;
+  if (shift > 8 || c->d > 256 || c->d % 16 || c->H > 65535) return FEM_ERR_UNSUPPORTED;
+  *out = PagedCacheView{c->k, c->v, static_cast<uint8_t *>(c->k_exp), static_cast<uint8_t *>(c->v_exp), c->format,
+                        c->num_pages, c->H, shift, c->d};
+  return FEM_OK;
+}
+
+// Strides of [N, heads, d] inputs: rows of d elements on 16-byte boundaries.
+static bool strides_ok(int64_t sn, int64_t sh, int format) {
+  const int64_t per = format == FEM_CACHE_F32 ? 4 : 8;
+  return sn >= 0 && sh >= 0 && sn % per == 0 && sh % per == 0;
+}
+
+int fem_cache_write(const fem_paged_cache *cache, const void *k, const void *v, int64_t k_stride_n,
+                    int64_t k_stride_h, int64_t v_stride_n, int64_t v_stride_h, const int64_t *slots, int N,
+                    void *stream) {
+  PagedCacheView c;
+  int rc = cache_view(cache, &c);
+  if (rc != FEM_OK) return rc;
+  if (N < 0 || (N > 0 && (!k || !v || !slots))) return FEM_ERR_INVALID_ARG;
+  if (!aligned16(k) || !aligned16(v) || (reinterpret_cast<uintptr_t>(slots) & 7u)) return FEM_ERR_INVALID_ARG;
+  if (!strides_ok(k_stride_n, k_stride_h, c.format) || !strides_ok(v_stride_n, v_stride_h, c.format))
+    return FEM_ERR_INVALID_ARG;
+  if (N == 0) return FEM_OK;
+  DeviceState *ds = nullptr;
+  if ((rc = device_state(&ds)) != FEM_OK) return rc;
+  return map_cuda(launch_cache_write(c, k, v, k_stride_n, k_stride_h, v_stride_n, v_stride_h,
+                                     reinterpret_cast<const long long *>(slots), N, ds->err, ds->num_sms,
+                                     static_cast<cudaStream_t>(stream)));
+}
+
+int fem_cache_gather(const fem_paged_cache *cache, const int *block_table, int max_pages, const int *starts,
+                     const int *offsets, int S, void *k_out, void *v_out, int total, void *stream) {
+  PagedCacheView c;
+  int rc = cache_view(cache, &c);
+  if (rc != FEM_OK) return rc;
+  if (total < 0 || (total > 0 && (S <= 0 || max_pages <= 0 || !block_table || !starts || !offsets || !k_out || !v_out)))
+    return FEM_ERR_INVALID_ARG;
+  if (!aligned16(k_out) || !aligned16(v_out)) return FEM_ERR_INVALID_ARG;
+  if (total == 0) return FEM_OK;
+  DeviceState *ds = nullptr;
+  if ((rc = device_state(&ds)) != FEM_OK) return rc;
+  return map_cuda(launch_cache_gather(c, block_table, max_pages, starts, offsets, S, total, k_out, v_out, ds->err,
+                                      static_cast<cudaStream_t>(stream)));
+}
+
+int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride_n, int64_t q_stride_h,
+                   const float *beta, const int *q_offsets, const int *ctx_lens, const int *block_table,
+                   int max_pages, int S, int N, int Hq, int max_q, int causal, void *out, float *lse,
+                   void *stream) {
+  PagedReadArgs a;
+  int rc = cache_view(cache, &a.c);
+  if (rc != FEM_OK) return rc;
+  if (N < 0 || Hq <= 0 || max_q < 0 || (causal != 0 && causal != 1)) return FEM_ERR_INVALID_ARG;
+  if (N > 0 && (S <= 0 || max_pages <= 0 || !q || !q_offsets || !ctx_lens || !block_table || !out))
+    return FEM_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(out)) return FEM_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(beta) & 3u) || (reinterpret_cast<uintptr_t>(lse) & 3u)) return FEM_ERR_INVALID_ARG;
+  if (!strides_ok(q_stride_n, q_stride_h, a.c.format)) return FEM_ERR_INVALID_ARG;
+  if (Hq % a.c.H) return FEM_ERR_INVALID_ARG;
+  if (Hq > 65535 || static_cast<long long>(N) * Hq >= (1ll << 31)) return FEM_ERR_UNSUPPORTED;
+  if (N == 0) return FEM_OK;
+  DeviceState *ds = nullptr;
+  if ((rc = device_state(&ds)) != FEM_OK) return rc;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (beta && (rc = debug_check_beta(beta, static_cast<long long>(a.c.H) * a.c.d, ds, s)) != FEM_OK) return rc;
+  a.q = q;
+  a.q_sn = q_stride_n;
+  a.q_sh = q_stride_h;
+  a.beta = beta;
+  a.q_off = q_offsets;
+  a.ctx = ctx_lens;
+  a.table = block_table;
+  a.max_pages = max_pages;
+  a.S = S;
+  a.N = N;
+  a.Hq = Hq;
+  a.group = Hq / a.c.H;
+  a.causal = causal;
+  a.scale = 1.f / std::sqrt(static_cast<float>(a.c.d));
+  a.out = out;
+  a.lse = lse;
+  a.err = ds->err;
+  return map_cuda(launch_paged_exact(a, s));
 }
 
 int fem_last_fixup_rows(void *stream) {

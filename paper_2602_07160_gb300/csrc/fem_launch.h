@@ -154,4 +154,16 @@ cudaError_t launch_f32(const float *q, const float *k, const float *v, const flo
 cudaError_t launch_simt_bf16(const void *q, const void *k, const void *v, const float *beta, float *out, float *lse,
                              int B, int H, int T, int d, int causal, cudaStream_t stream);
 
+// Paged cache (fem_paged.cuh).  Write N tokens' rows at `slots` (page * page_size + row; negative: left
+// out); read S sequences' stretches back; the read over it, a block per row, exact to fp32 rounding.
+struct PagedCacheView;
+struct PagedReadArgs;
+cudaError_t launch_cache_write(const PagedCacheView &c, const void *k, const void *v, long long k_sn, long long k_sh,
+                               long long v_sn, long long v_sh, const long long *slots, int N, unsigned *err,
+                               int num_sms, cudaStream_t stream);
+cudaError_t launch_cache_gather(const PagedCacheView &c, const int *table, int max_pages, const int *starts,
+                                const int *offsets, int S, int total, void *k, void *v, unsigned *err,
+                                cudaStream_t stream);
+cudaError_t launch_paged_exact(const PagedReadArgs &a, cudaStream_t stream);
+
 }  // namespace fem

@@ -24,7 +24,8 @@ STATUS = {0: "FEM_OK", 1: "FEM_ERR_INVALID_ARG", 2: "FEM_ERR_UNSUPPORTED", 3: "F
 EXPORTS = ["fem_fwd", "fem_fwd_ws", "fem_fwd_workspace_bytes", "fem_fwd_f32", "fem_fwd_host",
            "fem_check_device_error", "fem_last_fixup_rows", "fem_set_kernel_events", "fem_status_str",
            "fem_fwd_noalloc", "fem_fwd_gated", "fem_decode", "fem_gla_fwd", "fem_tdc_conv", "fem_bwd_f32",
-           "fem_probe_wait_timeout", "fem_attn_fwd", "fem_gla_fwd_tc"]
+           "fem_probe_wait_timeout", "fem_attn_fwd", "fem_gla_fwd_tc", "fem_cache_write", "fem_cache_gather",
+           "fem_paged_read"]
 
 
 class FemError(RuntimeError):
@@ -67,6 +68,13 @@ def load(path: str | None = None):
         lib.fem_tdc_conv.restype = i
         lib.fem_bwd_f32.argtypes = [vp] * 11 + [i, i, i, i, i, vp]
         lib.fem_bwd_f32.restype = i
+        i64 = ctypes.c_int64
+        lib.fem_cache_write.argtypes = [vp, vp, vp, i64, i64, i64, i64, vp, i, vp]
+        lib.fem_cache_write.restype = i
+        lib.fem_cache_gather.argtypes = [vp, vp, i, vp, vp, i, vp, vp, i, vp]
+        lib.fem_cache_gather.restype = i
+        lib.fem_paged_read.argtypes = [vp, vp, i64, i64, vp, vp, vp, vp, i, i, i, i, i, i, vp, vp, vp]
+        lib.fem_paged_read.restype = i
         lib.fem_fwd_workspace_bytes.argtypes = [i, i, i, i, i]
         lib.fem_fwd_workspace_bytes.restype = sz
         lib.fem_check_device_error.argtypes = [vp]
@@ -314,6 +322,156 @@ def fem_fwd_noalloc(q, k, v, beta, causal: bool = True, out=None, lse=None, stre
                                 _stream(stream, q.device))
     if rc != 0:
         raise FemError("fem_fwd_noalloc", rc)
+    return out, (None if lse is False else lse)
+
+
+class _CacheStruct(ctypes.Structure):
+    """fem_paged_cache of include/fem.h."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("format", ctypes.c_int), ("num_pages", ctypes.c_int), ("H", ctypes.c_int), ("page_size", ctypes.c_int),
+                ("d", ctypes.c_int)]
+
+
+class PagedCache:
+    """A paged key/value cache: k, v [num_pages, H, page_size, d] on one CUDA device.
+
+    bf16 and float32 caches are the two tensors; float8_e4m3fn ones have the rows' scale
+    exponents k_exp, v_exp (uint8 [num_pages, H, page_size]) beside them.  The object keeps
+    the tensors, checks them once, and is what ``fem_cache_write``, ``fem_cache_gather`` and
+    ``fem_paged_read`` take."""
+
+    FORMATS = {torch.bfloat16: 0, torch.float8_e4m3fn: 1, torch.float32: 2}
+
+    def __init__(self, k, v, k_exp=None, v_exp=None):
+        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or v.device != k.device:
+            raise ValueError("k and v must share the shape [num_pages, H, page_size, d], type and device")
+        if k.dtype not in self.FORMATS:
+            raise ValueError(f"a cache of {k.dtype} is not supported")
+        pages, H, page_size, d = k.shape
+        scaled = k.dtype == torch.float8_e4m3fn
+        if scaled != (k_exp is not None) or scaled != (v_exp is not None):
+            raise ValueError("k_exp and v_exp go with float8_e4m3fn caches, and only with them")
+        for name, t in (("k", k), ("v", v)) + ((("k_exp", k_exp), ("v_exp", v_exp)) if scaled else ()):
+            if not t.is_contiguous() or t.device.type != "cuda" or t.device != k.device:
+                raise ValueError(f"{name} must be a contiguous CUDA tensor on k's device")
+            if name.endswith("exp") and (t.dtype != torch.uint8 or t.shape != (pages, H, page_size)):
+                raise ValueError(f"{name} must be uint8 [num_pages, H, page_size]")
+        if page_size not in (16, 32, 64, 128, 256) or d % 16 or not 16 <= d <= 256 or pages < 1 or H < 1:
+            raise ValueError("page_size must be 16, 32, 64, 128 or 256 and d a multiple of 16 up to 256")
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self.num_pages, self.H, self.page_size, self.d = pages, H, page_size, d
+        self.device = k.device
+        self.row_dtype = torch.float32 if k.dtype == torch.float32 else torch.bfloat16  # of k, v, q given to the calls
+        self._struct = _CacheStruct(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if scaled else None,
+                                    v_exp.data_ptr() if scaled else None, self.FORMATS[k.dtype], pages, H, page_size, d)
+        self._ref = ctypes.addressof(self._struct)
+
+    @classmethod
+    def empty(cls, num_pages: int, H: int, d: int, page_size: int = 64, dtype=torch.bfloat16, device="cuda"):
+        """A cache of zeros."""
+        shape = (num_pages, H, page_size, d)
+        k, v = (torch.zeros(shape, dtype=torch.uint8 if dtype == torch.float8_e4m3fn else dtype, device=device)
+                for _ in range(2))
+        if dtype != torch.float8_e4m3fn:
+            return cls(k, v)
+        exps = (torch.full(shape[:3], 127, dtype=torch.uint8, device=device) for _ in range(2))
+        return cls(k.view(dtype), v.view(dtype), *exps)
+
+
+def _check_rows(name, t, cache, heads):
+    """A [N, heads, d] input of the cache's row type, d contiguous."""
+    if t.dim() != 3 or t.shape[2] != cache.d or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} must be [N, heads, d] with the cache's d" + ("" if heads is None else " and H"))
+    if t.dtype != cache.row_dtype or t.device != cache.device:
+        raise ValueError(f"{name} must be {cache.row_dtype} on the cache's device")
+    if t.stride(2) != 1:
+        raise ValueError(f"{name}'s last axis must be contiguous")
+
+
+def _row_strides(t):
+    """Token and head strides of a [N, heads, d] tensor; an axis of length one has none."""
+    return (t.stride(0) if t.shape[0] > 1 else 0), (t.stride(1) if t.shape[1] > 1 else 0)
+
+
+def _check_ints(name, t, shape, dtype, device):
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on the cache's device")
+
+
+def fem_cache_write(cache: PagedCache, k, v, slots, stream=None):
+    """Put N tokens' keys and values [N, H, d] into the cache at slots (int64 [N]: page *
+    page_size + row; negative: left out).  k and v may be strided views; a float8_e4m3fn
+    cache quantises each (token, head) row as it is written."""
+    N = k.shape[0]
+    _check_rows("k", k, cache, cache.H)
+    _check_rows("v", v, cache, cache.H)
+    if v.shape[0] != N:
+        raise ValueError("k and v must have as many tokens")
+    _check_ints("slots", slots, (N,), torch.int64, cache.device)
+    rc = load().fem_cache_write(cache._ref, k.data_ptr(), v.data_ptr(), *_row_strides(k), *_row_strides(v),
+                                slots.data_ptr(), N, _stream(stream, cache.device))
+    if rc != 0:
+        raise FemError("fem_cache_write", rc)
+
+
+def fem_cache_gather(cache: PagedCache, block_table, starts, offsets, total: int, k_out=None, v_out=None, stream=None):
+    """Read stretches of cached sequences back as contiguous (k, v) [total, H, d].
+
+    block_table: int32 [S, max_pages]; starts: int32 [S], each stretch's first position;
+    offsets: int32 [S + 1], its rows of the output; total = offsets[S]."""
+    S, shape = block_table.shape[0], (total, cache.H, cache.d)
+    _check_ints("block_table", block_table, (S, block_table.shape[1]), torch.int32, cache.device)
+    _check_ints("starts", starts, (S,), torch.int32, cache.device)
+    _check_ints("offsets", offsets, (S + 1,), torch.int32, cache.device)
+    if k_out is None:
+        k_out = torch.empty(shape, dtype=cache.row_dtype, device=cache.device)
+    if v_out is None:
+        v_out = torch.empty(shape, dtype=cache.row_dtype, device=cache.device)
+    _check_ints("k_out", k_out, shape, cache.row_dtype, cache.device)
+    _check_ints("v_out", v_out, shape, cache.row_dtype, cache.device)
+    rc = load().fem_cache_gather(cache._ref, block_table.data_ptr(), block_table.shape[1], starts.data_ptr(),
+                                 offsets.data_ptr(), S, k_out.data_ptr(), v_out.data_ptr(), total,
+                                 _stream(stream, cache.device))
+    if rc != 0:
+        raise FemError("fem_cache_gather", rc)
+    return k_out, v_out
+
+
+def fem_paged_read(q, cache: PagedCache, beta, q_offsets, ctx_lens, block_table, max_q: int, causal: bool = True,
+                   out=None, lse=None, stream=None):
+    """The read of new tokens q [N, Hq, d] over a paged cache that holds their own keys and values.
+
+    Sequence s has the rows q_offsets[s] .. q_offsets[s+1] - 1 (int32 [S + 1]) and ctx_lens[s]
+    (int32 [S]) cached positions; block_table is int32 [S, max_pages]; beta is float32 [H, d] of
+    the cache's heads or None (the prior mean, plain softmax attention); max_q bounds the rows
+    of a sequence.  Returns (out [N, Hq, d] of q's type, lse [N, Hq] float32); ``lse=False``
+    skips the log-normaliser."""
+    _check_rows("q", q, cache, None)
+    N, Hq, d = q.shape
+    if Hq % cache.H:
+        raise ValueError("q's heads must be a multiple of the cache's")
+    if beta is not None:
+        _check_ints("beta", beta, (cache.H, d), torch.float32, cache.device)
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [S, max_pages]")
+    S, max_pages = block_table.shape
+    _check_ints("block_table", block_table, (S, max_pages), torch.int32, cache.device)
+    _check_ints("q_offsets", q_offsets, (S + 1,), torch.int32, cache.device)
+    _check_ints("ctx_lens", ctx_lens, (S,), torch.int32, cache.device)
+    if out is None:
+        out = torch.empty((N, Hq, d), dtype=q.dtype, device=cache.device)
+    else:
+        _check_ints("out", out, (N, Hq, d), q.dtype, cache.device)
+    if lse is None:
+        lse = torch.empty((N, Hq), dtype=torch.float32, device=cache.device)
+    elif lse is not False:
+        _check_ints("lse", lse, (N, Hq), torch.float32, cache.device)
+    rc = load().fem_paged_read(cache._ref, q.data_ptr(), *_row_strides(q),
+                               None if beta is None else beta.data_ptr(), q_offsets.data_ptr(), ctx_lens.data_ptr(),
+                               block_table.data_ptr(), max_pages, S, N, Hq, int(max_q), int(bool(causal)),
+                               out.data_ptr(), None if lse is False else lse.data_ptr(), _stream(stream, cache.device))
+    if rc != 0:
+        raise FemError("fem_paged_read", rc)
     return out, (None if lse is False else lse)
 
 
