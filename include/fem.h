@@ -273,7 +273,8 @@ int fem_bwd_f32(const float *q, const float *k, const float *v, const float *bet
  *
  * A cache is caller-owned device memory in pages of page_size positions:
  *   k, v         : [num_pages, H, page_size, d], contiguous, 16-byte aligned
- *   k_exp, v_exp : uint8 [num_pages, H, page_size] (FEM_CACHE_E4M3), else NULL
+ *   k_exp, v_exp : uint8 [num_pages, H, page_size], 16-byte aligned
+ *                  (FEM_CACHE_E4M3), else NULL
  *   page_size    : 16, 32, 64, 128 or 256
  *   d            : a multiple of 16 up to 256
  * Formats:

@@ -21,6 +21,7 @@
 #include "fem_chunks.h"
 #include "fem_launch.h"
 #include "fem_paged.cuh"
+#include "fem_paged_split.cuh"
 
 namespace fem {
 namespace {
@@ -763,7 +764,7 @@ static int cache_view(const fem_paged_cache *c, PagedCacheView *out) {
   if (c->format != FEM_CACHE_BF16 && c->format != FEM_CACHE_E4M3 && c->format != FEM_CACHE_F32)
     return FEM_ERR_INVALID_ARG;
   if (c->num_pages <= 0 || c->H <= 0 || c->page_size <= 0 || c->d <= 0) return FEM_ERR_INVALID_ARG;
-  if (!aligned16(c->k) || !aligned16(c->v)) return FEM_ERR_INVALID_ARG;
+  if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->k_exp) || !aligned16(c->v_exp)) return FEM_ERR_INVALID_ARG;
   if (c->format == FEM_CACHE_E4M3 ? (!c->k_exp || !c->v_exp) : (c->k_exp || c->v_exp)) return FEM_ERR_INVALID_ARG;
   int shift = 4;
   while (shift <= 8 && (1 << shift) != c->page_size) ++shift;
@@ -771,6 +772,23 @@ static int cache_view(const fem_paged_cache *c, PagedCacheView *out) {
   *out = PagedCacheView{c->k, c->v, static_cast<uint8_t *>(c->k_exp), static_cast<uint8_t *>(c->v_exp), c->format,
                         c->num_pages, c->H, shift, c->d};
   return FEM_OK;
+}
+
+// The cache's k or v as [num_pages H, page_size, d], in boxes of `rows` rows of up to 128 bytes with the
+// swizzle of that width.
+static int cache_map(CUtensorMap *map, const void *base, const PagedCacheView &c, int rows) {
+  const int elem = c.format == FEM_CACHE_BF16 ? 2 : 1, row_bytes = c.d * elem, page = 1 << c.page_shift;
+  const int box_bytes = row_bytes < 128 ? row_bytes : 128;
+  cuuint64_t dims[3] = {static_cast<cuuint64_t>(c.d), static_cast<cuuint64_t>(page),
+                        static_cast<cuuint64_t>(c.num_pages) * c.H};
+  cuuint64_t strides[2] = {static_cast<cuuint64_t>(row_bytes), static_cast<cuuint64_t>(row_bytes) * page};
+  cuuint32_t box[3] = {static_cast<cuuint32_t>(box_bytes / elem), static_cast<cuuint32_t>(rows), 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = g_encode(map, elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 3,
+                        const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        box_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? FEM_OK : FEM_ERR_CUDA;
 }
 
 // Strides of [N, heads, d] inputs: rows of d elements on 16-byte boundaries.
@@ -849,7 +867,23 @@ int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride
   a.out = out;
   a.lse = lse;
   a.err = ds->err;
-  return map_cuda(launch_paged_exact(a, s));
+  const bool split = (a.c.d == 64 || a.c.d == 128) && a.c.format != FEM_CACHE_F32 &&
+                     static_cast<long long>(a.c.num_pages) * a.c.H < (1ll << 31);
+  if (!split) return map_cuda(launch_paged_exact(a, s));
+  const int rows = static_cast<int>(std::min<long long>(static_cast<long long>(max_q) * a.group, 1 << 30));
+  const int grid = 2 * ds->num_sms;
+  const SplitShape shape = {rows <= 8 ? 8 : 16, 64, 2};
+  CUtensorMap tk, tv;
+  if ((rc = cache_map(&tk, a.c.k, a.c, 16)) != FEM_OK || (rc = cache_map(&tv, a.c.v, a.c, 16)) != FEM_OK) return rc;
+  const size_t piece_b = round256(2 * static_cast<size_t>(grid) * piece_floats(shape.row_tile, a.c.d) * sizeof(float));
+  uint8_t *ws = nullptr;
+  cudaError_t e = ws_alloc(ds, reinterpret_cast<void **>(&ws), piece_b + static_cast<size_t>(N) * Hq, s);
+  if (e != cudaSuccess) return map_cuda(e);
+  const PagedSplit sp = {reinterpret_cast<float *>(ws), ws + piece_b};
+  e = launch_paged_token(tk, tv, a, sp, shape, grid, s);
+  if (e == cudaSuccess) e = launch_paged_finish(a, sp, shape, grid, ds->num_sms, s);
+  const cudaError_t ef = cudaFreeAsync(ws, s);
+  return map_cuda(e != cudaSuccess ? e : ef);
 }
 
 int fem_last_fixup_rows(void *stream) {

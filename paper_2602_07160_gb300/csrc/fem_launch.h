@@ -158,6 +158,8 @@ cudaError_t launch_simt_bf16(const void *q, const void *k, const void *v, const 
 // out); read S sequences' stretches back; the read over it, a block per row, exact to fp32 rounding.
 struct PagedCacheView;
 struct PagedReadArgs;
+struct PagedSplit;
+struct SplitShape;
 cudaError_t launch_cache_write(const PagedCacheView &c, const void *k, const void *v, long long k_sn, long long k_sh,
                                long long v_sn, long long v_sh, const long long *slots, int N, unsigned *err,
                                int num_sms, cudaStream_t stream);
@@ -165,5 +167,12 @@ cudaError_t launch_cache_gather(const PagedCacheView &c, const int *table, int m
                                 const int *offsets, int S, int total, void *k, void *v, unsigned *err,
                                 cudaStream_t stream);
 cudaError_t launch_paged_exact(const PagedReadArgs &a, cudaStream_t stream);
+// The read of few rows per sequence on `grid` CTAs that split the work evenly (fem_paged_split.cuh), for d = 64
+// and 128; tk, tv map the cache's k and v as [num_pages H, page_size, d] in boxes of 16 rows.  launch_paged_finish
+// follows on the same stream and joins what the CTAs' ends cut (a programmatic dependent launch).
+cudaError_t launch_paged_token(const CUtensorMap &tk, const CUtensorMap &tv, const PagedReadArgs &a,
+                               const PagedSplit &sp, const SplitShape &shape, int grid, cudaStream_t stream);
+cudaError_t launch_paged_finish(const PagedReadArgs &a, const PagedSplit &sp, const SplitShape &shape, int grid,
+                                int num_sms, cudaStream_t stream);
 
 }  // namespace fem

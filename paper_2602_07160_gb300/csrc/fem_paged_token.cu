@@ -1,0 +1,614 @@
+// The paged read of few new tokens per sequence: decode steps and drafted tokens.
+//
+// Bound by memory: the cached keys and values are read once and each is used by
+// the few rows of its head's group.  A CTA of four warps takes a stretch of the
+// line of work (fem_paged_split.cuh) in tiles of 64 keys, 16 per warp; each warp
+// runs its own ring of TMA copies, with no barrier between warps inside an item.
+// The scores are K Q^T with the keys as the rows of the matrix instruction and
+// the (8 or 16) query rows as its columns, so that no row of the wide side is
+// wasted; the second product is E^T P^T with the channels as rows.  Both
+// operands come straight from shared memory in the lane layout the instruction
+// wants: the contraction index of the first (channels of q and k) and the row
+// and contraction indices of the second (channels; keys) are renumbered so that
+// a lane's share is 16 contiguous bytes of a key's row, and key_of and chunk_of
+// keep the eight lanes of each quarter warp on distinct banks of the swizzled
+// tile.  The value bank is formed in registers on the way, once per value for
+// all rows.  mma.sync suffices here: at 8 rows the products take a fraction of
+// the time the bytes do.
+#include "fem_launch.h"
+#include "fem_paged.cuh"
+#include "fem_paged_split.cuh"
+
+namespace fem {
+
+namespace {
+
+constexpr int kTokWarps = 4;
+constexpr int kTokThreads = 32 * kTokWarps;
+constexpr int kTokKeys = 16;                          // keys per warp and stage
+
+
+template <int FORMAT, int D, int NT>
+struct TokLayout {
+  static constexpr int kElem = FORMAT == kCacheBf16 ? 2 : 1;
+  static constexpr int kRow = D * kElem;                       // bytes of a cached row
+  static constexpr int kBox = kRow < 128 ? kRow : 128;         // bytes of a row in one TMA box
+  static constexpr int kBoxes = kRow / kBox;
+  static constexpr int kStage = 2 * kTokKeys * kRow;           // K and V of 16 keys
+  static constexpr int kStages = 24576 / kStage < 6 ? 24576 / kStage : 6;
+  static constexpr int kRows = 8 * NT;
+  static constexpr int kRedStride = D + 4;
+  // shared memory: rings, then scale bytes, barriers, coefficients, the join's rows
+  static constexpr int kScale = kTokWarps * kStages * kStage;
+  static constexpr int kBar = kScale + kTokWarps * kStages * 32;
+  static constexpr int kCoef4 = (kBar + kTokWarps * kStages * 8 + 15) & ~15;
+  static constexpr int kCoef2 = kCoef4 + D * 16;
+  static constexpr int kShift = kCoef2 + D * 8;
+  static constexpr int kRed = kShift + D * 4;
+  static constexpr int kStat = kRed + kRows * kRedStride * 4;  // [warps][rows] {m, L}
+  static constexpr int kWideFlag = kStat + kTokWarps * kRows * 8;
+  static constexpr int kRowBad = kWideFlag + 4;  // per row: some channel needs the exact path
+  static constexpr int kBytes = kRowBad + kRows * 4;
+  static constexpr int kAlloc = kBytes + 1024;
+};
+
+// Key (of 16) at row or contraction index x of the matrix instruction.
+template <bool ROW128>
+__device__ __forceinline__ int key_of(int x) {
+  return ROW128 ? (x & 8) + ((x & 7) >> 1) + 4 * (x & 1) : x;
+}
+
+__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
+  return v;
+}
+
+// Byte offset of 16-byte chunk `chunk` of row `row` in a stage's K or V tile.
+template <int BOX>
+__device__ __forceinline__ uint32_t tok_offset(int row, int chunk) {
+  if (BOX == 128) return (chunk >> 3) * (kTokKeys * 128) + sw128_offset(row, chunk & 7);
+  return row * 64 + ((chunk ^ ((row >> 1) & 3)) << 4);  // the 64-byte swizzle of 64-byte rows
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __int_as_float(static_cast<int>(w << 16)); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __int_as_float(static_cast<int>(w & 0xffff0000u)); }
+
+// Four e4m3 codes as two words of bf16 pairs, exactly.  The code's exponent and
+// fraction bits moved down four places read, as bf16, as the value times 2^-120.
+__device__ __forceinline__ uint2 e4m3x4_to_bf16(uint32_t x, uint32_t scale2) {
+  const uint32_t lo = __byte_perm(x, 0, 0x1404), hi = __byte_perm(x, 0, 0x3424);  // each code in the upper byte of a half
+  uint2 r;
+  r.x = (lo & 0x80008000u) | ((lo & 0x7f007f00u) >> 4);
+  r.y = (hi & 0x80008000u) | ((hi & 0x7f007f00u) >> 4);
+  const __nv_bfloat162 k = *reinterpret_cast<const __nv_bfloat162 *>(&scale2);
+  __nv_bfloat162 a = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&r.x), k);
+  __nv_bfloat162 b = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&r.y), k);
+  return make_uint2(*reinterpret_cast<uint32_t *>(&a), *reinterpret_cast<uint32_t *>(&b));
+}
+
+// A sequence's stretch of a CTA.
+struct TokSeg {
+  int s, h, row0, rows;  // sequence, head, first row and rows of the row tile (all rows of the sequence: total)
+  int total;
+  int kt0, kt1, kt_all;
+  SeqInfo si;
+};
+
+template <int FORMAT, int D, int NT, bool BETA>
+__global__ void __launch_bounds__(kTokThreads, 2)
+    paged_token_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                       const PagedReadArgs a, const PagedSplit sp, const SplitShape shape) {
+  using Lay = TokLayout<FORMAT, D, NT>;
+  constexpr bool R128 = Lay::kBox == 128;
+  constexpr int kRows = Lay::kRows, NS = Lay::kStages, MT = D / 16;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  __shared__ SplitScan<kTokThreads> scan;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+  const int g = lane >> 2, i4 = lane & 3;
+  const uint32_t sbase = smem_u32(smem);
+  const uint32_t ring = sbase + warp * NS * Lay::kStage;
+  const uint32_t scales = sbase + Lay::kScale + warp * NS * 32;
+  const uint32_t bars = sbase + Lay::kBar + warp * NS * 8;
+  float4 *coef4 = reinterpret_cast<float4 *>(smem + Lay::kCoef4);
+  float2 *coef2 = reinterpret_cast<float2 *>(smem + Lay::kCoef2);
+  float *s_shift = reinterpret_cast<float *>(smem + Lay::kShift);
+  float *s_red = reinterpret_cast<float *>(smem + Lay::kRed);
+  float2 *s_stat = reinterpret_cast<float2 *>(smem + Lay::kStat);
+  int *s_wide = reinterpret_cast<int *>(smem + Lay::kWideFlag);
+  int *s_bad = reinterpret_cast<int *>(smem + Lay::kRowBad);
+
+  grid_dep_launch_dependents();
+  if (lane == 0) {
+    for (int st = 0; st < NS; ++st) mbar_init(bars + 8 * st, 1);
+    fence_mbar_init();
+  }
+  const long long W = split_total(a, shape, scan);
+  if (W == 0) return;
+  const int G = split_ctas(W, gridDim.x, shape), cta = blockIdx.x;
+  if (cta >= G) return;
+  const long long x0 = split_start(W, G, cta), x1 = split_start(W, G, cta + 1);
+  int s;
+  long long prefix;
+  split_locate(a, shape, x0, scan, &s, &prefix);
+  long long local = x0 - prefix;
+  unsigned phases = 0;  // parity of each stage's barrier
+  bool alive = true;
+
+  for (long long x = x0; x < x1;) {
+    // ---- the next segment
+    TokSeg sg;
+    sg.si = paged_seq(a, s);
+    const int rt = seq_row_tiles(sg.si, a.group, shape);
+    sg.kt_all = seq_key_tiles(sg.si, shape);
+    const long long cost = static_cast<long long>(a.c.H) * rt * sg.kt_all;
+    if (local >= cost) {  // the next sequence (one without rows has no tiles)
+      local -= cost;
+      ++s;
+      continue;
+    }
+    const int item = static_cast<int>(local / sg.kt_all);
+    sg.s = s;
+    sg.h = item / rt;
+    sg.row0 = (item % rt) * kRows;
+    sg.total = sg.si.n * a.group;
+    sg.rows = min(kRows, sg.total - sg.row0);
+    sg.kt0 = static_cast<int>(local - static_cast<long long>(item) * sg.kt_all);
+    sg.kt1 = static_cast<int>(min(static_cast<long long>(sg.kt_all), sg.kt0 + (x1 - x)));
+    x += sg.kt1 - sg.kt0;
+    local += sg.kt1 - sg.kt0;
+
+    // ---- this warp's stages: key groups kt * 4 + warp, kt0 <= kt < kt1, that hold a key
+    const int n_st = [&] {
+      const int groups = (sg.si.ctx + kTokKeys - 1) / kTokKeys;  // of the sequence
+      const int last = min(sg.kt1, (groups - warp + kTokWarps - 1) / kTokWarps);
+      return max(last - sg.kt0, 0);
+    }();
+    int page_base = -1, page_reg = -1;  // lane l: the table's entry page_base + l
+    unsigned valid = 0;                 // stages whose page is there
+    auto issue = [&](int j) {
+      const int st = j % NS;
+      const int key0 = ((sg.kt0 + j) * kTokWarps + warp) * kTokKeys;
+      const int pi = key0 >> a.c.page_shift;
+      if (page_base < 0 || pi >= page_base + 32) {
+        page_base = pi;
+        const int mine = pi + lane;
+        page_reg = mine < a.max_pages ? __ldg(a.table + static_cast<long long>(sg.s) * a.max_pages + mine) : -1;
+      }
+      const int page = __shfl_sync(0xffffffffu, page_reg, pi - page_base);
+      if (static_cast<unsigned>(page) < static_cast<unsigned>(a.c.num_pages)) {
+        valid |= 1u << st;
+        if (lane == 0) {
+          const uint32_t dst = ring + st * Lay::kStage, bar = bars + 8 * st;
+          mbar_arrive_expect_tx(bar, Lay::kStage + (FORMAT == kCacheE4m3 ? 32 : 0));
+          const int y = key0 & ((1 << a.c.page_shift) - 1), z = page * a.c.H + sg.h;
+#pragma unroll
+          for (int b = 0; b < Lay::kBoxes; ++b) {
+            tma_load_3d(dst + b * kTokKeys * Lay::kBox, &tmap_k, bar, b * (Lay::kBox / Lay::kElem), y, z);
+            tma_load_3d(dst + Lay::kStage / 2 + b * kTokKeys * Lay::kBox, &tmap_v, bar, b * (Lay::kBox / Lay::kElem), y,
+                        z);
+          }
+          if (FORMAT == kCacheE4m3) {
+            const long long row = paged_row(a.c, page, sg.h, key0);
+            bulk_load(scales + st * 32, a.c.ke + row, 16, bar);
+            bulk_load(scales + st * 32 + 16, a.c.ve + row, 16, bar);
+          }
+        }
+      } else {
+        valid &= ~(1u << st);
+        if (lane == 0) atomicOr(a.err, kErrPageRange);
+      }
+    };
+    for (int j = 0; alive && j < min(n_st, NS); ++j) issue(j);
+
+    // ---- the bank's coefficients, from the sequence's first keys (thread per channel)
+    if (tid == 0) *s_wide = 0;
+    if (tid < kRows) s_bad[tid] = 0;
+    if (BETA) {
+      if (tid < D) {
+        float vmax = -INFINITY, vabs = 0.f;
+        const int page = sg.si.ctx > 0 ? paged_page(a, sg.s, 0) : -1;
+        if (page >= 0) {
+          const long long row = paged_row(a.c, page, sg.h, 0);
+          const int cnt = min(kSampleKeys, sg.si.ctx);
+          float v[kSampleKeys];
+#pragma unroll
+          for (int kk = 0; kk < kSampleKeys; ++kk) {
+            const long long r = row + min(kk, cnt - 1);
+            if (FORMAT == kCacheBf16) v[kk] = __bfloat162float(static_cast<const __nv_bfloat16 *>(a.c.v)[r * D + tid]);
+            else v[kk] = e4m3x2_to_float2(static_cast<const uint8_t *>(a.c.v)[r * D + tid]).x * paged_scale(a.c.ve[r]);
+          }
+#pragma unroll
+          for (int kk = 0; kk < kSampleKeys; ++kk) {
+            vmax = fmaxf(vmax, v[kk]);
+            vabs = fmaxf(vabs, fabsf(v[kk]));
+          }
+        }
+        const BankCoef c = bank_coef(a.beta[static_cast<long long>(sg.h) * D + tid], vmax, vabs);
+        // element e of a lane's piece of 8 channels, lanes side by side
+        const int at = Lay::kElem == 2 || !R128 ? (tid & ~63) + (tid & 7) * 8 + ((tid >> 3) & 7)
+                                                : (tid & 15) * 8 + (tid >> 4);
+        coef4[at] = make_float4(c.b, c.s, c.ia, c.ic);
+        coef2[at] = make_float2(c.hb, c.theta);
+        s_shift[tid] = c.theta == 0.f ? c.s : __int_as_float(0x7fffffff);
+      }
+    } else if (tid < D) {
+      s_shift[tid] = __int_as_float(0x7fffffff);
+    }
+
+    // ---- Q^T as the second operand: column g of row tile t, the lane's channels in the order K's 16-byte pieces bring them
+    uint32_t qf[NT][MT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int r = sg.row0 + 8 * t + g;
+      const bool on = r < sg.total;
+      const int tok = on ? r / a.group : 0, hq = sg.h * a.group + (on ? r % a.group : 0);
+      const __nv_bfloat16 *qp = static_cast<const __nv_bfloat16 *>(a.q) +
+                                (static_cast<long long>(sg.si.q0) + tok) * a.q_sn + hq * a.q_sh;
+#pragma unroll
+      for (int kk = 0; kk < MT; ++kk) {
+        // bf16: piece kk/2 of 8 channels at 32 (kk/2) + 8 i, half kk%2; e4m3: piece kk/4 of 16 at 64 (kk/4) + 16 i, quarter kk%4
+        const int at = FORMAT == kCacheBf16 ? 32 * (kk >> 1) + 8 * i4 + 4 * (kk & 1) : 64 * (kk >> 2) + 16 * i4 + 4 * (kk & 3);
+        const uint2 w = on ? *reinterpret_cast<const uint2 *>(qp + at) : make_uint2(0, 0);
+        qf[t][kk][0] = w.x;
+        qf[t][kk][1] = w.y;
+      }
+    }
+    // keys seen by the lane's columns (rows 2 i, 2 i + 1 of each row tile)
+    int lim[NT][2], lim_min = 0x7fffffff;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int r = sg.row0 + 8 * t + 2 * i4 + u;
+        lim[t][u] = r < sg.total ? min(paged_limit(sg.si, r / a.group, a.causal), sg.si.ctx) : 0;
+        if (r < sg.total) lim_min = min(lim_min, lim[t][u]);
+      }
+    lim_min = __reduce_min_sync(0xffffffffu, lim_min);
+    float m[NT][2], L[NT][2], acc[NT][MT][4], emax = 0.f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      m[t][0] = m[t][1] = -INFINITY;
+      L[t][0] = L[t][1] = 0.f;
+#pragma unroll
+      for (int u = 0; u < MT; ++u) acc[t][u][0] = acc[t][u][1] = acc[t][u][2] = acc[t][u][3] = 0.f;
+    }
+    const float qk_scale = a.scale * kLog2e;
+    __syncthreads();  // coefficients
+
+    for (int j = 0; j < n_st; ++j) {
+      const int st = j % NS, key0 = ((sg.kt0 + j) * kTokWarps + warp) * kTokKeys;
+      if ((valid >> st) & 1u) {
+        // after a wait that gave up nothing is issued, and what is in flight is still waited for, with the limit
+        if (!__all_sync(0xffffffffu, mbar_wait(bars + 8 * st, (phases >> st) & 1u, a.err, kErrWaitTma))) alive = false;
+        phases ^= 1u << st;
+        if (alive) {
+          const uint32_t kt = ring + st * Lay::kStage, vt = kt + Lay::kStage / 2;
+          // ---- S^T = K Q^T
+          float sc[NT][4];
+#pragma unroll
+          for (int t = 0; t < NT; ++t) sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
+          const int r0 = key_of<R128>(g), r1 = key_of<R128>(g + 8);
+          uint32_t ksc0 = 0, ksc1 = 0;
+          if (FORMAT == kCacheBf16) {
+#pragma unroll
+            for (int p = 0; p < MT / 2; ++p) {
+              const uint4 x = lds128(kt + tok_offset<Lay::kBox>(r0, 4 * p + i4));
+              const uint4 y = lds128(kt + tok_offset<Lay::kBox>(r1, 4 * p + i4));
+#pragma unroll
+              for (int t = 0; t < NT; ++t) {
+                mma_bf16(sc[t], x.x, y.x, x.y, y.y, qf[t][2 * p][0], qf[t][2 * p][1]);
+                mma_bf16(sc[t], x.z, y.z, x.w, y.w, qf[t][2 * p + 1][0], qf[t][2 * p + 1][1]);
+              }
+            }
+          } else {
+            // codes go in as their values (times 2^0); the keys' scales multiply the scores
+            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(ksc0) : "r"(scales + st * 32 + r0));
+            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(ksc1) : "r"(scales + st * 32 + r1));
+#pragma unroll
+            for (int p = 0; p < MT / 4; ++p) {
+              const uint4 x = lds128(kt + tok_offset<Lay::kBox>(r0, 4 * p + i4));
+              const uint4 y = lds128(kt + tok_offset<Lay::kBox>(r1, 4 * p + i4));
+              const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+              for (int u = 0; u < 4; ++u) {
+                const uint2 xa = e4m3x4_to_bf16(xs[u], 0x7b807b80u), ya = e4m3x4_to_bf16(ys[u], 0x7b807b80u);  // 2^120
+#pragma unroll
+                for (int t = 0; t < NT; ++t) mma_bf16(sc[t], xa.x, ya.x, xa.y, ya.y, qf[t][4 * p + u][0], qf[t][4 * p + u][1]);
+              }
+            }
+          }
+          const float f0 = FORMAT == kCacheE4m3 ? qk_scale * paged_scale(ksc0) : qk_scale;
+          const float f1 = FORMAT == kCacheE4m3 ? qk_scale * paged_scale(ksc1) : qk_scale;
+          const bool tail = key0 + kTokKeys > lim_min;
+          bool raise = false;
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            sc[t][0] *= f0;
+            sc[t][1] *= f0;
+            sc[t][2] *= f1;
+            sc[t][3] *= f1;
+            if (tail) {
+              if (key0 + r0 >= lim[t][0]) sc[t][0] = -INFINITY;
+              if (key0 + r0 >= lim[t][1]) sc[t][1] = -INFINITY;
+              if (key0 + r1 >= lim[t][0]) sc[t][2] = -INFINITY;
+              if (key0 + r1 >= lim[t][1]) sc[t][3] = -INFINITY;
+            }
+            raise = raise || fmaxf(sc[t][0], sc[t][2]) > m[t][0] + kRowMaxLag || fmaxf(sc[t][1], sc[t][3]) > m[t][1] + kRowMaxLag;
+          }
+          if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                float mx = fmaxf(sc[t][u], sc[t][u + 2]);
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+                if (mx > m[t][u] + kRowMaxLag) {
+                  const float alpha = ex2_approx(m[t][u] - mx);  // 0 the first time
+                  m[t][u] = mx;
+                  L[t][u] *= alpha;
+#pragma unroll
+                  for (int c = 0; c < MT; ++c) {
+                    acc[t][c][u] *= alpha;
+                    acc[t][c][u + 2] *= alpha;
+                  }
+                }
+              }
+          }
+          // ---- P^T as the second operand of the second product
+          uint32_t pf[NT][2];
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const float m0 = m[t][0] == -INFINITY ? 0.f : m[t][0], m1 = m[t][1] == -INFINITY ? 0.f : m[t][1];
+            const float p0 = ex2_approx(sc[t][0] - m0), p1 = ex2_approx(sc[t][1] - m1);
+            const float p2 = ex2_approx(sc[t][2] - m0), p3 = ex2_approx(sc[t][3] - m1);
+            L[t][0] += p0 + p2;
+            L[t][1] += p1 + p3;
+            pf[t][0] = transpose8x8(pack_bf16(p0, p1));
+            pf[t][1] = transpose8x8(pack_bf16(p2, p3));
+          }
+          // ---- O^T += E^T P^T: the lane's keys are contraction indices 2 i, 2 i + 1, 2 i + 8, 2 i + 9
+          int vr[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) vr[u] = key_of<R128>(2 * i4 + (u & 1) + 8 * (u >> 1));
+          unsigned dead = 0;  // keys past the sequence: whatever their rows hold, no weight
+          if (tail) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) dead |= key0 + vr[u] >= sg.si.ctx ? 1u << u : 0u;
+          }
+          float vscale[4];
+          if (FORMAT == kCacheE4m3) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              uint32_t b;
+              asm volatile("ld.shared.u8 %0, [%1];" : "=r"(b) : "r"(scales + st * 32 + 16 + vr[u]));
+              vscale[u] = paged_scale(b);
+            }
+          }
+          constexpr int kPieces = FORMAT == kCacheBf16 ? Lay::kBoxes : 1;  // of a lane, per key
+          constexpr int kPer = MT * 2 / kPieces;                           // channels of a piece (8 or 16)
+#pragma unroll
+          for (int pc = 0; pc < kPieces; ++pc) {
+            uint32_t w[4][4];
+            if (R128) {
+              const int chunk = 8 * pc + (g >> 1) + 4 * (g & 1);
+#pragma unroll
+              for (int u = 0; u < 4; ++u) {
+                const uint4 x = lds128(vt + tok_offset<Lay::kBox>(vr[u], chunk));
+                w[u][0] = x.x;
+                w[u][1] = x.y;
+                w[u][2] = x.z;
+                w[u][3] = x.w;
+              }
+            } else {
+#pragma unroll
+              for (int u = 0; u < 4; ++u) {
+                const uint2 x = lds64(vt + tok_offset<Lay::kBox>(vr[u], g >> 1) + 8 * (g & 1));
+                w[u][0] = x.x;
+                w[u][1] = x.y;
+              }
+            }
+            const int lane_g = R128 ? (g >> 1) + 4 * (g & 1) : g;  // the piece's place among the coefficients
+#pragma unroll
+            for (int q = 0; q < kPer / 2; ++q) {  // pairs of channels: one row block of the product each
+              uint32_t a0, a1, a2, a3;
+              float lo[4], hi[4];
+              if (FORMAT == kCacheBf16) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                  lo[u] = bf16_lo(w[u][q]);
+                  hi[u] = bf16_hi(w[u][q]);
+                }
+              } else {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                  const float2 f = e4m3x2_to_float2((w[u][q >> 1] >> (16 * (q & 1))) & 0xffffu);
+                  lo[u] = f.x * vscale[u];
+                  hi[u] = f.y * vscale[u];
+                }
+              }
+              if (BETA) {
+                const int at = pc * 64 + 2 * q * 8 + lane_g;
+                const float4 ca = coef4[at], cb = coef4[at + 8];
+                const float2 da = coef2[at], db = coef2[at + 8];
+                const BankCoef A = {ca.x, ca.y, ca.z, ca.w, da.x, da.y}, B = {cb.x, cb.y, cb.z, cb.w, db.x, db.y};
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                  lo[u] = bank_value(A, lo[u]);
+                  hi[u] = bank_value(B, hi[u]);
+                }
+                if (dead) {
+#pragma unroll
+                  for (int u = 0; u < 4; ++u)
+                    if ((dead >> u) & 1u) lo[u] = hi[u] = 0.f;
+                }
+                emax = fmax3(emax, fmax3(lo[0], lo[1], lo[2]), lo[3]);
+                emax = fmax3(emax, fmax3(hi[0], hi[1], hi[2]), hi[3]);
+              } else if (dead) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                  if ((dead >> u) & 1u) lo[u] = hi[u] = 0.f;
+              }
+              a0 = pack_bf16(lo[0], lo[1]);
+              a1 = pack_bf16(hi[0], hi[1]);
+              a2 = pack_bf16(lo[2], lo[3]);
+              a3 = pack_bf16(hi[2], hi[3]);
+#pragma unroll
+              for (int t = 0; t < NT; ++t) mma_bf16(acc[t][pc * (kPer / 2) + q], a0, a1, a2, a3, pf[t][0], pf[t][1]);
+            }
+          }
+        }
+        __syncwarp();
+      }
+      if (alive && j + NS < n_st) issue(j + NS);
+      else if (!alive) valid &= ~(1u << st);
+    }
+
+    // ---- join the warps: rows' sums over the lanes that share them, then one warp after the other
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) L[t][u] += __shfl_xor_sync(0xffffffffu, L[t][u], o);
+        if (g == 0) s_stat[warp * kRows + 8 * t + 2 * i4 + u] = make_float2(m[t][u], L[t][u]);
+      }
+    if (BETA && __any_sync(0xffffffffu, emax > kWideE) && lane == 0) *s_wide = 1;
+    __syncthreads();
+    float wgt[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float M = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < kTokWarps; ++q) M = fmaxf(M, s_stat[q * kRows + 8 * t + 2 * i4 + u].x);
+        wgt[t][u] = m[t][u] == -INFINITY ? 0.f : ex2_approx(m[t][u] - M);
+      }
+#pragma unroll 1
+    for (int q = 0; q < kTokWarps; ++q) {
+      if (warp == q) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int c = 0; c < MT; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              // channel of the product's row g (e < 2) or g + 8 (e >= 2)
+              const int ch = FORMAT == kCacheBf16
+                                 ? 64 * (c >> 2) + 8 * ((g >> 1) + 4 * (g & 1)) + 2 * (c & 3) + (e >> 1)
+                                 : R128 ? 16 * ((g >> 1) + 4 * (g & 1)) + 2 * c + (e >> 1) : 8 * g + 2 * c + (e >> 1);
+              float *p = s_red + (8 * t + 2 * i4 + (e & 1)) * Lay::kRedStride + ch;
+              const float v = acc[t][c][e] * wgt[t][e & 1];
+              *p = q == 0 ? v : *p + v;
+            }
+      }
+      __syncthreads();
+    }
+    // ---- the segment's rows: their output, or a piece of it
+    const bool whole = sg.kt0 == 0 && sg.kt1 == sg.kt_all;
+    const int slot = cta * 2 + (sg.kt0 == 0 ? 1 : 0);
+    float *piece = sp.pieces + static_cast<size_t>(slot) * piece_floats(kRows, D);
+    const bool wide = *s_wide != 0;
+    for (int r = 0; r < sg.rows; ++r) {
+      float M = -INFINITY, Lr = 0.f;
+#pragma unroll
+      for (int q = 0; q < kTokWarps; ++q) M = fmaxf(M, s_stat[q * kRows + r].x);
+#pragma unroll
+      for (int q = 0; q < kTokWarps; ++q) {
+        const float2 st = s_stat[q * kRows + r];
+        if (st.x != -INFINITY) Lr += st.y * ex2_approx(st.x - M);
+        else if (st.y != st.y) Lr = st.y;  // a row of NaN scores has no maximum
+      }
+      const int rr = sg.row0 + r, tok = rr / a.group, hq = sg.h * a.group + rr % a.group;
+      const long long orow = (static_cast<long long>(sg.si.q0) + tok) * a.Hq + hq;
+      if (whole) {
+        if (tid < D) {
+          bool ok = true;
+          float o = 0.f;
+          if (!(M == -INFINITY && Lr == 0.f)) {
+            const float av = s_red[r * Lay::kRedStride + tid] / Lr;
+            o = BETA ? paged_out(a.beta[static_cast<long long>(sg.h) * D + tid], s_shift[tid], av, wide, &ok)
+                     : paged_out(0.f, s_shift[tid], av, false, &ok);
+          }
+          if (!ok) s_bad[r] = 1;
+          static_cast<__nv_bfloat16 *>(a.out)[orow * D + tid] = __float2bfloat16_rn(o);
+        }
+        if (tid == 0 && a.lse != nullptr)
+          a.lse[orow] = M == -INFINITY && Lr == 0.f ? -INFINITY : (M + log2f(Lr)) * kLn2;
+      } else {
+        if (tid < D) piece[static_cast<size_t>(r) * D + tid] = s_red[r * Lay::kRedStride + tid];
+        if (tid == 0) {
+          piece[kRows * D + 2 * r] = M;
+          piece[kRows * D + 2 * r + 1] = Lr;
+        }
+      }
+    }
+    if (!whole) {
+      if (tid < D) piece[kRows * D + 2 * kRows + tid] = s_shift[tid];
+      if (tid == 0) piece[kRows * D + 2 * kRows + D] = wide ? 1.f : 0.f;
+    }
+    __syncthreads();
+    if (tid < sg.rows) {
+      const int rr = sg.row0 + tid, tok = rr / a.group, hq = sg.h * a.group + rr % a.group;
+      sp.todo[(static_cast<long long>(sg.si.q0) + tok) * a.Hq + hq] =
+          whole ? (s_bad[tid] ? kRowExact : kRowDone) : kRowSplit;
+    }
+  }
+}
+
+}  // namespace
+
+template <int FORMAT, int D, int NT>
+static cudaError_t launch_token_n(const CUtensorMap &tk, const CUtensorMap &tv, const PagedReadArgs &a,
+                                  const PagedSplit &sp, const SplitShape &shape, int grid, cudaStream_t stream) {
+  const size_t smem = TokLayout<FORMAT, D, NT>::kAlloc;
+  auto go = [&](auto kernel) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e != cudaSuccess) return e;
+    kernel<<<grid, kTokThreads, smem, stream>>>(tk, tv, a, sp, shape);
+    return cudaGetLastError();
+  };
+  return a.beta ? go(paged_token_kernel<FORMAT, D, NT, true>) : go(paged_token_kernel<FORMAT, D, NT, false>);
+}
+
+cudaError_t launch_paged_token(const CUtensorMap &tk, const CUtensorMap &tv, const PagedReadArgs &a,
+                               const PagedSplit &sp, const SplitShape &shape, int grid, cudaStream_t stream) {
+#define FEM_TOK(F, DD)                                                                            \
+  if (a.c.format == F && a.c.d == DD)                                                             \
+    return shape.row_tile == 8 ? launch_token_n<F, DD, 1>(tk, tv, a, sp, shape, grid, stream)     \
+                               : launch_token_n<F, DD, 2>(tk, tv, a, sp, shape, grid, stream);
+  FEM_TOK(kCacheBf16, 64)
+  FEM_TOK(kCacheBf16, 128)
+  FEM_TOK(kCacheE4m3, 64)
+  FEM_TOK(kCacheE4m3, 128)
+#undef FEM_TOK
+  return cudaErrorInvalidValue;
+}
+
+}  // namespace fem
