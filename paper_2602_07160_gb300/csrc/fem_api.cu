@@ -830,6 +830,9 @@ int fem_cache_gather(const fem_paged_cache *cache, const int *block_table, int m
                                       static_cast<cudaStream_t>(stream)));
 }
 
+// Query rows per key/value head up to which the paged read takes the kernel of few rows.
+static constexpr int kTokenRows = 16;
+
 int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride_n, int64_t q_stride_h,
                    const float *beta, const int *q_offsets, const int *ctx_lens, const int *block_table,
                    int max_pages, int S, int N, int Hq, int max_q, int causal, void *out, float *lse,
@@ -871,16 +874,21 @@ int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride
                      static_cast<long long>(a.c.num_pages) * a.c.H < (1ll << 31);
   if (!split) return map_cuda(launch_paged_exact(a, s));
   const int rows = static_cast<int>(std::min<long long>(static_cast<long long>(max_q) * a.group, 1 << 30));
-  const int grid = 2 * ds->num_sms;
-  const SplitShape shape = {rows <= 8 ? 8 : 16, 64, 2};
+  // few rows per head: the kernel that is bound by memory; more: the tensor cores
+  const bool chunk = rows > kTokenRows && a.group <= 256;
+  const int grid = chunk ? ds->num_sms : 2 * ds->num_sms;
+  const SplitShape shape = chunk ? SplitShape{256, 128, 256 / a.group, 1} : SplitShape{rows <= 8 ? 8 : 16, 64, 0, 2};
+  const int box_rows = chunk ? std::min(1 << a.c.page_shift, 128) : 16;
   CUtensorMap tk, tv;
-  if ((rc = cache_map(&tk, a.c.k, a.c, 16)) != FEM_OK || (rc = cache_map(&tv, a.c.v, a.c, 16)) != FEM_OK) return rc;
+  if ((rc = cache_map(&tk, a.c.k, a.c, box_rows)) != FEM_OK || (rc = cache_map(&tv, a.c.v, a.c, box_rows)) != FEM_OK)
+    return rc;
   const size_t piece_b = round256(2 * static_cast<size_t>(grid) * piece_floats(shape.row_tile, a.c.d) * sizeof(float));
   uint8_t *ws = nullptr;
   cudaError_t e = ws_alloc(ds, reinterpret_cast<void **>(&ws), piece_b + static_cast<size_t>(N) * Hq, s);
   if (e != cudaSuccess) return map_cuda(e);
   const PagedSplit sp = {reinterpret_cast<float *>(ws), ws + piece_b};
-  e = launch_paged_token(tk, tv, a, sp, shape, grid, s);
+  e = chunk ? launch_paged_chunk(tk, tv, a, sp, shape, grid, box_rows, s)
+            : launch_paged_token(tk, tv, a, sp, shape, grid, s);
   if (e == cudaSuccess) e = launch_paged_finish(a, sp, shape, grid, ds->num_sms, s);
   const cudaError_t ef = cudaFreeAsync(ws, s);
   return map_cuda(e != cudaSuccess ? e : ef);

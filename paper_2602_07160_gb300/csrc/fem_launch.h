@@ -172,6 +172,10 @@ cudaError_t launch_paged_exact(const PagedReadArgs &a, cudaStream_t stream);
 // follows on the same stream and joins what the CTAs' ends cut (a programmatic dependent launch).
 cudaError_t launch_paged_token(const CUtensorMap &tk, const CUtensorMap &tv, const PagedReadArgs &a,
                                const PagedSplit &sp, const SplitShape &shape, int grid, cudaStream_t stream);
+// The same for many rows per sequence, on the tensor cores (tcgen05); tk, tv in boxes of box_rows rows.
+cudaError_t launch_paged_chunk(const CUtensorMap &tk, const CUtensorMap &tv, const PagedReadArgs &a,
+                               const PagedSplit &sp, const SplitShape &shape, int grid, int box_rows,
+                               cudaStream_t stream);
 cudaError_t launch_paged_finish(const PagedReadArgs &a, const PagedSplit &sp, const SplitShape &shape, int grid,
                                 int num_sms, cudaStream_t stream);
 

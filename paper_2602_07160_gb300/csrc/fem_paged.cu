@@ -77,8 +77,11 @@ __global__ void __launch_bounds__(kExactThreads)
     bool exact = sp.todo[orow] == kRowExact;
     if (!exact) {
       if (W < 0) W = split_total(a, shape, scan);
-      const int G = split_ctas(W, grid, shape), h = hq / a.group, r = t * a.group + hq % a.group;
-      const int rt = seq_row_tiles(si, a.group, shape), kt = seq_key_tiles(si, shape);
+      // the row's place: packed rows, or row tiles of whole tokens
+      const int G = split_ctas(W, grid, shape), h = hq / a.group, gr = hq % a.group;
+      const int tile = shape.tok ? t / shape.tok : (t * a.group + gr) / shape.row_tile;
+      const int rr = shape.tok ? (t - tile * shape.tok) * a.group + gr : (t * a.group + gr) % shape.row_tile;
+      const int kt = row_key_tiles(si, tile, a.causal, shape);
       if (s_of != lo) {
         // tiles before sequence lo
         long long w = 0;
@@ -93,10 +96,10 @@ __global__ void __launch_bounds__(kExactThreads)
         for (int i = 0; i < kExactThreads / 32; ++i) prefix += scan.warp[i];
         s_of = lo;
       }
-      const long long x = prefix + (static_cast<long long>(h) * rt + r / shape.row_tile) * kt;
+      const long long x = prefix + h * head_key_tiles(si, seq_row_tiles(si, a.group, shape), a.group, a.causal, shape) +
+                          head_key_tiles(si, tile, a.group, a.causal, shape);
       const int g0 = split_owner(W, G, x), g1 = split_owner(W, G, x + kt - 1), n = g1 - g0 + 1;
       const size_t size = piece_floats(shape.row_tile, d);
-      const int rr = r % shape.row_tile;
       const float *p0 = sp.pieces + (static_cast<size_t>(g0) * 2 + 1) * size;  // then every other slot 0
       auto piece = [&](int i) { return i == 0 ? p0 : sp.pieces + static_cast<size_t>(g0 + i) * 2 * size; };
       const float *stat = nullptr;

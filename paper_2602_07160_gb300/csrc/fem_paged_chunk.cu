@@ -1,0 +1,667 @@
+// The paged read of many new tokens per sequence: chunks of prompts and whole prompts.
+//
+// Bound by the tensor cores and by the exponentials that feed them.  A CTA takes
+// a stretch of the line of work (fem_paged_split.cuh) in tiles of up to 256 query
+// rows (whole tokens, the head's group interleaved) by 128 keys.  The 256 rows
+// are two tiles of 128 that share every key tile, so the value bank is formed
+// once for both and each tile's softmax runs under the other's products:
+//
+//   warps 0-3    bank: the key tile's values (TMA, 128-byte swizzle) become E(v) in
+//                place; e4m3 keys and values are widened to bf16 from a staging
+//                tile.  Rows past the sequence, or of pages that are not there,
+//                become zeros
+//   warps 4-7    softmax of row tile 0 (thread = row): S from TMEM, P = 2^(s - m)
+//                as bf16 over the first 64 columns of S, the row sum, the lazily
+//                raised maximum (and, when it moves, the accumulator's rescale);
+//                the rows' queries into shared memory at an item's start, their
+//                output or piece at its end
+//   warps 8-11   the same for row tile 1
+//   warp 12      TMA of K and V, one box per page (or part of a page) of the tile
+//   warp 13      issues the products, one thread: S0 = Q0 K^T, S1 = Q1 K^T, then for
+//                each tile, once its P is written, O += P E and the next S.  The
+//                tensor pipe takes them in the order issued, so S of the next key
+//                tile may overwrite a P whose product was issued before it, and
+//                the commit of S also says that the product before it is done: the
+//                softmax may then rescale O
+//
+// TMEM: S0 [0,128), S1 [128,256), O0 [256, 256 + D), O1 after it.
+// Shared memory: Q (two tiles), K and E (two stages each), and for e4m3 a staging
+// tile for K and one for V; [128 x D] tiles of bf16 in 64-column blocks of 128
+// rows x 128 bytes, chunk c of row r at chunk c ^ (r & 7).
+#include "fem_launch.h"
+#include "fem_paged.cuh"
+#include "fem_paged_split.cuh"
+
+namespace fem {
+
+namespace {
+
+constexpr int kChunkThreads = 512;
+constexpr int kChunkKeys = 128;
+constexpr int kInvRing = 8;   // key tiles whose missing pages are remembered
+constexpr int kSegRing = 4;   // segments whose channel shifts are remembered: at most three are alive
+
+template <int FORMAT, int D>
+struct ChunkLayout {
+  static constexpr uint32_t kTile = 128 * D * 2;
+  static constexpr uint32_t kRaw = FORMAT == kCacheE4m3 ? 128 * D : 0;  // a staging tile of codes
+  static constexpr uint32_t kQ = 0;
+  static constexpr uint32_t kK = 2 * kTile;
+  static constexpr uint32_t kE = kK + 2 * kTile;
+  static constexpr uint32_t kRawK = kE + 2 * kTile;
+  static constexpr uint32_t kRawV = kRawK + kRaw;
+  static constexpr uint32_t kCtl = kRawV + kRaw;
+  static constexpr uint32_t kShift = kCtl;                                // [kSegRing][D]
+  static constexpr uint32_t kInv = kShift + kSegRing * D * 4;             // [kInvRing]
+  static constexpr uint32_t kWide = kInv + kInvRing * 4;                  // [kSegRing]: number (from 1) of the segment whose |E| went wide
+  static constexpr uint32_t kScaleK = kWide + kSegRing * 4;  // e4m3: scale bytes of the staged keys, then values
+  static constexpr uint32_t kScaleV = kScaleK + 128;
+  static constexpr uint32_t kBars = kScaleV + 128;
+  static constexpr uint32_t kNumBars = 24;
+  static constexpr uint32_t kTmem = kBars + kNumBars * 8;
+  static constexpr uint32_t kAbort = kTmem + 4;
+  static constexpr uint32_t kScan = kAbort + 4;
+  static constexpr uint32_t kBytes = kScan + sizeof(SplitScan<kChunkThreads>);
+  static_assert(kBytes <= 227 * 1024, "shared memory");
+};
+
+enum : int {
+  kCbQ = 0,        // + row tile: its queries are in shared memory (128 arrivals)
+  kCbKFull = 2,    // + stage: K as bf16 (TMA, or 128 arrivals of the bank warps)
+  kCbKEmpty = 4,   // + stage: both S of the tile are done
+  kCbVFull = 6,    // + stage: V as TMA brought it (bf16)
+  kCbEFull = 8,    // + stage: the bank (128 arrivals)
+  kCbEEmpty = 10,  // + stage: both P E of the tile are done
+  kCbRawKFull = 12,
+  kCbRawVFull = 13,
+  kCbRawKEmpty = 14,  // 128 arrivals
+  kCbRawVEmpty = 15,
+  kCbS = 16,       // + row tile: S is in TMEM
+  kCbP = 18,       // + row tile: P is in TMEM (128 arrivals)
+  kCbO = 20,       // every product of the segment is done
+  kCbDone = 21,    // every product this CTA issued is done
+};
+
+__device__ __forceinline__ bool chunk_wait(uint32_t bar, uint32_t parity, unsigned *err, unsigned code,
+                                           volatile int *abort_flag) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const unsigned long long t0 = global_timer_ns();
+  while (true) {
+    if (mbar_try_wait_sleep(bar, parity, 200000u)) return true;
+    if (*abort_flag) return false;
+    if (global_timer_ns() - t0 > kWaitLimitNs) {
+      atomicOr(err, code);
+      *abort_flag = 1;
+      return false;
+    }
+  }
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __int_as_float(static_cast<int>(w << 16)); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __int_as_float(static_cast<int>(w & 0xffff0000u)); }
+
+// Rows of a segment's two row tiles.
+struct ChunkRows {
+  int tok0, rows, tiles;  // first token, rows, row tiles in use (1 or 2)
+};
+__device__ __forceinline__ ChunkRows chunk_rows(const SplitSeg &g, int group, const SplitShape &sh) {
+  ChunkRows r;
+  r.tok0 = g.r * sh.tok;
+  r.rows = min(sh.tok, g.si.n - r.tok0) * group;
+  r.tiles = r.rows > 128 ? 2 : 1;
+  return r;
+}
+
+template <int FORMAT, int D, bool BETA>
+__global__ void __launch_bounds__(kChunkThreads, 1)
+    paged_chunk_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                       const PagedReadArgs a, const PagedSplit sp, const SplitShape shape, int box_shift) {
+  using Lay = ChunkLayout<FORMAT, D>;
+  constexpr bool kCodes = FORMAT == kCacheE4m3;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t sbase = smem_u32(smem);
+  const uint32_t bars = sbase + Lay::kBars;
+#define FEM_CB(i) (bars + 8u * static_cast<uint32_t>(i))
+  volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + Lay::kAbort);
+  SplitScan<kChunkThreads> &scan = *reinterpret_cast<SplitScan<kChunkThreads> *>(smem + Lay::kScan);
+  float *s_shift = reinterpret_cast<float *>(smem + Lay::kShift);
+  volatile unsigned *s_inv = reinterpret_cast<volatile unsigned *>(smem + Lay::kInv);
+  volatile int *s_wide = reinterpret_cast<volatile int *>(smem + Lay::kWide);
+  const int box_rows = 1 << box_shift;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+
+  grid_dep_launch_dependents();
+  const long long W = split_total(a, shape, scan);
+  if (W == 0) return;
+  const int G = split_ctas(W, gridDim.x, shape), cta = blockIdx.x;
+  if (cta >= G) return;
+  SplitWalk walk;
+  walk.x = split_start(W, G, cta);
+  walk.x1 = split_start(W, G, cta + 1);
+  {
+    long long prefix;
+    split_locate(a, shape, walk.x, scan, &walk.s, &prefix);
+    walk.local = walk.x - prefix;
+  }
+  if (warp == 12) {
+    tmem_alloc(sbase + Lay::kTmem, 512);
+    tmem_relinquish();
+  }
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(FEM_CB(kCbQ + i), 128);
+      mbar_init(FEM_CB(kCbKFull + i), kCodes ? 128 : 1);
+      mbar_init(FEM_CB(kCbKEmpty + i), 1);
+      mbar_init(FEM_CB(kCbVFull + i), 1);
+      mbar_init(FEM_CB(kCbEFull + i), 128);
+      mbar_init(FEM_CB(kCbEEmpty + i), 1);
+      mbar_init(FEM_CB(kCbS + i), 1);
+      mbar_init(FEM_CB(kCbP + i), 128);
+    }
+    mbar_init(FEM_CB(kCbRawKFull), 1);
+    mbar_init(FEM_CB(kCbRawVFull), 1);
+    mbar_init(FEM_CB(kCbRawKEmpty), 128);
+    mbar_init(FEM_CB(kCbRawVEmpty), 128);
+    mbar_init(FEM_CB(kCbO), 1);
+    mbar_init(FEM_CB(kCbDone), 1);
+    fence_mbar_init();
+    *abort_flag = 0;
+    for (int i = 0; i < kSegRing; ++i) s_wide[i] = 0;
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(smem + Lay::kTmem);
+  SplitSeg sg;
+
+  // The block's registers are 512 x 128; the softmax warps take 184 each, the bank's 104, the others 40:
+  // 256 x 184 + 128 x 104 + 128 x 40 = 512 x 128.
+  if (warp >= 12) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+  if (warp == 12) {
+    // ------------------------------------------------------------ TMA of K and V
+    const int boxes = kChunkKeys / box_rows;
+    constexpr int kCols = kCodes ? (D < 128 ? D : 128) : 64;  // elements of a box's row
+    constexpr int kBlocks = D / kCols;
+    const uint32_t box_bytes = static_cast<uint32_t>(box_rows) * kCols * (kCodes ? 1 : 2);
+    unsigned n = 0;  // key tiles so far
+    bool ok = true;
+    while (ok && walk.next(a, shape, sg)) {
+      for (int kt = sg.kt0; ok && kt < sg.kt1; ++kt, ++n) {
+        const int st = n & 1;
+        const unsigned use = n >> 1;
+        // lane b: box b of the tile
+        const int key = kt * kChunkKeys + lane * box_rows;
+        const bool wanted = lane < boxes && key < sg.si.ctx;
+        const int page = wanted ? paged_page(a, sg.s, key) : -1;
+        const unsigned there = __ballot_sync(0xffffffffu, page >= 0), want = __ballot_sync(0xffffffffu, wanted);
+        if (lane == 0) s_inv[n % kInvRing] = want & ~there;
+        __syncwarp();
+        const uint32_t bytes = __popc(there) * (box_bytes * kBlocks + (kCodes ? box_rows : 0));
+        const long long row = page >= 0 ? paged_row(a.c, page, sg.h, key) : 0;
+        const int y = key & ((1 << a.c.page_shift) - 1), z = page * a.c.H + sg.h;
+        auto load = [&](const CUtensorMap *map, uint32_t dst, uint32_t bar, uint32_t sc, const uint8_t *exps) {
+          if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
+          __syncwarp();
+          if (page >= 0) {
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+              tma_load_3d(dst + b * (128 * kCols * (kCodes ? 1 : 2)) + lane * box_bytes, map, bar, b * kCols, y, z);
+            if (kCodes) bulk_load(sc + lane * box_rows, exps + row, box_rows, bar);
+          }
+        };
+        if (kCodes) {
+          if (n > 0) ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbRawKEmpty), (n - 1) & 1, a.err, kErrWaitMma, abort_flag));
+          if (ok) load(&tmap_k, sbase + Lay::kRawK, FEM_CB(kCbRawKFull), sbase + Lay::kScaleK, a.c.ke);
+          if (ok && n > 0) ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbRawVEmpty), (n - 1) & 1, a.err, kErrWaitMma, abort_flag));
+          if (ok) load(&tmap_v, sbase + Lay::kRawV, FEM_CB(kCbRawVFull), sbase + Lay::kScaleV, a.c.ve);
+        } else {
+          if (use > 0) ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbKEmpty + st), (use - 1) & 1, a.err, kErrWaitMma, abort_flag));
+          if (ok) load(&tmap_k, sbase + Lay::kK + st * Lay::kTile, FEM_CB(kCbKFull + st), 0, nullptr);
+          if (ok && use > 0) ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbEEmpty + st), (use - 1) & 1, a.err, kErrWaitMma, abort_flag));
+          if (ok) load(&tmap_v, sbase + Lay::kE + st * Lay::kTile, FEM_CB(kCbVFull + st), 0, nullptr);
+        }
+      }
+    }
+    if (!ok && lane == 0) {
+      // another role gave up: the copies in flight land before the block ends (tiles n - 1 and n at most)
+      for (int i = 0; i < 2; ++i) {
+        const unsigned t = n + 1 - i;  // tile t - 1
+        if (t == 0) continue;
+        const unsigned par = kCodes ? ((t - 1) & 1) : (((t - 1) >> 1) & 1);
+        const int st = (t - 1) & 1;
+        mbar_wait_for(FEM_CB(kCodes ? kCbRawKFull : kCbKFull + st), par, a.err, kErrWaitTma, 100000000ull);
+        mbar_wait_for(FEM_CB(kCodes ? kCbRawVFull : kCbVFull + st), par, a.err, kErrWaitTma, 100000000ull);
+      }
+    }
+  } else if (warp == 13) {
+    // ------------------------------------------------------------ products
+    if (lane == 0) {
+      constexpr uint32_t idesc_s = idesc_f16(128, 128, true, false);
+      constexpr uint32_t idesc_o = idesc_f16(128, D, true, true);
+      unsigned n = 0, np[2] = {0, 0}, seg = 0;  // key tiles, P of each row tile, segments so far
+      bool ok = true;
+      auto issue_s = [&](int t, int st) {
+        const uint32_t sK = sbase + Lay::kK + st * Lay::kTile, sQ = sbase + Lay::kQ + t * Lay::kTile;
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+          const uint32_t off = (kk >> 2) * 16384 + (kk & 3) * 32;
+          mma_f16_ss(tmem + t * 128, smem_desc_sw128(sQ + off, 16, 1024), smem_desc_sw128(sK + off, 16, 1024), idesc_s,
+                     kk > 0 ? 1u : 0u);
+        }
+        mma_commit(FEM_CB(kCbS + t));
+      };
+      while (ok && walk.next(a, shape, sg)) {
+        const int tiles = chunk_rows(sg, a.group, shape).tiles, nk = sg.kt1 - sg.kt0;
+        for (int t = 0; t < tiles; ++t)
+          ok = ok && chunk_wait(FEM_CB(kCbQ + t), seg & 1, a.err, kErrWaitMma, abort_flag);
+        // a row tile out of use keeps its barrier's phase with the others': its warps arrive all the same
+        if (tiles == 1) ok = ok && chunk_wait(FEM_CB(kCbQ + 1), seg & 1, a.err, kErrWaitMma, abort_flag);
+        for (int k = 0; ok && k <= nk; ++k) {
+          const unsigned i = n + k;  // this key tile
+          if (k < nk) {
+            ok = chunk_wait(FEM_CB(kCbKFull + (i & 1)), (i >> 1) & 1, a.err, kErrWaitTma, abort_flag);
+            if (!ok) break;
+            tc_fence_after_sync();
+          }
+          for (int t = 0; t < tiles; ++t) {
+            if (k > 0) {
+              // O_t += P_t E of key tile i - 1
+              const unsigned e = i - 1;
+              if (t == 0) ok = ok && chunk_wait(FEM_CB(kCbEFull + (e & 1)), (e >> 1) & 1, a.err, kErrWaitMma, abort_flag);
+              ok = ok && chunk_wait(FEM_CB(kCbP + t), np[t] & 1, a.err, kErrWaitMma, abort_flag);
+              if (!ok) break;
+              ++np[t];
+              tc_fence_after_sync();
+              const uint32_t sE = sbase + Lay::kE + (e & 1) * Lay::kTile;
+#pragma unroll
+              for (int kk = 0; kk < 8; ++kk)
+                mma_f16_ts(tmem + 256 + t * D, tmem + t * 128 + kk * 8, smem_desc_sw128(sE + kk * 2048, 16384, 1024),
+                           idesc_o, (k > 1 || kk > 0) ? 1u : 0u);
+              if (t == tiles - 1) mma_commit(FEM_CB(kCbEEmpty + (e & 1)));
+            }
+            if (k < nk) {
+              issue_s(t, i & 1);
+              if (t == tiles - 1) mma_commit(FEM_CB(kCbKEmpty + (i & 1)));
+            }
+          }
+        }
+        if (ok) mma_commit(FEM_CB(kCbO));
+        n += nk;
+        ++seg;
+      }
+      mma_commit(FEM_CB(kCbDone));
+      // nothing may be in flight when TMEM is freed
+      mbar_wait(FEM_CB(kCbDone), 0, a.err, kErrWaitMma);
+    }
+  } else if (warp < 4) {
+    // ------------------------------------------------------------ the bank
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    const int rl = tid & 7, cc = tid >> 3;  // rows rl, rl + 8, ...; 16-byte chunk cc (of bf16)
+    constexpr int kChunks = D / 8;          // per row: 16 at D = 128, 8 at D = 64 (then two row groups)
+    const int col = cc % kChunks, r_first = rl + 8 * (cc / kChunks);
+    constexpr int kRowStep = 8 * (16 / kChunks), kRowsEach = 128 / kRowStep;
+    BankCoef co[8];
+    int last_s = -1, last_h = -1;
+    unsigned n = 0, seg = 0;
+    bool ok = true;
+    while (ok && walk.next(a, shape, sg)) {
+      // coefficients of the thread's 8 channels, from the sequence's first values
+      if (BETA && (sg.s != last_s || sg.h != last_h)) {
+        last_s = sg.s;
+        last_h = sg.h;
+        float vmax[8], vabs[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          vmax[e] = -INFINITY;
+          vabs[e] = 0.f;
+        }
+        const int page = sg.si.ctx > 0 ? paged_page(a, sg.s, 0) : -1;
+        if (page >= 0) {
+          const long long row = paged_row(a.c, page, sg.h, 0);
+          const int cnt = min(kSampleKeys, sg.si.ctx);
+#pragma unroll 4
+          for (int kk = 0; kk < cnt; ++kk) {
+            float v[8];
+            if (kCodes) {
+              const uint2 w = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(a.c.v) + (row + kk) * D + col * 8);
+              const float sc = paged_scale(a.c.ve[row + kk]);
+              const uint32_t x[4] = {w.x & 0xffffu, w.x >> 16, w.y & 0xffffu, w.y >> 16};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float2 f = e4m3x2_to_float2(x[e]);
+                v[2 * e] = f.x * sc;
+                v[2 * e + 1] = f.y * sc;
+              }
+            } else {
+              const uint4 w = *reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.c.v) + (row + kk) * D + col * 8);
+              const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                v[2 * e] = bf16_lo(x[e]);
+                v[2 * e + 1] = bf16_hi(x[e]);
+              }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              vmax[e] = fmaxf(vmax[e], v[e]);
+              vabs[e] = fmaxf(vabs[e], fabsf(v[e]));
+            }
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          co[e] = bank_coef(__ldg(a.beta + static_cast<long long>(sg.h) * D + col * 8 + e), vmax[e], vabs[e]);
+      }
+      float emax = 0.f;
+      bool wrote = false;  // this segment's shifts, once its first stage is free
+      for (int kt = sg.kt0; ok && kt < sg.kt1; ++kt, ++n) {
+        const int st = n & 1;
+        const unsigned use = n >> 1;
+        const int k0 = kt * kChunkKeys;
+        uint8_t *tE = smem + Lay::kE + st * Lay::kTile;
+        if (kCodes) {
+          // K: codes to bf16
+          ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbRawKFull), n & 1, a.err, kErrWaitTma, abort_flag));
+          if (ok && use > 0) ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbKEmpty + st), (use - 1) & 1, a.err, kErrWaitMma, abort_flag));
+          if (!ok) break;
+        } else {
+          ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbVFull + st), use & 1, a.err, kErrWaitTma, abort_flag));
+          if (!ok) break;
+        }
+        const unsigned inv = s_inv[n % kInvRing];
+        const bool ragged = inv != 0 || k0 + kChunkKeys > sg.si.ctx;
+        auto gone = [&](int r) { return k0 + r >= sg.si.ctx || ((inv >> (r >> box_shift)) & 1u); };
+        if (kCodes) {
+          uint8_t *tK = smem + Lay::kK + st * Lay::kTile;
+          const uint8_t *raw = smem + Lay::kRawK;
+#pragma unroll 4
+          for (int i = 0; i < kRowsEach; ++i) {
+            const int r = r_first + kRowStep * i;
+            uint4 y = make_uint4(0, 0, 0, 0);
+            if (!gone(r)) {
+              const uint32_t off = D == 128 ? sw128_offset(r, col >> 1) + 8 * (col & 1)
+                                            : r * 64 + (((col >> 1) ^ ((r >> 1) & 3)) << 4) + 8 * (col & 1);
+              const uint2 w = *reinterpret_cast<const uint2 *>(raw + off);
+              const float sc = paged_scale(smem[Lay::kScaleK + r]);
+              const float2 f0 = e4m3x2_to_float2(w.x & 0xffffu), f1 = e4m3x2_to_float2(w.x >> 16);
+              const float2 f2 = e4m3x2_to_float2(w.y & 0xffffu), f3 = e4m3x2_to_float2(w.y >> 16);
+              y = make_uint4(pack_bf16(f0.x * sc, f0.y * sc), pack_bf16(f1.x * sc, f1.y * sc),
+                             pack_bf16(f2.x * sc, f2.y * sc), pack_bf16(f3.x * sc, f3.y * sc));
+            }
+            *reinterpret_cast<uint4 *>(tK + (col >> 3) * 16384 + sw128_offset(r, col & 7)) = y;
+          }
+          fence_proxy_async_smem();
+          mbar_arrive(FEM_CB(kCbKFull + st));
+          mbar_arrive(FEM_CB(kCbRawKEmpty));
+          ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbRawVFull), n & 1, a.err, kErrWaitTma, abort_flag));
+          if (ok && use > 0) ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbEEmpty + st), (use - 1) & 1, a.err, kErrWaitMma, abort_flag));
+          if (!ok) break;
+        }
+        if (!wrote) {
+          // the stage is free: of earlier segments at most two are not yet written out (see kSegRing)
+          wrote = true;
+          if (rl == 0 && cc < kChunks) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              s_shift[(seg % kSegRing) * D + col * 8 + e] = BETA && co[e].theta == 0.f ? co[e].s : __int_as_float(0x7fffffff);
+          }
+        }
+        if (BETA || kCodes || ragged) {
+#pragma unroll 4
+          for (int i = 0; i < kRowsEach; ++i) {
+            const int r = r_first + kRowStep * i;
+            uint4 *at = reinterpret_cast<uint4 *>(tE + (col >> 3) * 16384 + sw128_offset(r, col & 7));
+            uint4 y = make_uint4(0, 0, 0, 0);
+            if (!(ragged && gone(r))) {
+              float v[8];
+              if (kCodes) {
+                const uint32_t off = D == 128 ? sw128_offset(r, col >> 1) + 8 * (col & 1)
+                                              : r * 64 + (((col >> 1) ^ ((r >> 1) & 3)) << 4) + 8 * (col & 1);
+                const uint2 w = *reinterpret_cast<const uint2 *>(smem + Lay::kRawV + off);
+                const float sc = paged_scale(smem[Lay::kScaleV + r]);
+                const uint32_t x[4] = {w.x & 0xffffu, w.x >> 16, w.y & 0xffffu, w.y >> 16};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const float2 f = e4m3x2_to_float2(x[e]);
+                  v[2 * e] = f.x * sc;
+                  v[2 * e + 1] = f.y * sc;
+                }
+              } else {
+                const uint4 w = *at;
+                const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  v[2 * e] = bf16_lo(x[e]);
+                  v[2 * e + 1] = bf16_hi(x[e]);
+                }
+              }
+              if (BETA) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = bank_value(co[e], v[e]);
+                emax = fmax3(emax, fmax3(v[0], v[1], v[2]), fmax3(v[3], v[4], v[5]));
+                emax = fmax3(emax, v[6], v[7]);
+              }
+              y = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+            }
+            *at = y;
+          }
+          if (BETA && emax > kWideE) s_wide[seg % kSegRing] = static_cast<int>(seg + 1);
+        }
+        fence_proxy_async_smem();
+        mbar_arrive(FEM_CB(kCbEFull + st));
+        if (kCodes) mbar_arrive(FEM_CB(kCbRawVEmpty));
+      }
+      ++seg;
+    }
+  } else if (warp < 12) {
+    // ------------------------------------------------------------ softmax, queries and output of a row tile
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    const int t = (warp >> 2) - 1, r = tid & 127;
+    const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t tS = tmem + t * 128 + lane_off, tO = tmem + 256 + t * D + lane_off;
+    const float qk_scale = a.scale * kLog2e;
+    unsigned n = 0, ns = 0, seg = 0;
+    bool ok = true;
+    while (ok && walk.next(a, shape, sg)) {
+      const ChunkRows cr = chunk_rows(sg, a.group, shape);
+      const int nk = sg.kt1 - sg.kt0, ir = t * 128 + r;  // row of the item
+      const bool on = ir < cr.rows;
+      const int tok = cr.tok0 + (on ? ir / a.group : 0), hq = sg.h * a.group + (on ? ir % a.group : 0);
+      const long long qrow = static_cast<long long>(sg.si.q0) + tok, orow = qrow * a.Hq + hq;
+      const int lim = on ? min(paged_limit(sg.si, tok, a.causal), sg.si.ctx) : 0;
+      if (t < cr.tiles) {
+        // the last S of the item before is done (its commit was waited for), so Q may be replaced
+        uint8_t *tQ = smem + Lay::kQ + t * Lay::kTile;
+        const uint4 *qp = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.q) + qrow * a.q_sn + hq * a.q_sh);
+#pragma unroll 8
+        for (int c = 0; c < D / 8; ++c)
+          *reinterpret_cast<uint4 *>(tQ + (c >> 3) * 16384 + sw128_offset(r, c & 7)) = on ? __ldg(qp + c) : make_uint4(0, 0, 0, 0);
+        fence_proxy_async_smem();
+      }
+      mbar_arrive(FEM_CB(kCbQ + t));
+      float m = -INFINITY, L = 0.f;
+      if (t < cr.tiles) {
+        for (int k = 0; k < nk; ++k, ++ns) {
+          ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbS + t), ns & 1, a.err, kErrWaitMma, abort_flag));
+          if (!ok) break;
+          tc_fence_after_sync();
+          uint32_t sr[128];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[c * 32]));
+          tmem_ld_wait();
+          float *s = reinterpret_cast<float *>(sr);
+          const int k0 = (sg.kt0 + k) * kChunkKeys;
+          const unsigned inv = s_inv[(n + k) % kInvRing];
+          if (__any_sync(0xffffffffu, k0 + kChunkKeys > lim) || inv) {
+#pragma unroll
+            for (int j = 0; j < 128; ++j) s[j] = k0 + j < lim ? s[j] : -INFINITY;
+            if (inv) {
+#pragma unroll
+              for (int j = 0; j < 128; ++j) s[j] = (inv >> (j >> box_shift)) & 1u ? -INFINITY : s[j];
+            }
+          }
+          float mx[8];
+#pragma unroll
+          for (int u = 0; u < 8; ++u) mx[u] = fmax3(s[u], s[u + 8], s[u + 16]);
+#pragma unroll
+          for (int j = 24; j < 120; j += 16)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) mx[u] = fmax3(mx[u], s[j + u], s[j + 8 + u]);
+#pragma unroll
+          for (int u = 0; u < 8; ++u) mx[u] = fmaxf(mx[u], s[120 + u]);
+          const float tmax = fmax3(fmax3(mx[0], mx[1], mx[2]), fmax3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * qk_scale;
+          float alpha = 1.f;
+          if (tmax > m + kRowMaxLag) {
+            alpha = ex2_approx(m - tmax);  // 0 the first time
+            m = tmax;
+            L *= alpha;
+          }
+          if (k > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
+            // O holds the products of the key tiles before (see the issue order)
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t v[32];
+              tmem_ld32(tO + c * 32, v);
+              tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
+              tmem_st32(tO + c * 32, v);
+            }
+            tmem_st_wait();
+          }
+          const float mz = m == -INFINITY ? 0.f : m;
+          const float2 scale2 = make_float2(qk_scale, qk_scale), negm2 = make_float2(-mz, -mz);
+          float2 ls[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) ls[u] = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t p[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float2 x = __ffma2_rn(make_float2(s[c * 32 + 2 * i], s[c * 32 + 2 * i + 1]), scale2, negm2);
+              const float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+              ls[i & 3] = __fadd2_rn(ls[i & 3], e);
+              p[i] = pack_bf16(e.x, e.y);
+            }
+            tmem_st16(tS + c * 16, p);
+          }
+          L += (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y) + (ls[2].x + ls[2].y) + (ls[3].x + ls[3].y);
+          tmem_st_wait();
+          tc_fence_before_sync();
+          mbar_arrive(FEM_CB(kCbP + t));
+        }
+        if (!ok) break;
+      }
+      // a row tile out of use waits too: its arrivals stay one segment ahead of the products at most
+      ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbO), seg & 1, a.err, kErrWaitMma, abort_flag));
+      if (!ok) break;
+      tc_fence_after_sync();
+      if (t < cr.tiles) {
+        // ---- the row's output, or its piece
+        const bool whole = sg.kt0 == 0 && sg.kt1 == sg.kt_all;
+        const bool wide = BETA && s_wide[seg % kSegRing] == static_cast<int>(seg + 1);
+        const float *shift = s_shift + (seg % kSegRing) * D;
+        float *piece = sp.pieces + static_cast<size_t>(cta * 2 + (sg.kt0 == 0 ? 1 : 0)) * piece_floats(256, D);
+        const bool empty = m == -INFINITY && L == 0.f;
+        const float inv_l = empty ? 0.f : 1.f / L;
+        bool good = true;
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t v[32];
+          tmem_ld32(tO + c * 32, v);
+          tmem_ld_wait();
+          if (!on) continue;
+          if (whole) {
+            uint32_t o[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              float x[2];
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                const int j = c * 32 + 2 * i + u;
+                bool fine = true;
+                const float av = __uint_as_float(v[2 * i + u]) * inv_l;
+                x[u] = BETA ? paged_out(__ldg(a.beta + static_cast<long long>(sg.h) * D + j), shift[j], av, wide, &fine)
+                            : av;
+                if (!BETA) fine = fabsf(av) < kMostA;
+                if (empty) x[u] = 0.f;
+                good = good && (fine || empty);
+              }
+              o[i] = pack_bf16(x[0], x[1]);
+            }
+            uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + orow * D + c * 32);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+          } else {
+            float4 *dst = reinterpret_cast<float4 *>(piece + static_cast<size_t>(ir) * D + c * 32);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              dst[i] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]),
+                                   __uint_as_float(v[4 * i + 3]));
+          }
+        }
+        if (on) {
+          if (whole) {
+            if (a.lse != nullptr) a.lse[orow] = empty ? -INFINITY : (m + log2f(L)) * kLn2;
+          } else {
+            piece[256 * D + 2 * ir] = m;
+            piece[256 * D + 2 * ir + 1] = L;
+          }
+          sp.todo[orow] = whole ? (good ? kRowDone : kRowExact) : kRowSplit;
+        }
+        if (!whole && t == 0) {
+          if (r < D) piece[256 * D + 512 + r] = shift[r];
+          if (r == 0) piece[256 * D + 512 + D] = wide ? 1.f : 0.f;
+        }
+        tc_fence_before_sync();  // the next item's products may overwrite O after this thread's next arrival
+      }
+      n += nk;
+      ++seg;
+    }
+  }
+
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 12) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, 512);
+  }
+#undef FEM_CB
+}
+
+}  // namespace
+
+template <int FORMAT, int D>
+static cudaError_t launch_chunk_d(const CUtensorMap &tk, const CUtensorMap &tv, const PagedReadArgs &a,
+                                  const PagedSplit &sp, const SplitShape &shape, int grid, int box_shift,
+                                  cudaStream_t stream) {
+  const size_t smem = ChunkLayout<FORMAT, D>::kBytes;
+  auto go = [&](auto kernel) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e != cudaSuccess) return e;
+    kernel<<<grid, kChunkThreads, smem, stream>>>(tk, tv, a, sp, shape, box_shift);
+    return cudaGetLastError();
+  };
+  return a.beta ? go(paged_chunk_kernel<FORMAT, D, true>) : go(paged_chunk_kernel<FORMAT, D, false>);
+}
+
+cudaError_t launch_paged_chunk(const CUtensorMap &tk, const CUtensorMap &tv, const PagedReadArgs &a,
+                               const PagedSplit &sp, const SplitShape &shape, int grid, int box_rows,
+                               cudaStream_t stream) {
+  int box_shift = 4;
+  while ((1 << box_shift) < box_rows) ++box_shift;
+  if ((1 << box_shift) != box_rows || box_rows > kChunkKeys) return cudaErrorInvalidValue;
+  if (shape.row_tile != 256 || shape.key_tile != kChunkKeys || shape.tok < 1) return cudaErrorInvalidValue;
+  if (a.c.format == kCacheBf16)
+    return a.c.d == 64 ? launch_chunk_d<kCacheBf16, 64>(tk, tv, a, sp, shape, grid, box_shift, stream)
+                       : launch_chunk_d<kCacheBf16, 128>(tk, tv, a, sp, shape, grid, box_shift, stream);
+  return a.c.d == 64 ? launch_chunk_d<kCacheE4m3, 64>(tk, tv, a, sp, shape, grid, box_shift, stream)
+                     : launch_chunk_d<kCacheE4m3, 128>(tk, tv, a, sp, shape, grid, box_shift, stream);
+}
+
+}  // namespace fem

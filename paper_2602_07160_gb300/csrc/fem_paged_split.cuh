@@ -36,9 +36,9 @@ constexpr float kLeastA = 1.3552527e-20f;     // 2^-66
 constexpr float kMostA = 1.2980742e33f;       // 2^110
 constexpr float kLeastLinear = 0.25f;         // 1 + beta a: less cancels more than two bits
 
-// E(v) = |v| < theta ? v + hb v^2 : ia 2^(b v + s) + ic
+// E(v) = |v| < theta ? v + hb v^2 : 2^(b v + s) + ic; linear channels have s = -log2 beta, ic = -1/beta
 struct BankCoef {
-  float b, s, ia, ic, hb, theta;
+  float b, s, ic, hb, theta;
 };
 
 __device__ __forceinline__ BankCoef bank_coef(float beta, float vmax, float vabs) {
@@ -47,13 +47,11 @@ __device__ __forceinline__ BankCoef bank_coef(float beta, float vmax, float vabs
   c.hb = 0.5f * beta;
   const bool linear = !(beta * vabs > kLinearReach);
   if (linear) {
-    c.s = 0.f;
-    c.ia = beta > 0.f ? 1.f / beta : 0.f;
-    c.ic = -c.ia;
+    c.s = beta > 0.f ? -log2f(beta) : 0.f;
+    c.ic = beta > 0.f ? -1.f / beta : 0.f;
     c.theta = beta > 0.f ? kSmallX / beta : INFINITY;
   } else {
     c.s = -c.b * vmax;
-    c.ia = 1.f;
     c.ic = 0.f;
     c.theta = 0.f;
   }
@@ -61,20 +59,22 @@ __device__ __forceinline__ BankCoef bank_coef(float beta, float vmax, float vabs
 }
 
 __device__ __forceinline__ float bank_value(const BankCoef &c, float v) {
-  const float e = fmaf(ex2_approx(fmaf(c.b, v, c.s)), c.ia, c.ic);
+  const float e = ex2_approx(fmaf(c.b, v, c.s)) + c.ic;
   return fabsf(v) < c.theta ? fmaf(c.hb * v, v, v) : e;
 }
 
 // The read from a; `shift` is the coefficient s of a shifted channel, NaN of a linear one.  ok: false
 // where the ranges could have spoilt it.
 __device__ __forceinline__ float paged_out(float beta, float shift, float a, bool wide, bool *ok) {
+  const float ib = rcp_approx(beta * kLog2e);
   if (shift != shift) {
     const float x = beta * a;
     *ok = !wide && x > kLeastLinear - 1.f && x < kMostA && fabsf(a) < kMostA;
-    return fabsf(x) < 1e-4f ? a * fmaf(-0.5f, x, 1.f) : log1pf(x) / beta;
+    // log1p(x) / beta; the series is good to 2^-18 where it is used, lg2's 2^-22 to 2^-16 elsewhere
+    return fabsf(x) < kSmallX ? a * fmaf(x, fmaf(x, 1.f / 3.f, -0.5f), 1.f) : lg2_approx(1.f + x) * ib;
   }
   *ok = a > (wide ? kWideE : kLeastA) && a < kMostA;
-  return (log2f(a) - shift) / (beta * kLog2e);
+  return (lg2_approx(a) - shift) * ib;
 }
 
 // ---------------------------------------------------------------------------
@@ -82,20 +82,97 @@ __device__ __forceinline__ float paged_out(float beta, float shift, float a, boo
 // ---------------------------------------------------------------------------
 struct SplitShape {
   int row_tile, key_tile;  // rows and keys of a tile
+  int tok;                 // tokens of a row tile (row_tile / group, whole tokens), or 0: rows packed without regard to tokens
   int least;               // key tiles a CTA takes at least
 };
 
-// Row tiles and key tiles of a sequence; a sequence without rows has none, and
-// one with rows has at least one key tile, so that its rows are written.
+// Row tiles of a sequence, for each of its heads; a sequence without rows has none.
 __device__ __forceinline__ int seq_row_tiles(const SeqInfo &si, int group, const SplitShape &sh) {
-  return (si.n * group + sh.row_tile - 1) / sh.row_tile;
+  return sh.tok ? (si.n + sh.tok - 1) / sh.tok : (si.n * group + sh.row_tile - 1) / sh.row_tile;
 }
-__device__ __forceinline__ int seq_key_tiles(const SeqInfo &si, const SplitShape &sh) {
-  return max((si.ctx + sh.key_tile - 1) / sh.key_tile, 1);
+// Key tiles of row tile r: those its last row sees (tiles of whole tokens), or all.  At least one, so
+// that rows which see nothing are written.
+__device__ __forceinline__ int row_key_tiles(const SeqInfo &si, int r, int causal, const SplitShape &sh) {
+  int keys = si.ctx;
+  if (sh.tok && causal) keys = si.ctx - si.n + min((r + 1) * sh.tok, si.n);
+  return max((keys + sh.key_tile - 1) / sh.key_tile, 1);
+}
+// Key tiles of row tiles 0 .. R - 1 of one head (R at most seq_row_tiles).
+__device__ __forceinline__ long long head_key_tiles(const SeqInfo &si, int R, int group, int causal,
+                                                    const SplitShape &sh) {
+  if (R <= 0) return 0;
+  if (!(sh.tok && causal)) return static_cast<long long>(R) * row_key_tiles(si, 0, 0, sh);
+  // sum of ceil((c + i tok) / key_tile), i = 0 .. R' - 1, over the tiles of tok whole tokens; the last
+  // tile of the sequence may hold fewer
+  const int all = seq_row_tiles(si, group, sh);
+  long long sum = 0;
+  int n = R, i0 = 0;
+  if (R == all) {
+    sum = row_key_tiles(si, R - 1, causal, sh);
+    n = R - 1;
+  }
+  const int base = si.ctx - si.n;
+  if (base + sh.tok < 1) {  // leading tiles that see nothing count one each
+    i0 = min(n, (-base) / sh.tok);
+    while (i0 < n && base + (i0 + 1) * sh.tok < 1) ++i0;
+    sum += i0;
+  }
+  n -= i0;
+  // ceil(x / T) = floor((x + T - 1) / T); floor sum = (sum of x - sum of x mod T) / T, the residues with
+  // period P = T / gcd(tok, T) (T a power of two), a full period's being g times 0 .. P - 1 plus b mod g
+  const int T = sh.key_tile, step = sh.tok;
+  const long long b = static_cast<long long>(base) + static_cast<long long>(i0 + 1) * step + T - 1;
+  const int gcd = min(step & -step, T), P = T / gcd, rem = n % P;
+  const long long full = n / P;
+  long long res = full * (static_cast<long long>(P) * (b & (gcd - 1)) + static_cast<long long>(gcd) * P * (P - 1) / 2);
+  for (int i = 0; i < rem; ++i) res += (b + static_cast<long long>(i) * step) & (T - 1);
+  const long long x = n * b + static_cast<long long>(step) * n * (n - 1) / 2;
+  return sum + (x - res) / T;
 }
 __device__ __forceinline__ long long seq_tiles(const PagedReadArgs &a, const SeqInfo &si, const SplitShape &sh) {
-  return static_cast<long long>(a.c.H) * seq_row_tiles(si, a.group, sh) * seq_key_tiles(si, sh);
+  return a.c.H * head_key_tiles(si, seq_row_tiles(si, a.group, sh), a.group, a.causal, sh);
 }
+
+// An item and the key tiles kt0 .. kt1 - 1 of it (kt_all in the whole item).
+struct SplitSeg {
+  SeqInfo si;
+  int s, h, r;  // sequence, head, row tile
+  int kt0, kt1, kt_all;
+};
+
+// Walks a CTA's stretch, item by item.
+struct SplitWalk {
+  long long x, x1, local;  // next tile, the stretch's end, x within sequence s
+  int s;
+  __device__ __forceinline__ bool next(const PagedReadArgs &a, const SplitShape &sh, SplitSeg &g) {
+    if (x >= x1) return false;
+    while (true) {
+      g.si = paged_seq(a, s);
+      const int R = seq_row_tiles(g.si, a.group, sh);
+      const long long per = head_key_tiles(g.si, R, a.group, a.causal, sh), cost = per * a.c.H;
+      if (local >= cost) {  // a sequence done, or one without rows
+        local -= cost;
+        ++s;
+        continue;
+      }
+      g.s = s;
+      g.h = static_cast<int>(local / per);
+      const long long in = local - g.h * per;
+      int lo = 0, hi = R;  // the last r whose tiles begin at or before `in`
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (head_key_tiles(g.si, mid, a.group, a.causal, sh) <= in) lo = mid; else hi = mid;
+      }
+      g.r = lo;
+      g.kt_all = row_key_tiles(g.si, lo, a.causal, sh);
+      g.kt0 = static_cast<int>(in - head_key_tiles(g.si, lo, a.group, a.causal, sh));
+      g.kt1 = static_cast<int>(min(static_cast<long long>(g.kt_all), g.kt0 + (x1 - x)));
+      x += g.kt1 - g.kt0;
+      local += g.kt1 - g.kt0;
+      return true;
+    }
+  }
+};
 
 // CTAs that take part, and CTA g's first tile.
 __device__ __forceinline__ int split_ctas(long long W, int grid, const SplitShape &sh) {

@@ -42,8 +42,8 @@ struct TokLayout {
   static constexpr int kScale = kTokWarps * kStages * kStage;
   static constexpr int kBar = kScale + kTokWarps * kStages * 32;
   static constexpr int kCoef4 = (kBar + kTokWarps * kStages * 8 + 15) & ~15;
-  static constexpr int kCoef2 = kCoef4 + D * 16;
-  static constexpr int kShift = kCoef2 + D * 8;
+  static constexpr int kCoef1 = kCoef4 + D * 16;
+  static constexpr int kShift = kCoef1 + D * 4;
   static constexpr int kRed = kShift + D * 4;
   static constexpr int kStat = kRed + kRows * kRedStride * 4;  // [warps][rows] {m, L}
   static constexpr int kWideFlag = kStat + kTokWarps * kRows * 8;
@@ -110,14 +110,6 @@ __device__ __forceinline__ uint2 e4m3x4_to_bf16(uint32_t x, uint32_t scale2) {
   return make_uint2(*reinterpret_cast<uint32_t *>(&a), *reinterpret_cast<uint32_t *>(&b));
 }
 
-// A sequence's stretch of a CTA.
-struct TokSeg {
-  int s, h, row0, rows;  // sequence, head, first row and rows of the row tile (all rows of the sequence: total)
-  int total;
-  int kt0, kt1, kt_all;
-  SeqInfo si;
-};
-
 template <int FORMAT, int D, int NT, bool BETA>
 __global__ void __launch_bounds__(kTokThreads, 2)
     paged_token_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
@@ -135,7 +127,7 @@ __global__ void __launch_bounds__(kTokThreads, 2)
   const uint32_t scales = sbase + Lay::kScale + warp * NS * 32;
   const uint32_t bars = sbase + Lay::kBar + warp * NS * 8;
   float4 *coef4 = reinterpret_cast<float4 *>(smem + Lay::kCoef4);
-  float2 *coef2 = reinterpret_cast<float2 *>(smem + Lay::kCoef2);
+  float *coef1 = reinterpret_cast<float *>(smem + Lay::kCoef1);
   float *s_shift = reinterpret_cast<float *>(smem + Lay::kShift);
   float *s_red = reinterpret_cast<float *>(smem + Lay::kRed);
   float2 *s_stat = reinterpret_cast<float2 *>(smem + Lay::kStat);
@@ -155,33 +147,13 @@ __global__ void __launch_bounds__(kTokThreads, 2)
   int s;
   long long prefix;
   split_locate(a, shape, x0, scan, &s, &prefix);
-  long long local = x0 - prefix;
+  SplitWalk walk = {x0, x1, x0 - prefix, s};
+  SplitSeg sg;
   unsigned phases = 0;  // parity of each stage's barrier
   bool alive = true;
 
-  for (long long x = x0; x < x1;) {
-    // ---- the next segment
-    TokSeg sg;
-    sg.si = paged_seq(a, s);
-    const int rt = seq_row_tiles(sg.si, a.group, shape);
-    sg.kt_all = seq_key_tiles(sg.si, shape);
-    const long long cost = static_cast<long long>(a.c.H) * rt * sg.kt_all;
-    if (local >= cost) {  // the next sequence (one without rows has no tiles)
-      local -= cost;
-      ++s;
-      continue;
-    }
-    const int item = static_cast<int>(local / sg.kt_all);
-    sg.s = s;
-    sg.h = item / rt;
-    sg.row0 = (item % rt) * kRows;
-    sg.total = sg.si.n * a.group;
-    sg.rows = min(kRows, sg.total - sg.row0);
-    sg.kt0 = static_cast<int>(local - static_cast<long long>(item) * sg.kt_all);
-    sg.kt1 = static_cast<int>(min(static_cast<long long>(sg.kt_all), sg.kt0 + (x1 - x)));
-    x += sg.kt1 - sg.kt0;
-    local += sg.kt1 - sg.kt0;
-
+  while (walk.next(a, shape, sg)) {
+    const int row0 = sg.r * kRows, total = sg.si.n * a.group, n_rows = min(kRows, total - row0);
     // ---- this warp's stages: key groups kt * 4 + warp, kt0 <= kt < kt1, that hold a key
     const int n_st = [&] {
       const int groups = (sg.si.ctx + kTokKeys - 1) / kTokKeys;  // of the sequence
@@ -252,8 +224,8 @@ __global__ void __launch_bounds__(kTokThreads, 2)
         // element e of a lane's piece of 8 channels, lanes side by side
         const int at = Lay::kElem == 2 || !R128 ? (tid & ~63) + (tid & 7) * 8 + ((tid >> 3) & 7)
                                                 : (tid & 15) * 8 + (tid >> 4);
-        coef4[at] = make_float4(c.b, c.s, c.ia, c.ic);
-        coef2[at] = make_float2(c.hb, c.theta);
+        coef4[at] = make_float4(c.b, c.s, c.ic, c.hb);
+        coef1[at] = c.theta;
         s_shift[tid] = c.theta == 0.f ? c.s : __int_as_float(0x7fffffff);
       }
     } else if (tid < D) {
@@ -264,8 +236,8 @@ __global__ void __launch_bounds__(kTokThreads, 2)
     uint32_t qf[NT][MT][2];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const int r = sg.row0 + 8 * t + g;
-      const bool on = r < sg.total;
+      const int r = row0 + 8 * t + g;
+      const bool on = r < total;
       const int tok = on ? r / a.group : 0, hq = sg.h * a.group + (on ? r % a.group : 0);
       const __nv_bfloat16 *qp = static_cast<const __nv_bfloat16 *>(a.q) +
                                 (static_cast<long long>(sg.si.q0) + tok) * a.q_sn + hq * a.q_sh;
@@ -284,9 +256,9 @@ __global__ void __launch_bounds__(kTokThreads, 2)
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const int r = sg.row0 + 8 * t + 2 * i4 + u;
-        lim[t][u] = r < sg.total ? min(paged_limit(sg.si, r / a.group, a.causal), sg.si.ctx) : 0;
-        if (r < sg.total) lim_min = min(lim_min, lim[t][u]);
+        const int r = row0 + 8 * t + 2 * i4 + u;
+        lim[t][u] = r < total ? min(paged_limit(sg.si, r / a.group, a.causal), sg.si.ctx) : 0;
+        if (r < total) lim_min = min(lim_min, lim[t][u]);
       }
     lim_min = __reduce_min_sync(0xffffffffu, lim_min);
     float m[NT][2], L[NT][2], acc[NT][MT][4], emax = 0.f;
@@ -455,8 +427,7 @@ __global__ void __launch_bounds__(kTokThreads, 2)
               if (BETA) {
                 const int at = pc * 64 + 2 * q * 8 + lane_g;
                 const float4 ca = coef4[at], cb = coef4[at + 8];
-                const float2 da = coef2[at], db = coef2[at + 8];
-                const BankCoef A = {ca.x, ca.y, ca.z, ca.w, da.x, da.y}, B = {cb.x, cb.y, cb.z, cb.w, db.x, db.y};
+                const BankCoef A = {ca.x, ca.y, ca.z, ca.w, coef1[at]}, B = {cb.x, cb.y, cb.z, cb.w, coef1[at + 8]};
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
                   lo[u] = bank_value(A, lo[u]);
@@ -535,7 +506,7 @@ __global__ void __launch_bounds__(kTokThreads, 2)
     const int slot = cta * 2 + (sg.kt0 == 0 ? 1 : 0);
     float *piece = sp.pieces + static_cast<size_t>(slot) * piece_floats(kRows, D);
     const bool wide = *s_wide != 0;
-    for (int r = 0; r < sg.rows; ++r) {
+    for (int r = 0; r < n_rows; ++r) {
       float M = -INFINITY, Lr = 0.f;
 #pragma unroll
       for (int q = 0; q < kTokWarps; ++q) M = fmaxf(M, s_stat[q * kRows + r].x);
@@ -545,7 +516,7 @@ __global__ void __launch_bounds__(kTokThreads, 2)
         if (st.x != -INFINITY) Lr += st.y * ex2_approx(st.x - M);
         else if (st.y != st.y) Lr = st.y;  // a row of NaN scores has no maximum
       }
-      const int rr = sg.row0 + r, tok = rr / a.group, hq = sg.h * a.group + rr % a.group;
+      const int rr = row0 + r, tok = rr / a.group, hq = sg.h * a.group + rr % a.group;
       const long long orow = (static_cast<long long>(sg.si.q0) + tok) * a.Hq + hq;
       if (whole) {
         if (tid < D) {
@@ -574,8 +545,8 @@ __global__ void __launch_bounds__(kTokThreads, 2)
       if (tid == 0) piece[kRows * D + 2 * kRows + D] = wide ? 1.f : 0.f;
     }
     __syncthreads();
-    if (tid < sg.rows) {
-      const int rr = sg.row0 + tid, tok = rr / a.group, hq = sg.h * a.group + rr % a.group;
+    if (tid < n_rows) {
+      const int rr = row0 + tid, tok = rr / a.group, hq = sg.h * a.group + rr % a.group;
       sp.todo[(static_cast<long long>(sg.si.q0) + tok) * a.Hq + hq] =
           whole ? (s_bad[tid] ? kRowExact : kRowDone) : kRowSplit;
     }
