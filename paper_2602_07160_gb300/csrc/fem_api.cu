@@ -884,9 +884,9 @@ int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride
     return rc;
   const size_t piece_b = round256(2 * static_cast<size_t>(grid) * piece_floats(shape.row_tile, a.c.d) * sizeof(float));
   uint8_t *ws = nullptr;
-  cudaError_t e = ws_alloc(ds, reinterpret_cast<void **>(&ws), piece_b + static_cast<size_t>(N) * Hq, s);
+  cudaError_t e = ws_alloc(ds, reinterpret_cast<void **>(&ws), piece_b + static_cast<size_t>(N) * Hq * sizeof(uint32_t), s);
   if (e != cudaSuccess) return map_cuda(e);
-  const PagedSplit sp = {reinterpret_cast<float *>(ws), ws + piece_b};
+  const PagedSplit sp = {reinterpret_cast<float *>(ws), reinterpret_cast<uint32_t *>(ws + piece_b)};
   e = chunk ? launch_paged_chunk(tk, tv, a, sp, shape, grid, box_rows, s)
             : launch_paged_token(tk, tv, a, sp, shape, grid, s);
   if (e == cudaSuccess) e = launch_paged_finish(a, sp, shape, grid, ds->num_sms, s);

@@ -28,136 +28,112 @@ template <int FORMAT>
 __global__ void __launch_bounds__(kExactThreads) paged_exact_kernel(const PagedReadArgs a) {
   __shared__ ExactShared sh;
   const int row = blockIdx.x, hq = blockIdx.y;
-  // the sequence that owns the row: the last s with q_off[s] <= row (empty sequences in between own none)
-  int lo = 0, hi = a.S;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (__ldg(a.q_off + mid) <= row) lo = mid; else hi = mid;
-  }
-  const SeqInfo si = paged_seq(a, lo);
+  const int s = paged_owner(a, row);
+  const SeqInfo si = paged_seq(a, s);
   const int t = row - si.q0;
   if (t < 0 || t >= si.n) return;  // a row no sequence owns
-  paged_exact_row<FORMAT>(a, lo, si, t, hq, sh);
+  paged_exact_row<FORMAT>(a, s, si, t, hq, sh);
 }
 
 // The rows that the reading kernel left: items cut by the ends of CTAs'
-// stretches are joined from their pieces, in the line's order, and rows whose
-// result the ranges could have spoilt are recomputed.  Blocks take RB rows.
-constexpr int kMaxSplitCtas = 1024;
-
-template <int FORMAT>
+// stretches are joined from their pieces, in the line's order, a warp per row
+// (its lanes side by side over the channels); rows whose result the ranges
+// could have spoilt are then recomputed by the whole block.  A warp looks after
+// RW rows.
+template <int FORMAT, int D>
 __global__ void __launch_bounds__(kExactThreads)
-    paged_finish_kernel(const PagedReadArgs a, const PagedSplit sp, const SplitShape shape, int grid, int RB) {
+    paged_finish_kernel(const PagedReadArgs a, const PagedSplit sp, int row_tile, int grid, int RW) {
+  constexpr int E = D / 32;  // channels per lane
   __shared__ ExactShared sh;
-  __shared__ SplitScan<kExactThreads> scan;
-  __shared__ float s_w[kMaxSplitCtas];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, d = a.c.d;
-  const long long rows = static_cast<long long>(a.N) * a.Hq, first = static_cast<long long>(blockIdx.x) * RB;
+  __shared__ long long s_list[kExactThreads];
+  __shared__ int s_count;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const long long rows = static_cast<long long>(a.N) * a.Hq;
+  const long long first = (static_cast<long long>(blockIdx.x) * (kExactThreads / 32) + warp) * RW;
+  if (tid == 0) s_count = 0;
+  __syncthreads();
   grid_dep_wait();
-  unsigned mask = 0;
-  if (RB == 1) {
-    mask = sp.todo[first] == kRowDone ? 0u : 1u;
-  } else {
-    mask = __ballot_sync(0xffffffffu, lane < RB && first + lane < rows && sp.todo[first + lane] != kRowDone);
-  }
-  long long W = -1;
-  int s_of = -1;  // the sequence that prefix belongs to
-  long long prefix = 0;
-  for (; mask; mask &= mask - 1) {
-    const long long orow = first + __ffs(mask) - 1;
-    const int row = static_cast<int>(orow / a.Hq), hq = static_cast<int>(orow - static_cast<long long>(row) * a.Hq);
-    int lo = 0, hi = a.S;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (__ldg(a.q_off + mid) <= row) lo = mid; else hi = mid;
-    }
-    const SeqInfo si = paged_seq(a, lo);
-    const int t = row - si.q0;
-    if (t < 0 || t >= si.n) continue;  // nobody's row: its mark was never written
-    bool exact = sp.todo[orow] == kRowExact;
+  const uint32_t mine = lane < RW && first + lane < rows ? sp.todo[first + lane] : 0u;
+  const size_t size = piece_floats(row_tile, D);
+  for (unsigned mask = __ballot_sync(0xffffffffu, mine != 0u); mask; mask &= mask - 1) {
+    const int at = __ffs(mask) - 1;
+    const uint32_t word = __shfl_sync(0xffffffffu, mine, at);
+    const long long orow = first + at;
+    bool exact = word == kRowExact;
     if (!exact) {
-      if (W < 0) W = split_total(a, shape, scan);
-      // the row's place: packed rows, or row tiles of whole tokens
-      const int G = split_ctas(W, grid, shape), h = hq / a.group, gr = hq % a.group;
-      const int tile = shape.tok ? t / shape.tok : (t * a.group + gr) / shape.row_tile;
-      const int rr = shape.tok ? (t - tile * shape.tok) * a.group + gr : (t * a.group + gr) % shape.row_tile;
-      const int kt = row_key_tiles(si, tile, a.causal, shape);
-      if (s_of != lo) {
-        // tiles before sequence lo
-        long long w = 0;
-        for (int s = tid; s < lo; s += kExactThreads) w += seq_tiles(a, paged_seq(a, s), shape);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
-        __syncthreads();
-        if (lane == 0) scan.warp[warp] = w;
-        __syncthreads();
-        prefix = 0;
-#pragma unroll
-        for (int i = 0; i < kExactThreads / 32; ++i) prefix += scan.warp[i];
-        s_of = lo;
-      }
-      const long long x = prefix + h * head_key_tiles(si, seq_row_tiles(si, a.group, shape), a.group, a.causal, shape) +
-                          head_key_tiles(si, tile, a.group, a.causal, shape);
-      const int g0 = split_owner(W, G, x), g1 = split_owner(W, G, x + kt - 1), n = g1 - g0 + 1;
-      const size_t size = piece_floats(shape.row_tile, d);
-      const float *p0 = sp.pieces + (static_cast<size_t>(g0) * 2 + 1) * size;  // then every other slot 0
-      auto piece = [&](int i) { return i == 0 ? p0 : sp.pieces + static_cast<size_t>(g0 + i) * 2 * size; };
-      const float *stat = nullptr;
+      const int rr = (word >> 2) & 255, g0 = (word >> 10) & 1023, n = static_cast<int>(word >> 20);
+      // a word that a reading kernel which gave up left unwritten
+      if ((word & 3u) != kRowSplit || rr >= row_tile || n < 1 || g0 + n > grid) continue;
+      const int hq = static_cast<int>(orow % a.Hq), h = hq / a.group;
+      const float *base = sp.pieces + static_cast<size_t>(g0) * 2 * size;  // piece 0 in slot 1, the others in slot 0
+      auto piece = [&](int i) { return base + (static_cast<size_t>(i) * 2 + (i == 0 ? 1 : 0)) * size; };
       float M = -INFINITY;
-      for (int i = tid; i < n; i += kExactThreads) {
-        stat = piece(i) + static_cast<size_t>(shape.row_tile) * d + 2 * rr;
-        M = fmaxf(M, stat[0]);
-      }
+      for (int i = lane; i < n; i += 32) M = fmaxf(M, piece(i)[row_tile * D + 2 * rr]);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-      __syncthreads();
-      if (lane == 0) sh.red[0][warp] = M;
-      __syncthreads();
-      M = fmaxf(fmaxf(sh.red[0][0], sh.red[0][1]), fmaxf(sh.red[0][2], sh.red[0][3]));
-      float L = 0.f, wide = 0.f;
-      for (int i = tid; i < n; i += kExactThreads) {
-        stat = piece(i) + static_cast<size_t>(shape.row_tile) * d + 2 * rr;
-        const float m = stat[0], l = stat[1];
-        const float w = m == -INFINITY ? (l != l ? 1.f : 0.f) : ex2_approx(m - M);  // NaN scores have no maximum
-        s_w[i] = w;
-        L += w * l;
-        wide += piece(i)[static_cast<size_t>(shape.row_tile) * d + 2 * shape.row_tile + d];
+      float acc[E], L = 0.f, wide = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = 0.f;
+      for (int i0 = 0; i0 < n; i0 += 32) {
+        float w = 0.f;
+        if (i0 + lane < n) {
+          const float *p = piece(i0 + lane);
+          const float m = p[row_tile * D + 2 * rr], l = p[row_tile * D + 2 * rr + 1];
+          w = m == -INFINITY ? (l != l ? 1.f : 0.f) : ex2_approx(m - M);  // NaN scores have no maximum
+          L += w * l;
+          wide += p[row_tile * D + 2 * row_tile + D];
+        }
+        const int cnt = min(32, n - i0);
+#pragma unroll 8
+        for (int i = 0; i < cnt; ++i) {
+          const float wi = __shfl_sync(0xffffffffu, w, i);
+          const float *p = piece(i0 + i) + static_cast<size_t>(rr) * D + lane * E;
+          if (E == 4) {
+            const float4 v = *reinterpret_cast<const float4 *>(p);
+            acc[0] = fmaf(wi, v.x, acc[0]);
+            acc[1] = fmaf(wi, v.y, acc[1]);
+            acc[E - 2] = fmaf(wi, v.z, acc[E - 2]);
+            acc[E - 1] = fmaf(wi, v.w, acc[E - 1]);
+          } else {
+            const float2 v = *reinterpret_cast<const float2 *>(p);
+            acc[0] = fmaf(wi, v.x, acc[0]);
+            acc[1] = fmaf(wi, v.y, acc[1]);
+          }
+        }
       }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) {
         L += __shfl_xor_sync(0xffffffffu, L, o);
         wide += __shfl_xor_sync(0xffffffffu, wide, o);
       }
-      __syncthreads();
-      if (lane == 0) {
-        sh.red[0][warp] = L;
-        sh.red[1][warp] = wide;
-      }
-      __syncthreads();
-      L = (sh.red[0][0] + sh.red[0][1]) + (sh.red[0][2] + sh.red[0][3]);
-      wide = (sh.red[1][0] + sh.red[1][1]) + (sh.red[1][2] + sh.red[1][3]);
-      bool ok = true;
-      if (tid < d) {
-        float acc = 0.f;
-        int i = 0;
-        for (; i + 16 <= n; i += 16) {
-          float v[16];
+      const bool empty = M == -INFINITY && L == 0.f;
+      bool good = true;
+      float o[E];
 #pragma unroll
-          for (int u = 0; u < 16; ++u) v[u] = piece(i + u)[static_cast<size_t>(rr) * d + tid];
-#pragma unroll
-          for (int u = 0; u < 16; ++u) acc = fmaf(s_w[i + u], v[u], acc);
-        }
-        for (; i < n; ++i) acc = fmaf(s_w[i], piece(i)[static_cast<size_t>(rr) * d + tid], acc);
-        const float shift = p0[static_cast<size_t>(shape.row_tile) * d + 2 * shape.row_tile + tid];
-        float o = 0.f;
-        if (!(M == -INFINITY && L == 0.f))
-          o = paged_out(a.beta ? a.beta[static_cast<long long>(h) * d + tid] : 0.f, shift, acc / L, wide != 0.f, &ok);
-        static_cast<__nv_bfloat16 *>(a.out)[orow * d + tid] = __float2bfloat16_rn(o);
+      for (int e = 0; e < E; ++e) {
+        bool ok = true;
+        const int j = lane * E + e;
+        o[e] = paged_out(a.beta ? a.beta[static_cast<long long>(h) * D + j] : 0.f,
+                         piece(0)[row_tile * D + 2 * row_tile + j], acc[e] / L, wide != 0.f, &ok);
+        if (empty) o[e] = 0.f;
+        good = good && (ok || empty);
       }
-      if (tid == 0 && a.lse != nullptr) a.lse[orow] = M == -INFINITY && L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
-      exact = !__syncthreads_and(ok);
+      __nv_bfloat162 *dst = reinterpret_cast<__nv_bfloat162 *>(static_cast<__nv_bfloat16 *>(a.out) + orow * D + lane * E);
+#pragma unroll
+      for (int e = 0; e < E; e += 2) dst[e / 2] = __floats2bfloat162_rn(o[e], o[e + 1]);
+      if (lane == 0 && a.lse != nullptr) a.lse[orow] = empty ? -INFINITY : (M + log2f(L)) * kLn2;
+      exact = !__all_sync(0xffffffffu, good);
     }
-    if (exact) paged_exact_row<FORMAT>(a, lo, si, t, hq, sh);
+    if (exact && lane == 0) s_list[atomicAdd(&s_count, 1)] = orow;
+  }
+  __syncthreads();
+  for (int i = 0; i < s_count; ++i) {
+    const long long orow = s_list[i];
+    const int row = static_cast<int>(orow / a.Hq), hq = static_cast<int>(orow - static_cast<long long>(row) * a.Hq);
+    const int s = paged_owner(a, row);
+    const SeqInfo si = paged_seq(a, s);
+    const int t = row - si.q0;
+    if (t >= 0 && t < si.n) paged_exact_row<FORMAT>(a, s, si, t, hq, sh);
   }
 }
 
@@ -165,16 +141,17 @@ __global__ void __launch_bounds__(kExactThreads)
 
 cudaError_t launch_paged_finish(const PagedReadArgs &a, const PagedSplit &sp, const SplitShape &shape, int grid,
                                 int num_sms, cudaStream_t stream) {
-  if (grid > kMaxSplitCtas) return cudaErrorInvalidValue;
+  if (grid > kMaxSplitCtas || shape.row_tile > 256) return cudaErrorInvalidValue;
   const long long rows = static_cast<long long>(a.N) * a.Hq;
-  // a block per row while that is a few waves; then 32 rows, most of which need nothing
-  const int RB = rows <= 32ll * num_sms ? 1 : 32;
-  const dim3 blocks(static_cast<unsigned>((rows + RB - 1) / RB));
+  // a row per warp while that is at most about one wave of blocks; then 8, most of which need nothing
+  const int warps = kExactThreads / 32, RW = rows <= 16ll * warps * num_sms ? 1 : 8;
+  const dim3 blocks(static_cast<unsigned>((rows + RW * warps - 1) / (RW * warps)));
+  auto go = [&](auto kernel) {
+    return launch_kernel(kernel, blocks, dim3(kExactThreads), 0, stream, true, a, sp, shape.row_tile, grid, RW);
+  };
   if (a.c.format == kCacheBf16)
-    return launch_kernel(paged_finish_kernel<kCacheBf16>, blocks, dim3(kExactThreads), 0, stream, true, a, sp, shape, grid,
-                         RB);
-  return launch_kernel(paged_finish_kernel<kCacheE4m3>, blocks, dim3(kExactThreads), 0, stream, true, a, sp, shape, grid,
-                       RB);
+    return a.c.d == 64 ? go(paged_finish_kernel<kCacheBf16, 64>) : go(paged_finish_kernel<kCacheBf16, 128>);
+  return a.c.d == 64 ? go(paged_finish_kernel<kCacheE4m3, 64>) : go(paged_finish_kernel<kCacheE4m3, 128>);
 }
 
 cudaError_t launch_paged_exact(const PagedReadArgs &a, cudaStream_t stream) {

@@ -59,6 +59,16 @@ __device__ __forceinline__ SeqInfo paged_seq(const PagedReadArgs &a, int s) {
   return r;
 }
 
+// The sequence that owns a query row, if any does: the last s with q_off[s] <= row.
+__device__ __forceinline__ int paged_owner(const PagedReadArgs &a, int row) {
+  int lo = 0, hi = a.S;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (__ldg(a.q_off + mid) <= row) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
 // Keys that row t (of n) of a sequence sees: positions 0 .. limit - 1.
 __device__ __forceinline__ int paged_limit(const SeqInfo &si, int t, int causal) {
   return causal ? max(si.ctx - si.n + t + 1, 0) : si.ctx;

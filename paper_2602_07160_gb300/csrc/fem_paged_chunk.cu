@@ -135,6 +135,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
 
   grid_dep_launch_dependents();
+  if (blockIdx.x == 0) split_mark_unowned<kChunkThreads>(a, sp.todo);
   const long long W = split_total(a, shape, scan);
   if (W == 0) return;
   const int G = split_ctas(W, gridDim.x, shape), cta = blockIdx.x;
@@ -612,7 +613,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             piece[256 * D + 2 * ir] = m;
             piece[256 * D + 2 * ir + 1] = L;
           }
-          sp.todo[orow] = whole ? (good ? kRowDone : kRowExact) : kRowSplit;
+          if (whole) sp.todo[orow] = good ? kRowDone : kRowExact;
+          else if (sg.kt0 == 0) sp.todo[orow] = row_split(ir, cta, split_owner(W, G, sg.x_end - 1) - cta + 1);
         }
         if (!whole && t == 0) {
           if (r < D) piece[256 * D + 512 + r] = shift[r];

@@ -133,11 +133,21 @@ __device__ __forceinline__ long long seq_tiles(const PagedReadArgs &a, const Seq
   return a.c.H * head_key_tiles(si, seq_row_tiles(si, a.group, sh), a.group, a.causal, sh);
 }
 
+// Rows no sequence owns need nothing (rows from the first offset to the last are owned).
+template <int THREADS>
+__device__ __forceinline__ void split_mark_unowned(const PagedReadArgs &a, uint32_t *todo) {
+  const int first = min(max(__ldg(a.q_off), 0), a.N), last = min(max(__ldg(a.q_off + a.S), first), a.N);
+  for (long long i = threadIdx.x; i < static_cast<long long>(first) * a.Hq; i += THREADS) todo[i] = 0;
+  for (long long i = static_cast<long long>(last) * a.Hq + threadIdx.x; i < static_cast<long long>(a.N) * a.Hq; i += THREADS)
+    todo[i] = 0;
+}
+
 // An item and the key tiles kt0 .. kt1 - 1 of it (kt_all in the whole item).
 struct SplitSeg {
   SeqInfo si;
   int s, h, r;  // sequence, head, row tile
   int kt0, kt1, kt_all;
+  long long x_end;  // the line's tile after the item's last
 };
 
 // Walks a CTA's stretch, item by item.
@@ -167,6 +177,7 @@ struct SplitWalk {
       g.kt_all = row_key_tiles(g.si, lo, a.causal, sh);
       g.kt0 = static_cast<int>(in - head_key_tiles(g.si, lo, a.group, a.causal, sh));
       g.kt1 = static_cast<int>(min(static_cast<long long>(g.kt_all), g.kt0 + (x1 - x)));
+      g.x_end = x + (g.kt_all - g.kt0);
       x += g.kt1 - g.kt0;
       local += g.kt1 - g.kt0;
       return true;
@@ -254,12 +265,17 @@ __host__ __device__ constexpr size_t piece_floats(int rows, int D) {
   return static_cast<size_t>(rows) * D + 2 * rows + D + 4;
 }
 
-// Per output row, what is left to do after the reading kernel.
-enum : uint8_t { kRowDone = 0, kRowExact = 1, kRowSplit = 2 };
+// Per output row, what is left to do after the reading kernel, in one word: nothing, the exact
+// path, or a join of the n pieces of CTAs g0 .. g0 + n - 1, row rr of each.
+enum : uint32_t { kRowDone = 0, kRowExact = 1, kRowSplit = 2 };
+constexpr int kMaxSplitCtas = 1023;
+__device__ __forceinline__ uint32_t row_split(int rr, int g0, int n) {
+  return kRowSplit | (static_cast<uint32_t>(rr) << 2) | (static_cast<uint32_t>(g0) << 10) | (static_cast<uint32_t>(n) << 20);
+}
 
 struct PagedSplit {
   float *pieces;  // two slots per CTA
-  uint8_t *todo;  // [N, Hq]
+  uint32_t *todo;  // [N, Hq]
 };
 
 }  // namespace fem

@@ -139,6 +139,7 @@ __global__ void __launch_bounds__(kTokThreads, 2)
     for (int st = 0; st < NS; ++st) mbar_init(bars + 8 * st, 1);
     fence_mbar_init();
   }
+  if (blockIdx.x == 0) split_mark_unowned<kTokThreads>(a, sp.todo);
   const long long W = split_total(a, shape, scan);
   if (W == 0) return;
   const int G = split_ctas(W, gridDim.x, shape), cta = blockIdx.x;
@@ -545,10 +546,10 @@ __global__ void __launch_bounds__(kTokThreads, 2)
       if (tid == 0) piece[kRows * D + 2 * kRows + D] = wide ? 1.f : 0.f;
     }
     __syncthreads();
-    if (tid < n_rows) {
+    if (tid < n_rows && (whole || sg.kt0 == 0)) {
       const int rr = row0 + tid, tok = rr / a.group, hq = sg.h * a.group + rr % a.group;
       sp.todo[(static_cast<long long>(sg.si.q0) + tok) * a.Hq + hq] =
-          whole ? (s_bad[tid] ? kRowExact : kRowDone) : kRowSplit;
+          whole ? (s_bad[tid] ? kRowExact : kRowDone) : row_split(tid, cta, split_owner(W, G, sg.x_end - 1) - cta + 1);
     }
   }
 }
