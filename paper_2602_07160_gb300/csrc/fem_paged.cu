@@ -67,6 +67,32 @@ __global__ void __launch_bounds__(kExactThreads)
       const int hq = static_cast<int>(orow % a.Hq), h = hq / a.group;
       const float *base = sp.pieces + static_cast<size_t>(g0) * 2 * size;  // piece 0 in slot 1, the others in slot 0
       auto piece = [&](int i) { return base + (static_cast<size_t>(i) * 2 + (i == 0 ? 1 : 0)) * size; };
+      // the first pieces' accumulators are on their way while the weights are formed
+      constexpr int kAhead = 4;
+      float v[kAhead][E];
+      auto load = [&](int i, float (&x)[E]) {
+        const float *p = piece(i) + static_cast<size_t>(rr) * D + lane * E;
+        if (E == 4) {
+          const float4 y = *reinterpret_cast<const float4 *>(p);
+          x[0] = y.x;
+          x[1] = y.y;
+          x[E - 2] = y.z;
+          x[E - 1] = y.w;
+        } else {
+          const float2 y = *reinterpret_cast<const float2 *>(p);
+          x[0] = y.x;
+          x[1] = y.y;
+        }
+      };
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        if (i < n) load(i, v[i]);
+      float beta[E], kind[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        beta[e] = a.beta ? __ldg(a.beta + static_cast<long long>(h) * D + lane * E + e) : 0.f;
+        kind[e] = piece(0)[row_tile * D + 2 * row_tile + lane * E + e];
+      }
       float M = -INFINITY;
       for (int i = lane; i < n; i += 32) M = fmaxf(M, piece(i)[row_tile * D + 2 * rr]);
 #pragma unroll
@@ -84,21 +110,23 @@ __global__ void __launch_bounds__(kExactThreads)
           wide += p[row_tile * D + 2 * row_tile + D];
         }
         const int cnt = min(32, n - i0);
-#pragma unroll 8
-        for (int i = 0; i < cnt; ++i) {
-          const float wi = __shfl_sync(0xffffffffu, w, i);
-          const float *p = piece(i0 + i) + static_cast<size_t>(rr) * D + lane * E;
-          if (E == 4) {
-            const float4 v = *reinterpret_cast<const float4 *>(p);
-            acc[0] = fmaf(wi, v.x, acc[0]);
-            acc[1] = fmaf(wi, v.y, acc[1]);
-            acc[E - 2] = fmaf(wi, v.z, acc[E - 2]);
-            acc[E - 1] = fmaf(wi, v.w, acc[E - 1]);
-          } else {
-            const float2 v = *reinterpret_cast<const float2 *>(p);
-            acc[0] = fmaf(wi, v.x, acc[0]);
-            acc[1] = fmaf(wi, v.y, acc[1]);
+        if (i0 == 0) {
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) {
+            const float wi = __shfl_sync(0xffffffffu, w, i);
+            if (i < n) {
+#pragma unroll
+              for (int e = 0; e < E; ++e) acc[e] = fmaf(wi, v[i][e], acc[e]);
+            }
           }
+        }
+#pragma unroll 8
+        for (int i = i0 == 0 ? kAhead : 0; i < cnt; ++i) {
+          const float wi = __shfl_sync(0xffffffffu, w, i);
+          float x[E];
+          load(i0 + i, x);
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[e] = fmaf(wi, x[e], acc[e]);
         }
       }
 #pragma unroll
@@ -111,10 +139,8 @@ __global__ void __launch_bounds__(kExactThreads)
       float o[E];
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        bool ok = true;
-        const int j = lane * E + e;
-        o[e] = paged_out(a.beta ? a.beta[static_cast<long long>(h) * D + j] : 0.f,
-                         piece(0)[row_tile * D + 2 * row_tile + j], acc[e] / L, wide != 0.f, &ok);
+        bool ok;
+        o[e] = paged_out(out_coef(beta[e], kind[e], a.beta && wide != 0.f), acc[e] / L, &ok);
         if (empty) o[e] = 0.f;
         good = good && (ok || empty);
       }

@@ -17,7 +17,7 @@
 //                output or piece at its end
 //   warps 8-11   the same for row tile 1
 //   warp 12      TMA of K and V, one box per page (or part of a page) of the tile
-//   warp 13      issues the products, one thread: S0 = Q0 K^T, S1 = Q1 K^T, then for
+//   warp 13      issues the products: S0 = Q0 K^T, S1 = Q1 K^T, then for
 //                each tile, once its P is written, O += P E and the next S.  The
 //                tensor pipe takes them in the order issued, so S of the next key
 //                tile may overwrite a P whose product was issued before it, and
@@ -95,6 +95,13 @@ __device__ __forceinline__ bool chunk_wait(uint32_t bar, uint32_t parity, unsign
       return false;
     }
   }
+}
+
+// True in one thread of the warp, always the same one.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -179,9 +186,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(smem + Lay::kTmem);
   SplitSeg sg;
 
-  // The block's registers are 512 x 128; the softmax warps take 184 each, the bank's 104, the others 40:
-  // 256 x 184 + 128 x 104 + 128 x 40 = 512 x 128.
-  if (warp >= 12) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+  // The block's registers are 512 x 128; the softmax warps take 168 each, the bank's 104, the others 72:
+  // 256 x 168 + 128 x 104 + 128 x 72 = 512 x 128.
+  if (warp >= 12) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
   if (warp == 12) {
     // ------------------------------------------------------------ TMA of K and V
     const int boxes = kChunkKeys / box_rows;
@@ -240,60 +247,69 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     }
   } else if (warp == 13) {
     // ------------------------------------------------------------ products
-    if (lane == 0) {
-      constexpr uint32_t idesc_s = idesc_f16(128, 128, true, false);
-      constexpr uint32_t idesc_o = idesc_f16(128, D, true, true);
-      unsigned n = 0, np[2] = {0, 0}, seg = 0;  // key tiles, P of each row tile, segments so far
-      bool ok = true;
-      auto issue_s = [&](int t, int st) {
-        const uint32_t sK = sbase + Lay::kK + st * Lay::kTile, sQ = sbase + Lay::kQ + t * Lay::kTile;
-#pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          const uint32_t off = (kk >> 2) * 16384 + (kk & 3) * 32;
-          mma_f16_ss(tmem + t * 128, smem_desc_sw128(sQ + off, 16, 1024), smem_desc_sw128(sK + off, 16, 1024), idesc_s,
-                     kk > 0 ? 1u : 0u);
+    // The whole warp walks the loop and one elected thread issues: the loop then stays uniform, and the
+    // operands' descriptors are sums of per-tile bases and constants in uniform registers.  With one
+    // thread in the loop alone its address arithmetic, between the other warps' instructions, took 6000
+    // cycles a key tile, and the tensor pipe was idle for three quarters of them.
+    constexpr uint32_t idesc_s = idesc_f16(128, 128, true, false);
+    constexpr uint32_t idesc_o = idesc_f16(128, D, true, true);
+    const uint64_t desc_q = smem_desc_sw128(sbase + Lay::kQ, 16, 1024), desc_k = smem_desc_sw128(sbase + Lay::kK, 16, 1024);
+    const uint64_t desc_e = smem_desc_sw128(sbase + Lay::kE, 16384, 1024);
+    const bool leader = elect_one();
+    unsigned n = 0, np0 = 0, np1 = 0, seg = 0;  // key tiles, P of each row tile, segments so far
+    bool ok = true;
+    auto wait = [&](int bar, unsigned parity, unsigned code) {
+      return __all_sync(0xffffffffu, chunk_wait(FEM_CB(bar), parity & 1, a.err, code, abort_flag)) != 0;
+    };
+    while (ok && walk.next(a, shape, sg)) {
+      const int tiles = chunk_rows(sg, a.group, shape).tiles, nk = sg.kt1 - sg.kt0;
+      // both row tiles' warps arrive whether their tile is in use or not: the phases stay together
+      ok = wait(kCbQ, seg, kErrWaitMma) && wait(kCbQ + 1, seg, kErrWaitMma);
+      for (int k = 0; ok && k <= nk; ++k) {
+        const unsigned i = n + k, e = i - 1;  // this key tile, and the one whose bank is used
+        if (k < nk) {
+          if (!(ok = wait(kCbKFull + (i & 1), i >> 1, kErrWaitTma))) break;
         }
-        mma_commit(FEM_CB(kCbS + t));
-      };
-      while (ok && walk.next(a, shape, sg)) {
-        const int tiles = chunk_rows(sg, a.group, shape).tiles, nk = sg.kt1 - sg.kt0;
-        for (int t = 0; t < tiles; ++t)
-          ok = ok && chunk_wait(FEM_CB(kCbQ + t), seg & 1, a.err, kErrWaitMma, abort_flag);
-        // a row tile out of use keeps its barrier's phase with the others': its warps arrive all the same
-        if (tiles == 1) ok = ok && chunk_wait(FEM_CB(kCbQ + 1), seg & 1, a.err, kErrWaitMma, abort_flag);
-        for (int k = 0; ok && k <= nk; ++k) {
-          const unsigned i = n + k;  // this key tile
-          if (k < nk) {
-            ok = chunk_wait(FEM_CB(kCbKFull + (i & 1)), (i >> 1) & 1, a.err, kErrWaitTma, abort_flag);
-            if (!ok) break;
+        if (k > 0) {
+          if (!(ok = wait(kCbEFull + (e & 1), e >> 1, kErrWaitMma))) break;
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (t >= tiles) break;
+          if (k > 0) {
+            // O_t += P_t E of key tile e
+            if (!(ok = wait(kCbP + t, t ? np1 : np0, kErrWaitMma))) break;
+            if (t) ++np1; else ++np0;
             tc_fence_after_sync();
-          }
-          for (int t = 0; t < tiles; ++t) {
-            if (k > 0) {
-              // O_t += P_t E of key tile i - 1
-              const unsigned e = i - 1;
-              if (t == 0) ok = ok && chunk_wait(FEM_CB(kCbEFull + (e & 1)), (e >> 1) & 1, a.err, kErrWaitMma, abort_flag);
-              ok = ok && chunk_wait(FEM_CB(kCbP + t), np[t] & 1, a.err, kErrWaitMma, abort_flag);
-              if (!ok) break;
-              ++np[t];
-              tc_fence_after_sync();
-              const uint32_t sE = sbase + Lay::kE + (e & 1) * Lay::kTile;
+            const uint64_t de = desc_e + (e & 1) * (Lay::kTile >> 4);
+            if (leader) {
 #pragma unroll
               for (int kk = 0; kk < 8; ++kk)
-                mma_f16_ts(tmem + 256 + t * D, tmem + t * 128 + kk * 8, smem_desc_sw128(sE + kk * 2048, 16384, 1024),
-                           idesc_o, (k > 1 || kk > 0) ? 1u : 0u);
+                mma_f16_ts(tmem + 256 + t * D, tmem + t * 128 + kk * 8, de + ((kk * 2048) >> 4), idesc_o,
+                           (k > 1 || kk > 0) ? 1u : 0u);
               if (t == tiles - 1) mma_commit(FEM_CB(kCbEEmpty + (e & 1)));
             }
-            if (k < nk) {
-              issue_s(t, i & 1);
+          }
+          if (k < nk) {
+            tc_fence_after_sync();
+            const uint64_t dq = desc_q + t * (Lay::kTile >> 4), dk = desc_k + (i & 1) * (Lay::kTile >> 4);
+            if (leader) {
+#pragma unroll
+              for (int kk = 0; kk < D / 16; ++kk) {
+                const uint32_t off = ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
+                mma_f16_ss(tmem + t * 128, dq + off, dk + off, idesc_s, kk > 0 ? 1u : 0u);
+              }
+              mma_commit(FEM_CB(kCbS + t));
               if (t == tiles - 1) mma_commit(FEM_CB(kCbKEmpty + (i & 1)));
             }
           }
         }
-        if (ok) mma_commit(FEM_CB(kCbO));
-        n += nk;
-        ++seg;
       }
+      if (ok && leader) mma_commit(FEM_CB(kCbO));
+      n += nk;
+      ++seg;
+    }
+    if (leader) {
       mma_commit(FEM_CB(kCbDone));
       // nothing may be in flight when TMEM is freed
       mbar_wait(FEM_CB(kCbDone), 0, a.err, kErrWaitMma);
@@ -305,7 +321,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     constexpr int kChunks = D / 8;          // per row: 16 at D = 128, 8 at D = 64 (then two row groups)
     const int col = cc % kChunks, r_first = rl + 8 * (cc / kChunks);
     constexpr int kRowStep = 8 * (16 / kChunks), kRowsEach = 128 / kRowStep;
-    BankCoef co[8];
+    constexpr int kBatch = 4;
+    // the thread's 8 codes of a row in a staging tile
+    auto raw_offset = [&](int r) {
+      return D == 128 ? sw128_offset(r, col >> 1) + 8 * (col & 1) : r * 64 + (((col >> 1) ^ ((r >> 1) & 3)) << 4) + 8 * (col & 1);
+    };
+    float2 cb[4], cs[4], ci[4], cd[4];  // the thread's channels, in pairs
     int last_s = -1, last_h = -1;
     unsigned n = 0, seg = 0;
     bool ok = true;
@@ -354,8 +375,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           }
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          co[e] = bank_coef(__ldg(a.beta + static_cast<long long>(sg.h) * D + col * 8 + e), vmax[e], vabs[e]);
+        for (int e = 0; e < 8; e += 2) {
+          const float *bp = a.beta + static_cast<long long>(sg.h) * D + col * 8 + e;
+          const BankCoef x = bank_coef(__ldg(bp), vmax[e], vabs[e]), y = bank_coef(__ldg(bp + 1), vmax[e + 1], vabs[e + 1]);
+          cb[e / 2] = make_float2(x.b, y.b);
+          cs[e / 2] = make_float2(x.s, y.s);
+          ci[e / 2] = make_float2(x.ic, y.ic);
+          cd[e / 2] = make_float2(x.d, y.d);
+        }
       }
       float emax = 0.f;
       bool wrote = false;  // this segment's shifts, once its first stage is free
@@ -379,21 +406,26 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         if (kCodes) {
           uint8_t *tK = smem + Lay::kK + st * Lay::kTile;
           const uint8_t *raw = smem + Lay::kRawK;
-#pragma unroll 4
-          for (int i = 0; i < kRowsEach; ++i) {
-            const int r = r_first + kRowStep * i;
-            uint4 y = make_uint4(0, 0, 0, 0);
-            if (!gone(r)) {
-              const uint32_t off = D == 128 ? sw128_offset(r, col >> 1) + 8 * (col & 1)
-                                            : r * 64 + (((col >> 1) ^ ((r >> 1) & 3)) << 4) + 8 * (col & 1);
-              const uint2 w = *reinterpret_cast<const uint2 *>(raw + off);
-              const float sc = paged_scale(smem[Lay::kScaleK + r]);
-              const float2 f0 = e4m3x2_to_float2(w.x & 0xffffu), f1 = e4m3x2_to_float2(w.x >> 16);
-              const float2 f2 = e4m3x2_to_float2(w.y & 0xffffu), f3 = e4m3x2_to_float2(w.y >> 16);
-              y = make_uint4(pack_bf16(f0.x * sc, f0.y * sc), pack_bf16(f1.x * sc, f1.y * sc),
-                             pack_bf16(f2.x * sc, f2.y * sc), pack_bf16(f3.x * sc, f3.y * sc));
+#pragma unroll 1
+          for (int i0 = 0; i0 < kRowsEach; i0 += kBatch) {
+            uint2 w[kBatch];
+            float sc[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+              const int r = r_first + kRowStep * (i0 + u);
+              w[u] = *reinterpret_cast<const uint2 *>(raw + raw_offset(r));
+              sc[u] = paged_scale(smem[Lay::kScaleK + r]);
             }
-            *reinterpret_cast<uint4 *>(tK + (col >> 3) * 16384 + sw128_offset(r, col & 7)) = y;
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+              const int r = r_first + kRowStep * (i0 + u);
+              const float2 s2 = make_float2(sc[u], sc[u]);
+              const float2 f0 = __fmul2_rn(e4m3x2_to_float2(w[u].x & 0xffffu), s2), f1 = __fmul2_rn(e4m3x2_to_float2(w[u].x >> 16), s2);
+              const float2 f2 = __fmul2_rn(e4m3x2_to_float2(w[u].y & 0xffffu), s2), f3 = __fmul2_rn(e4m3x2_to_float2(w[u].y >> 16), s2);
+              uint4 y = make_uint4(pack_bf16(f0.x, f0.y), pack_bf16(f1.x, f1.y), pack_bf16(f2.x, f2.y), pack_bf16(f3.x, f3.y));
+              if (ragged && gone(r)) y = make_uint4(0, 0, 0, 0);
+              *reinterpret_cast<uint4 *>(tK + (col >> 3) * 16384 + sw128_offset(r, col & 7)) = y;
+            }
           }
           fence_proxy_async_smem();
           mbar_arrive(FEM_CB(kCbKFull + st));
@@ -408,47 +440,47 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           if (rl == 0 && cc < kChunks) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              s_shift[(seg % kSegRing) * D + col * 8 + e] = BETA && co[e].theta == 0.f ? co[e].s : __int_as_float(0x7fffffff);
+              s_shift[(seg % kSegRing) * D + col * 8 + e] =
+                  BETA ? bank_kind(e & 1 ? BankCoef{cb[e / 2].y, cs[e / 2].y, ci[e / 2].y, cd[e / 2].y}
+                                         : BankCoef{cb[e / 2].x, cs[e / 2].x, ci[e / 2].x, cd[e / 2].x})
+                       : INFINITY;
           }
         }
         if (BETA || kCodes || ragged) {
-#pragma unroll 4
-          for (int i = 0; i < kRowsEach; ++i) {
-            const int r = r_first + kRowStep * i;
-            uint4 *at = reinterpret_cast<uint4 *>(tE + (col >> 3) * 16384 + sw128_offset(r, col & 7));
-            uint4 y = make_uint4(0, 0, 0, 0);
-            if (!(ragged && gone(r))) {
-              float v[8];
+          // rows in batches: their loads leave together (a store to the tile would hold the next row's back)
+#pragma unroll 1
+          for (int i0 = 0; i0 < kRowsEach; i0 += kBatch) {
+            uint4 w[kBatch];
+            float sc[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+              const int r = r_first + kRowStep * (i0 + u);
               if (kCodes) {
-                const uint32_t off = D == 128 ? sw128_offset(r, col >> 1) + 8 * (col & 1)
-                                              : r * 64 + (((col >> 1) ^ ((r >> 1) & 3)) << 4) + 8 * (col & 1);
-                const uint2 w = *reinterpret_cast<const uint2 *>(smem + Lay::kRawV + off);
-                const float sc = paged_scale(smem[Lay::kScaleV + r]);
-                const uint32_t x[4] = {w.x & 0xffffu, w.x >> 16, w.y & 0xffffu, w.y >> 16};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const float2 f = e4m3x2_to_float2(x[e]);
-                  v[2 * e] = f.x * sc;
-                  v[2 * e + 1] = f.y * sc;
-                }
+                const uint2 x = *reinterpret_cast<const uint2 *>(smem + Lay::kRawV + raw_offset(r));
+                w[u] = make_uint4(x.x & 0xffffu, x.x >> 16, x.y & 0xffffu, x.y >> 16);
+                sc[u] = paged_scale(smem[Lay::kScaleV + r]);
               } else {
-                const uint4 w = *at;
-                const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  v[2 * e] = bf16_lo(x[e]);
-                  v[2 * e + 1] = bf16_hi(x[e]);
-                }
+                w[u] = *reinterpret_cast<const uint4 *>(tE + (col >> 3) * 16384 + sw128_offset(r, col & 7));
               }
-              if (BETA) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = bank_value(co[e], v[e]);
-                emax = fmax3(emax, fmax3(v[0], v[1], v[2]), fmax3(v[3], v[4], v[5]));
-                emax = fmax3(emax, v[6], v[7]);
-              }
-              y = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
             }
-            *at = y;
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+              const int r = r_first + kRowStep * (i0 + u);
+              const uint32_t x[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
+              uint32_t y[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                float2 v = kCodes ? __fmul2_rn(e4m3x2_to_float2(x[e]), make_float2(sc[u], sc[u]))
+                                  : make_float2(bf16_lo(x[e]), bf16_hi(x[e]));
+                if (BETA) {
+                  v = bank_pair(cb[e], cs[e], ci[e], cd[e], v);
+                  emax = fmaxf(fmaxf(emax, fabsf(v.x)), fabsf(v.y));
+                }
+                y[e] = pack_bf16(v.x, v.y);
+              }
+              if (ragged && gone(r)) y[0] = y[1] = y[2] = y[3] = 0;
+              *reinterpret_cast<uint4 *>(tE + (col >> 3) * 16384 + sw128_offset(r, col & 7)) = make_uint4(y[0], y[1], y[2], y[3]);
+            }
           }
           if (BETA && emax > kWideE) s_wide[seg % kSegRing] = static_cast<int>(seg + 1);
         }
@@ -460,30 +492,55 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     }
   } else if (warp < 12) {
     // ------------------------------------------------------------ softmax, queries and output of a row tile
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
     const int t = (warp >> 2) - 1, r = tid & 127;
     const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + t * 128 + lane_off, tO = tmem + 256 + t * D + lane_off;
     const float qk_scale = a.scale * kLog2e;
     unsigned n = 0, ns = 0, seg = 0;
-    bool ok = true;
-    while (ok && walk.next(a, shape, sg)) {
-      const ChunkRows cr = chunk_rows(sg, a.group, shape);
-      const int nk = sg.kt1 - sg.kt0, ir = t * 128 + r;  // row of the item
-      const bool on = ir < cr.rows;
-      const int tok = cr.tok0 + (on ? ir / a.group : 0), hq = sg.h * a.group + (on ? ir % a.group : 0);
-      const long long qrow = static_cast<long long>(sg.si.q0) + tok, orow = qrow * a.Hq + hq;
-      const int lim = on ? min(paged_limit(sg.si, tok, a.causal), sg.si.ctx) : 0;
-      if (t < cr.tiles) {
-        // the last S of the item before is done (its commit was waited for), so Q may be replaced
+    // The thread's row of a segment: whether there is one, its place in the output, the keys it sees.
+    struct Row {
+      bool on;
+      int lim;
+      long long qrow, orow;
+      int hq;
+    };
+    auto row_of = [&](const SplitSeg &g, const ChunkRows &cr) {
+      const int ir = t * 128 + r;
+      Row w;
+      w.on = ir < cr.rows;
+      const int tok = cr.tok0 + (w.on ? ir / a.group : 0);
+      w.hq = g.h * a.group + (w.on ? ir % a.group : 0);
+      w.qrow = static_cast<long long>(g.si.q0) + tok;
+      w.orow = w.qrow * a.Hq + w.hq;
+      w.lim = w.on ? min(paged_limit(g.si, tok, a.causal), g.si.ctx) : 0;
+      return w;
+    };
+    // The row's query into shared memory, and the arrival that lets the segment's products start.
+    auto load_q = [&](const Row &w, bool used) {
+      if (used) {
         uint8_t *tQ = smem + Lay::kQ + t * Lay::kTile;
-        const uint4 *qp = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.q) + qrow * a.q_sn + hq * a.q_sh);
-#pragma unroll 8
-        for (int c = 0; c < D / 8; ++c)
-          *reinterpret_cast<uint4 *>(tQ + (c >> 3) * 16384 + sw128_offset(r, c & 7)) = on ? __ldg(qp + c) : make_uint4(0, 0, 0, 0);
+        const uint4 *qp = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.q) + w.qrow * a.q_sn + w.hq * a.q_sh);
+        uint4 x[D / 8];
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) x[c] = w.on ? __ldg(qp + c) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) *reinterpret_cast<uint4 *>(tQ + (c >> 3) * 16384 + sw128_offset(r, c & 7)) = x[c];
         fence_proxy_async_smem();
       }
       mbar_arrive(FEM_CB(kCbQ + t));
+    };
+    bool ok = walk.next(a, shape, sg);
+    ChunkRows cr;
+    Row w;
+    if (ok) {
+      cr = chunk_rows(sg, a.group, shape);
+      w = row_of(sg, cr);
+      load_q(w, t < cr.tiles);
+    }
+    while (ok) {
+      const int nk = sg.kt1 - sg.kt0, ir = t * 128 + r;
+      const int lim = w.lim;
       float m = -INFINITY, L = 0.f;
       if (t < cr.tiles) {
         for (int k = 0; k < nk; ++k, ++ns) {
@@ -558,10 +615,22 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         }
         if (!ok) break;
       }
-      // a row tile out of use waits too: its arrivals stay one segment ahead of the products at most
+      // The next segment's queries, before this one's output: its S then wait for nothing.  The last S
+      // of this row tile is done.  A row tile out of use has seen none, and first waits for the segment's
+      // end, so that its arrivals stay within one segment of the products.
+      SplitSeg sg2;
+      ChunkRows cr2;
+      Row w2;
+      const bool more = walk.next(a, shape, sg2);
+      if (more) {
+        cr2 = chunk_rows(sg2, a.group, shape);
+        w2 = row_of(sg2, cr2);
+        if (t < cr.tiles) load_q(w2, t < cr2.tiles);
+      }
       ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbO), seg & 1, a.err, kErrWaitMma, abort_flag));
       if (!ok) break;
       tc_fence_after_sync();
+      if (more && t >= cr.tiles) load_q(w2, t < cr2.tiles);
       if (t < cr.tiles) {
         // ---- the row's output, or its piece
         const bool whole = sg.kt0 == 0 && sg.kt1 == sg.kt_all;
@@ -576,29 +645,39 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           uint32_t v[32];
           tmem_ld32(tO + c * 32, v);
           tmem_ld_wait();
-          if (!on) continue;
           if (whole) {
+            // lane l has channel 32 c + l's coefficients; every row needs all of them
+            const OutCoef oc = out_coef(BETA ? __ldg(a.beta + static_cast<long long>(sg.h) * D + c * 32 + lane) : 0.f,
+                                        shift[c * 32 + lane], wide);
             uint32_t o[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               float x[2];
 #pragma unroll
               for (int u = 0; u < 2; ++u) {
-                const int j = c * 32 + 2 * i + u;
-                bool fine = true;
                 const float av = __uint_as_float(v[2 * i + u]) * inv_l;
-                x[u] = BETA ? paged_out(__ldg(a.beta + static_cast<long long>(sg.h) * D + j), shift[j], av, wide, &fine)
-                            : av;
-                if (!BETA) fine = fabsf(av) < kMostA;
-                if (empty) x[u] = 0.f;
-                good = good && (fine || empty);
+                if (BETA) {
+                  OutCoef k;
+                  k.g = __shfl_sync(0xffffffffu, oc.g, 2 * i + u);
+                  k.z = __shfl_sync(0xffffffffu, oc.z, 2 * i + u);
+                  k.y = __shfl_sync(0xffffffffu, oc.y, 2 * i + u);
+                  k.w = __shfl_sync(0xffffffffu, oc.w, 2 * i + u);
+                  k.lo = __shfl_sync(0xffffffffu, oc.lo, 2 * i + u);
+                  bool fine;
+                  x[u] = paged_out(k, av, &fine);
+                  good = good && fine;
+                } else {
+                  x[u] = av;
+                  good = good && fabsf(av) < kMostA;
+                }
               }
-              o[i] = pack_bf16(x[0], x[1]);
+              o[i] = empty ? 0u : pack_bf16(x[0], x[1]);
             }
-            uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + orow * D + c * 32);
+            if (!w.on) continue;
+            uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + w.orow * D + c * 32);
 #pragma unroll
             for (int i = 0; i < 4; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-          } else {
+          } else if (w.on) {
             float4 *dst = reinterpret_cast<float4 *>(piece + static_cast<size_t>(ir) * D + c * 32);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -606,24 +685,28 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                                    __uint_as_float(v[4 * i + 3]));
           }
         }
-        if (on) {
+        if (w.on) {
           if (whole) {
-            if (a.lse != nullptr) a.lse[orow] = empty ? -INFINITY : (m + log2f(L)) * kLn2;
+            if (a.lse != nullptr) a.lse[w.orow] = empty ? -INFINITY : (m + log2f(L)) * kLn2;
           } else {
             piece[256 * D + 2 * ir] = m;
             piece[256 * D + 2 * ir + 1] = L;
           }
-          if (whole) sp.todo[orow] = good ? kRowDone : kRowExact;
-          else if (sg.kt0 == 0) sp.todo[orow] = row_split(ir, cta, split_owner(W, G, sg.x_end - 1) - cta + 1);
+          if (whole) sp.todo[w.orow] = good || empty ? kRowDone : kRowExact;
+          else if (sg.kt0 == 0) sp.todo[w.orow] = row_split(ir, cta, split_owner(W, G, sg.x_end - 1) - cta + 1);
         }
         if (!whole && t == 0) {
           if (r < D) piece[256 * D + 512 + r] = shift[r];
           if (r == 0) piece[256 * D + 512 + D] = wide ? 1.f : 0.f;
         }
-        tc_fence_before_sync();  // the next item's products may overwrite O after this thread's next arrival
+        tc_fence_before_sync();  // the next segment's P E overwrite O, after this thread's next P arrives
       }
       n += nk;
       ++seg;
+      if (!more) break;
+      sg = sg2;
+      cr = cr2;
+      w = w2;
     }
   }
 

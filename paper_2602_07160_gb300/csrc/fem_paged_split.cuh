@@ -12,13 +12,16 @@
 //
 // Value bank.  The read mixes the prior weights P = 2^(s - m) against a bank
 // E(v), in bf16 with fp32 sums, a = sum P E / sum P.  Channel j of a sequence
-// and head is read from its first kSampleKeys values v:
-//   linear   (beta max|v| <= 2)  E = expm1(beta v) / beta,  o = log1p(beta a) / beta
-//   shifted  (else)              E = exp(beta (v - max v)), o = max v + log(a) / beta
-// Linear keeps small beta free of cancellation (beta = 0: E = v).  bf16 has
-// fp32's range, so the shift needs no running update: later values may lie far
-// from the sample's, and a result the ranges could have spoilt is seen in a
-// (paged_out) and its row recomputed exactly.
+// and head goes by its first kSampleKeys values v:
+//   tiny     (beta max|v| <= 2^-12)  E = D v,                    o = a / D
+//   linear   (beta max|v| <= 2)      E = expm1(beta v),          o = log1p(a) / beta
+//   shifted  (else)                  E = exp(beta (v - max v)),  o = max v + log(a) / beta
+// Tiny and linear keep small beta free of cancellation: E = v leaves out
+// beta v^2 / 2, at most 2^-9 |v| where it is let through, and expm1 by
+// subtraction is off by 2^-22, 2^-10 of the largest E.  (beta = 0 is tiny.)
+// bf16 has fp32's range, so the shift needs no running update: later values may
+// lie far from the sample's, and a result that could spoil is seen in a or in
+// the largest |E| (paged_out), and its row recomputed exactly.
 #pragma once
 
 #include "fem_paged.cuh"
@@ -26,55 +29,79 @@
 namespace fem {
 
 constexpr int kSampleKeys = 16;
-constexpr float kLinearReach = 2.f;     // beta max|v| up to which a channel is linear
-constexpr float kSmallX = 0.015625f;    // |beta v| under which expm1(beta v) is its series (x^2/6 below 2^-14)
+constexpr float kLinearReach = 2.f;            // beta max|v| up to which a channel is linear
+constexpr float kTinyReach = 0.000244140625f;  // 2^-12: up to which it is tiny
 // What the range of bf16 and fp32 may cost: a term whose weight or bank underflows is lost.  It is
 // at most 2^-126 times the other factor's largest: 2^8 (P) or the largest |E| met.  While that is at
-// most 2^kWideLog2, the lost terms of 2^20 keys stay under 2^-76, against a >= 2^-66.
-constexpr float kWideE = 1073741824.f;        // 2^30
-constexpr float kLeastA = 1.3552527e-20f;     // 2^-66
-constexpr float kMostA = 1.2980742e33f;       // 2^110
-constexpr float kLeastLinear = 0.25f;         // 1 + beta a: less cancels more than two bits
+// most 2^30, the lost terms of 2^20 keys stay under 2^-76, against a >= 2^-66.
+constexpr float kWideE = 1073741824.f;      // 2^30
+constexpr float kLeastA = 1.3552527e-20f;   // 2^-66
+constexpr float kMostA = 1.2980742e33f;     // 2^110
+constexpr float kLeastLinear = 0.25f;       // 1 + a of a linear channel: less cancels more than two bits
 
-// E(v) = |v| < theta ? v + hb v^2 : 2^(b v + s) + ic; linear channels have s = -log2 beta, ic = -1/beta
+// Scale D of a tiny channel, a power of two: |E| reaches 2^30 where beta |v| reaches 2^-8 (to a factor 2).
+__device__ __forceinline__ float tiny_scale(float beta) {
+  // 2^38 times beta without its fraction
+  return beta > 0.f ? __int_as_float(__float_as_int(beta * 274877906944.f) & 0x7f800000) : 1.f;
+}
+
+// E(v) = 2^(b v + s) + ic + d v: shifted {beta log2 e, -b max v, 0, 0}, linear {b, 0, -1, 0}, tiny {0, 0, -1, D}
 struct BankCoef {
-  float b, s, ic, hb, theta;
+  float b, s, ic, d;
 };
 
 __device__ __forceinline__ BankCoef bank_coef(float beta, float vmax, float vabs) {
+  const float x = beta * (vabs > 0.f ? vabs : 1.f);
   BankCoef c;
   c.b = beta * kLog2e;
-  c.hb = 0.5f * beta;
-  const bool linear = !(beta * vabs > kLinearReach);
-  if (linear) {
-    c.s = beta > 0.f ? -log2f(beta) : 0.f;
-    c.ic = beta > 0.f ? -1.f / beta : 0.f;
-    c.theta = beta > 0.f ? kSmallX / beta : INFINITY;
-  } else {
+  c.s = 0.f;
+  c.ic = -1.f;
+  c.d = 0.f;
+  if (x <= kTinyReach) {
+    c.b = 0.f;
+    c.d = tiny_scale(beta);
+  } else if (!(x <= kLinearReach)) {
     c.s = -c.b * vmax;
     c.ic = 0.f;
-    c.theta = 0.f;
   }
   return c;
 }
-
-__device__ __forceinline__ float bank_value(const BankCoef &c, float v) {
-  const float e = ex2_approx(fmaf(c.b, v, c.s)) + c.ic;
-  return fabsf(v) < c.theta ? fmaf(c.hb * v, v, v) : e;
+// The channel's kind, and a shifted one's s, in one float: NaN linear, infinity tiny.
+__device__ __forceinline__ float bank_kind(const BankCoef &c) {
+  return c.ic == 0.f ? c.s : c.d != 0.f ? INFINITY : __int_as_float(0x7fffffff);
 }
 
-// The read from a; `shift` is the coefficient s of a shifted channel, NaN of a linear one.  ok: false
-// where the ranges could have spoilt it.
-__device__ __forceinline__ float paged_out(float beta, float shift, float a, bool wide, bool *ok) {
+// E of two values; coefficients of both
+__device__ __forceinline__ float2 bank_pair(const float2 b, const float2 s, const float2 ic, const float2 d, const float2 v) {
+  const float2 x = __ffma2_rn(b, v, s);
+  return __ffma2_rn(d, v, __fadd2_rn(make_float2(ex2_approx(x.x), ex2_approx(x.y)), ic));
+}
+
+// The read from a, o = |a| g < 2^-6 and w != 0 ? a w (1 - g (a/2 - a^2/3)) : lg2(a + g) z + y:
+//   tiny {g 0, w 1/D}, linear {g 1, w 1/beta, z 1/b, y 0}, shifted {g 0, w 0, z 1/b, y -s/b}
+// (log1p's series is good to 2^-18 where it is used, lg2's 2^-22 to 2^-16 elsewhere.)  It stands when
+// lo < a + g < 2^110; otherwise the ranges could have spoilt it.  No branch: the kinds of a row's
+// channels are mixed.
+struct OutCoef {
+  float g, z, y, w, lo;
+};
+__device__ __forceinline__ OutCoef out_coef(float beta, float kind, bool wide) {
   const float ib = rcp_approx(beta * kLog2e);
-  if (shift != shift) {
-    const float x = beta * a;
-    *ok = !wide && x > kLeastLinear - 1.f && x < kMostA && fabsf(a) < kMostA;
-    // log1p(x) / beta; the series is good to 2^-18 where it is used, lg2's 2^-22 to 2^-16 elsewhere
-    return fabsf(x) < kSmallX ? a * fmaf(x, fmaf(x, 1.f / 3.f, -0.5f), 1.f) : lg2_approx(1.f + x) * ib;
-  }
-  *ok = a > (wide ? kWideE : kLeastA) && a < kMostA;
-  return (lg2_approx(a) - shift) * ib;
+  OutCoef c;
+  const bool tiny = kind == INFINITY, linear = kind != kind;
+  c.g = linear ? 1.f : 0.f;
+  c.z = tiny ? 0.f : ib;
+  c.y = tiny || linear ? 0.f : -kind * ib;
+  c.w = tiny ? (beta > 0.f ? 1.f / tiny_scale(beta) : 1.f) : linear ? ib * kLog2e : 0.f;
+  c.lo = tiny ? (wide ? INFINITY : -kMostA) : linear ? (wide ? INFINITY : kLeastLinear) : (wide ? kWideE : kLeastA);
+  return c;
+}
+__device__ __forceinline__ float paged_out(const OutCoef &c, float a, bool *ok) {
+  const float x = a + c.g;
+  *ok = x > c.lo && x < kMostA;
+  const float log = fmaf(lg2_approx(x), c.z, c.y);
+  const float series = a * c.w * fmaf(c.g * a, fmaf(a, 1.f / 3.f, -0.5f), 1.f);
+  return fabsf(a) * c.g < 0.015625f && c.w != 0.f ? series : log;
 }
 
 // ---------------------------------------------------------------------------
@@ -259,7 +286,7 @@ __device__ void split_locate(const PagedReadArgs &a, const SplitShape &shape, lo
 // Pieces.  CTA g's slot 0 holds the piece at its stretch's start that continues
 // an item of an earlier CTA, slot 1 the piece that begins an item it does not
 // end.  A piece: per row the accumulators [D] (not normalised), then per row
-// {m, L} (log2 units), then the shifts [D] (NaN: linear), then whether |E| went wide.
+// {m, L} (log2 units), then the channels' kinds [D], then whether |E| went wide.
 // ---------------------------------------------------------------------------
 __host__ __device__ constexpr size_t piece_floats(int rows, int D) {
   return static_cast<size_t>(rows) * D + 2 * rows + D + 4;

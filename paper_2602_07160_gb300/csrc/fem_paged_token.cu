@@ -42,8 +42,7 @@ struct TokLayout {
   static constexpr int kScale = kTokWarps * kStages * kStage;
   static constexpr int kBar = kScale + kTokWarps * kStages * 32;
   static constexpr int kCoef4 = (kBar + kTokWarps * kStages * 8 + 15) & ~15;
-  static constexpr int kCoef1 = kCoef4 + D * 16;
-  static constexpr int kShift = kCoef1 + D * 4;
+  static constexpr int kShift = kCoef4 + D * 16;
   static constexpr int kRed = kShift + D * 4;
   static constexpr int kStat = kRed + kRows * kRedStride * 4;  // [warps][rows] {m, L}
   static constexpr int kWideFlag = kStat + kTokWarps * kRows * 8;
@@ -126,8 +125,7 @@ __global__ void __launch_bounds__(kTokThreads, 2)
   const uint32_t ring = sbase + warp * NS * Lay::kStage;
   const uint32_t scales = sbase + Lay::kScale + warp * NS * 32;
   const uint32_t bars = sbase + Lay::kBar + warp * NS * 8;
-  float4 *coef4 = reinterpret_cast<float4 *>(smem + Lay::kCoef4);
-  float *coef1 = reinterpret_cast<float *>(smem + Lay::kCoef1);
+  float *s_coef = reinterpret_cast<float *>(smem + Lay::kCoef4);
   float *s_shift = reinterpret_cast<float *>(smem + Lay::kShift);
   float *s_red = reinterpret_cast<float *>(smem + Lay::kRed);
   float2 *s_stat = reinterpret_cast<float2 *>(smem + Lay::kStat);
@@ -225,12 +223,16 @@ __global__ void __launch_bounds__(kTokThreads, 2)
         // element e of a lane's piece of 8 channels, lanes side by side
         const int at = Lay::kElem == 2 || !R128 ? (tid & ~63) + (tid & 7) * 8 + ((tid >> 3) & 7)
                                                 : (tid & 15) * 8 + (tid >> 4);
-        coef4[at] = make_float4(c.b, c.s, c.ic, c.hb);
-        coef1[at] = c.theta;
-        s_shift[tid] = c.theta == 0.f ? c.s : __int_as_float(0x7fffffff);
+        // coefficients of a pair of channels side by side: {b, b', s, s'}, {ic, ic', d, d'}
+        float *cp = s_coef + (at & ~8) * 4 + ((at >> 3) & 1);
+        cp[0] = c.b;
+        cp[2] = c.s;
+        cp[32] = c.ic;
+        cp[34] = c.d;
+        s_shift[tid] = bank_kind(c);
       }
     } else if (tid < D) {
-      s_shift[tid] = __int_as_float(0x7fffffff);
+      s_shift[tid] = INFINITY;
     }
 
     // ---- Q^T as the second operand: column g of row tile t, the lane's channels in the order K's 16-byte pieces bring them
@@ -426,21 +428,23 @@ __global__ void __launch_bounds__(kTokThreads, 2)
                 }
               }
               if (BETA) {
-                const int at = pc * 64 + 2 * q * 8 + lane_g;
-                const float4 ca = coef4[at], cb = coef4[at + 8];
-                const BankCoef A = {ca.x, ca.y, ca.z, ca.w, coef1[at]}, B = {cb.x, cb.y, cb.z, cb.w, coef1[at + 8]};
+                const float4 *cp = reinterpret_cast<const float4 *>(s_coef) + pc * 64 + 2 * q * 8 + lane_g;
+                const float4 bs = cp[0], id = cp[8];
+                const float2 b2 = make_float2(bs.x, bs.y), s2 = make_float2(bs.z, bs.w);
+                const float2 ic2 = make_float2(id.x, id.y), d2 = make_float2(id.z, id.w);
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                  lo[u] = bank_value(A, lo[u]);
-                  hi[u] = bank_value(B, hi[u]);
+                  const float2 e = bank_pair(b2, s2, ic2, d2, make_float2(lo[u], hi[u]));
+                  lo[u] = e.x;
+                  hi[u] = e.y;
                 }
                 if (dead) {
 #pragma unroll
                   for (int u = 0; u < 4; ++u)
                     if ((dead >> u) & 1u) lo[u] = hi[u] = 0.f;
                 }
-                emax = fmax3(emax, fmax3(lo[0], lo[1], lo[2]), lo[3]);
-                emax = fmax3(emax, fmax3(hi[0], hi[1], hi[2]), hi[3]);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) emax = fmaxf(fmaxf(emax, fabsf(lo[u])), fabsf(hi[u]));
               } else if (dead) {
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
@@ -507,6 +511,8 @@ __global__ void __launch_bounds__(kTokThreads, 2)
     const int slot = cta * 2 + (sg.kt0 == 0 ? 1 : 0);
     float *piece = sp.pieces + static_cast<size_t>(slot) * piece_floats(kRows, D);
     const bool wide = *s_wide != 0;
+    const OutCoef oc = out_coef(BETA && tid < D ? a.beta[static_cast<long long>(sg.h) * D + tid] : 0.f,
+                                tid < D ? s_shift[tid] : INFINITY, wide);
     for (int r = 0; r < n_rows; ++r) {
       float M = -INFINITY, Lr = 0.f;
 #pragma unroll
@@ -525,8 +531,7 @@ __global__ void __launch_bounds__(kTokThreads, 2)
           float o = 0.f;
           if (!(M == -INFINITY && Lr == 0.f)) {
             const float av = s_red[r * Lay::kRedStride + tid] / Lr;
-            o = BETA ? paged_out(a.beta[static_cast<long long>(sg.h) * D + tid], s_shift[tid], av, wide, &ok)
-                     : paged_out(0.f, s_shift[tid], av, false, &ok);
+            o = paged_out(oc, av, &ok);
           }
           if (!ok) s_bad[r] = 1;
           static_cast<__nv_bfloat16 *>(a.out)[orow * D + tid] = __float2bfloat16_rn(o);
