@@ -877,7 +877,10 @@ int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride
   // few rows per head: the kernel that is bound by memory; more: the tensor cores
   const bool chunk = rows > kTokenRows && a.group <= 256;
   const int grid = chunk ? ds->num_sms : 2 * ds->num_sms;
-  const SplitShape shape = chunk ? SplitShape{256, 128, 256 / a.group, 1} : SplitShape{rows <= 8 ? 8 : 16, 64, 0, 2};
+  // whole tokens per row tile, a multiple of 8 where there are as many (the closed sum over row tiles is
+  // then short: fem_paged_split.cuh)
+  const int tok = 256 / a.group;
+  const SplitShape shape = chunk ? SplitShape{256, 7, tok >= 8 ? tok & ~7 : tok, 1} : SplitShape{rows <= 8 ? 8 : 16, 6, 0, 2};
   const int box_rows = chunk ? std::min(1 << a.c.page_shift, 128) : 16;
   CUtensorMap tk, tv;
   if ((rc = cache_map(&tk, a.c.k, a.c, box_rows)) != FEM_OK || (rc = cache_map(&tv, a.c.v, a.c, box_rows)) != FEM_OK)

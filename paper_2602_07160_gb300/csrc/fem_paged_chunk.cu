@@ -143,18 +143,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
 
   grid_dep_launch_dependents();
   if (blockIdx.x == 0) split_mark_unowned<kChunkThreads>(a, sp.todo);
-  const long long W = split_total(a, shape, scan);
-  if (W == 0) return;
-  const int G = split_ctas(W, gridDim.x, shape), cta = blockIdx.x;
-  if (cta >= G) return;
+  const int cta = blockIdx.x;
   SplitWalk walk;
-  walk.x = split_start(W, G, cta);
-  walk.x1 = split_start(W, G, cta + 1);
-  {
-    long long prefix;
-    split_locate(a, shape, walk.x, scan, &walk.s, &prefix);
-    walk.local = walk.x - prefix;
-  }
+  if (!split_begin(a, shape, cta, gridDim.x, scan, walk)) return;
   if (warp == 12) {
     tmem_alloc(sbase + Lay::kTmem, 512);
     tmem_relinquish();
@@ -693,7 +684,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             piece[256 * D + 2 * ir + 1] = L;
           }
           if (whole) sp.todo[w.orow] = good || empty ? kRowDone : kRowExact;
-          else if (sg.kt0 == 0) sp.todo[w.orow] = row_split(ir, cta, split_owner(W, G, sg.x_end - 1) - cta + 1);
+          else if (sg.kt0 == 0) sp.todo[w.orow] = row_split(ir, cta, split_owner(walk.W, walk.G, sg.x_end - 1) - cta + 1);
         }
         if (!whole && t == 0) {
           if (r < D) piece[256 * D + 512 + r] = shift[r];
@@ -741,7 +732,7 @@ cudaError_t launch_paged_chunk(const CUtensorMap &tk, const CUtensorMap &tv, con
   int box_shift = 4;
   while ((1 << box_shift) < box_rows) ++box_shift;
   if ((1 << box_shift) != box_rows || box_rows > kChunkKeys) return cudaErrorInvalidValue;
-  if (shape.row_tile != 256 || shape.key_tile != kChunkKeys || shape.tok < 1) return cudaErrorInvalidValue;
+  if (shape.row_tile != 256 || (1 << shape.key_shift) != kChunkKeys || shape.tok < 1) return cudaErrorInvalidValue;
   if (a.c.format == kCacheBf16)
     return a.c.d == 64 ? launch_chunk_d<kCacheBf16, 64>(tk, tv, a, sp, shape, grid, box_shift, stream)
                        : launch_chunk_d<kCacheBf16, 128>(tk, tv, a, sp, shape, grid, box_shift, stream);

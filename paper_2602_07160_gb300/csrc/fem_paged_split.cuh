@@ -108,56 +108,72 @@ __device__ __forceinline__ float paged_out(const OutCoef &c, float a, bool *ok) 
 // The line of work
 // ---------------------------------------------------------------------------
 struct SplitShape {
-  int row_tile, key_tile;  // rows and keys of a tile
-  int tok;                 // tokens of a row tile (row_tile / group, whole tokens), or 0: rows packed without regard to tokens
-  int least;               // key tiles a CTA takes at least
+  int row_tile, key_shift;  // rows of a tile, log2 of its keys
+  int tok;                  // tokens of a row tile (whole tokens), or 0: rows packed without regard to tokens
+  int least;                // key tiles a CTA takes at least
 };
 
 // Row tiles of a sequence, for each of its heads; a sequence without rows has none.
-__device__ __forceinline__ int seq_row_tiles(const SeqInfo &si, int group, const SplitShape &sh) {
+__host__ __device__ __forceinline__ int seq_row_tiles(const SeqInfo &si, int group, const SplitShape &sh) {
   return sh.tok ? (si.n + sh.tok - 1) / sh.tok : (si.n * group + sh.row_tile - 1) / sh.row_tile;
 }
 // Key tiles of row tile r: those its last row sees (tiles of whole tokens), or all.  At least one, so
 // that rows which see nothing are written.
-__device__ __forceinline__ int row_key_tiles(const SeqInfo &si, int r, int causal, const SplitShape &sh) {
+__host__ __device__ __forceinline__ int row_key_tiles(const SeqInfo &si, int r, int causal, const SplitShape &sh) {
   int keys = si.ctx;
-  if (sh.tok && causal) keys = si.ctx - si.n + min((r + 1) * sh.tok, si.n);
-  return max((keys + sh.key_tile - 1) / sh.key_tile, 1);
+  if (sh.tok && causal) {
+    const int last = (r + 1) * sh.tok;
+    keys = si.ctx - si.n + (last < si.n ? last : si.n);
+  }
+  const int tiles = (keys + (1 << sh.key_shift) - 1) >> sh.key_shift;
+  return tiles > 1 ? tiles : 1;
 }
-// Key tiles of row tiles 0 .. R - 1 of one head (R at most seq_row_tiles).
-__device__ __forceinline__ long long head_key_tiles(const SeqInfo &si, int R, int group, int causal,
-                                                    const SplitShape &sh) {
+// Key tiles of row tiles 0 .. R - 1 of one head (R at most `all`, the sequence's).
+__host__ __device__ __forceinline__ long long head_key_tiles(const SeqInfo &si, int R, int all, int causal,
+                                                             const SplitShape &sh) {
   if (R <= 0) return 0;
   if (!(sh.tok && causal)) return static_cast<long long>(R) * row_key_tiles(si, 0, 0, sh);
-  // sum of ceil((c + i tok) / key_tile), i = 0 .. R' - 1, over the tiles of tok whole tokens; the last
-  // tile of the sequence may hold fewer
-  const int all = seq_row_tiles(si, group, sh);
+  // sum of ceil((c + i tok) / T), i = 0 .. n - 1, over the tiles of tok whole tokens; the sequence's
+  // last tile may hold fewer
   long long sum = 0;
   int n = R, i0 = 0;
   if (R == all) {
     sum = row_key_tiles(si, R - 1, causal, sh);
     n = R - 1;
   }
-  const int base = si.ctx - si.n;
-  if (base + sh.tok < 1) {  // leading tiles that see nothing count one each
-    i0 = min(n, (-base) / sh.tok);
-    while (i0 < n && base + (i0 + 1) * sh.tok < 1) ++i0;
+  const int base = si.ctx - si.n, step = sh.tok, shift = sh.key_shift, T = 1 << shift;
+  if (base + step < 1) {  // leading tiles that see nothing count one each
+    i0 = -base / step;
+    if (i0 > n) i0 = n;
+    while (i0 < n && base + (i0 + 1) * step < 1) ++i0;
     sum += i0;
   }
   n -= i0;
-  // ceil(x / T) = floor((x + T - 1) / T); floor sum = (sum of x - sum of x mod T) / T, the residues with
-  // period P = T / gcd(tok, T) (T a power of two), a full period's being g times 0 .. P - 1 plus b mod g
-  const int T = sh.key_tile, step = sh.tok;
+  // ceil(x / T) = floor((x + T - 1) / T); floor sum = (sum of x - sum of x mod T) / T.  The residues have
+  // the period P = T / gcd(tok, T), a full period's being g times 0 .. P - 1 plus b mod g (T is a power
+  // of two, and so are g and P).
   const long long b = static_cast<long long>(base) + static_cast<long long>(i0 + 1) * step + T - 1;
-  const int gcd = min(step & -step, T), P = T / gcd, rem = n % P;
-  const long long full = n / P;
+  int lg = 0;
+  while (lg < shift && !((step >> lg) & 1)) ++lg;
+  const int gcd = 1 << lg, P = T >> lg, rem = n & (P - 1);
+  const long long full = n >> (shift - lg);
   long long res = full * (static_cast<long long>(P) * (b & (gcd - 1)) + static_cast<long long>(gcd) * P * (P - 1) / 2);
   for (int i = 0; i < rem; ++i) res += (b + static_cast<long long>(i) * step) & (T - 1);
   const long long x = n * b + static_cast<long long>(step) * n * (n - 1) / 2;
-  return sum + (x - res) / T;
+  return sum + ((x - res) >> shift);
 }
 __device__ __forceinline__ long long seq_tiles(const PagedReadArgs &a, const SeqInfo &si, const SplitShape &sh) {
-  return a.c.H * head_key_tiles(si, seq_row_tiles(si, a.group, sh), a.group, a.causal, sh);
+  const int R = seq_row_tiles(si, a.group, sh);
+  return a.c.H * head_key_tiles(si, R, R, a.causal, sh);
+}
+
+// CTA g's first tile of W (below 2^31) split over G: floor(W g / G).
+__host__ __device__ __forceinline__ unsigned split_start(unsigned W, unsigned G, unsigned g) {
+  return W / G * g + W % G * g / G;
+}
+// The CTA that has tile x.
+__host__ __device__ __forceinline__ int split_owner(unsigned W, unsigned G, unsigned x) {
+  return static_cast<int>((static_cast<unsigned long long>(x + 1) * G - 1) / W);
 }
 
 // Rows no sequence owns need nothing (rows from the first offset to the last are owned).
@@ -174,87 +190,57 @@ struct SplitSeg {
   SeqInfo si;
   int s, h, r;  // sequence, head, row tile
   int kt0, kt1, kt_all;
-  long long x_end;  // the line's tile after the item's last
+  unsigned x_end;  // the line's tile after the item's last
 };
 
 // Walks a CTA's stretch, item by item.
 struct SplitWalk {
-  long long x, x1, local;  // next tile, the stretch's end, x within sequence s
-  int s;
+  unsigned x, left;  // next tile, tiles to go
+  unsigned W, G;     // the line's tiles, CTAs that take part
+  SeqInfo si;
+  int s, h, r, kt0, R;
   __device__ __forceinline__ bool next(const PagedReadArgs &a, const SplitShape &sh, SplitSeg &g) {
-    if (x >= x1) return false;
-    while (true) {
-      g.si = paged_seq(a, s);
-      const int R = seq_row_tiles(g.si, a.group, sh);
-      const long long per = head_key_tiles(g.si, R, a.group, a.causal, sh), cost = per * a.c.H;
-      if (local >= cost) {  // a sequence done, or one without rows
-        local -= cost;
-        ++s;
-        continue;
+    if (left == 0) return false;
+    g.si = si;
+    g.s = s;
+    g.h = h;
+    g.r = r;
+    g.kt0 = kt0;
+    g.kt_all = row_key_tiles(si, r, a.causal, sh);
+    const unsigned rest = g.kt_all - kt0, take = min(rest, left);
+    g.kt1 = kt0 + take;
+    g.x_end = x + rest;
+    x += take;
+    left -= take;
+    kt0 = 0;
+    if (left && ++r == R) {
+      r = 0;
+      if (++h == a.c.H) {
+        h = 0;
+        do {  // the next sequence with rows: there is one, as tiles are left
+          si = paged_seq(a, ++s);
+          R = seq_row_tiles(si, a.group, sh);
+        } while (R == 0);
       }
-      g.s = s;
-      g.h = static_cast<int>(local / per);
-      const long long in = local - g.h * per;
-      int lo = 0, hi = R;  // the last r whose tiles begin at or before `in`
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (head_key_tiles(g.si, mid, a.group, a.causal, sh) <= in) lo = mid; else hi = mid;
-      }
-      g.r = lo;
-      g.kt_all = row_key_tiles(g.si, lo, a.causal, sh);
-      g.kt0 = static_cast<int>(in - head_key_tiles(g.si, lo, a.group, a.causal, sh));
-      g.kt1 = static_cast<int>(min(static_cast<long long>(g.kt_all), g.kt0 + (x1 - x)));
-      g.x_end = x + (g.kt_all - g.kt0);
-      x += g.kt1 - g.kt0;
-      local += g.kt1 - g.kt0;
-      return true;
     }
+    return true;
   }
 };
-
-// CTAs that take part, and CTA g's first tile.
-__device__ __forceinline__ int split_ctas(long long W, int grid, const SplitShape &sh) {
-  const long long most = (W + sh.least - 1) / sh.least;
-  return static_cast<int>(most < grid ? most : grid);
-}
-__device__ __forceinline__ long long split_start(long long W, int G, int g) { return W * g / G; }
-// the CTA that has tile x
-__device__ __forceinline__ int split_owner(long long W, int G, long long x) {
-  return static_cast<int>(((x + 1) * G - 1) / W);
-}
 
 template <int THREADS>
 struct SplitScan {
   long long warp[THREADS / 32];
-  long long prefix;
-  int s;
+  int s, h, r, kt0;
 };
 
-// Tiles of all sequences.  All THREADS threads of the block.
+// The stretch of CTA `cta` of a grid of `grid`; false where it has none.  All THREADS threads of the block.
 template <int THREADS>
-__device__ long long split_total(const PagedReadArgs &a, const SplitShape &shape, SplitScan<THREADS> &sc) {
-  long long w = 0;
-  for (int s = threadIdx.x; s < a.S; s += THREADS) w += seq_tiles(a, paged_seq(a, s), shape);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) sc.warp[threadIdx.x >> 5] = w;
-  __syncthreads();
-  w = 0;
-#pragma unroll
-  for (int i = 0; i < THREADS / 32; ++i) w += sc.warp[i];
-  return w;
-}
-
-// The sequence that holds tile x (0 <= x < total), and the tiles before that sequence.
-template <int THREADS>
-__device__ void split_locate(const PagedReadArgs &a, const SplitShape &shape, long long x, SplitScan<THREADS> &sc,
-                             int *s_out, long long *prefix_out) {
-  long long before = 0;
+__device__ bool split_begin(const PagedReadArgs &a, const SplitShape &shape, int cta, int grid, SplitScan<THREADS> &sc,
+                            SplitWalk &walk) {
+  constexpr int kWarps = THREADS / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int base = 0; base < a.S; base += THREADS) {
-    const int s = base + threadIdx.x;
-    const long long w = s < a.S ? seq_tiles(a, paged_seq(a, s), shape) : 0;
+  // inclusive sums of the tiles of sequences base .. base + THREADS - 1 (thread = sequence)
+  auto scan = [&](long long w, long long &all) {
     long long inc = w;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -264,22 +250,74 @@ __device__ void split_locate(const PagedReadArgs &a, const SplitShape &shape, lo
     __syncthreads();
     if (lane == 31) sc.warp[warp] = inc;
     __syncthreads();
-    long long off = before, all = 0;
+    all = 0;
 #pragma unroll
-    for (int i = 0; i < THREADS / 32; ++i) {
-      if (i < warp) off += sc.warp[i];
+    for (int i = 0; i < kWarps; ++i) {
+      if (i < warp) inc += sc.warp[i];
       all += sc.warp[i];
     }
-    if (x >= off + inc - w && x < off + inc) {
+    return inc;
+  };
+  SeqInfo si = {0, 0, 0};
+  if (threadIdx.x < a.S) si = paged_seq(a, threadIdx.x);
+  long long w = seq_tiles(a, si, shape), all, W;
+  long long inc = scan(w, all);
+  W = all;
+  for (int base = THREADS; base < a.S; base += THREADS) {  // more sequences than threads
+    const int s = base + threadIdx.x;
+    scan(s < a.S ? seq_tiles(a, paged_seq(a, s), shape) : 0, all);
+    W += all;
+  }
+  if (W <= 0) return false;
+  if (W >= (1ll << 31)) {  // hours of work: lengths that are not meant
+    if (threadIdx.x == 0) atomicOr(a.err, kErrPageRange);
+    return false;
+  }
+  const long long most = (W + shape.least - 1) / shape.least;
+  walk.W = static_cast<unsigned>(W);
+  walk.G = static_cast<unsigned>(most < grid ? most : grid);
+  if (cta >= static_cast<int>(walk.G)) return false;
+  walk.x = split_start(walk.W, walk.G, cta);
+  walk.left = split_start(walk.W, walk.G, cta + 1) - walk.x;
+  long long before = 0;
+  int s = threadIdx.x;
+  for (int base = 0;; base += THREADS) {
+    if (base > 0) {
+      s = base + threadIdx.x;
+      si = {0, 0, 0};
+      if (s < a.S) si = paged_seq(a, s);
+      w = seq_tiles(a, si, shape);
+      inc = scan(w, all) + before;
+    } else if (a.S > THREADS) {
+      inc = scan(w, all);  // all: of this round again
+    }
+    if (walk.x >= inc - w && walk.x < inc) {
+      // this thread's sequence holds the stretch's first tile
+      const int R = seq_row_tiles(si, a.group, shape);
+      const unsigned per = static_cast<unsigned>(head_key_tiles(si, R, R, a.causal, shape));
+      const unsigned local = static_cast<unsigned>(walk.x - (inc - w));
+      const unsigned h = local / per, in = local - h * per;
+      int lo = 0, hi = R;  // the last row tile whose key tiles begin at or before `in`
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (head_key_tiles(si, mid, R, a.causal, shape) <= in) lo = mid; else hi = mid;
+      }
       sc.s = s;
-      sc.prefix = off + inc - w;
+      sc.h = static_cast<int>(h);
+      sc.r = lo;
+      sc.kt0 = static_cast<int>(in - head_key_tiles(si, lo, R, a.causal, shape));
     }
     before += all;
-    if (x < before) break;  // the same for every thread
+    if (walk.x < before) break;  // the same for every thread
   }
   __syncthreads();
-  *s_out = sc.s;
-  *prefix_out = sc.prefix;
+  walk.s = sc.s;
+  walk.h = sc.h;
+  walk.r = sc.r;
+  walk.kt0 = sc.kt0;
+  walk.si = paged_seq(a, walk.s);
+  walk.R = seq_row_tiles(walk.si, a.group, shape);
+  return true;
 }
 
 // ---------------------------------------------------------------------------

@@ -37,14 +37,14 @@ struct TokLayout {
   static constexpr int kStage = 2 * kTokKeys * kRow;           // K and V of 16 keys
   static constexpr int kStages = 24576 / kStage < 6 ? 24576 / kStage : 6;
   static constexpr int kRows = 8 * NT;
-  static constexpr int kRedStride = D + 4;
-  // shared memory: rings, then scale bytes, barriers, coefficients, the join's rows
+  static constexpr int kRedStride = D + 1;  // so that the lanes of a store to the join meet on two banks at most
+  static_assert(kRows * kRedStride * 4 <= kStages * kStage, "a warp's ring holds its rows");
+  // shared memory: rings (in the join, the warps' rows), then scale bytes, barriers, coefficients
   static constexpr int kScale = kTokWarps * kStages * kStage;
   static constexpr int kBar = kScale + kTokWarps * kStages * 32;
   static constexpr int kCoef4 = (kBar + kTokWarps * kStages * 8 + 15) & ~15;
   static constexpr int kShift = kCoef4 + D * 16;
-  static constexpr int kRed = kShift + D * 4;
-  static constexpr int kStat = kRed + kRows * kRedStride * 4;  // [warps][rows] {m, L}
+  static constexpr int kStat = kShift + D * 4;  // [warps][rows] {m, L}
   static constexpr int kWideFlag = kStat + kTokWarps * kRows * 8;
   static constexpr int kRowBad = kWideFlag + 4;  // per row: some channel needs the exact path
   static constexpr int kBytes = kRowBad + kRows * 4;
@@ -127,7 +127,6 @@ __global__ void __launch_bounds__(kTokThreads, 2)
   const uint32_t bars = sbase + Lay::kBar + warp * NS * 8;
   float *s_coef = reinterpret_cast<float *>(smem + Lay::kCoef4);
   float *s_shift = reinterpret_cast<float *>(smem + Lay::kShift);
-  float *s_red = reinterpret_cast<float *>(smem + Lay::kRed);
   float2 *s_stat = reinterpret_cast<float2 *>(smem + Lay::kStat);
   int *s_wide = reinterpret_cast<int *>(smem + Lay::kWideFlag);
   int *s_bad = reinterpret_cast<int *>(smem + Lay::kRowBad);
@@ -138,21 +137,35 @@ __global__ void __launch_bounds__(kTokThreads, 2)
     fence_mbar_init();
   }
   if (blockIdx.x == 0) split_mark_unowned<kTokThreads>(a, sp.todo);
-  const long long W = split_total(a, shape, scan);
-  if (W == 0) return;
-  const int G = split_ctas(W, gridDim.x, shape), cta = blockIdx.x;
-  if (cta >= G) return;
-  const long long x0 = split_start(W, G, cta), x1 = split_start(W, G, cta + 1);
-  int s;
-  long long prefix;
-  split_locate(a, shape, x0, scan, &s, &prefix);
-  SplitWalk walk = {x0, x1, x0 - prefix, s};
+  const int cta = blockIdx.x;
+  SplitWalk walk;
+  if (!split_begin(a, shape, cta, gridDim.x, scan, walk)) return;
   SplitSeg sg;
   unsigned phases = 0;  // parity of each stage's barrier
   bool alive = true;
 
   while (walk.next(a, shape, sg)) {
     const int row0 = sg.r * kRows, total = sg.si.n * a.group, n_rows = min(kRows, total - row0);
+    // loads that wait for nothing go first
+    const float beta_c = BETA && tid < D ? __ldg(a.beta + static_cast<long long>(sg.h) * D + tid) : 0.f;
+    // ---- Q^T as the second operand: column g of row tile t, the lane's channels in the order K's 16-byte pieces bring them
+    uint32_t qf[NT][MT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int r = row0 + 8 * t + g;
+      const bool on = r < total;
+      const int tok = on ? r / a.group : 0, hq = sg.h * a.group + (on ? r % a.group : 0);
+      const __nv_bfloat16 *qp = static_cast<const __nv_bfloat16 *>(a.q) +
+                                (static_cast<long long>(sg.si.q0) + tok) * a.q_sn + hq * a.q_sh;
+#pragma unroll
+      for (int kk = 0; kk < MT; ++kk) {
+        // bf16: piece kk/2 of 8 channels at 32 (kk/2) + 8 i, half kk%2; e4m3: piece kk/4 of 16 at 64 (kk/4) + 16 i, quarter kk%4
+        const int at = FORMAT == kCacheBf16 ? 32 * (kk >> 1) + 8 * i4 + 4 * (kk & 1) : 64 * (kk >> 2) + 16 * i4 + 4 * (kk & 3);
+        const uint2 w = on ? *reinterpret_cast<const uint2 *>(qp + at) : make_uint2(0, 0);
+        qf[t][kk][0] = w.x;
+        qf[t][kk][1] = w.y;
+      }
+    }
     // ---- this warp's stages: key groups kt * 4 + warp, kt0 <= kt < kt1, that hold a key
     const int n_st = [&] {
       const int groups = (sg.si.ctx + kTokKeys - 1) / kTokKeys;  // of the sequence
@@ -219,7 +232,7 @@ __global__ void __launch_bounds__(kTokThreads, 2)
             vabs = fmaxf(vabs, fabsf(v[kk]));
           }
         }
-        const BankCoef c = bank_coef(a.beta[static_cast<long long>(sg.h) * D + tid], vmax, vabs);
+        const BankCoef c = bank_coef(beta_c, vmax, vabs);
         // element e of a lane's piece of 8 channels, lanes side by side
         const int at = Lay::kElem == 2 || !R128 ? (tid & ~63) + (tid & 7) * 8 + ((tid >> 3) & 7)
                                                 : (tid & 15) * 8 + (tid >> 4);
@@ -235,24 +248,6 @@ __global__ void __launch_bounds__(kTokThreads, 2)
       s_shift[tid] = INFINITY;
     }
 
-    // ---- Q^T as the second operand: column g of row tile t, the lane's channels in the order K's 16-byte pieces bring them
-    uint32_t qf[NT][MT][2];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const int r = row0 + 8 * t + g;
-      const bool on = r < total;
-      const int tok = on ? r / a.group : 0, hq = sg.h * a.group + (on ? r % a.group : 0);
-      const __nv_bfloat16 *qp = static_cast<const __nv_bfloat16 *>(a.q) +
-                                (static_cast<long long>(sg.si.q0) + tok) * a.q_sn + hq * a.q_sh;
-#pragma unroll
-      for (int kk = 0; kk < MT; ++kk) {
-        // bf16: piece kk/2 of 8 channels at 32 (kk/2) + 8 i, half kk%2; e4m3: piece kk/4 of 16 at 64 (kk/4) + 16 i, quarter kk%4
-        const int at = FORMAT == kCacheBf16 ? 32 * (kk >> 1) + 8 * i4 + 4 * (kk & 1) : 64 * (kk >> 2) + 16 * i4 + 4 * (kk & 3);
-        const uint2 w = on ? *reinterpret_cast<const uint2 *>(qp + at) : make_uint2(0, 0);
-        qf[t][kk][0] = w.x;
-        qf[t][kk][1] = w.y;
-      }
-    }
     // keys seen by the lane's columns (rows 2 i, 2 i + 1 of each row tile)
     int lim[NT][2], lim_min = 0x7fffffff;
 #pragma unroll
@@ -465,7 +460,7 @@ __global__ void __launch_bounds__(kTokThreads, 2)
       else if (!alive) valid &= ~(1u << st);
     }
 
-    // ---- join the warps: rows' sums over the lanes that share them, then one warp after the other
+    // ---- join the warps: each leaves its rows' {m, L} and accumulators (over its own ring, which is idle)
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -475,53 +470,40 @@ __global__ void __launch_bounds__(kTokThreads, 2)
         if (g == 0) s_stat[warp * kRows + 8 * t + 2 * i4 + u] = make_float2(m[t][u], L[t][u]);
       }
     if (BETA && __any_sync(0xffffffffu, emax > kWideE) && lane == 0) *s_wide = 1;
-    __syncthreads();
-    float wgt[NT][2];
+    {
+      float *own = reinterpret_cast<float *>(smem + warp * NS * Lay::kStage);
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float M = -INFINITY;
+        for (int c = 0; c < MT; ++c)
 #pragma unroll
-        for (int q = 0; q < kTokWarps; ++q) M = fmaxf(M, s_stat[q * kRows + 8 * t + 2 * i4 + u].x);
-        wgt[t][u] = m[t][u] == -INFINITY ? 0.f : ex2_approx(m[t][u] - M);
-      }
-#pragma unroll 1
-    for (int q = 0; q < kTokWarps; ++q) {
-      if (warp == q) {
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int c = 0; c < MT; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              // channel of the product's row g (e < 2) or g + 8 (e >= 2)
-              const int ch = FORMAT == kCacheBf16
-                                 ? 64 * (c >> 2) + 8 * ((g >> 1) + 4 * (g & 1)) + 2 * (c & 3) + (e >> 1)
-                                 : R128 ? 16 * ((g >> 1) + 4 * (g & 1)) + 2 * c + (e >> 1) : 8 * g + 2 * c + (e >> 1);
-              float *p = s_red + (8 * t + 2 * i4 + (e & 1)) * Lay::kRedStride + ch;
-              const float v = acc[t][c][e] * wgt[t][e & 1];
-              *p = q == 0 ? v : *p + v;
-            }
-      }
-      __syncthreads();
+          for (int e = 0; e < 4; ++e) {
+            // channel of the product's row g (e < 2) or g + 8 (e >= 2)
+            const int ch = FORMAT == kCacheBf16
+                               ? 64 * (c >> 2) + 8 * ((g >> 1) + 4 * (g & 1)) + 2 * (c & 3) + (e >> 1)
+                               : R128 ? 16 * ((g >> 1) + 4 * (g & 1)) + 2 * c + (e >> 1) : 8 * g + 2 * c + (e >> 1);
+            own[(8 * t + 2 * i4 + (e & 1)) * Lay::kRedStride + ch] = acc[t][c][e];
+          }
     }
+    __syncthreads();
     // ---- the segment's rows: their output, or a piece of it
     const bool whole = sg.kt0 == 0 && sg.kt1 == sg.kt_all;
     const int slot = cta * 2 + (sg.kt0 == 0 ? 1 : 0);
     float *piece = sp.pieces + static_cast<size_t>(slot) * piece_floats(kRows, D);
     const bool wide = *s_wide != 0;
-    const OutCoef oc = out_coef(BETA && tid < D ? a.beta[static_cast<long long>(sg.h) * D + tid] : 0.f,
-                                tid < D ? s_shift[tid] : INFINITY, wide);
+    const OutCoef oc = out_coef(beta_c, tid < D ? s_shift[tid] : INFINITY, wide);
     for (int r = 0; r < n_rows; ++r) {
-      float M = -INFINITY, Lr = 0.f;
+      float M = -INFINITY, Lr = 0.f, av = 0.f;
 #pragma unroll
       for (int q = 0; q < kTokWarps; ++q) M = fmaxf(M, s_stat[q * kRows + r].x);
 #pragma unroll
       for (int q = 0; q < kTokWarps; ++q) {
         const float2 st = s_stat[q * kRows + r];
-        if (st.x != -INFINITY) Lr += st.y * ex2_approx(st.x - M);
-        else if (st.y != st.y) Lr = st.y;  // a row of NaN scores has no maximum
+        // a row of NaN scores has no maximum
+        const float wq = st.x != -INFINITY ? ex2_approx(st.x - M) : st.y != st.y ? 1.f : 0.f;
+        Lr = fmaf(wq, st.y, Lr);
+        const float x = tid < D ? reinterpret_cast<const float *>(smem + q * NS * Lay::kStage)[r * Lay::kRedStride + tid] : 0.f;
+        if (wq != 0.f) av = fmaf(wq, x, av);
       }
       const int rr = row0 + r, tok = rr / a.group, hq = sg.h * a.group + rr % a.group;
       const long long orow = (static_cast<long long>(sg.si.q0) + tok) * a.Hq + hq;
@@ -530,8 +512,7 @@ __global__ void __launch_bounds__(kTokThreads, 2)
           bool ok = true;
           float o = 0.f;
           if (!(M == -INFINITY && Lr == 0.f)) {
-            const float av = s_red[r * Lay::kRedStride + tid] / Lr;
-            o = paged_out(oc, av, &ok);
+            o = paged_out(oc, av / Lr, &ok);
           }
           if (!ok) s_bad[r] = 1;
           static_cast<__nv_bfloat16 *>(a.out)[orow * D + tid] = __float2bfloat16_rn(o);
@@ -539,7 +520,7 @@ __global__ void __launch_bounds__(kTokThreads, 2)
         if (tid == 0 && a.lse != nullptr)
           a.lse[orow] = M == -INFINITY && Lr == 0.f ? -INFINITY : (M + log2f(Lr)) * kLn2;
       } else {
-        if (tid < D) piece[static_cast<size_t>(r) * D + tid] = s_red[r * Lay::kRedStride + tid];
+        if (tid < D) piece[static_cast<size_t>(r) * D + tid] = av;
         if (tid == 0) {
           piece[kRows * D + 2 * r] = M;
           piece[kRows * D + 2 * r + 1] = Lr;
@@ -550,11 +531,12 @@ __global__ void __launch_bounds__(kTokThreads, 2)
       if (tid < D) piece[kRows * D + 2 * kRows + tid] = s_shift[tid];
       if (tid == 0) piece[kRows * D + 2 * kRows + D] = wide ? 1.f : 0.f;
     }
+    fence_proxy_async_smem();  // the rings go back to the copies
     __syncthreads();
     if (tid < n_rows && (whole || sg.kt0 == 0)) {
       const int rr = row0 + tid, tok = rr / a.group, hq = sg.h * a.group + rr % a.group;
       sp.todo[(static_cast<long long>(sg.si.q0) + tok) * a.Hq + hq] =
-          whole ? (s_bad[tid] ? kRowExact : kRowDone) : row_split(tid, cta, split_owner(W, G, sg.x_end - 1) - cta + 1);
+          whole ? (s_bad[tid] ? kRowExact : kRowDone) : row_split(tid, cta, split_owner(walk.W, walk.G, sg.x_end - 1) - cta + 1);
     }
   }
 }

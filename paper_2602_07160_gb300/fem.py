@@ -360,7 +360,7 @@ class PagedCache:
             raise ValueError("page_size must be 16, 32, 64, 128 or 256 and d a multiple of 16 up to 256")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.num_pages, self.H, self.page_size, self.d = pages, H, page_size, d
-        self.device = k.device
+        self.device, self.index = k.device, k.get_device()
         self.row_dtype = torch.float32 if k.dtype == torch.float32 else torch.bfloat16  # of k, v, q given to the calls
         self._struct = _CacheStruct(k.data_ptr(), v.data_ptr(), k_exp.data_ptr() if scaled else None,
                                     v_exp.data_ptr() if scaled else None, self.FORMATS[k.dtype], pages, H, page_size, d)
@@ -378,11 +378,16 @@ class PagedCache:
         return cls(k.view(dtype), v.view(dtype), *exps)
 
 
+def _raw_stream(stream, cache):
+    """The stream a paged-cache call runs on, as a number."""
+    return torch._C._cuda_getCurrentRawStream(cache.index) if stream is None else stream.cuda_stream
+
+
 def _check_rows(name, t, cache, heads):
     """A [N, heads, d] input of the cache's row type, d contiguous."""
     if t.dim() != 3 or t.shape[2] != cache.d or (heads is not None and t.shape[1] != heads):
         raise ValueError(f"{name} must be [N, heads, d] with the cache's d" + ("" if heads is None else " and H"))
-    if t.dtype != cache.row_dtype or t.device != cache.device:
+    if t.dtype is not cache.row_dtype or t.get_device() != cache.index:
         raise ValueError(f"{name} must be {cache.row_dtype} on the cache's device")
     if t.stride(2) != 1:
         raise ValueError(f"{name}'s last axis must be contiguous")
@@ -390,12 +395,15 @@ def _check_rows(name, t, cache, heads):
 
 def _row_strides(t):
     """Token and head strides of a [N, heads, d] tensor; an axis of length one has none."""
-    return (t.stride(0) if t.shape[0] > 1 else 0), (t.stride(1) if t.shape[1] > 1 else 0)
+    n, h, _ = t.stride()
+    return (n if t.shape[0] > 1 else 0), (h if t.shape[1] > 1 else 0)
 
 
-def _check_ints(name, t, shape, dtype, device):
-    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+def _check_whole(name, t, shape, dtype, index):
+    """A contiguous tensor of a shape and type on CUDA device `index`; returns its address."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on the cache's device")
+    return t.data_ptr()
 
 
 def fem_cache_write(cache: PagedCache, k, v, slots, stream=None):
@@ -407,9 +415,9 @@ def fem_cache_write(cache: PagedCache, k, v, slots, stream=None):
     _check_rows("v", v, cache, cache.H)
     if v.shape[0] != N:
         raise ValueError("k and v must have as many tokens")
-    _check_ints("slots", slots, (N,), torch.int64, cache.device)
     rc = load().fem_cache_write(cache._ref, k.data_ptr(), v.data_ptr(), *_row_strides(k), *_row_strides(v),
-                                slots.data_ptr(), N, _stream(stream, cache.device))
+                                _check_whole("slots", slots, (N,), torch.int64, cache.index), N,
+                                _raw_stream(stream, cache))
     if rc != 0:
         raise FemError("fem_cache_write", rc)
 
@@ -419,19 +427,19 @@ def fem_cache_gather(cache: PagedCache, block_table, starts, offsets, total: int
 
     block_table: int32 [S, max_pages]; starts: int32 [S], each stretch's first position;
     offsets: int32 [S + 1], its rows of the output; total = offsets[S]."""
-    S, shape = block_table.shape[0], (total, cache.H, cache.d)
-    _check_ints("block_table", block_table, (S, block_table.shape[1]), torch.int32, cache.device)
-    _check_ints("starts", starts, (S,), torch.int32, cache.device)
-    _check_ints("offsets", offsets, (S + 1,), torch.int32, cache.device)
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [S, max_pages]")
+    (S, max_pages), shape, index = block_table.shape, (total, cache.H, cache.d), cache.index
     if k_out is None:
-        k_out = torch.empty(shape, dtype=cache.row_dtype, device=cache.device)
+        k_out = cache.k.new_empty(shape, dtype=cache.row_dtype)
     if v_out is None:
-        v_out = torch.empty(shape, dtype=cache.row_dtype, device=cache.device)
-    _check_ints("k_out", k_out, shape, cache.row_dtype, cache.device)
-    _check_ints("v_out", v_out, shape, cache.row_dtype, cache.device)
-    rc = load().fem_cache_gather(cache._ref, block_table.data_ptr(), block_table.shape[1], starts.data_ptr(),
-                                 offsets.data_ptr(), S, k_out.data_ptr(), v_out.data_ptr(), total,
-                                 _stream(stream, cache.device))
+        v_out = cache.k.new_empty(shape, dtype=cache.row_dtype)
+    rc = load().fem_cache_gather(cache._ref, _check_whole("block_table", block_table, (S, max_pages), torch.int32, index),
+                                 max_pages, _check_whole("starts", starts, (S,), torch.int32, index),
+                                 _check_whole("offsets", offsets, (S + 1,), torch.int32, index), S,
+                                 _check_whole("k_out", k_out, shape, cache.row_dtype, index),
+                                 _check_whole("v_out", v_out, shape, cache.row_dtype, index), total,
+                                 _raw_stream(stream, cache))
     if rc != 0:
         raise FemError("fem_cache_gather", rc)
     return k_out, v_out
@@ -450,26 +458,28 @@ def fem_paged_read(q, cache: PagedCache, beta, q_offsets, ctx_lens, block_table,
     N, Hq, d = q.shape
     if Hq % cache.H:
         raise ValueError("q's heads must be a multiple of the cache's")
-    if beta is not None:
-        _check_ints("beta", beta, (cache.H, d), torch.float32, cache.device)
     if block_table.dim() != 2:
         raise ValueError("block_table must be [S, max_pages]")
-    S, max_pages = block_table.shape
-    _check_ints("block_table", block_table, (S, max_pages), torch.int32, cache.device)
-    _check_ints("q_offsets", q_offsets, (S + 1,), torch.int32, cache.device)
-    _check_ints("ctx_lens", ctx_lens, (S,), torch.int32, cache.device)
+    (S, max_pages), index = block_table.shape, cache.index
+    out_ptr = lse_ptr = beta_ptr = None
     if out is None:
-        out = torch.empty((N, Hq, d), dtype=q.dtype, device=cache.device)
+        out = q.new_empty((N, Hq, d))
+        out_ptr = out.data_ptr()
     else:
-        _check_ints("out", out, (N, Hq, d), q.dtype, cache.device)
+        out_ptr = _check_whole("out", out, (N, Hq, d), q.dtype, index)
     if lse is None:
-        lse = torch.empty((N, Hq), dtype=torch.float32, device=cache.device)
+        lse = q.new_empty((N, Hq), dtype=torch.float32)
+        lse_ptr = lse.data_ptr()
     elif lse is not False:
-        _check_ints("lse", lse, (N, Hq), torch.float32, cache.device)
-    rc = load().fem_paged_read(cache._ref, q.data_ptr(), *_row_strides(q),
-                               None if beta is None else beta.data_ptr(), q_offsets.data_ptr(), ctx_lens.data_ptr(),
-                               block_table.data_ptr(), max_pages, S, N, Hq, int(max_q), int(bool(causal)),
-                               out.data_ptr(), None if lse is False else lse.data_ptr(), _stream(stream, cache.device))
+        lse_ptr = _check_whole("lse", lse, (N, Hq), torch.float32, index)
+    if beta is not None:
+        beta_ptr = _check_whole("beta", beta, (cache.H, d), torch.float32, index)
+    rc = load().fem_paged_read(cache._ref, q.data_ptr(), *_row_strides(q), beta_ptr,
+                               _check_whole("q_offsets", q_offsets, (S + 1,), torch.int32, index),
+                               _check_whole("ctx_lens", ctx_lens, (S,), torch.int32, index),
+                               _check_whole("block_table", block_table, (S, max_pages), torch.int32, index),
+                               max_pages, S, N, Hq, int(max_q), int(bool(causal)), out_ptr, lse_ptr,
+                               _raw_stream(stream, cache))
     if rc != 0:
         raise FemError("fem_paged_read", rc)
     return out, (None if lse is False else lse)
