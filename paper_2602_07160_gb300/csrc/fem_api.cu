@@ -886,13 +886,14 @@ int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride
   if ((rc = cache_map(&tk, a.c.k, a.c, box_rows)) != FEM_OK || (rc = cache_map(&tv, a.c.v, a.c, box_rows)) != FEM_OK)
     return rc;
   const size_t piece_b = round256(2 * static_cast<size_t>(grid) * piece_floats(shape.row_tile, a.c.d) * sizeof(float));
+  const size_t record_b = round256(static_cast<size_t>(grid) * sizeof(SplitRecord));
   uint8_t *ws = nullptr;
-  cudaError_t e = ws_alloc(ds, reinterpret_cast<void **>(&ws), piece_b + static_cast<size_t>(N) * Hq * sizeof(uint32_t), s);
+  cudaError_t e = ws_alloc(ds, reinterpret_cast<void **>(&ws), piece_b + record_b + static_cast<size_t>(N) * Hq, s);
   if (e != cudaSuccess) return map_cuda(e);
-  const PagedSplit sp = {reinterpret_cast<float *>(ws), reinterpret_cast<uint32_t *>(ws + piece_b)};
+  const PagedSplit sp = {reinterpret_cast<float *>(ws), reinterpret_cast<SplitRecord *>(ws + piece_b), ws + piece_b + record_b};
   e = chunk ? launch_paged_chunk(tk, tv, a, sp, shape, grid, box_rows, s)
             : launch_paged_token(tk, tv, a, sp, shape, grid, s);
-  if (e == cudaSuccess) e = launch_paged_finish(a, sp, shape, grid, ds->num_sms, s);
+  if (e == cudaSuccess) e = launch_paged_finish(a, sp, shape, grid, s);
   const cudaError_t ef = cudaFreeAsync(ws, s);
   return map_cuda(e != cudaSuccess ? e : ef);
 }

@@ -177,6 +177,6 @@ cudaError_t launch_paged_chunk(const CUtensorMap &tk, const CUtensorMap &tv, con
                                const PagedSplit &sp, const SplitShape &shape, int grid, int box_rows,
                                cudaStream_t stream);
 cudaError_t launch_paged_finish(const PagedReadArgs &a, const PagedSplit &sp, const SplitShape &shape, int grid,
-                                int num_sms, cudaStream_t stream);
+                                cudaStream_t stream);
 
 }  // namespace fem

@@ -35,98 +35,64 @@ __global__ void __launch_bounds__(kExactThreads) paged_exact_kernel(const PagedR
   paged_exact_row<FORMAT>(a, s, si, t, hq, sh);
 }
 
-// The rows that the reading kernel left: items cut by the ends of CTAs'
-// stretches are joined from their pieces, in the line's order, a warp per row
-// (its lanes side by side over the channels); rows whose result the ranges
-// could have spoilt are then recomputed by the whole block.  A warp looks after
-// RW rows.
+// What the reading kernel left.  Block (g, part): the item that CTA g began and
+// did not end is joined from its pieces, in the line's order, a warp per row
+// (its lanes side by side over the channels), RW rows per warp; then rows whose
+// result the ranges could have spoilt, these and those CTA g finished, are
+// recomputed by the whole block.
 template <int FORMAT, int D>
 __global__ void __launch_bounds__(kExactThreads)
-    paged_finish_kernel(const PagedReadArgs a, const PagedSplit sp, int row_tile, int grid, int RW) {
-  constexpr int E = D / 32;  // channels per lane
+    paged_finish_kernel(const PagedReadArgs a, const PagedSplit sp, const SplitShape shape, int grid, int RW) {
+  constexpr int E = D / 32, kWarps = kExactThreads / 32;  // channels per lane
   __shared__ ExactShared sh;
-  __shared__ long long s_list[kExactThreads];
+  __shared__ int s_list[256];
   __shared__ int s_count;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const long long rows = static_cast<long long>(a.N) * a.Hq;
-  const long long first = (static_cast<long long>(blockIdx.x) * (kExactThreads / 32) + warp) * RW;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g0 = blockIdx.x, part = blockIdx.y;
+  const int row_tile = shape.row_tile;
   if (tid == 0) s_count = 0;
   __syncthreads();
   grid_dep_wait();
-  const uint32_t mine = lane < RW && first + lane < rows ? sp.todo[first + lane] : 0u;
+  const SplitRecord rec = sp.records[g0];
   const size_t size = piece_floats(row_tile, D);
-  for (unsigned mask = __ballot_sync(0xffffffffu, mine != 0u); mask; mask &= mask - 1) {
-    const int at = __ffs(mask) - 1;
-    const uint32_t word = __shfl_sync(0xffffffffu, mine, at);
-    const long long orow = first + at;
-    bool exact = word == kRowExact;
-    if (!exact) {
-      const int rr = (word >> 2) & 255, g0 = (word >> 10) & 1023, n = static_cast<int>(word >> 20);
-      // a word that a reading kernel which gave up left unwritten
-      if ((word & 3u) != kRowSplit || rr >= row_tile || n < 1 || g0 + n > grid) continue;
-      const int hq = static_cast<int>(orow % a.Hq), h = hq / a.group;
-      const float *base = sp.pieces + static_cast<size_t>(g0) * 2 * size;  // piece 0 in slot 1, the others in slot 0
-      auto piece = [&](int i) { return base + (static_cast<size_t>(i) * 2 + (i == 0 ? 1 : 0)) * size; };
-      // the first pieces' accumulators are on their way while the weights are formed
-      constexpr int kAhead = 4;
-      float v[kAhead][E];
-      auto load = [&](int i, float (&x)[E]) {
-        const float *p = piece(i) + static_cast<size_t>(rr) * D + lane * E;
-        if (E == 4) {
-          const float4 y = *reinterpret_cast<const float4 *>(p);
-          x[0] = y.x;
-          x[1] = y.y;
-          x[E - 2] = y.z;
-          x[E - 1] = y.w;
-        } else {
-          const float2 y = *reinterpret_cast<const float2 *>(p);
-          x[0] = y.x;
-          x[1] = y.y;
-        }
-      };
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i)
-        if (i < n) load(i, v[i]);
-      float beta[E], kind[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        beta[e] = a.beta ? __ldg(a.beta + static_cast<long long>(h) * D + lane * E + e) : 0.f;
-        kind[e] = piece(0)[row_tile * D + 2 * row_tile + lane * E + e];
-      }
-      float M = -INFINITY;
-      for (int i = lane; i < n; i += 32) M = fmaxf(M, piece(i)[row_tile * D + 2 * rr]);
+  const int n = rec.n;
+  if (n > 0) {
+    const SeqInfo si = paged_seq(a, rec.s);
+    const float *base = sp.pieces + static_cast<size_t>(g0) * 2 * size;  // piece 0 in slot 1, the others in slot 0
+    auto piece = [&](int i) { return (static_cast<size_t>(i) * 2 + (i == 0 ? 1 : 0)) * size; };
+    for (int k = 0; k < RW; ++k) {
+      const int rr = (part * kWarps + warp) * RW + k, h = rec.h;
+      if (rr >= rec.rows) break;
+      const int t = (rec.row0 + rr) / a.group, hq = h * a.group + (rec.row0 + rr) % a.group;
+      const long long orow = (static_cast<long long>(si.q0) + t) * a.Hq + hq;
+      const float *row = base + static_cast<size_t>(rr) * D + lane * E, *stat = base + row_tile * D + 2 * rr;
+      // lane: piece; then every lane its channels of one piece after the other
+      float M = -INFINITY, L = 0.f, wide = 0.f, acc[E];
+#pragma unroll 1
+      for (int i = lane; i < n; i += 32) M = fmaxf(M, stat[piece(i)]);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-      float acc[E], L = 0.f, wide = 0.f;
 #pragma unroll
       for (int e = 0; e < E; ++e) acc[e] = 0.f;
+#pragma unroll 1
       for (int i0 = 0; i0 < n; i0 += 32) {
         float w = 0.f;
         if (i0 + lane < n) {
-          const float *p = piece(i0 + lane);
-          const float m = p[row_tile * D + 2 * rr], l = p[row_tile * D + 2 * rr + 1];
+          const float m = stat[piece(i0 + lane)], l = stat[piece(i0 + lane) + 1];
           w = m == -INFINITY ? (l != l ? 1.f : 0.f) : ex2_approx(m - M);  // NaN scores have no maximum
           L += w * l;
-          wide += p[row_tile * D + 2 * row_tile + D];
+          wide += base[piece(i0 + lane) + row_tile * D + 2 * row_tile + D];
         }
         const int cnt = min(32, n - i0);
-        if (i0 == 0) {
-#pragma unroll
-          for (int i = 0; i < kAhead; ++i) {
-            const float wi = __shfl_sync(0xffffffffu, w, i);
-            if (i < n) {
-#pragma unroll
-              for (int e = 0; e < E; ++e) acc[e] = fmaf(wi, v[i][e], acc[e]);
-            }
-          }
-        }
-#pragma unroll 8
-        for (int i = i0 == 0 ? kAhead : 0; i < cnt; ++i) {
+#pragma unroll 4
+        for (int i = 0; i < cnt; ++i) {
           const float wi = __shfl_sync(0xffffffffu, w, i);
-          float x[E];
-          load(i0 + i, x);
+          const float2 *p = reinterpret_cast<const float2 *>(row + piece(i0 + i));
 #pragma unroll
-          for (int e = 0; e < E; ++e) acc[e] = fmaf(wi, x[e], acc[e]);
+          for (int e = 0; e < E; e += 2) {
+            const float2 x = p[e / 2];
+            acc[e] = fmaf(wi, x.x, acc[e]);
+            acc[e + 1] = fmaf(wi, x.y, acc[e + 1]);
+          }
         }
       }
 #pragma unroll
@@ -140,7 +106,9 @@ __global__ void __launch_bounds__(kExactThreads)
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         bool ok;
-        o[e] = paged_out(out_coef(beta[e], kind[e], a.beta && wide != 0.f), acc[e] / L, &ok);
+        const int j = lane * E + e;
+        const float beta = a.beta ? __ldg(a.beta + static_cast<long long>(h) * D + j) : 0.f;
+        o[e] = paged_out(out_coef(beta, base[piece(0) + row_tile * D + 2 * row_tile + j], a.beta && wide != 0.f), acc[e] / L, &ok);
         if (empty) o[e] = 0.f;
         good = good && (ok || empty);
       }
@@ -148,32 +116,50 @@ __global__ void __launch_bounds__(kExactThreads)
 #pragma unroll
       for (int e = 0; e < E; e += 2) dst[e / 2] = __floats2bfloat162_rn(o[e], o[e + 1]);
       if (lane == 0 && a.lse != nullptr) a.lse[orow] = empty ? -INFINITY : (M + log2f(L)) * kLn2;
-      exact = !__all_sync(0xffffffffu, good);
+      if (!__all_sync(0xffffffffu, good) && lane == 0) s_list[atomicAdd(&s_count, 1)] = rr;
     }
-    if (exact && lane == 0) s_list[atomicAdd(&s_count, 1)] = orow;
+    __syncthreads();
+    for (int i = 0; i < s_count; ++i) {
+      const int r = rec.row0 + s_list[i];
+      paged_exact_row<FORMAT>(a, rec.s, si, r / a.group, rec.h * a.group + r % a.group, sh);
+    }
   }
-  __syncthreads();
-  for (int i = 0; i < s_count; ++i) {
-    const long long orow = s_list[i];
-    const int row = static_cast<int>(orow / a.Hq), hq = static_cast<int>(orow - static_cast<long long>(row) * a.Hq);
-    const int s = paged_owner(a, row);
-    const SeqInfo si = paged_seq(a, s);
-    const int t = row - si.q0;
-    if (t >= 0 && t < si.n) paged_exact_row<FORMAT>(a, s, si, t, hq, sh);
+  if (rec.any_exact) {
+    // CTA g's whole items again, for their marked rows
+    __shared__ SplitScan<kExactThreads> scan;
+    SplitWalk walk;
+    SplitSeg sg;
+    if (!split_begin(a, shape, g0, grid, scan, walk)) return;
+    while (walk.next(a, shape, sg)) {
+      if (sg.kt0 != 0 || sg.kt1 != sg.kt_all) continue;
+      const int row0 = shape.tok ? sg.r * shape.tok * a.group : sg.r * row_tile;
+      const int rows = min(shape.tok ? shape.tok * a.group : row_tile, sg.si.n * a.group - row0);
+      // the rows this block looks after, a thread each (at most 256 / gridDim.y of them)
+      const int mine = part + tid * gridDim.y;
+      __syncthreads();
+      if (tid == 0) s_count = 0;
+      __syncthreads();
+      if (mine < rows) {
+        const int t = (row0 + mine) / a.group, hq = sg.h * a.group + (row0 + mine) % a.group;
+        if (sp.exact[(static_cast<long long>(sg.si.q0) + t) * a.Hq + hq]) s_list[atomicAdd(&s_count, 1)] = row0 + mine;
+      }
+      __syncthreads();
+      for (int i = 0; i < s_count; ++i)
+        paged_exact_row<FORMAT>(a, sg.s, sg.si, s_list[i] / a.group, sg.h * a.group + s_list[i] % a.group, sh);
+    }
   }
 }
 
 }  // namespace
 
 cudaError_t launch_paged_finish(const PagedReadArgs &a, const PagedSplit &sp, const SplitShape &shape, int grid,
-                                int num_sms, cudaStream_t stream) {
-  if (grid > kMaxSplitCtas || shape.row_tile > 256) return cudaErrorInvalidValue;
-  const long long rows = static_cast<long long>(a.N) * a.Hq;
-  // a row per warp while that is at most about one wave of blocks; then 8, most of which need nothing
-  const int warps = kExactThreads / 32, RW = rows <= 16ll * warps * num_sms ? 1 : 8;
-  const dim3 blocks(static_cast<unsigned>((rows + RW * warps - 1) / (RW * warps)));
+                                cudaStream_t stream) {
+  if (shape.row_tile > 256) return cudaErrorInvalidValue;
+  // a row per warp for the row tiles of few rows, two for those of 256
+  const int warps = kExactThreads / 32, RW = shape.row_tile > 16 ? 2 : 1;
+  const dim3 blocks(grid, shape.row_tile / (RW * warps));
   auto go = [&](auto kernel) {
-    return launch_kernel(kernel, blocks, dim3(kExactThreads), 0, stream, true, a, sp, shape.row_tile, grid, RW);
+    return launch_kernel(kernel, blocks, dim3(kExactThreads), 0, stream, true, a, sp, shape, grid, RW);
   };
   if (a.c.format == kCacheBf16)
     return a.c.d == 64 ? go(paged_finish_kernel<kCacheBf16, 64>) : go(paged_finish_kernel<kCacheBf16, 128>);

@@ -52,7 +52,8 @@ struct ChunkLayout {
   static constexpr uint32_t kRawV = kRawK + kRaw;
   static constexpr uint32_t kCtl = kRawV + kRaw;
   static constexpr uint32_t kShift = kCtl;                                // [kSegRing][D]
-  static constexpr uint32_t kInv = kShift + kSegRing * D * 4;             // [kInvRing]
+  static constexpr uint32_t kRecord = kShift + kSegRing * D * 4;
+  static constexpr uint32_t kInv = kRecord + sizeof(SplitRecord);         // [kInvRing]
   static constexpr uint32_t kWide = kInv + kInvRing * 4;                  // [kSegRing]: number (from 1) of the segment whose |E| went wide
   static constexpr uint32_t kScaleK = kWide + kSegRing * 4;  // e4m3: scale bytes of the staged keys, then values
   static constexpr uint32_t kScaleV = kScaleK + 128;
@@ -142,10 +143,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
 
   grid_dep_launch_dependents();
-  if (blockIdx.x == 0) split_mark_unowned<kChunkThreads>(a, sp.todo);
   const int cta = blockIdx.x;
   SplitWalk walk;
-  if (!split_begin(a, shape, cta, gridDim.x, scan, walk)) return;
+  SplitRecord &record = *reinterpret_cast<SplitRecord *>(smem + Lay::kRecord);
+  if (tid == 0) record = SplitRecord{};
+  if (!split_begin(a, shape, cta, gridDim.x, scan, walk)) {
+    if (tid == 0) sp.records[cta] = SplitRecord{};
+    return;
+  }
   if (warp == 12) {
     tmem_alloc(sbase + Lay::kTmem, 512);
     tmem_relinquish();
@@ -683,12 +688,24 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             piece[256 * D + 2 * ir] = m;
             piece[256 * D + 2 * ir + 1] = L;
           }
-          if (whole) sp.todo[w.orow] = good || empty ? kRowDone : kRowExact;
-          else if (sg.kt0 == 0) sp.todo[w.orow] = row_split(ir, cta, split_owner(walk.W, walk.G, sg.x_end - 1) - cta + 1);
+          if (whole) {
+            const bool exact = !good && !empty;
+            sp.exact[w.orow] = exact;
+            if (exact) record.any_exact = 1;
+          }
         }
         if (!whole && t == 0) {
           if (r < D) piece[256 * D + 512 + r] = shift[r];
-          if (r == 0) piece[256 * D + 512 + D] = wide ? 1.f : 0.f;
+          if (r == 0) {
+            piece[256 * D + 512 + D] = wide ? 1.f : 0.f;
+            if (sg.kt0 == 0) {
+              record.n = split_owner(walk.W, walk.G, sg.x_end - 1) - cta + 1;
+              record.s = sg.s;
+              record.h = sg.h;
+              record.row0 = cr.tok0 * a.group;
+              record.rows = cr.rows;
+            }
+          }
         }
         tc_fence_before_sync();  // the next segment's P E overwrite O, after this thread's next P arrives
       }
@@ -703,6 +720,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
 
   tc_fence_before_sync();
   __syncthreads();
+  if (tid == 0) sp.records[cta] = record;
   if (warp == 12) {
     tc_fence_after_sync();
     tmem_dealloc(tmem, 512);

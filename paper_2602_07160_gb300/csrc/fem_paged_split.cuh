@@ -176,15 +176,6 @@ __host__ __device__ __forceinline__ int split_owner(unsigned W, unsigned G, unsi
   return static_cast<int>((static_cast<unsigned long long>(x + 1) * G - 1) / W);
 }
 
-// Rows no sequence owns need nothing (rows from the first offset to the last are owned).
-template <int THREADS>
-__device__ __forceinline__ void split_mark_unowned(const PagedReadArgs &a, uint32_t *todo) {
-  const int first = min(max(__ldg(a.q_off), 0), a.N), last = min(max(__ldg(a.q_off + a.S), first), a.N);
-  for (long long i = threadIdx.x; i < static_cast<long long>(first) * a.Hq; i += THREADS) todo[i] = 0;
-  for (long long i = static_cast<long long>(last) * a.Hq + threadIdx.x; i < static_cast<long long>(a.N) * a.Hq; i += THREADS)
-    todo[i] = 0;
-}
-
 // An item and the key tiles kt0 .. kt1 - 1 of it (kt_all in the whole item).
 struct SplitSeg {
   SeqInfo si;
@@ -330,17 +321,19 @@ __host__ __device__ constexpr size_t piece_floats(int rows, int D) {
   return static_cast<size_t>(rows) * D + 2 * rows + D + 4;
 }
 
-// Per output row, what is left to do after the reading kernel, in one word: nothing, the exact
-// path, or a join of the n pieces of CTAs g0 .. g0 + n - 1, row rr of each.
-enum : uint32_t { kRowDone = 0, kRowExact = 1, kRowSplit = 2 };
-constexpr int kMaxSplitCtas = 1023;
-__device__ __forceinline__ uint32_t row_split(int rr, int g0, int n) {
-  return kRowSplit | (static_cast<uint32_t>(rr) << 2) | (static_cast<uint32_t>(g0) << 10) | (static_cast<uint32_t>(n) << 20);
-}
+// What a CTA leaves to the kernel that follows: the item it begins and does not end (n pieces, of
+// this CTA and the n - 1 after it; none: 0), and whether rows that it finished need the exact path.
+struct __align__(32) SplitRecord {
+  int n;
+  int s, h;        // the item's sequence and head
+  int row0, rows;  // its first row among the sequence's (token * group + head of the group), its rows
+  int any_exact;
+};
 
 struct PagedSplit {
-  float *pieces;  // two slots per CTA
-  uint32_t *todo;  // [N, Hq]
+  float *pieces;         // two slots per CTA
+  SplitRecord *records;  // per CTA
+  uint8_t *exact;        // [N, Hq]: 1 where a finished row needs the exact path (read where a record says so)
 };
 
 }  // namespace fem

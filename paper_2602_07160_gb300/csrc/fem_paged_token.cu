@@ -136,10 +136,14 @@ __global__ void __launch_bounds__(kTokThreads, 2)
     for (int st = 0; st < NS; ++st) mbar_init(bars + 8 * st, 1);
     fence_mbar_init();
   }
-  if (blockIdx.x == 0) split_mark_unowned<kTokThreads>(a, sp.todo);
   const int cta = blockIdx.x;
   SplitWalk walk;
-  if (!split_begin(a, shape, cta, gridDim.x, scan, walk)) return;
+  __shared__ SplitRecord record;
+  if (tid == 0) record = SplitRecord{};
+  if (!split_begin(a, shape, cta, gridDim.x, scan, walk)) {
+    if (tid == 0) sp.records[cta] = SplitRecord{};
+    return;
+  }
   SplitSeg sg;
   unsigned phases = 0;  // parity of each stage's barrier
   bool alive = true;
@@ -533,12 +537,21 @@ __global__ void __launch_bounds__(kTokThreads, 2)
     }
     fence_proxy_async_smem();  // the rings go back to the copies
     __syncthreads();
-    if (tid < n_rows && (whole || sg.kt0 == 0)) {
+    if (whole && tid < n_rows) {
       const int rr = row0 + tid, tok = rr / a.group, hq = sg.h * a.group + rr % a.group;
-      sp.todo[(static_cast<long long>(sg.si.q0) + tok) * a.Hq + hq] =
-          whole ? (s_bad[tid] ? kRowExact : kRowDone) : row_split(tid, cta, split_owner(walk.W, walk.G, sg.x_end - 1) - cta + 1);
+      sp.exact[(static_cast<long long>(sg.si.q0) + tok) * a.Hq + hq] = s_bad[tid] != 0;
+      if (s_bad[tid]) record.any_exact = 1;
+    }
+    if (!whole && sg.kt0 == 0 && tid == 0) {
+      record.n = split_owner(walk.W, walk.G, sg.x_end - 1) - cta + 1;
+      record.s = sg.s;
+      record.h = sg.h;
+      record.row0 = row0;
+      record.rows = n_rows;
     }
   }
+  __syncthreads();
+  if (tid == 0) sp.records[cta] = record;
 }
 
 }  // namespace
