@@ -876,7 +876,7 @@ int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride
   const int rows = static_cast<int>(std::min<long long>(static_cast<long long>(max_q) * a.group, 1 << 30));
   // few rows per head: the kernel that is bound by memory; more: the tensor cores
   const bool chunk = rows > kTokenRows && a.group <= 256;
-  const int grid = chunk ? ds->num_sms : 2 * ds->num_sms;
+  const int grid = chunk ? ds->num_sms : paged_token_ctas(a.c.format, a.c.d) * ds->num_sms;
   // whole tokens per row tile, a multiple of 8 where there are as many (the closed sum over row tiles is
   // then short: fem_paged_split.cuh)
   const int tok = 256 / a.group;

@@ -170,6 +170,7 @@ cudaError_t launch_paged_exact(const PagedReadArgs &a, cudaStream_t stream);
 // The read of few rows per sequence on `grid` CTAs that split the work evenly (fem_paged_split.cuh), for d = 64
 // and 128; tk, tv map the cache's k and v as [num_pages H, page_size, d] in boxes of 16 rows.  launch_paged_finish
 // follows on the same stream and joins what the CTAs' ends cut (a programmatic dependent launch).
+int paged_token_ctas(int format, int d);  // CTAs per SM, of which `grid` is to be a multiple
 cudaError_t launch_paged_token(const CUtensorMap &tk, const CUtensorMap &tv, const PagedReadArgs &a,
                                const PagedSplit &sp, const SplitShape &shape, int grid, cudaStream_t stream);
 // The same for many rows per sequence, on the tensor cores (tcgen05); tk, tv in boxes of box_rows rows.

@@ -37,6 +37,7 @@ constexpr float kTinyReach = 0.000244140625f;  // 2^-12: up to which it is tiny
 constexpr float kWideE = 1073741824.f;      // 2^30
 constexpr float kLeastA = 1.3552527e-20f;   // 2^-66
 constexpr float kMostA = 1.2980742e33f;     // 2^110
+constexpr float kDeepP = -100.f;            // log2 of a weight below which its term may be lost (the kernel that looks)
 constexpr float kLeastLinear = 0.25f;       // 1 + a of a linear channel: less cancels more than two bits
 
 // Scale D of a tiny channel, a power of two: |E| reaches 2^30 where beta |v| reaches 2^-8 (to a factor 2).

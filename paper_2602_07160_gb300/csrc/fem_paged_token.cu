@@ -35,7 +35,11 @@ struct TokLayout {
   static constexpr int kBox = kRow < 128 ? kRow : 128;         // bytes of a row in one TMA box
   static constexpr int kBoxes = kRow / kBox;
   static constexpr int kStage = 2 * kTokKeys * kRow;           // K and V of 16 keys
-  static constexpr int kStages = 24576 / kStage < 6 ? 24576 / kStage : 6;
+  // CTAs per SM, and the ring: at d = 128 in bf16 a key takes 512 bytes, and two CTAs with three stages
+  // keep more in flight than three with two (token_long: 106 us against 118); the others gain from the
+  // twelve warps (a batch over e4m3: 158 us against 185)
+  static constexpr int kCtas = kStage >= 8192 ? 2 : 3;
+  static constexpr int kStages = (kCtas == 2 ? 24576 : 16384) / kStage < 6 ? (kCtas == 2 ? 24576 : 16384) / kStage : 6;
   static constexpr int kRows = 8 * NT;
   static constexpr int kRedStride = D + 1;  // so that the lanes of a store to the join meet on two banks at most
   static_assert(kRows * kRedStride * 4 <= kStages * kStage, "a warp's ring holds its rows");
@@ -61,6 +65,14 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
                                          uint32_t b1) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                        uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -96,21 +108,18 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __int_as_float(static_cast<int>(w << 16)); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __int_as_float(static_cast<int>(w & 0xffff0000u)); }
 
-// Four e4m3 codes as two words of bf16 pairs, exactly.  The code's exponent and
-// fraction bits moved down four places read, as bf16, as the value times 2^-120.
-__device__ __forceinline__ uint2 e4m3x4_to_bf16(uint32_t x, uint32_t scale2) {
-  const uint32_t lo = __byte_perm(x, 0, 0x1404), hi = __byte_perm(x, 0, 0x3424);  // each code in the upper byte of a half
+// Four e4m3 codes as two words of f16 pairs, exactly.
+__device__ __forceinline__ uint2 e4m3x4_to_f16(uint32_t x) {
   uint2 r;
-  r.x = (lo & 0x80008000u) | ((lo & 0x7f007f00u) >> 4);
-  r.y = (hi & 0x80008000u) | ((hi & 0x7f007f00u) >> 4);
-  const __nv_bfloat162 k = *reinterpret_cast<const __nv_bfloat162 *>(&scale2);
-  __nv_bfloat162 a = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&r.x), k);
-  __nv_bfloat162 b = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&r.y), k);
-  return make_uint2(*reinterpret_cast<uint32_t *>(&a), *reinterpret_cast<uint32_t *>(&b));
+  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}"
+      : "=r"(r.x), "=r"(r.y)
+      : "r"(x));
+  return r;
 }
+__device__ __forceinline__ float2 f16x2_to_float2(uint32_t x) { return __half22float2(*reinterpret_cast<const __half2 *>(&x)); }
 
 template <int FORMAT, int D, int NT, bool BETA>
-__global__ void __launch_bounds__(kTokThreads, 2)
+__global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas))
     paged_token_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                        const PagedReadArgs a, const PagedSplit sp, const SplitShape shape) {
   using Lay = TokLayout<FORMAT, D, NT>;
@@ -168,6 +177,36 @@ __global__ void __launch_bounds__(kTokThreads, 2)
         const uint2 w = on ? *reinterpret_cast<const uint2 *>(qp + at) : make_uint2(0, 0);
         qf[t][kk][0] = w.x;
         qf[t][kk][1] = w.y;
+      }
+    }
+    // e4m3: codes are f16 numbers exactly, and the scores' product runs in f16.  A query row goes in times
+    // the power of two that brings its largest element to [2^7, 2^8); what f16 then loses of its smaller
+    // elements is under 2^-32 of that largest.  row_scale undoes it (columns 2 i, 2 i + 1).
+    float row_scale[NT][2];
+    if (FORMAT == kCacheE4m3) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        uint32_t top = 0;  // magnitudes of bf16 order as their bits
+#pragma unroll
+        for (int kk = 0; kk < MT; ++kk)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) top = max(top, max(qf[t][kk][u] & 0x7fffu, (qf[t][kk][u] >> 16) & 0x7fffu));
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        // exponent field of the scale: 127 + 7 - (x - 127) for a largest element of exponent field x (infinities
+        // and NaN stay what they are; a row of subnormals, far under any score, keeps a representable scale)
+        const int x = min(max(static_cast<int>(top >> 7), 8), 254);
+        const float sc = __int_as_float((261 - x) << 23);
+#pragma unroll
+        for (int kk = 0; kk < MT; ++kk)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const __half2 h = __floats2half2_rn(bf16_lo(qf[t][kk][u]) * sc, bf16_hi(qf[t][kk][u]) * sc);
+            qf[t][kk][u] = *reinterpret_cast<const uint32_t *>(&h);
+          }
+        const float undo = __int_as_float((x - 7) << 23);  // 2^(x - 134)
+        row_scale[t][0] = __shfl_sync(0xffffffffu, undo, 8 * i4);
+        row_scale[t][1] = __shfl_sync(0xffffffffu, undo, 8 * i4 + 4);
       }
     }
     // ---- this warp's stages: key groups kt * 4 + warp, kt0 <= kt < kt1, that hold a key
@@ -272,7 +311,7 @@ __global__ void __launch_bounds__(kTokThreads, 2)
       for (int u = 0; u < MT; ++u) acc[t][u][0] = acc[t][u][1] = acc[t][u][2] = acc[t][u][3] = 0.f;
     }
     const float qk_scale = a.scale * kLog2e;
-    __syncthreads();  // coefficients
+    const bool tiny = __syncthreads_or(BETA && tid < D && beta_c > 0.f && s_shift[tid] == INFINITY) != 0;  // coefficients
 
     for (int j = 0; j < n_st; ++j) {
       const int st = j % NS, key0 = ((sg.kt0 + j) * kTokWarps + warp) * kTokKeys;
@@ -300,7 +339,7 @@ __global__ void __launch_bounds__(kTokThreads, 2)
               }
             }
           } else {
-            // codes go in as their values (times 2^0); the keys' scales multiply the scores
+            // codes go in as their values; the keys' and rows' scales multiply the scores
             asm volatile("ld.shared.u8 %0, [%1];" : "=r"(ksc0) : "r"(scales + st * 32 + r0));
             asm volatile("ld.shared.u8 %0, [%1];" : "=r"(ksc1) : "r"(scales + st * 32 + r1));
 #pragma unroll
@@ -310,9 +349,9 @@ __global__ void __launch_bounds__(kTokThreads, 2)
               const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
               for (int u = 0; u < 4; ++u) {
-                const uint2 xa = e4m3x4_to_bf16(xs[u], 0x7b807b80u), ya = e4m3x4_to_bf16(ys[u], 0x7b807b80u);  // 2^120
+                const uint2 xa = e4m3x4_to_f16(xs[u]), ya = e4m3x4_to_f16(ys[u]);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) mma_bf16(sc[t], xa.x, ya.x, xa.y, ya.y, qf[t][4 * p + u][0], qf[t][4 * p + u][1]);
+                for (int t = 0; t < NT; ++t) mma_f16(sc[t], xa.x, ya.x, xa.y, ya.y, qf[t][4 * p + u][0], qf[t][4 * p + u][1]);
               }
             }
           }
@@ -322,10 +361,11 @@ __global__ void __launch_bounds__(kTokThreads, 2)
           bool raise = false;
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
-            sc[t][0] *= f0;
-            sc[t][1] *= f0;
-            sc[t][2] *= f1;
-            sc[t][3] *= f1;
+            const float c0 = FORMAT == kCacheE4m3 ? row_scale[t][0] : 1.f, c1 = FORMAT == kCacheE4m3 ? row_scale[t][1] : 1.f;
+            sc[t][0] *= f0 * c0;
+            sc[t][1] *= f0 * c1;
+            sc[t][2] *= f1 * c0;
+            sc[t][3] *= f1 * c1;
             if (tail) {
               if (key0 + r0 >= lim[t][0]) sc[t][0] = -INFINITY;
               if (key0 + r0 >= lim[t][1]) sc[t][1] = -INFINITY;
@@ -356,16 +396,26 @@ __global__ void __launch_bounds__(kTokThreads, 2)
           }
           // ---- P^T as the second operand of the second product
           uint32_t pf[NT][2];
+          bool deep = false;
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
             const float m0 = m[t][0] == -INFINITY ? 0.f : m[t][0], m1 = m[t][1] == -INFINITY ? 0.f : m[t][1];
-            const float p0 = ex2_approx(sc[t][0] - m0), p1 = ex2_approx(sc[t][1] - m1);
-            const float p2 = ex2_approx(sc[t][2] - m0), p3 = ex2_approx(sc[t][3] - m1);
+            const float x0 = sc[t][0] - m0, x1 = sc[t][1] - m1, x2 = sc[t][2] - m0, x3 = sc[t][3] - m1;
+            if (BETA) {
+              const float low = fminf(fminf(x0, x1), fminf(x2, x3));
+              if (low < kDeepP) {  // seldom, and then mostly keys that are not seen
+                deep = deep || (x0 < kDeepP && x0 > -INFINITY) || (x1 < kDeepP && x1 > -INFINITY) ||
+                       (x2 < kDeepP && x2 > -INFINITY) || (x3 < kDeepP && x3 > -INFINITY);
+              }
+            }
+            const float p0 = ex2_approx(x0), p1 = ex2_approx(x1), p2 = ex2_approx(x2), p3 = ex2_approx(x3);
             L[t][0] += p0 + p2;
             L[t][1] += p1 + p3;
             pf[t][0] = transpose8x8(pack_bf16(p0, p1));
             pf[t][1] = transpose8x8(pack_bf16(p2, p3));
           }
+          // |E| matters where weights come near the end of the range, or where a tiny channel could leave its own
+          const bool track = BETA && (tiny || __any_sync(0xffffffffu, deep));
           // ---- O^T += E^T P^T: the lane's keys are contraction indices 2 i, 2 i + 1, 2 i + 8, 2 i + 9
           int vr[4];
 #pragma unroll
@@ -389,6 +439,7 @@ __global__ void __launch_bounds__(kTokThreads, 2)
 #pragma unroll
           for (int pc = 0; pc < kPieces; ++pc) {
             uint32_t w[4][4];
+            uint2 vh[4];
             if (R128) {
               const int chunk = 8 * pc + (g >> 1) + 4 * (g & 1);
 #pragma unroll
@@ -412,6 +463,10 @@ __global__ void __launch_bounds__(kTokThreads, 2)
             for (int q = 0; q < kPer / 2; ++q) {  // pairs of channels: one row block of the product each
               uint32_t a0, a1, a2, a3;
               float lo[4], hi[4];
+              if (FORMAT == kCacheE4m3 && !(q & 1)) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) vh[u] = e4m3x4_to_f16(w[u][q >> 1]);
+              }
               if (FORMAT == kCacheBf16) {
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
@@ -421,9 +476,9 @@ __global__ void __launch_bounds__(kTokThreads, 2)
               } else {
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                  const float2 f = e4m3x2_to_float2((w[u][q >> 1] >> (16 * (q & 1))) & 0xffffu);
-                  lo[u] = f.x * vscale[u];
-                  hi[u] = f.y * vscale[u];
+                  const float2 f = __fmul2_rn(f16x2_to_float2(q & 1 ? vh[u].y : vh[u].x), make_float2(vscale[u], vscale[u]));
+                  lo[u] = f.x;
+                  hi[u] = f.y;
                 }
               }
               if (BETA) {
@@ -442,8 +497,10 @@ __global__ void __launch_bounds__(kTokThreads, 2)
                   for (int u = 0; u < 4; ++u)
                     if ((dead >> u) & 1u) lo[u] = hi[u] = 0.f;
                 }
+                if (track) {
 #pragma unroll
-                for (int u = 0; u < 4; ++u) emax = fmaxf(fmaxf(emax, fabsf(lo[u])), fabsf(hi[u]));
+                  for (int u = 0; u < 4; ++u) emax = fmaxf(fmaxf(emax, fabsf(lo[u])), fabsf(hi[u]));
+                }
               } else if (dead) {
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
@@ -568,6 +625,11 @@ static cudaError_t launch_token_n(const CUtensorMap &tk, const CUtensorMap &tv, 
   };
   return a.beta ? go(paged_token_kernel<FORMAT, D, NT, true>) : go(paged_token_kernel<FORMAT, D, NT, false>);
 }
+
+int paged_token_ctas(int format, int d) { return format == kCacheBf16 && d == 128 ? 2 : 3; }
+static_assert(TokLayout<kCacheBf16, 128, 1>::kCtas == 2 && TokLayout<kCacheBf16, 64, 1>::kCtas == 3 &&
+                  TokLayout<kCacheE4m3, 128, 1>::kCtas == 3 && TokLayout<kCacheE4m3, 64, 1>::kCtas == 3,
+              "paged_token_ctas");
 
 cudaError_t launch_paged_token(const CUtensorMap &tk, const CUtensorMap &tv, const PagedReadArgs &a,
                                const PagedSplit &sp, const SplitShape &shape, int grid, cudaStream_t stream) {
