@@ -83,15 +83,19 @@ __global__ void __launch_bounds__(kExactThreads)
           wide += base[piece(i0 + lane) + row_tile * D + 2 * row_tile + D];
         }
         const int cnt = min(32, n - i0);
-#pragma unroll 4
+#pragma unroll 8
         for (int i = 0; i < cnt; ++i) {
           const float wi = __shfl_sync(0xffffffffu, w, i);
-          const float2 *p = reinterpret_cast<const float2 *>(row + piece(i0 + i));
-#pragma unroll
-          for (int e = 0; e < E; e += 2) {
-            const float2 x = p[e / 2];
-            acc[e] = fmaf(wi, x.x, acc[e]);
-            acc[e + 1] = fmaf(wi, x.y, acc[e + 1]);
+          if (E == 4) {
+            const float4 x = *reinterpret_cast<const float4 *>(row + piece(i0 + i));
+            acc[0] = fmaf(wi, x.x, acc[0]);
+            acc[1] = fmaf(wi, x.y, acc[1]);
+            acc[E - 2] = fmaf(wi, x.z, acc[E - 2]);
+            acc[E - 1] = fmaf(wi, x.w, acc[E - 1]);
+          } else {
+            const float2 x = *reinterpret_cast<const float2 *>(row + piece(i0 + i));
+            acc[0] = fmaf(wi, x.x, acc[0]);
+            acc[1] = fmaf(wi, x.y, acc[1]);
           }
         }
       }

@@ -39,29 +39,35 @@ namespace {
 constexpr int kChunkThreads = 512;
 constexpr int kChunkKeys = 128;
 constexpr int kInvRing = 8;   // key tiles whose missing pages are remembered
-constexpr int kSegRing = 4;   // segments whose channel shifts are remembered: at most three are alive
 
 template <int FORMAT, int D>
 struct ChunkLayout {
   static constexpr uint32_t kTile = 128 * D * 2;
   static constexpr uint32_t kRaw = FORMAT == kCacheE4m3 ? 128 * D : 0;  // a staging tile of codes
+  // bank stages: a third lets the copies of V and the bank's warps run ahead of the products (e4m3 at
+  // d = 128 has no room for it beside the staging tiles, which hold a tile more themselves)
+  static constexpr int kES = FORMAT == kCacheE4m3 ? 2 : 3;
+  // Segments whose channels' kinds are remembered.  When the bank's warps begin a segment, the product kES
+  // tiles back is done; so at most the segments of the kES tiles from that one on, their own, and one
+  // before them, which a row tile out of use since may still be writing out, are alive.
+  static constexpr int kSegRing = kES + 2;
   static constexpr uint32_t kQ = 0;
   static constexpr uint32_t kK = 2 * kTile;
   static constexpr uint32_t kE = kK + 2 * kTile;
-  static constexpr uint32_t kRawK = kE + 2 * kTile;
+  static constexpr uint32_t kRawK = kE + kES * kTile;
   static constexpr uint32_t kRawV = kRawK + kRaw;
   static constexpr uint32_t kCtl = kRawV + kRaw;
   static constexpr uint32_t kShift = kCtl;                                // [kSegRing][D]
   static constexpr uint32_t kRecord = kShift + kSegRing * D * 4;
   static constexpr uint32_t kInv = kRecord + sizeof(SplitRecord);         // [kInvRing]
   static constexpr uint32_t kWide = kInv + kInvRing * 4;                  // [kSegRing]: number (from 1) of the segment whose |E| went wide
-  static constexpr uint32_t kScaleK = kWide + kSegRing * 4;  // e4m3: scale bytes of the staged keys, then values
-  static constexpr uint32_t kScaleV = kScaleK + 128;
-  static constexpr uint32_t kBars = kScaleV + 128;
-  static constexpr uint32_t kNumBars = 24;
+  static constexpr uint32_t kScaleK = (kWide + kSegRing * 4 + 15) & ~15u;  // e4m3: scale bytes of the staged keys, then values
+  static constexpr uint32_t kScaleV = kScaleK + (FORMAT == kCacheE4m3 ? 128 : 0);
+  static constexpr uint32_t kBars = (kScaleV + (FORMAT == kCacheE4m3 ? 128 : 0) + 7) & ~7u;
+  static constexpr uint32_t kNumBars = 25;
   static constexpr uint32_t kTmem = kBars + kNumBars * 8;
   static constexpr uint32_t kAbort = kTmem + 4;
-  static constexpr uint32_t kScan = kAbort + 4;
+  static constexpr uint32_t kScan = (kAbort + 4 + 7) & ~7u;
   static constexpr uint32_t kBytes = kScan + sizeof(SplitScan<kChunkThreads>);
   static_assert(kBytes <= 227 * 1024, "shared memory");
 };
@@ -70,17 +76,17 @@ enum : int {
   kCbQ = 0,        // + row tile: its queries are in shared memory (128 arrivals)
   kCbKFull = 2,    // + stage: K as bf16 (TMA, or 128 arrivals of the bank warps)
   kCbKEmpty = 4,   // + stage: both S of the tile are done
-  kCbVFull = 6,    // + stage: V as TMA brought it (bf16)
-  kCbEFull = 8,    // + stage: the bank (128 arrivals)
-  kCbEEmpty = 10,  // + stage: both P E of the tile are done
-  kCbRawKFull = 12,
-  kCbRawVFull = 13,
-  kCbRawKEmpty = 14,  // 128 arrivals
-  kCbRawVEmpty = 15,
-  kCbS = 16,       // + row tile: S is in TMEM
-  kCbP = 18,       // + row tile: P is in TMEM (128 arrivals)
-  kCbO = 20,       // every product of the segment is done
-  kCbDone = 21,    // every product this CTA issued is done
+  kCbVFull = 6,    // + bank stage: V as TMA brought it (bf16)
+  kCbEFull = 9,    // + bank stage: the bank (128 arrivals)
+  kCbEEmpty = 12,  // + bank stage: both P E of the tile are done
+  kCbRawKFull = 15,
+  kCbRawVFull = 16,
+  kCbRawKEmpty = 17,  // 128 arrivals
+  kCbRawVEmpty = 18,
+  kCbS = 19,       // + row tile: S is in TMEM
+  kCbP = 21,       // + row tile: P is in TMEM (128 arrivals)
+  kCbO = 23,       // every product of the segment is done
+  kCbDone = 24,    // every product this CTA issued is done
 };
 
 __device__ __forceinline__ bool chunk_wait(uint32_t bar, uint32_t parity, unsigned *err, unsigned code,
@@ -130,6 +136,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                        const PagedReadArgs a, const PagedSplit sp, const SplitShape shape, int box_shift) {
   using Lay = ChunkLayout<FORMAT, D>;
   constexpr bool kCodes = FORMAT == kCacheE4m3;
+  constexpr unsigned kES = Lay::kES, kSegRing = Lay::kSegRing;
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t sbase = smem_u32(smem);
   const uint32_t bars = sbase + Lay::kBars;
@@ -160,11 +167,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       mbar_init(FEM_CB(kCbQ + i), 128);
       mbar_init(FEM_CB(kCbKFull + i), kCodes ? 128 : 1);
       mbar_init(FEM_CB(kCbKEmpty + i), 1);
+      mbar_init(FEM_CB(kCbS + i), 1);
+      mbar_init(FEM_CB(kCbP + i), 128);
+    }
+    for (unsigned i = 0; i < kES; ++i) {
       mbar_init(FEM_CB(kCbVFull + i), 1);
       mbar_init(FEM_CB(kCbEFull + i), 128);
       mbar_init(FEM_CB(kCbEEmpty + i), 1);
-      mbar_init(FEM_CB(kCbS + i), 1);
-      mbar_init(FEM_CB(kCbP + i), 128);
     }
     mbar_init(FEM_CB(kCbRawKFull), 1);
     mbar_init(FEM_CB(kCbRawVFull), 1);
@@ -174,7 +183,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     mbar_init(FEM_CB(kCbDone), 1);
     fence_mbar_init();
     *abort_flag = 0;
-    for (int i = 0; i < kSegRing; ++i) s_wide[i] = 0;
+    for (unsigned i = 0; i < kSegRing; ++i) s_wide[i] = 0;
   }
   tc_fence_before_sync();
   __syncthreads();
@@ -195,8 +204,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     bool ok = true;
     while (ok && walk.next(a, shape, sg)) {
       for (int kt = sg.kt0; ok && kt < sg.kt1; ++kt, ++n) {
-        const int st = n & 1;
-        const unsigned use = n >> 1;
+        const unsigned st = n & 1, use = n >> 1, es = n % kES, euse = n / kES;
         // lane b: box b of the tile
         const int key = kt * kChunkKeys + lane * box_rows;
         const bool wanted = lane < boxes && key < sg.si.ctx;
@@ -225,20 +233,21 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         } else {
           if (use > 0) ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbKEmpty + st), (use - 1) & 1, a.err, kErrWaitMma, abort_flag));
           if (ok) load(&tmap_k, sbase + Lay::kK + st * Lay::kTile, FEM_CB(kCbKFull + st), 0, nullptr);
-          if (ok && use > 0) ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbEEmpty + st), (use - 1) & 1, a.err, kErrWaitMma, abort_flag));
-          if (ok) load(&tmap_v, sbase + Lay::kE + st * Lay::kTile, FEM_CB(kCbVFull + st), 0, nullptr);
+          if (ok && euse > 0) ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbEEmpty + es), (euse - 1) & 1, a.err, kErrWaitMma, abort_flag));
+          if (ok) load(&tmap_v, sbase + Lay::kE + es * Lay::kTile, FEM_CB(kCbVFull + es), 0, nullptr);
         }
       }
     }
     if (!ok && lane == 0) {
-      // another role gave up: the copies in flight land before the block ends (tiles n - 1 and n at most)
-      for (int i = 0; i < 2; ++i) {
-        const unsigned t = n + 1 - i;  // tile t - 1
-        if (t == 0) continue;
-        const unsigned par = kCodes ? ((t - 1) & 1) : (((t - 1) >> 1) & 1);
-        const int st = (t - 1) & 1;
-        mbar_wait_for(FEM_CB(kCodes ? kCbRawKFull : kCbKFull + st), par, a.err, kErrWaitTma, 100000000ull);
-        mbar_wait_for(FEM_CB(kCodes ? kCbRawVFull : kCbVFull + st), par, a.err, kErrWaitTma, 100000000ull);
+      // another role gave up: the copies in flight land before the block ends (the last few tiles')
+      for (unsigned t = n + 1 > kES ? n + 1 - kES : 0; t <= n; ++t) {
+        if (kCodes) {
+          mbar_wait_for(FEM_CB(kCbRawKFull), t & 1, a.err, kErrWaitTma, 100000000ull);
+          mbar_wait_for(FEM_CB(kCbRawVFull), t & 1, a.err, kErrWaitTma, 100000000ull);
+        } else {
+          mbar_wait_for(FEM_CB(kCbKFull + (t & 1)), (t >> 1) & 1, a.err, kErrWaitTma, 100000000ull);
+          mbar_wait_for(FEM_CB(kCbVFull + t % kES), (t / kES) & 1, a.err, kErrWaitTma, 100000000ull);
+        }
       }
     }
   } else if (warp == 13) {
@@ -267,7 +276,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           if (!(ok = wait(kCbKFull + (i & 1), i >> 1, kErrWaitTma))) break;
         }
         if (k > 0) {
-          if (!(ok = wait(kCbEFull + (e & 1), e >> 1, kErrWaitMma))) break;
+          if (!(ok = wait(kCbEFull + e % kES, e / kES, kErrWaitMma))) break;
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -277,13 +286,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             if (!(ok = wait(kCbP + t, t ? np1 : np0, kErrWaitMma))) break;
             if (t) ++np1; else ++np0;
             tc_fence_after_sync();
-            const uint64_t de = desc_e + (e & 1) * (Lay::kTile >> 4);
+            const uint64_t de = desc_e + (e % kES) * (Lay::kTile >> 4);
             if (leader) {
 #pragma unroll
               for (int kk = 0; kk < 8; ++kk)
                 mma_f16_ts(tmem + 256 + t * D, tmem + t * 128 + kk * 8, de + ((kk * 2048) >> 4), idesc_o,
                            (k > 1 || kk > 0) ? 1u : 0u);
-              if (t == tiles - 1) mma_commit(FEM_CB(kCbEEmpty + (e & 1)));
+              if (t == tiles - 1) mma_commit(FEM_CB(kCbEEmpty + e % kES));
             }
           }
           if (k < nk) {
@@ -383,17 +392,16 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       float emax = 0.f;
       bool wrote = false;  // this segment's shifts, once its first stage is free
       for (int kt = sg.kt0; ok && kt < sg.kt1; ++kt, ++n) {
-        const int st = n & 1;
-        const unsigned use = n >> 1;
+        const unsigned st = n & 1, use = n >> 1, es = n % kES, euse = n / kES;
         const int k0 = kt * kChunkKeys;
-        uint8_t *tE = smem + Lay::kE + st * Lay::kTile;
+        uint8_t *tE = smem + Lay::kE + es * Lay::kTile;
         if (kCodes) {
           // K: codes to bf16
           ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbRawKFull), n & 1, a.err, kErrWaitTma, abort_flag));
           if (ok && use > 0) ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbKEmpty + st), (use - 1) & 1, a.err, kErrWaitMma, abort_flag));
           if (!ok) break;
         } else {
-          ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbVFull + st), use & 1, a.err, kErrWaitTma, abort_flag));
+          ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbVFull + es), euse & 1, a.err, kErrWaitTma, abort_flag));
           if (!ok) break;
         }
         const unsigned inv = s_inv[n % kInvRing];
@@ -427,11 +435,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           mbar_arrive(FEM_CB(kCbKFull + st));
           mbar_arrive(FEM_CB(kCbRawKEmpty));
           ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbRawVFull), n & 1, a.err, kErrWaitTma, abort_flag));
-          if (ok && use > 0) ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbEEmpty + st), (use - 1) & 1, a.err, kErrWaitMma, abort_flag));
+          if (ok && euse > 0) ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbEEmpty + es), (euse - 1) & 1, a.err, kErrWaitMma, abort_flag));
           if (!ok) break;
         }
         if (!wrote) {
-          // the stage is free: of earlier segments at most two are not yet written out (see kSegRing)
+          // the stage is free: see kSegRing
           wrote = true;
           if (rl == 0 && cc < kChunks) {
 #pragma unroll
@@ -481,7 +489,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           if (BETA && emax > kWideE) s_wide[seg % kSegRing] = static_cast<int>(seg + 1);
         }
         fence_proxy_async_smem();
-        mbar_arrive(FEM_CB(kCbEFull + st));
+        mbar_arrive(FEM_CB(kCbEFull + es));
         if (kCodes) mbar_arrive(FEM_CB(kCbRawVEmpty));
       }
       ++seg;
