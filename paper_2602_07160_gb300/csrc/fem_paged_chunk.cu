@@ -6,18 +6,21 @@
 // are two tiles of 128 that share every key tile, so the value bank is formed
 // once for both and each tile's softmax runs under the other's products:
 //
-//   warps 0-3    bank: the key tile's values (TMA, 128-byte swizzle) become E(v) in
+//   warps 0-7    bank: the key tile's values (TMA, 128-byte swizzle) become E(v) in
 //                place; e4m3 keys and values are widened to bf16 from a staging
 //                tile.  Rows past the sequence, or of pages that are not there,
 //                become zeros
-//   warps 4-7    softmax of row tile 0 (thread = row): S from TMEM, P = 2^(s - m)
-//                as bf16 over the first 64 columns of S, the row sum, the lazily
-//                raised maximum (and, when it moves, the accumulator's rescale);
-//                the rows' queries into shared memory at an item's start, their
-//                output or piece at its end
-//   warps 8-11   the same for row tile 1
-//   warp 12      TMA of K and V, one box per page (or part of a page) of the tile
-//   warp 13      issues the products: S0 = Q0 K^T, S1 = Q1 K^T, then for
+//   warps 8-15   softmax of row tile 0, two threads per row (64 keys each): S from
+//                TMEM, P = 2^(s - m) as bf16 over the first 32 of their 64 columns of S,
+//                the row's sum; the rows' queries into shared memory at an item's start,
+//                their output or piece at its end.  A tile's chain S, softmax, P E, S is
+//                what the pace hangs on.  The maximum m need only keep P in range, and
+//                bf16's is fp32's: it is found once, in a segment's first tile, and raised
+//                when a tile's weights sum to over 2^40, at the tile after (then O is
+//                rescaled), so that the two threads never wait for each other in between
+//   warps 16-23  the same for row tile 1
+//   warp 24      TMA of K and V, one box per page (or part of a page) of the tile
+//   warp 25      issues the products: S0 = Q0 K^T, S1 = Q1 K^T, then for
 //                each tile, once its P is written, O += P E and the next S.  The
 //                tensor pipe takes them in the order issued, so S of the next key
 //                tile may overwrite a P whose product was issued before it, and
@@ -36,8 +39,10 @@ namespace fem {
 
 namespace {
 
-constexpr int kChunkThreads = 512;
+constexpr int kChunkThreads = 896;
 constexpr int kChunkKeys = 128;
+constexpr int kBankThreads = 256;
+constexpr float kAskSum = 1.0995116e12f;  // 2^40
 constexpr int kInvRing = 8;   // key tiles whose missing pages are remembered
 
 template <int FORMAT, int D>
@@ -57,14 +62,16 @@ struct ChunkLayout {
   static constexpr uint32_t kRawK = kE + kES * kTile;
   static constexpr uint32_t kRawV = kRawK + kRaw;
   static constexpr uint32_t kCtl = kRawV + kRaw;
-  static constexpr uint32_t kShift = kCtl;                                // [kSegRing][D]
-  static constexpr uint32_t kRecord = kShift + kSegRing * D * 4;
+  static constexpr uint32_t kShift = kCtl;                       // channels' kinds, 16 bits, [kSegRing][D]
+  static constexpr uint32_t kRow = kShift + kSegRing * D * 2;  // what the threads of a row exchange: 4 bytes per row
+  static constexpr uint32_t kAsk = kRow + 2 * 128 * 4;         // per pair of warps and half: see the softmax
+  static constexpr uint32_t kRecord = kAsk + 16 * 4;
   static constexpr uint32_t kInv = kRecord + sizeof(SplitRecord);         // [kInvRing]
   static constexpr uint32_t kWide = kInv + kInvRing * 4;                  // [kSegRing]: number (from 1) of the segment whose |E| went wide
   static constexpr uint32_t kScaleK = (kWide + kSegRing * 4 + 15) & ~15u;  // e4m3: scale bytes of the staged keys, then values
   static constexpr uint32_t kScaleV = kScaleK + (FORMAT == kCacheE4m3 ? 128 : 0);
   static constexpr uint32_t kBars = (kScaleV + (FORMAT == kCacheE4m3 ? 128 : 0) + 7) & ~7u;
-  static constexpr uint32_t kNumBars = 25;
+  static constexpr uint32_t kNumBars = 33;
   static constexpr uint32_t kTmem = kBars + kNumBars * 8;
   static constexpr uint32_t kAbort = kTmem + 4;
   static constexpr uint32_t kScan = (kAbort + 4 + 7) & ~7u;
@@ -73,20 +80,21 @@ struct ChunkLayout {
 };
 
 enum : int {
-  kCbQ = 0,        // + row tile: its queries are in shared memory (128 arrivals)
-  kCbKFull = 2,    // + stage: K as bf16 (TMA, or 128 arrivals of the bank warps)
+  kCbQ = 0,        // + row tile: its queries are in shared memory (256 arrivals)
+  kCbKFull = 2,    // + stage: K as bf16 (TMA, or an arrival of each bank thread)
   kCbKEmpty = 4,   // + stage: both S of the tile are done
   kCbVFull = 6,    // + bank stage: V as TMA brought it (bf16)
-  kCbEFull = 9,    // + bank stage: the bank (128 arrivals)
+  kCbEFull = 9,    // + bank stage: the bank (an arrival of each of its threads)
   kCbEEmpty = 12,  // + bank stage: both P E of the tile are done
   kCbRawKFull = 15,
   kCbRawVFull = 16,
-  kCbRawKEmpty = 17,  // 128 arrivals
+  kCbRawKEmpty = 17,  // an arrival of each bank thread
   kCbRawVEmpty = 18,
   kCbS = 19,       // + row tile: S is in TMEM
-  kCbP = 21,       // + row tile: P is in TMEM (128 arrivals)
+  kCbP = 21,       // + row tile: P is in TMEM (256 arrivals)
   kCbO = 23,       // every product of the segment is done
   kCbDone = 24,    // every product this CTA issued is done
+  kCbPair = 25,    // + pair of softmax warps (64 arrivals)
 };
 
 __device__ __forceinline__ bool chunk_wait(uint32_t bar, uint32_t parity, unsigned *err, unsigned code,
@@ -104,11 +112,41 @@ __device__ __forceinline__ bool chunk_wait(uint32_t bar, uint32_t parity, unsign
   }
 }
 
+// tcgen05.mma and its commit by the one thread with leader != 0, in code that the whole warp runs: the
+// operands are then formed once per warp, in uniform registers.
+__device__ __forceinline__ void mma_ss(uint32_t leader, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc),
+      "r"(leader)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t leader, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc),
+      "r"(leader)
+      : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t leader, uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(leader)
+      : "memory");
+}
+
 // True in one thread of the warp, always the same one.
-__device__ __forceinline__ bool elect_one() {
+__device__ __forceinline__ uint32_t elect_one() {
   uint32_t r;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
-  return r != 0;
+  return r;
+}
+
+// max(|a|, |b|, |c|)
+__device__ __forceinline__ float fmax3_abs(float a, float b, float c) {
+  float r;
+  asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -143,7 +181,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
 #define FEM_CB(i) (bars + 8u * static_cast<uint32_t>(i))
   volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + Lay::kAbort);
   SplitScan<kChunkThreads> &scan = *reinterpret_cast<SplitScan<kChunkThreads> *>(smem + Lay::kScan);
-  float *s_shift = reinterpret_cast<float *>(smem + Lay::kShift);
+  short *s_shift = reinterpret_cast<short *>(smem + Lay::kShift);
   volatile unsigned *s_inv = reinterpret_cast<volatile unsigned *>(smem + Lay::kInv);
   volatile int *s_wide = reinterpret_cast<volatile int *>(smem + Lay::kWide);
   const int box_rows = 1 << box_shift;
@@ -158,32 +196,34 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     if (tid == 0) sp.records[cta] = SplitRecord{};
     return;
   }
-  if (warp == 12) {
+  if (warp == 24) {
     tmem_alloc(sbase + Lay::kTmem, 512);
     tmem_relinquish();
   }
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(FEM_CB(kCbQ + i), 128);
-      mbar_init(FEM_CB(kCbKFull + i), kCodes ? 128 : 1);
+      mbar_init(FEM_CB(kCbQ + i), 256);
+      mbar_init(FEM_CB(kCbKFull + i), kCodes ? kBankThreads : 1);
       mbar_init(FEM_CB(kCbKEmpty + i), 1);
       mbar_init(FEM_CB(kCbS + i), 1);
-      mbar_init(FEM_CB(kCbP + i), 128);
+      mbar_init(FEM_CB(kCbP + i), 256);
     }
     for (unsigned i = 0; i < kES; ++i) {
       mbar_init(FEM_CB(kCbVFull + i), 1);
-      mbar_init(FEM_CB(kCbEFull + i), 128);
+      mbar_init(FEM_CB(kCbEFull + i), kBankThreads);
       mbar_init(FEM_CB(kCbEEmpty + i), 1);
     }
+    for (int i = 0; i < 8; ++i) mbar_init(FEM_CB(kCbPair + i), 64);
     mbar_init(FEM_CB(kCbRawKFull), 1);
     mbar_init(FEM_CB(kCbRawVFull), 1);
-    mbar_init(FEM_CB(kCbRawKEmpty), 128);
-    mbar_init(FEM_CB(kCbRawVEmpty), 128);
+    mbar_init(FEM_CB(kCbRawKEmpty), kBankThreads);
+    mbar_init(FEM_CB(kCbRawVEmpty), kBankThreads);
     mbar_init(FEM_CB(kCbO), 1);
     mbar_init(FEM_CB(kCbDone), 1);
     fence_mbar_init();
     *abort_flag = 0;
     for (unsigned i = 0; i < kSegRing; ++i) s_wide[i] = 0;
+    for (int i = 0; i < 16; ++i) reinterpret_cast<unsigned *>(smem + Lay::kAsk)[i] = 0u;  // tiles count from 1
   }
   tc_fence_before_sync();
   __syncthreads();
@@ -191,10 +231,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(smem + Lay::kTmem);
   SplitSeg sg;
 
-  // The block's registers are 512 x 128; the softmax warps take 168 each, the bank's 104, the others 72:
-  // 256 x 168 + 128 x 104 + 128 x 72 = 512 x 128.
-  if (warp >= 12) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-  if (warp == 12) {
+  // The block's registers are 896 x 72; the softmax warps take 88 each, the bank's 56, the others 40:
+  // 512 x 88 + 256 x 56 + 128 x 40 = 896 x 72.
+  if (warp >= 24) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+  if (warp == 24) {
     // ------------------------------------------------------------ TMA of K and V
     const int boxes = kChunkKeys / box_rows;
     constexpr int kCols = kCodes ? (D < 128 ? D : 128) : 64;  // elements of a box's row
@@ -250,7 +290,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         }
       }
     }
-  } else if (warp == 13) {
+  } else if (warp == 25) {
     // ------------------------------------------------------------ products
     // The whole warp walks the loop and one elected thread issues: the loop then stays uniform, and the
     // operands' descriptors are sums of per-tile bases and constants in uniform registers.  With one
@@ -260,7 +300,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     constexpr uint32_t idesc_o = idesc_f16(128, D, true, true);
     const uint64_t desc_q = smem_desc_sw128(sbase + Lay::kQ, 16, 1024), desc_k = smem_desc_sw128(sbase + Lay::kK, 16, 1024);
     const uint64_t desc_e = smem_desc_sw128(sbase + Lay::kE, 16384, 1024);
-    const bool leader = elect_one();
+    const uint32_t leader = elect_one();
     unsigned n = 0, np0 = 0, np1 = 0, seg = 0;  // key tiles, P of each row tile, segments so far
     bool ok = true;
     auto wait = [&](int bar, unsigned parity, unsigned code) {
@@ -287,30 +327,26 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             if (t) ++np1; else ++np0;
             tc_fence_after_sync();
             const uint64_t de = desc_e + (e % kES) * (Lay::kTile >> 4);
-            if (leader) {
 #pragma unroll
-              for (int kk = 0; kk < 8; ++kk)
-                mma_f16_ts(tmem + 256 + t * D, tmem + t * 128 + kk * 8, de + ((kk * 2048) >> 4), idesc_o,
-                           (k > 1 || kk > 0) ? 1u : 0u);
-              if (t == tiles - 1) mma_commit(FEM_CB(kCbEEmpty + e % kES));
-            }
+            for (int kk = 0; kk < 8; ++kk)
+              mma_ts(leader, tmem + 256 + t * D, tmem + t * 128 + (kk >> 2) * 64 + (kk & 3) * 8, de + ((kk * 2048) >> 4), idesc_o,
+                     (k > 1 || kk > 0) ? 1u : 0u);
+            if (t == tiles - 1) commit(leader, FEM_CB(kCbEEmpty + e % kES));
           }
           if (k < nk) {
             tc_fence_after_sync();
             const uint64_t dq = desc_q + t * (Lay::kTile >> 4), dk = desc_k + (i & 1) * (Lay::kTile >> 4);
-            if (leader) {
 #pragma unroll
-              for (int kk = 0; kk < D / 16; ++kk) {
-                const uint32_t off = ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
-                mma_f16_ss(tmem + t * 128, dq + off, dk + off, idesc_s, kk > 0 ? 1u : 0u);
-              }
-              mma_commit(FEM_CB(kCbS + t));
-              if (t == tiles - 1) mma_commit(FEM_CB(kCbKEmpty + (i & 1)));
+            for (int kk = 0; kk < D / 16; ++kk) {
+              const uint32_t off = ((kk >> 2) * 16384 + (kk & 3) * 32) >> 4;
+              mma_ss(leader, tmem + t * 128, dq + off, dk + off, idesc_s, kk > 0 ? 1u : 0u);
             }
+            commit(leader, FEM_CB(kCbS + t));
+            if (t == tiles - 1) commit(leader, FEM_CB(kCbKEmpty + (i & 1)));
           }
         }
       }
-      if (ok && leader) mma_commit(FEM_CB(kCbO));
+      if (ok) commit(leader, FEM_CB(kCbO));
       n += nk;
       ++seg;
     }
@@ -319,30 +355,34 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       // nothing may be in flight when TMEM is freed
       mbar_wait(FEM_CB(kCbDone), 0, a.err, kErrWaitMma);
     }
-  } else if (warp < 4) {
+  } else if (warp < 8) {
     // ------------------------------------------------------------ the bank
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-    const int rl = tid & 7, cc = tid >> 3;  // rows rl, rl + 8, ...; 16-byte chunk cc (of bf16)
-    constexpr int kChunks = D / 8;          // per row: 16 at D = 128, 8 at D = 64 (then two row groups)
-    const int col = cc % kChunks, r_first = rl + 8 * (cc / kChunks);
-    constexpr int kRowStep = 8 * (16 / kChunks), kRowsEach = 128 / kRowStep;
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    // A thread has 4 channels (8 bytes of bf16) of every kRowStep-th row: the lanes of a half warp the two
+    // halves of one 16-byte chunk in 8 rows, which the swizzle keeps on distinct banks.
+    const int rl = tid & 7, col = (tid >> 3) % (D / 4);
+    constexpr int kRowStep = kBankThreads / (D / 4), kRowsEach = 128 / kRowStep;
+    const int r_first = rl + 8 * ((tid >> 3) / (D / 4));
     constexpr int kBatch = 4;
-    // the thread's 8 codes of a row in a staging tile
-    auto raw_offset = [&](int r) {
-      return D == 128 ? sw128_offset(r, col >> 1) + 8 * (col & 1) : r * 64 + (((col >> 1) ^ ((r >> 1) & 3)) << 4) + 8 * (col & 1);
-    };
-    float2 cb[4], cs[4], ci[4], cd[4];  // the thread's channels, in pairs
+    // The thread's 4 codes of its first row in a staging tile, and its 4 elements in a tile of bf16; its rows
+    // are a multiple of 8 apart, so they share the swizzle's pattern and lie at a fixed distance.
+    static_assert(kRowStep % 8 == 0, "rows share the swizzle's pattern");
+    const uint32_t raw_first =
+        (D == 128 ? sw128_offset(r_first, col >> 2) : r_first * 64 + (((col >> 2) ^ ((r_first >> 1) & 3)) << 4)) + 4 * (col & 3);
+    const uint32_t first = (col >> 4) * 16384 + sw128_offset(r_first, (col >> 1) & 7) + 8 * (col & 1);
+    constexpr uint32_t kRawStep = kRowStep * (D == 128 ? 128 : 64), kStep = kRowStep * 128;
+    float2 cb[2], cs[2], ci[2], cd[2];  // the thread's channels, in pairs
     int last_s = -1, last_h = -1;
     unsigned n = 0, seg = 0;
     bool ok = true;
     while (ok && walk.next(a, shape, sg)) {
-      // coefficients of the thread's 8 channels, from the sequence's first values
+      // coefficients of the thread's channels, from the sequence's first values
       if (BETA && (sg.s != last_s || sg.h != last_h)) {
         last_s = sg.s;
         last_h = sg.h;
-        float vmax[8], vabs[8];
+        float vmax[4], vabs[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 4; ++e) {
           vmax[e] = -INFINITY;
           vabs[e] = 0.f;
         }
@@ -352,36 +392,29 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           const int cnt = min(kSampleKeys, sg.si.ctx);
 #pragma unroll 4
           for (int kk = 0; kk < cnt; ++kk) {
-            float v[8];
+            float2 v[2];
             if (kCodes) {
-              const uint2 w = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(a.c.v) + (row + kk) * D + col * 8);
+              const uint32_t x = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(a.c.v) + (row + kk) * D + col * 4);
               const float sc = paged_scale(a.c.ve[row + kk]);
-              const uint32_t x[4] = {w.x & 0xffffu, w.x >> 16, w.y & 0xffffu, w.y >> 16};
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float2 f = e4m3x2_to_float2(x[e]);
-                v[2 * e] = f.x * sc;
-                v[2 * e + 1] = f.y * sc;
-              }
+              v[0] = __fmul2_rn(e4m3x2_to_float2(x & 0xffffu), make_float2(sc, sc));
+              v[1] = __fmul2_rn(e4m3x2_to_float2(x >> 16), make_float2(sc, sc));
             } else {
-              const uint4 w = *reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.c.v) + (row + kk) * D + col * 8);
-              const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                v[2 * e] = bf16_lo(x[e]);
-                v[2 * e + 1] = bf16_hi(x[e]);
-              }
+              const uint2 x = *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(a.c.v) + (row + kk) * D + col * 4);
+              v[0] = make_float2(bf16_lo(x.x), bf16_hi(x.x));
+              v[1] = make_float2(bf16_lo(x.y), bf16_hi(x.y));
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              vmax[e] = fmaxf(vmax[e], v[e]);
-              vabs[e] = fmaxf(vabs[e], fabsf(v[e]));
+            for (int e = 0; e < 2; ++e) {
+              vmax[2 * e] = fmaxf(vmax[2 * e], v[e].x);
+              vmax[2 * e + 1] = fmaxf(vmax[2 * e + 1], v[e].y);
+              vabs[2 * e] = fmaxf(vabs[2 * e], fabsf(v[e].x));
+              vabs[2 * e + 1] = fmaxf(vabs[2 * e + 1], fabsf(v[e].y));
             }
           }
         }
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-          const float *bp = a.beta + static_cast<long long>(sg.h) * D + col * 8 + e;
+        for (int e = 0; e < 4; e += 2) {
+          const float *bp = a.beta + static_cast<long long>(sg.h) * D + col * 4 + e;
           const BankCoef x = bank_coef(__ldg(bp), vmax[e], vabs[e]), y = bank_coef(__ldg(bp + 1), vmax[e + 1], vabs[e + 1]);
           cb[e / 2] = make_float2(x.b, y.b);
           cs[e / 2] = make_float2(x.s, y.s);
@@ -412,23 +445,21 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           const uint8_t *raw = smem + Lay::kRawK;
 #pragma unroll 1
           for (int i0 = 0; i0 < kRowsEach; i0 += kBatch) {
-            uint2 w[kBatch];
+            uint32_t w[kBatch];
             float sc[kBatch];
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
-              const int r = r_first + kRowStep * (i0 + u);
-              w[u] = *reinterpret_cast<const uint2 *>(raw + raw_offset(r));
-              sc[u] = paged_scale(smem[Lay::kScaleK + r]);
+              w[u] = *reinterpret_cast<const uint32_t *>(raw + raw_first + kRawStep * (i0 + u));
+              sc[u] = paged_scale(smem[Lay::kScaleK + r_first + kRowStep * (i0 + u)]);
             }
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
               const int r = r_first + kRowStep * (i0 + u);
               const float2 s2 = make_float2(sc[u], sc[u]);
-              const float2 f0 = __fmul2_rn(e4m3x2_to_float2(w[u].x & 0xffffu), s2), f1 = __fmul2_rn(e4m3x2_to_float2(w[u].x >> 16), s2);
-              const float2 f2 = __fmul2_rn(e4m3x2_to_float2(w[u].y & 0xffffu), s2), f3 = __fmul2_rn(e4m3x2_to_float2(w[u].y >> 16), s2);
-              uint4 y = make_uint4(pack_bf16(f0.x, f0.y), pack_bf16(f1.x, f1.y), pack_bf16(f2.x, f2.y), pack_bf16(f3.x, f3.y));
-              if (ragged && gone(r)) y = make_uint4(0, 0, 0, 0);
-              *reinterpret_cast<uint4 *>(tK + (col >> 3) * 16384 + sw128_offset(r, col & 7)) = y;
+              const float2 f0 = __fmul2_rn(e4m3x2_to_float2(w[u] & 0xffffu), s2), f1 = __fmul2_rn(e4m3x2_to_float2(w[u] >> 16), s2);
+              uint2 y = make_uint2(pack_bf16(f0.x, f0.y), pack_bf16(f1.x, f1.y));
+              if (ragged && gone(r)) y = make_uint2(0, 0);
+              *reinterpret_cast<uint2 *>(tK + first + kStep * (i0 + u)) = y;
             }
           }
           fence_proxy_async_smem();
@@ -441,49 +472,48 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         if (!wrote) {
           // the stage is free: see kSegRing
           wrote = true;
-          if (rl == 0 && cc < kChunks) {
+          if (tid < 8 * (D / 4) && rl == 0) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              s_shift[(seg % kSegRing) * D + col * 8 + e] =
-                  BETA ? bank_kind(e & 1 ? BankCoef{cb[e / 2].y, cs[e / 2].y, ci[e / 2].y, cd[e / 2].y}
-                                         : BankCoef{cb[e / 2].x, cs[e / 2].x, ci[e / 2].x, cd[e / 2].x})
-                       : INFINITY;
+            for (int e = 0; e < 4; ++e)
+              s_shift[(seg % kSegRing) * D + col * 4 + e] =
+                  kind_pack(BETA ? bank_kind(e & 1 ? BankCoef{cb[e / 2].y, cs[e / 2].y, ci[e / 2].y, cd[e / 2].y}
+                                                   : BankCoef{cb[e / 2].x, cs[e / 2].x, ci[e / 2].x, cd[e / 2].x})
+                                 : INFINITY);
           }
         }
         if (BETA || kCodes || ragged) {
           // rows in batches: their loads leave together (a store to the tile would hold the next row's back)
 #pragma unroll 1
           for (int i0 = 0; i0 < kRowsEach; i0 += kBatch) {
-            uint4 w[kBatch];
+            uint2 w[kBatch];
             float sc[kBatch];
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
-              const int r = r_first + kRowStep * (i0 + u);
               if (kCodes) {
-                const uint2 x = *reinterpret_cast<const uint2 *>(smem + Lay::kRawV + raw_offset(r));
-                w[u] = make_uint4(x.x & 0xffffu, x.x >> 16, x.y & 0xffffu, x.y >> 16);
-                sc[u] = paged_scale(smem[Lay::kScaleV + r]);
+                const uint32_t x = *reinterpret_cast<const uint32_t *>(smem + Lay::kRawV + raw_first + kRawStep * (i0 + u));
+                w[u] = make_uint2(x & 0xffffu, x >> 16);
+                sc[u] = paged_scale(smem[Lay::kScaleV + r_first + kRowStep * (i0 + u)]);
               } else {
-                w[u] = *reinterpret_cast<const uint4 *>(tE + (col >> 3) * 16384 + sw128_offset(r, col & 7));
+                w[u] = *reinterpret_cast<const uint2 *>(tE + first + kStep * (i0 + u));
               }
             }
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
               const int r = r_first + kRowStep * (i0 + u);
-              const uint32_t x[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
-              uint32_t y[4];
+              const uint32_t x[2] = {w[u].x, w[u].y};
+              uint32_t y[2];
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
+              for (int e = 0; e < 2; ++e) {
                 float2 v = kCodes ? __fmul2_rn(e4m3x2_to_float2(x[e]), make_float2(sc[u], sc[u]))
                                   : make_float2(bf16_lo(x[e]), bf16_hi(x[e]));
                 if (BETA) {
                   v = bank_pair(cb[e], cs[e], ci[e], cd[e], v);
-                  emax = fmaxf(fmaxf(emax, fabsf(v.x)), fabsf(v.y));
+                  emax = fmax3_abs(emax, v.x, v.y);
                 }
                 y[e] = pack_bf16(v.x, v.y);
               }
-              if (ragged && gone(r)) y[0] = y[1] = y[2] = y[3] = 0;
-              *reinterpret_cast<uint4 *>(tE + (col >> 3) * 16384 + sw128_offset(r, col & 7)) = make_uint4(y[0], y[1], y[2], y[3]);
+              if (ragged && gone(r)) y[0] = y[1] = 0;
+              *reinterpret_cast<uint2 *>(tE + first + kStep * (i0 + u)) = make_uint2(y[0], y[1]);
             }
           }
           if (BETA && emax > kWideE) s_wide[seg % kSegRing] = static_cast<int>(seg + 1);
@@ -494,20 +524,34 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       }
       ++seg;
     }
-  } else if (warp < 12) {
+  } else if (warp < 24) {
     // ------------------------------------------------------------ softmax, queries and output of a row tile
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
-    const int t = (warp >> 2) - 1, r = tid & 127;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 88;");
+    // Row tile t.  Two threads have row r: half 0 its keys 0 .. 63 of a key tile and channels 0 .. D/2 - 1,
+    // half 1 the others.  Their warps are a pair, and meet at a barrier of their own now and then.
+    const int t = (warp - 8) >> 3, half = ((warp - 8) >> 2) & 1, r = (warp & 3) * 32 + lane;
+    const uint32_t pair = FEM_CB(kCbPair + t * 4 + (warp & 3));
+    unsigned met = 0;
+    constexpr int kHalfD = D / 2;
     const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t tS = tmem + t * 128 + lane_off, tO = tmem + 256 + t * D + lane_off;
+    const uint32_t tS = tmem + t * 128 + half * 64 + lane_off;  // P goes over the first 32 of these 64 columns
+    const uint32_t tO = tmem + 256 + t * D + half * kHalfD + lane_off;
+    // per row: a maximum of each half in bf16, or a sum; per half and warp: the tile of its last request
+    float *s_row = reinterpret_cast<float *>(smem + Lay::kRow) + t * 128;
+    volatile __nv_bfloat16 *s_top = reinterpret_cast<volatile __nv_bfloat16 *>(s_row);
+    volatile unsigned *s_ask = reinterpret_cast<volatile unsigned *>(smem + Lay::kAsk) + (t * 4 + (warp & 3)) * 2;
     const float qk_scale = a.scale * kLog2e;
     unsigned n = 0, ns = 0, seg = 0;
+    // (like every wait it gives up in the end; then both warps of the pair do)
+    auto meet = [&]() {
+      mbar_arrive(pair);
+      return __all_sync(0xffffffffu, chunk_wait(pair, met++ & 1, a.err, kErrWaitMma, abort_flag)) != 0;
+    };
     // The thread's row of a segment: whether there is one, its place in the output, the keys it sees.
     struct Row {
       bool on;
-      int lim;
-      long long qrow, orow;
-      int hq;
+      int lim, hq;
+      int qrow;
     };
     auto row_of = [&](const SplitSeg &g, const ChunkRows &cr) {
       const int ir = t * 128 + r;
@@ -515,21 +559,24 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       w.on = ir < cr.rows;
       const int tok = cr.tok0 + (w.on ? ir / a.group : 0);
       w.hq = g.h * a.group + (w.on ? ir % a.group : 0);
-      w.qrow = static_cast<long long>(g.si.q0) + tok;
-      w.orow = w.qrow * a.Hq + w.hq;
+      w.qrow = g.si.q0 + tok;
       w.lim = w.on ? min(paged_limit(g.si, tok, a.causal), g.si.ctx) : 0;
       return w;
     };
-    // The row's query into shared memory, and the arrival that lets the segment's products start.
+    // Half of the row's query into shared memory, and the arrival that lets the segment's products start.
     auto load_q = [&](const Row &w, bool used) {
       if (used) {
         uint8_t *tQ = smem + Lay::kQ + t * Lay::kTile;
-        const uint4 *qp = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.q) + w.qrow * a.q_sn + w.hq * a.q_sh);
-        uint4 x[D / 8];
+        const uint4 *qp = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.q) + w.qrow * a.q_sn + w.hq * a.q_sh) +
+                          half * (kHalfD / 8);
+        uint4 x[kHalfD / 8];
 #pragma unroll
-        for (int c = 0; c < D / 8; ++c) x[c] = w.on ? __ldg(qp + c) : make_uint4(0, 0, 0, 0);
+        for (int c = 0; c < kHalfD / 8; ++c) x[c] = w.on ? __ldg(qp + c) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int c = 0; c < D / 8; ++c) *reinterpret_cast<uint4 *>(tQ + (c >> 3) * 16384 + sw128_offset(r, c & 7)) = x[c];
+        for (int c = 0; c < kHalfD / 8; ++c) {
+          const int ch = half * (kHalfD / 8) + c;
+          *reinterpret_cast<uint4 *>(tQ + (ch >> 3) * 16384 + sw128_offset(r, ch & 7)) = x[c];
+        }
         fence_proxy_async_smem();
       }
       mbar_arrive(FEM_CB(kCbQ + t));
@@ -543,76 +590,107 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       load_q(w, t < cr.tiles);
     }
     while (ok) {
-      const int nk = sg.kt1 - sg.kt0, ir = t * 128 + r;
-      const int lim = w.lim;
-      float m = -INFINITY, L = 0.f;
+      const int nk = sg.kt1 - sg.kt0;
+      // a row that sees nothing of the segment needs no maximum
+      float m = w.lim > sg.kt0 * kChunkKeys ? -INFINITY : 0.f, L = 0.f;
       if (t < cr.tiles) {
-        for (int k = 0; k < nk; ++k, ++ns) {
-          ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbS + t), ns & 1, a.err, kErrWaitMma, abort_flag));
+        for (int k = 0; k < nk; ++k) {
+          ++ns;  // this tile's number; its S is the barrier's phase ns - 1
+          ok = __all_sync(0xffffffffu, chunk_wait(FEM_CB(kCbS + t), (ns - 1) & 1, a.err, kErrWaitMma, abort_flag));
           if (!ok) break;
           tc_fence_after_sync();
-          uint32_t sr[128];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[c * 32]));
-          tmem_ld_wait();
-          float *s = reinterpret_cast<float *>(sr);
-          const int k0 = (sg.kt0 + k) * kChunkKeys;
+          const int k0 = (sg.kt0 + k) * kChunkKeys + half * 64;
           const unsigned inv = s_inv[(n + k) % kInvRing];
-          if (__any_sync(0xffffffffu, k0 + kChunkKeys > lim) || inv) {
+          const bool masked = __any_sync(0xffffffffu, k0 + 64 > w.lim) || inv;
+          auto mask = [&](int c, uint32_t (&sr)[32]) {
 #pragma unroll
-            for (int j = 0; j < 128; ++j) s[j] = k0 + j < lim ? s[j] : -INFINITY;
-            if (inv) {
-#pragma unroll
-              for (int j = 0; j < 128; ++j) s[j] = (inv >> (j >> box_shift)) & 1u ? -INFINITY : s[j];
+            for (int j = 0; j < 32; ++j) {
+              const bool seen = k0 + c * 32 + j < w.lim && !((inv >> ((half * 64 + c * 32 + j) >> box_shift)) & 1u);
+              sr[j] = seen ? sr[j] : 0xff800000u;
             }
-          }
-          float mx[8];
-#pragma unroll
-          for (int u = 0; u < 8; ++u) mx[u] = fmax3(s[u], s[u + 8], s[u + 16]);
-#pragma unroll
-          for (int j = 24; j < 120; j += 16)
-#pragma unroll
-            for (int u = 0; u < 8; ++u) mx[u] = fmax3(mx[u], s[j + u], s[j + 8 + u]);
-#pragma unroll
-          for (int u = 0; u < 8; ++u) mx[u] = fmaxf(mx[u], s[120 + u]);
-          const float tmax = fmax3(fmax3(mx[0], mx[1], mx[2]), fmax3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * qk_scale;
-          float alpha = 1.f;
-          if (tmax > m + kRowMaxLag) {
-            alpha = ex2_approx(m - tmax);  // 0 the first time
-            m = tmax;
-            L *= alpha;
-          }
-          if (k > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
-            // O holds the products of the key tiles before (see the issue order)
+          };
+          // The half row's largest score, rounded to bf16: a maximum need not be exact, only the same for
+          // both threads.
+          auto largest = [&]() {
+            float y = -INFINITY;
 #pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
-              uint32_t v[32];
-              tmem_ld32(tO + c * 32, v);
+            for (int c = 0; c < 2; ++c) {
+              uint32_t sr[32];
+              tmem_ld32(tS + c * 32, sr);
               tmem_ld_wait();
+              if (masked) mask(c, sr);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
-              tmem_st32(tO + c * 32, v);
+              for (int j = 0; j < 32; j += 2) y = fmax3(y, __uint_as_float(sr[j]), __uint_as_float(sr[j + 1]));
             }
-            tmem_st_wait();
+            return __float2bfloat16_rn(y * qk_scale);
+          };
+          // The row's maximum moves to `top`: its sum, and its half of the products so far (of the key tiles
+          // before: see the issue order), are rescaled.  Whole warps.
+          auto raise = [&](float top, bool products) {
+            float alpha = 1.f;
+            if (top > m) {
+              alpha = m == -INFINITY ? 0.f : ex2_approx(m - top);
+              m = top;
+              L *= alpha;
+            }
+            if (products) {
+#pragma unroll 1
+              for (int c = 0; c < kHalfD / 32; ++c) {
+                uint32_t v[32];
+                tmem_ld32(tO + c * 32, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
+                tmem_st32(tO + c * 32, v);
+              }
+            }
+          };
+          if (__any_sync(0xffffffffu, m == -INFINITY)) {
+            // the first tile with something to see: the two threads agree on a maximum
+            const __nv_bfloat16 mine = largest();
+            s_top[2 * r + half] = mine;
+            if (!(ok = meet())) break;
+            raise(fmaxf(__bfloat162float(mine), __bfloat162float(s_top[2 * r + (half ^ 1)])), k > 0);
+          } else {
+            // a maximum asked for during the tile before: what either thread wrote then is seen by both
+            // now, through the arrivals of P and the product they let start
+            const unsigned q0 = s_ask[0], q1 = s_ask[1];
+            if (q0 == ns - 1 || q1 == ns - 1) {
+              const float t0 = q0 == ns - 1 ? __bfloat162float(s_top[2 * r]) : -INFINITY;
+              const float t1 = q1 == ns - 1 ? __bfloat162float(s_top[2 * r + 1]) : -INFINITY;
+              if (!(ok = meet())) break;  // both have read what the next request overwrites
+              raise(fmaxf(t0, t1), true);
+            }
           }
+          // The weights against the maximum so far, and their sum.  bf16 and fp32 hold them however far a
+          // score lies above it (to 2^127; beyond, the sum is infinite and the row goes to the exact path);
+          // a sum over 2^kAskSum asks for a larger one from the next tile on.
           const float mz = m == -INFINITY ? 0.f : m;
           const float2 scale2 = make_float2(qk_scale, qk_scale), negm2 = make_float2(-mz, -mz);
-          float2 ls[4];
+          float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          uint32_t p[32];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) ls[u] = make_float2(0.f, 0.f);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t p[16];
+          for (int c = 0; c < 2; ++c) {
+            uint32_t sr[32];
+            tmem_ld32(tS + c * 32, sr);
+            tmem_ld_wait();
+            if (masked) mask(c, sr);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const float2 x = __ffma2_rn(make_float2(s[c * 32 + 2 * i], s[c * 32 + 2 * i + 1]), scale2, negm2);
+              const float2 x = __ffma2_rn(make_float2(__uint_as_float(sr[2 * i]), __uint_as_float(sr[2 * i + 1])), scale2, negm2);
               const float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
-              ls[i & 3] = __fadd2_rn(ls[i & 3], e);
-              p[i] = pack_bf16(e.x, e.y);
+              ls[i & 1] = __fadd2_rn(ls[i & 1], e);
+              p[c * 16 + i] = pack_bf16(e.x, e.y);
             }
-            tmem_st16(tS + c * 16, p);
           }
-          L += (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y) + (ls[2].x + ls[2].y) + (ls[3].x + ls[3].y);
+          const float sum = (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
+          if (__any_sync(0xffffffffu, sum > kAskSum)) {
+            const __nv_bfloat16 mine = largest();
+            s_top[2 * r + half] = sum > kAskSum ? mine : __float2bfloat16_rn(-INFINITY);
+            if (lane == 0) s_ask[half] = ns;
+          }
+          tmem_st32(tS, p);
+          L += sum;
           tmem_st_wait();
           tc_fence_before_sync();
           mbar_arrive(FEM_CB(kCbP + t));
@@ -636,75 +714,87 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       tc_fence_after_sync();
       if (more && t >= cr.tiles) load_q(w2, t < cr2.tiles);
       if (t < cr.tiles) {
-        // ---- the row's output, or its piece
+        // the row's sum: half 1's goes to half 0, and the whole comes back
+        if (half == 1) s_row[r] = L;
+        if (!(ok = meet())) break;
+        if (half == 0) s_row[r] = L = L + s_row[r];
+        if (!(ok = meet())) break;
+        if (half == 1) L = s_row[r];
+        // ---- the row's output (half of its channels), or its piece
+        if (L == 0.f) m = -INFINITY;  // nothing seen
+        const int ir = t * 128 + r;
+        const long long orow = static_cast<long long>(w.qrow) * a.Hq + w.hq;
         const bool whole = sg.kt0 == 0 && sg.kt1 == sg.kt_all;
         const bool wide = BETA && s_wide[seg % kSegRing] == static_cast<int>(seg + 1);
-        const float *shift = s_shift + (seg % kSegRing) * D;
+        const short *shift = s_shift + (seg % kSegRing) * D + half * kHalfD;
         float *piece = sp.pieces + static_cast<size_t>(cta * 2 + (sg.kt0 == 0 ? 1 : 0)) * piece_floats(256, D);
-        const bool empty = m == -INFINITY && L == 0.f;
+        const bool empty = L == 0.f;
         const float inv_l = empty ? 0.f : 1.f / L;
         bool good = true;
 #pragma unroll 1
-        for (int c = 0; c < D / 32; ++c) {
+        for (int c = 0; c < kHalfD / 32; ++c) {
           uint32_t v[32];
           tmem_ld32(tO + c * 32, v);
           tmem_ld_wait();
           if (whole) {
-            // lane l has channel 32 c + l's coefficients; every row needs all of them
-            const OutCoef oc = out_coef(BETA ? __ldg(a.beta + static_cast<long long>(sg.h) * D + c * 32 + lane) : 0.f,
-                                        shift[c * 32 + lane], wide);
-            uint32_t o[16];
+            // lane l has the coefficients of the chunk's channel l; every row needs all of them
+            const OutCoef oc = out_coef(BETA ? __ldg(a.beta + static_cast<long long>(sg.h) * D + half * kHalfD + c * 32 + lane) : 0.f,
+                                        kind_unpack(shift[c * 32 + lane]), wide);
+            uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + orow * D + half * kHalfD + c * 32);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              float x[2];
+            for (int i4 = 0; i4 < 4; ++i4) {
+              uint32_t o[4];
 #pragma unroll
-              for (int u = 0; u < 2; ++u) {
-                const float av = __uint_as_float(v[2 * i + u]) * inv_l;
-                if (BETA) {
-                  OutCoef k;
-                  k.g = __shfl_sync(0xffffffffu, oc.g, 2 * i + u);
-                  k.z = __shfl_sync(0xffffffffu, oc.z, 2 * i + u);
-                  k.y = __shfl_sync(0xffffffffu, oc.y, 2 * i + u);
-                  k.w = __shfl_sync(0xffffffffu, oc.w, 2 * i + u);
-                  k.lo = __shfl_sync(0xffffffffu, oc.lo, 2 * i + u);
-                  bool fine;
-                  x[u] = paged_out(k, av, &fine);
-                  good = good && fine;
-                } else {
-                  x[u] = av;
-                  good = good && fabsf(av) < kMostA;
+              for (int i = 0; i < 4; ++i) {
+                float x[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                  const int j = 8 * i4 + 2 * i + u;
+                  const float av = __uint_as_float(v[j]) * inv_l;
+                  if (BETA) {
+                    OutCoef kf;
+                    kf.g = __shfl_sync(0xffffffffu, oc.g, j);
+                    kf.z = __shfl_sync(0xffffffffu, oc.z, j);
+                    kf.y = __shfl_sync(0xffffffffu, oc.y, j);
+                    kf.w = __shfl_sync(0xffffffffu, oc.w, j);
+                    kf.lo = __shfl_sync(0xffffffffu, oc.lo, j);
+                    bool fine;
+                    x[u] = paged_out(kf, av, &fine);
+                    good = good && fine;
+                  } else {
+                    x[u] = av;
+                    good = good && fabsf(av) < kMostA;
+                  }
                 }
+                o[i] = empty ? 0u : pack_bf16(x[0], x[1]);
               }
-              o[i] = empty ? 0u : pack_bf16(x[0], x[1]);
+              if (w.on) dst[i4] = make_uint4(o[0], o[1], o[2], o[3]);
             }
-            if (!w.on) continue;
-            uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + w.orow * D + c * 32);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
           } else if (w.on) {
-            float4 *dst = reinterpret_cast<float4 *>(piece + static_cast<size_t>(ir) * D + c * 32);
+            float4 *dst = reinterpret_cast<float4 *>(piece + static_cast<size_t>(ir) * D + half * kHalfD + c * 32);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
               dst[i] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]),
                                    __uint_as_float(v[4 * i + 3]));
           }
         }
-        if (w.on) {
+        // both halves' verdict (and the exchange above is read before the next segment's)
+        const bool exact = whole && !good && !empty && w.on;
+        if (whole && half == 0 && w.on) sp.exact[orow] = exact;
+        if (!(ok = meet())) break;
+        if (half == 1 && exact) sp.exact[orow] = 1;
+        if (exact) record.any_exact = 1;
+        if (w.on && half == 0) {
           if (whole) {
-            if (a.lse != nullptr) a.lse[w.orow] = empty ? -INFINITY : (m + log2f(L)) * kLn2;
+            if (a.lse != nullptr) a.lse[orow] = empty ? -INFINITY : (m + log2f(L)) * kLn2;
           } else {
             piece[256 * D + 2 * ir] = m;
             piece[256 * D + 2 * ir + 1] = L;
           }
-          if (whole) {
-            const bool exact = !good && !empty;
-            sp.exact[w.orow] = exact;
-            if (exact) record.any_exact = 1;
-          }
         }
         if (!whole && t == 0) {
-          if (r < D) piece[256 * D + 512 + r] = shift[r];
-          if (r == 0) {
+          if (half == 0 && r < D) piece[256 * D + 512 + r] = kind_unpack(s_shift[(seg % kSegRing) * D + r]);
+          if (half == 0 && r == 0) {
             piece[256 * D + 512 + D] = wide ? 1.f : 0.f;
             if (sg.kt0 == 0) {
               record.n = split_owner(walk.W, walk.G, sg.x_end - 1) - cta + 1;
@@ -729,7 +819,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
   tc_fence_before_sync();
   __syncthreads();
   if (tid == 0) sp.records[cta] = record;
-  if (warp == 12) {
+  if (warp == 24) {
     tc_fence_after_sync();
     tmem_dealloc(tmem, 512);
   }

@@ -15,7 +15,7 @@
 // and head goes by its first kSampleKeys values v:
 //   tiny     (beta max|v| <= 2^-12)  E = D v,                    o = a / D
 //   linear   (beta max|v| <= 2)      E = expm1(beta v),          o = log1p(a) / beta
-//   shifted  (else)                  E = exp(beta (v - max v)),  o = max v + log(a) / beta
+//   shifted  (else)                  E = exp(beta (v - c)),      o = c + log(a) / beta,  c about max v
 // Tiny and linear keep small beta free of cancellation: E = v leaves out
 // beta v^2 / 2, at most 2^-9 |v| where it is let through, and expm1 by
 // subtraction is off by 2^-22, 2^-10 of the largest E.  (beta = 0 is tiny.)
@@ -34,6 +34,7 @@ constexpr float kTinyReach = 0.000244140625f;  // 2^-12: up to which it is tiny
 // What the range of bf16 and fp32 may cost: a term whose weight or bank underflows is lost.  It is
 // at most 2^-126 times the other factor's largest: 2^8 (P) or the largest |E| met.  While that is at
 // most 2^30, the lost terms of 2^20 keys stay under 2^-76, against a >= 2^-66.
+constexpr float kMostShift = 32000.f;  // of a shifted channel's s (beyond it the exact path takes over)
 constexpr float kWideE = 1073741824.f;      // 2^30
 constexpr float kLeastA = 1.3552527e-20f;   // 2^-66
 constexpr float kMostA = 1.2980742e33f;     // 2^110
@@ -46,7 +47,7 @@ __device__ __forceinline__ float tiny_scale(float beta) {
   return beta > 0.f ? __int_as_float(__float_as_int(beta * 274877906944.f) & 0x7f800000) : 1.f;
 }
 
-// E(v) = 2^(b v + s) + ic + d v: shifted {beta log2 e, -b max v, 0, 0}, linear {b, 0, -1, 0}, tiny {0, 0, -1, D}
+// E(v) = 2^(b v + s) + ic + d v: shifted {beta log2 e, -b max v rounded to a whole number, 0, 0}, linear {b, 0, -1, 0}, tiny {0, 0, -1, D}
 struct BankCoef {
   float b, s, ic, d;
 };
@@ -62,14 +63,22 @@ __device__ __forceinline__ BankCoef bank_coef(float beta, float vmax, float vabs
     c.b = 0.f;
     c.d = tiny_scale(beta);
   } else if (!(x <= kLinearReach)) {
-    c.s = -c.b * vmax;
+    c.s = fminf(fmaxf(-rintf(c.b * vmax), -kMostShift), kMostShift);
     c.ic = 0.f;
   }
   return c;
 }
-// The channel's kind, and a shifted one's s, in one float: NaN linear, infinity tiny.
+// The channel's kind, and a shifted one's s (a whole number), in one float: NaN linear, infinity tiny.
 __device__ __forceinline__ float bank_kind(const BankCoef &c) {
   return c.ic == 0.f ? c.s : c.d != 0.f ? INFINITY : __int_as_float(0x7fffffff);
+}
+
+// The same in 16 bits.
+__device__ __forceinline__ short kind_pack(float kind) {
+  return kind == INFINITY ? 32766 : kind != kind ? 32767 : static_cast<short>(kind);
+}
+__device__ __forceinline__ float kind_unpack(short k) {
+  return k == 32766 ? INFINITY : k == 32767 ? __int_as_float(0x7fffffff) : static_cast<float>(k);
 }
 
 // E of two values; coefficients of both
@@ -112,6 +121,7 @@ struct SplitShape {
   int row_tile, key_shift;  // rows of a tile, log2 of its keys
   int tok;                  // tokens of a row tile (whole tokens), or 0: rows packed without regard to tokens
   int least;                // key tiles a CTA takes at least
+  int fixed;                // what beginning an item costs, in key tiles: the line counts them before its tiles
 };
 
 // Row tiles of a sequence, for each of its heads; a sequence without rows has none.
@@ -129,17 +139,17 @@ __host__ __device__ __forceinline__ int row_key_tiles(const SeqInfo &si, int r, 
   const int tiles = (keys + (1 << sh.key_shift) - 1) >> sh.key_shift;
   return tiles > 1 ? tiles : 1;
 }
-// Key tiles of row tiles 0 .. R - 1 of one head (R at most `all`, the sequence's).
+// Key tiles of row tiles 0 .. R - 1 of one head (R at most `all`, the sequence's), and the items' fixed costs.
 __host__ __device__ __forceinline__ long long head_key_tiles(const SeqInfo &si, int R, int all, int causal,
                                                              const SplitShape &sh) {
   if (R <= 0) return 0;
-  if (!(sh.tok && causal)) return static_cast<long long>(R) * row_key_tiles(si, 0, 0, sh);
+  if (!(sh.tok && causal)) return static_cast<long long>(R) * (row_key_tiles(si, 0, 0, sh) + sh.fixed);
   // sum of ceil((c + i tok) / T), i = 0 .. n - 1, over the tiles of tok whole tokens; the sequence's
   // last tile may hold fewer
-  long long sum = 0;
+  long long sum = static_cast<long long>(R) * sh.fixed;
   int n = R, i0 = 0;
   if (R == all) {
-    sum = row_key_tiles(si, R - 1, causal, sh);
+    sum += row_key_tiles(si, R - 1, causal, sh);
     n = R - 1;
   }
   const int base = si.ctx - si.n, step = sh.tok, shift = sh.key_shift, T = 1 << shift;
@@ -190,39 +200,42 @@ struct SplitWalk {
   unsigned x, left;  // next tile, tiles to go
   unsigned W, G;     // the line's tiles, CTAs that take part
   SeqInfo si;
-  int s, h, r, kt0, R;
+  int s, h, r, R;
+  int at;  // the next tile's place in the item's stretch of the line (its fixed cost, then its key tiles)
   __device__ __forceinline__ bool next(const PagedReadArgs &a, const SplitShape &sh, SplitSeg &g) {
-    if (left == 0) return false;
-    g.si = si;
-    g.s = s;
-    g.h = h;
-    g.r = r;
-    g.kt0 = kt0;
-    g.kt_all = row_key_tiles(si, r, a.causal, sh);
-    const unsigned rest = g.kt_all - kt0, take = min(rest, left);
-    g.kt1 = kt0 + take;
-    g.x_end = x + rest;
-    x += take;
-    left -= take;
-    kt0 = 0;
-    if (left && ++r == R) {
-      r = 0;
-      if (++h == a.c.H) {
-        h = 0;
-        do {  // the next sequence with rows: there is one, as tiles are left
-          si = paged_seq(a, ++s);
-          R = seq_row_tiles(si, a.group, sh);
-        } while (R == 0);
+    while (left) {
+      g.si = si;
+      g.s = s;
+      g.h = h;
+      g.r = r;
+      g.kt_all = row_key_tiles(si, r, a.causal, sh);
+      const unsigned rest = g.kt_all + sh.fixed - at, take = min(rest, left);
+      g.kt0 = max(at - sh.fixed, 0);
+      g.kt1 = at + static_cast<int>(take) - sh.fixed;
+      g.x_end = x + rest;
+      x += take;
+      left -= take;
+      at = 0;
+      if (left && ++r == R) {
+        r = 0;
+        if (++h == a.c.H) {
+          h = 0;
+          do {  // the next sequence with rows: there is one, as tiles are left
+            si = paged_seq(a, ++s);
+            R = seq_row_tiles(si, a.group, sh);
+          } while (R == 0);
+        }
       }
+      if (g.kt1 > 0) return true;  // else the stretch ends inside the item's fixed cost: the next CTA begins it
     }
-    return true;
+    return false;
   }
 };
 
 template <int THREADS>
 struct SplitScan {
   long long warp[THREADS / 32];
-  int s, h, r, kt0;
+  int s, h, r, at;
 };
 
 // The stretch of CTA `cta` of a grid of `grid`; false where it has none.  All THREADS threads of the block.
@@ -297,7 +310,7 @@ __device__ bool split_begin(const PagedReadArgs &a, const SplitShape &shape, int
       sc.s = s;
       sc.h = static_cast<int>(h);
       sc.r = lo;
-      sc.kt0 = static_cast<int>(in - head_key_tiles(si, lo, R, a.causal, shape));
+      sc.at = static_cast<int>(in - head_key_tiles(si, lo, R, a.causal, shape));
     }
     before += all;
     if (walk.x < before) break;  // the same for every thread
@@ -306,7 +319,7 @@ __device__ bool split_begin(const PagedReadArgs &a, const SplitShape &shape, int
   walk.s = sc.s;
   walk.h = sc.h;
   walk.r = sc.r;
-  walk.kt0 = sc.kt0;
+  walk.at = sc.at;
   walk.si = paged_seq(a, walk.s);
   walk.R = seq_row_tiles(walk.si, a.group, shape);
   return true;
