@@ -833,7 +833,7 @@ int fem_cache_gather(const fem_paged_cache *cache, const int *block_table, int m
 // Query rows per key/value head up to which the paged read takes the kernel of few rows.
 static constexpr int kTokenRows = 16;
 // What an item costs the kernel of many rows beside its key tiles (queries, a maximum, output), in key tiles.
-static constexpr int kChunkFixed = 3;
+static constexpr int kChunkFixed = 7;
 
 int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride_n, int64_t q_stride_h,
                    const float *beta, const int *q_offsets, const int *ctx_lens, const int *block_table,

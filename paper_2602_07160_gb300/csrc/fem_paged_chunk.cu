@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     fence_mbar_init();
     *abort_flag = 0;
     for (unsigned i = 0; i < kSegRing; ++i) s_wide[i] = 0;
-    for (int i = 0; i < 16; ++i) reinterpret_cast<unsigned *>(smem + Lay::kAsk)[i] = 0u;  // tiles count from 1
+    for (int i = 0; i < 16; ++i) reinterpret_cast<unsigned *>(smem + Lay::kAsk)[i] = ~0u;  // no tile
   }
   tc_fence_before_sync();
   __syncthreads();
@@ -501,18 +501,17 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             for (int u = 0; u < kBatch; ++u) {
               const int r = r_first + kRowStep * (i0 + u);
               const uint32_t x[2] = {w[u].x, w[u].y};
+              const bool none = ragged && gone(r);  // whatever is there, it has no part in the largest |E| either
               uint32_t y[2];
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
                 float2 v = kCodes ? __fmul2_rn(e4m3x2_to_float2(x[e]), make_float2(sc[u], sc[u]))
                                   : make_float2(bf16_lo(x[e]), bf16_hi(x[e]));
-                if (BETA) {
-                  v = bank_pair(cb[e], cs[e], ci[e], cd[e], v);
-                  emax = fmax3_abs(emax, v.x, v.y);
-                }
+                if (BETA) v = bank_pair(cb[e], cs[e], ci[e], cd[e], v);
+                if (none) v = make_float2(0.f, 0.f);
+                if (BETA) emax = fmax3_abs(emax, v.x, v.y);
                 y[e] = pack_bf16(v.x, v.y);
               }
-              if (ragged && gone(r)) y[0] = y[1] = 0;
               *reinterpret_cast<uint2 *>(tE + first + kStep * (i0 + u)) = make_uint2(y[0], y[1]);
             }
           }

@@ -116,39 +116,50 @@ __device__ void paged_exact_row(const PagedReadArgs &a, int s, const SeqInfo &si
     const float alpha = m == m_new ? 1.f : expf(m - m_new);  // 0 for the first weight
     const float dm = m == m_new ? 0.f : m - m_new;
     const int cnt = min(limit - k0, kExactTile);
-    float Lj = 0.f;
+    const float L_old = L * alpha;
+    float L_new = L_old;
+    for (int kk = 0; kk < cnt; ++kk) L_new += sh.p[kk];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int j = tid + u * kExactThreads;
-      Lj = L * alpha;
+      if (j >= d) continue;
+      const float b = beta[u];
       // log weights are kept relative to m: the old maximum moves with it (-inf: nothing yet)
       W[u] *= alpha;
       if (top[u] != -INFINITY) top[u] += dm;
+      // the tile's largest value and log weight, then its sums against them (the values come twice, from L1
+      // the second time; without a branch on each key the loads of several keys are under way at once)
+      float vmax = -INFINITY, xmax = -INFINITY;
+#pragma unroll 8
       for (int kk = 0; kk < cnt; ++kk) {
         const long long r = sh.row[kk];
-        if (r < 0) continue;
-        const float pk = sh.p[kk];
-        if (j < d) {
+        if (r >= 0) {
           const float v = paged_value<FORMAT>(c, r, j, FORMAT == kCacheE4m3 ? sh.vs[kk] : 1.f);
-          const float b = beta[u];
-          if (v > ref[u] || v != v) {
-            if (Lj > 0.f)
-              W[u] = (ref[u] == -INFINITY ? 0.f : expf(b * (ref[u] - v)) * W[u]) + exact_em1(b, ref[u] - v) * Lj;
-            ref[u] = v;
-          }
-          if (v != ref[u]) W[u] += pk * exact_em1(b, v - ref[u]);
-          const float x = sh.lp[kk] + b * v;
-          if (x > top[u]) {
-            A[u] = A[u] * expf(top[u] - x) + 1.f;
-            top[u] = x;
-          } else if (x != -INFINITY) {
-            A[u] += expf(x - top[u]);
-          }
+          vmax = fmaxf(vmax, v);
+          xmax = fmaxf(xmax, fmaf(b, v, sh.lp[kk]));
         }
-        Lj += pk;
+      }
+      if (vmax > ref[u]) {
+        if (L_old > 0.f)
+          W[u] = (ref[u] == -INFINITY ? 0.f : expf(b * (ref[u] - vmax)) * W[u]) + exact_em1(b, ref[u] - vmax) * L_old;
+        ref[u] = vmax;
+      }
+      if (xmax > top[u]) {
+        A[u] *= expf(top[u] - xmax);
+        top[u] = xmax;
+      }
+      const float t0 = top[u] == -INFINITY ? 0.f : top[u];
+#pragma unroll 8
+      for (int kk = 0; kk < cnt; ++kk) {
+        const long long r = sh.row[kk];
+        if (r >= 0) {
+          const float v = paged_value<FORMAT>(c, r, j, FORMAT == kCacheE4m3 ? sh.vs[kk] : 1.f);
+          W[u] = fmaf(sh.p[kk], exact_em1(b, v == ref[u] ? 0.f : v - ref[u]), W[u]);
+          A[u] += expf(fmaf(b, v, sh.lp[kk]) - t0);
+        }
       }
     }
-    L = Lj;
+    L = L_new;
     m = m_new;
     __syncthreads();
   }
