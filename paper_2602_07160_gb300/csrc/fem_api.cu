@@ -811,7 +811,7 @@ int fem_cache_write(const fem_paged_cache *cache, const void *k, const void *v, 
   DeviceState *ds = nullptr;
   if ((rc = device_state(&ds)) != FEM_OK) return rc;
   return map_cuda(launch_cache_write(c, k, v, k_stride_n, k_stride_h, v_stride_n, v_stride_h,
-                                     reinterpret_cast<const long long *>(slots), N, ds->err, ds->num_sms,
+                                     reinterpret_cast<const long long *>(slots), N, ds->err,
                                      static_cast<cudaStream_t>(stream)));
 }
 
@@ -834,6 +834,7 @@ int fem_cache_gather(const fem_paged_cache *cache, const int *block_table, int m
 static constexpr int kTokenRows = 16;
 // What an item costs the kernel of many rows beside its key tiles (queries, a maximum, output), in key tiles.
 static constexpr int kChunkFixed = 7;
+static constexpr int kTokenFixed = 4;
 
 int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride_n, int64_t q_stride_h,
                    const float *beta, const int *q_offsets, const int *ctx_lens, const int *block_table,
@@ -883,7 +884,7 @@ int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride
   // then short: fem_paged_split.cuh)
   const int tok = 256 / a.group;
   const SplitShape shape = chunk ? SplitShape{256, 7, tok >= 8 ? tok & ~7 : tok, 1, kChunkFixed}
-                                 : SplitShape{rows <= 8 ? 8 : 16, 6, 0, 2, 0};
+                                 : SplitShape{rows <= 8 ? 8 : 16, 6, 0, 2, kTokenFixed};
   const int box_rows = chunk ? std::min(1 << a.c.page_shift, 128) : 16;
   CUtensorMap tk, tv;
   if ((rc = cache_map(&tk, a.c.k, a.c, box_rows)) != FEM_OK || (rc = cache_map(&tv, a.c.v, a.c, box_rows)) != FEM_OK)

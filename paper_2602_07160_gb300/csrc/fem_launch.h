@@ -162,7 +162,7 @@ struct PagedSplit;
 struct SplitShape;
 cudaError_t launch_cache_write(const PagedCacheView &c, const void *k, const void *v, long long k_sn, long long k_sh,
                                long long v_sn, long long v_sh, const long long *slots, int N, unsigned *err,
-                               int num_sms, cudaStream_t stream);
+                               cudaStream_t stream);
 cudaError_t launch_cache_gather(const PagedCacheView &c, const int *table, int max_pages, const int *starts,
                                 const int *offsets, int S, int total, void *k, void *v, unsigned *err,
                                 cudaStream_t stream);
