@@ -311,7 +311,8 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
       for (int u = 0; u < MT; ++u) acc[t][u][0] = acc[t][u][1] = acc[t][u][2] = acc[t][u][3] = 0.f;
     }
     const float qk_scale = a.scale * kLog2e;
-    const bool tiny = __syncthreads_or(BETA && tid < D && beta_c > 0.f && s_shift[tid] == INFINITY) != 0;  // coefficients
+    // the coefficients are there
+    const bool tiny = __syncthreads_or(BETA && tid < D && beta_c > 0.f && s_shift[tid] == INFINITY) != 0;
 
     for (int j = 0; j < n_st; ++j) {
       const int st = j % NS, key0 = ((sg.kt0 + j) * kTokWarps + warp) * kTokKeys;
@@ -414,16 +415,15 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
             pf[t][0] = transpose8x8(pack_bf16(p0, p1));
             pf[t][1] = transpose8x8(pack_bf16(p2, p3));
           }
-          // |E| matters where weights come near the end of the range, or where a tiny channel could leave its own
-          const bool track = BETA && (tiny || __any_sync(0xffffffffu, deep));
           // ---- O^T += E^T P^T: the lane's keys are contraction indices 2 i, 2 i + 1, 2 i + 8, 2 i + 9
           int vr[4];
 #pragma unroll
           for (int u = 0; u < 4; ++u) vr[u] = key_of<R128>(2 * i4 + (u & 1) + 8 * (u >> 1));
-          unsigned dead = 0;  // keys past the sequence: whatever their rows hold, no weight
           if (tail) {
+            // a key past the sequence has no weight, but whatever its row holds must not be infinite either:
+            // the stage's first key, which is there, stands in for it
 #pragma unroll
-            for (int u = 0; u < 4; ++u) dead |= key0 + vr[u] >= sg.si.ctx ? 1u << u : 0u;
+            for (int u = 0; u < 4; ++u) vr[u] = key0 + vr[u] >= sg.si.ctx ? 0 : vr[u];
           }
           float vscale[4];
           if (FORMAT == kCacheE4m3) {
@@ -492,19 +492,6 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
                   lo[u] = e.x;
                   hi[u] = e.y;
                 }
-                if (dead) {
-#pragma unroll
-                  for (int u = 0; u < 4; ++u)
-                    if ((dead >> u) & 1u) lo[u] = hi[u] = 0.f;
-                }
-                if (track) {
-#pragma unroll
-                  for (int u = 0; u < 4; ++u) emax = fmaxf(fmaxf(emax, fabsf(lo[u])), fabsf(hi[u]));
-                }
-              } else if (dead) {
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-                  if ((dead >> u) & 1u) lo[u] = hi[u] = 0.f;
               }
               a0 = pack_bf16(lo[0], lo[1]);
               a1 = pack_bf16(hi[0], hi[1]);
@@ -512,6 +499,25 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
               a3 = pack_bf16(hi[2], hi[3]);
 #pragma unroll
               for (int t = 0; t < NT; ++t) mma_bf16(acc[t][pc * (kPer / 2) + q], a0, a1, a2, a3, pf[t][0], pf[t][1]);
+            }
+          }
+          // The largest |E| matters where weights come near the end of the range, or where a tiny channel
+          // could leave its own: it is then found by forming the bank once more, out of the loop above, which
+          // stays one stretch of code.  (Channel ch of the tile, lane by lane; the keys one after the other.)
+          if (BETA && (tiny || __any_sync(0xffffffffu, deep))) {
+#pragma unroll 1
+            for (int ch = lane; ch < D; ch += 32) {
+              const int at = Lay::kElem == 2 || !R128 ? (ch & ~63) + (ch & 7) * 8 + ((ch >> 3) & 7) : (ch & 15) * 8 + (ch >> 4);
+              const float *cp = s_coef + (at & ~8) * 4 + ((at >> 3) & 1);
+              const BankCoef c = {cp[0], cp[2], cp[32], cp[34]};
+#pragma unroll 1
+              for (int kk = 0; kk < kTokKeys && key0 + kk < sg.si.ctx; ++kk) {
+                const uint8_t *p = smem + (vt - sbase) + tok_offset<Lay::kBox>(kk, ch * Lay::kElem >> 4) + (ch * Lay::kElem & 15);
+                const float v = FORMAT == kCacheBf16
+                                    ? __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(p))
+                                    : e4m3x2_to_float2(*p).x * paged_scale(smem[scales - sbase + st * 32 + 16 + kk]);
+                emax = fmaxf(emax, fabsf(fmaf(c.d, v, ex2_approx(fmaf(c.b, v, c.s)) + c.ic)));
+              }
             }
           }
         }
