@@ -835,6 +835,8 @@ static constexpr int kTokenRows = 16;
 // What an item costs the kernel of many rows beside its key tiles (queries, a maximum, output), in key tiles.
 static constexpr int kChunkFixed = 7;
 static constexpr int kTokenFixed = 4;
+static constexpr int kChunkWhole = 8;
+static constexpr int kTokenWhole = 0;
 
 int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride_n, int64_t q_stride_h,
                    const float *beta, const int *q_offsets, const int *ctx_lens, const int *block_table,
@@ -883,8 +885,8 @@ int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride
   // whole tokens per row tile, a multiple of 8 where there are as many (the closed sum over row tiles is
   // then short: fem_paged_split.cuh)
   const int tok = 256 / a.group;
-  const SplitShape shape = chunk ? SplitShape{256, 7, tok >= 8 ? tok & ~7 : tok, 1, kChunkFixed}
-                                 : SplitShape{rows <= 8 ? 8 : 16, 6, 0, 2, kTokenFixed};
+  const SplitShape shape = chunk ? SplitShape{256, 7, tok >= 8 ? tok & ~7 : tok, 1, kChunkFixed, kChunkWhole}
+                                 : SplitShape{rows <= 8 ? 8 : 16, 6, 0, 2, kTokenFixed, kTokenWhole};
   const int box_rows = chunk ? std::min(1 << a.c.page_shift, 128) : 16;
   CUtensorMap tk, tv;
   if ((rc = cache_map(&tk, a.c.k, a.c, box_rows)) != FEM_OK || (rc = cache_map(&tv, a.c.v, a.c, box_rows)) != FEM_OK)

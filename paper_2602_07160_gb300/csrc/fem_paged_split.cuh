@@ -122,6 +122,7 @@ struct SplitShape {
   int tok;                  // tokens of a row tile (whole tokens), or 0: rows packed without regard to tokens
   int least;                // key tiles a CTA takes at least
   int fixed;                // what beginning an item costs, in key tiles: the line counts them before its tiles
+  int whole;                // items of up to so many key tiles are not cut: the CTA that has their start has them
 };
 
 // Row tiles of a sequence, for each of its heads; a sequence without rows has none.
@@ -212,6 +213,10 @@ struct SplitWalk {
       const unsigned rest = g.kt_all + sh.fixed - at, take = min(rest, left);
       g.kt0 = max(at - sh.fixed, 0);
       g.kt1 = at + static_cast<int>(take) - sh.fixed;
+      if (g.kt_all <= sh.whole) {
+        g.kt0 = 0;
+        g.kt1 = at == 0 ? g.kt_all : 0;
+      }
       g.x_end = x + rest;
       x += take;
       left -= take;
@@ -226,7 +231,9 @@ struct SplitWalk {
           } while (R == 0);
         }
       }
-      if (g.kt1 > 0) return true;  // else the stretch ends inside the item's fixed cost: the next CTA begins it
+      // else the stretch ends inside the item's fixed cost (the next CTA begins it), or begins inside an item
+      // that is not cut
+      if (g.kt1 > 0) return true;
     }
     return false;
   }
