@@ -35,98 +35,119 @@ __global__ void __launch_bounds__(kExactThreads) paged_exact_kernel(const PagedR
   paged_exact_row<FORMAT>(a, s, si, t, hq, sh);
 }
 
-// What the reading kernel left.  Block (g, part): the item that CTA g began and
-// did not end is joined from its pieces, in the line's order, a warp per row
-// (its lanes side by side over the channels), RW rows per warp; then rows whose
-// result the ranges could have spoilt, these and those CTA g finished, are
-// recomputed by the whole block.
+// What the reading kernel left.  Block (g, part): rows 8 part .. of the item that
+// CTA g began and did not end are joined from its pieces.  The four warps share
+// the pieces out; a lane has row (lane & 7) and every fourth group of 4
+// channels, so that each load is four full lines of a piece, whatever its
+// length; the warps' sums meet in shared memory in the pieces' order.  Then
+// rows whose result the ranges could have spoilt, these and those CTA g
+// finished, are recomputed by the whole block.
 template <int FORMAT, int D>
 __global__ void __launch_bounds__(kExactThreads)
-    paged_finish_kernel(const PagedReadArgs a, const PagedSplit sp, const SplitShape shape, int grid, int RW) {
-  constexpr int E = D / 32, kWarps = kExactThreads / 32;  // channels per lane
-  __shared__ ExactShared sh;
+    paged_finish_kernel(const PagedReadArgs a, const PagedSplit sp, const SplitShape shape, int grid) {
+  constexpr int kWarps = kExactThreads / 32, C = D / 16;  // C: groups of 4 channels per lane
+  __shared__ union {
+    ExactShared exact;
+    float part[kWarps][8][D + 4];
+  } u;
+  __shared__ float s_m[kWarps][8], s_l[kWarps][8], s_wide[kWarps];
   __shared__ int s_list[256];
   __shared__ int s_count;
+  ExactShared &sh = u.exact;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g0 = blockIdx.x, part = blockIdx.y;
   const int row_tile = shape.row_tile;
   if (tid == 0) s_count = 0;
-  __syncthreads();
   grid_dep_wait();
   const SplitRecord rec = sp.records[g0];
   const size_t size = piece_floats(row_tile, D);
   const int n = rec.n;
-  if (n > 0) {
-    const SeqInfo si = paged_seq(a, rec.s);
+  if (part * 8 < rec.rows && n > 0) {
     const float *base = sp.pieces + static_cast<size_t>(g0) * 2 * size;  // piece 0 in slot 1, the others in slot 0
-    auto piece = [&](int i) { return (static_cast<size_t>(i) * 2 + (i == 0 ? 1 : 0)) * size; };
-    for (int k = 0; k < RW; ++k) {
-      const int rr = (part * kWarps + warp) * RW + k, h = rec.h;
-      if (rr >= rec.rows) break;
-      const int t = (rec.row0 + rr) / a.group, hq = h * a.group + (rec.row0 + rr) % a.group;
-      const long long orow = (static_cast<long long>(si.q0) + t) * a.Hq + hq;
-      const float *row = base + static_cast<size_t>(rr) * D + lane * E, *stat = base + row_tile * D + 2 * rr;
-      // lane: piece; then every lane its channels of one piece after the other
-      float M = -INFINITY, L = 0.f, wide = 0.f, acc[E];
-#pragma unroll 1
-      for (int i = lane; i < n; i += 32) M = fmaxf(M, stat[piece(i)]);
+    auto piece = [&](int i) { return base + (static_cast<size_t>(i) * 2 + (i == 0 ? 1 : 0)) * size; };
+    const int r8 = lane & 7, c0 = lane >> 3, rr = part * 8 + r8;
+    const bool on = rr < rec.rows;
+    // this warp's pieces, its rows' sums against the largest maximum among them
+    float m = -INFINITY, l = 0.f, wide = 0.f, acc[C][4];
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    for (int c = 0; c < C; ++c) acc[c][0] = acc[c][1] = acc[c][2] = acc[c][3] = 0.f;
+#pragma unroll 2
+    for (int i = warp; i < n; i += kWarps) {
+      const float *p = piece(i);
+      const float2 st = on ? *reinterpret_cast<const float2 *>(p + row_tile * D + 2 * rr) : make_float2(-INFINITY, 0.f);
+      float4 v[C];
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = 0.f;
-#pragma unroll 1
-      for (int i0 = 0; i0 < n; i0 += 32) {
-        float w = 0.f;
-        if (i0 + lane < n) {
-          const float m = stat[piece(i0 + lane)], l = stat[piece(i0 + lane) + 1];
-          w = m == -INFINITY ? (l != l ? 1.f : 0.f) : ex2_approx(m - M);  // NaN scores have no maximum
-          L += w * l;
-          wide += base[piece(i0 + lane) + row_tile * D + 2 * row_tile + D];
-        }
-        const int cnt = min(32, n - i0);
-#pragma unroll 8
-        for (int i = 0; i < cnt; ++i) {
-          const float wi = __shfl_sync(0xffffffffu, w, i);
-          if (E == 4) {
-            const float4 x = *reinterpret_cast<const float4 *>(row + piece(i0 + i));
-            acc[0] = fmaf(wi, x.x, acc[0]);
-            acc[1] = fmaf(wi, x.y, acc[1]);
-            acc[E - 2] = fmaf(wi, x.z, acc[E - 2]);
-            acc[E - 1] = fmaf(wi, x.w, acc[E - 1]);
-          } else {
-            const float2 x = *reinterpret_cast<const float2 *>(row + piece(i0 + i));
-            acc[0] = fmaf(wi, x.x, acc[0]);
-            acc[1] = fmaf(wi, x.y, acc[1]);
-          }
-        }
+      for (int c = 0; c < C; ++c)
+        v[c] = on ? *reinterpret_cast<const float4 *>(p + piece_at(rr, c0 + 4 * c, D)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      wide += p[row_tile * D + 2 * row_tile + D];
+      const float top = fmaxf(m, st.x);
+      const float w0 = m == -INFINITY ? (l != l ? 1.f : 0.f) : ex2_approx(m - top);
+      const float w1 = st.x == -INFINITY ? (st.y != st.y ? 1.f : 0.f) : ex2_approx(st.x - top);  // NaN scores have no maximum
+      m = top;
+      l = l * w0 + st.y * w1;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        acc[c][0] = fmaf(v[c].x, w1, acc[c][0] * w0);
+        acc[c][1] = fmaf(v[c].y, w1, acc[c][1] * w0);
+        acc[c][2] = fmaf(v[c].z, w1, acc[c][2] * w0);
+        acc[c][3] = fmaf(v[c].w, w1, acc[c][3] * w0);
       }
+    }
+    if (c0 == 0) {
+      s_m[warp][r8] = m;
+      s_l[warp][r8] = l;
+    }
+    if (lane == 0) s_wide[warp] = wide;
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        L += __shfl_xor_sync(0xffffffffu, L, o);
-        wide += __shfl_xor_sync(0xffffffffu, wide, o);
+    for (int c = 0; c < C; ++c)
+      *reinterpret_cast<float4 *>(&u.part[warp][r8][4 * (c0 + 4 * c)]) = make_float4(acc[c][0], acc[c][1], acc[c][2], acc[c][3]);
+    __syncthreads();
+    // warp: rows 2 warp, 2 warp + 1; lane: D / 32 channels side by side
+    const SeqInfo si = paged_seq(a, rec.s);
+    wide = (s_wide[0] + s_wide[1]) + (s_wide[2] + s_wide[3]);
+    constexpr int E = D / 32;
+    OutCoef oc[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int j = lane * E + e;
+      oc[e] = out_coef(a.beta ? __ldg(a.beta + static_cast<long long>(rec.h) * D + j) : 0.f,
+                       piece(0)[row_tile * D + 2 * row_tile + j], a.beta && wide != 0.f);
+    }
+#pragma unroll
+    for (int k = 0; k < 8 / kWarps; ++k) {
+      const int row = warp * (8 / kWarps) + k, rr2 = part * 8 + row;
+      if (rr2 >= rec.rows) break;
+      float M = -INFINITY, L = 0.f, x[E];
+#pragma unroll
+      for (int q = 0; q < kWarps; ++q) M = fmaxf(M, s_m[q][row]);
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = 0.f;
+#pragma unroll
+      for (int q = 0; q < kWarps; ++q) {
+        const float wq = s_m[q][row] == -INFINITY ? (s_l[q][row] != s_l[q][row] ? 1.f : 0.f) : ex2_approx(s_m[q][row] - M);
+        L = fmaf(wq, s_l[q][row], L);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = fmaf(wq, u.part[q][row][lane * E + e], x[e]);
       }
       const bool empty = M == -INFINITY && L == 0.f;
       bool good = true;
-      float o[E];
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         bool ok;
-        const int j = lane * E + e;
-        const float beta = a.beta ? __ldg(a.beta + static_cast<long long>(h) * D + j) : 0.f;
-        o[e] = paged_out(out_coef(beta, base[piece(0) + row_tile * D + 2 * row_tile + j], a.beta && wide != 0.f), acc[e] / L, &ok);
-        if (empty) o[e] = 0.f;
+        x[e] = paged_out(oc[e], x[e] / L, &ok);
+        if (empty) x[e] = 0.f;
         good = good && (ok || empty);
       }
+      const int t = (rec.row0 + rr2) / a.group, hq = rec.h * a.group + (rec.row0 + rr2) % a.group;
+      const long long orow = (static_cast<long long>(si.q0) + t) * a.Hq + hq;
       __nv_bfloat162 *dst = reinterpret_cast<__nv_bfloat162 *>(static_cast<__nv_bfloat16 *>(a.out) + orow * D + lane * E);
 #pragma unroll
-      for (int e = 0; e < E; e += 2) dst[e / 2] = __floats2bfloat162_rn(o[e], o[e + 1]);
+      for (int e = 0; e < E; e += 2) dst[e / 2] = __floats2bfloat162_rn(x[e], x[e + 1]);
       if (lane == 0 && a.lse != nullptr) a.lse[orow] = empty ? -INFINITY : (M + log2f(L)) * kLn2;
-      if (!__all_sync(0xffffffffu, good) && lane == 0) s_list[atomicAdd(&s_count, 1)] = rr;
+      if (!__all_sync(0xffffffffu, good) && lane == 0) s_list[atomicAdd(&s_count, 1)] = rec.row0 + rr2;
     }
     __syncthreads();
-    for (int i = 0; i < s_count; ++i) {
-      const int r = rec.row0 + s_list[i];
-      paged_exact_row<FORMAT>(a, rec.s, si, r / a.group, rec.h * a.group + r % a.group, sh);
-    }
+    for (int i = 0; i < s_count; ++i)
+      paged_exact_row<FORMAT>(a, rec.s, si, s_list[i] / a.group, rec.h * a.group + s_list[i] % a.group, sh);
   }
   if (rec.any_exact) {
     // CTA g's whole items again, for their marked rows
@@ -159,11 +180,9 @@ __global__ void __launch_bounds__(kExactThreads)
 cudaError_t launch_paged_finish(const PagedReadArgs &a, const PagedSplit &sp, const SplitShape &shape, int grid,
                                 cudaStream_t stream) {
   if (shape.row_tile > 256) return cudaErrorInvalidValue;
-  // a row per warp for the row tiles of few rows, two for those of 256
-  const int warps = kExactThreads / 32, RW = shape.row_tile > 16 ? 2 : 1;
-  const dim3 blocks(grid, shape.row_tile / (RW * warps));
+  const dim3 blocks(grid, shape.row_tile / 8);
   auto go = [&](auto kernel) {
-    return launch_kernel(kernel, blocks, dim3(kExactThreads), 0, stream, true, a, sp, shape, grid, RW);
+    return launch_kernel(kernel, blocks, dim3(kExactThreads), 0, stream, true, a, sp, shape, grid);
   };
   if (a.c.format == kCacheBf16)
     return a.c.d == 64 ? go(paged_finish_kernel<kCacheBf16, 64>) : go(paged_finish_kernel<kCacheBf16, 128>);

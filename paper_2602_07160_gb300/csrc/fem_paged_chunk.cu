@@ -563,6 +563,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       return w;
     };
     // Half of the row's query into shared memory, and the arrival that lets the segment's products start.
+
     auto load_q = [&](const Row &w, bool used) {
       if (used) {
         uint8_t *tQ = smem + Lay::kQ + t * Lay::kTile;
@@ -739,7 +740,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             // lane l has the coefficients of the chunk's channel l; every row needs all of them
             const OutCoef oc = out_coef(BETA ? __ldg(a.beta + static_cast<long long>(sg.h) * D + half * kHalfD + c * 32 + lane) : 0.f,
                                         kind_unpack(shift[c * 32 + lane]), wide);
-            uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + orow * D + half * kHalfD + c * 32);
+            __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.out) + orow * D + half * kHalfD + c * 32;
 #pragma unroll
             for (int i4 = 0; i4 < 4; ++i4) {
               uint32_t o[4];
@@ -767,14 +768,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                 }
                 o[i] = empty ? 0u : pack_bf16(x[0], x[1]);
               }
-              if (w.on) dst[i4] = make_uint4(o[0], o[1], o[2], o[3]);
+              if (w.on) *reinterpret_cast<uint4 *>(dst + i4 * 8) = make_uint4(o[0], o[1], o[2], o[3]);
             }
           } else if (w.on) {
-            float4 *dst = reinterpret_cast<float4 *>(piece + static_cast<size_t>(ir) * D + half * kHalfD + c * 32);
+            float *dst = piece + piece_at(ir, (half * kHalfD + c * 32) >> 2, D);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-              dst[i] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]),
-                                   __uint_as_float(v[4 * i + 3]));
+              *reinterpret_cast<float4 *>(dst + i * 32) = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]),
+                                                                      __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
           }
         }
         // both halves' verdict (and the exchange above is read before the next segment's)

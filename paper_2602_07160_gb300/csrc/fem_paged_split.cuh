@@ -335,9 +335,16 @@ __device__ bool split_begin(const PagedReadArgs &a, const SplitShape &shape, int
 // ---------------------------------------------------------------------------
 // Pieces.  CTA g's slot 0 holds the piece at its stretch's start that continues
 // an item of an earlier CTA, slot 1 the piece that begins an item it does not
-// end.  A piece: per row the accumulators [D] (not normalised), then per row
-// {m, L} (log2 units), then the channels' kinds [D], then whether |E| went wide.
+// end.  A piece: the rows' accumulators [rows][D] (not normalised), in groups of
+// 8 rows with 4 channels of the 8 side by side (128 bytes), so that a warp whose
+// lanes are rows and one whose lanes are channels both write full lines; then
+// per row {m, L} (log2 units), then the channels' kinds [D], then whether |E|
+// went wide.
 // ---------------------------------------------------------------------------
+// Channels 4 c4 .. of row `row`, in floats.
+__host__ __device__ constexpr size_t piece_at(int row, int c4, int D) {
+  return (static_cast<size_t>(row >> 3) * (D / 4) + c4) * 32 + (row & 7) * 4;
+}
 __host__ __device__ constexpr size_t piece_floats(int rows, int D) {
   return static_cast<size_t>(rows) * D + 2 * rows + D + 4;
 }

@@ -587,7 +587,7 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
         if (tid == 0 && a.lse != nullptr)
           a.lse[orow] = M == -INFINITY && Lr == 0.f ? -INFINITY : (M + log2f(Lr)) * kLn2;
       } else {
-        if (tid < D) piece[static_cast<size_t>(r) * D + tid] = av;
+        if (tid < D) piece[piece_at(r, tid >> 2, D) + (tid & 3)] = av;
         if (tid == 0) {
           piece[kRows * D + 2 * r] = M;
           piece[kRows * D + 2 * r + 1] = Lr;
