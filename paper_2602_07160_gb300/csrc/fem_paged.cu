@@ -32,30 +32,32 @@ __global__ void __launch_bounds__(kExactThreads) paged_exact_kernel(const PagedR
   const SeqInfo si = paged_seq(a, s);
   const int t = row - si.q0;
   if (t < 0 || t >= si.n) return;  // a row no sequence owns
-  paged_exact_row<FORMAT>(a, s, si, t, hq, sh);
+  paged_exact_row<FORMAT>(a, s, si, t, hq, sh, 0, a.c.d);
 }
 
 // What the reading kernel left.  Block (g, part): rows 8 part .. of the item that
 // CTA g began and did not end are joined from its pieces.  The four warps share
 // the pieces out; a lane has row (lane & 7) and every fourth group of 4
 // channels, so that each load is four full lines of a piece, whatever its
-// length; the warps' sums meet in shared memory in the pieces' order.  Then
+// length; the warps' sums meet in shared memory in the pieces' order.  Where
+// there are few rows and many pieces the channels are shared out over blocks as
+// well, CH to each (blockIdx.z).  Then
 // rows whose result the ranges could have spoilt, these and those CTA g
 // finished, are recomputed by the whole block.
-template <int FORMAT, int D>
+template <int FORMAT, int D, int CH>
 __global__ void __launch_bounds__(kExactThreads)
     paged_finish_kernel(const PagedReadArgs a, const PagedSplit sp, const SplitShape shape, int grid) {
-  constexpr int kWarps = kExactThreads / 32, C = D / 16;  // C: groups of 4 channels per lane
+  constexpr int kWarps = kExactThreads / 32, C = CH / 16;  // C: groups of 4 channels per lane
   __shared__ union {
     ExactShared exact;
-    float part[kWarps][8][D + 4];
+    float part[kWarps][8][CH + 4];
   } u;
   __shared__ float s_m[kWarps][8], s_l[kWarps][8], s_wide[kWarps];
   __shared__ int s_list[256];
   __shared__ int s_count;
   ExactShared &sh = u.exact;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g0 = blockIdx.x, part = blockIdx.y;
-  const int row_tile = shape.row_tile;
+  const int row_tile = shape.row_tile, j_lo = blockIdx.z * CH;
   if (tid == 0) s_count = 0;
   grid_dep_wait();
   const SplitRecord rec = sp.records[g0];
@@ -64,20 +66,20 @@ __global__ void __launch_bounds__(kExactThreads)
   if (part * 8 < rec.rows && n > 0) {
     const float *base = sp.pieces + static_cast<size_t>(g0) * 2 * size;  // piece 0 in slot 1, the others in slot 0
     auto piece = [&](int i) { return base + (static_cast<size_t>(i) * 2 + (i == 0 ? 1 : 0)) * size; };
-    const int r8 = lane & 7, c0 = lane >> 3, rr = part * 8 + r8;
+    const int r8 = lane & 7, c0 = lane >> 3, rr = part * 8 + r8, c4 = j_lo / 4 + c0;
     const bool on = rr < rec.rows;
     // this warp's pieces, its rows' sums against the largest maximum among them
     float m = -INFINITY, l = 0.f, wide = 0.f, acc[C][4];
 #pragma unroll
     for (int c = 0; c < C; ++c) acc[c][0] = acc[c][1] = acc[c][2] = acc[c][3] = 0.f;
-#pragma unroll 2
+#pragma unroll(32 / C)
     for (int i = warp; i < n; i += kWarps) {
       const float *p = piece(i);
       const float2 st = on ? *reinterpret_cast<const float2 *>(p + row_tile * D + 2 * rr) : make_float2(-INFINITY, 0.f);
       float4 v[C];
 #pragma unroll
       for (int c = 0; c < C; ++c)
-        v[c] = on ? *reinterpret_cast<const float4 *>(p + piece_at(rr, c0 + 4 * c, D)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        v[c] = on ? *reinterpret_cast<const float4 *>(p + piece_at(rr, c4 + 4 * c, D)) : make_float4(0.f, 0.f, 0.f, 0.f);
       wide += p[row_tile * D + 2 * row_tile + D];
       const float top = fmaxf(m, st.x);
       const float w0 = m == -INFINITY ? (l != l ? 1.f : 0.f) : ex2_approx(m - top);
@@ -101,14 +103,14 @@ __global__ void __launch_bounds__(kExactThreads)
     for (int c = 0; c < C; ++c)
       *reinterpret_cast<float4 *>(&u.part[warp][r8][4 * (c0 + 4 * c)]) = make_float4(acc[c][0], acc[c][1], acc[c][2], acc[c][3]);
     __syncthreads();
-    // warp: rows 2 warp, 2 warp + 1; lane: D / 32 channels side by side
+    // warp: rows 2 warp, 2 warp + 1; lane: CH / 32 channels side by side
     const SeqInfo si = paged_seq(a, rec.s);
     wide = (s_wide[0] + s_wide[1]) + (s_wide[2] + s_wide[3]);
-    constexpr int E = D / 32;
+    constexpr int E = CH / 32;
     OutCoef oc[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const int j = lane * E + e;
+      const int j = j_lo + lane * E + e;
       oc[e] = out_coef(a.beta ? __ldg(a.beta + static_cast<long long>(rec.h) * D + j) : 0.f,
                        piece(0)[row_tile * D + 2 * row_tile + j], a.beta && wide != 0.f);
     }
@@ -139,15 +141,20 @@ __global__ void __launch_bounds__(kExactThreads)
       }
       const int t = (rec.row0 + rr2) / a.group, hq = rec.h * a.group + (rec.row0 + rr2) % a.group;
       const long long orow = (static_cast<long long>(si.q0) + t) * a.Hq + hq;
-      __nv_bfloat162 *dst = reinterpret_cast<__nv_bfloat162 *>(static_cast<__nv_bfloat16 *>(a.out) + orow * D + lane * E);
+      __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.out) + orow * D + j_lo + lane * E;
+      if (E == 1) {
+        *dst = __float2bfloat16_rn(x[0]);
+      } else {
 #pragma unroll
-      for (int e = 0; e < E; e += 2) dst[e / 2] = __floats2bfloat162_rn(x[e], x[e + 1]);
-      if (lane == 0 && a.lse != nullptr) a.lse[orow] = empty ? -INFINITY : (M + log2f(L)) * kLn2;
+        for (int e = 0; e < E; e += 2)
+          *reinterpret_cast<__nv_bfloat162 *>(dst + e) = __floats2bfloat162_rn(x[e], x[e + (E > 1 ? 1 : 0)]);
+      }
+      if (lane == 0 && j_lo == 0 && a.lse != nullptr) a.lse[orow] = empty ? -INFINITY : (M + log2f(L)) * kLn2;
       if (!__all_sync(0xffffffffu, good) && lane == 0) s_list[atomicAdd(&s_count, 1)] = rec.row0 + rr2;
     }
     __syncthreads();
     for (int i = 0; i < s_count; ++i)
-      paged_exact_row<FORMAT>(a, rec.s, si, s_list[i] / a.group, rec.h * a.group + s_list[i] % a.group, sh);
+      paged_exact_row<FORMAT>(a, rec.s, si, s_list[i] / a.group, rec.h * a.group + s_list[i] % a.group, sh, j_lo, j_lo + CH);
   }
   if (rec.any_exact) {
     // CTA g's whole items again, for their marked rows
@@ -170,7 +177,7 @@ __global__ void __launch_bounds__(kExactThreads)
       }
       __syncthreads();
       for (int i = 0; i < s_count; ++i)
-        paged_exact_row<FORMAT>(a, sg.s, sg.si, s_list[i] / a.group, sg.h * a.group + s_list[i] % a.group, sh);
+        paged_exact_row<FORMAT>(a, sg.s, sg.si, s_list[i] / a.group, sg.h * a.group + s_list[i] % a.group, sh, j_lo, j_lo + CH);
     }
   }
 }
@@ -180,13 +187,19 @@ __global__ void __launch_bounds__(kExactThreads)
 cudaError_t launch_paged_finish(const PagedReadArgs &a, const PagedSplit &sp, const SplitShape &shape, int grid,
                                 cudaStream_t stream) {
   if (shape.row_tile > 256) return cudaErrorInvalidValue;
-  const dim3 blocks(grid, shape.row_tile / 8);
-  auto go = [&](auto kernel) {
-    return launch_kernel(kernel, blocks, dim3(kExactThreads), 0, stream, true, a, sp, shape, grid);
+  const bool few = shape.row_tile <= 16;
+  auto go = [&](auto kernel, int channels) {
+    return launch_kernel(kernel, dim3(grid, shape.row_tile / 8, a.c.d / channels), dim3(kExactThreads), 0, stream, true, a, sp,
+                         shape, grid);
   };
-  if (a.c.format == kCacheBf16)
-    return a.c.d == 64 ? go(paged_finish_kernel<kCacheBf16, 64>) : go(paged_finish_kernel<kCacheBf16, 128>);
-  return a.c.d == 64 ? go(paged_finish_kernel<kCacheE4m3, 64>) : go(paged_finish_kernel<kCacheE4m3, 128>);
+#define FEM_FINISH(F, DD) \
+  if (a.c.format == F && a.c.d == DD) return few ? go(paged_finish_kernel<F, DD, 32>, 32) : go(paged_finish_kernel<F, DD, DD>, DD);
+  FEM_FINISH(kCacheBf16, 64)
+  FEM_FINISH(kCacheBf16, 128)
+  FEM_FINISH(kCacheE4m3, 64)
+  FEM_FINISH(kCacheE4m3, 128)
+#undef FEM_FINISH
+  return cudaErrorInvalidValue;
 }
 
 cudaError_t launch_paged_exact(const PagedReadArgs &a, cudaStream_t stream) {

@@ -66,10 +66,12 @@ __device__ __forceinline__ float paged_dot(const PagedCacheView &c, long long ro
   return FORMAT == kCacheE4m3 ? acc * paged_scale(__ldg(c.ke + row)) : acc;
 }
 
-// Row t of sequence s (si), query head hq, into a.out and a.lse.  All threads
-// of a block of kExactThreads call it together.
+// Row t of sequence s (si), query head hq: channels j_lo .. j_hi - 1 into a.out, and
+// with the first of them a.lse.  All threads of a block of kExactThreads call it
+// together.
 template <int FORMAT>
-__device__ void paged_exact_row(const PagedReadArgs &a, int s, const SeqInfo &si, int t, int hq, ExactShared &sh) {
+__device__ void paged_exact_row(const PagedReadArgs &a, int s, const SeqInfo &si, int t, int hq, ExactShared &sh,
+                                int j_lo, int j_hi) {
   const PagedCacheView &c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, d = c.d, h = hq / a.group;
   const long long qrow = static_cast<long long>(si.q0) + t;
@@ -122,7 +124,7 @@ __device__ void paged_exact_row(const PagedReadArgs &a, int s, const SeqInfo &si
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int j = tid + u * kExactThreads;
-      if (j >= d) continue;
+      if (j < j_lo || j >= j_hi) continue;
       const float b = beta[u];
       // log weights are kept relative to m: the old maximum moves with it (-inf: nothing yet)
       W[u] *= alpha;
@@ -168,7 +170,7 @@ __device__ void paged_exact_row(const PagedReadArgs &a, int s, const SeqInfo &si
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int j = tid + u * kExactThreads;
-    if (j >= d) continue;
+    if (j < j_lo || j >= j_hi) continue;
     float o = 0.f;
     if (!empty) {
       const float b = beta[u], x = b * W[u] / L;
@@ -179,7 +181,7 @@ __device__ void paged_exact_row(const PagedReadArgs &a, int s, const SeqInfo &si
     if (FORMAT == kCacheF32) static_cast<float *>(a.out)[orow * d + j] = o;
     else static_cast<__nv_bfloat16 *>(a.out)[orow * d + j] = __float2bfloat16_rn(o);
   }
-  if (a.lse != nullptr && tid == 0) a.lse[orow] = empty ? -INFINITY : m + logf(L);
+  if (a.lse != nullptr && tid == 0 && j_lo == 0) a.lse[orow] = empty ? -INFINITY : m + logf(L);
 }
 
 }  // namespace fem
