@@ -53,7 +53,8 @@ __device__ __forceinline__ SeqInfo paged_seq(const PagedReadArgs &a, int s) {
   SeqInfo r;
   r.q0 = min(max(q0, 0), a.N);
   r.n = max(min(q1, a.N) - r.q0, 0);
-  const long long cap = static_cast<long long>(a.max_pages) << a.c.page_shift;
+  // (2^30 positions, more than the memory holds, keep every sum of positions in 32 bits)
+  const long long cap = min(static_cast<long long>(a.max_pages) << a.c.page_shift, 1ll << 30);
   r.ctx = static_cast<int>(min(static_cast<long long>(max(ctx, 0)), cap));
   if (r.q0 != q0 || r.n != q1 - q0 || r.ctx != ctx) atomicOr(a.err, kErrPageRange);
   return r;

@@ -721,7 +721,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         if (!(ok = meet())) break;
         if (half == 1) L = s_row[r];
         // ---- the row's output (half of its channels), or its piece
-        if (L == 0.f) m = -INFINITY;  // nothing seen
+        // No weight at all: nothing was seen, or (the segment held keys for the row) every weight fell under
+        // the range, against a maximum so large that bf16 rounds it by more; that is left to the exact path.
+        if (L == 0.f) {
+          m = -INFINITY;
+          if (w.lim > sg.kt0 * kChunkKeys) L = __int_as_float(0x7fffffff);
+        }
         const int ir = t * 128 + r;
         const long long orow = static_cast<long long>(w.qrow) * a.Hq + w.hq;
         const bool whole = sg.kt0 == 0 && sg.kt1 == sg.kt_all;

@@ -273,6 +273,93 @@ def test_read_in_a_graph_follows_the_device_arrays(n):
     assert torch.equal(out, want) and torch.equal(lse, want_lse)
 
 
+@pytest.mark.parametrize("H,Hq,d", [(1, 5, 64), (1, 7, 128), (2, 24, 64), (1, 40, 128), (1, 130, 64), (1, 300, 64)])
+@pytest.mark.parametrize("n", [1, 3, 90])
+def test_any_number_of_query_heads(H, Hq, d, n):
+    """Groups that are no power of two, wider than a row tile's tokens, wider than a row tile."""
+    lens = [(n, n + 200), (1, 1), (n, n)]
+    args = make("e4m3", H, Hq, d, 32, lens, seed=Hq)
+    check(args[0], args[1], make_beta((0.1, 5.0), H, d), *args[2:], causal=True, max_q=n)
+
+
+@pytest.mark.parametrize("n,S", [(1, 200), (2, 1000), (20, 300)])
+def test_many_sequences(n, S):
+    """More sequences than a block has threads, some without rows, some without a cache."""
+    lens = [(0, 5) if s % 7 == 3 else (1, 0) if s % 31 == 30 else (1 + s % n, 1 + s % n + (s * 13) % 150) for s in range(S)]
+    args = make("bf16", 1, 2, 64, 16, lens, seed=S)
+    check(args[0], args[1], make_beta((0.1, 5.0), 1, 64), *args[2:], causal=True, max_q=n)
+
+
+@pytest.mark.parametrize("n", [1, 4, 60])
+@pytest.mark.parametrize("jump", [40.0, 80.0, 300.0, 40000.0])
+def test_scores_that_jump(n, jump):
+    """Scores that rise or fall by far more than the weights' range from one key tile to another."""
+    for sign in (1.0, -1.0):
+        q, cache, off, ctx, table = make("bf16", 1, 2, 64, 64, [(n, 900)], seed=21)
+        pos = torch.arange(900, device=DEV)
+        where, row = table[0].long()[pos // 64], pos % 64
+        q.zero_()
+        q[..., 0] = 8.0                       # score: k_0 in natural units
+        k0 = torch.where(pos >= 450, sign * jump, 0.0) + torch.sin(pos.float())
+        cache.k[where, 0, row] = 0
+        cache.k[where, 0, row, 0] = k0.to(torch.bfloat16)
+        for beta in (None, torch.full((1, 64), 0.7, device=DEV), torch.full((1, 64), 8.0, device=DEV)):
+            check(q, cache, beta, off, ctx, table, causal=True, max_q=n, rms=False)
+
+
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("big", [50.0, 3.0e4])
+def test_values_far_from_the_first_ones(n, big):
+    """Channels whose first values are tiny, zero or negative and whose later ones are not."""
+    q, cache, off, ctx, table = make("bf16", 1, 2, 64, 16, [(n, 300)], seed=22, q_scale=3.0)
+    pos = torch.arange(300, device=DEV)
+    where, row = table[0].long()[pos // 16], pos % 16
+    g = torch.Generator().manual_seed(5)
+    v = torch.randn((300, 64), generator=g).to(DEV)
+    v[:16, :16] = 0
+    v[:16, 16:32] *= 1e-4
+    v[:16, 32:48] = -big
+    v[200, 8:40] = big
+    cache.v[where, 0, row] = v.to(torch.bfloat16)
+    for beta in (1e-5, 1e-3, 0.3, 4.0):
+        check(q, cache, torch.full((1, 64), beta, device=DEV), off, ctx, table, causal=True, max_q=n, rms=False)
+
+
+def test_read_over_a_cache_past_32_bits():
+    """Pages past 2^31 elements of the cache are read at their own place."""
+    H, d, page = 8, 128, 64
+    pages = (1 << 31) // (H * d * page) + 8
+    k = torch.empty((pages, H, page, d), dtype=torch.bfloat16, device=DEV)
+    cache = fem.PagedCache(k, torch.empty_like(k))
+    g = torch.Generator().manual_seed(2)
+    table = torch.tensor([[pages - 1, 3, pages - 4]], dtype=torch.int32, device=DEV)
+    for p in table[0].tolist():
+        cache.k[p] = torch.randn((H, page, d), generator=g).to(torch.bfloat16).to(DEV)
+        cache.v[p] = torch.randn((H, page, d), generator=g).to(torch.bfloat16).to(DEV)
+    beta = make_beta((0.1, 5.0), H, d)
+    for n in (1, 100):
+        q = torch.randn((n, H, d), generator=g).to(torch.bfloat16).to(DEV)
+        off = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+        check(q, cache, beta, off, torch.tensor([170], dtype=torch.int32, device=DEV), table, causal=True, max_q=n)
+
+
+@pytest.mark.parametrize("n", [1, 50])
+def test_infinite_and_nan_rows(n):
+    """A query of NaN gives NaN in its own row alone; a key of -inf has no weight."""
+    q, cache, off, ctx, table = make("bf16", 1, 2, 128, 32, [(n, 333), (n, 100)], seed=30)
+    q[0, 0] = math.nan
+    beta = make_beta((0.1, 5.0), 1, 128)
+    for b in (None, beta):
+        out, lse = fem.fem_paged_read(q, cache, b, off, ctx, table, max_q=n)
+        assert torch.isnan(out[0, 0]).all() and torch.isnan(lse[0, 0])
+        ref, ref_lse, big = R.read(q, cache, b, off, ctx, table, True)
+        ok = torch.isfinite(ref_lse)
+        assert ok.sum().item() == ok.numel() - 1
+        assert torch.isfinite(out[ok]).all()
+        assert ((out.double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2.0 ** -7 * big)[ok].all()
+    fem.check_device_error()
+
+
 def test_matches_the_contiguous_reads():
     """The same tokens through fem_decode and fem_fwd (contiguous, one head per key/value head)."""
     H, d, T = 4, 128, 700
