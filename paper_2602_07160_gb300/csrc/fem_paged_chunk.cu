@@ -142,6 +142,13 @@ __device__ __forceinline__ uint32_t elect_one() {
   return r;
 }
 
+// 8 columns of the warp's lanes of TMEM (see tmem_ld32).
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
+}
+
 // max(|a|, |b|, |c|)
 __device__ __forceinline__ float fmax3_abs(float a, float b, float c) {
   float r;
@@ -363,7 +370,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     const int rl = tid & 7, col = (tid >> 3) % (D / 4);
     constexpr int kRowStep = kBankThreads / (D / 4), kRowsEach = 128 / kRowStep;
     const int r_first = rl + 8 * ((tid >> 3) / (D / 4));
-    constexpr int kBatch = 4;
+    constexpr int kBatch = kCodes ? 4 : 8;  // rows whose loads are under way together (fewer where each takes more registers)
     // The thread's 4 codes of its first row in a staging tile, and its 4 elements in a tile of bf16; its rows
     // are a multiple of 8 apart, so they share the swizzle's pattern and lie at a fixed distance.
     static_assert(kRowStep % 8 == 0, "rows share the swizzle's pattern");
@@ -668,10 +675,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           const float mz = m == -INFINITY ? 0.f : m;
           const float2 scale2 = make_float2(qk_scale, qk_scale), negm2 = make_float2(-mz, -mz);
           float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-          uint32_t p[32];
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            uint32_t sr[32];
+            uint32_t sr[32], p[16];
             tmem_ld32(tS + c * 32, sr);
             tmem_ld_wait();
             if (masked) mask(c, sr);
@@ -680,16 +686,16 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
               const float2 x = __ffma2_rn(make_float2(__uint_as_float(sr[2 * i]), __uint_as_float(sr[2 * i + 1])), scale2, negm2);
               const float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y));
               ls[i & 1] = __fadd2_rn(ls[i & 1], e);
-              p[c * 16 + i] = pack_bf16(e.x, e.y);
+              p[i] = pack_bf16(e.x, e.y);
             }
+            tmem_st16(tS + c * 16, p);  // over columns already read
           }
           const float sum = (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
           if (__any_sync(0xffffffffu, sum > kAskSum)) {
-            const __nv_bfloat16 mine = largest();
-            s_top[2 * r + half] = sum > kAskSum ? mine : __float2bfloat16_rn(-INFINITY);
+            // m + log2(sum) is at least the largest score, and at most 6 more
+            s_top[2 * r + half] = __float2bfloat16_rn(sum > kAskSum ? m + lg2_approx(sum) : -INFINITY);
             if (lane == 0) s_ask[half] = ns;
           }
-          tmem_st32(tS, p);
           L += sum;
           tmem_st_wait();
           tc_fence_before_sync();
@@ -736,51 +742,51 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         const bool empty = L == 0.f;
         const float inv_l = empty ? 0.f : 1.f / L;
         bool good = true;
+        // 8 channels at a time (a loop of a few lines: the instruction cache serves all roles at once).  Lane l has
+        // the coefficients of channel l of a group of 32; every row needs all of them
+        OutCoef oc = {};
 #pragma unroll 1
-        for (int c = 0; c < kHalfD / 32; ++c) {
-          uint32_t v[32];
-          tmem_ld32(tO + c * 32, v);
+        for (int c = 0; c < kHalfD; c += 8) {
+          uint32_t v[8];
+          tmem_ld8(tO + c, v);
           tmem_ld_wait();
           if (whole) {
-            // lane l has the coefficients of the chunk's channel l; every row needs all of them
-            const OutCoef oc = out_coef(BETA ? __ldg(a.beta + static_cast<long long>(sg.h) * D + half * kHalfD + c * 32 + lane) : 0.f,
-                                        kind_unpack(shift[c * 32 + lane]), wide);
-            __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.out) + orow * D + half * kHalfD + c * 32;
+            if (BETA && (c & 31) == 0)
+              oc = out_coef(__ldg(a.beta + static_cast<long long>(sg.h) * D + half * kHalfD + c + lane), kind_unpack(shift[c + lane]), wide);
+            uint32_t o[4];
 #pragma unroll
-            for (int i4 = 0; i4 < 4; ++i4) {
-              uint32_t o[4];
+            for (int i = 0; i < 4; ++i) {
+              float x[2];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                float x[2];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                  const int j = 8 * i4 + 2 * i + u;
-                  const float av = __uint_as_float(v[j]) * inv_l;
-                  if (BETA) {
-                    OutCoef kf;
-                    kf.g = __shfl_sync(0xffffffffu, oc.g, j);
-                    kf.z = __shfl_sync(0xffffffffu, oc.z, j);
-                    kf.y = __shfl_sync(0xffffffffu, oc.y, j);
-                    kf.w = __shfl_sync(0xffffffffu, oc.w, j);
-                    kf.lo = __shfl_sync(0xffffffffu, oc.lo, j);
-                    bool fine;
-                    x[u] = paged_out(kf, av, &fine);
-                    good = good && fine;
-                  } else {
-                    x[u] = av;
-                    good = good && fabsf(av) < kMostA;
-                  }
+              for (int u = 0; u < 2; ++u) {
+                const float av = __uint_as_float(v[2 * i + u]) * inv_l;
+                if (BETA) {
+                  const int from = (c & 31) + 2 * i + u;
+                  OutCoef kf;
+                  kf.g = __shfl_sync(0xffffffffu, oc.g, from);
+                  kf.z = __shfl_sync(0xffffffffu, oc.z, from);
+                  kf.y = __shfl_sync(0xffffffffu, oc.y, from);
+                  kf.w = __shfl_sync(0xffffffffu, oc.w, from);
+                  kf.lo = __shfl_sync(0xffffffffu, oc.lo, from);
+                  bool fine;
+                  x[u] = paged_out(kf, av, &fine);
+                  good = good && fine;
+                } else {
+                  x[u] = av;
+                  good = good && fabsf(av) < kMostA;
                 }
-                o[i] = empty ? 0u : pack_bf16(x[0], x[1]);
               }
-              if (w.on) *reinterpret_cast<uint4 *>(dst + i4 * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+              o[i] = empty ? 0u : pack_bf16(x[0], x[1]);
             }
+            if (w.on)
+              *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + orow * D + half * kHalfD + c) =
+                  make_uint4(o[0], o[1], o[2], o[3]);
           } else if (w.on) {
-            float *dst = piece + piece_at(ir, (half * kHalfD + c * 32) >> 2, D);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              *reinterpret_cast<float4 *>(dst + i * 32) = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]),
-                                                                      __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+            float *dst = piece + piece_at(ir, (half * kHalfD + c) >> 2, D);
+            *reinterpret_cast<float4 *>(dst) =
+                make_float4(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]), __uint_as_float(v[3]));
+            *reinterpret_cast<float4 *>(dst + 32) =
+                make_float4(__uint_as_float(v[4]), __uint_as_float(v[5]), __uint_as_float(v[6]), __uint_as_float(v[7]));
           }
         }
         // both halves' verdict (and the exchange above is read before the next segment's)
