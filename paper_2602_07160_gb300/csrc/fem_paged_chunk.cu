@@ -675,11 +675,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           const float mz = m == -INFINITY ? 0.f : m;
           const float2 scale2 = make_float2(qk_scale, qk_scale), negm2 = make_float2(-mz, -mz);
           float2 ls[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          uint32_t both[2][32];
+          tmem_ld32(tS, both[0]);
+          tmem_ld32(tS + 32, both[1]);
+          tmem_ld_wait();
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            uint32_t sr[32], p[16];
-            tmem_ld32(tS + c * 32, sr);
-            tmem_ld_wait();
+            uint32_t p[16];
+            uint32_t(&sr)[32] = both[c];
             if (masked) mask(c, sr);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {

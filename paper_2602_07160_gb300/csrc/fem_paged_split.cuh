@@ -14,7 +14,7 @@
 // E(v), in bf16 with fp32 sums, a = sum P E / sum P.  Channel j of a sequence
 // and head goes by its first kSampleKeys values v:
 //   tiny     (beta max|v| <= 2^-12)  E = D v,                    o = a / D
-//   linear   (beta max|v| <= 2)      E = expm1(beta v),          o = log1p(a) / beta
+//   linear   (beta max|v| <= 1.25)   E = expm1(beta v),          o = log1p(a) / beta
 //   shifted  (else)                  E = exp(beta (v - c)),      o = c + log(a) / beta,  c about max v
 // Tiny and linear keep small beta free of cancellation: E = v leaves out
 // beta v^2 / 2, at most 2^-9 |v| where it is let through, and expm1 by
@@ -29,7 +29,8 @@
 namespace fem {
 
 constexpr int kSampleKeys = 16;
-constexpr float kLinearReach = 2.f;            // beta max|v| up to which a channel is linear
+constexpr float kLinearReach = 1.25f;          // beta max|v| up to which a channel is linear: rows that see only the
+                                               // sample then keep 1 + a over e^-1.25 > kLeastLinear
 constexpr float kTinyReach = 0.000244140625f;  // 2^-12: up to which it is tiny
 // What the range of bf16 and fp32 may cost: a term whose weight or bank underflows is lost.  It is
 // at most 2^-126 times the other factor's largest: 2^8 (P) or the largest |E| met.  While that is at
