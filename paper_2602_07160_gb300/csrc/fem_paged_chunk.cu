@@ -616,8 +616,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
               sr[j] = seen ? sr[j] : 0xff800000u;
             }
           };
-          // The half row's largest score, rounded to bf16: a maximum need not be exact, only the same for
-          // both threads.
+          // the half row's largest score
           auto largest = [&]() {
             float y = -INFINITY;
 #pragma unroll 1
@@ -629,7 +628,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
 #pragma unroll
               for (int j = 0; j < 32; j += 2) y = fmax3(y, __uint_as_float(sr[j]), __uint_as_float(sr[j + 1]));
             }
-            return __float2bfloat16_rn(y * qk_scale);
+            return y * qk_scale;
           };
           // The row's maximum moves to `top`: its sum, and its half of the products so far (of the key tiles
           // before: see the issue order), are rescaled.  Whole warps.
@@ -653,11 +652,15 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             }
           };
           if (__any_sync(0xffffffffu, m == -INFINITY)) {
-            // the first tile with something to see: the two threads agree on a maximum
-            const __nv_bfloat16 mine = largest();
-            s_top[2 * r + half] = mine;
+            // the first tile with something to see: the two threads agree on the row's maximum, exactly, so
+            // that the weight of its key is 1 and not a rounding of it
+            float top = largest();
+            if (half == 1) s_row[r] = top;
             if (!(ok = meet())) break;
-            raise(fmaxf(__bfloat162float(mine), __bfloat162float(s_top[2 * r + (half ^ 1)])), k > 0);
+            if (half == 0) s_row[r] = top = fmaxf(top, s_row[r]);
+            if (!(ok = meet())) break;
+            if (half == 1) top = s_row[r];
+            raise(top, k > 0);
           } else {
             // a maximum asked for during the tile before: what either thread wrote then is seen by both
             // now, through the arrivals of P and the product they let start

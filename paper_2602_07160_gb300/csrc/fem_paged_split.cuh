@@ -14,7 +14,7 @@
 // E(v), in bf16 with fp32 sums, a = sum P E / sum P.  Channel j of a sequence
 // and head goes by its first kSampleKeys values v:
 //   tiny     (beta max|v| <= 2^-12)  E = D v,                    o = a / D
-//   linear   (beta max|v| <= 1.25)   E = expm1(beta v),          o = log1p(a) / beta
+//   linear   (beta max|v| <= 1)      E = expm1(beta v),          o = log1p(a) / beta
 //   shifted  (else)                  E = exp(beta (v - c)),      o = c + log(a) / beta,  c about max v
 // Tiny and linear keep small beta free of cancellation: E = v leaves out
 // beta v^2 / 2, at most 2^-9 |v| where it is let through, and expm1 by
@@ -29,8 +29,8 @@
 namespace fem {
 
 constexpr int kSampleKeys = 16;
-constexpr float kLinearReach = 1.25f;          // beta max|v| up to which a channel is linear: rows that see only the
-                                               // sample then keep 1 + a over e^-1.25 > kLeastLinear
+constexpr float kLinearReach = 1.f;            // beta max|v| up to which a channel is linear: rows that see only the
+                                               // sample then keep 1 + a over e^-1 > kLeastLinear
 constexpr float kTinyReach = 0.000244140625f;  // 2^-12: up to which it is tiny
 // What the range of bf16 and fp32 may cost: a term whose weight or bank underflows is lost.  It is
 // at most 2^-126 times the other factor's largest: 2^8 (P) or the largest |E| met.  While that is at
@@ -40,7 +40,8 @@ constexpr float kWideE = 1073741824.f;      // 2^30
 constexpr float kLeastA = 1.3552527e-20f;   // 2^-66
 constexpr float kMostA = 1.2980742e33f;     // 2^110
 constexpr float kDeepP = -100.f;            // log2 of a weight below which its term may be lost (the kernel that looks)
-constexpr float kLeastLinear = 0.25f;       // 1 + a of a linear channel: less cancels more than two bits
+constexpr float kLeastLinear = 0.3125f;     // 1 + a of a linear channel: there a rounding of E (2^-8 of it) is
+                                            // 2^-8 (1 - 1/(1 + a)) / beta in the result, under 2^-7 |v|
 
 // Scale D of a tiny channel, a power of two: |E| reaches 2^30 where beta |v| reaches 2^-8 (to a factor 2).
 __device__ __forceinline__ float tiny_scale(float beta) {
