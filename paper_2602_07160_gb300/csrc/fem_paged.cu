@@ -32,7 +32,7 @@ __global__ void __launch_bounds__(kExactThreads) paged_exact_kernel(const PagedR
   const SeqInfo si = paged_seq(a, s);
   const int t = row - si.q0;
   if (t < 0 || t >= si.n) return;  // a row no sequence owns
-  paged_exact_row<FORMAT>(a, s, si, t, hq, sh, 0, a.c.d);
+  paged_exact_row<FORMAT>(a, s, si, t, hq, sh, 0, a.c.d, false);
 }
 
 // What the reading kernel left.  Block (g, part): rows 8 part .. of the item that
@@ -42,10 +42,10 @@ __global__ void __launch_bounds__(kExactThreads) paged_exact_kernel(const PagedR
 // length; the warps' sums meet in shared memory in the pieces' order.  Where
 // there are few rows and many pieces the channels are shared out over blocks as
 // well, CH to each (blockIdx.z).  Then
-// rows whose result the ranges could have spoilt, these and those CTA g
-// finished, are recomputed by the whole block.
+// channels whose result the ranges could have spoilt (marked in the output), of
+// these rows and of those CTA g finished, are recomputed by the whole block.
 template <int FORMAT, int D, int CH>
-__global__ void __launch_bounds__(kExactThreads)
+__global__ void __launch_bounds__(kExactThreads, 7)
     paged_finish_kernel(const PagedReadArgs a, const PagedSplit sp, const SplitShape shape, int grid) {
   constexpr int kWarps = kExactThreads / 32, C = CH / 16;  // C: groups of 4 channels per lane
   __shared__ union {
@@ -63,9 +63,15 @@ __global__ void __launch_bounds__(kExactThreads)
   const SplitRecord rec = sp.records[g0];
   const size_t size = piece_floats(row_tile, D);
   const int n = rec.n;
+  const float *base = sp.pieces + static_cast<size_t>(g0) * 2 * size;  // piece 0 in slot 1, the others in slot 0
+  auto piece = [&](int i) { return base + (static_cast<size_t>(i) * 2 + (i == 0 ? 1 : 0)) * size; };
+  // the class of channel j: the largest of its pieces'
+  auto widest = [&](int j) {
+    float most = 0.f;
+    for (int i = 0; i < n; ++i) most = fmaxf(most, piece(i)[piece_classes(row_tile, D) + j]);
+    return static_cast<int>(most);
+  };
   if (part * 8 < rec.rows && n > 0) {
-    const float *base = sp.pieces + static_cast<size_t>(g0) * 2 * size;  // piece 0 in slot 1, the others in slot 0
-    auto piece = [&](int i) { return base + (static_cast<size_t>(i) * 2 + (i == 0 ? 1 : 0)) * size; };
     const int r8 = lane & 7, c0 = lane >> 3, rr = part * 8 + r8, c4 = j_lo / 4 + c0;
     const bool on = rr < rec.rows;
     // this warp's pieces, its rows' sums against the largest maximum among them
@@ -80,7 +86,8 @@ __global__ void __launch_bounds__(kExactThreads)
 #pragma unroll
       for (int c = 0; c < C; ++c)
         v[c] = on ? *reinterpret_cast<const float4 *>(p + piece_at(rr, c4 + 4 * c, D)) : make_float4(0.f, 0.f, 0.f, 0.f);
-      wide += p[row_tile * D + 2 * row_tile + D];
+      const float4 wd = *reinterpret_cast<const float4 *>(p + piece_wide(row_tile, D));
+      wide += (wd.x + wd.y) + (wd.z + wd.w);
       const float top = fmaxf(m, st.x);
       const float w0 = m == -INFINITY ? (l != l ? 1.f : 0.f) : ex2_approx(m - top);
       const float w1 = st.x == -INFINITY ? (st.y != st.y ? 1.f : 0.f) : ex2_approx(st.x - top);  // NaN scores have no maximum
@@ -112,7 +119,7 @@ __global__ void __launch_bounds__(kExactThreads)
     for (int e = 0; e < E; ++e) {
       const int j = j_lo + lane * E + e;
       oc[e] = out_coef(a.beta ? __ldg(a.beta + static_cast<long long>(rec.h) * D + j) : 0.f,
-                       piece(0)[row_tile * D + 2 * row_tile + j], a.beta && wide != 0.f);
+                       piece(0)[piece_kinds(row_tile, D) + j], a.beta && wide != 0.f ? widest(j) : 0);
     }
 #pragma unroll
     for (int k = 0; k < 8 / kWarps; ++k) {
@@ -135,7 +142,8 @@ __global__ void __launch_bounds__(kExactThreads)
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         bool ok;
-        x[e] = paged_out(oc[e], x[e] / L, &ok);
+        x[e] = paged_out(oc[e], x[e] * ((a.beta ? kBankUnit : 1.f) / L), &ok);
+        if (!ok) x[e] = __int_as_float(0x7fffffff);  // the mark, as bf16
         if (empty) x[e] = 0.f;
         good = good && (ok || empty);
       }
@@ -154,7 +162,8 @@ __global__ void __launch_bounds__(kExactThreads)
     }
     __syncthreads();
     for (int i = 0; i < s_count; ++i)
-      paged_exact_row<FORMAT>(a, rec.s, si, s_list[i] / a.group, rec.h * a.group + s_list[i] % a.group, sh, j_lo, j_lo + CH);
+      paged_exact_row<FORMAT>(a, rec.s, si, s_list[i] / a.group, rec.h * a.group + s_list[i] % a.group, sh, j_lo, j_lo + CH,
+                              true);
   }
   if (rec.any_exact) {
     // CTA g's whole items again, for their marked rows
@@ -177,7 +186,8 @@ __global__ void __launch_bounds__(kExactThreads)
       }
       __syncthreads();
       for (int i = 0; i < s_count; ++i)
-        paged_exact_row<FORMAT>(a, sg.s, sg.si, s_list[i] / a.group, sg.h * a.group + s_list[i] % a.group, sh, j_lo, j_lo + CH);
+        paged_exact_row<FORMAT>(a, sg.s, sg.si, s_list[i] / a.group, sg.h * a.group + s_list[i] % a.group, sh, j_lo, j_lo + CH,
+                                true);
     }
   }
 }

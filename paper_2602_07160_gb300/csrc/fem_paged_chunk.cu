@@ -63,19 +63,23 @@ struct ChunkLayout {
   static constexpr uint32_t kRawV = kRawK + kRaw;
   static constexpr uint32_t kCtl = kRawV + kRaw;
   static constexpr uint32_t kShift = kCtl;                       // channels' kinds, 16 bits, [kSegRing][D]
-  static constexpr uint32_t kRow = kShift + kSegRing * D * 2;  // what the threads of a row exchange: 4 bytes per row
+  // classes of the channels' |E|, four of 4 bits in 16: [kSegRing], one for each group of the bank's threads
+  // that has the channel, [D / 4]
+  static constexpr int kParts = 128 / D;
+  static constexpr uint32_t kClass = kShift + kSegRing * D * 2;
+  static constexpr uint32_t kRow = (kClass + kSegRing * kParts * (D / 4) * 2 + 15) & ~15u;  // what the threads of a row exchange: 4 bytes per row
   static constexpr uint32_t kAsk = kRow + 2 * 128 * 4;         // per pair of warps and half: see the softmax
   static constexpr uint32_t kRecord = kAsk + 16 * 4;
   static constexpr uint32_t kInv = kRecord + sizeof(SplitRecord);         // [kInvRing]
-  static constexpr uint32_t kWide = kInv + kInvRing * 4;                  // [kSegRing]: number (from 1) of the segment whose |E| went wide
-  static constexpr uint32_t kScaleK = (kWide + kSegRing * 4 + 15) & ~15u;  // e4m3: scale bytes of the staged keys, then values
+  static constexpr uint32_t kScaleK = (kInv + kInvRing * 4 + 15) & ~15u;  // e4m3: scale bytes of the staged keys, then values
   static constexpr uint32_t kScaleV = kScaleK + (FORMAT == kCacheE4m3 ? 128 : 0);
   static constexpr uint32_t kBars = (kScaleV + (FORMAT == kCacheE4m3 ? 128 : 0) + 7) & ~7u;
   static constexpr uint32_t kNumBars = 33;
   static constexpr uint32_t kTmem = kBars + kNumBars * 8;
   static constexpr uint32_t kAbort = kTmem + 4;
-  static constexpr uint32_t kScan = (kAbort + 4 + 7) & ~7u;
-  static constexpr uint32_t kBytes = kScan + sizeof(SplitScan<kChunkThreads>);
+  static constexpr uint32_t kScan = kRow;  // before the roles begin
+  static_assert(sizeof(SplitScan<kChunkThreads>) <= 1024, "the scan lies over kRow");
+  static constexpr uint32_t kBytes = kAbort + 4;
   static_assert(kBytes <= 227 * 1024, "shared memory");
 };
 
@@ -149,13 +153,6 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
                : "r"(taddr));
 }
 
-// max(|a|, |b|, |c|)
-__device__ __forceinline__ float fmax3_abs(float a, float b, float c) {
-  float r;
-  asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t *>(&v);
@@ -190,7 +187,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
   SplitScan<kChunkThreads> &scan = *reinterpret_cast<SplitScan<kChunkThreads> *>(smem + Lay::kScan);
   short *s_shift = reinterpret_cast<short *>(smem + Lay::kShift);
   volatile unsigned *s_inv = reinterpret_cast<volatile unsigned *>(smem + Lay::kInv);
-  volatile int *s_wide = reinterpret_cast<volatile int *>(smem + Lay::kWide);
+  unsigned short *s_class = reinterpret_cast<unsigned short *>(smem + Lay::kClass);
   const int box_rows = 1 << box_shift;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
 
@@ -229,7 +226,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     mbar_init(FEM_CB(kCbDone), 1);
     fence_mbar_init();
     *abort_flag = 0;
-    for (unsigned i = 0; i < kSegRing; ++i) s_wide[i] = 0;
     for (int i = 0; i < 16; ++i) reinterpret_cast<unsigned *>(smem + Lay::kAsk)[i] = ~0u;  // no tile
   }
   tc_fence_before_sync();
@@ -429,7 +425,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           cd[e / 2] = make_float2(x.d, y.d);
         }
       }
-      float emax = 0.f;
+      uint32_t most = 0;   // of each of the thread's channels, a byte: the exponent field of its largest |E| in tiles with a wide one
       bool wrote = false;  // this segment's shifts, once its first stage is free
       for (int kt = sg.kt0; ok && kt < sg.kt1; ++kt, ++n) {
         const unsigned st = n & 1, use = n >> 1, es = n % kES, euse = n / kES;
@@ -489,6 +485,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           }
         }
         if (BETA || kCodes || ragged) {
+          uint32_t all[2] = {0, 0};  // the bits of the tile's E
           // rows in batches: their loads leave together (a store to the tile would hold the next row's back)
 #pragma unroll 1
           for (int i0 = 0; i0 < kRowsEach; i0 += kBatch) {
@@ -506,9 +503,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             }
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
-              const int r = r_first + kRowStep * (i0 + u);
               const uint32_t x[2] = {w[u].x, w[u].y};
-              const bool none = ragged && gone(r);  // whatever is there, it has no part in the largest |E| either
+              const bool none = ragged && gone(r_first + kRowStep * (i0 + u));  // whatever is there, it has no part in the largest |E| either
               uint32_t y[2];
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
@@ -516,13 +512,31 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                                   : make_float2(bf16_lo(x[e]), bf16_hi(x[e]));
                 if (BETA) v = bank_pair(cb[e], cs[e], ci[e], cd[e], v);
                 if (none) v = make_float2(0.f, 0.f);
-                if (BETA) emax = fmax3_abs(emax, v.x, v.y);
                 y[e] = pack_bf16(v.x, v.y);
+                if (BETA) all[e] |= y[e];
               }
               *reinterpret_cast<uint2 *>(tE + first + kStep * (i0 + u)) = make_uint2(y[0], y[1]);
             }
           }
-          if (BETA && emax > kWideE) s_wide[seg % kSegRing] = static_cast<int>(seg + 1);
+          // 2 or more sets the exponent's highest bit
+          if (BETA && ((all[0] | all[1]) & 0x40004000u)) {
+#pragma unroll 1
+            for (int u = 0; u < kRowsEach; ++u) {
+              const uint2 y = *reinterpret_cast<const uint2 *>(tE + first + kStep * u);
+              most = __vmaxu4(most, __byte_perm((y.x >> 7) & 0xff00ffu, (y.y >> 7) & 0xff00ffu, 0x6420));
+            }
+          }
+        }
+        if (BETA && kt == sg.kt1 - 1) {
+          // the channels' classes over the segment: eight lanes (rl) have them, one writes
+          uint32_t c = 0;
+          if (__any_sync(0xffffffffu, most != 0)) {
+#pragma unroll 1
+            for (int o = 1; o < 8; o <<= 1) most = __vmaxu4(most, __shfl_xor_sync(0xffffffffu, most, o));
+#pragma unroll 1
+            for (int e = 0; e < 16; e += 4) c |= static_cast<uint32_t>(wide_class((most >> (2 * e)) & 0xff)) << e;
+          }
+          if (rl == 0) s_class[(seg % kSegRing * Lay::kParts + (tid >> 3) / (D / 4)) * (D / 4) + col] = static_cast<unsigned short>(c);
         }
         fence_proxy_async_smem();
         mbar_arrive(FEM_CB(kCbEFull + es));
@@ -542,7 +556,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + t * 128 + half * 64 + lane_off;  // P goes over the first 32 of these 64 columns
     const uint32_t tO = tmem + 256 + t * D + half * kHalfD + lane_off;
-    // per row: a maximum of each half in bf16, or a sum; per half and warp: the tile of its last request
+    // per row: a maximum or a sum, or a maximum of each half in bf16; per half and warp: the tile of its last
+    // request
     float *s_row = reinterpret_cast<float *>(smem + Lay::kRow) + t * 128;
     volatile __nv_bfloat16 *s_top = reinterpret_cast<volatile __nv_bfloat16 *>(s_row);
     volatile unsigned *s_ask = reinterpret_cast<volatile unsigned *>(smem + Lay::kAsk) + (t * 4 + (warp & 3)) * 2;
@@ -570,7 +585,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
       return w;
     };
     // Half of the row's query into shared memory, and the arrival that lets the segment's products start.
-
     auto load_q = [&](const Row &w, bool used) {
       if (used) {
         uint8_t *tQ = smem + Lay::kQ + t * Lay::kTile;
@@ -742,11 +756,17 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         const int ir = t * 128 + r;
         const long long orow = static_cast<long long>(w.qrow) * a.Hq + w.hq;
         const bool whole = sg.kt0 == 0 && sg.kt1 == sg.kt_all;
-        const bool wide = BETA && s_wide[seg % kSegRing] == static_cast<int>(seg + 1);
+        const unsigned short *classes = s_class + seg % kSegRing * Lay::kParts * (D / 4);
+        auto wide = [&](int j) {
+          int c = 0;
+#pragma unroll
+          for (int i = 0; i < Lay::kParts; ++i) c = max(c, (classes[i * (D / 4) + (j >> 2)] >> (4 * (j & 3))) & 15);
+          return c;
+        };
         const short *shift = s_shift + (seg % kSegRing) * D + half * kHalfD;
         float *piece = sp.pieces + static_cast<size_t>(cta * 2 + (sg.kt0 == 0 ? 1 : 0)) * piece_floats(256, D);
         const bool empty = L == 0.f;
-        const float inv_l = empty ? 0.f : 1.f / L;
+        const float inv_l = empty ? 0.f : (BETA ? kBankUnit : 1.f) / L;
         bool good = true;
         // 8 channels at a time (a loop of a few lines: the instruction cache serves all roles at once).  Lane l has
         // the coefficients of channel l of a group of 32; every row needs all of them
@@ -758,7 +778,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           tmem_ld_wait();
           if (whole) {
             if (BETA && (c & 31) == 0)
-              oc = out_coef(__ldg(a.beta + static_cast<long long>(sg.h) * D + half * kHalfD + c + lane), kind_unpack(shift[c + lane]), wide);
+              oc = out_coef(__ldg(a.beta + static_cast<long long>(sg.h) * D + half * kHalfD + c + lane), kind_unpack(shift[c + lane]),
+                            wide(half * kHalfD + c + lane));
             uint32_t o[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -777,9 +798,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                   bool fine;
                   x[u] = paged_out(kf, av, &fine);
                   good = good && fine;
+                  if (!fine) x[u] = __int_as_float(0x7fffffff);  // the mark, as bf16
                 } else {
-                  x[u] = av;
-                  good = good && fabsf(av) < kMostA;
+                  const bool fine = fabsf(av) < kMostA;
+                  x[u] = fine ? av : __int_as_float(0x7fffffff);
+                  good = good && fine;
                 }
               }
               o[i] = empty ? 0u : pack_bf16(x[0], x[1]);
@@ -810,9 +833,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           }
         }
         if (!whole && t == 0) {
-          if (half == 0 && r < D) piece[256 * D + 512 + r] = kind_unpack(s_shift[(seg % kSegRing) * D + r]);
+          const int cls = BETA && half == 0 && r < D ? wide(r) : 0;
+          const bool any = __any_sync(0xffffffffu, cls != 0);
+          if (half == 0 && r < D) {
+            piece[piece_kinds(256, D) + r] = kind_unpack(s_shift[(seg % kSegRing) * D + r]);
+            piece[piece_classes(256, D) + r] = static_cast<float>(cls);
+          }
+          if (half == 0 && lane == 0) piece[piece_wide(256, D) + (warp & 3)] = any ? 1.f : 0.f;
           if (half == 0 && r == 0) {
-            piece[256 * D + 512 + D] = wide ? 1.f : 0.f;
             if (sg.kt0 == 0) {
               record.n = split_owner(walk.W, walk.G, sg.x_end - 1) - cta + 1;
               record.s = sg.s;

@@ -14,14 +14,15 @@
 // E(v), in bf16 with fp32 sums, a = sum P E / sum P.  Channel j of a sequence
 // and head goes by its first kSampleKeys values v:
 //   tiny     (beta max|v| <= 2^-12)  E = D v,                    o = a / D
-//   linear   (beta max|v| <= 1)      E = expm1(beta v),          o = log1p(a) / beta
+//   linear   (beta max|v| <= 0.7)    E = expm1(beta v),          o = log1p(a) / beta
 //   shifted  (else)                  E = exp(beta (v - c)),      o = c + log(a) / beta,  c about max v
 // Tiny and linear keep small beta free of cancellation: E = v leaves out
 // beta v^2 / 2, at most 2^-9 |v| where it is let through, and expm1 by
 // subtraction is off by 2^-22, 2^-10 of the largest E.  (beta = 0 is tiny.)
 // bf16 has fp32's range, so the shift needs no running update: later values may
-// lie far from the sample's, and a result that could spoil is seen in a or in
-// the largest |E| (paged_out), and its row recomputed exactly.
+// lie far from the sample's (at beta = 20 normal values reach E = 2^80), and a
+// result that could spoil is seen in a and in its channel's largest |E|
+// (paged_out), and its row recomputed exactly.
 #pragma once
 
 #include "fem_paged.cuh"
@@ -29,27 +30,39 @@
 namespace fem {
 
 constexpr int kSampleKeys = 16;
-constexpr float kLinearReach = 1.f;            // beta max|v| up to which a channel is linear: rows that see only the
-                                               // sample then keep 1 + a over e^-1 > kLeastLinear
+constexpr float kLinearReach = 0.7f;           // beta max|v| up to which a channel is linear: there both forms round to
+                                               // 2^-9 / (1/2 beta), the linear one at v = -max|v|, the other at any v
 constexpr float kTinyReach = 0.000244140625f;  // 2^-12: up to which it is tiny
 // What the range of bf16 and fp32 may cost: a term whose weight or bank underflows is lost.  It is
-// at most 2^-126 times the other factor's largest: 2^8 (P) or the largest |E| met.  While that is at
-// most 2^30, the lost terms of 2^20 keys stay under 2^-76, against a >= 2^-66.
+// at most 2^-126 times the other factor's largest: 2^8 (P) or the largest |E| that the channel met.
+// While that is at most 2^30, the lost terms of 2^20 keys stay under 2^-76, against a >= 2^-66; where
+// it is more, the channel's class c (2^30 to 2^(30 + 6 c)) raises the bound on a by as much.  One
+// class for a whole head would send every channel of small beta to the exact path because of one of
+// large beta: reads of 4096 keys at beta 0.05 to 20 took 28 ms in place of 0.37.
 constexpr float kMostShift = 32000.f;  // of a shifted channel's s (beyond it the exact path takes over)
-constexpr float kWideE = 1073741824.f;      // 2^30
+// The bank is held times 2^-29 (of E as written above): 2^30, where class 0 ends, then sets the highest bit of
+// the exponent, which the OR of a channel's E tells, at half the cost of a maximum.
+constexpr int kBankShift = -29;
+constexpr float kBankScale = 1.8626451e-9f;  // 2^-29
+constexpr float kBankUnit = 536870912.f;     // 2^29
+constexpr int kWidest = 15;                 // the class of |E| from 2^114 on, infinities and NaN
+constexpr int kWideLinear = 7;              // a linear channel's last class: lost terms under 2^-34, its a from 2^-12
 constexpr float kLeastA = 1.3552527e-20f;   // 2^-66
 constexpr float kMostA = 1.2980742e33f;     // 2^110
 constexpr float kDeepP = -100.f;            // log2 of a weight below which its term may be lost (the kernel that looks)
-constexpr float kLeastLinear = 0.3125f;     // 1 + a of a linear channel: there a rounding of E (2^-8 of it) is
-                                            // 2^-8 (1 - 1/(1 + a)) / beta in the result, under 2^-7 |v|
+constexpr float kLeastLinear = 0.125f;      // x = 1 + a of a linear channel: there a rounding of E (2^-9, as |E| < 1) is
+                                            // 2^-9 / (beta x) = 2^-9 |v| / (-x log x) in the result, under 2^-7 |v|;
+                                            // and v is three times the sample's largest at least, seldom even in rows of one key
 
-// Scale D of a tiny channel, a power of two: |E| reaches 2^30 where beta |v| reaches 2^-8 (to a factor 2).
+// Scale D of a tiny channel, a power of two: |E| reaches 2^30 where beta |v| reaches 2^-8 (to a factor 2), or, where
+// beta is under 2^-38, |v| 2^30.
 __device__ __forceinline__ float tiny_scale(float beta) {
   // 2^38 times beta without its fraction
-  return beta > 0.f ? __int_as_float(__float_as_int(beta * 274877906944.f) & 0x7f800000) : 1.f;
+  return fmaxf(__int_as_float(__float_as_int(beta * 274877906944.f) & 0x7f800000), 1.f);
 }
 
-// E(v) = 2^(b v + s) + ic + d v: shifted {beta log2 e, -b max v rounded to a whole number, 0, 0}, linear {b, 0, -1, 0}, tiny {0, 0, -1, D}
+// 2^-29 E(v) = 2^(b v + s) + ic + d v, with b = beta log2 e: shifted {b, -b max v rounded to a whole number, less 29, 0, 0},
+// linear {b, -29, -2^-29, 0}, tiny {0, -1000, 0, 2^-29 D}
 struct BankCoef {
   float b, s, ic, d;
 };
@@ -58,21 +71,23 @@ __device__ __forceinline__ BankCoef bank_coef(float beta, float vmax, float vabs
   const float x = beta * (vabs > 0.f ? vabs : 1.f);
   BankCoef c;
   c.b = beta * kLog2e;
-  c.s = 0.f;
-  c.ic = -1.f;
+  c.s = kBankShift;
+  c.ic = -kBankScale;
   c.d = 0.f;
   if (x <= kTinyReach) {
     c.b = 0.f;
-    c.d = tiny_scale(beta);
+    c.s = -1000.f;
+    c.ic = 0.f;
+    c.d = tiny_scale(beta) * kBankScale;
   } else if (!(x <= kLinearReach)) {
-    c.s = fminf(fmaxf(-rintf(c.b * vmax), -kMostShift), kMostShift);
+    c.s = fminf(fmaxf(-rintf(c.b * vmax), -kMostShift), kMostShift) + kBankShift;
     c.ic = 0.f;
   }
   return c;
 }
-// The channel's kind, and a shifted one's s (a whole number), in one float: NaN linear, infinity tiny.
+// The channel's kind, and a shifted one's s (a whole number, of E), in one float: NaN linear, infinity tiny.
 __device__ __forceinline__ float bank_kind(const BankCoef &c) {
-  return c.ic == 0.f ? c.s : c.d != 0.f ? INFINITY : __int_as_float(0x7fffffff);
+  return c.d != 0.f ? INFINITY : c.ic == 0.f ? c.s - kBankShift : __int_as_float(0x7fffffff);
 }
 
 // The same in 16 bits.
@@ -83,7 +98,12 @@ __device__ __forceinline__ float kind_unpack(short k) {
   return k == 32766 ? INFINITY : k == 32767 ? __int_as_float(0x7fffffff) : static_cast<float>(k);
 }
 
-// E of two values; coefficients of both
+// The class of a largest |E| by the exponent field of what is held.
+__device__ __forceinline__ int wide_class(int field) {
+  return field < 128 ? 0 : min(kWidest, 1 + (field - 128) / 6);
+}
+
+// 2^-29 E of two values; coefficients of both
 __device__ __forceinline__ float2 bank_pair(const float2 b, const float2 s, const float2 ic, const float2 d, const float2 v) {
   const float2 x = __ffma2_rn(b, v, s);
   return __ffma2_rn(d, v, __fadd2_rn(make_float2(ex2_approx(x.x), ex2_approx(x.y)), ic));
@@ -97,15 +117,17 @@ __device__ __forceinline__ float2 bank_pair(const float2 b, const float2 s, cons
 struct OutCoef {
   float g, z, y, w, lo;
 };
-__device__ __forceinline__ OutCoef out_coef(float beta, float kind, bool wide) {
+__device__ __forceinline__ OutCoef out_coef(float beta, float kind, int wide) {
   const float ib = rcp_approx(beta * kLog2e);
   OutCoef c;
   const bool tiny = kind == INFINITY, linear = kind != kind;
   c.g = linear ? 1.f : 0.f;
   c.z = tiny ? 0.f : ib;
   c.y = tiny || linear ? 0.f : -kind * ib;
-  c.w = tiny ? (beta > 0.f ? 1.f / tiny_scale(beta) : 1.f) : linear ? ib * kLog2e : 0.f;
-  c.lo = tiny ? (wide ? INFINITY : -kMostA) : linear ? (wide ? INFINITY : kLeastLinear) : (wide ? kWideE : kLeastA);
+  c.w = tiny ? 1.f / tiny_scale(beta) : linear ? ib * kLog2e : 0.f;
+  // a tiny channel's |E| over 2^30 says that it is none
+  const float least = kLeastA * __int_as_float((127 + 6 * wide) << 23);
+  c.lo = tiny ? (wide ? INFINITY : -kMostA) : linear ? (wide > kWideLinear ? INFINITY : kLeastLinear) : (wide == kWidest ? INFINITY : least);
   return c;
 }
 __device__ __forceinline__ float paged_out(const OutCoef &c, float a, bool *ok) {
@@ -340,16 +362,20 @@ __device__ bool split_begin(const PagedReadArgs &a, const SplitShape &shape, int
 // end.  A piece: the rows' accumulators [rows][D] (not normalised), in groups of
 // 8 rows with 4 channels of the 8 side by side (128 bytes), so that a warp whose
 // lanes are rows and one whose lanes are channels both write full lines; then
-// per row {m, L} (log2 units), then the channels' kinds [D], then whether |E|
-// went wide.
+// per row {m, L} (log2 units), then the channels' kinds [D] and classes of |E|
+// [D], then four numbers whose sum is 0 where every class is.
 // ---------------------------------------------------------------------------
 // Channels 4 c4 .. of row `row`, in floats.
 __host__ __device__ constexpr size_t piece_at(int row, int c4, int D) {
   return (static_cast<size_t>(row >> 3) * (D / 4) + c4) * 32 + (row & 7) * 4;
 }
 __host__ __device__ constexpr size_t piece_floats(int rows, int D) {
-  return static_cast<size_t>(rows) * D + 2 * rows + D + 4;
+  return (static_cast<size_t>(rows) * D + 2 * rows + 2 * D + 4 + 31) / 32 * 32;  // full lines
 }
+// Where the kinds, the classes and the four numbers begin.
+__host__ __device__ constexpr int piece_kinds(int rows, int D) { return rows * D + 2 * rows; }
+__host__ __device__ constexpr int piece_classes(int rows, int D) { return rows * D + 2 * rows + D; }
+__host__ __device__ constexpr int piece_wide(int rows, int D) { return rows * D + 2 * rows + 2 * D; }
 
 // What a CTA leaves to the kernel that follows: the item it begins and does not end (n pieces, of
 // this CTA and the n - 1 after it; none: 0), and whether rows that it finished need the exact path.

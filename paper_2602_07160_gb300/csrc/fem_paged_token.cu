@@ -49,8 +49,8 @@ struct TokLayout {
   static constexpr int kCoef4 = (kBar + kTokWarps * kStages * 8 + 15) & ~15;
   static constexpr int kShift = kCoef4 + D * 16;
   static constexpr int kStat = kShift + D * 4;  // [warps][rows] {m, L}
-  static constexpr int kWideFlag = kStat + kTokWarps * kRows * 8;
-  static constexpr int kRowBad = kWideFlag + 4;  // per row: some channel needs the exact path
+  static constexpr int kEmax = kStat + kTokWarps * kRows * 8;  // per channel: largest |E| as held (its bits) where wide, or 0
+  static constexpr int kRowBad = kEmax + D * 4;  // per row: some channel needs the exact path
   static constexpr int kBytes = kRowBad + kRows * 4;
   static constexpr int kAlloc = kBytes + 1024;
 };
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
   float *s_coef = reinterpret_cast<float *>(smem + Lay::kCoef4);
   float *s_shift = reinterpret_cast<float *>(smem + Lay::kShift);
   float2 *s_stat = reinterpret_cast<float2 *>(smem + Lay::kStat);
-  int *s_wide = reinterpret_cast<int *>(smem + Lay::kWideFlag);
+  int *s_emax = reinterpret_cast<int *>(smem + Lay::kEmax);
   int *s_bad = reinterpret_cast<int *>(smem + Lay::kRowBad);
 
   grid_dep_launch_dependents();
@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
     for (int j = 0; alive && j < min(n_st, NS); ++j) issue(j);
 
     // ---- the bank's coefficients, from the sequence's first keys (thread per channel)
-    if (tid == 0) *s_wide = 0;
+    if (tid < D) s_emax[tid] = 0;
     if (tid < kRows) s_bad[tid] = 0;
     if (BETA) {
       if (tid < D) {
@@ -302,7 +302,7 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
         if (r < total) lim_min = min(lim_min, lim[t][u]);
       }
     lim_min = __reduce_min_sync(0xffffffffu, lim_min);
-    float m[NT][2], L[NT][2], acc[NT][MT][4], emax = 0.f;
+    float m[NT][2], L[NT][2], acc[NT][MT][4];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       m[t][0] = m[t][1] = -INFINITY;
@@ -510,14 +510,17 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
               const int at = Lay::kElem == 2 || !R128 ? (ch & ~63) + (ch & 7) * 8 + ((ch >> 3) & 7) : (ch & 15) * 8 + (ch >> 4);
               const float *cp = s_coef + (at & ~8) * 4 + ((at >> 3) & 1);
               const BankCoef c = {cp[0], cp[2], cp[32], cp[34]};
-#pragma unroll 1
-              for (int kk = 0; kk < kTokKeys && key0 + kk < sg.si.ctx; ++kk) {
+              float emax = 0.f;
+#pragma unroll 4
+              for (int kx = 0; kx < kTokKeys; ++kx) {
+                const int kk = min(kx, sg.si.ctx - 1 - key0);
                 const uint8_t *p = smem + (vt - sbase) + tok_offset<Lay::kBox>(kk, ch * Lay::kElem >> 4) + (ch * Lay::kElem & 15);
                 const float v = FORMAT == kCacheBf16
                                     ? __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(p))
                                     : e4m3x2_to_float2(*p).x * paged_scale(smem[scales - sbase + st * 32 + 16 + kk]);
                 emax = fmaxf(emax, fabsf(fmaf(c.d, v, ex2_approx(fmaf(c.b, v, c.s)) + c.ic)));
               }
+              if (emax >= 2.f) atomicMax(s_emax + ch, __float_as_int(emax));
             }
           }
         }
@@ -536,7 +539,6 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
         for (int o = 4; o < 32; o <<= 1) L[t][u] += __shfl_xor_sync(0xffffffffu, L[t][u], o);
         if (g == 0) s_stat[warp * kRows + 8 * t + 2 * i4 + u] = make_float2(m[t][u], L[t][u]);
       }
-    if (BETA && __any_sync(0xffffffffu, emax > kWideE) && lane == 0) *s_wide = 1;
     {
       float *own = reinterpret_cast<float *>(smem + warp * NS * Lay::kStage);
 #pragma unroll
@@ -557,7 +559,7 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
     const bool whole = sg.kt0 == 0 && sg.kt1 == sg.kt_all;
     const int slot = cta * 2 + (sg.kt0 == 0 ? 1 : 0);
     float *piece = sp.pieces + static_cast<size_t>(slot) * piece_floats(kRows, D);
-    const bool wide = *s_wide != 0;
+    const int wide = tid < D ? wide_class(s_emax[tid] >> 23) : 0;
     const OutCoef oc = out_coef(beta_c, tid < D ? s_shift[tid] : INFINITY, wide);
     for (int r = 0; r < n_rows; ++r) {
       float M = -INFINITY, Lr = 0.f, av = 0.f;
@@ -579,9 +581,12 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
           bool ok = true;
           float o = 0.f;
           if (!(M == -INFINITY && Lr == 0.f)) {
-            o = paged_out(oc, av / Lr, &ok);
+            o = paged_out(oc, av * ((BETA ? kBankUnit : 1.f) / Lr), &ok);
           }
-          if (!ok) s_bad[r] = 1;
+          if (!ok) {
+            s_bad[r] = 1;
+            o = __int_as_float(0x7fffffff);  // the mark, as bf16
+          }
           static_cast<__nv_bfloat16 *>(a.out)[orow * D + tid] = __float2bfloat16_rn(o);
         }
         if (tid == 0 && a.lse != nullptr)
@@ -595,8 +600,12 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
       }
     }
     if (!whole) {
-      if (tid < D) piece[kRows * D + 2 * kRows + tid] = s_shift[tid];
-      if (tid == 0) piece[kRows * D + 2 * kRows + D] = wide ? 1.f : 0.f;
+      if (tid < D) {
+        piece[piece_kinds(kRows, D) + tid] = s_shift[tid];
+        piece[piece_classes(kRows, D) + tid] = static_cast<float>(wide);
+      }
+      const bool any = __any_sync(0xffffffffu, wide != 0);
+      if (lane == 0) piece[piece_wide(kRows, D) + warp] = any ? 1.f : 0.f;
     }
     fence_proxy_async_smem();  // the rings go back to the copies
     __syncthreads();

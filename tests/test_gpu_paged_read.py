@@ -377,3 +377,30 @@ def test_matches_the_contiguous_reads():
     dec, dec_lse = fem.fem_decode(as_bhtd[0][:, :, -1].contiguous(), as_bhtd[1], as_bhtd[2], beta)
     assert (tok[0].float() - dec[0]).abs().max() <= 2e-2
     assert (tok_lse[0] - dec_lse[0]).abs().max() <= 1e-4
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("lens", ["tokens", "chunks"])
+@pytest.mark.parametrize("q_scale", [1.0, 6.0])
+@pytest.mark.parametrize("d", [64, 128])
+def test_read_with_small_and_large_beta_in_one_head(fmt, lens, q_scale, d):
+    """beta 1e-4 to 20 side by side: the largest |E| of one channel decides nothing about another's."""
+    lens = LENS[lens]
+    q, cache, off, ctx, table = make(fmt, 2, 8, d, 32, lens, seed=17, q_scale=q_scale)
+    check(q, cache, make_beta((1e-4, 20.0), 2, d, seed=3), off, ctx, table, causal=True, max_q=max(n for n, _ in lens),
+          rms=False)
+
+
+@pytest.mark.parametrize("beta", [0.3, 5.0])
+@pytest.mark.parametrize("n", [1, 40])
+def test_a_few_channels_of_a_row_again(n, beta):
+    """Values whose first ones mislead in a few channels: those alone are recomputed."""
+    q, cache, off, ctx, table = make("bf16", 1, 4, 128, 64, [(n, 1500)], seed=23, poison=False)
+    order = table[0, :24].long()
+    v = cache.v[order]  # [pages, 1, 64, 128]: positions in order
+    v[0, 0, :16, 3:9] = 0.01 * v[0, 0, :16, 3:9]
+    v[2:, 0, :, 5] -= 40.0
+    v[2:, 0, :, 7] += 40.0
+    cache.v[order] = v
+    b = torch.full((1, 128), beta, device=DEV)
+    check(q, cache, b, off, ctx, table, causal=True, max_q=n, rms=False)
