@@ -431,9 +431,9 @@ def fem_cache_gather(cache: PagedCache, block_table, starts, offsets, total: int
         raise ValueError("block_table must be [S, max_pages]")
     (S, max_pages), shape, index = block_table.shape, (total, cache.H, cache.d), cache.index
     if k_out is None:
-        k_out = cache.k.new_empty(shape, dtype=cache.row_dtype)
+        k_out = torch.empty(shape, dtype=cache.row_dtype, device=cache.device)
     if v_out is None:
-        v_out = cache.k.new_empty(shape, dtype=cache.row_dtype)
+        v_out = torch.empty(shape, dtype=cache.row_dtype, device=cache.device)
     rc = load().fem_cache_gather(cache._ref, _check_whole("block_table", block_table, (S, max_pages), torch.int32, index),
                                  max_pages, _check_whole("starts", starts, (S,), torch.int32, index),
                                  _check_whole("offsets", offsets, (S + 1,), torch.int32, index), S,
@@ -463,12 +463,12 @@ def fem_paged_read(q, cache: PagedCache, beta, q_offsets, ctx_lens, block_table,
     (S, max_pages), index = block_table.shape, cache.index
     out_ptr = lse_ptr = beta_ptr = None
     if out is None:
-        out = q.new_empty((N, Hq, d))
+        out = torch.empty((N, Hq, d), dtype=cache.row_dtype, device=cache.device)
         out_ptr = out.data_ptr()
     else:
         out_ptr = _check_whole("out", out, (N, Hq, d), q.dtype, index)
     if lse is None:
-        lse = q.new_empty((N, Hq), dtype=torch.float32)
+        lse = torch.empty((N, Hq), dtype=torch.float32, device=cache.device)
         lse_ptr = lse.data_ptr()
     elif lse is not False:
         lse_ptr = _check_whole("lse", lse, (N, Hq), torch.float32, index)
