@@ -830,13 +830,20 @@ int fem_cache_gather(const fem_paged_cache *cache, const int *block_table, int m
                                       static_cast<cudaStream_t>(stream)));
 }
 
-// Query rows per key/value head up to which the paged read takes the kernel of few rows.
+// Query rows per key/value head up to which the paged read takes the kernel of few rows.  64 sequences of 4096
+// keys, 8 heads of 128, us with it and with the kernel of many rows: bf16 172 and 292 at 8 rows, 195 and 293 at 16,
+// 353 and 299 at 24, 692 and 287 at 64; e4m3 152 and 366 at 8, 239 and 366 at 16.  8 sequences of 512, bf16: 17.2 and
+// 29.5 at 8, 21.5 and 29.6 at 16, 24.6 and 29.8 at 24, 34.4 and 30.4 at 48.
 static constexpr int kTokenRows = 16;
-// What an item costs the kernel of many rows beside its key tiles (queries, a maximum, output), in key tiles.
+// What an item costs beside its key tiles, in key tiles, when the line of work is split (queries, a maximum, output).
+// Many rows, at 0, 3, 5, 7, 10, 14: a causal prompt of 8192 366, 324, 295, 272, 283, 293 us, six ragged chunks over
+// e4m3 116, 93, 96, 98, 98, 101 us.  Few rows, at 0, 2, 4, 8: up to five drafted tokens of nine sequences 22.3, 17.7,
+// 17.9, 18.1 us, a token of each of 48 over e4m3 139.9, 137.3, 134.9, 140.5 us.
 static constexpr int kChunkFixed = 7;
 static constexpr int kTokenFixed = 4;
+// Items of up to so many key tiles are not cut by the kernel of many rows: 40 to 80 tokens of 32 sequences over 197
+// keys 27.9 us with every item cut where a stretch ends, 27.1 at 4, 8 and 16; the prompt 272 us up to 8, 303 at 16.
 static constexpr int kChunkWhole = 8;
-static constexpr int kTokenWhole = 0;
 
 int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride_n, int64_t q_stride_h,
                    const float *beta, const int *q_offsets, const int *ctx_lens, const int *block_table,
@@ -877,7 +884,7 @@ int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride
   a.err = ds->err;
   const bool split = (a.c.d == 64 || a.c.d == 128) && a.c.format != FEM_CACHE_F32 &&
                      static_cast<long long>(a.c.num_pages) * a.c.H < (1ll << 31);
-  if (!split) return map_cuda(launch_paged_exact(a, s));
+  if (!split) return map_cuda(launch_paged_exact(a, ds->num_sms, s));
   const int rows = static_cast<int>(std::min<long long>(static_cast<long long>(max_q) * a.group, 1 << 30));
   // few rows per head: the kernel that is bound by memory; more: the tensor cores
   const bool chunk = rows > kTokenRows && a.group <= 256;
@@ -886,7 +893,7 @@ int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride
   // then short: fem_paged_split.cuh)
   const int tok = 256 / a.group;
   const SplitShape shape = chunk ? SplitShape{256, 7, tok >= 8 ? tok & ~7 : tok, 1, kChunkFixed, kChunkWhole}
-                                 : SplitShape{rows <= 8 ? 8 : 16, 6, 0, 2, kTokenFixed, kTokenWhole};
+                                 : SplitShape{rows <= 8 ? 8 : 16, 6, 0, 2, kTokenFixed, 0};
   const int box_rows = chunk ? std::min(1 << a.c.page_shift, 128) : 16;
   CUtensorMap tk, tv;
   if ((rc = cache_map(&tk, a.c.k, a.c, box_rows)) != FEM_OK || (rc = cache_map(&tv, a.c.v, a.c, box_rows)) != FEM_OK)

@@ -166,7 +166,7 @@ cudaError_t launch_cache_write(const PagedCacheView &c, const void *k, const voi
 cudaError_t launch_cache_gather(const PagedCacheView &c, const int *table, int max_pages, const int *starts,
                                 const int *offsets, int S, int total, void *k, void *v, unsigned *err,
                                 cudaStream_t stream);
-cudaError_t launch_paged_exact(const PagedReadArgs &a, cudaStream_t stream);
+cudaError_t launch_paged_exact(const PagedReadArgs &a, int num_sms, cudaStream_t stream);
 // The read of few rows per sequence on `grid` CTAs that split the work evenly (fem_paged_split.cuh), for d = 64
 // and 128; tk, tv map the cache's k and v as [num_pages H, page_size, d] in boxes of 16 rows.  launch_paged_finish
 // follows on the same stream and joins what the CTAs' ends cut (a programmatic dependent launch).
