@@ -347,9 +347,14 @@ int fem_cache_gather(const fem_paged_cache *cache, const int *block_table, int m
  *               split over the GPU; n above it is still read correctly)
  *   out       : device, [N, Hq, d], contiguous, q's type (bf16 or float32)
  *   lse       : device, float32 [N, Hq], or NULL
- * Rows that no sequence owns are not written.  N = 0 does nothing.  Accuracy:
- * scores, softmax statistics and sums in fp32; FEM_CACHE_F32 and head dimensions
- * other than 64 and 128 are exact to fp32 rounding.
+ * Rows that no sequence owns are not written.  N = 0 does nothing.  Hq up to
+ * 65535 and N Hq below 2^31 (else FEM_ERR_UNSUPPORTED).  Accuracy: scores, softmax
+ * statistics and sums in fp32; FEM_CACHE_F32 and head dimensions other than 64 and
+ * 128 are exact to fp32 rounding, on CUDA cores.  The others run on the tensor
+ * cores with the softmax weights and exp(beta_j v) rounded to bf16 (each at most
+ * 2^-8 of a term), and recompute in fp32 the channels whose result the range of
+ * those could have spoilt.  The same inputs give the same bits.  The workspace
+ * comes from the library's stream-ordered pool.
  */
 int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride_n, int64_t q_stride_h,
                    const float *beta, const int *q_offsets, const int *ctx_lens, const int *block_table,
