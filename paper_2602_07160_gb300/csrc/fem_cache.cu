@@ -1,9 +1,10 @@
 // Writing a paged cache and reading it back (layout and format in fem_paged.cuh).
 //
 // Both are bound by memory: every element is read once and written once, and
-// the quantisation's arithmetic is kept under the copies.  The rows are short (d elements of one token and
-// head), so a group of G lanes takes a row with 16-byte accesses, and the
-// row's largest magnitude (the e4m3 scale) is a butterfly over the group.
+// the quantisation's arithmetic is kept under the copies.  The rows are short (d
+// elements of one token and head), so a group of G lanes takes a row with 16-byte
+// accesses, and the row's largest magnitude (the e4m3 scale) is a butterfly over
+// the group.
 #include <cuda_fp8.h>
 
 #include "fem_launch.h"
@@ -31,16 +32,19 @@ __device__ __forceinline__ int scale_exponent(float amax) {
   return min(max(e, kScaleExpMin), kScaleExpMax);
 }
 
-// G lanes per row, 16 bytes per lane.  A group takes kWriteUnroll rows of one token (of its keys' heads, then its
-// values'), whose loads leave together.  8192 tokens of 16 heads of 128 into e4m3 take 21.1 us, 4.8 TB/s (one row
-// at a time 3.0 TB/s, 2 rows 22.3 us, 8 rows 23.8 us).  With a comparison and a clamp per element, where words of
-// two elements do and no clamp is needed, the integer pipe was busy for 73 % of 24.0 us.
-constexpr int kWriteUnroll = 4;
+// G lanes per row.  A group takes write_rows rows of one token (of its keys' heads, then its values'), whose loads, 64
+// bytes a lane, leave together.  8192 tokens of 16 heads of 128 into e4m3 take 19.3 us, 5.2 TB/s (4 rows 20.5 us, one
+// 20.6, 8 24.4; half the elements to a lane 21.1).  With a comparison and a clamp per element, where words of two
+// elements do and no clamp is needed, the integer pipe was busy for 73 % of 24.0 us.
+__host__ __device__ constexpr int write_rows(int format) { return format == kCacheE4m3 ? 2 : 4; }
 
 template <int G, int FORMAT>
 __global__ void __launch_bounds__(256) cache_write_kernel(const CacheWrite a) {
-  constexpr int E = FORMAT == kCacheF32 ? 4 : 8, kIn = FORMAT == kCacheF32 ? 4 : 2;  // elements per lane, bytes of one
-  constexpr int kPieces = FORMAT == kCacheF32 ? 2 : 1;  // of a lane: fp32 rows of up to 256 in two
+  // elements per lane and step, bytes of one
+  constexpr int E = FORMAT == kCacheF32 ? 4 : FORMAT == kCacheBf16 ? 8 : 16, kIn = FORMAT == kCacheF32 ? 4 : 2;
+  // 16-byte pieces of a lane, and the elements between them: fp32 rows of up to 256 take two steps; 16 elements side by
+  // side become 16 bytes of codes
+  constexpr int kRows = write_rows(FORMAT), kPieces = FORMAT == kCacheBf16 ? 1 : 2, kStep = FORMAT == kCacheE4m3 ? 8 : G * E;
   const int lane = threadIdx.x % G, n = blockIdx.x * (256 / G) + threadIdx.x / G, j = lane * E;
   const int H = a.c.H, d = a.c.d, page_mask = (1 << a.c.page_shift) - 1;
   const long long n_slots = static_cast<long long>(a.c.num_pages) << a.c.page_shift;
@@ -49,32 +53,35 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const CacheWrite a) {
   if (slot >= n_slots && lane == 0) atomicOr(a.err, kErrPageRange);
   const bool on = slot >= 0 && slot < n_slots;
   const int page = on ? static_cast<int>(slot >> a.c.page_shift) : 0, inside = static_cast<int>(slot & page_mask);
-  uint4 x[kWriteUnroll][kPieces];
+  uint4 x[kRows][kPieces];
 #pragma unroll
-  for (int u = 0; u < kWriteUnroll; ++u) {
-    const int row = blockIdx.y * kWriteUnroll + u, h = row < H ? row : row - H;
+  for (int u = 0; u < kRows; ++u) {
+    const int row = blockIdx.y * kRows + u, h = row < H ? row : row - H;
     const long long src = row < H ? n * a.k_sn + h * a.k_sh : n * a.v_sn + h * a.v_sh;
     const uint8_t *p = static_cast<const uint8_t *>(row < H ? a.k : a.v) + (src + j) * kIn;
 #pragma unroll
     for (int q = 0; q < kPieces; ++q)
-      x[u][q] = on && row < 2 * H && j + q * G * E < d ? __ldcs(reinterpret_cast<const uint4 *>(p + q * G * E * kIn))
+      x[u][q] = on && row < 2 * H && j + q * kStep < d ? __ldcs(reinterpret_cast<const uint4 *>(p + q * kStep * kIn))
                                                       : make_uint4(0, 0, 0, 0);
   }
 #pragma unroll
-  for (int u = 0; u < kWriteUnroll; ++u) {
-    const int row = blockIdx.y * kWriteUnroll + u, h = row < H ? row : row - H;
+  for (int u = 0; u < kRows; ++u) {
+    const int row = blockIdx.y * kRows + u, h = row < H ? row : row - H;
     const bool put = on && row < 2 * H && j < d;
     const long long at = paged_row(a.c, page, row < 2 * H ? h : 0, inside);
     if (FORMAT != kCacheE4m3) {
       uint8_t *dst = static_cast<uint8_t *>(row < H ? a.c.k : a.c.v) + (at * d + j) * kIn;
 #pragma unroll
       for (int q = 0; q < kPieces; ++q)
-        if (put && j + q * G * E < d) *reinterpret_cast<uint4 *>(dst + q * G * E * kIn) = x[u][q];
+        if (put && j + q * kStep < d) *reinterpret_cast<uint4 *>(dst + q * kStep * kIn) = x[u][q];
     } else {
-      const uint32_t w[4] = {x[u][0].x, x[u][0].y, x[u][0].z, x[u][0].w};
+      const uint4 y = x[u][0], z = x[u][kPieces - 1];
+      const uint32_t w[8] = {y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
       // magnitudes of bf16 order as their bits, two to a word; infinities and NaN come last
       constexpr uint32_t kMag = 0x7fff7fffu;
-      uint32_t top = __vmaxu2(__vmaxu2(w[0] & kMag, w[1] & kMag), __vmaxu2(w[2] & kMag, w[3] & kMag));
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) top = __vimax3_u16x2(top, w[i] & kMag, w[i + 1] & kMag);
 #pragma unroll
       for (int o = G / 2; o > 0; o >>= 1) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
       top = max(top & 0xffffu, top >> 16);
@@ -82,9 +89,9 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const CacheWrite a) {
       const int e = scale_exponent(__int_as_float(static_cast<int>(top << 16)));
       // 2^-e is a normal number for e in [-100, 120]; the products are exact, and none is over 448
       const float inv = __int_as_float((127 - e) << 23);
-      uint32_t code[2];
+      uint32_t code[4];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < 4; ++i) {
         uint32_t c[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -96,10 +103,11 @@ __global__ void __launch_bounds__(256) cache_write_kernel(const CacheWrite a) {
       }
       if (e == kScaleExpMax) {  // 256 2^120 would read back as an infinity: codes stop at 240
 #pragma unroll
-        for (int i = 0; i < 2; ++i) code[i] = __vminu4(code[i] & 0x7f7f7f7fu, 0x77777777u) | (code[i] & 0x80808080u);
+        for (int i = 0; i < 4; ++i) code[i] = __vminu4(code[i] & 0x7f7f7f7fu, 0x77777777u) | (code[i] & 0x80808080u);
       }
       if (put) {
-        *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(row < H ? a.c.k : a.c.v) + at * d + j) = make_uint2(code[0], code[1]);
+        *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(row < H ? a.c.k : a.c.v) + at * d + j) =
+            make_uint4(code[0], code[1], code[2], code[3]);
         if (lane == 0) (row < H ? a.c.ke : a.c.ve)[at] = static_cast<uint8_t>(bad ? kScaleNan : e + kScaleBias);
       }
     }
@@ -195,16 +203,16 @@ __global__ void __launch_bounds__(256) cache_gather_kernel(const CacheGather a) 
 
 template <int FORMAT>
 cudaError_t launch_write_f(const CacheWrite &a, cudaStream_t s) {
-  const int per = a.c.d / (FORMAT == kCacheF32 ? 4 : 8);
+  const int per = a.c.d / (FORMAT == kCacheF32 ? 4 : FORMAT == kCacheBf16 ? 8 : 16);
   int G = 2;
   while (G < per && G < 32) G *= 2;
-  const dim3 grid((a.N + 256 / G - 1) / (256 / G), (2 * a.c.H + kWriteUnroll - 1) / kWriteUnroll);
+  const dim3 grid((a.N + 256 / G - 1) / (256 / G), (2 * a.c.H + write_rows(FORMAT) - 1) / write_rows(FORMAT));
   switch (G) {
     case 2: cache_write_kernel<2, FORMAT><<<grid, 256, 0, s>>>(a); break;
     case 4: cache_write_kernel<4, FORMAT><<<grid, 256, 0, s>>>(a); break;
     case 8: cache_write_kernel<8, FORMAT><<<grid, 256, 0, s>>>(a); break;
     case 16: cache_write_kernel<16, FORMAT><<<grid, 256, 0, s>>>(a); break;
-    default: cache_write_kernel<32, FORMAT><<<grid, 256, 0, s>>>(a); break;
+    default: cache_write_kernel<FORMAT == kCacheE4m3 ? 16 : 32, FORMAT><<<grid, 256, 0, s>>>(a); break;  // e4m3: 16 at most
   }
   return cudaGetLastError();
 }
