@@ -353,8 +353,10 @@ int fem_cache_gather(const fem_paged_cache *cache, const int *block_table, int m
  * 128 are exact to fp32 rounding, on CUDA cores.  The others run on the tensor
  * cores with the softmax weights and exp(beta_j v) rounded to bf16 (each at most
  * 2^-8 of a term), and recompute in fp32 the channels whose result the range of
- * those could have spoilt.  The same inputs give the same bits.  The workspace
- * comes from the library's stream-ordered pool.
+ * those could have spoilt: a channel whose beta_j v rises by more than about 75
+ * over that of the sequence's first 16 positions costs what it costs in
+ * FEM_CACHE_F32, a hundred times as much.  The same inputs give the same bits.
+ * The workspace comes from the library's stream-ordered pool.
  */
 int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride_n, int64_t q_stride_h,
                    const float *beta, const int *q_offsets, const int *ctx_lens, const int *block_table,
