@@ -104,9 +104,11 @@ __device__ __forceinline__ int wide_class(int field) {
 }
 
 // 2^-29 E of two values; coefficients of both
-__device__ __forceinline__ float2 bank_pair(const float2 b, const float2 s, const float2 ic, const float2 d, const float2 v) {
+__device__ __forceinline__ float2 bank_pair(const float2 b, const float2 s, const float2 ic, const float2 d, const float2 v,
+                                            bool tiny = true) {
   const float2 x = __ffma2_rn(b, v, s);
-  return __ffma2_rn(d, v, __fadd2_rn(make_float2(ex2_approx(x.x), ex2_approx(x.y)), ic));
+  const float2 e = __fadd2_rn(make_float2(ex2_approx(x.x), ex2_approx(x.y)), ic);
+  return tiny ? __ffma2_rn(d, v, e) : e;
 }
 
 // The read from a, o = |a| g < 2^-6 and w != 0 ? a w (1 - g (a/2 - a^2/3)) : lg2(a + g) z + y:

@@ -17,8 +17,10 @@
 // the time the bytes do (tensor pipe 9 to 10 % busy).
 // One token over 131071 keys, 8 heads of 128 for 32 query heads, bf16: 100 us with
 // the join, 5.4 TB/s of the 6.8 that a copy reaches.  48 tokens over 2048 to 8192
-// keys each in e4m3: 137 us, 3.7 TB/s: the bytes are half and the bank the same, and
+// keys each in e4m3: 131 us, 3.8 TB/s: the bytes are half and the bank the same, and
 // the eleven warps of an SM that its registers leave issue in 55 % of the cycles.
+#include <type_traits>
+
 #include "fem_launch.h"
 #include "fem_paged.cuh"
 #include "fem_paged_split.cuh"
@@ -315,7 +317,8 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
     }
     const float qk_scale = a.scale * kLog2e;
     // the coefficients are there
-    const bool tiny = __syncthreads_or(BETA && tid < D && beta_c > 0.f && s_shift[tid] == INFINITY) != 0;
+    const bool any_dv = __syncthreads_or(BETA && tid < D && s_shift[tid] == INFINITY) != 0;  // tiny channels, beta = 0 among them
+    const bool tiny = any_dv && __syncthreads_or(beta_c > 0.f && s_shift[min(tid, D - 1)] == INFINITY) != 0;
 
     for (int j = 0; j < n_st; ++j) {
       const int st = j % NS, key0 = ((sg.kt0 + j) * kTokWarps + warp) * kTokKeys;
@@ -326,9 +329,11 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
         if (alive) {
           const uint32_t kt = ring + st * Lay::kStage, vt = kt + Lay::kStage / 2;
           // ---- S^T = K Q^T
-          float sc[NT][4];
+          float sc[NT][4], s2[NT][4];  // two sums, so that every other product need not wait for the one before
 #pragma unroll
-          for (int t = 0; t < NT; ++t) sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc[t][i] = s2[t][i] = 0.f;
           const int r0 = key_of<R128>(g), r1 = key_of<R128>(g + 8);
           uint32_t ksc0 = 0, ksc1 = 0;
           if (FORMAT == kCacheBf16) {
@@ -339,7 +344,7 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
 #pragma unroll
               for (int t = 0; t < NT; ++t) {
                 mma_bf16(sc[t], x.x, y.x, x.y, y.y, qf[t][2 * p][0], qf[t][2 * p][1]);
-                mma_bf16(sc[t], x.z, y.z, x.w, y.w, qf[t][2 * p + 1][0], qf[t][2 * p + 1][1]);
+                mma_bf16(s2[t], x.z, y.z, x.w, y.w, qf[t][2 * p + 1][0], qf[t][2 * p + 1][1]);
               }
             }
           } else {
@@ -355,10 +360,14 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
               for (int u = 0; u < 4; ++u) {
                 const uint2 xa = e4m3x4_to_f16(xs[u]), ya = e4m3x4_to_f16(ys[u]);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) mma_f16(sc[t], xa.x, ya.x, xa.y, ya.y, qf[t][4 * p + u][0], qf[t][4 * p + u][1]);
+                for (int t = 0; t < NT; ++t) mma_f16(u & 1 ? s2[t] : sc[t], xa.x, ya.x, xa.y, ya.y, qf[t][4 * p + u][0], qf[t][4 * p + u][1]);
               }
             }
           }
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc[t][i] += s2[t][i];
           const float f0 = FORMAT == kCacheE4m3 ? qk_scale * paged_scale(ksc0) : qk_scale;
           const float f1 = FORMAT == kCacheE4m3 ? qk_scale * paged_scale(ksc1) : qk_scale;
           const bool tail = key0 + kTokKeys > lim_min;
@@ -439,71 +448,78 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
           }
           constexpr int kPieces = FORMAT == kCacheBf16 ? Lay::kBoxes : 1;  // of a lane, per key
           constexpr int kPer = MT * 2 / kPieces;                           // channels of a piece (8 or 16)
+          // Without a tiny channel the bank has no term d v: 136 us to 132 for 48 sequences over e4m3.  Over bf16, bound
+          // by memory, one copy of the code is 2 % faster than two.
+          auto mix = [&](auto tiny_head) {
+            constexpr bool kTiny = decltype(tiny_head)::value;
 #pragma unroll
-          for (int pc = 0; pc < kPieces; ++pc) {
-            uint32_t w[4][4];
-            uint2 vh[4];
-            if (R128) {
-              const int chunk = 8 * pc + (g >> 1) + 4 * (g & 1);
-#pragma unroll
-              for (int u = 0; u < 4; ++u) {
-                const uint4 x = lds128(vt + tok_offset<Lay::kBox>(vr[u], chunk));
-                w[u][0] = x.x;
-                w[u][1] = x.y;
-                w[u][2] = x.z;
-                w[u][3] = x.w;
-              }
-            } else {
-#pragma unroll
-              for (int u = 0; u < 4; ++u) {
-                const uint2 x = lds64(vt + tok_offset<Lay::kBox>(vr[u], g >> 1) + 8 * (g & 1));
-                w[u][0] = x.x;
-                w[u][1] = x.y;
-              }
-            }
-            const int lane_g = R128 ? (g >> 1) + 4 * (g & 1) : g;  // the piece's place among the coefficients
-#pragma unroll
-            for (int q = 0; q < kPer / 2; ++q) {  // pairs of channels: one row block of the product each
-              uint32_t a0, a1, a2, a3;
-              float lo[4], hi[4];
-              if (FORMAT == kCacheE4m3 && !(q & 1)) {
-#pragma unroll
-                for (int u = 0; u < 4; ++u) vh[u] = e4m3x4_to_f16(w[u][q >> 1]);
-              }
-              if (FORMAT == kCacheBf16) {
+            for (int pc = 0; pc < kPieces; ++pc) {
+              uint32_t w[4][4];
+              uint2 vh[4];
+              if (R128) {
+                const int chunk = 8 * pc + (g >> 1) + 4 * (g & 1);
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                  lo[u] = bf16_lo(w[u][q]);
-                  hi[u] = bf16_hi(w[u][q]);
+                  const uint4 x = lds128(vt + tok_offset<Lay::kBox>(vr[u], chunk));
+                  w[u][0] = x.x;
+                  w[u][1] = x.y;
+                  w[u][2] = x.z;
+                  w[u][3] = x.w;
                 }
               } else {
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
-                  const float2 f = __fmul2_rn(f16x2_to_float2(q & 1 ? vh[u].y : vh[u].x), make_float2(vscale[u], vscale[u]));
-                  lo[u] = f.x;
-                  hi[u] = f.y;
+                  const uint2 x = lds64(vt + tok_offset<Lay::kBox>(vr[u], g >> 1) + 8 * (g & 1));
+                  w[u][0] = x.x;
+                  w[u][1] = x.y;
                 }
               }
-              if (BETA) {
-                const float4 *cp = reinterpret_cast<const float4 *>(s_coef) + pc * 64 + 2 * q * 8 + lane_g;
-                const float4 bs = cp[0], id = cp[8];
-                const float2 b2 = make_float2(bs.x, bs.y), s2 = make_float2(bs.z, bs.w);
-                const float2 ic2 = make_float2(id.x, id.y), d2 = make_float2(id.z, id.w);
+              const int lane_g = R128 ? (g >> 1) + 4 * (g & 1) : g;  // the piece's place among the coefficients
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                  const float2 e = bank_pair(b2, s2, ic2, d2, make_float2(lo[u], hi[u]));
-                  lo[u] = e.x;
-                  hi[u] = e.y;
+              for (int q = 0; q < kPer / 2; ++q) {  // pairs of channels: one row block of the product each
+                uint32_t a0, a1, a2, a3;
+                float lo[4], hi[4];
+                if (FORMAT == kCacheE4m3 && !(q & 1)) {
+#pragma unroll
+                  for (int u = 0; u < 4; ++u) vh[u] = e4m3x4_to_f16(w[u][q >> 1]);
                 }
-              }
-              a0 = pack_bf16(lo[0], lo[1]);
-              a1 = pack_bf16(hi[0], hi[1]);
-              a2 = pack_bf16(lo[2], lo[3]);
-              a3 = pack_bf16(hi[2], hi[3]);
+                if (FORMAT == kCacheBf16) {
 #pragma unroll
-              for (int t = 0; t < NT; ++t) mma_bf16(acc[t][pc * (kPer / 2) + q], a0, a1, a2, a3, pf[t][0], pf[t][1]);
+                  for (int u = 0; u < 4; ++u) {
+                    lo[u] = bf16_lo(w[u][q]);
+                    hi[u] = bf16_hi(w[u][q]);
+                  }
+                } else {
+#pragma unroll
+                  for (int u = 0; u < 4; ++u) {
+                    const float2 f = __fmul2_rn(f16x2_to_float2(q & 1 ? vh[u].y : vh[u].x), make_float2(vscale[u], vscale[u]));
+                    lo[u] = f.x;
+                    hi[u] = f.y;
+                  }
+                }
+                if (BETA) {
+                  const float4 *cp = reinterpret_cast<const float4 *>(s_coef) + pc * 64 + 2 * q * 8 + lane_g;
+                  const float4 bs = cp[0], id = cp[8];
+                  const float2 b2 = make_float2(bs.x, bs.y), s2 = make_float2(bs.z, bs.w);
+                  const float2 ic2 = make_float2(id.x, id.y), d2 = make_float2(id.z, id.w);
+#pragma unroll
+                  for (int u = 0; u < 4; ++u) {
+                    const float2 e = bank_pair(b2, s2, ic2, d2, make_float2(lo[u], hi[u]), kTiny);
+                    lo[u] = e.x;
+                    hi[u] = e.y;
+                  }
+                }
+                a0 = pack_bf16(lo[0], lo[1]);
+                a1 = pack_bf16(hi[0], hi[1]);
+                a2 = pack_bf16(lo[2], lo[3]);
+                a3 = pack_bf16(hi[2], hi[3]);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) mma_bf16(acc[t][pc * (kPer / 2) + q], a0, a1, a2, a3, pf[t][0], pf[t][1]);
+              }
             }
-          }
+          };
+          if (BETA && (FORMAT == kCacheBf16 || any_dv)) mix(std::true_type{});
+          else mix(std::false_type{});
           // The largest |E| matters where weights come near the end of the range, or where a tiny channel
           // could leave its own: it is then found by forming the bank once more, out of the loop above, which
           // stays one stretch of code (a head with a tiny channel takes 2 to 2.5 times as long).  (Channel ch of the
