@@ -96,16 +96,17 @@ __global__ void __launch_bounds__(kExactThreads, 7)
       const float4 wd = *reinterpret_cast<const float4 *>(p + piece_wide(row_tile, D));
       wide += (wd.x + wd.y) + (wd.z + wd.w);
       const float top = fmaxf(m, st.x);
-      const float w0 = m == -INFINITY ? (l != l ? 1.f : 0.f) : ex2_approx(m - top);
-      const float w1 = st.x == -INFINITY ? (st.y != st.y ? 1.f : 0.f) : ex2_approx(st.x - top);  // NaN scores have no maximum
+      // roots of the weights, applied twice
+      const float r0 = m == -INFINITY ? (l != l ? 1.f : 0.f) : weight_root(m - top);
+      const float r1 = st.x == -INFINITY ? (st.y != st.y ? 1.f : 0.f) : weight_root(st.x - top);  // NaN scores have no maximum
       m = top;
-      l = l * w0 + st.y * w1;
+      l = fmaf(st.y * r1, r1, l * r0 * r0);
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        acc[c][0] = fmaf(v[c].x, w1, acc[c][0] * w0);
-        acc[c][1] = fmaf(v[c].y, w1, acc[c][1] * w0);
-        acc[c][2] = fmaf(v[c].z, w1, acc[c][2] * w0);
-        acc[c][3] = fmaf(v[c].w, w1, acc[c][3] * w0);
+        acc[c][0] = fmaf(v[c].x * r1, r1, acc[c][0] * r0 * r0);
+        acc[c][1] = fmaf(v[c].y * r1, r1, acc[c][1] * r0 * r0);
+        acc[c][2] = fmaf(v[c].z * r1, r1, acc[c][2] * r0 * r0);
+        acc[c][3] = fmaf(v[c].w * r1, r1, acc[c][3] * r0 * r0);
       }
     }
     if (c0 == 0) {
@@ -139,10 +140,10 @@ __global__ void __launch_bounds__(kExactThreads, 7)
       for (int e = 0; e < E; ++e) x[e] = 0.f;
 #pragma unroll
       for (int q = 0; q < kWarps; ++q) {
-        const float wq = s_m[q][row] == -INFINITY ? (s_l[q][row] != s_l[q][row] ? 1.f : 0.f) : ex2_approx(s_m[q][row] - M);
-        L = fmaf(wq, s_l[q][row], L);
+        const float root = s_m[q][row] == -INFINITY ? (s_l[q][row] != s_l[q][row] ? 1.f : 0.f) : weight_root(s_m[q][row] - M);
+        L = fmaf(root, root * s_l[q][row], L);
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = fmaf(wq, u.part[q][row][lane * E + e], x[e]);
+        for (int e = 0; e < E; ++e) x[e] = fmaf(root, root * u.part[q][row][lane * E + e], x[e]);
       }
       const bool empty = M == -INFINITY && L == 0.f;
       bool good = true;

@@ -34,9 +34,13 @@ constexpr float kLinearReach = 0.7f;           // beta max|v| up to which a chan
                                                // 2^-9 / (1/2 beta), the linear one at v = -max|v|, the other at any v
 constexpr float kTinyReach = 0.000244140625f;  // 2^-12: up to which it is tiny
 // What the range of bf16 and fp32 may cost: a term whose weight or bank underflows is lost.  It is
-// at most 2^-126 times the other factor's largest: 2^8 (P) or the largest |E| that the channel met.
+// at most 2^-126 times the other factor's largest: 2^8 (P) or the largest |E| among the keys of such a weight.
 // While that is at most 2^30, the lost terms of 2^20 keys stay under 2^-76, against a >= 2^-66; where
-// it is more, the channel's class c (2^30 to 2^(30 + 6 c)) raises the bound on a by as much.  One
+// it is more, the channel's class c (2^30 to 2^(30 + 6 c)) raises the bound on a by as much.  The kernel of
+// many rows knows the largest |E| of every key tile; the kernel of few rows looks for it in the tiles that
+// hold a weight under 2^kDeepP of the maximum at that time.  What earlier tiles, another warp or another CTA
+// summed against a smaller maximum, however large its |E|, is moved to the larger one without such a loss
+// (weight_root).  One
 // class for a whole head would send every channel of small beta to the exact path because of one of
 // large beta: reads of 4096 keys at beta 0.05 to 20 took 28 ms in place of 0.37.
 constexpr float kMostShift = 32000.f;  // of a shifted channel's s (beyond it the exact path takes over)
@@ -49,7 +53,7 @@ constexpr int kWidest = 15;                 // the class of |E| from 2^114 on, i
 constexpr int kWideLinear = 7;              // a linear channel's last class: lost terms under 2^-34, its a from 2^-12
 constexpr float kLeastA = 1.3552527e-20f;   // 2^-66
 constexpr float kMostA = 1.2980742e33f;     // 2^110
-constexpr float kDeepP = -100.f;            // log2 of a weight below which its term may be lost (the kernel that looks)
+constexpr float kDeepP = -100.f;            // log2 of a weight below which its term may be lost (the kernel of few rows)
 constexpr float kLeastLinear = 0.125f;      // x = 1 + a of a linear channel: there a rounding of E (2^-9, as |E| < 1) is
                                             // 2^-9 / (beta x) = 2^-9 |v| / (-x log x) in the result, under 2^-7 |v|;
                                             // and v is three times the sample's largest at least, seldom even in rows of one key
@@ -60,6 +64,11 @@ __device__ __forceinline__ float tiny_scale(float beta) {
   // 2^38 times beta without its fraction
   return fmaxf(__int_as_float(__float_as_int(beta * 274877906944.f) & 0x7f800000), 1.f);
 }
+
+// The root of 2^x, x <= 0, by which a sum is multiplied twice when a maximum rises by -x: 2^x itself is 0 from 126
+// on, where a sum of up to 2^127 still matters.  With the root no lower than 2^-126, what is lost or left over is
+// under 2^-124 of what is held, 2^-95 of E, against a >= 2^-66.
+__device__ __forceinline__ float weight_root(float x) { return ex2_approx(fmaxf(0.5f * x, -126.f)); }
 
 // 2^-29 E(v) = 2^(b v + s) + ic + d v, with b = beta log2 e: shifted {b, -b max v rounded to a whole number, less 29, 0, 0},
 // linear {b, -29, -2^-29, 0}, tiny {0, -1000, 0, 2^-29 D}

@@ -396,13 +396,13 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
                 if (mx > m[t][u] + kRowMaxLag) {
-                  const float alpha = ex2_approx(m[t][u] - mx);  // 0 the first time
+                  const float root = weight_root(m[t][u] - mx);  // (the first time there is nothing to move)
                   m[t][u] = mx;
-                  L[t][u] *= alpha;
+                  L[t][u] = L[t][u] * root * root;
 #pragma unroll
                   for (int c = 0; c < MT; ++c) {
-                    acc[t][c][u] *= alpha;
-                    acc[t][c][u + 2] *= alpha;
+                    acc[t][c][u] = acc[t][c][u] * root * root;
+                    acc[t][c][u + 2] = acc[t][c][u + 2] * root * root;
                   }
                 }
               }
@@ -589,10 +589,10 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
       for (int q = 0; q < kTokWarps; ++q) {
         const float2 st = s_stat[q * kRows + r];
         // a row of NaN scores has no maximum
-        const float wq = st.x != -INFINITY ? ex2_approx(st.x - M) : st.y != st.y ? 1.f : 0.f;
-        Lr = fmaf(wq, st.y, Lr);
+        const float root = st.x != -INFINITY ? weight_root(st.x - M) : st.y != st.y ? 1.f : 0.f;
+        Lr = fmaf(root, root * st.y, Lr);
         const float x = tid < D ? reinterpret_cast<const float *>(smem + q * NS * Lay::kStage)[r * Lay::kRedStride + tid] : 0.f;
-        if (wq != 0.f) av = fmaf(wq, x, av);
+        if (root != 0.f) av = fmaf(root, root * x, av);
       }
       const int rr = row0 + r, tok = rr / a.group, hq = sg.h * a.group + rr % a.group;
       const long long orow = (static_cast<long long>(sg.si.q0) + tok) * a.Hq + hq;

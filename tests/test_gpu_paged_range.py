@@ -1,0 +1,54 @@
+"""The paged read where scores and values leave the range of fp32 between key tiles (needs a GB300).
+
+Scores: q is 8 in its first channels and 0 elsewhere, so that with d = 64 a key's score is the sum of its
+first channels (sqrt(2) less at d = 128).  The bounds are the ones of the other paged reads: what is
+recomputed, and what is not, has to meet them alike.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2602_07160_gb300 import fem
+from tests.test_gpu_paged_read import DEV, check, lib, make  # noqa: F401  (lib: builds and loads the library)
+
+pytestmark = pytest.mark.gpu
+
+
+def rewrite(cache, table, k, v):
+    """The keys and values [ctx, d] of the only head of sequence 0."""
+    pos = torch.arange(len(k), device=DEV)
+    slots = table[0].long()[pos // cache.page_size] * cache.page_size + pos % cache.page_size
+    fem.fem_cache_write(cache, k.to(torch.bfloat16)[:, None].contiguous(), v.to(torch.bfloat16)[:, None].contiguous(), slots)
+
+
+# (keys, the outlying value's key, the keys whose scores lie higher)
+JUMPS = {"one_warp": (192, 20, (64, 192)),        # the warp that has the value meets the higher scores
+         "another_warp": (192, 20, (64, 80)),     # only the warp beside it does
+         "another_cta": (40000, 20, (30000, 40000))}
+
+
+@pytest.mark.parametrize("fmt,d", [("bf16", 64), ("bf16", 128), ("e4m3", 64), ("e4m3", 128)])
+@pytest.mark.parametrize("where", sorted(JUMPS))
+@pytest.mark.parametrize("n", [1, 4, 40])
+@pytest.mark.parametrize("beta", [5.0, 8.0, 20.0])
+def test_a_prior_that_jumps_over_an_outlying_value(fmt, d, where, n, beta):
+    """A value far above the others in an early key, and later scores higher by more than a weight's range:
+    the value's term, e^(beta v) times next to nothing, is still the larger one."""
+    ctx, at, (lo, hi) = JUMPS[where]
+    q, cache, off, cl, table = make(fmt, 1, 2, d, 64, [(n, ctx)], seed=40)
+    q.zero_()
+    q[..., 0] = 8.0
+    g = torch.Generator().manual_seed(41)
+    for nats in (90.0, 100.0, 110.0, 140.0):
+        k = torch.zeros((ctx, d))
+        k[:, 0] = torch.randn(ctx, generator=g)
+        k[lo:hi, 0] += nats
+        k[:, 0] *= math.sqrt(d) / 8
+        v = torch.rand((ctx, d), generator=g) * 0.5 - 0.5
+        v[:16] = torch.rand((16, d), generator=g) * 2 - 1
+        v[lo:hi] = -0.5
+        # some ten nats over the later keys' term, in half of the channels
+        v[at, ::2] = (nats + 10.0) / beta - 0.5
+        rewrite(cache, table, k.to(DEV), v.to(DEV))
+        check(q, cache, torch.full((1, d), beta, device=DEV), off, cl, table, causal=True, max_q=n, rms=False)
