@@ -146,6 +146,7 @@ __global__ void __launch_bounds__(kExactThreads, 7)
         for (int e = 0; e < E; ++e) x[e] = fmaf(root, root * u.part[q][row][lane * E + e], x[e]);
       }
       const bool empty = M == -INFINITY && L == 0.f;
+      if (L == INFINITY) L = __int_as_float(0x7fffffff);  // finite pieces, a sum past the range: no channel stands
       bool good = true;
 #pragma unroll
       for (int e = 0; e < E; ++e) {

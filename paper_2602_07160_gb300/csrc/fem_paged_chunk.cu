@@ -691,7 +691,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             }
           }
           // The weights against the maximum so far, and their sum.  bf16 and fp32 hold them however far a
-          // score lies above it (to 2^127; beyond, the sum is infinite and the row goes to the exact path);
+          // score lies above it (to 2^127; where they or their sum are beyond, the row goes to the exact path);
           // a sum over kAskSum asks for a larger one from the next tile on.
           const float mz = m == -INFINITY ? 0.f : m;
           const float2 scale2 = make_float2(qk_scale, qk_scale), negm2 = make_float2(-mz, -mz);
@@ -753,7 +753,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         // ---- the row's output (half of its channels), or its piece
         // No weight at all: nothing was seen, or (the segment held keys for the row) every weight fell under
         // the range, against a maximum so large that bf16 rounds it by more; that is left to the exact path.
-        if (L == 0.f) {
+        // So is a sum past the range: the last tile's weights may each be within it, to 2^127, and O with them.
+        if (L == 0.f || L == INFINITY) {
           m = -INFINITY;
           if (w.lim > sg.kt0 * kChunkKeys) L = __int_as_float(0x7fffffff);
         }

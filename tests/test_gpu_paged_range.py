@@ -52,3 +52,41 @@ def test_a_prior_that_jumps_over_an_outlying_value(fmt, d, where, n, beta):
         v[at, ::2] = (nats + 10.0) / beta - 0.5
         rewrite(cache, table, k.to(DEV), v.to(DEV))
         check(q, cache, torch.full((1, d), beta, device=DEV), off, cl, table, causal=True, max_q=n, rms=False)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("beta", [None, 0.0, 0.1, 0.7, 8.0])
+@pytest.mark.parametrize("ctx", [1024, 30 * 1024])
+@pytest.mark.parametrize("nats", [84.0, 84.5, 85.0, 86.0, 87.0, 88.0, 88.5, 89.0])
+def test_weights_that_are_finite_and_whose_sum_is_not(fmt, beta, ctx, nats):
+    """Scores that rise in a row's last key tile until its weights against the maximum so far are still in
+    fp32's range and their sum is not; a read in one piece, and one that is joined."""
+    n, d = 60, 64
+    q, cache, off, cl, table = make(fmt, 1, 2, d, 64, [(n, ctx)], seed=42)
+    q.zero_()
+    q[..., 0] = 8.0
+    k = torch.zeros((ctx, d))
+    k[ctx - 128:, 0] = nats
+    for spread in (0.02, 1.0):
+        v = spread * torch.randn((ctx, d), generator=torch.Generator().manual_seed(43))
+        rewrite(cache, table, k.to(DEV), v.to(DEV))
+        b = None if beta is None else torch.full((1, d), beta, device=DEV)
+        check(q, cache, b, off, cl, table, causal=True, max_q=n, rms=False)
+
+
+@pytest.mark.parametrize("beta", [None, 0.7])
+def test_pieces_whose_sums_are_finite_and_together_are_not(beta):
+    """One key of a high score in each of two key tiles, eight tiles apart in a long context, that end
+    the stretches of two CTAs in one of the steps below."""
+    n, d, tiles = 20, 64, 608
+    ctx = 128 * tiles
+    q, cache, off, cl, table = make("bf16", 1, 2, d, 64, [(n, ctx)], seed=48)
+    q.zero_()
+    q[..., 0] = 8.0
+    v = torch.randn((ctx, d), generator=torch.Generator().manual_seed(49))
+    for step in range(8):
+        k = torch.zeros((ctx, d))
+        k[[128 * (100 + step) + 3, 128 * (108 + step) + 3], 0] = 88.5
+        rewrite(cache, table, k.to(DEV), v.to(DEV))
+        b = None if beta is None else torch.full((1, d), beta, device=DEV)
+        check(q, cache, b, off, cl, table, causal=True, max_q=n, rms=False)
