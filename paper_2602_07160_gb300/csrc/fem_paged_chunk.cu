@@ -649,13 +649,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             return y * qk_scale;
           };
           // The row's maximum moves to `top`: its sum, and its half of the products so far (of the key tiles
-          // before: see the issue order), are rescaled.  Whole warps.
+          // before: see the issue order), are rescaled.  (By up to 2^-128 at once, when the tile before had its
+          // weights near the end of the range: they are worth 1 after that.)  Whole warps.
           auto raise = [&](float top, bool products) {
-            float alpha = 1.f;
+            float root = 1.f;
             if (top > m) {
-              alpha = m == -INFINITY ? 0.f : ex2_approx(m - top);
+              root = weight_root(m - top);
               m = top;
-              L *= alpha;
+              L = L * root * root;
             }
             if (products) {
 #pragma unroll 1
@@ -664,7 +665,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
                 tmem_ld32(tO + c * 32, v);
                 tmem_ld_wait();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
+                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * root * root);
                 tmem_st32(tO + c * 32, v);
               }
             }

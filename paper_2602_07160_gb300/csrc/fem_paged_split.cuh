@@ -39,8 +39,8 @@ constexpr float kTinyReach = 0.000244140625f;  // 2^-12: up to which it is tiny
 // it is more, the channel's class c (2^30 to 2^(30 + 6 c)) raises the bound on a by as much.  The kernel of
 // many rows knows the largest |E| of every key tile; the kernel of few rows looks for it in the tiles that
 // hold a weight under 2^kDeepP of the maximum at that time.  What earlier tiles, another warp or another CTA
-// summed against a smaller maximum, however large its |E|, is moved to the larger one without such a loss
-// (weight_root).  One
+// summed against a smaller maximum, however large its |E| or its weights, is moved to the larger one without such
+// a loss (weight_root).  One
 // class for a whole head would send every channel of small beta to the exact path because of one of
 // large beta: reads of 4096 keys at beta 0.05 to 20 took 28 ms in place of 0.37.
 constexpr float kMostShift = 32000.f;  // of a shifted channel's s (beyond it the exact path takes over)

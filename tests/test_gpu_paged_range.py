@@ -90,3 +90,20 @@ def test_pieces_whose_sums_are_finite_and_together_are_not(beta):
         rewrite(cache, table, k.to(DEV), v.to(DEV))
         b = None if beta is None else torch.full((1, d), beta, device=DEV)
         check(q, cache, b, off, cl, table, causal=True, max_q=n, rms=False)
+
+
+@pytest.mark.parametrize("beta", [None, 0.1, 0.7, 8.0])
+@pytest.mark.parametrize("nats", [86.5, 87.0, 87.5, 88.0, 88.5])
+def test_weights_near_the_end_of_the_range_before_the_maximum_rises(beta, nats):
+    """Two key tiles that hold a few keys of the same high score each: the first tile's weights, up to the
+    end of fp32's range against the maximum so far, are worth as much as the second's."""
+    n, ctx, d = 60, 1024, 64
+    q, cache, off, cl, table = make("bf16", 1, 2, d, 64, [(n, ctx)], seed=44)
+    q.zero_()
+    q[..., 0] = 8.0
+    k = torch.zeros((ctx, d))
+    k[[515, 600, 650, 720], 0] = nats  # a key of either half of key tiles 4 and 5
+    v = torch.randn((ctx, d), generator=torch.Generator().manual_seed(45))
+    rewrite(cache, table, k.to(DEV), v.to(DEV))
+    b = None if beta is None else torch.full((1, d), beta, device=DEV)
+    check(q, cache, b, off, cl, table, causal=True, max_q=n, rms=False)
