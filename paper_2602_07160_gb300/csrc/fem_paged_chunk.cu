@@ -47,6 +47,7 @@ constexpr int kChunkThreads = 896;
 constexpr int kChunkKeys = 128;
 constexpr int kBankThreads = 256;
 constexpr float kAskSum = 1.0995116e12f;  // 2^40
+constexpr float kLeastSum = 0.25f;
 constexpr int kInvRing = 8;   // key tiles whose missing pages are remembered
 
 template <int FORMAT, int D>
@@ -560,8 +561,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
     const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t tS = tmem + t * 128 + half * 64 + lane_off;  // P goes over the first 32 of these 64 columns
     const uint32_t tO = tmem + 256 + t * D + half * kHalfD + lane_off;
-    // per row: a maximum or a sum, or a maximum of each half in bf16; per half and warp: the tile of its last
-    // request
+    // per row: a maximum or a sum, or a rise asked for by each half in bf16; per half and warp: the tile of its
+    // last request
     float *s_row = reinterpret_cast<float *>(smem + Lay::kRow) + t * 128;
     volatile __nv_bfloat16 *s_top = reinterpret_cast<volatile __nv_bfloat16 *>(s_row);
     volatile unsigned *s_ask = reinterpret_cast<volatile unsigned *>(smem + Lay::kAsk) + (t * 4 + (warp & 3)) * 2;
@@ -681,14 +682,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
             if (half == 1) top = s_row[r];
             raise(top, k > 0);
           } else {
-            // a maximum asked for during the tile before: what either thread wrote then is seen by both
+            // a rise asked for during the tile before: what either thread wrote then is seen by both
             // now, through the arrivals of P and the product they let start
             const unsigned q0 = s_ask[0], q1 = s_ask[1];
             if (q0 == ns - 1 || q1 == ns - 1) {
               const float t0 = q0 == ns - 1 ? __bfloat162float(s_top[2 * r]) : -INFINITY;
               const float t1 = q1 == ns - 1 ? __bfloat162float(s_top[2 * r + 1]) : -INFINITY;
               if (!(ok = meet())) break;  // both have read what the next request overwrites
-              raise(fmaxf(t0, t1), true);
+              raise(m + fmaxf(t0, t1), true);
             }
           }
           // The weights against the maximum so far, and their sum.  bf16 and fp32 hold them however far a
@@ -717,8 +718,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           }
           const float sum = (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
           if (__any_sync(0xffffffffu, sum > kAskSum)) {
-            // m + log2(sum) is at least the largest score, and at most 6 more
-            s_top[2 * r + half] = __float2bfloat16_rn(sum > kAskSum ? m + lg2_approx(sum) : -INFINITY);
+            // m + log2(sum) is at least the largest score, and at most 6 more.  The rise, from 40 to 128, goes over in
+            // bf16, within 1/2; of a maximum in the tens of thousands bf16 keeps no more than 128.
+            s_top[2 * r + half] = __float2bfloat16_rn(sum > kAskSum ? lg2_approx(sum) : -INFINITY);
             if (lane == 0) s_ask[half] = ns;
           }
           L += sum;
@@ -752,10 +754,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
         if (!(ok = meet())) break;
         if (half == 1) L = s_row[r];
         // ---- the row's output (half of its channels), or its piece
-        // No weight at all: nothing was seen, or (the segment held keys for the row) every weight fell under
-        // the range, against a maximum so large that bf16 rounds it by more; that is left to the exact path.
-        // So is a sum past the range: the last tile's weights may each be within it, to 2^127, and O with them.
-        if (L == 0.f || L == INFINITY) {
+        // A row that saw nothing has no weight.  Where the segment held keys for it, the sum lies between 1/2 and
+        // the end of the range, or the row is left to the exact path: the last tile's weights may each be within
+        // the range, to 2^127, and O with them, and their sum be past it; and scores past 2^24 are rounded to
+        // whole numbers, the maximum apart from the weights.  (What paged_out takes for lost is relative to a
+        // sum of about 1 or more.)
+        if (!(L >= kLeastSum && L < INFINITY)) {
           m = -INFINITY;
           if (w.lim > sg.kt0 * kChunkKeys) L = __int_as_float(0x7fffffff);
         }

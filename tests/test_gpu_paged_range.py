@@ -107,3 +107,40 @@ def test_weights_near_the_end_of_the_range_before_the_maximum_rises(beta, nats):
     rewrite(cache, table, k.to(DEV), v.to(DEV))
     b = None if beta is None else torch.full((1, d), beta, device=DEV)
     check(q, cache, b, off, cl, table, causal=True, max_q=n, rms=False)
+
+
+@pytest.mark.parametrize("beta", [None, 0.1, 0.7, 8.0])
+@pytest.mark.parametrize("base", [15104.0, 30208.0, 60416.0])
+def test_a_maximum_that_rises_among_scores_of_tens_of_thousands(beta, base):
+    """Scores so large that a maximum in 8 bits could lie a weight's range over the true one."""
+    n, ctx, d = 40, 1024, 64
+    q, cache, off, cl, table = make("bf16", 1, 2, d, 64, [(n, ctx)], seed=46)
+    q.zero_()
+    q[..., :3] = 8.0
+    b = None if beta is None else torch.full((1, d), beta, device=DEV)
+    v = torch.randn((ctx, d), generator=torch.Generator().manual_seed(47))
+    for step in range(0, 48):
+        k = torch.zeros((ctx, d))
+        k[:, 0] = base                    # to multiples of 128 or 256, in bf16
+        k[:, 1] = 2.0 * step              # where the maximum falls between them
+        k[[520, 640, 700], 2] = 42.0      # the largest scores, in key tiles 4 and 5
+        k[[521, 641, 701], 2] = 40.0      # an eighth of their weight
+        rewrite(cache, table, k.to(DEV), v.to(DEV))
+        check(q, cache, b, off, cl, table, causal=True, max_q=n, rms=False)
+
+
+@pytest.mark.parametrize("spread", [0.25, 1.0, 2.0])
+def test_scores_whose_fp32_steps_are_tens(spread):
+    """Equal scores of 2^30 and up, where fp32's steps are 64 and 128, over values far under the first ones':
+    the rounding of a maximum takes no part of the weights with it."""
+    n, ctx, d = 40, 1024, 64
+    q, cache, off, cl, table = make("bf16", 1, 2, d, 64, [(n, ctx)], seed=50)
+    q.zero_()
+    q[..., 0] = 8.0
+    v = spread * torch.rand((ctx, d), generator=torch.Generator().manual_seed(51)) - 5.0 - spread / 2
+    v[:16] = 0.0
+    for step in range(64):
+        k = torch.zeros((ctx, d))
+        k[16:, 0] = 2.0 ** 30 * (1 + step / 64)
+        rewrite(cache, table, k.to(DEV), v.to(DEV))
+        check(q, cache, torch.full((1, d), 8.0, device=DEV), off, cl, table, causal=True, max_q=n, rms=False)
