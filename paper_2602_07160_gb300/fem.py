@@ -338,7 +338,7 @@ class PagedCache:
     bf16 and float32 caches are the two tensors; float8_e4m3fn ones have the rows' scale
     exponents k_exp, v_exp (uint8 [num_pages, H, page_size]) beside them.  The object keeps
     the tensors, checks them once, and is what ``fem_cache_write``, ``fem_cache_gather`` and
-    ``fem_paged_read`` take."""
+    ``fem_paged_read`` take.  Those run on the cache's device, which has to be the current one."""
 
     FORMATS = {torch.bfloat16: 0, torch.float8_e4m3fn: 1, torch.float32: 2}
 
@@ -378,6 +378,12 @@ class PagedCache:
         return cls(k.view(dtype), v.view(dtype), *exps)
 
 
+def _check_device(cache):
+    """The library launches on the current device, with its workspace and error word."""
+    if torch.cuda.current_device() != cache.index:
+        raise ValueError("the cache's device must be the current one")
+
+
 def _raw_stream(stream, cache):
     """The stream a paged-cache call runs on, as a number."""
     return torch._C._cuda_getCurrentRawStream(cache.index) if stream is None else stream.cuda_stream
@@ -410,6 +416,7 @@ def fem_cache_write(cache: PagedCache, k, v, slots, stream=None):
     """Put N tokens' keys and values [N, H, d] into the cache at slots (int64 [N]: page *
     page_size + row; negative: left out).  k and v may be strided views; a float8_e4m3fn
     cache quantises each (token, head) row as it is written."""
+    _check_device(cache)
     N = k.shape[0]
     _check_rows("k", k, cache, cache.H)
     _check_rows("v", v, cache, cache.H)
@@ -427,6 +434,7 @@ def fem_cache_gather(cache: PagedCache, block_table, starts, offsets, total: int
 
     block_table: int32 [S, max_pages]; starts: int32 [S], each stretch's first position;
     offsets: int32 [S + 1], its rows of the output; total = offsets[S]."""
+    _check_device(cache)
     if block_table.dim() != 2:
         raise ValueError("block_table must be [S, max_pages]")
     (S, max_pages), shape, index = block_table.shape, (total, cache.H, cache.d), cache.index
@@ -454,6 +462,7 @@ def fem_paged_read(q, cache: PagedCache, beta, q_offsets, ctx_lens, block_table,
     the cache's heads or None (the prior mean, plain softmax attention); max_q bounds the rows
     of a sequence.  Returns (out [N, Hq, d] of q's type, lse [N, Hq] float32); ``lse=False``
     skips the log-normaliser."""
+    _check_device(cache)
     _check_rows("q", q, cache, None)
     N, Hq, d = q.shape
     if Hq % cache.H:
