@@ -389,6 +389,17 @@ def _raw_stream(stream, cache):
     return torch._C._cuda_getCurrentRawStream(cache.index) if stream is None else stream.cuda_stream
 
 
+def _output(shape, dtype, cache, stream):
+    """An output a call allocates: memory of the stream that writes it.  With another stream than the current
+    one, the current one's later use is waited for as well before the memory is given out again."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=cache.device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=cache.device)
+    t.record_stream(torch.cuda.current_stream(cache.device))
+    return t
+
+
 def _check_rows(name, t, cache, heads):
     """A [N, heads, d] input of the cache's row type, d contiguous."""
     if t.dim() != 3 or t.shape[2] != cache.d or (heads is not None and t.shape[1] != heads):
@@ -439,9 +450,9 @@ def fem_cache_gather(cache: PagedCache, block_table, starts, offsets, total: int
         raise ValueError("block_table must be [S, max_pages]")
     (S, max_pages), shape, index = block_table.shape, (total, cache.H, cache.d), cache.index
     if k_out is None:
-        k_out = torch.empty(shape, dtype=cache.row_dtype, device=cache.device)
+        k_out = _output(shape, cache.row_dtype, cache, stream)
     if v_out is None:
-        v_out = torch.empty(shape, dtype=cache.row_dtype, device=cache.device)
+        v_out = _output(shape, cache.row_dtype, cache, stream)
     rc = load().fem_cache_gather(cache._ref, _check_whole("block_table", block_table, (S, max_pages), torch.int32, index),
                                  max_pages, _check_whole("starts", starts, (S,), torch.int32, index),
                                  _check_whole("offsets", offsets, (S + 1,), torch.int32, index), S,
@@ -472,12 +483,12 @@ def fem_paged_read(q, cache: PagedCache, beta, q_offsets, ctx_lens, block_table,
     (S, max_pages), index = block_table.shape, cache.index
     out_ptr = lse_ptr = beta_ptr = None
     if out is None:
-        out = torch.empty((N, Hq, d), dtype=cache.row_dtype, device=cache.device)
+        out = _output((N, Hq, d), cache.row_dtype, cache, stream)
         out_ptr = out.data_ptr()
     else:
         out_ptr = _check_whole("out", out, (N, Hq, d), q.dtype, index)
     if lse is None:
-        lse = torch.empty((N, Hq), dtype=torch.float32, device=cache.device)
+        lse = _output((N, Hq), torch.float32, cache, stream)
         lse_ptr = lse.data_ptr()
     elif lse is not False:
         lse_ptr = _check_whole("lse", lse, (N, Hq), torch.float32, index)

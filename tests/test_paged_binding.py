@@ -1,4 +1,5 @@
 """The binding of the paged cache's calls against a stand-in library and cache (CPU only)."""
+import contextlib
 import types
 
 import pytest
@@ -53,3 +54,32 @@ def test_another_current_device_is_refused(library, monkeypatch, name):
     with pytest.raises(ValueError, match="current"):
         calls(stand_in(), stream)[name]()
     assert library.calls == []
+
+
+@pytest.mark.parametrize("name,outputs", [("fem_cache_gather", 2), ("fem_paged_read", 2)])
+def test_outputs_are_memory_of_the_stream_that_writes_them(library, monkeypatch, name, outputs):
+    """Memory of the current stream could still be in use there, or be given out again there, while the
+    call's own stream writes it."""
+    side, main = types.SimpleNamespace(cuda_stream=5), types.SimpleNamespace(cuda_stream=0)
+    inside, made, recorded = [main], [], []
+
+    @contextlib.contextmanager
+    def use(stream):
+        inside.append(stream)
+        yield
+        inside.pop()
+
+    empty = torch.empty
+
+    def allocate(*args, **kw):
+        made.append(inside[-1])
+        return empty(*args, **kw)
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: inside[-1])
+    monkeypatch.setattr(torch.cuda, "stream", use)
+    monkeypatch.setattr(torch, "empty", allocate)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: recorded.append(s), raising=False)
+    calls(stand_in(), side)[name]()
+    assert library.calls == [name]
+    assert made == [side] * outputs and recorded == [main] * outputs
