@@ -394,6 +394,18 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
           vmax[e] = -INFINITY;
           vabs[e] = 0.f;
         }
+        auto values = [&](long long row, float2 (&v)[2]) {
+          if (kCodes) {
+            const uint32_t x = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(a.c.v) + row * D + col * 4);
+            const float sc = paged_scale(a.c.ve[row]);
+            v[0] = __fmul2_rn(e4m3x2_to_float2(x & 0xffffu), make_float2(sc, sc));
+            v[1] = __fmul2_rn(e4m3x2_to_float2(x >> 16), make_float2(sc, sc));
+          } else {
+            const uint2 x = *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(a.c.v) + row * D + col * 4);
+            v[0] = make_float2(bf16_lo(x.x), bf16_hi(x.x));
+            v[1] = make_float2(bf16_lo(x.y), bf16_hi(x.y));
+          }
+        };
         const int page = sg.si.ctx > 0 ? paged_page(a, sg.s, 0) : -1;
         if (page >= 0) {
           const long long row = paged_row(a.c, page, sg.h, 0);
@@ -401,22 +413,34 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
 #pragma unroll 4
           for (int kk = 0; kk < cnt; ++kk) {
             float2 v[2];
-            if (kCodes) {
-              const uint32_t x = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(a.c.v) + (row + kk) * D + col * 4);
-              const float sc = paged_scale(a.c.ve[row + kk]);
-              v[0] = __fmul2_rn(e4m3x2_to_float2(x & 0xffffu), make_float2(sc, sc));
-              v[1] = __fmul2_rn(e4m3x2_to_float2(x >> 16), make_float2(sc, sc));
-            } else {
-              const uint2 x = *reinterpret_cast<const uint2 *>(static_cast<const __nv_bfloat16 *>(a.c.v) + (row + kk) * D + col * 4);
-              v[0] = make_float2(bf16_lo(x.x), bf16_hi(x.x));
-              v[1] = make_float2(bf16_lo(x.y), bf16_hi(x.y));
-            }
+            values(row + kk, v);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               vmax[2 * e] = fmaxf(vmax[2 * e], v[e].x);
               vmax[2 * e + 1] = fmaxf(vmax[2 * e + 1], v[e].y);
               vabs[2 * e] = fmaxf(vabs[2 * e], fabsf(v[e].x));
               vabs[2 * e + 1] = fmaxf(vabs[2 * e + 1], fabsf(v[e].y));
+            }
+          }
+        }
+        unsigned zero = 0;  // the channels that have met nothing but zeros
+#pragma unroll
+        for (int e = 0; e < 4; ++e) zero |= vabs[e] == 0.f ? 1u << e : 0u;
+        if (zero) {
+#pragma unroll 2
+          for (int i = sample_last(sg.si.ctx); i < sg.si.ctx; ++i) {
+            const int p = sample_page(a, sg.s, i);
+            if (p >= 0) {
+              float2 v[2];
+              values(paged_row(a.c, p, sg.h, i), v);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float x = e & 1 ? v[e / 2].y : v[e / 2].x;
+                if ((zero >> e) & 1u) {
+                  vmax[e] = fmaxf(vmax[e], x);
+                  vabs[e] = fmaxf(vabs[e], fabsf(x));
+                }
+              }
             }
           }
         }

@@ -12,7 +12,8 @@
 //
 // Value bank.  The read mixes the prior weights P = 2^(s - m) against a bank
 // E(v), in bf16 with fp32 sums, a = sum P E / sum P.  Channel j of a sequence
-// and head goes by its first kSampleKeys values v:
+// and head goes by its first kSampleKeys values v (where those are all zero, by its
+// last ones):
 //   tiny     (beta max|v| <= 2^-12)  E = D v,                    o = a / D
 //   linear   (beta max|v| <= 0.7)    E = expm1(beta v),          o = log1p(a) / beta
 //   shifted  (else)                  E = exp(beta (v - c)),      o = c + log(a) / beta,  c about max v
@@ -75,6 +76,17 @@ __device__ __forceinline__ float weight_root(float x) { return ex2_approx(fmaxf(
 struct BankCoef {
   float b, s, ic, d;
 };
+
+// A channel whose first values are all zero (tokens without a value of their own, as at the start of many
+// sequences) goes by the last kSampleKeys of those after them.  Taken as of order one, values of 0.01 at beta 2
+// would be read to 2^-9 / beta, a tenth of them.  (Where the last ones are zero too, channels of padding say, order
+// one it is.)
+__device__ __forceinline__ int sample_last(int ctx) { return max(ctx - kSampleKeys, kSampleKeys); }
+// Page of such a position, or -1; the read of its own key tile records what is not there.
+__device__ __forceinline__ int sample_page(const PagedReadArgs &a, int s, int i) {
+  const int p = __ldg(a.table + static_cast<long long>(s) * a.max_pages + (i >> a.c.page_shift));
+  return static_cast<unsigned>(p) < static_cast<unsigned>(a.c.num_pages) ? p : -1;
+}
 
 __device__ __forceinline__ BankCoef bank_coef(float beta, float vmax, float vabs) {
   const float x = beta * (vabs > 0.f ? vabs : 1.f);

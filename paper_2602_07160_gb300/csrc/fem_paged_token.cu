@@ -280,6 +280,20 @@ __global__ void __launch_bounds__(kTokThreads, (TokLayout<FORMAT, D, NT>::kCtas)
             vabs = fmaxf(vabs, fabsf(v[kk]));
           }
         }
+        if (vabs == 0.f) {
+#pragma unroll 1
+          for (int i = sample_last(sg.si.ctx); i < sg.si.ctx; ++i) {
+            const int p = sample_page(a, sg.s, i);
+            if (p >= 0) {
+              const long long r = paged_row(a.c, p, sg.h, i);
+              const float x = FORMAT == kCacheBf16
+                                  ? __bfloat162float(static_cast<const __nv_bfloat16 *>(a.c.v)[r * D + tid])
+                                  : e4m3x2_to_float2(static_cast<const uint8_t *>(a.c.v)[r * D + tid]).x * paged_scale(a.c.ve[r]);
+              vmax = fmaxf(vmax, x);
+              vabs = fmaxf(vabs, fabsf(x));
+            }
+          }
+        }
         const BankCoef c = bank_coef(beta_c, vmax, vabs);
         // element e of a lane's piece of 8 channels, lanes side by side
         const int at = Lay::kElem == 2 || !R128 ? (tid & ~63) + (tid & 7) * 8 + ((tid >> 3) & 7)

@@ -144,3 +144,18 @@ def test_scores_whose_fp32_steps_are_tens(spread):
         k[16:, 0] = 2.0 ** 30 * (1 + step / 64)
         rewrite(cache, table, k.to(DEV), v.to(DEV))
         check(q, cache, torch.full((1, d), 8.0, device=DEV), off, cl, table, causal=True, max_q=n, rms=False)
+
+
+@pytest.mark.parametrize("fmt,d", [("bf16", 64), ("e4m3", 128)])
+@pytest.mark.parametrize("n,ctx", [(1, 20), (1, 300), (1, 5000), (4, 300), (40, 300), (40, 5000)])
+@pytest.mark.parametrize("spread", [0.001, 0.01, 0.1, 1.0])
+def test_channels_whose_first_values_are_zero(fmt, d, n, ctx, spread):
+    """Half of the channels begin with zeros, which say nothing of the values that follow: those are read
+    as well as any."""
+    q, cache, off, cl, table = make(fmt, 1, 2, d, 64, [(n, ctx)], seed=52)
+    g = torch.Generator().manual_seed(53)
+    v = spread * torch.randn((ctx, d), generator=g)
+    v[:16, ::2] = 0
+    rewrite(cache, table, torch.randn((ctx, d), generator=g).to(DEV), v.to(DEV))
+    for beta in (1e-4, 0.01, 0.1, 0.75, 2.0, 20.0):
+        check(q, cache, torch.full((1, d), beta, device=DEV), off, cl, table, causal=True, max_q=n, rms=False)
