@@ -287,7 +287,8 @@ int fem_bwd_f32(const float *q, const float *k, const float *v, const float *bet
  *   FEM_CACHE_F32   float32 elements
  * Sequence s's position i lives in page block_table[s * max_pages + i /
  * page_size], row i % page_size; table entries past a sequence's length are not
- * read.  Slots, tables, offsets and lengths are device arrays and are not
+ * read.  The cache and every array of a call are memory of the current device.
+ * Slots, tables, offsets and lengths are device arrays and are not
  * inspected on the host.  An entry that points outside its buffers is left out
  * (a key that is not there, a row not written, a gathered row of zeros) and
  * recorded: fem_check_device_error() then returns FEM_ERR_INVALID_ARG.
@@ -355,7 +356,9 @@ int fem_cache_gather(const fem_paged_cache *cache, const int *block_table, int m
  * 2^-8 of a term), and recompute in fp32 the channels whose result the range of
  * those could have spoilt: a channel whose beta_j v rises by more than about 75
  * over that of the sequence's first 16 positions costs what it costs in
- * FEM_CACHE_F32, a hundred times as much.  The same inputs give the same bits.
+ * FEM_CACHE_F32, a hundred times as much, and so does a row whose scores rise by
+ * more than about 84 in the last 128 keys that a block reads of it (reads of more
+ * than 16 query rows to a key/value head).  The same inputs give the same bits.
  * The workspace comes from the library's stream-ordered pool.
  */
 int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride_n, int64_t q_stride_h,

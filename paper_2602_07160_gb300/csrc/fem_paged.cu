@@ -48,8 +48,8 @@ __global__ void __launch_bounds__(kExactThreads) paged_exact_kernel(const PagedR
 // well, CH to each (blockIdx.z).  Then
 // channels whose result the ranges could have spoilt (marked in the output), of
 // these rows and of those CTA g finished, are recomputed by the whole block.
-// Alone it takes 20 us after a prompt of 8192 (304 pieces of 256 rows, 40 MB from L2)
-// and 10 us after one token over 131071 keys; as a programmatic dependent its launch
+// Alone it takes 21 us after a prompt of 8192 (304 pieces of 256 rows, 40 MB from L2)
+// and 13 us after one token over 131071 keys; as a programmatic dependent its launch
 // hides behind the reading kernel's tail.
 template <int FORMAT, int D, int CH>
 __global__ void __launch_bounds__(kExactThreads, 7)

@@ -27,7 +27,7 @@
 //                the commit of S also says that the product before it is done: the
 //                softmax may then rescale O
 //
-// A causal prompt of 8192, 16 heads of 128, bf16: 277 us with the join, 990 TFLOP/s
+// A causal prompt of 8192, 16 heads of 128, bf16: 281 us with the join, 979 TFLOP/s
 // (tensor pipe 48 % busy, issue slots 60 %; without the value bank 207 us before the
 // join); the bank's OR of what it forms, which finds the wide channels, takes 10 us.
 //

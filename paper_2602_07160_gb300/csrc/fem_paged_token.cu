@@ -15,8 +15,8 @@
 // tile.  The value bank is formed in registers on the way, once per value for
 // all rows.  mma.sync suffices here: at 8 rows the products take a fraction of
 // the time the bytes do (tensor pipe 9 to 10 % busy).
-// One token over 131071 keys, 8 heads of 128 for 32 query heads, bf16: 100 us with
-// the join, 5.4 TB/s of the 6.8 that a copy reaches.  48 tokens over 2048 to 8192
+// One token over 131071 keys, 8 heads of 128 for 32 query heads, bf16: 101 us with
+// the join, 5.3 TB/s of the 6.8 that a copy reaches.  48 tokens over 2048 to 8192
 // keys each in e4m3: 131 us, 3.8 TB/s: the bytes are half and the bank the same, and
 // the eleven warps of an SM that its registers leave issue in 55 % of the cycles.
 #include <type_traits>
