@@ -367,12 +367,163 @@ int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride
                    void *stream);
 
 /*
+ * What stands around the read in a layer: rotary positions of its queries and
+ * keys, the gated recurrence of a conditioner, and the norms, gate and residual
+ * that end one block and begin the next.  Element types of their arrays:
+ */
+typedef enum { FEM_BF16 = 0, FEM_F32 = 2 } fem_type; /* as FEM_CACHE_BF16, FEM_CACHE_F32 */
+
+/*
+ * An array of heads: element (b, t, h, j) of [B, T, H, d] at p + b stride_b +
+ * t stride_t + h stride_h + j, strides in elements, none negative.  The read's
+ * [B, H, T, d], a projection's [N, H, d] (B = 1) and parts of either are such
+ * arrays.  Any alignment of whole elements will do; 16-byte aligned pointers and
+ * strides are faster.
+ */
+typedef struct {
+    void *p;
+    int64_t stride_b, stride_t, stride_h;
+} fem_heads;
+
+/*
+ * fem_rope_turns -- the rate of every rotated pair, on the host: turns[i] =
+ * theta_i / (2 pi) as a fraction of 2^64, so that a position's angle is one
+ * integer product, exact for any position.  i = 0 .. rotary/2 - 1,
+ * theta_i = base^(-2 i / rotary), scaled for contexts `factor` times as long:
+ *   FEM_ROPE_PLAIN   as it is
+ *   FEM_ROPE_LINEAR  theta_i / factor
+ *   FEM_ROPE_BASE    base factor^(rotary / (rotary - 2)) in place of base
+ *   FEM_ROPE_PARTS   g theta_i + (1 - g) theta_i / factor, g = (c_i - low) /
+ *                    (high - low) clamped to [0, 1], c_i = context theta_i /
+ *                    (2 pi) the pair's turns over the original context
+ * rotary even, 2 .. 1024; base, factor > 0, context > 0 and low < high finite.
+ */
+typedef enum { FEM_ROPE_PLAIN = 0, FEM_ROPE_LINEAR = 1, FEM_ROPE_BASE = 2, FEM_ROPE_PARTS = 3 } fem_rope_scaling;
+int fem_rope_turns(int rotary, double base, int scaling, double factor, double context, double low, double high,
+                   uint64_t *turns);
+
+/*
+ * fem_rope -- rotary positions of queries and keys in one launch: of every head
+ * the first `rotary` elements, in pairs (a, b), become
+ *
+ *   a' = A (a cos x - b sin x),  b' = A (b cos x + a sin x),  x = pos theta_i,
+ *
+ * pair i being elements i and i + rotary/2 (interleaved = 0) or 2 i and 2 i + 1
+ * (1); the others are copied.  inverse = 1 turns by -x, which is the gradient's
+ * way back.
+ *   q, k         : device, [B, T, Hq, d] and [B, T, Hk, d] of `type`; k NULL: none
+ *   q_out, k_out : as q and k; the same pointer and strides rotate in place
+ *   turns        : device, uint64 [rotary/2] (fem_rope_turns); amplitude A
+ *   positions    : device, int32 [B, T], any sign, or NULL: 0 .. T - 1 in every b
+ * d up to 1024, rotary even and 2 .. d.  Angles are exact to fp32 rounding, the
+ * rotation is fp32 arithmetic rounded once.  B = 0 or T = 0 does nothing.
+ */
+int fem_rope(const fem_heads *q, const fem_heads *q_out, int Hq, const fem_heads *k, const fem_heads *k_out, int Hk,
+             int B, int T, int d, int type, const uint64_t *turns, int rotary, int interleaved, float amplitude,
+             const int *positions, int inverse, void *stream);
+
+/*
+ * fem_recur_fwd -- the gated linear recurrence of every channel,
+ *
+ *   h_t = exp(-s_t) h_{t-1} + w(s_t) u_t,  w = 1 (mean = 0) or 1 - exp(-s_t) (mean = 1):
+ *
+ * with w = 1 fem_tdc_conv's, otherwise a weighted running mean.  S sequences of
+ * T steps each (offsets NULL, N = S T rows), or of the rows offsets[s] ..
+ * offsets[s + 1] - 1 of N packed ones.
+ *   s, u, h     : device, [N, C] of `type`, the channels of a row contiguous,
+ *                 rows s_stride, u_stride, h_stride elements apart; s >= 0
+ *   offsets     : device, int32 [S + 1], ascending, or NULL
+ *   T           : the sequences' length, with offsets at least the largest (a
+ *                 bound that chooses the split; longer ones are still right)
+ *   h0, h_last  : device, float32 [num_states, C]: states before the first step
+ *                 and after the last, or NULL: zero, not kept.  The same array
+ *                 updates states in place.
+ *   state_rows  : device, int32 [S]: each sequence's row of them, or NULL: row s.
+ *                 Negative: that sequence starts from zero and is not kept.  Which
+ *                 of two sequences with one row stays is not defined.
+ * Rows of no sequence are not written.  A sequence of length zero hands its state
+ * on.  States, decays and sums are fp32; the same inputs give the same bits.  An
+ * offset or state row outside its array is left out and recorded
+ * (fem_check_device_error returns FEM_ERR_INVALID_ARG).  S = 0 does nothing.  No
+ * workspace.
+ */
+int fem_recur_fwd(const void *s, const void *u, int64_t s_stride, int64_t u_stride, const int *offsets, int S, int T,
+                  int N, int C, int type, int mean, const float *h0, float *h_last, const int *state_rows,
+                  int num_states, void *h, int64_t h_stride, void *stream);
+
+/*
+ * fem_recur_bwd -- its gradients, from the forward's own outputs h:
+ *
+ *   m_t = exp(-s_t) (dh_t + m_{t+1}),  m after the last step = dh_last,
+ *   ds_t = -m_t h_{t-1} (mean: m_t (u_t - h_{t-1})),  du_t = w(s_t) (dh_t + m_{t+1}),  dh0 = m_first
+ *
+ *   s, u, h, dh, ds, du : device, [N, C] of `type`, strides as above; u is read
+ *                         with mean = 1 only and may be NULL otherwise
+ *   h0, dh_last         : device, float32 [S, C] or NULL (zero)
+ *   dh0                 : device, float32 [S, C] or NULL (not wanted)
+ * The rest as above.
+ */
+int fem_recur_bwd(const void *s, const void *u, const void *h, const void *dh, int64_t s_stride, int64_t u_stride,
+                  int64_t h_stride, int64_t dh_stride, const int *offsets, int S, int T, int N, int C, int type,
+                  int mean, const float *h0, const float *dh_last, void *ds, void *du, int64_t ds_stride,
+                  int64_t du_stride, float *dh0, void *stream);
+
+/*
+ * A block's end and the next one's start, D = H d channels:
+ *
+ *   r = x + scale act(gate) (w_post P(y) + b_post)    the residual stream after the block
+ *   z = w_pre Q(r) + b_pre                            what the next block reads
+ *
+ * P and Q are no norm, v / sqrt(mean v^2 + eps) or (v - mean v) / sqrt(var v + eps),
+ * act nothing, the sigmoid or g sigmoid(g).  Without a norm w_post is a scale of the
+ * branch's channels.
+ */
+typedef enum { FEM_NORM_NONE = 0, FEM_NORM_RMS = 1, FEM_NORM_LAYER = 2 } fem_norm_kind;
+typedef enum { FEM_GATE_IDENTITY = 0, FEM_GATE_SIGMOID = 1, FEM_GATE_SILU = 2 } fem_gate_act;
+typedef struct {
+    int B, T, H, d;         /* N = B T rows of D = H d channels */
+    int x_type, y_type;     /* of x, r, dr, dx; of y, gate, z, dy, dgate, dz (bf16, bf16; f32, bf16; f32, f32) */
+    int post, pre;          /* fem_norm_kind of P and Q; pre NONE: no z */
+    int gate_act;           /* fem_gate_act */
+    float scale, eps;
+    const float *w_post, *b_post, *w_pre, *b_pre; /* device, [D], or NULL: 1 and 0 */
+} fem_norm;
+
+/*
+ * fem_norm_fwd -- r and z.
+ *   x, r    : device, [N, D] contiguous; the same pointer updates the stream in place
+ *   y, gate : device, heads; gate NULL: none.  y NULL: no block before (r = x is
+ *             not written, gate must be NULL)
+ *   z       : device, [N, D] contiguous; NULL if and only if pre is NONE
+ * D up to 16384.  Sums and statistics in fp32; r rounded once, z formed from r
+ * before its rounding.  N = 0 does nothing.  No workspace.
+ */
+int fem_norm_fwd(const fem_norm *norm, const void *x, const fem_heads *y, const fem_heads *gate, void *r, void *z,
+                 void *stream);
+
+/*
+ * fem_norm_bwd -- the gradients, from the saved r, y and gate.
+ *   dr          : device, [N, D] contiguous: what reaches r past the next block, or NULL: nothing
+ *   dz          : device, [N, D] contiguous; NULL if and only if pre is NONE
+ *   dx          : device, [N, D] contiguous; may be dr
+ *   dy, dgate   : device, heads; NULL if and only if y and gate are
+ *   dw_post ... : device, float32 [D], sums over all rows, or NULL: not wanted
+ *                 (dw_post and db_post need y; a pre of NONE has neither dw_pre nor db_pre)
+ * Statistics are formed again from r and y.  N = 0 writes zeros to the weights'
+ * gradients.  The weights' sums over rows are taken in a fixed order: the same
+ * inputs give the same bits.  Workspace from the library's stream-ordered pool.
+ */
+int fem_norm_bwd(const fem_norm *norm, const void *r, const fem_heads *y, const fem_heads *gate, const void *dr,
+                 const void *dz, void *dx, const fem_heads *dy, const fem_heads *dgate, float *dw_post,
+                 float *db_post, float *dw_pre, float *db_pre, void *stream);
+
+/*
  * fem_check_device_error -- synchronises `stream`, then returns FEM_OK, or
  * FEM_ERR_TIMEOUT if any kernel of this library on the current device gave up
  * on a bounded wait since the last check (the word is cleared), or
  * FEM_ERR_INVALID_ARG if none did but a paged-cache call met a slot, page or
- * row range outside its buffers (the word is cleared), or FEM_ERR_CUDA if the
- * synchronisation failed.
+ * row range, or a recurrence an offset or state row, outside its buffers (the
+ * word is cleared), or FEM_ERR_CUDA if the synchronisation failed.
  */
 int fem_check_device_error(void *stream);
 

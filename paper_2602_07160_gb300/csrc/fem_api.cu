@@ -20,6 +20,7 @@
 #include "fem.h"
 #include "fem_chunks.h"
 #include "fem_launch.h"
+#include "fem_layer.cuh"
 #include "fem_paged.cuh"
 #include "fem_paged_split.cuh"
 
@@ -908,6 +909,255 @@ int fem_paged_read(const fem_paged_cache *cache, const void *q, int64_t q_stride
             : launch_paged_token(tk, tv, a, sp, shape, grid, s);
   if (e == cudaSuccess) e = launch_paged_finish(a, sp, shape, grid, s);
   const cudaError_t ef = cudaFreeAsync(ws, s);
+  return map_cuda(e != cudaSuccess ? e : ef);
+}
+
+// --- the operators around the read
+
+static bool known_type(int type) { return type == FEM_BF16 || type == FEM_F32; }
+static bool element_aligned(const void *p, int type) {
+  return (reinterpret_cast<uintptr_t>(p) & (type == FEM_F32 ? 3u : 1u)) == 0;
+}
+
+// An array of heads [B, T, H, d] as the kernels take it.  One that is written has an address for each element.
+static int heads_view(const fem_heads *v, int B, int T, int H, int type, bool written, HeadsView *out) {
+  if (!v || !v->p || !element_aligned(v->p, type) || v->stride_b < 0 || v->stride_t < 0 || v->stride_h < 0)
+    return FEM_ERR_INVALID_ARG;
+  if (written && ((B > 1 && v->stride_b == 0) || (T > 1 && v->stride_t == 0) || (H > 1 && v->stride_h == 0)))
+    return FEM_ERR_INVALID_ARG;
+  *out = {v->p, v->stride_b, v->stride_t, v->stride_h};
+  return FEM_OK;
+}
+
+int fem_rope_turns(int rotary, double base, int scaling, double factor, double context, double low, double high,
+                   uint64_t *turns) {
+  if (!turns || rotary < 2 || rotary > 1024 || rotary % 2 || !(base > 0) || std::isinf(base)) return FEM_ERR_INVALID_ARG;
+  if (scaling < FEM_ROPE_PLAIN || scaling > FEM_ROPE_PARTS) return FEM_ERR_INVALID_ARG;
+  if (scaling != FEM_ROPE_PLAIN && (!(factor > 0) || std::isinf(factor))) return FEM_ERR_INVALID_ARG;
+  if (scaling == FEM_ROPE_PARTS && (!(context > 0) || std::isinf(context) || !(low < high) || std::isinf(low) || std::isinf(high)))
+    return FEM_ERR_INVALID_ARG;
+  const double two_pi = 6.283185307179586476925;
+  // one pair has the rate 1 whatever the base
+  if (scaling == FEM_ROPE_BASE && rotary > 2) base *= std::pow(factor, static_cast<double>(rotary) / (rotary - 2));
+  for (int i = 0; i < rotary / 2; ++i) {
+    double theta = std::pow(base, -2.0 * i / rotary);
+    if (scaling == FEM_ROPE_LINEAR) theta /= factor;
+    if (scaling == FEM_ROPE_PARTS) {
+      const double g = std::min(1.0, std::max(0.0, (context * theta / two_pi - low) / (high - low)));
+      theta = g * theta + (1.0 - g) * theta / factor;
+    }
+    const double turn = theta / two_pi;
+    if (!std::isfinite(turn)) return FEM_ERR_INVALID_ARG;
+    // of a turn of 2^64; a fraction of a double has at most 53 bits, so that the scaled one stays under 2^64
+    turns[i] = static_cast<uint64_t>(std::ldexp(turn - std::floor(turn), 64));
+  }
+  return FEM_OK;
+}
+
+int fem_rope(const fem_heads *q, const fem_heads *q_out, int Hq, const fem_heads *k, const fem_heads *k_out, int Hk,
+             int B, int T, int d, int type, const uint64_t *turns, int rotary, int interleaved, float amplitude,
+             const int *positions, int inverse, void *stream) {
+  if (B < 0 || T < 0 || Hq <= 0 || d <= 0 || !known_type(type)) return FEM_ERR_INVALID_ARG;
+  if (rotary < 2 || rotary % 2 || rotary > d || (k && Hk <= 0)) return FEM_ERR_INVALID_ARG;
+  if ((interleaved != 0 && interleaved != 1) || (inverse != 0 && inverse != 1)) return FEM_ERR_INVALID_ARG;
+  if (!turns || (reinterpret_cast<uintptr_t>(turns) & 7u) || (reinterpret_cast<uintptr_t>(positions) & 3u)) return FEM_ERR_INVALID_ARG;
+  if (d > 1024) return FEM_ERR_UNSUPPORTED;
+  if (static_cast<long long>(B) * T >= (1ll << 31) - 256 || static_cast<long long>(Hq) + (k ? Hk : 0) >= (1ll << 30))
+    return FEM_ERR_UNSUPPORTED;
+  if (B == 0 || T == 0) return FEM_OK;
+  RopeArgs a = {};
+  int rc;
+  if ((rc = heads_view(q, B, T, Hq, type, false, &a.in[0])) != FEM_OK) return rc;
+  if ((rc = heads_view(q_out, B, T, Hq, type, true, &a.out[0])) != FEM_OK) return rc;
+  a.heads[0] = Hq;
+  if (k) {
+    if ((rc = heads_view(k, B, T, Hk, type, false, &a.in[1])) != FEM_OK) return rc;
+    if ((rc = heads_view(k_out, B, T, Hk, type, true, &a.out[1])) != FEM_OK) return rc;
+    a.heads[1] = Hk;
+  }
+  a.B = B;
+  a.T = T;
+  a.d = d;
+  a.rotary = rotary;
+  a.turns = reinterpret_cast<const unsigned long long *>(turns);
+  a.pos = positions;
+  a.amplitude = amplitude;
+  a.inverse = inverse;
+  return map_cuda(launch_rope(a, type, interleaved != 0, static_cast<cudaStream_t>(stream)));
+}
+
+// What both passes of the recurrence check; rows and states are wanted.
+static int recur_common(RecurArgs &a, const int *offsets, int S, int T, int N, int C, int type, int mean) {
+  if (S < 0 || T < 0 || N < 0 || C <= 0 || !known_type(type) || (mean != 0 && mean != 1)) return FEM_ERR_INVALID_ARG;
+  if (!offsets && static_cast<long long>(S) * T != N) return FEM_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(offsets) & 3u) return FEM_ERR_INVALID_ARG;
+  if (static_cast<long long>(S) * ((C + 31) / 32) >= (1ll << 27)) return FEM_ERR_UNSUPPORTED;
+  a.offsets = offsets;
+  a.S = S;
+  a.T = T;
+  a.N = N;
+  a.C = C;
+  return FEM_OK;
+}
+// A [N, C] array: rows `stride` elements apart, further than a row is long where it is written.
+static bool rows_ok(const void *p, int64_t stride, int N, int C, int type, bool written) {
+  if (N == 0) return true;
+  return p && element_aligned(p, type) && stride >= 0 && (!written || N == 1 || stride >= C);
+}
+
+int fem_recur_fwd(const void *s, const void *u, int64_t s_stride, int64_t u_stride, const int *offsets, int S, int T,
+                  int N, int C, int type, int mean, const float *h0, float *h_last, const int *state_rows,
+                  int num_states, void *h, int64_t h_stride, void *stream) {
+  RecurArgs a = {};
+  int rc = recur_common(a, offsets, S, T, N, C, type, mean);
+  if (rc != FEM_OK) return rc;
+  if (!rows_ok(s, s_stride, N, C, type, false) || !rows_ok(u, u_stride, N, C, type, false) ||
+      !rows_ok(h, h_stride, N, C, type, true))
+    return FEM_ERR_INVALID_ARG;
+  for (const void *p : {static_cast<const void *>(h0), static_cast<const void *>(h_last), static_cast<const void *>(state_rows)})
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return FEM_ERR_INVALID_ARG;
+  if ((h0 || h_last) && (num_states < 0 || (!state_rows && num_states < S))) return FEM_ERR_INVALID_ARG;
+  if (S == 0) return FEM_OK;
+  DeviceState *ds = nullptr;
+  if ((rc = device_state(&ds)) != FEM_OK) return rc;
+  a.s = s;
+  a.u = u;
+  a.s_st = s_stride;
+  a.u_st = u_stride;
+  a.out = h;
+  a.out_st = h_stride;
+  a.state_rows = h0 || h_last ? state_rows : nullptr;
+  a.num_states = num_states;
+  a.first = h0;
+  a.last = h_last;
+  a.err = ds->err;
+  return map_cuda(launch_recur_fwd(a, type, mean != 0, ds->num_sms, static_cast<cudaStream_t>(stream)));
+}
+
+int fem_recur_bwd(const void *s, const void *u, const void *h, const void *dh, int64_t s_stride, int64_t u_stride,
+                  int64_t h_stride, int64_t dh_stride, const int *offsets, int S, int T, int N, int C, int type,
+                  int mean, const float *h0, const float *dh_last, void *ds_out, void *du, int64_t ds_stride,
+                  int64_t du_stride, float *dh0, void *stream) {
+  RecurArgs a = {};
+  int rc = recur_common(a, offsets, S, T, N, C, type, mean);
+  if (rc != FEM_OK) return rc;
+  if (!rows_ok(s, s_stride, N, C, type, false) || (mean && !rows_ok(u, u_stride, N, C, type, false)) ||
+      !rows_ok(h, h_stride, N, C, type, false) || !rows_ok(dh, dh_stride, N, C, type, false) ||
+      !rows_ok(ds_out, ds_stride, N, C, type, true) || !rows_ok(du, du_stride, N, C, type, true))
+    return FEM_ERR_INVALID_ARG;
+  for (const void *p : {static_cast<const void *>(h0), static_cast<const void *>(dh_last), static_cast<const void *>(dh0)})
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return FEM_ERR_INVALID_ARG;
+  if (S == 0) return FEM_OK;
+  DeviceState *ds = nullptr;
+  if ((rc = device_state(&ds)) != FEM_OK) return rc;
+  a.s = s;
+  a.u = mean ? u : nullptr;
+  a.h = h;
+  a.dh = dh;
+  a.s_st = s_stride;
+  a.u_st = u_stride;
+  a.h_st = h_stride;
+  a.dh_st = dh_stride;
+  a.out = ds_out;
+  a.out_st = ds_stride;
+  a.du = du;
+  a.du_st = du_stride;
+  a.num_states = S;
+  a.first = dh_last;
+  a.last = dh0;
+  a.h0 = h0;
+  a.err = ds->err;
+  return map_cuda(launch_recur_bwd(a, type, mean != 0, ds->num_sms, static_cast<cudaStream_t>(stream)));
+}
+
+// What both passes of the norms check; `back`: the gradients' arrays are looked at as well.
+static int norm_common(NormArgs &a, const fem_norm *n, const void *x, const fem_heads *y, const fem_heads *gate) {
+  if (!n || n->B < 0 || n->T < 0 || n->H <= 0 || n->d <= 0 || !known_type(n->x_type) || !known_type(n->y_type))
+    return FEM_ERR_INVALID_ARG;
+  if (n->x_type == FEM_BF16 && n->y_type == FEM_F32) return FEM_ERR_UNSUPPORTED;
+  for (int kind : {n->post, n->pre})
+    if (kind < FEM_NORM_NONE || kind > FEM_NORM_LAYER) return FEM_ERR_INVALID_ARG;
+  if (n->gate_act < FEM_GATE_IDENTITY || n->gate_act > FEM_GATE_SILU) return FEM_ERR_INVALID_ARG;
+  if (!(n->eps > 0.f) || std::isinf(n->eps) || !std::isfinite(n->scale)) return FEM_ERR_INVALID_ARG;
+  if ((gate && !y) || (!y && n->pre == FEM_NORM_NONE)) return FEM_ERR_INVALID_ARG;
+  for (const void *p : {static_cast<const void *>(n->w_post), static_cast<const void *>(n->b_post),
+                        static_cast<const void *>(n->w_pre), static_cast<const void *>(n->b_pre)})
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return FEM_ERR_INVALID_ARG;
+  if (static_cast<long long>(n->H) * n->d > 16384) return FEM_ERR_UNSUPPORTED;
+  if (static_cast<long long>(n->B) * n->T >= (1ll << 31) - 256) return FEM_ERR_UNSUPPORTED;
+  a.B = n->B;
+  a.T = n->T;
+  a.H = n->H;
+  a.d = n->d;
+  a.N = n->B * n->T;
+  a.D = n->H * n->d;
+  a.post = n->post;
+  a.pre = n->pre;
+  a.act = n->gate_act;
+  a.scale = n->scale;
+  a.eps = n->eps;
+  a.w_post = n->w_post;
+  a.b_post = n->b_post;
+  a.w_pre = n->w_pre;
+  a.b_pre = n->b_pre;
+  if (a.N == 0) return FEM_OK;
+  if (!x || !element_aligned(x, n->x_type)) return FEM_ERR_INVALID_ARG;
+  a.x = x;
+  int rc;
+  if (y && (rc = heads_view(y, a.B, a.T, a.H, n->y_type, false, &a.y)) != FEM_OK) return rc;
+  if (gate && (rc = heads_view(gate, a.B, a.T, a.H, n->y_type, false, &a.gate)) != FEM_OK) return rc;
+  return FEM_OK;
+}
+
+int fem_norm_fwd(const fem_norm *norm, const void *x, const fem_heads *y, const fem_heads *gate, void *r, void *z,
+                 void *stream) {
+  NormArgs a = {};
+  int rc = norm_common(a, norm, x, y, gate);
+  if (rc != FEM_OK) return rc;
+  if (a.N == 0) return FEM_OK;
+  if ((y && (!r || !element_aligned(r, norm->x_type))) || (a.pre != 0) != (z != nullptr) || !element_aligned(z, norm->y_type))
+    return FEM_ERR_INVALID_ARG;
+  a.r = y ? r : nullptr;
+  a.z = z;
+  DeviceState *ds = nullptr;
+  if ((rc = device_state(&ds)) != FEM_OK) return rc;
+  return map_cuda(launch_norm_fwd(a, norm->x_type, norm->y_type, ds->num_sms, static_cast<cudaStream_t>(stream)));
+}
+
+int fem_norm_bwd(const fem_norm *norm, const void *r, const fem_heads *y, const fem_heads *gate, const void *dr,
+                 const void *dz, void *dx, const fem_heads *dy, const fem_heads *dgate, float *dw_post,
+                 float *db_post, float *dw_pre, float *db_pre, void *stream) {
+  NormArgs a = {};
+  int rc = norm_common(a, norm, r, y, gate);
+  if (rc != FEM_OK) return rc;
+  float *sums[4] = {dw_post, db_post, dw_pre, db_pre};
+  for (int i = 0; i < 4; ++i) {
+    if (reinterpret_cast<uintptr_t>(sums[i]) & 3u) return FEM_ERR_INVALID_ARG;
+    if (sums[i] && (i < 2 ? !y : a.pre == 0)) return FEM_ERR_INVALID_ARG;
+    a.dw[i] = sums[i];
+  }
+  if ((y != nullptr) != (dy != nullptr) || (gate != nullptr) != (dgate != nullptr)) return FEM_ERR_INVALID_ARG;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (a.N == 0) {
+    for (float *p : sums)
+      if (p)
+        if (cudaError_t e = cudaMemsetAsync(p, 0, static_cast<size_t>(a.D) * sizeof(float), s); e != cudaSuccess) return map_cuda(e);
+    return FEM_OK;
+  }
+  if (!dx || !element_aligned(dx, norm->x_type) || !element_aligned(dr, norm->x_type)) return FEM_ERR_INVALID_ARG;
+  if ((a.pre != 0) != (dz != nullptr) || !element_aligned(dz, norm->y_type)) return FEM_ERR_INVALID_ARG;
+  if (dy && (rc = heads_view(dy, a.B, a.T, a.H, norm->y_type, true, &a.dy)) != FEM_OK) return rc;
+  if (dgate && (rc = heads_view(dgate, a.B, a.T, a.H, norm->y_type, true, &a.dgate)) != FEM_OK) return rc;
+  a.dr = dr;
+  a.dz = dz;
+  a.dx = dx;
+  DeviceState *ds = nullptr;
+  if ((rc = device_state(&ds)) != FEM_OK) return rc;
+  const size_t bytes = static_cast<size_t>(norm_bwd_blocks(a.N, a.D, ds->num_sms)) * 4 * a.D * sizeof(float);
+  cudaError_t e = ws_alloc(ds, reinterpret_cast<void **>(&a.part), bytes, s);
+  if (e != cudaSuccess) return map_cuda(e);
+  e = launch_norm_bwd(a, norm->x_type, norm->y_type, ds->num_sms, s);
+  const cudaError_t ef = cudaFreeAsync(a.part, s);
   return map_cuda(e != cudaSuccess ? e : ef);
 }
 

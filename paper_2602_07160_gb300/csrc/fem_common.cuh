@@ -72,7 +72,8 @@ constexpr unsigned kErrWaitTma = 1u;
 constexpr unsigned kErrWaitMma = 2u;
 constexpr unsigned kErrTmemAlloc = 4u;
 constexpr unsigned kErrWaitProbe = 8u;  // the diagnostic wait probe gave up (fem_probe_wait_timeout)
-// a slot, page or row range of a paged cache call points outside its buffers (the access was left out)
+// a slot, page or row range of a paged cache call, or an offset or state row of a recurrence, points outside its
+// buffers (the access was left out)
 constexpr unsigned kErrPageRange = 16u;
 
 constexpr unsigned long long kWaitLimitNs = 1000000000ull;  // 1 s per wait

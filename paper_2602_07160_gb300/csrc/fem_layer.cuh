@@ -1,0 +1,118 @@
+// Shared by the operators around the read (rotary positions, the gated recurrence, norms with gate and residual):
+// their arguments as the kernels take them, and rows in pieces of eight elements.
+#pragma once
+
+#include "fem_common.cuh"
+
+namespace fem {
+
+constexpr int kTypeBf16 = 0, kTypeF32 = 2;  // fem_type
+
+// Element (b, t, h, j) of [B, T, H, d] at p + b sb + t st + h sh + j.
+struct HeadsView {
+  void *p;
+  long long sb, st, sh;
+};
+
+struct RopeArgs {
+  HeadsView in[2], out[2];  // queries, keys
+  int heads[2];             // heads[1] = 0: no keys
+  int B, T, d, rotary;
+  const unsigned long long *turns;
+  const int *pos;
+  float amplitude;
+  int inverse;
+};
+cudaError_t launch_rope(const RopeArgs &a, int type, bool interleaved, cudaStream_t stream);
+
+struct RecurArgs {
+  const void *s, *u, *h, *dh;  // h is read by the backward pass only
+  long long s_st, u_st, h_st, dh_st;
+  void *out, *du;  // h, or ds and du
+  long long out_st, du_st;
+  const int *offsets, *state_rows;
+  int S, T, N, C, num_states;
+  const float *first;  // h0, or dh_last: the state that a scan starts from
+  float *last;         // h_last, or dh0
+  const float *h0;     // backward: what precedes h at a sequence's first step
+  unsigned *err;
+};
+cudaError_t launch_recur_fwd(const RecurArgs &a, int type, bool mean, int num_sms, cudaStream_t stream);
+cudaError_t launch_recur_bwd(const RecurArgs &a, int type, bool mean, int num_sms, cudaStream_t stream);
+
+struct NormArgs {
+  int B, T, H, d, N, D;
+  int post, pre, act;  // fem_norm_kind; act -1: no gate
+  float scale, eps;
+  const float *w_post, *b_post, *w_pre, *b_pre;
+  const void *x;       // forward: x; backward: r
+  HeadsView y, gate;   // y.p NULL: no block before
+  void *r, *z;         // forward's outputs
+  const void *dr, *dz;
+  void *dx;
+  HeadsView dy, dgate;
+  float *dw[4];        // dw_post, db_post, dw_pre, db_pre, or NULL
+  float *part;         // [norm_bwd_blocks, sums wanted, D]
+};
+cudaError_t launch_norm_fwd(const NormArgs &a, int x_type, int y_type, int num_sms, cudaStream_t stream);
+// Blocks of the backward kernel, each of which leaves a row of partial sums of the weights' gradients.
+int norm_bwd_blocks(int N, int D, int num_sms);
+cudaError_t launch_norm_bwd(const NormArgs &a, int x_type, int y_type, int num_sms, cudaStream_t stream);
+
+// ---------------------------------------------------------------------------
+// Eight elements of a row as they lie in memory, and in fp32.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ uint32_t bf16_pack(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+template <typename T>
+struct Eight;
+template <>
+struct Eight<__nv_bfloat16> {
+  uint4 a;
+  __device__ __forceinline__ void load(const __nv_bfloat16 *p) { a = __ldcs(reinterpret_cast<const uint4 *>(p)); }
+  __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *reinterpret_cast<uint4 *>(p) = a; }
+  __device__ __forceinline__ void zero() { a = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    f[0] = bf16_lo(a.x), f[1] = bf16_hi(a.x), f[2] = bf16_lo(a.y), f[3] = bf16_hi(a.y);
+    f[4] = bf16_lo(a.z), f[5] = bf16_hi(a.z), f[6] = bf16_lo(a.w), f[7] = bf16_hi(a.w);
+  }
+  __device__ __forceinline__ void put(const float (&f)[8]) {
+    a = make_uint4(bf16_pack(f[0], f[1]), bf16_pack(f[2], f[3]), bf16_pack(f[4], f[5]), bf16_pack(f[6], f[7]));
+  }
+};
+template <>
+struct Eight<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float *p) {
+    a = __ldcs(reinterpret_cast<const float4 *>(p));
+    b = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
+  }
+  __device__ __forceinline__ void store(float *p) const {
+    *reinterpret_cast<float4 *>(p) = a;
+    *(reinterpret_cast<float4 *>(p) + 1) = b;
+  }
+  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+  }
+  __device__ __forceinline__ void put(const float (&f)[8]) {
+    a = make_float4(f[0], f[1], f[2], f[3]);
+    b = make_float4(f[4], f[5], f[6], f[7]);
+  }
+};
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T>
+__device__ __forceinline__ T from_f32(float x);
+template <>
+__device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+}  // namespace fem

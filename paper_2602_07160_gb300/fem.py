@@ -25,7 +25,7 @@ EXPORTS = ["fem_fwd", "fem_fwd_ws", "fem_fwd_workspace_bytes", "fem_fwd_f32", "f
            "fem_check_device_error", "fem_last_fixup_rows", "fem_set_kernel_events", "fem_status_str",
            "fem_fwd_noalloc", "fem_fwd_gated", "fem_decode", "fem_gla_fwd", "fem_tdc_conv", "fem_bwd_f32",
            "fem_probe_wait_timeout", "fem_attn_fwd", "fem_gla_fwd_tc", "fem_cache_write", "fem_cache_gather",
-           "fem_paged_read"]
+           "fem_paged_read", "fem_rope_turns", "fem_rope", "fem_recur_fwd", "fem_recur_bwd", "fem_norm_fwd", "fem_norm_bwd"]
 
 
 class FemError(RuntimeError):
@@ -75,6 +75,19 @@ def load(path: str | None = None):
         lib.fem_cache_gather.restype = i
         lib.fem_paged_read.argtypes = [vp, vp, i64, i64, vp, vp, vp, vp, i, i, i, i, i, i, vp, vp, vp]
         lib.fem_paged_read.restype = i
+        f32, f64 = ctypes.c_float, ctypes.c_double
+        lib.fem_rope_turns.argtypes = [i, f64, i, f64, f64, f64, f64, vp]
+        lib.fem_rope_turns.restype = i
+        lib.fem_rope.argtypes = [vp, vp, i, vp, vp, i, i, i, i, i, vp, i, i, f32, vp, i, vp]
+        lib.fem_rope.restype = i
+        lib.fem_recur_fwd.argtypes = [vp, vp, i64, i64, vp, i, i, i, i, i, i, vp, vp, vp, i, vp, i64, vp]
+        lib.fem_recur_fwd.restype = i
+        lib.fem_recur_bwd.argtypes = [vp] * 4 + [i64] * 4 + [vp] + [i] * 6 + [vp] * 4 + [i64] * 2 + [vp] * 2
+        lib.fem_recur_bwd.restype = i
+        lib.fem_norm_fwd.argtypes = [vp] * 7
+        lib.fem_norm_fwd.restype = i
+        lib.fem_norm_bwd.argtypes = [vp] * 14
+        lib.fem_norm_bwd.restype = i
         lib.fem_fwd_workspace_bytes.argtypes = [i, i, i, i, i]
         lib.fem_fwd_workspace_bytes.restype = sz
         lib.fem_check_device_error.argtypes = [vp]
@@ -505,6 +518,367 @@ def fem_paged_read(q, cache: PagedCache, beta, q_offsets, ctx_lens, block_table,
     return out, (None if lse is False else lse)
 
 
+class _Heads(ctypes.Structure):
+    """fem_heads of include/fem.h."""
+    _fields_ = [("p", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_t", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
+
+
+_TYPES = {torch.bfloat16: 0, torch.float32: 2}  # fem_type
+
+
+def _current(index):
+    """The library launches on the current device, where its error word and workspaces are."""
+    if index < 0 or torch.cuda.current_device() != index:
+        raise ValueError("the tensors' device must be a CUDA device and the current one")
+
+
+def _stream_number(stream, index):
+    return torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+
+
+def _optional(name, t, shape, dtype, index):
+    """Address of a contiguous tensor that may be absent."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on the other tensors' device")
+    return t.data_ptr()
+
+
+def _heads(name, t, dtype, index):
+    """[N, H, d] or [B, H, T, d] as fem_heads, with (B, T, H, d)."""
+    if t.dtype is not dtype or t.get_device() != index:
+        raise ValueError(f"{name} must be {dtype} on the other tensors' device")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}'s last axis must be contiguous")
+    if t.dim() == 3:
+        (n, h, d), (sn, sh, _) = t.shape, t.stride()
+        return _Heads(t.data_ptr(), 0, sn, sh), (1, n, h, d)
+    (b, h, n, d), (sb, sh, sn, _) = t.shape, t.stride()
+    return _Heads(t.data_ptr(), sb, sn, sh), (b, n, h, d)
+
+
+class Rope:
+    """The rates of rotary positions, for ``fem_rope``: of every head the first ``rotary_dim`` elements turn in pairs,
+    elements i and i + rotary_dim/2, or 2 i and 2 i + 1 where ``interleaved``, by pos * base^(-2 i / rotary_dim).
+
+    ``scaling`` stretches the rates for contexts ``factor`` times as long: "linear" all of them, "base" by a larger
+    base, "parts" those that turn less than ``low`` times over ``context`` positions, those that turn more than
+    ``high`` times not, and those between in part.  ``amplitude`` multiplies the rotated part.  The table lives on
+    ``device``."""
+
+    SCALINGS = {None: 0, "linear": 1, "base": 2, "parts": 3}
+
+    def __init__(self, rotary_dim: int, base: float = 10000.0, interleaved: bool = False, scaling=None, factor: float = 1.0,
+                 context: float = 4096.0, low: float = 1.0, high: float = 32.0, amplitude: float = 1.0, device="cuda"):
+        if scaling not in self.SCALINGS:
+            raise ValueError(f"scaling must be one of {list(self.SCALINGS)}")
+        table = (ctypes.c_uint64 * max(1, rotary_dim // 2))()
+        rc = load().fem_rope_turns(rotary_dim, base, self.SCALINGS[scaling], factor, context, low, high, table)
+        if rc != 0:
+            raise FemError("fem_rope_turns", rc)
+        signed = [v - (1 << 64) if v >> 63 else v for v in table]
+        self.turns = torch.tensor(signed, dtype=torch.int64).to(device)
+        self.rotary_dim, self.interleaved, self.amplitude = rotary_dim, bool(interleaved), float(amplitude)
+
+
+def fem_rope(rope: Rope, q, k=None, positions=None, inverse: bool = False, out=None, stream=None):
+    """Rotary positions of queries and keys, [N, heads, d] or [B, heads, T, d] of bf16 or float32 (k may be None).
+
+    positions: int32 [N] or [B, T]; None counts from 0 along N or T.  ``inverse`` turns back, which takes the outputs'
+    gradients to the inputs'.  Strided views are taken as they are.  ``out``: the pair of output tensors, which may be
+    (q, k) themselves.  Returns (q, k)."""
+    if q.dim() not in (3, 4) or (k is not None and k.dim() != q.dim()):
+        raise ValueError("q and k must both be [N, heads, d] or [B, heads, T, d]")
+    if q.dtype not in _TYPES:
+        raise ValueError(f"q has dtype {q.dtype}")
+    index = q.get_device()
+    _current(index)
+    if rope.turns.get_device() != index:
+        raise ValueError("the rope's table must be on q's device")
+    qv, (B, T, Hq, d) = _heads("q", q, q.dtype, index)
+    pos = _optional("positions", positions, (T,) if q.dim() == 3 else (B, T), torch.int32, index)
+    q_out, k_out = out if out is not None else (None, None)
+    if q_out is None:
+        q_out = _output(q.shape, q.dtype, q, stream)
+    elif q_out.shape != q.shape:
+        raise ValueError("out must have the inputs' shapes")
+    qo, _ = _heads("out", q_out, q.dtype, index)
+    kv = ko = None
+    Hk = 0
+    if k is not None:
+        kv, (Bk, Tk, Hk, dk) = _heads("k", k, q.dtype, index)
+        if (Bk, Tk, dk) != (B, T, d):
+            raise ValueError("q and k must have the same tokens and d")
+        if k_out is None:
+            k_out = _output(k.shape, k.dtype, k, stream)
+        elif k_out.shape != k.shape:
+            raise ValueError("out must have the inputs' shapes")
+        ko, _ = _heads("out", k_out, q.dtype, index)
+        kv, ko = ctypes.byref(kv), ctypes.byref(ko)
+    elif k_out is not None:
+        raise ValueError("out has keys and the call none")
+    rc = load().fem_rope(ctypes.byref(qv), ctypes.byref(qo), Hq, kv, ko, Hk, B, T, d, _TYPES[q.dtype],
+                         rope.turns.data_ptr(), rope.rotary_dim, int(rope.interleaved), rope.amplitude, pos,
+                         int(bool(inverse)), _stream_number(stream, index))
+    if rc != 0:
+        raise FemError("fem_rope", rc)
+    return q_out, (None if k is None else k_out)
+
+
+def _recur_rows(name, t, like, packed):
+    """Address and row stride of a [N, C] (packed) or [B, T, C] tensor shaped like `like`."""
+    if t.shape != like.shape or t.dtype is not like.dtype or t.get_device() != like.get_device():
+        raise ValueError(f"{name} must have s's shape, type and device")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}'s last axis must be contiguous")
+    if packed:
+        return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    B, T, C = t.shape
+    row = t.stride(1) if T > 1 else t.stride(0) if B > 1 else C
+    if B > 1 and T > 1 and t.stride(0) != T * row:
+        raise ValueError(f"{name}'s rows must be evenly spaced over batch and time")
+    return t.data_ptr(), row
+
+
+def _recur_sizes(s, offsets, max_len):
+    """(address of the offsets, S, T, N, C) of a call; checks s and the offsets."""
+    if s.dim() != (3 if offsets is None else 2):
+        raise ValueError("s must be [B, T, C], or [N, C] with offsets")
+    if s.dtype not in _TYPES:
+        raise ValueError(f"s has dtype {s.dtype}")
+    index = s.get_device()
+    _current(index)
+    if offsets is None:
+        B, T, C = s.shape
+        return None, B, T, B * T, C
+    if offsets.dim() != 1 or offsets.shape[0] < 1:
+        raise ValueError("offsets must be int32 [S + 1]")
+    S, (N, C) = offsets.shape[0] - 1, s.shape
+    return _optional("offsets", offsets, (S + 1,), torch.int32, index), S, N if max_len is None else int(max_len), N, C
+
+
+def fem_recur_fwd(s, u, offsets=None, max_len=None, h0=None, state_rows=None, mean: bool = False, out=None,
+                  state_out=None, stream=None):
+    """The gated linear recurrence h_t = exp(-s_t) h_{t-1} + w(s_t) u_t of every channel, w = 1, or 1 - exp(-s_t)
+    where ``mean``, on bf16 or float32 CUDA tensors.
+
+    s, u: [B, T, C], or packed [N, C] with offsets int32 [S + 1] (``max_len`` bounds their lengths); s >= 0.
+    h0: float32 states before the first step, [S, C], or [num_states, C] with state_rows int32 [S] (negative: none).
+    state_out: where the states after the last step go, shaped like h0: None allocates [S, C], or with state_rows
+    updates h0 in place; False skips them.  Returns (h, states)."""
+    off, S, T, N, C = _recur_sizes(s, offsets, max_len)
+    index, packed = s.get_device(), offsets is not None
+    if state_out is None and state_rows is not None and h0 is not None:
+        state_out = h0
+    states = [t for t in (h0, state_out) if t is not None and t is not False]
+    if any(t.dim() != 2 or t.shape != states[0].shape for t in states):
+        raise ValueError("h0 and state_out must share the shape [num_states, C]")
+    if state_rows is not None and not states:
+        raise ValueError("state_rows goes with h0 or state_out")
+    num = states[0].shape[0] if states else S
+    if state_rows is None and num != S:
+        raise ValueError("h0 and state_out must have a row for each sequence, or state_rows")
+    h0_ptr = _optional("h0", h0, (num, C), torch.float32, index)
+    rows_ptr = _optional("state_rows", state_rows, (S,), torch.int32, index)
+    s_ptr, s_st = _recur_rows("s", s, s, packed)
+    u_ptr, u_st = _recur_rows("u", u, s, packed)
+    if out is None:
+        out = _output(s.shape, s.dtype, s, stream)
+    h_ptr, h_st = _recur_rows("out", out, s, packed)
+    if state_out is None:
+        state_out = _output((S, C), torch.float32, s, stream)
+    last_ptr = None if state_out is False else _optional("state_out", state_out, (num, C), torch.float32, index)
+    rc = load().fem_recur_fwd(s_ptr, u_ptr, s_st, u_st, off, S, T, N, C, _TYPES[s.dtype], int(bool(mean)), h0_ptr, last_ptr,
+                              rows_ptr, num, h_ptr, h_st, _stream_number(stream, index))
+    if rc != 0:
+        raise FemError("fem_recur_fwd", rc)
+    return out, (None if state_out is False else state_out)
+
+
+def fem_recur_bwd(s, u, h, dh, offsets=None, max_len=None, h0=None, dstate=None, mean: bool = False, stream=None):
+    """Gradients of ``fem_recur_fwd`` from its outputs h and their cotangents dh, and the last states' dstate
+    (float32 [S, C] or None).  h0: float32 [S, C] or None, as the forward had it.  u is read where ``mean`` only.
+
+    Returns (ds, du, dh0), dh0 None where h0 is."""
+    off, S, T, N, C = _recur_sizes(s, offsets, max_len)
+    index, packed = s.get_device(), offsets is not None
+    ins = [_recur_rows(name, t, s, packed) for name, t in (("s", s), ("u", u), ("h", h), ("dh", dh))]
+    ds, du = _output(s.shape, s.dtype, s, stream), _output(s.shape, s.dtype, s, stream)
+    dh0 = None if h0 is None else _output((S, C), torch.float32, s, stream)
+    rc = load().fem_recur_bwd(*(p for p, _ in ins), *(st for _, st in ins), off, S, T, N, C, _TYPES[s.dtype], int(bool(mean)),
+                              _optional("h0", h0, (S, C), torch.float32, index),
+                              _optional("dstate", dstate, (S, C), torch.float32, index), ds.data_ptr(), du.data_ptr(), C, C,
+                              None if dh0 is None else dh0.data_ptr(), _stream_number(stream, index))
+    if rc != 0:
+        raise FemError("fem_recur_bwd", rc)
+    return ds, du, dh0
+
+
+class _NormStruct(ctypes.Structure):
+    """fem_norm of include/fem.h."""
+    _fields_ = [(n, ctypes.c_int) for n in ("B", "T", "H", "d", "x_type", "y_type", "post", "pre", "gate_act")] + \
+               [("scale", ctypes.c_float), ("eps", ctypes.c_float)] + \
+               [(n, ctypes.c_void_p) for n in ("w_post", "b_post", "w_pre", "b_pre")]
+
+
+class BlockNorm:
+    """A block's end and the next one's start, for ``fem_norm_fwd`` and ``fem_norm_bwd``:
+
+        r = x + scale act(gate) (w_post P(y) + b_post),    z = w_pre Q(r) + b_pre
+
+    ``post`` and ``pre`` name P and Q: "none", "rms" or "layer" (``pre`` "none": there is no z); ``gate`` the gate's act:
+    "none" (no gate), "identity", "sigmoid" or "silu".  The weights are float32 [width] CUDA tensors or None (1 and 0); the object
+    keeps them and reads them at each call."""
+
+    KINDS = {"none": 0, "rms": 1, "layer": 2}
+    ACTS = {"none": 0, "identity": 0, "sigmoid": 1, "silu": 2}
+
+    def __init__(self, width: int, post: str = "rms", pre: str = "rms", gate: str = "none", w_post=None, b_post=None,
+                 w_pre=None, b_pre=None, scale: float = 1.0, eps: float = 1e-6):
+        if post not in self.KINDS or pre not in self.KINDS or gate not in self.ACTS:
+            raise ValueError(f"post and pre are one of {list(self.KINDS)}, gate one of {list(self.ACTS)}")
+        self.width, self.post, self.pre, self.gate, self.scale, self.eps = width, post, pre, gate, float(scale), float(eps)
+        self.weights = {"w_post": w_post, "b_post": b_post, "w_pre": w_pre, "b_pre": b_pre}
+        self.index = None  # of the weights' device
+        for name, t in self.weights.items():
+            if t is None:
+                continue
+            if t.dtype != torch.float32 or t.shape != (width,) or not t.is_contiguous() or t.device.type != "cuda":
+                raise ValueError(f"{name} must be a contiguous float32 CUDA tensor of shape ({width},)")
+            if self.index not in (None, t.get_device()):
+                raise ValueError("the weights must be on one device")
+            self.index = t.get_device()
+
+    def _struct(self, x, y):
+        """fem_norm for a call on x and y, with its (B, T, H, d) and number of rows."""
+        rows = x.numel() // self.width
+        if y is None or y.shape == x.shape:
+            B, T, H, d = 1, rows, 1, self.width
+        elif y.dim() == 3:
+            B, T, H, d = 1, y.shape[0], y.shape[1], y.shape[2]
+        elif y.dim() == 4:
+            B, T, H, d = y.shape[0], y.shape[2], y.shape[1], y.shape[3]
+        else:
+            raise ValueError("y must have x's shape or be [N, H, d] or [B, H, T, d]")
+        if B * T != rows or H * d != self.width:
+            raise ValueError("y must have x's rows, and heads of its width together")
+        if x.dim() == 3 and y is not None and y.dim() == 4 and (B, T) != tuple(x.shape[:2]):
+            raise ValueError("y [B, H, T, d] must have the B and T of x [B, T, width]")
+        w = self.weights
+        return _NormStruct(B, T, H, d, _TYPES[x.dtype], _TYPES[x.dtype if y is None else y.dtype], self.KINDS[self.post],
+                           self.KINDS[self.pre], self.ACTS[self.gate], self.scale, self.eps,
+                           *(None if w[n] is None else w[n].data_ptr() for n in ("w_post", "b_post", "w_pre", "b_pre")))
+
+
+def _norm_heads(name, t, x, shape, dtype, index):
+    """A branch tensor (x's shape, [N, H, d] or [B, H, T, d]) as fem_heads."""
+    if t.shape != shape:
+        raise ValueError(f"{name} must have the shape {tuple(shape)}")
+    if t.shape != x.shape:
+        return _heads(name, t, dtype, index)[0]
+    if t.dtype is not dtype or t.get_device() != index:
+        raise ValueError(f"{name} must be {dtype} on x's device")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}'s last axis must be contiguous")
+    row, span = None, 1  # rows of all leading axes, evenly spaced
+    for n, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n > 1:
+            if row is not None and st != row * span:
+                raise ValueError(f"{name}'s rows must be evenly spaced")
+            row = st // span if row is None else row
+            span *= n
+    return _Heads(t.data_ptr(), 0, 0 if row is None else row, 0)
+
+
+def _norm_check(norm, x, name):
+    if x.dtype not in _TYPES or x.dim() < 1 or x.shape[-1] != norm.width or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous bf16 or float32 tensor [..., {norm.width}]")
+    index = x.get_device()
+    _current(index)
+    if norm.index not in (None, index):
+        raise ValueError(f"{name} must be on the weights' device")
+    return index
+
+
+def fem_norm_fwd(norm: BlockNorm, x, y=None, gate=None, out=None, z_out=None, stream=None):
+    """The residual stream after a block and what the next block reads (``BlockNorm``), in one pass.
+
+    x: contiguous [..., width], bf16 or float32; y and gate: x's shape, or heads [N, H, d] or [B, H, T, d] (the read's
+    outputs as they are), bf16, or float32 with a float32 x; without y there is no block before and r is x.  ``out`` may
+    be x itself.  Returns (r, z), z of y's type (without y of z_out's, or x's)."""
+    index = _norm_check(norm, x, "x")
+    if (norm.gate != "none") != (gate is not None) and y is not None or (y is None and gate is not None):
+        raise ValueError("gate goes with y and with a norm that has one")
+    if y is not None and y.dtype not in _TYPES:
+        raise ValueError(f"y has dtype {y.dtype}")
+    struct = norm._struct(x, y)
+    z_type = y.dtype if y is not None else x.dtype if z_out is None else z_out.dtype
+    if z_type not in _TYPES:
+        raise ValueError(f"z_out has dtype {z_type}")
+    struct.y_type = _TYPES[z_type]
+    yv = gv = r_ptr = z_ptr = None
+    if y is not None:
+        yv = ctypes.byref(_norm_heads("y", y, x, y.shape, y.dtype, index))
+        if gate is not None:
+            gv = ctypes.byref(_norm_heads("gate", gate, x, y.shape, y.dtype, index))
+        if out is None:
+            out = _output(x.shape, x.dtype, x, stream)
+        r_ptr = _optional("out", out, x.shape, x.dtype, index)
+    elif out is not None:
+        raise ValueError("out goes with y")
+    if norm.pre != "none":
+        if z_out is None:
+            z_out = _output(x.shape, z_type, x, stream)
+        z_ptr = _optional("z_out", z_out, x.shape, z_type, index)
+    elif z_out is not None:
+        raise ValueError("z_out goes with a pre norm")
+    rc = load().fem_norm_fwd(ctypes.byref(struct), x.data_ptr(), yv, gv, r_ptr, z_ptr, _stream_number(stream, index))
+    if rc != 0:
+        raise FemError("fem_norm_fwd", rc)
+    return (x if y is None else out), z_out
+
+
+def fem_norm_bwd(norm: BlockNorm, r, y=None, gate=None, dr=None, dz=None, stream=None):
+    """Gradients of ``fem_norm_fwd`` from its r, y and gate and the cotangents dr (or None) and dz (with a pre norm).
+
+    Returns (dx, dy, dgate, dw_post, db_post, dw_pre, db_pre): dy and dgate of y's shape, contiguous; the weights'
+    float32 [width], summed over all rows; None for what is not there (biases' where the norm has none)."""
+    index = _norm_check(norm, r, "r")
+    if (norm.gate != "none") != (gate is not None) and y is not None or (y is None and gate is not None):
+        raise ValueError("gate goes with y and with a norm that has one")
+    if (norm.pre != "none") != (dz is not None):
+        raise ValueError("dz goes with a pre norm")
+    if y is not None and y.dtype not in _TYPES:
+        raise ValueError(f"y has dtype {y.dtype}")
+    struct = norm._struct(r, y)
+    y_type = y.dtype if y is not None else dz.dtype if dz is not None else r.dtype
+    if y is None:
+        if y_type not in _TYPES:
+            raise ValueError(f"dz has dtype {y_type}")
+        struct.y_type = _TYPES[y_type]
+    dr_ptr = _optional("dr", dr, r.shape, r.dtype, index)
+    dz_ptr = _optional("dz", dz, r.shape, y_type, index)
+    dx = _output(r.shape, r.dtype, r, stream)
+    dy = dgate = yv = gv = dyv = dgv = None
+    if y is not None:
+        yv = ctypes.byref(_norm_heads("y", y, r, y.shape, y_type, index))
+        dy = _output(y.shape, y_type, r, stream)
+        dyv = ctypes.byref(_norm_heads("dy", dy, r, y.shape, y_type, index))
+        if gate is not None:
+            gv = ctypes.byref(_norm_heads("gate", gate, r, y.shape, y_type, index))
+            dgate = _output(y.shape, y_type, r, stream)
+            dgv = ctypes.byref(_norm_heads("dgate", dgate, r, y.shape, y_type, index))
+    wanted = {"w_post": y is not None, "b_post": y is not None and norm.weights["b_post"] is not None,
+              "w_pre": norm.pre != "none", "b_pre": norm.pre != "none" and norm.weights["b_pre"] is not None}
+    sums = [_output((norm.width,), torch.float32, r, stream) if on else None for on in wanted.values()]
+    rc = load().fem_norm_bwd(ctypes.byref(struct), r.data_ptr(), yv, gv, dr_ptr, dz_ptr, dx.data_ptr(), dyv, dgv,
+                             *(None if t is None else t.data_ptr() for t in sums), _stream_number(stream, index))
+    if rc != 0:
+        raise FemError("fem_norm_bwd", rc)
+    return dx, dy, dgate, *sums
+
+
 def probe_wait_timeout(limit_us: int, stream=None, device=None):
     """Enqueue the library's wait probe: a bounded wait on an mbarrier nothing completes,
     which gives up after limit_us microseconds and records a timeout in the error word."""
@@ -515,7 +889,7 @@ def probe_wait_timeout(limit_us: int, stream=None, device=None):
 
 
 def check_device_error(stream=None, device=None):
-    """Synchronise and raise FemError if a kernel gave up on a bounded wait."""
+    """Synchronise and raise FemError if a kernel gave up on a bounded wait or met an index outside its buffers."""
     dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
     rc = load().fem_check_device_error(_stream(stream, dev))
     if rc != 0:
