@@ -999,6 +999,12 @@ static int recur_common(RecurArgs &a, const int *offsets, int S, int T, int N, i
   a.C = C;
   return FEM_OK;
 }
+// The kernels reach a tile of rows by 32-bit offsets.
+static bool strides_long(std::initializer_list<int64_t> strides, int C) {
+  for (int64_t st : strides)
+    if (st >= kRecurMostStride) return true;
+  return C >= kRecurMostStride;
+}
 // A [N, C] array: rows `stride` elements apart, further than a row is long where it is written.
 static bool rows_ok(const void *p, int64_t stride, int N, int C, int type, bool written) {
   if (N == 0) return true;
@@ -1014,6 +1020,7 @@ int fem_recur_fwd(const void *s, const void *u, int64_t s_stride, int64_t u_stri
   if (!rows_ok(s, s_stride, N, C, type, false) || !rows_ok(u, u_stride, N, C, type, false) ||
       !rows_ok(h, h_stride, N, C, type, true))
     return FEM_ERR_INVALID_ARG;
+  if (strides_long({s_stride, u_stride, h_stride}, C)) return FEM_ERR_UNSUPPORTED;
   for (const void *p : {static_cast<const void *>(h0), static_cast<const void *>(h_last), static_cast<const void *>(state_rows)})
     if (reinterpret_cast<uintptr_t>(p) & 3u) return FEM_ERR_INVALID_ARG;
   if ((h0 || h_last) && (num_states < 0 || (!state_rows && num_states < S))) return FEM_ERR_INVALID_ARG;
@@ -1045,6 +1052,7 @@ int fem_recur_bwd(const void *s, const void *u, const void *h, const void *dh, i
       !rows_ok(h, h_stride, N, C, type, false) || !rows_ok(dh, dh_stride, N, C, type, false) ||
       !rows_ok(ds_out, ds_stride, N, C, type, true) || !rows_ok(du, du_stride, N, C, type, true))
     return FEM_ERR_INVALID_ARG;
+  if (strides_long({s_stride, mean ? u_stride : 0, h_stride, dh_stride, ds_stride, du_stride}, C)) return FEM_ERR_UNSUPPORTED;
   for (const void *p : {static_cast<const void *>(h0), static_cast<const void *>(dh_last), static_cast<const void *>(dh0)})
     if (reinterpret_cast<uintptr_t>(p) & 3u) return FEM_ERR_INVALID_ARG;
   if (S == 0) return FEM_OK;

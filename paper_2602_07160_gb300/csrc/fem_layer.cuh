@@ -25,6 +25,7 @@ struct RopeArgs {
 };
 cudaError_t launch_rope(const RopeArgs &a, int type, bool interleaved, cudaStream_t stream);
 
+constexpr long long kRecurMostStride = 1ll << 20;  // elements between rows: a tile of at most 1024 rows stays under 2^32 bytes
 struct RecurArgs {
   const void *s, *u, *h, *dh;  // h is read by the backward pass only
   long long s_st, u_st, h_st, dh_st;
