@@ -1092,7 +1092,7 @@ static int norm_common(NormArgs &a, const fem_norm *n, const void *x, const fem_
                         static_cast<const void *>(n->w_pre), static_cast<const void *>(n->b_pre)})
     if (reinterpret_cast<uintptr_t>(p) & 3u) return FEM_ERR_INVALID_ARG;
   if (static_cast<long long>(n->H) * n->d > 16384) return FEM_ERR_UNSUPPORTED;
-  if (static_cast<long long>(n->B) * n->T >= (1ll << 31) - 256) return FEM_ERR_UNSUPPORTED;
+  if (static_cast<long long>(n->B) * n->T >= (1ll << 31) - (1 << 20)) return FEM_ERR_UNSUPPORTED;  // rows and a step of the grid
   a.B = n->B;
   a.T = n->T;
   a.H = n->H;
@@ -1161,10 +1161,12 @@ int fem_norm_bwd(const fem_norm *norm, const void *r, const fem_heads *y, const 
   a.dx = dx;
   DeviceState *ds = nullptr;
   if ((rc = device_state(&ds)) != FEM_OK) return rc;
-  const size_t bytes = static_cast<size_t>(norm_bwd_blocks(a.N, a.D, ds->num_sms)) * 4 * a.D * sizeof(float);
-  cudaError_t e = ws_alloc(ds, reinterpret_cast<void **>(&a.part), bytes, s);
+  int blocks = 0;
+  cudaError_t e = norm_bwd_blocks(a, norm->x_type, norm->y_type, ds->num_sms, &blocks);
   if (e != cudaSuccess) return map_cuda(e);
-  e = launch_norm_bwd(a, norm->x_type, norm->y_type, ds->num_sms, s);
+  e = ws_alloc(ds, reinterpret_cast<void **>(&a.part), static_cast<size_t>(blocks) * 4 * a.D * sizeof(float), s);
+  if (e != cudaSuccess) return map_cuda(e);
+  e = launch_norm_bwd(a, norm->x_type, norm->y_type, blocks, s);
   const cudaError_t ef = cudaFreeAsync(a.part, s);
   return map_cuda(e != cudaSuccess ? e : ef);
 }

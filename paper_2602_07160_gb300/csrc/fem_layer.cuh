@@ -2,6 +2,8 @@
 // their arguments as the kernels take them, and rows in pieces of eight elements.
 #pragma once
 
+#include <atomic>
+
 #include "fem_common.cuh"
 
 namespace fem {
@@ -53,12 +55,32 @@ struct NormArgs {
   void *dx;
   HeadsView dy, dgate;
   float *dw[4];        // dw_post, db_post, dw_pre, db_pre, or NULL
-  float *part;         // [norm_bwd_blocks, sums wanted, D]
+  float *part;         // [blocks, 4, D] at most
 };
 cudaError_t launch_norm_fwd(const NormArgs &a, int x_type, int y_type, int num_sms, cudaStream_t stream);
-// Blocks of the backward kernel, each of which leaves a row of partial sums of the weights' gradients.
-int norm_bwd_blocks(int N, int D, int num_sms);
-cudaError_t launch_norm_bwd(const NormArgs &a, int x_type, int y_type, int num_sms, cudaStream_t stream);
+// `blocks` of norm_bwd_blocks, each of which leaves a row of partial sums of the weights' gradients.
+cudaError_t norm_bwd_blocks(const NormArgs &a, int x_type, int y_type, int num_sms, int *blocks);
+cudaError_t launch_norm_bwd(const NormArgs &a, int x_type, int y_type, int blocks, cudaStream_t stream);
+
+// Blocks of `kernel` that an SM holds, with `smem` bytes of dynamic shared memory, which it is allowed to have; asked of
+// the driver once for each device and `Tag`, a type of the kernel's own.
+template <typename Tag, typename Kernel>
+cudaError_t resident_blocks(Kernel *kernel, int threads, int smem, int *blocks) {
+  static std::atomic<int> known[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 64 && (*blocks = known[dev].load(std::memory_order_relaxed)) > 0) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(blocks, kernel, threads, smem);
+  if (e == cudaSuccess && *blocks < 1) e = cudaErrorInvalidConfiguration;
+  if (e == cudaSuccess && dev < 64) known[dev].store(*blocks, std::memory_order_relaxed);
+  return e;
+}
+
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
 // ---------------------------------------------------------------------------
 // Eight elements of a row as they lie in memory, and in fp32.

@@ -4,134 +4,182 @@
 // Bound by memory: x, y and the gate are read once, r and z written once.  A row stays in its threads' registers from
 // the first load to the last store; the sums for a norm are a butterfly in each warp and one meeting of a row's warps,
 // and the variance of a layer norm is taken about its mean, which costs a second one but no cancellation.
+#include <algorithm>
+
 #include "fem_norm.cuh"
 
 namespace fem {
 
 namespace {
 
+// Blocks on an SM that registers allow for: 80 a thread, 64 from 512 threads on.
+template <typename S>
+constexpr int kBlocks = S::THREADS > 512 ? 1 : S::THREADS > 256 ? 2 : 768 / S::THREADS;
 template <typename S, typename TX, typename TY>
-__global__ void __launch_bounds__(S::THREADS) norm_fwd_kernel(const NormArgs a) {
+constexpr int kRow = Copied<S, TX>::BYTES + 2 * Copied<S, TY>::BYTES;
+template <typename S, bool BIAS>
+constexpr int kWeights = (BIAS ? 4 : 2) * S::WEIGHT;
+template <typename S, typename TX, typename TY, bool BIAS>
+constexpr int kSmem = rows_smem<S>(kRow<S, TX, TY>, kWeights<S, BIAS>, kBlocks<S>);
+
+template <typename S, typename TX, typename TY, bool BIAS>
+__global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_fwd_kernel(const NormArgs a) {
+  using CX = Copied<S, TX>;
+  using CY = Copied<S, TY>;
+  extern __shared__ __align__(16) char smem[];
   __shared__ float s_red[2 * kRowRed];
   int turn = 0;
   const int lane = threadIdx.x % S::TPR, D = a.D;
+  const Mine<S> mine(lane, D);
   const float inv_d = 1.f / static_cast<float>(D);
-  for (long long row0 = static_cast<long long>(blockIdx.x) * S::ROWS; row0 < a.N; row0 += static_cast<long long>(gridDim.x) * S::ROWS) {
-    const long long n = row0 + threadIdx.x / S::TPR;
-    const bool on = n < a.N;
-    const int Dn = on ? D : 0;  // a row past the end has no elements, and its threads meet the others
-    float r[S::K][8];
+  const bool branch = a.y.p != nullptr, gated = a.gate.p != nullptr;
+  // x, then y, then the gate in a stage
+  constexpr bool HOLD = keeps_weights<S>(kRow<S, TX, TY>, kWeights<S, BIAS>);
+  constexpr int kept = HOLD ? kWeights<S, BIAS> : 0;  // weights, ahead of the stages
+  const int stage_bytes = CX::BYTES + (branch ? CY::BYTES : 0) + (gated ? CY::BYTES : 0);
+  const int stages = S::VEC ? min(4, (kSmem<S, TX, TY, BIAS> - kept) / stage_bytes) : 1;
+  int y_off[S::RUNS], g_off[S::RUNS];
+  if (S::VEC && branch)
 #pragma unroll
-    for (int i = 0; i < S::K; ++i) load_piece<S, TX>(static_cast<const TX *>(a.x) + n * D, Dn, lane, i, r[i]);
-    if (a.y.p) {
-      const int b = static_cast<int>(n / a.T), t = static_cast<int>(n - static_cast<long long>(b) * a.T);
-      float y[S::K][8];
+    for (int k = 0; k < S::RUNS; ++k) {
+      const int e = min((lane + k * S::TPR) * S::RUN, D - S::RUN);
+      y_off[k] = static_cast<int>(head_offset(a.y, a.d, e));
+      g_off[k] = static_cast<int>(head_offset(a.gate, a.d, e));
+    }
+  auto weights = [&](int k, int i) {
+    const float *p = k == 0 ? a.w_post : k == 1 ? a.w_pre : k == 2 ? a.b_post : a.b_pre;
+    if (k >= 2 && !BIAS) p = nullptr;
+    return load_weights<S>(p, k < 2 ? 1.f : 0.f, D, lane, i);
+  };
+  auto weight = [&](int k, int i) {
+    if (HOLD && (BIAS || k < 2)) return kept_weights<S>(smem + k * S::WEIGHT, i);
+    return weights(k, i);
+  };
+  if (HOLD)
+    for (int k = 0; k < (BIAS ? 4 : 2); ++k)
 #pragma unroll
-      for (int i = 0; i < S::K; ++i) load_heads<S, TY>(a.y, b * a.y.sb + t * a.y.st, Dn, a.d, lane, i, y[i]);
-      if (a.post != 0) {
-        float sum[1], mean = 0.f;
-        if (a.post == 2) {
-          sum[0] = 0.f;
+      for (int i = 0; i < S::K; ++i) keep_weights<S>(smem + k * S::WEIGHT, weights(k, i), i);
+  const int step = gridDim.x * S::ROWS;
+  auto heads_row = [&](const HeadsView &v, int b, int t) { return static_cast<const TY *>(v.p) + heads_start<S>(v, b, t); };
+  int first = blockIdx.x * S::ROWS, n = first + threadIdx.x / S::TPR, stage = 0;  // the block's rows at a time, the thread's
+  RowAt here(n, a.T), ahead = here;
+  auto issue = [&](int n, int stage) {
+    const bool there = n < a.N;
+    const int m = there ? n : 0, b = there ? ahead.b : 0, t = there ? ahead.t : 0;
+    const uint32_t to = smem_u32(smem) + kept + stage * stage_bytes;
+    CX::issue(to, static_cast<const TX *>(a.x) + static_cast<long long>(m) * D, nullptr, lane, mine, there);
+    if (branch) CY::issue(to + CX::BYTES, heads_row(a.y, b, t), y_off, lane, mine, there);
+    if (gated) CY::issue(to + CX::BYTES + CY::BYTES, heads_row(a.gate, b, t), g_off, lane, mine, there);
+    ahead.go(step, a.T);
+  };
+  if constexpr (S::VEC) {
+    clear_smem<S>(smem + kept, stages * stage_bytes);
+    for (int k = 0; k < stages - 1; ++k) {
+      if (k == 0 || first < a.N - k * step) issue(n + k * step, k);
+      copy_commit();
+    }
+  }
+  for (; first < a.N; first += step, n += step, here.go(step, a.T)) {
+    const int Dn = n < a.N ? D : 0;  // a row past the end has no elements, and its threads meet the others
+    const char *slot = smem + kept + stage * stage_bytes;
+    if constexpr (S::VEC) {
+      if (first < a.N - (stages - 1) * step) issue(n + (stages - 1) * step, stage == 0 ? stages - 1 : stage - 1);
+      copy_commit();
+      rows_wait(stages);
+      stage = stage == stages - 1 ? 0 : stage + 1;
+    }
+    const long long at = static_cast<long long>(n) * D;
+    const int b = here.b, t = here.t;
+    Piece r[S::K];
 #pragma unroll
-          for (int i = 0; i < S::K; ++i)
+    for (int i = 0; i < S::K; ++i) {
+      if constexpr (S::VEC) r[i] = CX::read(slot, i);
+      else r[i] = load_single<S, TX>(static_cast<const TX *>(a.x) + at, nullptr, 0, Dn, lane, i);
+    }
+    auto factor = [&](Piece (&x)[S::K], int kind) {  // 1 / the norm; a layer norm's mean is taken off x
+      float sum[1];
+      float2 s = both(0.f);
+      if (kind == 2) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum[0] += y[i][j];
-          row_sums<S>(sum, s_red, turn);
-          mean = sum[0] * inv_d;
-        }
-        sum[0] = 0.f;
-#pragma unroll
-        for (int i = 0; i < S::K; ++i)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            y[i][j] = S::at(lane, i, j) < D ? y[i][j] - mean : 0.f;
-            sum[0] = fmaf(y[i][j], y[i][j], sum[0]);
-          }
+        for (int i = 0; i < S::K; ++i) add_to(s, x[i]);
+        sum[0] = s.x + s.y;
         row_sums<S>(sum, s_red, turn);
-        const float inv = rsqrtf(sum[0] * inv_d + a.eps);
+        s = both(0.f);
 #pragma unroll
-        for (int i = 0; i < S::K; ++i)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) y[i][j] *= inv;
+        for (int i = 0; i < S::K; ++i) centre<S>(x[i], sum[0] * inv_d, mine, i);
       }
 #pragma unroll
-      for (int i = 0; i < S::K; ++i) {
-        float w[8], c[8], g[8];
-        load_weights<S>(a.w_post, D, lane, i, 1.f, w);
-        load_weights<S>(a.b_post, D, lane, i, 0.f, c);
-        if (a.gate.p) load_heads<S, TY>(a.gate, b * a.gate.sb + t * a.gate.st, Dn, a.d, lane, i, g);
+      for (int i = 0; i < S::K; ++i) add_product(s, x[i], x[i]);
+      sum[0] = s.x + s.y;
+      row_sums<S>(sum, s_red, turn);
+      return rsqrtf(fmaf(sum[0], inv_d, a.eps));
+    };
+    if (branch) {
+      Piece y[S::K];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          float v = fmaf(y[i][j], w[j], c[j]);
-          if (a.gate.p) v *= gate_value(g[j], a.act);
-          r[i][j] = fmaf(a.scale, v, r[i][j]);
+      for (int i = 0; i < S::K; ++i) {
+        if constexpr (S::VEC) y[i] = CY::read(slot + CX::BYTES, i);
+        else y[i] = load_single<S, TY>(heads_row(a.y, b, t), &a.y, a.d, Dn, lane, i);
+      }
+      const float inv = a.post != 0 ? factor(y, a.post) : 1.f;
+#pragma unroll
+      for (int i = 0; i < S::K; ++i) {
+        Piece v = weighted(times(y[i], inv), weight(0, i), weight(2, i));
+        if (gated) {
+          Piece g, value, slope;
+          if constexpr (S::VEC) g = CY::read(slot + CX::BYTES + CY::BYTES, i);
+          else g = load_single<S, TY>(heads_row(a.gate, b, t), &a.gate, a.d, Dn, lane, i);
+          gate_piece(g, a.act, value, slope);
+          v = times(v, value);
         }
-        store_piece<S, TX>(static_cast<TX *>(a.r) + n * D, Dn, lane, i, r[i]);
+        FEM_EACH_PAIR r[i].v[j] = __ffma2_rn(v.v[j], both(a.scale), r[i].v[j]);
+        store_piece<S, TX>(static_cast<TX *>(a.r) + at, nullptr, nullptr, 0, Dn, lane, mine, i, r[i]);
+        if (BIAS) FEM_EACH_PAIR r[i].v[j] = __fmul2_rn(r[i].v[j], mine.pair(1.f, i, j));  // a bias is not the row's behind its end
       }
     }
     if (a.pre != 0) {
-      float sum[1], mean = 0.f;
-      if (a.pre == 2) {
-        sum[0] = 0.f;
-#pragma unroll
-        for (int i = 0; i < S::K; ++i)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) sum[0] += S::at(lane, i, j) < D ? r[i][j] : 0.f;
-        row_sums<S>(sum, s_red, turn);
-        mean = sum[0] * inv_d;
-      }
-      sum[0] = 0.f;
+      const float inv = factor(r, a.pre);
 #pragma unroll
       for (int i = 0; i < S::K; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          r[i][j] = S::at(lane, i, j) < D ? r[i][j] - mean : 0.f;
-          sum[0] = fmaf(r[i][j], r[i][j], sum[0]);
-        }
-      row_sums<S>(sum, s_red, turn);
-      const float inv = rsqrtf(sum[0] * inv_d + a.eps);
-#pragma unroll
-      for (int i = 0; i < S::K; ++i) {
-        float w[8], c[8], z[8];
-        load_weights<S>(a.w_pre, D, lane, i, 1.f, w);
-        load_weights<S>(a.b_pre, D, lane, i, 0.f, c);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = fmaf(r[i][j] * inv, w[j], c[j]);
-        store_piece<S, TY>(static_cast<TY *>(a.z) + n * D, Dn, lane, i, z);
-      }
+        store_piece<S, TY>(static_cast<TY *>(a.z) + at, nullptr, nullptr, 0, Dn, lane, mine, i,
+                           weighted(times(r[i], inv), weight(1, i), weight(3, i)));
     }
   }
 }
 
-template <typename S, typename TX, typename TY>
-cudaError_t launch_shape(const NormArgs &a, cudaStream_t stream) {
-  const int groups = (a.N + S::ROWS - 1) / S::ROWS;
-  norm_fwd_kernel<S, TX, TY><<<groups, S::THREADS, 0, stream>>>(a);
-  return cudaGetLastError();
-}
+template <typename S, typename TX, typename TY, bool BIAS>
+struct Tag;
+
+template <typename TX, typename TY, bool BIAS>
+struct Launch {
+  template <typename S>
+  struct With {
+    static cudaError_t call(const NormArgs &a, int num_sms, cudaStream_t stream) {
+      auto *kernel = norm_fwd_kernel<S, TX, TY, BIAS>;
+      int per_sm = 0;
+      const cudaError_t e = resident_blocks<Tag<S, TX, TY, BIAS>>(kernel, S::THREADS, kSmem<S, TX, TY, BIAS>, &per_sm);
+      if (e != cudaSuccess) return e;
+      const int groups = (a.N + S::ROWS - 1) / S::ROWS;
+      kernel<<<std::min(groups, per_sm * num_sms), S::THREADS, kSmem<S, TX, TY, BIAS>, stream>>>(a);
+      return cudaGetLastError();
+    }
+  };
+};
 
 template <typename TX, typename TY>
-cudaError_t launch_types(const NormArgs &a, cudaStream_t stream) {
-  if (!norm_pieces(a, sizeof(TY))) {
-    if (a.D <= 1024) return launch_shape<RowShape<128, 1, false>, TX, TY>(a, stream);
-    if (a.D <= 4096) return launch_shape<RowShape<256, 2, false>, TX, TY>(a, stream);
-    return launch_shape<RowShape<512, 4, false>, TX, TY>(a, stream);
-  }
-  if (a.D <= 256) return launch_shape<RowShape<32, 1, true>, TX, TY>(a, stream);
-  if (a.D <= 512) return launch_shape<RowShape<32, 2, true>, TX, TY>(a, stream);
-  if (a.D <= 1024) return launch_shape<RowShape<32, 4, true>, TX, TY>(a, stream);
-  if (a.D <= 2048) return launch_shape<RowShape<128, 2, true>, TX, TY>(a, stream);
-  if (a.D <= 4096) return launch_shape<RowShape<256, 2, true>, TX, TY>(a, stream);
-  if (a.D <= 8192) return launch_shape<RowShape<512, 2, true>, TX, TY>(a, stream);
-  return launch_shape<RowShape<1024, 2, true>, TX, TY>(a, stream);
+cudaError_t launch_types(const NormArgs &a, int num_sms, cudaStream_t stream) {
+  constexpr int RUN = sizeof(TX) == 4 ? 4 : 8;
+  const bool pieces = norm_pieces(a, sizeof(TY), RUN);
+  return a.b_post || a.b_pre ? with_shape<RUN, false, 1, Launch<TX, TY, true>::template With>(a.D, pieces, a, num_sms, stream)
+                             : with_shape<RUN, false, 1, Launch<TX, TY, false>::template With>(a.D, pieces, a, num_sms, stream);
 }
 
 }  // namespace
 
-cudaError_t launch_norm_fwd(const NormArgs &a, int x_type, int y_type, int, cudaStream_t stream) {
-  if (y_type == kTypeF32) return launch_types<float, float>(a, stream);
-  if (x_type == kTypeF32) return launch_types<float, __nv_bfloat16>(a, stream);
-  return launch_types<__nv_bfloat16, __nv_bfloat16>(a, stream);
+cudaError_t launch_norm_fwd(const NormArgs &a, int x_type, int y_type, int num_sms, cudaStream_t stream) {
+  if (y_type == kTypeF32) return launch_types<float, float>(a, num_sms, stream);
+  if (x_type == kTypeF32) return launch_types<float, __nv_bfloat16>(a, num_sms, stream);
+  return launch_types<__nv_bfloat16, __nv_bfloat16>(a, num_sms, stream);
 }
 
 }  // namespace fem

@@ -1,145 +1,362 @@
 // What the forward and backward kernels of the norms share (include/fem.h, fem_norm): a row's elements in registers.
 //
-// TPR threads take a row, K pieces of eight elements each; a block of max(256, TPR) threads takes as many rows at a
-// time.  Where the row's length, alignment and strides allow (VEC) a piece is 16 bytes of bf16 and neighbouring threads
-// have neighbouring pieces; elsewhere neighbouring threads have neighbouring elements.
+// TPR threads take a row, K pieces of eight elements each; a block goes through rows, as many at a time as 256 (128)
+// threads have room for.  Where the row's length, alignment and strides allow (VEC) a piece is one or two 16-byte
+// copies and neighbouring threads have neighbouring pieces; the next row's copies into shared memory are under way while
+// a row is worked on, and as a thread reads back only what it copied itself, no barrier stands between.  Elsewhere
+// neighbouring threads have neighbouring elements and read them when they need them.
 #pragma once
+
+#include <type_traits>
 
 #include "fem_layer.cuh"
 
 namespace fem {
 
-template <int TPR_, int K_, bool VEC_>
+// A piece is made of runs of RUN elements that lie together: 8 where all is bf16, 4 with fp32 (16 bytes of it, so that a
+// warp's accesses have no gaps), 1 where single elements are read.
+template <int TPR_, int K_, int RUN_, int MOST_ = 256>
 struct RowShape {
-  static constexpr int TPR = TPR_, K = K_, THREADS = TPR_ < 256 ? 256 : TPR_, ROWS = THREADS / TPR_;
-  static constexpr bool VEC = VEC_;
-  static constexpr int WARPS = TPR_ / 32;  // of a row
+  static constexpr int TPR = TPR_, K = K_, RUN = RUN_, ROWS = TPR_ < MOST_ ? MOST_ / TPR_ : 1, THREADS = TPR_ * ROWS;
+  static constexpr bool VEC = RUN_ > 1;
+  static constexpr int RUNS = VEC ? K_ * 8 / RUN_ : 1;  // of a thread, places to keep
+  static constexpr int WARPS = TPR_ / 32;               // of a row
+  static constexpr int WEIGHT = THREADS * K * 32;       // bytes of a vector of weights
 
   // element j of piece i of thread `lane` of the row
-  __device__ static __forceinline__ int at(int lane, int i, int j) {
-    return VEC ? (lane + i * TPR) * 8 + j : lane + TPR * (i * 8 + j);
-  }
+  __device__ static __forceinline__ int at(int lane, int i, int j) { return (lane + (i * (8 / RUN) + j / RUN) * TPR) * RUN + j % RUN; }
 };
 
-// Sums of NV <= 4 values over a row's threads, the same bits in each.  The halves of s_red are used in turn, so that one
-// barrier a call does.
+// Sums of NV <= 4 values over a row's threads, the same bits in each.  In a warp the values are shared out as they are
+// added (half the lanes go on with half of them), so that four cost little more than one; the warps' sums meet in shared
+// memory, whose halves are used in turn, so that one barrier a call does, and rows of a block meet apart.
 constexpr int kRowRed = 32 * 4;
 template <typename S, int NV>
 __device__ __forceinline__ void row_sums(float (&v)[NV], float *s_red, int &turn) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  float x;
+  if constexpr (NV == 1) {
+    x = v[0];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  } else {  // value 2 (lane / 16) + lane / 8 % 2 stays with a lane
+    const bool hi = lane & 16, odd = lane & 8;
+    float a, b = 0.f;
+    if constexpr (NV == 2) {  // value lane / 16
+      a = (hi ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, hi ? v[0] : v[1], 16);
+      x = a + __shfl_xor_sync(0xffffffffu, a, 8);
+    } else {
+      const float v3 = NV > 3 ? v[NV - 1] : 0.f;
+      a = (hi ? v[2] : v[0]) + __shfl_xor_sync(0xffffffffu, hi ? v[0] : v[2], 16);
+      b = (hi ? v3 : v[1]) + __shfl_xor_sync(0xffffffffu, hi ? v[1] : v3, 16);
+      x = (odd ? b : a) + __shfl_xor_sync(0xffffffffu, odd ? a : b, 8);
+    }
 #pragma unroll
-    for (int k = 0; k < NV; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    for (int o = 4; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  }
+  constexpr int EACH = NV == 1 ? 32 : NV == 2 ? 16 : 8;  // lanes that hold a value
   if constexpr (S::WARPS > 1) {
     float *red = s_red + turn * kRowRed;
-    const int w = threadIdx.x >> 5;
-    if ((threadIdx.x & 31) == 0)
+    if (lane % EACH == 0 && lane / EACH < NV) red[(lane / EACH) * 32 + w] = x;
+    bar_sync(1 + static_cast<int>(threadIdx.x) / S::TPR, S::TPR);
+    const int w0 = w - w % S::WARPS;
+    if constexpr (S::WARPS == 2 || S::WARPS == 4 || S::WARPS == 8) {  // lanes 8 k on add value k
+      x = red[(lane >> 3) * 32 + w0 + (lane & (S::WARPS - 1))];
 #pragma unroll
-      for (int k = 0; k < NV; ++k) red[k * 32 + w] = v[k];
-    __syncthreads();
-    const int from = w - w % S::WARPS + (threadIdx.x & 31) % S::WARPS;
+      for (int o = S::WARPS / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
 #pragma unroll
-    for (int k = 0; k < NV; ++k) v[k] = red[k * 32 + from];
+      for (int k = 0; k < NV; ++k) v[k] = __shfl_sync(0xffffffffu, x, 8 * k);
+    } else if constexpr ((S::WARPS & (S::WARPS - 1)) == 0) {
 #pragma unroll
-    for (int o = S::WARPS / 2; o > 0; o >>= 1)
+      for (int k = 0; k < NV; ++k) v[k] = red[k * 32 + w0 + lane % S::WARPS];
 #pragma unroll
-      for (int k = 0; k < NV; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+      for (int o = S::WARPS / 2; o > 0; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < NV; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    } else {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        v[k] = red[k * 32 + w0];
+#pragma unroll
+        for (int o = 1; o < S::WARPS; ++o) v[k] += red[k * 32 + w0 + o];
+      }
+    }
     turn ^= 1;
+  } else {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) v[k] = NV == 1 ? x : __shfl_sync(0xffffffffu, x, EACH * k);
   }
 }
 
-// Piece i of a contiguous row of D elements; what is past its end is 0.
-template <typename S, typename T>
-__device__ __forceinline__ void load_piece(const T *row, int D, int lane, int i, float (&f)[8]) {
-  if constexpr (S::VEC) {
-    Eight<T> x;
-    if (S::at(lane, i, 0) < D) x.load(row + S::at(lane, i, 0));
-    else x.zero();
-    x.get(f);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = S::at(lane, i, j) < D ? to_f32(row[S::at(lane, i, j)]) : 0.f;
-  }
+// Eight elements of a row in fp32, in pairs.
+struct Piece {
+  float2 v[4];
+};
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+#define FEM_EACH_PAIR _Pragma("unroll") for (int j = 0; j < 4; ++j)
+
+__device__ __forceinline__ void add_to(float2 &sum, const Piece &x) { FEM_EACH_PAIR sum = __fadd2_rn(sum, x.v[j]); }
+__device__ __forceinline__ void add_product(float2 &sum, const Piece &x, const Piece &y) {
+  FEM_EACH_PAIR sum = __ffma2_rn(x.v[j], y.v[j], sum);
 }
+__device__ __forceinline__ Piece times(const Piece &x, const Piece &y) {
+  Piece z;
+  FEM_EACH_PAIR z.v[j] = __fmul2_rn(x.v[j], y.v[j]);
+  return z;
+}
+__device__ __forceinline__ Piece times(const Piece &x, float y) {
+  Piece z;
+  FEM_EACH_PAIR z.v[j] = __fmul2_rn(x.v[j], both(y));
+  return z;
+}
+// Which of a thread's runs (VEC) or elements a row has: 1, and 0 behind its end.
+template <typename S>
+struct Mine {
+  float f[S::VEC ? S::RUNS : 8 * S::K];
+  __device__ __forceinline__ Mine(int lane, int D) {
+#pragma unroll
+    for (int k = 0; k < (S::VEC ? S::RUNS : 8 * S::K); ++k)
+      f[k] = S::at(lane, S::VEC ? k * S::RUN / 8 : k / 8, S::VEC ? k * S::RUN % 8 : k % 8) < D ? 1.f : 0.f;
+  }
+  __device__ __forceinline__ bool run(int k) const { return f[k] != 0.f; }
+  // x in the elements 2 j and 2 j + 1 of piece i that there are
+  __device__ __forceinline__ float2 pair(float x, int i, int j) const {
+    return S::VEC ? both(f[(i * 8 + 2 * j) / S::RUN] * x) : make_float2(f[(i * 8 + 2 * j) % (8 * S::K)] * x, f[(i * 8 + 2 * j + 1) % (8 * S::K)] * x);
+  }
+};
+// x - mean where the row has elements; behind its end x is 0 and stays it.
+template <typename S>
+__device__ __forceinline__ void centre(Piece &x, float mean, const Mine<S> &mine, int i) {
+  FEM_EACH_PAIR x.v[j] = __fadd2_rn(x.v[j], mine.pair(-mean, i, j));
+}
+
+__device__ __forceinline__ Piece unpack(const Eight<__nv_bfloat16> &x) {
+  return {make_float2(bf16_lo(x.a.x), bf16_hi(x.a.x)), make_float2(bf16_lo(x.a.y), bf16_hi(x.a.y)),
+          make_float2(bf16_lo(x.a.z), bf16_hi(x.a.z)), make_float2(bf16_lo(x.a.w), bf16_hi(x.a.w))};
+}
+__device__ __forceinline__ Piece unpack(const Eight<float> &x) {
+  return {make_float2(x.a.x, x.a.y), make_float2(x.a.z, x.a.w), make_float2(x.b.x, x.b.y), make_float2(x.b.z, x.b.w)};
+}
+__device__ __forceinline__ void pack(Eight<__nv_bfloat16> &x, const Piece &f) {
+  x.a = make_uint4(bf16_pack(f.v[0].x, f.v[0].y), bf16_pack(f.v[1].x, f.v[1].y), bf16_pack(f.v[2].x, f.v[2].y),
+                   bf16_pack(f.v[3].x, f.v[3].y));
+}
+__device__ __forceinline__ void pack(Eight<float> &x, const Piece &f) {
+  x.a = make_float4(f.v[0].x, f.v[0].y, f.v[1].x, f.v[1].y);
+  x.b = make_float4(f.v[2].x, f.v[2].y, f.v[3].x, f.v[3].y);
+}
+
+__device__ __forceinline__ long long head_offset(const HeadsView &v, int d, int e) {
+  const int h = e / d;
+  return h * v.sh + (e - h * d);
+}
+// Row n = b T + t, followed from row to row.
+struct RowAt {
+  int b, t;
+  __device__ __forceinline__ RowAt(int n, int T) : b(n / T), t(n - n / T * T) {}
+  __device__ __forceinline__ void go(int rows, int T) {
+    t += rows;
+    if (t >= T) {
+      const int q = t / T;
+      b += q;
+      t -= q * T;
+    }
+  }
+};
+// Element (b, t, 0, 0); where runs are copied strides are under 2^31.
+template <typename S>
+__device__ __forceinline__ long long heads_start(const HeadsView &v, int b, int t) {
+  if (!S::VEC) return b * v.sb + t * v.st;
+  const long long at = static_cast<long long>(t) * static_cast<int>(v.st);
+  return b == 0 ? at : at + static_cast<long long>(b) * static_cast<int>(v.sb);
+}
+
+// One array's pieces of a row as a thread copies and reads them, a run beside its neighbours'.
 template <typename S, typename T>
-__device__ __forceinline__ void store_piece(T *row, int D, int lane, int i, const float (&f)[8]) {
+struct Copied {
+  static constexpr int SIZE = S::RUN * sizeof(T);  // of a run: 16 bytes, 8 for bf16 beside fp32
+  static constexpr int BYTES = S::K * 8 * sizeof(T) * S::THREADS;
+  using Unit = std::conditional_t<SIZE == 16, uint4, uint2>;
+  // `p` points at the row; run k is `off[k]` elements on, or where it is in a plain row if `off` is null.  A row that is
+  // not there is one of zeros; what is behind a row's end is never written.
+  __device__ static __forceinline__ void issue(uint32_t slot, const T *p, const int *off, int lane, const Mine<S> &mine, bool there) {
+    static_assert(!S::VEC || SIZE == 16 || SIZE == 8, "a copy's size");
+#pragma unroll
+    for (int k = 0; k < (S::VEC ? S::RUNS : 0); ++k) {
+      const T *src = p + (off ? off[k] : (lane + k * S::TPR) * S::RUN);
+      const uint32_t to = slot + (k * S::THREADS + threadIdx.x) * SIZE;
+      if (!there) zero(to);
+      else if (mine.run(k)) {
+        if (SIZE == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(src) : "memory");
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(src) : "memory");
+      }
+    }
+  }
+  __device__ static __forceinline__ void zero(uint32_t to) {
+    if (SIZE == 16) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
+    else asm volatile("st.shared.v2.b32 [%0], {%1, %1};" ::"r"(to), "r"(0) : "memory");
+  }
+  __device__ static __forceinline__ Piece read(const char *slot, int i) {
+    constexpr int N = 8 / S::RUN;  // runs of a piece
+    Unit u[N];
+#pragma unroll
+    for (int q = 0; q < N; ++q) u[q] = reinterpret_cast<const Unit *>(slot)[(i * N + q) * S::THREADS + threadIdx.x];
+    return unpack(*reinterpret_cast<const Eight<T> *>(u));
+  }
+};
+
+// Shared memory: `weights` bytes, where they fit beside a row, and copies of rows, of which the largest with all its arrays
+// has `row` bytes: an SM's share of a block where `blocks` are to be on it.  As many rows as fit are under way, up to four.
+constexpr int kMostSmem = 224 * 1024;
+template <typename S>
+constexpr bool keeps_weights(int row, int weights) { return S::VEC && row + weights <= kMostSmem; }
+template <typename S>
+constexpr int rows_smem(int row, int weights, int blocks) {
+  const int share = kMostSmem / blocks - (blocks > 1 ? 2048 : 0), least = row + (keeps_weights<S>(row, weights) ? weights : 0);
+  return !S::VEC ? 0 : share > least ? share : least;
+}
+// Zeros in the first `bytes` of shared memory behind `from`, 16 a thread.
+template <typename S>
+__device__ __forceinline__ void clear_smem(char *from, int bytes) {
+  for (int i = threadIdx.x * 16; i < bytes; i += S::THREADS * 16) *reinterpret_cast<uint4 *>(from + i) = make_uint4(0, 0, 0, 0);
+  __syncthreads();
+}
+__device__ __forceinline__ void rows_wait(int stages) {
+  if (stages == 4) copy_wait<3>();
+  else if (stages == 3) copy_wait<2>();
+  else if (stages == 2) copy_wait<1>();
+  else copy_wait<0>();
+}
+
+// Piece i of a row, element by element; what is past its end is 0.
+template <typename S, typename T>
+__device__ __forceinline__ Piece load_single(const T *row, const HeadsView *v, int d, int Dn, int lane, int i) {
+  float f[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int e = S::at(lane, i, j);
+    f[j] = e < Dn ? to_f32(row[v && v->sh != d ? head_offset(*v, d, e) : e]) : 0.f;
+  }
+  return {make_float2(f[0], f[1]), make_float2(f[2], f[3]), make_float2(f[4], f[5]), make_float2(f[6], f[7])};
+}
+// Writes piece i of a row; `off` as above (VEC), `v` the array of heads or null.
+template <typename S, typename T>
+__device__ __forceinline__ void store_piece(T *row, const HeadsView *v, const int *off, int d, int Dn, int lane,
+                                            const Mine<S> &mine, int i, const Piece &f) {
   if constexpr (S::VEC) {
+    constexpr int N = 8 / S::RUN;
     Eight<T> x;
-    x.put(f);
-    if (S::at(lane, i, 0) < D) x.store(row + S::at(lane, i, 0));
+    pack(x, f);
+    const auto *u = reinterpret_cast<const typename Copied<S, T>::Unit *>(&x);
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+      if (Dn && mine.run(i * N + q))
+        *reinterpret_cast<typename Copied<S, T>::Unit *>(row + (off ? off[i * N + q] : S::at(lane, i, q * S::RUN))) = u[q];
+    }
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (S::at(lane, i, j) < D) row[S::at(lane, i, j)] = from_f32<T>(f[j]);
+    for (int j = 0; j < 8; ++j) {
+      const int e = S::at(lane, i, j);
+      if (e < Dn) row[v && v->sh != d ? head_offset(*v, d, e) : e] = from_f32<T>(j % 2 ? f.v[j / 2].y : f.v[j / 2].x);
+    }
   }
 }
 
 // A weight vector's elements of a piece, `none` where there is no vector.
 template <typename S>
-__device__ __forceinline__ void load_weights(const float *w, int D, int lane, int i, float none, float (&f)[8]) {
+__device__ __forceinline__ Piece load_weights(const float *w, float none, int D, int lane, int i) {
+  Piece f;
   if (!w) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = none;
+    FEM_EACH_PAIR f.v[j] = both(none);
   } else if constexpr (S::VEC) {
-    const int e = S::at(lane, i, 0) < D ? S::at(lane, i, 0) : 0;  // past the end: any, nothing there counts
-    const float4 p = __ldg(reinterpret_cast<const float4 *>(w + e));
-    const float4 q = __ldg(reinterpret_cast<const float4 *>(w + e) + 1);
-    f[0] = p.x, f[1] = p.y, f[2] = p.z, f[3] = p.w, f[4] = q.x, f[5] = q.y, f[6] = q.z, f[7] = q.w;
+    // past the end: any, nothing there counts
+    const int e0 = S::at(lane, i, 0), e1 = S::at(lane, i, 4);
+    const float4 p = __ldg(reinterpret_cast<const float4 *>(w + (e0 < D ? e0 : 0)));
+    const float4 q = __ldg(reinterpret_cast<const float4 *>(w + (e1 < D ? e1 : 0)));
+    f = {make_float2(p.x, p.y), make_float2(p.z, p.w), make_float2(q.x, q.y), make_float2(q.z, q.w)};
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = S::at(lane, i, j) < D ? __ldg(w + S::at(lane, i, j)) : 0.f;
+    for (int j = 0; j < 8; ++j) {
+      const float x = S::at(lane, i, j) < D ? __ldg(w + S::at(lane, i, j)) : 0.f;
+      (j % 2 ? f.v[j / 2].y : f.v[j / 2].x) = x;
+    }
   }
+  return f;
+}
+// The same out of shared memory, where each thread keeps its own: registers are short, and beside so much shared memory
+// the L1 cache is too small for what is read row after row.
+template <typename S>
+__device__ __forceinline__ void keep_weights(char *slot, const Piece &f, int i) {
+  float4 *p = reinterpret_cast<float4 *>(slot) + 2 * i * S::THREADS + threadIdx.x;
+  p[0] = make_float4(f.v[0].x, f.v[0].y, f.v[1].x, f.v[1].y);
+  p[S::THREADS] = make_float4(f.v[2].x, f.v[2].y, f.v[3].x, f.v[3].y);
+}
+template <typename S>
+__device__ __forceinline__ Piece kept_weights(const char *slot, int i) {
+  const float4 *s = reinterpret_cast<const float4 *>(slot) + 2 * i * S::THREADS + threadIdx.x;
+  const float4 p = s[0], q = s[S::THREADS];
+  return {make_float2(p.x, p.y), make_float2(p.z, p.w), make_float2(q.x, q.y), make_float2(q.z, q.w)};
+}
+__device__ __forceinline__ Piece weighted(const Piece &x, const Piece &w, const Piece &b) {
+  Piece z;
+  FEM_EACH_PAIR z.v[j] = __ffma2_rn(x.v[j], w.v[j], b.v[j]);
+  return z;
 }
 
-// Piece i of row (b, t) of an array of heads.
-__device__ __forceinline__ long long head_offset(const HeadsView &v, int d, int e) {
-  const int h = e / d;
-  return h * v.sh + (e - h * d);
+// The sigmoid p of g and q = 1 - p = e p, e = e^(-g): no cancellation, and with e at most 2^126 no overflow (a NaN stays
+// one).  The approximated exponential and reciprocal are off by 2 ulp and 1, the rounded exponent by |g| units of 2^-24,
+// of what e is beside 1.
+__device__ __forceinline__ void sigmoid(float g, float &p, float &q) {
+  float t;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(t) : "f"(g * -kLog2e), "f"(126.f));
+  const float e = ex2_approx(t);
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(p) : "f"(1.f + e));
+  q = e * p;
 }
-template <typename S, typename T>
-__device__ __forceinline__ void load_heads(const HeadsView &v, long long row, int D, int d, int lane, int i, float (&f)[8]) {
-  const T *p = static_cast<const T *>(v.p) + row;
-  if constexpr (S::VEC) {
-    Eight<T> x;
-    if (S::at(lane, i, 0) < D) x.load(p + head_offset(v, d, S::at(lane, i, 0)));
-    else x.zero();
-    x.get(f);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = S::at(lane, i, j) < D ? to_f32(p[head_offset(v, d, S::at(lane, i, j))]) : 0.f;
-  }
-}
-template <typename S, typename T>
-__device__ __forceinline__ void store_heads(const HeadsView &v, long long row, int D, int d, int lane, int i, const float (&f)[8]) {
-  T *p = static_cast<T *>(v.p) + row;
-  if constexpr (S::VEC) {
-    Eight<T> x;
-    x.put(f);
-    if (S::at(lane, i, 0) < D) x.store(p + head_offset(v, d, S::at(lane, i, 0)));
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (S::at(lane, i, j) < D) p[head_offset(v, d, S::at(lane, i, j))] = from_f32<T>(f[j]);
-  }
-}
-
-// The gate's value and slope; act as fem_gate_act.
-__device__ __forceinline__ float gate_value(float g, int act) {
-  if (act == 0) return g;
-  const float p = 1.f / (1.f + expf(-g));
-  return act == 1 ? p : g * p;
-}
-__device__ __forceinline__ void gate_slope(float g, int act, float &value, float &slope) {
+// The gate's values and slopes; act as fem_gate_act.
+__device__ __forceinline__ void gate_piece(const Piece &g, int act, Piece &value, Piece &slope) {
   value = g;
-  slope = 1.f;
+  FEM_EACH_PAIR slope.v[j] = both(1.f);
   if (act == 0) return;
-  const float p = 1.f / (1.f + expf(-g)), q = 1.f / (1.f + expf(g));  // q = 1 - p without its cancellation
-  value = act == 1 ? p : g * p;
-  slope = act == 1 ? p * q : p * (1.f + g * q);
+  FEM_EACH_PAIR {
+    float2 p, q;
+    sigmoid(g.v[j].x, p.x, q.x);
+    sigmoid(g.v[j].y, p.y, q.y);
+    if (act == 1) {
+      value.v[j] = p;
+      slope.v[j] = __fmul2_rn(p, q);
+    } else {
+      value.v[j] = __fmul2_rn(g.v[j], p);
+      slope.v[j] = __ffma2_rn(value.v[j], q, p);
+    }
+  }
+}
+
+// The shape for rows of D elements; `pieces`: whether the arrays allow copies of runs of RUN elements.  A thread has one
+// piece, or two with TWO, in blocks of 128 threads, where no threads are idle for it; WIDE of them in rows of more than
+// 4096 elements.
+template <int RUN, bool TWO, int WIDE, template <typename> class F, typename... Args>
+cudaError_t with_shape(int D, bool pieces, Args &&...args) {
+  constexpr int K = TWO ? 2 : 1, MOST = TWO ? 128 : 256;
+  if (!pieces) {
+    if (D <= 1024) return F<RowShape<128, 1, 1>>::call(args...);
+    if (D <= 4096) return F<RowShape<512, 1, 1>>::call(args...);
+    if (D <= 8192) return F<RowShape<1024, 1, 1>>::call(args...);
+    return F<RowShape<1024, 2, 1>>::call(args...);
+  }
+  if (D <= 256) return F<RowShape<32, 1, RUN>>::call(args...);
+  if (D <= 512) return F<RowShape<64 / K, K, RUN, MOST>>::call(args...);
+  if (D <= 768) return F<RowShape<96, 1, RUN>>::call(args...);
+  if (D <= 1024) return F<RowShape<128 / K, K, RUN, MOST>>::call(args...);
+  if (D <= 1536) return F<RowShape<192 / K, K, RUN, MOST>>::call(args...);
+  if (D <= 2048) return F<RowShape<256 / K, K, RUN, MOST>>::call(args...);
+  if (D <= 4096) return F<RowShape<512, 1, RUN>>::call(args...);
+  if (D <= 8192) return F<RowShape<1024 / WIDE, WIDE, RUN>>::call(args...);
+  return F<RowShape<1024, 2, RUN>>::call(args...);
 }
 
 // Whether every array allows 16-byte pieces of eight elements.
-inline bool norm_pieces(const NormArgs &a, int y_size) {
+inline bool norm_pieces(const NormArgs &a, int y_size, int run) {
   auto whole = [](const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; };
   bool ok = a.D % 8 == 0;
   for (const void *p : {a.x, static_cast<const void *>(a.r), static_cast<const void *>(a.z), a.dr, a.dz,
@@ -149,7 +366,8 @@ inline bool norm_pieces(const NormArgs &a, int y_size) {
     ok = ok && whole(p);
   for (const HeadsView *v : {&a.y, &a.gate, &a.dy, &a.dgate})
     if (v->p)
-      ok = ok && a.d % 8 == 0 && whole(v->p) && v->sb * y_size % 16 == 0 && v->st * y_size % 16 == 0 && v->sh * y_size % 16 == 0;
+      ok = ok && a.d % 8 == 0 && reinterpret_cast<uintptr_t>(v->p) % (run * y_size) == 0 && v->sb % run == 0 && v->st % run == 0 && v->sh % run == 0 &&
+           v->sb < (1ll << 31) && v->st < (1ll << 31) && v->sh < (1ll << 31) / a.H;
   return ok;
 }
 

@@ -10,6 +10,8 @@
 // registers; the sums of r, y and dz need one meeting of the row's warps (layer norms: two, the variance about the
 // mean), those of g one more.  The weights' sums over rows stay in registers too while a block goes through its rows,
 // and leave as one row of partial sums per block, which a second kernel adds in order.
+#include <algorithm>
+
 #include "fem_launch.h"
 #include "fem_norm.cuh"
 
@@ -17,135 +19,211 @@ namespace fem {
 
 namespace {
 
+// Blocks on an SM that registers allow for: 170 a thread with two pieces, 112 to 128 with one.  (Spilled ones cost more than
+// fewer warps do: beside so much shared memory the L1 cache is small.)
+template <typename S>
+constexpr int kBlocks = S::THREADS > 256 ? 1 : S::THREADS <= 128 ? 384 / S::THREADS : S::THREADS < 256 ? 576 / S::THREADS : 2;
+template <typename S, typename TX, typename TY>
+constexpr int kRow = 2 * Copied<S, TX>::BYTES + 3 * Copied<S, TY>::BYTES;
+template <typename S, bool BIAS>
+constexpr int kWeights = (BIAS ? 3 : 2) * S::WEIGHT;
 template <typename S, typename TX, typename TY, bool BIAS>
-__global__ void __launch_bounds__(S::THREADS) norm_bwd_kernel(const NormArgs a) {
+constexpr int kSmem = rows_smem<S>(kRow<S, TX, TY>, kWeights<S, BIAS>, kBlocks<S>);
+
+template <typename S, typename TX, typename TY, bool BIAS>
+__global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_bwd_kernel(const NormArgs a) {
+  using CX = Copied<S, TX>;
+  using CY = Copied<S, TY>;
   constexpr int SUMS = BIAS ? 4 : 2;
+  extern __shared__ __align__(16) char smem[];
   __shared__ float s_red[2 * kRowRed];
   int turn = 0;
   const int lane = threadIdx.x % S::TPR, D = a.D;
+  const Mine<S> mine(lane, D);
   const float inv_d = 1.f / static_cast<float>(D);
-  const bool branch = a.y.p != nullptr, centred = a.pre == 2 || (branch && a.post == 2);
-  float acc[SUMS][S::K][8];  // dw_post, dw_pre, db_post, db_pre
+  const bool branch = a.y.p != nullptr, gated = a.gate.p != nullptr, normed = a.pre != 0;
+  Piece acc[SUMS][S::K];  // dw_post, dw_pre, db_post, db_pre
 #pragma unroll
   for (int k = 0; k < SUMS; ++k)
 #pragma unroll
-    for (int i = 0; i < S::K; ++i)
+    for (int i = 0; i < S::K; ++i) FEM_EACH_PAIR acc[k][i].v[j] = both(0.f);
+  constexpr bool HOLD = keeps_weights<S>(kRow<S, TX, TY>, kWeights<S, BIAS>);
+  constexpr int kept = HOLD ? kWeights<S, BIAS> : 0;  // weights, ahead of the stages
+  auto weights = [&](int k, int i) {
+    return load_weights<S>(k == 0 ? a.w_post : k == 1 ? a.w_pre : BIAS ? a.b_post : nullptr, k < 2 ? 1.f : 0.f, D, lane, i);
+  };
+  auto weight = [&](int k, int i) {
+    if (HOLD && (BIAS || k < 2)) return kept_weights<S>(smem + k * S::WEIGHT, i);
+    return weights(k, i);
+  };
+  if (HOLD)
+    for (int k = 0; k < (BIAS ? 3 : 2); ++k)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[k][i][j] = 0.f;
+      for (int i = 0; i < S::K; ++i) keep_weights<S>(smem + k * S::WEIGHT, weights(k, i), i);
+  // r, dr, dz, y and the gate in a stage, those that there are
+  const int at_dr = normed ? CX::BYTES : 0, at_dz = at_dr + (a.dr ? CX::BYTES : 0), at_y = at_dz + (normed ? CY::BYTES : 0);
+  const int at_gate = at_y + (branch ? CY::BYTES : 0), stage_bytes = at_gate + (gated ? CY::BYTES : 0);
+  const int stages = S::VEC ? min(4, (kSmem<S, TX, TY, BIAS> - kept) / stage_bytes) : 1;
+  // places of the pieces in the heads' arrays
+  int off[4][S::RUNS];
+  if (S::VEC && branch)
+#pragma unroll
+    for (int k = 0; k < S::RUNS; ++k) {
+      const int e = min((lane + k * S::TPR) * S::RUN, D - S::RUN);
+      off[0][k] = static_cast<int>(head_offset(a.y, a.d, e));
+      off[1][k] = static_cast<int>(head_offset(a.gate, a.d, e));
+      off[2][k] = static_cast<int>(head_offset(a.dy, a.d, e));
+      off[3][k] = static_cast<int>(head_offset(a.dgate, a.d, e));
+    }
+  const int step = gridDim.x * S::ROWS;
+  auto heads_row = [&](const HeadsView &v, int b, int t) { return static_cast<TY *>(v.p) + heads_start<S>(v, b, t); };
+  int first = blockIdx.x * S::ROWS, n = first + threadIdx.x / S::TPR, stage = 0;  // the block's rows at a time, the thread's
+  RowAt here(n, a.T), ahead = here;
+  auto issue = [&](int n, int stage) {
+    const bool there = n < a.N;
+    const int b = there ? ahead.b : 0, t = there ? ahead.t : 0;
+    const long long at = static_cast<long long>(there ? n : 0) * D;
+    const uint32_t to = smem_u32(smem) + kept + stage * stage_bytes;
+    if (normed) {
+      CX::issue(to, static_cast<const TX *>(a.x) + at, nullptr, lane, mine, there);
+      CY::issue(to + at_dz, static_cast<const TY *>(a.dz) + at, nullptr, lane, mine, there);
+    }
+    if (a.dr) CX::issue(to + at_dr, static_cast<const TX *>(a.dr) + at, nullptr, lane, mine, there);
+    if (branch) CY::issue(to + at_y, heads_row(a.y, b, t), off[0], lane, mine, there);
+    if (gated) CY::issue(to + at_gate, heads_row(a.gate, b, t), off[1], lane, mine, there);
+    ahead.go(step, a.T);
+  };
+  if constexpr (S::VEC) {
+    clear_smem<S>(smem + kept, stages * stage_bytes);
+    for (int k = 0; k < stages - 1; ++k) {
+      if (k == 0 || first < a.N - k * step) issue(n + k * step, k);
+      copy_commit();
+    }
+  }
 
-  for (long long row0 = static_cast<long long>(blockIdx.x) * S::ROWS; row0 < a.N; row0 += static_cast<long long>(gridDim.x) * S::ROWS) {
-    const long long n = row0 + threadIdx.x / S::TPR;
+  for (; first < a.N; first += step, n += step, here.go(step, a.T)) {
     const int Dn = n < a.N ? D : 0;  // a row past the end has no elements, and its threads meet the others
-    const int b = static_cast<int>(n / a.T), t = static_cast<int>(n - static_cast<long long>(b) * a.T);
-    float r[S::K][8], y[S::K][8], dz[S::K][8], dx[S::K][8];
+    const char *slot = smem + kept + stage * stage_bytes;
+    if constexpr (S::VEC) {
+      if (first < a.N - (stages - 1) * step) issue(n + (stages - 1) * step, stage == 0 ? stages - 1 : stage - 1);
+      copy_commit();
+      rows_wait(stages);
+      stage = stage == stages - 1 ? 0 : stage + 1;
+    }
+    const long long at = static_cast<long long>(n) * D;
+    const int b = here.b, t = here.t;
+    // r and y stay in registers; dz, dr and the gate are read where they are used
+    auto get_dz = [&](int i) {
+      if constexpr (S::VEC) return CY::read(slot + at_dz, i);
+      else return load_single<S, TY>(static_cast<const TY *>(a.dz) + at, nullptr, 0, Dn, lane, i);
+    };
+    Piece r[S::K], y[S::K], dx[S::K];
 #pragma unroll
     for (int i = 0; i < S::K; ++i) {
-      if (a.pre != 0) {
-        load_piece<S, TX>(static_cast<const TX *>(a.x) + n * D, Dn, lane, i, r[i]);
-        load_piece<S, TY>(static_cast<const TY *>(a.dz) + n * D, Dn, lane, i, dz[i]);
+      if (normed) {
+        if constexpr (S::VEC) r[i] = CX::read(slot, i);
+        else r[i] = load_single<S, TX>(static_cast<const TX *>(a.x) + at, nullptr, 0, Dn, lane, i);
       }
-      if (a.dr) load_piece<S, TX>(static_cast<const TX *>(a.dr) + n * D, Dn, lane, i, dx[i]);
-      else
-#pragma unroll
-        for (int j = 0; j < 8; ++j) dx[i][j] = 0.f;
-      if (branch) load_heads<S, TY>(a.y, b * a.y.sb + t * a.y.st, Dn, a.d, lane, i, y[i]);
+      if (branch) {
+        if constexpr (S::VEC) y[i] = CY::read(slot + at_y, i);
+        else y[i] = load_single<S, TY>(heads_row(a.y, b, t), &a.y, a.d, Dn, lane, i);
+      }
     }
-    // means for layer norms, then sums of squares and of f u, f being w_pre dz
-    float mean_r = 0.f, mean_y = 0.f, mean_f = 0.f;
-    if (centred) {
-      float v[3] = {0.f, 0.f, 0.f};
+    // means for layer norms, f being w_pre dz
+    float mean_f = 0.f;
+    if (a.pre == 2 || (branch && a.post == 2)) {
+      float2 sr = both(0.f), sy = both(0.f), sf = both(0.f);
 #pragma unroll
       for (int i = 0; i < S::K; ++i) {
-        float w[8];
-        load_weights<S>(a.w_pre, D, lane, i, 1.f, w);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if (a.pre == 2 && S::at(lane, i, j) < D) {
-            v[0] += r[i][j];
-            v[2] = fmaf(w[j], dz[i][j], v[2]);
-          }
-          if (branch && a.post == 2) v[1] += y[i][j];
+        if (a.pre == 2) {
+          add_to(sr, r[i]);
+          add_to(sf, times(get_dz(i), weight(1, i)));
         }
+        if (branch && a.post == 2) add_to(sy, y[i]);
       }
+      float v[3] = {sr.x + sr.y, sy.x + sy.y, sf.x + sf.y};
       row_sums<S>(v, s_red, turn);
-      mean_r = v[0] * inv_d;
-      mean_y = v[1] * inv_d;
       mean_f = v[2] * inv_d;
-    }
-    float v[3] = {0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < S::K; ++i) {
-      float w[8];
-      load_weights<S>(a.w_pre, D, lane, i, 1.f, w);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool in = S::at(lane, i, j) < D;
-        if (a.pre != 0) {
-          r[i][j] = in ? r[i][j] - mean_r : 0.f;
-          v[0] = fmaf(r[i][j], r[i][j], v[0]);
-          if (in) v[1] = fmaf(w[j] * dz[i][j], r[i][j], v[1]);
-        }
-        if (branch && a.post != 0) {
-          y[i][j] = in ? y[i][j] - mean_y : 0.f;
-          v[2] = fmaf(y[i][j], y[i][j], v[2]);
-        }
+      for (int i = 0; i < S::K; ++i) {
+        if (a.pre == 2) centre<S>(r[i], v[0] * inv_d, mine, i);
+        if (branch && a.post == 2) centre<S>(y[i], v[1] * inv_d, mine, i);
       }
     }
-    if (a.pre != 0 || (branch && a.post != 0)) row_sums<S>(v, s_red, turn);
-    const float rho = rsqrtf(fmaf(v[0], inv_d, a.eps)), fu = v[1] * inv_d * rho;
-    const float sigma = a.post != 0 ? rsqrtf(fmaf(v[2], inv_d, a.eps)) : 1.f;
+    // sums of squares, and of f r
+    float rho = 1.f, fu = 0.f, sigma = 1.f;
+    if (normed || (branch && a.post != 0)) {
+      float2 sr = both(0.f), sy = both(0.f), sf = both(0.f);
+#pragma unroll
+      for (int i = 0; i < S::K; ++i) {
+        if (normed) {
+          add_product(sr, r[i], r[i]);
+          add_product(sf, times(get_dz(i), weight(1, i)), r[i]);
+        }
+        if (branch && a.post != 0) add_product(sy, y[i], y[i]);
+      }
+      float v[3] = {sr.x + sr.y, sf.x + sf.y, sy.x + sy.y};
+      row_sums<S>(v, s_red, turn);
+      rho = rsqrtf(fmaf(v[0], inv_d, a.eps));
+      fu = v[1] * inv_d * rho;
+      if (a.post != 0) sigma = rsqrtf(fmaf(v[2], inv_d, a.eps));
+    }
     // dx, dgate, and g = w_post e' with its sums
-    float q[2] = {0.f, 0.f};
+    float2 q0 = both(0.f), q1 = both(0.f);
 #pragma unroll
     for (int i = 0; i < S::K; ++i) {
-      if (a.pre != 0) {
-        float w[8];
-        load_weights<S>(a.w_pre, D, lane, i, 1.f, w);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float u = r[i][j] * rho;
-          dx[i][j] += rho * (w[j] * dz[i][j] - mean_f - u * fu);
-          acc[1][i][j] = fmaf(dz[i][j], u, acc[1][i][j]);
-          if (BIAS) acc[SUMS - 1][i][j] += dz[i][j];
+      if (a.dr) {
+        if constexpr (S::VEC) dx[i] = CX::read(slot + at_dr, i);
+        else dx[i] = load_single<S, TX>(static_cast<const TX *>(a.dr) + at, nullptr, 0, Dn, lane, i);
+      } else {
+        FEM_EACH_PAIR dx[i].v[j] = both(0.f);
+      }
+      if (normed) {
+        const Piece dz = get_dz(i), f = times(dz, weight(1, i)), u = times(r[i], rho);
+        FEM_EACH_PAIR {
+          const float2 off_mean = __fadd2_rn(__ffma2_rn(u.v[j], both(-fu), f.v[j]), both(-mean_f));
+          dx[i].v[j] = __ffma2_rn(off_mean, both(rho), dx[i].v[j]);
+          acc[1][i].v[j] = __ffma2_rn(dz.v[j], u.v[j], acc[1][i].v[j]);
+          if (BIAS) acc[SUMS - 1][i].v[j] = __fadd2_rn(acc[SUMS - 1][i].v[j], dz.v[j]);
         }
       }
-      store_piece<S, TX>(static_cast<TX *>(a.dx) + n * D, Dn, lane, i, dx[i]);
+      store_piece<S, TX>(static_cast<TX *>(a.dx) + at, nullptr, nullptr, 0, Dn, lane, mine, i, dx[i]);
       if (!branch) continue;
-      float w[8], c[8], g[8];
-      load_weights<S>(a.w_post, D, lane, i, 1.f, w);
-      load_weights<S>(a.b_post, D, lane, i, 0.f, c);
-      if (a.gate.p) load_heads<S, TY>(a.gate, b * a.gate.sb + t * a.gate.st, Dn, a.d, lane, i, g);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float e = S::at(lane, i, j) < Dn ? a.scale * dx[i][j] : 0.f;
-        float value = 1.f, slope = 0.f;
-        if (a.gate.p) gate_slope(g[j], a.act, value, slope);
-        y[i][j] *= sigma;
-        g[j] = e * fmaf(y[i][j], w[j], c[j]) * slope;
-        const float gated = e * value;
-        acc[0][i][j] = fmaf(gated, y[i][j], acc[0][i][j]);
-        if (BIAS) acc[SUMS - 2][i][j] += gated;
-        dx[i][j] = w[j] * gated;
-        if (S::at(lane, i, j) < Dn) {
-          q[0] += dx[i][j];
-          q[1] = fmaf(dx[i][j], y[i][j], q[1]);
-        }
+      Piece e;  // nothing behind the row's end, where a mean has been taken off
+      FEM_EACH_PAIR e.v[j] = __fmul2_rn(dx[i].v[j], mine.pair(a.scale, i, j));
+      y[i] = times(y[i], sigma);
+      Piece value, slope;
+      if (gated) {
+        Piece g;
+        if constexpr (S::VEC) g = CY::read(slot + at_gate, i);
+        else g = load_single<S, TY>(heads_row(a.gate, b, t), &a.gate, a.d, Dn, lane, i);
+        gate_piece(g, a.act, value, slope);
+        store_piece<S, TY>(heads_row(a.dgate, b, t), &a.dgate, off[3], a.d, Dn, lane, mine, i,
+                           times(times(weighted(y[i], weight(0, i), weight(2, i)), slope), e));
+        e = times(e, value);
       }
-      if (a.gate.p) store_heads<S, TY>(a.dgate, b * a.dgate.sb + t * a.dgate.st, Dn, a.d, lane, i, g);
+      FEM_EACH_PAIR {
+        acc[0][i].v[j] = __ffma2_rn(e.v[j], y[i].v[j], acc[0][i].v[j]);
+        if (BIAS) acc[SUMS - 2][i].v[j] = __fadd2_rn(acc[SUMS - 2][i].v[j], e.v[j]);
+      }
+      dx[i] = times(e, weight(0, i));
+      add_to(q0, dx[i]);
+      add_product(q1, dx[i], y[i]);
     }
     if (!branch) continue;
     if (a.post != 0) {
+      float q[2] = {q0.x + q0.y, q1.x + q1.y};
       row_sums<S>(q, s_red, turn);
       const float mean_g = a.post == 2 ? q[0] * inv_d : 0.f, gv = q[1] * inv_d;
 #pragma unroll
       for (int i = 0; i < S::K; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) dx[i][j] = sigma * (dx[i][j] - mean_g - y[i][j] * gv);
+        FEM_EACH_PAIR dx[i].v[j] = __fmul2_rn(__fadd2_rn(__ffma2_rn(y[i].v[j], both(-gv), dx[i].v[j]), both(-mean_g)), both(sigma));
     }
 #pragma unroll
-    for (int i = 0; i < S::K; ++i) store_heads<S, TY>(a.dy, b * a.dy.sb + t * a.dy.st, Dn, a.d, lane, i, dx[i]);
+    for (int i = 0; i < S::K; ++i) store_piece<S, TY>(heads_row(a.dy, b, t), &a.dy, off[2], a.d, Dn, lane, mine, i, dx[i]);
   }
 
+  grid_dep_launch_dependents();
   // the block's sums: its rows' groups one after the other into row blockIdx.x of the partial sums
   float *part = a.part + static_cast<long long>(blockIdx.x) * SUMS * D;
   for (int g = 0; g < S::ROWS; ++g) {
@@ -158,70 +236,85 @@ __global__ void __launch_bounds__(S::THREADS) norm_bwd_kernel(const NormArgs a) 
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int e = S::at(lane, i, j);
-          if (e < D) part[k * D + e] = g == 0 ? acc[k][i][j] : part[k * D + e] + acc[k][i][j];
+          const float x = j % 2 ? acc[k][i].v[j / 2].y : acc[k][i].v[j / 2].x;
+          if (e < D) part[k * D + e] = g == 0 ? x : part[k * D + e] + x;
         }
   }
 }
 
-// Adds the partial sums of `blocks` rows, 32 columns a block, its eight warps taking every eighth row.
-__global__ void __launch_bounds__(256) norm_bwd_sum_kernel(const float *part, int blocks, int sums, int D, float *w_post,
-                                                           float *b_post, float *w_pre, float *b_pre) {
-  __shared__ float s_sum[8][32];
+// Adds the partial sums of `blocks` rows, 32 columns a block, its 32 warps taking every 32nd row; the first kernel's
+// dependent, it waits where that one's sums are read.
+__global__ void __launch_bounds__(1024) norm_bwd_sum_kernel(const float *part, int blocks, int sums, int D, float *w_post,
+                                                            float *b_post, float *w_pre, float *b_pre) {
+  __shared__ float s_sum[32][33];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, k = blockIdx.y, e = blockIdx.x * 32 + lane;
   float *out = k == 0 ? w_post : k == 1 ? w_pre : k == 2 ? b_post : b_pre;
+  grid_dep_wait();
   if (!out) return;
   float v = 0.f;
-  if (e < D)
-    for (int i = w; i < blocks; i += 8) v += part[(static_cast<long long>(i) * sums + k) * D + e];
+  if (e < D) {
+#pragma unroll 4
+    for (int i = w; i < blocks; i += 32) v += part[(static_cast<long long>(i) * sums + k) * D + e];
+  }
   s_sum[w][lane] = v;
   __syncthreads();
-  if (w != 0 || e >= D) return;
+  v = s_sum[lane][w];  // column w, the part of warp `lane`
 #pragma unroll
-  for (int i = 1; i < 8; ++i) v += s_sum[i][lane];
-  out[e] = v;
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (lane == 0 && blockIdx.x * 32 + w < D) out[blockIdx.x * 32 + w] = v;
 }
 
-template <typename S, typename TX, typename TY>
-cudaError_t launch_shape(const NormArgs &a, int blocks, cudaStream_t stream) {
-  const bool bias = a.dw[1] || a.dw[3];
-  if (bias) norm_bwd_kernel<S, TX, TY, true><<<blocks, S::THREADS, 0, stream>>>(a);
-  else norm_bwd_kernel<S, TX, TY, false><<<blocks, S::THREADS, 0, stream>>>(a);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess || !(a.dw[0] || a.dw[1] || a.dw[2] || a.dw[3])) return e;
-  const int sums = bias ? 4 : 2;
-  norm_bwd_sum_kernel<<<dim3((a.D + 31) / 32, sums), 256, 0, stream>>>(a.part, blocks, sums, a.D, a.dw[0], a.dw[1], a.dw[2], a.dw[3]);
-  return cudaGetLastError();
-}
+template <typename S, typename TX, typename TY, bool BIAS>
+struct Tag;
+
+// One of: how many blocks there will be (num_sms given), or the launch.
+template <typename TX, typename TY, bool BIAS>
+struct Launch {
+  template <typename S>
+  struct With {
+    static cudaError_t call(const NormArgs &a, int num_sms, int *blocks, cudaStream_t stream) {
+      auto *kernel = norm_bwd_kernel<S, TX, TY, BIAS>;
+      constexpr int smem = kSmem<S, TX, TY, BIAS>;
+      if (num_sms > 0) {
+        int per_sm = 0;
+        const cudaError_t e = resident_blocks<Tag<S, TX, TY, BIAS>>(kernel, S::THREADS, smem, &per_sm);
+        *blocks = std::min((a.N + S::ROWS - 1) / S::ROWS, per_sm * num_sms);
+        return e;
+      }
+      kernel<<<*blocks, S::THREADS, smem, stream>>>(a);
+      const cudaError_t e = cudaGetLastError();
+      if (e != cudaSuccess || !(a.dw[0] || a.dw[1] || a.dw[2] || a.dw[3])) return e;
+      const int sums = BIAS ? 4 : 2;
+      return launch_kernel(norm_bwd_sum_kernel, dim3((a.D + 31) / 32, sums), dim3(1024), 0, stream, true, a.part, *blocks, sums, a.D,
+                           a.dw[0], a.dw[1], a.dw[2], a.dw[3]);
+    }
+  };
+};
 
 template <typename TX, typename TY>
-cudaError_t launch_types(const NormArgs &a, int blocks, cudaStream_t stream) {
-  if (!norm_pieces(a, sizeof(TY))) {
-    if (a.D <= 1024) return launch_shape<RowShape<128, 1, false>, TX, TY>(a, blocks, stream);
-    if (a.D <= 4096) return launch_shape<RowShape<512, 1, false>, TX, TY>(a, blocks, stream);
-    return launch_shape<RowShape<1024, 2, false>, TX, TY>(a, blocks, stream);
-  }
-  if (a.D <= 256) return launch_shape<RowShape<32, 1, true>, TX, TY>(a, blocks, stream);
-  if (a.D <= 512) return launch_shape<RowShape<64, 1, true>, TX, TY>(a, blocks, stream);
-  if (a.D <= 1024) return launch_shape<RowShape<128, 1, true>, TX, TY>(a, blocks, stream);
-  if (a.D <= 2048) return launch_shape<RowShape<256, 1, true>, TX, TY>(a, blocks, stream);
-  if (a.D <= 4096) return launch_shape<RowShape<512, 1, true>, TX, TY>(a, blocks, stream);
-  if (a.D <= 8192) return launch_shape<RowShape<1024, 1, true>, TX, TY>(a, blocks, stream);
-  return launch_shape<RowShape<1024, 2, true>, TX, TY>(a, blocks, stream);
+cudaError_t types(const NormArgs &a, int num_sms, int *blocks, cudaStream_t stream) {
+  constexpr int RUN = sizeof(TX) == 4 ? 4 : 8;
+  // a row of all arrays that does not fit in shared memory is read element by element
+  const bool pieces = norm_pieces(a, sizeof(TY), RUN) && (a.D <= 8192 || (2 * sizeof(TX) + 3 * sizeof(TY)) * 16384 <= kMostSmem);
+  return a.dw[1] || a.dw[3] || a.b_post
+             ? with_shape<RUN, RUN == 8, 2, Launch<TX, TY, true>::template With>(a.D, pieces, a, num_sms, blocks, stream)
+             : with_shape<RUN, RUN == 8, 2, Launch<TX, TY, false>::template With>(a.D, pieces, a, num_sms, blocks, stream);
+}
+
+cudaError_t dispatch(const NormArgs &a, int x_type, int y_type, int num_sms, int *blocks, cudaStream_t stream) {
+  if (y_type == kTypeF32) return types<float, float>(a, num_sms, blocks, stream);
+  if (x_type == kTypeF32) return types<float, __nv_bfloat16>(a, num_sms, blocks, stream);
+  return types<__nv_bfloat16, __nv_bfloat16>(a, num_sms, blocks, stream);
 }
 
 }  // namespace
 
-int norm_bwd_blocks(int N, int D, int num_sms) {
-  const int rows = D <= 256 ? 8 : D <= 512 ? 4 : D <= 1024 ? 2 : 1, per_sm = D <= 2048 ? 2 : 1;
-  const int groups = (N + rows - 1) / rows, most = num_sms * per_sm;
-  return groups < most ? groups : most;
+cudaError_t norm_bwd_blocks(const NormArgs &a, int x_type, int y_type, int num_sms, int *blocks) {
+  return dispatch(a, x_type, y_type, num_sms, blocks, nullptr);
 }
 
-cudaError_t launch_norm_bwd(const NormArgs &a, int x_type, int y_type, int num_sms, cudaStream_t stream) {
-  const int blocks = norm_bwd_blocks(a.N, a.D, num_sms);
-  if (y_type == kTypeF32) return launch_types<float, float>(a, blocks, stream);
-  if (x_type == kTypeF32) return launch_types<float, __nv_bfloat16>(a, blocks, stream);
-  return launch_types<__nv_bfloat16, __nv_bfloat16>(a, blocks, stream);
+cudaError_t launch_norm_bwd(const NormArgs &a, int x_type, int y_type, int blocks, cudaStream_t stream) {
+  return dispatch(a, x_type, y_type, 0, &blocks, stream);
 }
 
 }  // namespace fem

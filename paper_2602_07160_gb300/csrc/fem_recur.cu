@@ -136,9 +136,6 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void *src, int by
   if (SIZE == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
   else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int LEFT>
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
 // A map into another CTA's shared memory, counted by its mbarrier.
 __device__ __forceinline__ uint32_t in_cta(uint32_t addr, int rank) {
