@@ -983,7 +983,9 @@ int fem_rope(const fem_heads *q, const fem_heads *q_out, int Hq, const fem_heads
   a.pos = positions;
   a.amplitude = amplitude;
   a.inverse = inverse;
-  return map_cuda(launch_rope(a, type, interleaved != 0, static_cast<cudaStream_t>(stream)));
+  DeviceState *ds = nullptr;
+  if ((rc = device_state(&ds)) != FEM_OK) return rc;
+  return map_cuda(launch_rope(a, type, interleaved != 0, ds->num_sms, static_cast<cudaStream_t>(stream)));
 }
 
 // What both passes of the recurrence check; rows and states are wanted.

@@ -25,7 +25,7 @@ struct RopeArgs {
   float amplitude;
   int inverse;
 };
-cudaError_t launch_rope(const RopeArgs &a, int type, bool interleaved, cudaStream_t stream);
+cudaError_t launch_rope(const RopeArgs &a, int type, bool interleaved, int num_sms, cudaStream_t stream);
 
 constexpr long long kRecurMostStride = 1ll << 20;  // elements between rows: a tile of at most 1024 rows stays under 2^32 bytes
 struct RecurArgs {

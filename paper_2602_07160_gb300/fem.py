@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 import threading
 
 import torch
@@ -518,22 +519,23 @@ def fem_paged_read(q, cache: PagedCache, beta, q_offsets, ctx_lens, block_table,
     return out, (None if lse is False else lse)
 
 
-class _Heads(ctypes.Structure):
-    """fem_heads of include/fem.h."""
-    _fields_ = [("p", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_t", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
-
-
 _TYPES = {torch.bfloat16: 0, torch.float32: 2}  # fem_type
+_heads_bytes = struct.Struct("@Pqqq").pack  # fem_heads of include/fem.h: address, strides over b, t and h
 
 
 def _current(index):
     """The library launches on the current device, where its error word and workspaces are."""
-    if index < 0 or torch.cuda.current_device() != index:
+    if index < 0 or torch._C._cuda_getDevice() != index:
         raise ValueError("the tensors' device must be a CUDA device and the current one")
 
 
 def _stream_number(stream, index):
     return torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+
+
+def _new(like, shape, dtype, stream):
+    """An output a call allocates, on `like`'s device (_output)."""
+    return torch.empty(shape, dtype=dtype, device=like.device) if stream is None else _output(shape, dtype, like, stream)
 
 
 def _optional(name, t, shape, dtype, index):
@@ -545,17 +547,23 @@ def _optional(name, t, shape, dtype, index):
     return t.data_ptr()
 
 
-def _heads(name, t, dtype, index):
-    """[N, H, d] or [B, H, T, d] as fem_heads, with (B, T, H, d)."""
-    if t.dtype is not dtype or t.get_device() != index:
-        raise ValueError(f"{name} must be {dtype} on the other tensors' device")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+def _heads(name, t, shape, dtype, index):
+    """[N, H, d] or [B, H, T, d] as fem_heads."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)} on the other tensors' device")
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name}'s last axis must be contiguous")
-    if t.dim() == 3:
-        (n, h, d), (sn, sh, _) = t.shape, t.stride()
-        return _Heads(t.data_ptr(), 0, sn, sh), (1, n, h, d)
-    (b, h, n, d), (sb, sh, sn, _) = t.shape, t.stride()
-    return _Heads(t.data_ptr(), sb, sn, sh), (b, n, h, d)
+    if len(st) == 3:
+        return _heads_bytes(t.data_ptr(), 0, st[0], st[1])
+    return _heads_bytes(t.data_ptr(), st[0], st[2], st[1])
+
+
+def _fresh_heads(t, shape):
+    """A contiguous tensor's fem_heads."""
+    if len(shape) == 3:
+        return _heads_bytes(t.data_ptr(), 0, shape[1] * shape[2], shape[2])
+    return _heads_bytes(t.data_ptr(), shape[1] * shape[2] * shape[3], shape[3], shape[2] * shape[3])
 
 
 class Rope:
@@ -579,7 +587,8 @@ class Rope:
             raise FemError("fem_rope_turns", rc)
         signed = [v - (1 << 64) if v >> 63 else v for v in table]
         self.turns = torch.tensor(signed, dtype=torch.int64).to(device)
-        self.rotary_dim, self.interleaved, self.amplitude = rotary_dim, bool(interleaved), float(amplitude)
+        self.table, self.index = self.turns.data_ptr(), self.turns.get_device()
+        self.rotary_dim, self.interleaved, self.amplitude = rotary_dim, int(bool(interleaved)), float(amplitude)
 
 
 def fem_rope(rope: Rope, q, k=None, positions=None, inverse: bool = False, out=None, stream=None):
@@ -588,74 +597,85 @@ def fem_rope(rope: Rope, q, k=None, positions=None, inverse: bool = False, out=N
     positions: int32 [N] or [B, T]; None counts from 0 along N or T.  ``inverse`` turns back, which takes the outputs'
     gradients to the inputs'.  Strided views are taken as they are.  ``out``: the pair of output tensors, which may be
     (q, k) themselves.  Returns (q, k)."""
-    if q.dim() not in (3, 4) or (k is not None and k.dim() != q.dim()):
-        raise ValueError("q and k must both be [N, heads, d] or [B, heads, T, d]")
-    if q.dtype not in _TYPES:
-        raise ValueError(f"q has dtype {q.dtype}")
-    index = q.get_device()
+    shape, dtype, index = q.shape, q.dtype, q.get_device()
+    if len(shape) == 3:
+        (T, Hq, d), B = shape, 1
+    elif len(shape) == 4:
+        B, Hq, T, d = shape
+    else:
+        raise ValueError("q must be [N, heads, d] or [B, heads, T, d]")
+    if dtype not in _TYPES:
+        raise ValueError(f"q has dtype {dtype}")
     _current(index)
-    if rope.turns.get_device() != index:
+    if rope.index != index:
         raise ValueError("the rope's table must be on q's device")
-    qv, (B, T, Hq, d) = _heads("q", q, q.dtype, index)
-    pos = _optional("positions", positions, (T,) if q.dim() == 3 else (B, T), torch.int32, index)
     q_out, k_out = out if out is not None else (None, None)
+    qv = _heads("q", q, shape, dtype, index)
     if q_out is None:
-        q_out = _output(q.shape, q.dtype, q, stream)
-    elif q_out.shape != q.shape:
-        raise ValueError("out must have the inputs' shapes")
-    qo, _ = _heads("out", q_out, q.dtype, index)
+        q_out = _new(q, shape, dtype, stream)
+        qo = _fresh_heads(q_out, shape)
+    else:
+        qo = _heads("out", q_out, shape, dtype, index)
     kv = ko = None
     Hk = 0
     if k is not None:
-        kv, (Bk, Tk, Hk, dk) = _heads("k", k, q.dtype, index)
-        if (Bk, Tk, dk) != (B, T, d):
+        k_shape = k.shape
+        if len(k_shape) != len(shape) or k_shape[-1] != d or (k_shape[0] != T if B == 1 and len(shape) == 3 else
+                                                              (k_shape[0], k_shape[2]) != (B, T)):
             raise ValueError("q and k must have the same tokens and d")
+        Hk = k_shape[1]
+        kv = _heads("k", k, k_shape, dtype, index)
         if k_out is None:
-            k_out = _output(k.shape, k.dtype, k, stream)
-        elif k_out.shape != k.shape:
-            raise ValueError("out must have the inputs' shapes")
-        ko, _ = _heads("out", k_out, q.dtype, index)
-        kv, ko = ctypes.byref(kv), ctypes.byref(ko)
+            k_out = _new(k, k_shape, dtype, stream)
+            ko = _fresh_heads(k_out, k_shape)
+        else:
+            ko = _heads("out", k_out, k_shape, dtype, index)
     elif k_out is not None:
         raise ValueError("out has keys and the call none")
-    rc = load().fem_rope(ctypes.byref(qv), ctypes.byref(qo), Hq, kv, ko, Hk, B, T, d, _TYPES[q.dtype],
-                         rope.turns.data_ptr(), rope.rotary_dim, int(rope.interleaved), rope.amplitude, pos,
-                         int(bool(inverse)), _stream_number(stream, index))
+    pos = None
+    if positions is not None:
+        pos = _optional("positions", positions, (T,) if len(shape) == 3 else (B, T), torch.int32, index)
+    rc = load().fem_rope(qv, qo, Hq, kv, ko, Hk, B, T, d, _TYPES[dtype], rope.table, rope.rotary_dim, rope.interleaved,
+                         rope.amplitude, pos, 1 if inverse else 0, _stream_number(stream, index))
     if rc != 0:
         raise FemError("fem_rope", rc)
-    return q_out, (None if k is None else k_out)
+    return q_out, k_out
 
 
-def _recur_rows(name, t, like, packed):
-    """Address and row stride of a [N, C] (packed) or [B, T, C] tensor shaped like `like`."""
-    if t.shape != like.shape or t.dtype is not like.dtype or t.get_device() != like.get_device():
+def _recur_rows(name, t, shape, dtype, index):
+    """Address and row stride of a [N, C] or [B, T, C] tensor."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
         raise ValueError(f"{name} must have s's shape, type and device")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.is_contiguous():
+        return t.data_ptr(), shape[-1]
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name}'s last axis must be contiguous")
-    if packed:
-        return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
-    B, T, C = t.shape
-    row = t.stride(1) if T > 1 else t.stride(0) if B > 1 else C
-    if B > 1 and T > 1 and t.stride(0) != T * row:
+    if len(shape) == 2:
+        return t.data_ptr(), (st[0] if shape[0] > 1 else shape[1])
+    B, T, C = shape
+    row = st[1] if T > 1 else st[0] if B > 1 else C
+    if B > 1 and T > 1 and st[0] != T * row:
         raise ValueError(f"{name}'s rows must be evenly spaced over batch and time")
     return t.data_ptr(), row
 
 
 def _recur_sizes(s, offsets, max_len):
-    """(address of the offsets, S, T, N, C) of a call; checks s and the offsets."""
-    if s.dim() != (3 if offsets is None else 2):
-        raise ValueError("s must be [B, T, C], or [N, C] with offsets")
-    if s.dtype not in _TYPES:
-        raise ValueError(f"s has dtype {s.dtype}")
-    index = s.get_device()
+    """(shape, dtype, device, address of the offsets, S, T, N, C) of a call; checks s and the offsets."""
+    shape, dtype, index = s.shape, s.dtype, s.get_device()
+    if dtype not in _TYPES:
+        raise ValueError(f"s has dtype {dtype}")
     _current(index)
+    if len(shape) != (3 if offsets is None else 2):
+        raise ValueError("s must be [B, T, C], or [N, C] with offsets")
     if offsets is None:
-        B, T, C = s.shape
-        return None, B, T, B * T, C
+        B, T, C = shape
+        return shape, dtype, index, None, B, T, B * T, C
     if offsets.dim() != 1 or offsets.shape[0] < 1:
         raise ValueError("offsets must be int32 [S + 1]")
-    S, (N, C) = offsets.shape[0] - 1, s.shape
-    return _optional("offsets", offsets, (S + 1,), torch.int32, index), S, N if max_len is None else int(max_len), N, C
+    S, (N, C) = offsets.shape[0] - 1, shape
+    off = _optional("offsets", offsets, (S + 1,), torch.int32, index)
+    return shape, dtype, index, off, S, N if max_len is None else int(max_len), N, C
 
 
 def fem_recur_fwd(s, u, offsets=None, max_len=None, h0=None, state_rows=None, mean: bool = False, out=None,
@@ -667,33 +687,40 @@ def fem_recur_fwd(s, u, offsets=None, max_len=None, h0=None, state_rows=None, me
     h0: float32 states before the first step, [S, C], or [num_states, C] with state_rows int32 [S] (negative: none).
     state_out: where the states after the last step go, shaped like h0: None allocates [S, C], or with state_rows
     updates h0 in place; False skips them.  Returns (h, states)."""
-    off, S, T, N, C = _recur_sizes(s, offsets, max_len)
-    index, packed = s.get_device(), offsets is not None
+    shape, dtype, index, off, S, T, N, C = _recur_sizes(s, offsets, max_len)
     if state_out is None and state_rows is not None and h0 is not None:
         state_out = h0
-    states = [t for t in (h0, state_out) if t is not None and t is not False]
-    if any(t.dim() != 2 or t.shape != states[0].shape for t in states):
-        raise ValueError("h0 and state_out must share the shape [num_states, C]")
-    if state_rows is not None and not states:
-        raise ValueError("state_rows goes with h0 or state_out")
-    num = states[0].shape[0] if states else S
-    if state_rows is None and num != S:
-        raise ValueError("h0 and state_out must have a row for each sequence, or state_rows")
+    kept = state_out is not None and state_out is not False
+    if h0 is None and not kept:
+        if state_rows is not None:
+            raise ValueError("state_rows goes with h0 or state_out")
+        num = S
+    else:
+        num = (state_out if h0 is None else h0).shape[0]
+        if state_rows is None and num != S:
+            raise ValueError("h0 and state_out must have a row for each sequence, or state_rows")
     h0_ptr = _optional("h0", h0, (num, C), torch.float32, index)
     rows_ptr = _optional("state_rows", state_rows, (S,), torch.int32, index)
-    s_ptr, s_st = _recur_rows("s", s, s, packed)
-    u_ptr, u_st = _recur_rows("u", u, s, packed)
+    s_ptr, s_st = _recur_rows("s", s, shape, dtype, index)
+    u_ptr, u_st = _recur_rows("u", u, shape, dtype, index)
     if out is None:
-        out = _output(s.shape, s.dtype, s, stream)
-    h_ptr, h_st = _recur_rows("out", out, s, packed)
-    if state_out is None:
-        state_out = _output((S, C), torch.float32, s, stream)
-    last_ptr = None if state_out is False else _optional("state_out", state_out, (num, C), torch.float32, index)
-    rc = load().fem_recur_fwd(s_ptr, u_ptr, s_st, u_st, off, S, T, N, C, _TYPES[s.dtype], int(bool(mean)), h0_ptr, last_ptr,
+        out = _new(s, shape, dtype, stream)
+        h_ptr, h_st = out.data_ptr(), C
+    else:
+        h_ptr, h_st = _recur_rows("out", out, shape, dtype, index)
+    if state_out is False:
+        last_ptr = state_out = None
+    elif state_out is None:
+        num = max(num, S)
+        state_out = _new(s, (S, C), torch.float32, stream)
+        last_ptr = state_out.data_ptr()
+    else:
+        last_ptr = _optional("state_out", state_out, (num, C), torch.float32, index)
+    rc = load().fem_recur_fwd(s_ptr, u_ptr, s_st, u_st, off, S, T, N, C, _TYPES[dtype], 1 if mean else 0, h0_ptr, last_ptr,
                               rows_ptr, num, h_ptr, h_st, _stream_number(stream, index))
     if rc != 0:
         raise FemError("fem_recur_fwd", rc)
-    return out, (None if state_out is False else state_out)
+    return out, state_out
 
 
 def fem_recur_bwd(s, u, h, dh, offsets=None, max_len=None, h0=None, dstate=None, mean: bool = False, stream=None):
@@ -701,12 +728,12 @@ def fem_recur_bwd(s, u, h, dh, offsets=None, max_len=None, h0=None, dstate=None,
     (float32 [S, C] or None).  h0: float32 [S, C] or None, as the forward had it.  u is read where ``mean`` only.
 
     Returns (ds, du, dh0), dh0 None where h0 is."""
-    off, S, T, N, C = _recur_sizes(s, offsets, max_len)
-    index, packed = s.get_device(), offsets is not None
-    ins = [_recur_rows(name, t, s, packed) for name, t in (("s", s), ("u", u), ("h", h), ("dh", dh))]
-    ds, du = _output(s.shape, s.dtype, s, stream), _output(s.shape, s.dtype, s, stream)
-    dh0 = None if h0 is None else _output((S, C), torch.float32, s, stream)
-    rc = load().fem_recur_bwd(*(p for p, _ in ins), *(st for _, st in ins), off, S, T, N, C, _TYPES[s.dtype], int(bool(mean)),
+    shape, dtype, index, off, S, T, N, C = _recur_sizes(s, offsets, max_len)
+    (s_ptr, s_st), (u_ptr, u_st), (h_ptr, h_st), (g_ptr, g_st) = (
+        _recur_rows(name, t, shape, dtype, index) for name, t in (("s", s), ("u", u), ("h", h), ("dh", dh)))
+    ds, du = _new(s, shape, dtype, stream), _new(s, shape, dtype, stream)
+    dh0 = None if h0 is None else _new(s, (S, C), torch.float32, stream)
+    rc = load().fem_recur_bwd(s_ptr, u_ptr, h_ptr, g_ptr, s_st, u_st, h_st, g_st, off, S, T, N, C, _TYPES[dtype], 1 if mean else 0,
                               _optional("h0", h0, (S, C), torch.float32, index),
                               _optional("dstate", dstate, (S, C), torch.float32, index), ds.data_ptr(), du.data_ptr(), C, C,
                               None if dh0 is None else dh0.data_ptr(), _stream_number(stream, index))
@@ -715,11 +742,7 @@ def fem_recur_bwd(s, u, h, dh, offsets=None, max_len=None, h0=None, dstate=None,
     return ds, du, dh0
 
 
-class _NormStruct(ctypes.Structure):
-    """fem_norm of include/fem.h."""
-    _fields_ = [(n, ctypes.c_int) for n in ("B", "T", "H", "d", "x_type", "y_type", "post", "pre", "gate_act")] + \
-               [("scale", ctypes.c_float), ("eps", ctypes.c_float)] + \
-               [(n, ctypes.c_void_p) for n in ("w_post", "b_post", "w_pre", "b_pre")]
+_norm_bytes = struct.Struct("@9i2f4P").pack  # fem_norm of include/fem.h
 
 
 class BlockNorm:
@@ -749,56 +772,65 @@ class BlockNorm:
             if self.index not in (None, t.get_device()):
                 raise ValueError("the weights must be on one device")
             self.index = t.get_device()
+        self._fixed = (self.KINDS[post], self.KINDS[pre], self.ACTS[gate], self.scale, self.eps,
+                       *(0 if t is None else t.data_ptr() for t in (w_post, b_post, w_pre, b_pre)))
 
-    def _struct(self, x, y):
-        """fem_norm for a call on x and y, with its (B, T, H, d) and number of rows."""
+    def _call(self, name, x, y, gate):
+        """((B, T, H, d), x's shape, x's and the branch's type, device) of a call; checks x, y and the gate."""
+        shape, dtype, index = x.shape, x.dtype, x.get_device()
+        if dtype not in _TYPES or not shape or shape[-1] != self.width or not x.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous bf16 or float32 tensor [..., {self.width}]")
+        _current(index)
+        if self.index is not None and self.index != index:
+            raise ValueError(f"{name} must be on the weights' device")
+        if (gate is not None) != (y is not None and self.gate != "none"):
+            raise ValueError("gate goes with y and with a norm that has one")
         rows = x.numel() // self.width
-        if y is None or y.shape == x.shape:
+        if y is None or y.shape == shape:
             B, T, H, d = 1, rows, 1, self.width
-        elif y.dim() == 3:
-            B, T, H, d = 1, y.shape[0], y.shape[1], y.shape[2]
-        elif y.dim() == 4:
-            B, T, H, d = y.shape[0], y.shape[2], y.shape[1], y.shape[3]
         else:
-            raise ValueError("y must have x's shape or be [N, H, d] or [B, H, T, d]")
-        if B * T != rows or H * d != self.width:
-            raise ValueError("y must have x's rows, and heads of its width together")
-        if x.dim() == 3 and y is not None and y.dim() == 4 and (B, T) != tuple(x.shape[:2]):
-            raise ValueError("y [B, H, T, d] must have the B and T of x [B, T, width]")
-        w = self.weights
-        return _NormStruct(B, T, H, d, _TYPES[x.dtype], _TYPES[x.dtype if y is None else y.dtype], self.KINDS[self.post],
-                           self.KINDS[self.pre], self.ACTS[self.gate], self.scale, self.eps,
-                           *(None if w[n] is None else w[n].data_ptr() for n in ("w_post", "b_post", "w_pre", "b_pre")))
+            y_shape = y.shape
+            if len(y_shape) == 3:
+                (T, H, d), B = y_shape, 1
+            elif len(y_shape) == 4:
+                B, H, T, d = y_shape
+            else:
+                raise ValueError("y must have x's shape or be [N, H, d] or [B, H, T, d]")
+            if B * T != rows or H * d != self.width or (len(shape) == 3 and len(y_shape) == 4 and (B, T) != shape[:2]):
+                raise ValueError("y must have x's rows, and heads of its width together")
+        y_type = dtype if y is None else y.dtype
+        if y_type not in _TYPES:
+            raise ValueError(f"y has dtype {y_type}")
+        return (B, T, H, d), shape, dtype, y_type, index
+
+    def _describe(self, sizes, x_type, y_type):
+        return _norm_bytes(*sizes, _TYPES[x_type], _TYPES[y_type], *self._fixed)
 
 
-def _norm_heads(name, t, x, shape, dtype, index):
+def _branch(name, t, x_shape, shape, dtype, index):
     """A branch tensor (x's shape, [N, H, d] or [B, H, T, d]) as fem_heads."""
-    if t.shape != shape:
-        raise ValueError(f"{name} must have the shape {tuple(shape)}")
-    if t.shape != x.shape:
-        return _heads(name, t, dtype, index)[0]
-    if t.dtype is not dtype or t.get_device() != index:
-        raise ValueError(f"{name} must be {dtype} on x's device")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.shape != x_shape:
+        return _heads(name, t, shape, dtype, index)
+    if t.dtype is not dtype or t.get_device() != index or shape != x_shape:
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)} on x's device")
+    width = x_shape[-1]
+    if t.is_contiguous():
+        return _heads_bytes(t.data_ptr(), 0, width, 0)
+    st = t.stride()
+    if st[-1] != 1 and width > 1:
         raise ValueError(f"{name}'s last axis must be contiguous")
     row, span = None, 1  # rows of all leading axes, evenly spaced
-    for n, st in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+    for n, step in zip(reversed(x_shape[:-1]), reversed(st[:-1])):
         if n > 1:
-            if row is not None and st != row * span:
+            if row is not None and step != row * span:
                 raise ValueError(f"{name}'s rows must be evenly spaced")
-            row = st // span if row is None else row
+            row = step if row is None else row
             span *= n
-    return _Heads(t.data_ptr(), 0, 0 if row is None else row, 0)
+    return _heads_bytes(t.data_ptr(), 0, 0 if row is None else row, 0)
 
 
-def _norm_check(norm, x, name):
-    if x.dtype not in _TYPES or x.dim() < 1 or x.shape[-1] != norm.width or not x.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous bf16 or float32 tensor [..., {norm.width}]")
-    index = x.get_device()
-    _current(index)
-    if norm.index not in (None, index):
-        raise ValueError(f"{name} must be on the weights' device")
-    return index
+def _fresh_branch(t, x_shape, shape):
+    return _heads_bytes(t.data_ptr(), 0, x_shape[-1], 0) if shape == x_shape else _fresh_heads(t, shape)
 
 
 def fem_norm_fwd(norm: BlockNorm, x, y=None, gate=None, out=None, z_out=None, stream=None):
@@ -807,36 +839,38 @@ def fem_norm_fwd(norm: BlockNorm, x, y=None, gate=None, out=None, z_out=None, st
     x: contiguous [..., width], bf16 or float32; y and gate: x's shape, or heads [N, H, d] or [B, H, T, d] (the read's
     outputs as they are), bf16, or float32 with a float32 x; without y there is no block before and r is x.  ``out`` may
     be x itself.  Returns (r, z), z of y's type (without y of z_out's, or x's)."""
-    index = _norm_check(norm, x, "x")
-    if (norm.gate != "none") != (gate is not None) and y is not None or (y is None and gate is not None):
-        raise ValueError("gate goes with y and with a norm that has one")
-    if y is not None and y.dtype not in _TYPES:
-        raise ValueError(f"y has dtype {y.dtype}")
-    struct = norm._struct(x, y)
-    z_type = y.dtype if y is not None else x.dtype if z_out is None else z_out.dtype
-    if z_type not in _TYPES:
-        raise ValueError(f"z_out has dtype {z_type}")
-    struct.y_type = _TYPES[z_type]
+    sizes, shape, dtype, y_type, index = norm._call("x", x, y, gate)
     yv = gv = r_ptr = z_ptr = None
     if y is not None:
-        yv = ctypes.byref(_norm_heads("y", y, x, y.shape, y.dtype, index))
+        y_shape = y.shape
+        yv = _branch("y", y, shape, y_shape, y_type, index)
         if gate is not None:
-            gv = ctypes.byref(_norm_heads("gate", gate, x, y.shape, y.dtype, index))
+            gv = _branch("gate", gate, shape, y_shape, y_type, index)
         if out is None:
-            out = _output(x.shape, x.dtype, x, stream)
-        r_ptr = _optional("out", out, x.shape, x.dtype, index)
+            out = _new(x, shape, dtype, stream)
+            r_ptr = out.data_ptr()
+        else:
+            r_ptr = _optional("out", out, shape, dtype, index)
     elif out is not None:
         raise ValueError("out goes with y")
+    else:
+        out = x
+        if z_out is not None:
+            y_type = z_out.dtype
+            if y_type not in _TYPES:
+                raise ValueError(f"z_out has dtype {y_type}")
     if norm.pre != "none":
         if z_out is None:
-            z_out = _output(x.shape, z_type, x, stream)
-        z_ptr = _optional("z_out", z_out, x.shape, z_type, index)
+            z_out = _new(x, shape, y_type, stream)
+            z_ptr = z_out.data_ptr()
+        else:
+            z_ptr = _optional("z_out", z_out, shape, y_type, index)
     elif z_out is not None:
         raise ValueError("z_out goes with a pre norm")
-    rc = load().fem_norm_fwd(ctypes.byref(struct), x.data_ptr(), yv, gv, r_ptr, z_ptr, _stream_number(stream, index))
+    rc = load().fem_norm_fwd(norm._describe(sizes, dtype, y_type), x.data_ptr(), yv, gv, r_ptr, z_ptr, _stream_number(stream, index))
     if rc != 0:
         raise FemError("fem_norm_fwd", rc)
-    return (x if y is None else out), z_out
+    return out, z_out
 
 
 def fem_norm_bwd(norm: BlockNorm, r, y=None, gate=None, dr=None, dz=None, stream=None):
@@ -844,35 +878,30 @@ def fem_norm_bwd(norm: BlockNorm, r, y=None, gate=None, dr=None, dz=None, stream
 
     Returns (dx, dy, dgate, dw_post, db_post, dw_pre, db_pre): dy and dgate of y's shape, contiguous; the weights'
     float32 [width], summed over all rows; None for what is not there (biases' where the norm has none)."""
-    index = _norm_check(norm, r, "r")
-    if (norm.gate != "none") != (gate is not None) and y is not None or (y is None and gate is not None):
-        raise ValueError("gate goes with y and with a norm that has one")
+    sizes, shape, dtype, y_type, index = norm._call("r", r, y, gate)
     if (norm.pre != "none") != (dz is not None):
         raise ValueError("dz goes with a pre norm")
-    if y is not None and y.dtype not in _TYPES:
-        raise ValueError(f"y has dtype {y.dtype}")
-    struct = norm._struct(r, y)
-    y_type = y.dtype if y is not None else dz.dtype if dz is not None else r.dtype
-    if y is None:
+    if y is None and dz is not None:
+        y_type = dz.dtype
         if y_type not in _TYPES:
             raise ValueError(f"dz has dtype {y_type}")
-        struct.y_type = _TYPES[y_type]
-    dr_ptr = _optional("dr", dr, r.shape, r.dtype, index)
-    dz_ptr = _optional("dz", dz, r.shape, y_type, index)
-    dx = _output(r.shape, r.dtype, r, stream)
+    dr_ptr = _optional("dr", dr, shape, dtype, index)
+    dz_ptr = _optional("dz", dz, shape, y_type, index)
+    dx = _new(r, shape, dtype, stream)
     dy = dgate = yv = gv = dyv = dgv = None
     if y is not None:
-        yv = ctypes.byref(_norm_heads("y", y, r, y.shape, y_type, index))
-        dy = _output(y.shape, y_type, r, stream)
-        dyv = ctypes.byref(_norm_heads("dy", dy, r, y.shape, y_type, index))
+        y_shape = y.shape
+        yv = _branch("y", y, shape, y_shape, y_type, index)
+        dy = _new(r, y_shape, y_type, stream)
+        dyv = _fresh_branch(dy, shape, y_shape)
         if gate is not None:
-            gv = ctypes.byref(_norm_heads("gate", gate, r, y.shape, y_type, index))
-            dgate = _output(y.shape, y_type, r, stream)
-            dgv = ctypes.byref(_norm_heads("dgate", dgate, r, y.shape, y_type, index))
-    wanted = {"w_post": y is not None, "b_post": y is not None and norm.weights["b_post"] is not None,
-              "w_pre": norm.pre != "none", "b_pre": norm.pre != "none" and norm.weights["b_pre"] is not None}
-    sums = [_output((norm.width,), torch.float32, r, stream) if on else None for on in wanted.values()]
-    rc = load().fem_norm_bwd(ctypes.byref(struct), r.data_ptr(), yv, gv, dr_ptr, dz_ptr, dx.data_ptr(), dyv, dgv,
+            gv = _branch("gate", gate, shape, y_shape, y_type, index)
+            dgate = _new(r, y_shape, y_type, stream)
+            dgv = _fresh_branch(dgate, shape, y_shape)
+    pre, weights = norm.pre != "none", norm.weights
+    wanted = (y is not None, y is not None and weights["b_post"] is not None, pre, pre and weights["b_pre"] is not None)
+    sums = [_new(r, (norm.width,), torch.float32, stream) if on else None for on in wanted]
+    rc = load().fem_norm_bwd(norm._describe(sizes, dtype, y_type), r.data_ptr(), yv, gv, dr_ptr, dz_ptr, dx.data_ptr(), dyv, dgv,
                              *(None if t is None else t.data_ptr() for t in sums), _stream_number(stream, index))
     if rc != 0:
         raise FemError("fem_norm_bwd", rc)

@@ -19,7 +19,7 @@ P = lambda x: ctypes.c_void_p(x) if x else None  # noqa: E731  fake, never deref
 
 
 def heads(p=16, sb=0, st=256, sh=64):
-    return None if p is None else ctypes.byref(fem._Heads(p, sb, st, sh))
+    return None if p is None else fem._heads_bytes(p, sb, st, sh)
 
 
 def test_rope_arguments(lib):
@@ -72,6 +72,8 @@ def test_recur_arguments(lib):
     for b in bad:
         assert fwd(**b) == 1, b
     assert fwd(S=1 << 27, T=0, N=0) == 2
+    for b in (dict(ss=1 << 20), dict(us=1 << 20), dict(hs=1 << 20), dict(C=1 << 20, ss=1 << 20, us=1 << 20, hs=1 << 20)):
+        assert fwd(**b) == 2, b
     assert fwd(S=0, T=0, N=0, s=0, u=0, h=0) == 0
 
     def bwd(s=16, u=16, h=16, dh=16, st=8, off=0, S=2, T=4, N=8, C=8, type=0, mean=1, h0=0, dl=0, ds=16, du=16, dst=8, dh0=0):
@@ -80,6 +82,7 @@ def test_recur_arguments(lib):
     for b in (dict(s=0), dict(u=0), dict(h=0), dict(dh=0), dict(ds=0), dict(du=0), dict(st=-8), dict(dst=4), dict(h0=17),
               dict(dl=18), dict(dh0=18), dict(N=7), dict(mean=-1)):
         assert bwd(**b) == 1, b
+    assert bwd(st=1 << 20) == 2 and bwd(dst=1 << 20) == 2
     assert bwd(S=0, T=0, N=0) == 0
 
 
@@ -87,7 +90,7 @@ def norm(**kw):
     a = dict(B=1, T=3, H=1, d=64, x_type=0, y_type=0, post=1, pre=1, gate_act=0, scale=1.0, eps=1e-6, w_post=0, b_post=0, w_pre=0,
              b_pre=0)
     a.update(kw)
-    return ctypes.byref(fem._NormStruct(*(a[n] for n, _ in fem._NormStruct._fields_)))
+    return fem._norm_bytes(*a.values())
 
 
 BAD_NORMS = [(dict(B=-1), 1), (dict(T=-1), 1), (dict(H=0), 1), (dict(d=0), 1), (dict(x_type=1), 1), (dict(y_type=4), 1),
