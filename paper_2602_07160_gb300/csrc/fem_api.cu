@@ -1013,6 +1013,17 @@ static bool rows_ok(const void *p, int64_t stride, int N, int C, int type, bool 
   return p && element_aligned(p, type) && stride >= 0 && (!written || N == 1 || stride >= C);
 }
 
+static int recur_run(const RecurArgs &a, int type, bool mean, bool bwd, DeviceState *ds, cudaStream_t s) {
+  const size_t bytes = recur_workspace_bytes(a, type, bwd, ds->num_sms);
+  if (bytes == 0) return map_cuda(launch_recur(a, type, mean, bwd, ds->num_sms, nullptr, s));
+  void *ws = nullptr;
+  cudaError_t e = ws_alloc(ds, &ws, bytes, s);
+  if (e != cudaSuccess) return map_cuda(e);
+  e = launch_recur(a, type, mean, bwd, ds->num_sms, ws, s);
+  const cudaError_t ef = cudaFreeAsync(ws, s);
+  return map_cuda(e != cudaSuccess ? e : ef);
+}
+
 int fem_recur_fwd(const void *s, const void *u, int64_t s_stride, int64_t u_stride, const int *offsets, int S, int T,
                   int N, int C, int type, int mean, const float *h0, float *h_last, const int *state_rows,
                   int num_states, void *h, int64_t h_stride, void *stream) {
@@ -1040,7 +1051,7 @@ int fem_recur_fwd(const void *s, const void *u, int64_t s_stride, int64_t u_stri
   a.first = h0;
   a.last = h_last;
   a.err = ds->err;
-  return map_cuda(launch_recur_fwd(a, type, mean != 0, ds->num_sms, static_cast<cudaStream_t>(stream)));
+  return recur_run(a, type, mean != 0, false, ds, static_cast<cudaStream_t>(stream));
 }
 
 int fem_recur_bwd(const void *s, const void *u, const void *h, const void *dh, int64_t s_stride, int64_t u_stride,
@@ -1077,7 +1088,7 @@ int fem_recur_bwd(const void *s, const void *u, const void *h, const void *dh, i
   a.last = dh0;
   a.h0 = h0;
   a.err = ds->err;
-  return map_cuda(launch_recur_bwd(a, type, mean != 0, ds->num_sms, static_cast<cudaStream_t>(stream)));
+  return recur_run(a, type, mean != 0, true, ds, static_cast<cudaStream_t>(stream));
 }
 
 // What both passes of the norms check; `back`: the gradients' arrays are looked at as well.

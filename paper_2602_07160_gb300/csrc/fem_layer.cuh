@@ -40,8 +40,9 @@ struct RecurArgs {
   const float *h0;     // backward: what precedes h at a sequence's first step
   unsigned *err;
 };
-cudaError_t launch_recur_fwd(const RecurArgs &a, int type, bool mean, int num_sms, cudaStream_t stream);
-cudaError_t launch_recur_bwd(const RecurArgs &a, int type, bool mean, int num_sms, cudaStream_t stream);
+// `ws` holds recur_workspace_bytes() bytes, 0 where lines are not cut.
+size_t recur_workspace_bytes(const RecurArgs &a, int type, bool bwd, int num_sms);
+cudaError_t launch_recur(const RecurArgs &a, int type, bool mean, bool bwd, int num_sms, void *ws, cudaStream_t stream);
 
 struct NormArgs {
   int B, T, H, d, N, D;

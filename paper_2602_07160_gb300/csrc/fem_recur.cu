@@ -2,24 +2,27 @@
 // (include/fem.h).
 //
 // Bound by memory: s and u are read once and h written once (backward: s, dh, h and perhaps u read, ds and du
-// written).  The time axis is what is left to share out, since channels are independent but few.  A step is an affine
-// map x -> a x + b of the state, maps compose, and a stretch of steps is a map again, so a line (one sequence, one
-// group of channels) is walked by a cluster of CTAs that hold the elements they read in registers:
+// written).  The time axis is what is left to share out, since channels are independent but may be few.  A step is an
+// affine map x -> a x + b of the state, maps compose, and a stretch of steps is a map again.  A CTA walks a line (one
+// sequence, one group of channels) tile by tile:
 //
-//   each thread reads R steps of its channels and composes their map,
-//   the maps of a CTA's threads meet in shared memory, and the maps of the CTAs in each other's,
-//   each thread starts from the state before its stretch and writes its steps,
+//   each thread composes the map of R steps of its channels, which it keeps in registers,
+//   the maps of the CTA's threads meet in shared memory,
+//   each thread starts from the state before its steps and writes them,
 //
-// while the next R steps' loads are under way.  The orders are fixed, so the same inputs give the same bits.  The
-// backward pass is the same walk from the last step to the first: with m_t = a_t (dh_t + m_(t+1)) the cotangent that
-// step t sends to the state before it, the map of a step is x -> a x + a dh.
-#include <cooperative_groups.h>
+// while the next tile's copies are under way.  Where there are too few lines for the GPU they are cut into chunks: a first
+// kernel forms the chunks' maps, and the second one starts each chunk from the maps of those before it; s and u are read
+// twice, out of L2 where they fit.  (A cluster of CTAs to a line that exchanged maps through each other's shared memory
+// needed no second reading, but its step took as long as a tile's work and clusters of 16 left SMs idle: one sequence of
+// 131072 steps of 256 channels took 90 us.)  The orders are fixed, so the same inputs give the same bits.  The backward
+// pass is the same walk from the last step to the first: with m_t = a_t (dh_t + m_(t+1)) the cotangent that step t sends
+// to the state before it, the map of a step is x -> a x + a dh.
 #include <algorithm>
 
+#include "fem_launch.h"
 #include "fem_layer.cuh"
 
 namespace fem {
-namespace cg = cooperative_groups;
 
 namespace {
 
@@ -137,24 +140,6 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void *src, int by
   else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
-// A map into another CTA's shared memory, counted by its mbarrier.
-__device__ __forceinline__ uint32_t in_cta(uint32_t addr, int rank) {
-  uint32_t to;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(addr), "r"(rank));
-  return to;
-}
-__device__ __forceinline__ void send(uint32_t to, uint32_t bar, const Map<1> &m) {
-  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];" ::"r"(to),
-               "r"(__float_as_uint(m.a.x)), "r"(__float_as_uint(m.b.x)), "r"(bar)
-               : "memory");
-}
-__device__ __forceinline__ void send(uint32_t to, uint32_t bar, const Map<2> &m) {
-  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to),
-               "r"(__float_as_uint(m.a.x.x)), "r"(__float_as_uint(m.a.x.y)), "r"(__float_as_uint(m.b.x.x)),
-               "r"(__float_as_uint(m.b.x.y)), "r"(bar)
-               : "memory");
-}
-
 template <int V>
 __device__ __forceinline__ Vec<V> shift_up(Vec<V> v, int lanes) {
   Vec<V> o;
@@ -170,127 +155,249 @@ __device__ __forceinline__ Map<V> after(const Map<V> &first, const Map<V> &then)
   return {first.a * then.a, fma(then.a, first.b, then.b)};
 }
 
-constexpr int kMostCtas = 16;  // of a cluster
-constexpr int kWarps = 4;
+constexpr int kWarps = 4;  // of a CTA that has a chunk
 
-// What the kernel needs for its size; the layout of its shared memory.
-template <typename T, int V, int L, bool MEAN, bool BWD>
-struct Walk {
-  static constexpr int W = kWarps, R = BWD ? 8 : 16, G = 32 / L, U = G * W, CH = L * V, TR = U * R;  // G threads behind each other in a warp
-  static constexpr int IN = BWD ? (MEAN ? 4 : 3) : 2, OUT = BWD ? 2 : 1;  // arrays read and written
-  static constexpr int WORD = V * sizeof(T), LINE = 32 * WORD, PART = R * LINE;  // of a warp: a step of its threads, its part of a tile
-  static constexpr int STAGES = 2;
-  static constexpr int kRing = W * STAGES * IN * PART, kMaps = 2 * W * L * sizeof(Map<V>);
-  static constexpr int kCarry = 2 * L * sizeof(Vec<V>);
-  static constexpr int bytes(int ctas) { return kRing + kMaps + (ctas > 1 ? ctas * 2 * L * static_cast<int>(sizeof(Map<V>)) + 16 : kCarry); }
+template <typename T, int V, int L, int W, bool MEAN, bool BWD, int GRAIN>
+struct Tag;
+
+// The chunk of a line that a CTA has: steps [k0, k0 + n) of the sequence's `all` in the order of the walk; step k is row
+// lo + k, backward hi - 1 - k.
+struct Chunk {
+  long long lo, hi, all, k0, n;
+  int line, q, c0, row, index, count;  // of the chunks that the sequence has
+  bool ok;
 };
 
-// L lanes side by side take V channels each, U threads behind each other R steps each; GRAIN bytes a copy.
-template <typename T, int V, int L, bool MEAN, bool BWD, int GRAIN>
-__global__ void __launch_bounds__(32 * kWarps, 4) recur_walk_kernel(const RecurArgs a, int groups, int ctas) {
-  using P = Walk<T, V, L, MEAN, BWD>;
-  using F = Vec<V>;
-  using Wd = Word<T, V>;
-  constexpr int R = P::R, G = P::G, W = P::W, S = P::STAGES;
-  extern __shared__ __align__(16) char smem[];
-  Map<V> *s_map = reinterpret_cast<Map<V> *>(smem + P::kRing);  // [2][W][L]: the warps' maps
-  F *s_carry = reinterpret_cast<F *>(s_map + 2 * W * L);  // alone, [2][L]: the state before a tile
-  Map<V> *s_cta = s_map + 2 * W * L;                      // in a cluster, [2][ctas][L]: the CTAs' maps
-  const uint32_t bars = smem_u32(s_cta + 2 * ctas * L);                    // [2]: they are there
-
-  const int line = blockIdx.x / ctas, rank = blockIdx.x % ctas, q = line / groups;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, lc = lane % L, inner = lane / L, sub = warp * G + inner;
-  const int c0 = (line % groups) * P::CH, c = c0 + lc * V;
-  const bool on = c < a.C;
-  long long lo, hi;
-  int row;
-  if (!sequence(a, q, lo, hi)) {  // the same for the whole cluster
-    if (threadIdx.x == 0 && rank == 0) atomicOr(a.err, kErrPageRange);
-    return;
+// per: steps of a chunk, at least; more where a sequence is longer than the bound that the chunks were counted by.
+template <bool BWD, int CH, int TR>
+__device__ __forceinline__ Chunk chunk_of(const RecurArgs &a, int groups, int chunks, int per) {
+  Chunk k;
+  k.line = blockIdx.x / chunks;
+  k.index = blockIdx.x % chunks;
+  k.q = k.line / groups;
+  k.c0 = k.line % groups * CH;
+  k.ok = sequence(a, k.q, k.lo, k.hi);
+  if (!k.ok) {
+    if (threadIdx.x == 0 && k.index == 0) atomicOr(a.err, kErrPageRange);
+    return k;
   }
-  if (!state_row(a, q, row) && (a.first || a.last) && threadIdx.x == 0 && rank == 0) atomicOr(a.err, kErrPageRange);
-  const long long state_at = static_cast<long long>(row) * a.C + c;
-  F carry = a.first && row >= 0 && on ? load_state<V>(a.first, state_at) : F::all(0.f);
-  const long long n = hi - lo, tile = static_cast<long long>(ctas) * P::TR;
-  const int tiles = static_cast<int>((n + tile - 1) / tile);
+  if (!state_row(a, k.q, k.row) && (a.first || a.last) && threadIdx.x == 0 && k.index == 0) atomicOr(a.err, kErrPageRange);
+  k.all = k.hi - k.lo;
+  long long each = per;
+  if (each * chunks < k.all) each = ((k.all + chunks - 1) / chunks + TR - 1) / TR * TR;
+  k.count = k.all == 0 ? 1 : static_cast<int>((k.all + each - 1) / each);
+  k.k0 = k.index * each;
+  k.n = min(each, k.all - k.k0);
+  if (k.index >= k.count) k.ok = false;
+  return k;
+}
 
-  if (ctas > 1 && tiles > 0) {
-    if (threadIdx.x == 0) {
-      mbar_init(bars, 1);
-      mbar_init(bars + 8, 1);
-      fence_mbar_init();
-    }
-    cg::this_cluster().sync();  // every CTA is there, its barriers ready, before another sends to it
-  }
+// A warp's copies of IN arrays into its part of shared memory: of every array a line of L V channels for each of R steps of
+// its G threads, GRAIN bytes a copy.
+template <typename T, int V, int L, int R, int IN, int STAGES, bool BWD, int GRAIN>
+struct Ring {
+  static constexpr int G = 32 / L, WORD = V * sizeof(T), LINE = 32 * WORD, PART = R * LINE, BYTES = STAGES * IN * PART;
+  static constexpr int PIECES = PART / (32 * GRAIN), PER_LINE = LINE / GRAIN, STEP = 32 / PER_LINE;  // lines between a lane's pieces
+  static constexpr int WAY = BWD ? -static_cast<int>(sizeof(T)) : static_cast<int>(sizeof(T));
+  char *part;            // the warp's
+  uint32_t to;           // this lane's first piece
+  const char *src[IN];   // where it comes from, tile after tile
+  long long st[IN], most[IN];
+  const void *safe;      // an address to name where nothing is read
+  long long k, hop;      // the piece's step, steps between tiles
+  int c, bytes, whole;   // its byte among the channels, bytes that there are, tiles that need no look
 
-  // --- this lane's part of the copies: of every array PIECES pieces of GRAIN bytes, STEP lines between them
-  constexpr int PIECES = P::PART / (32 * GRAIN), PER_LINE = P::LINE / GRAIN, STEP = 32 / PER_LINE;
-  const int in_line = lane % PER_LINE * GRAIN, copy_sub = warp * G + in_line / (L * P::WORD);
-  const int copy_k = copy_sub * R + lane / PER_LINE, copy_c = in_line % (L * P::WORD);  // first step, byte of the channels
-  const int copy_bytes = max(0, min(GRAIN, (a.C - c0) * static_cast<int>(sizeof(T)) - copy_c));
-  const uint32_t ring = smem_u32(smem) + warp * (S * P::IN * P::PART) + lane * GRAIN;
-  char *ring_p = smem + warp * (S * P::IN * P::PART);
-  // where the piece of tile 0 is in an array whose row lags `back` behind the step's
-  const long long r0 = BWD ? hi - 1 - (static_cast<long long>(rank) * P::TR + copy_k) : lo + static_cast<long long>(rank) * P::TR + copy_k;
-  auto first_piece = [&](const void *base, long long st, int back) {
-    return static_cast<const char *>(base) + ((r0 - back) * st + c0) * static_cast<int>(sizeof(T)) + copy_c;
-  };
-  constexpr int WAY = BWD ? -static_cast<int>(sizeof(T)) : static_cast<int>(sizeof(T));
-  const char *src[P::IN] = {first_piece(a.s, a.s_st, 0)};
-  if (BWD) {
-    src[1] = first_piece(a.dh, a.dh_st, 0);
-    src[2 < P::IN ? 2 : 1] = first_piece(a.h, a.h_st, 1);  // what came before a step; before the first one h0 does
-    if (MEAN) src[P::IN - 1] = first_piece(a.u, a.u_st, 0);
-  } else {
-    src[1] = first_piece(a.u, a.u_st, 0);
+  // sub: steps between the G threads' first ones; hop: between tiles
+  __device__ __forceinline__ void start(char *smem, const RecurArgs &a, const Chunk &z, int first_sub, long long sub, long long hop_) {
+    const int lane = threadIdx.x & 31, in_line = lane % PER_LINE * GRAIN;
+    part = smem;
+    to = smem_u32(smem) + lane * GRAIN;
+    c = in_line % (L * WORD);
+    k = (first_sub + in_line / (L * WORD)) * sub + lane / PER_LINE;
+    hop = hop_;
+    bytes = max(0, min(GRAIN, (a.C - z.c0) * static_cast<int>(sizeof(T)) - c));
+    safe = a.s;
+    whole = 0;
   }
-  char *dst[2] = {const_cast<char *>(first_piece(a.out, a.out_st, 0)), const_cast<char *>(first_piece(a.du, a.du_st, 0))};
-  auto stride = [&](int slot) { return slot == 0 ? a.s_st : !BWD || (MEAN && slot == P::IN - 1) ? a.u_st : slot == 1 ? a.dh_st : a.h_st; };
-  // tiles that are whole for this CTA, the step before the first one among them
-  const long long whole_n = n - (BWD ? 1 : 0) - static_cast<long long>(rank + 1) * P::TR;
-  const int whole = GRAIN == 2 || c0 + P::CH > a.C || whole_n < 0 ? 0 : static_cast<int>(whole_n / tile) + 1;
-  auto issue = [&](int tl, int stage) {
+  // array i, whose row lags `back` behind the step's; its steps from `most` on (of the chunk) are not there
+  __device__ __forceinline__ void array(int i, const void *base, long long stride, int back, const Chunk &z, long long most_) {
+    const long long r = (BWD ? z.hi - 1 - (z.k0 + k) : z.lo + z.k0 + k) - back;
+    src[i] = static_cast<const char *>(base) + (r * stride + z.c0) * static_cast<int>(sizeof(T)) + c;
+    st[i] = stride;
+    most[i] = most_;
+  }
+  // tiles that lie wholly in the chunk for a warp whose steps of a tile end `end` behind its first one's
+  __device__ __forceinline__ void full(const RecurArgs &a, const Chunk &z, long long end, long long most_) {
+    const long long left = most_ - end;
+    whole = GRAIN == 2 || z.c0 + L * V > a.C || left < 0 ? 0 : static_cast<int>(left / hop) + 1;
+  }
+  __device__ __forceinline__ void issue(int tl, int stage) {
     if (tl < whole) {
 #pragma unroll
-      for (int s = 0; s < P::IN; ++s)
+      for (int s = 0; s < IN; ++s)
 #pragma unroll
         for (int j = 0; j < PIECES; ++j)
-          copy_async<GRAIN>(ring + (stage * P::IN + s) * P::PART + 32 * j * GRAIN, src[s] + WAY * STEP * j * stride(s), GRAIN);
+          if constexpr (GRAIN >= 4) copy_async<GRAIN>(to + (stage * IN + s) * PART + 32 * j * GRAIN, src[s] + WAY * STEP * j * st[s], GRAIN);
     } else {
-      const long long k = tl * tile + static_cast<long long>(rank) * P::TR + copy_k;
 #pragma unroll
-      for (int s = 0; s < P::IN; ++s) {
-        const long long most = BWD && s == 2 ? n - 1 : n;
+      for (int s = 0; s < IN; ++s)
 #pragma unroll
         for (int j = 0; j < PIECES; ++j) {
-          const char *from = src[s] + WAY * STEP * j * stride(s);
-          const int bytes = k + STEP * j < most ? copy_bytes : 0;
-          if constexpr (GRAIN >= 4) {
-            copy_async<GRAIN>(ring + (stage * P::IN + s) * P::PART + 32 * j * GRAIN, bytes ? from : static_cast<const char *>(a.s), bytes);
-          } else {
-            *reinterpret_cast<uint16_t *>(ring_p + (stage * P::IN + s) * P::PART + (lane + 32 * j) * GRAIN) =
-                bytes ? *reinterpret_cast<const uint16_t *>(from) : uint16_t(0);
-          }
+          const char *from = src[s] + WAY * STEP * j * st[s];
+          const int there = k + tl * hop + STEP * j < most[s] ? bytes : 0;
+          const int at = (stage * IN + s) * PART + 32 * j * GRAIN;
+          if constexpr (GRAIN >= 4) copy_async<GRAIN>(to + at, there ? from : static_cast<const char *>(safe), there);
+          else *reinterpret_cast<uint16_t *>(part + at + (threadIdx.x & 31) * GRAIN) = there ? *reinterpret_cast<const uint16_t *>(from) : uint16_t(0);
         }
-      }
     }
 #pragma unroll
-    for (int s = 0; s < P::IN; ++s) src[s] += WAY * tile * stride(s);
-  };
-  auto word = [&](int stage, int slot, int i) {
-    return *reinterpret_cast<const Wd *>(ring_p + (stage * P::IN + slot) * P::PART + i * P::LINE + lane * P::WORD);
-  };
+    for (int s = 0; s < IN; ++s) src[s] += WAY * hop * st[s];
+  }
+  __device__ __forceinline__ Word<T, V> word(int stage, int slot, int i) const {
+    return *reinterpret_cast<const Word<T, V> *>(part + (stage * IN + slot) * PART + i * LINE + (threadIdx.x & 31) * WORD);
+  }
+};
+
+// With the maps of the threads before it in the warp; the warp's own to shared memory.
+template <int V, int L>
+__device__ __forceinline__ void meet(Map<V> &m, Map<V> *s_map) {
+  constexpr int G = 32 / L;
+  const int lane = threadIdx.x & 31, inner = lane / L;
+#pragma unroll
+  for (int o = 1; o < G; o *= 2) {
+    const Map<V> before = shift_up(m, o * L);
+    if (inner >= o) m = after(before, m);
+  }
+  if (inner == G - 1) s_map[(threadIdx.x >> 5) * L + lane % L] = m;
+}
+
+// The maps of the chunks but the last of each line, [line][chunks][L].  No thread waits for another: each walks a stretch of
+// its own.
+template <typename T, int V, int L, bool MEAN, bool BWD, int GRAIN>
+__global__ void __launch_bounds__(32 * kWarps, 6) recur_maps_kernel(const RecurArgs a, int groups, int chunks, int per, Map<V> *maps) {
+  constexpr int W = kWarps, R = 8, U = 32 / L * W, S = 3;
+  using F = Vec<V>;
+  using Rg = Ring<T, V, L, R, 2, S, BWD, GRAIN>;
+  extern __shared__ __align__(16) char smem[];
+  __shared__ Map<V> s_map[W * L];
+  grid_dep_launch_dependents();
+  const Chunk z = chunk_of<BWD, L * V, (BWD ? 8 : 16) * U>(a, groups, chunks, per);
+  if (!z.ok || z.index == z.count - 1) return;  // such a chunk has a multiple of R U steps
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long each = z.n / U;
+  Rg ring;
+  ring.start(smem + warp * Rg::BYTES, a, z, warp * (32 / L), each, R);
+  ring.array(0, a.s, a.s_st, 0, z, z.n);
+  if (BWD) ring.array(1, a.dh, a.dh_st, 0, z, z.n);
+  else ring.array(1, a.u, a.u_st, 0, z, z.n);
+  const int tiles = static_cast<int>(each / R);
+  ring.whole = GRAIN == 2 || z.c0 + L * V > a.C ? 0 : tiles;
   for (int tl = 0; tl < S - 1; ++tl) {
-    if (tl < tiles) issue(tl, tl);
+    if (tl < tiles) ring.issue(tl, tl);
     copy_commit();
   }
-
+  Map<V> m = {F::all(1.f), F::all(0.f)};
   int stage = 0;
   for (int tl = 0; tl < tiles; ++tl) {
-    const int buf = tl & 1;
-    if (tl + S - 1 < tiles) issue(tl + S - 1, stage == 0 ? S - 1 : stage - 1);  // over the tile before, which this warp has read
+    if (tl + S - 1 < tiles) ring.issue(tl + S - 1, stage == 0 ? S - 1 : stage - 1);
     copy_commit();
     copy_wait<S - 1>();
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      F d, w;
+      decay<V>(ring.word(stage, 0, i).get(), d, w);
+      const F v = ring.word(stage, 1, i).get();
+      m.b = BWD ? d * (v + m.b) : fma(d, m.b, MEAN ? w * v : v);
+      m.a = m.a * d;
+    }
+    stage = stage == S - 1 ? 0 : stage + 1;
+    __syncwarp();
+  }
+  meet<V, L>(m, s_map);
+  __syncthreads();
+  if (threadIdx.x >= L) return;
+  Map<V> whole = s_map[lane];
+#pragma unroll
+  for (int i = 1; i < W; ++i) whole = after(whole, s_map[i * L + lane]);
+  maps[(static_cast<long long>(z.line) * chunks + z.index) * L + lane] = whole;
+}
+
+// Walks a chunk, which is the whole line where there is one.  L lanes side by side take V channels each, 32 W / L threads
+// behind each other R steps each.
+template <typename T, int V, int L, int W, bool MEAN, bool BWD, int GRAIN>
+struct Walk {
+  static constexpr int R = BWD ? 8 : 16, G = 32 / L, U = G * W, TR = U * R;
+  static constexpr int IN = BWD ? (MEAN ? 4 : 3) : 2, OUT = BWD ? 2 : 1;  // arrays read and written
+  using Rg = Ring<T, V, L, R, IN, 2, BWD, GRAIN>;
+  static constexpr int kMaps = 2 * W * L * sizeof(Map<V>), BYTES = W * Rg::BYTES + kMaps + 2 * L * sizeof(Vec<V>);
+};
+
+template <typename T, int V, int L, int W, bool MEAN, bool BWD, int GRAIN>
+__global__ void __launch_bounds__(32 * W, 16 / W)
+    recur_walk_kernel(const RecurArgs a, int groups, int chunks, int per, const Map<V> *maps) {
+  using P = Walk<T, V, L, W, MEAN, BWD, GRAIN>;
+  using F = Vec<V>;
+  using Wd = Word<T, V>;
+  using Rg = typename P::Rg;
+  constexpr int R = P::R, G = P::G;
+  extern __shared__ __align__(16) char smem[];
+  Map<V> *s_map = reinterpret_cast<Map<V> *>(smem + W * Rg::BYTES);  // [2][W][L]: the warps' maps
+  F *s_carry = reinterpret_cast<F *>(s_map + 2 * W * L);             // [2][L]: the state before a tile
+
+  const Chunk z = chunk_of<BWD, L * V, P::TR>(a, groups, chunks, per);
+  if (!z.ok) {
+    if (chunks > 1) grid_dep_wait();
+    return;
+  }
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, lc = lane % L, inner = lane / L, sub = warp * G + inner;
+  const int c = z.c0 + lc * V;
+  const bool on = c < a.C, end = warp == W - 1 && inner == G - 1;
+  const long long state_at = static_cast<long long>(z.row) * a.C + c;
+  const int tiles = static_cast<int>((z.n + P::TR - 1) / P::TR);
+
+  Rg ring;
+  ring.start(smem + warp * Rg::BYTES, a, z, warp * G, R, P::TR);
+  ring.array(0, a.s, a.s_st, 0, z, z.n);
+  if (BWD) {
+    ring.array(1, a.dh, a.dh_st, 0, z, z.n);
+    ring.array(2 % P::IN, a.h, a.h_st, 1, z, min(z.n, z.all - 1 - z.k0));  // what came before a step; before the first one h0 does
+    if (MEAN) ring.array(P::IN - 1, a.u, a.u_st, 0, z, z.n);
+  } else {
+    ring.array(1, a.u, a.u_st, 0, z, z.n);
+  }
+  ring.full(a, z, P::TR, BWD ? min(z.n, z.all - 1 - z.k0) : z.n);
+  char *dst[2];
+  {
+    const long long r = BWD ? z.hi - 1 - (z.k0 + ring.k) : z.lo + z.k0 + ring.k;
+    dst[0] = static_cast<char *>(a.out) + (r * a.out_st + z.c0) * static_cast<int>(sizeof(T)) + ring.c;
+    dst[1] = static_cast<char *>(a.du) + (r * a.du_st + z.c0) * static_cast<int>(sizeof(T)) + ring.c;
+  }
+  if (tiles > 0) ring.issue(0, 0);
+  copy_commit();
+
+  F carry = a.first && z.row >= 0 && on ? load_state<V>(a.first, state_at) : F::all(0.f);
+  if (chunks > 1) {
+    grid_dep_wait();  // the maps, and whatever ran before them
+    if (z.index > 0) {  // the chunks before this one, a stretch of them a thread
+      Map<V> m = {F::all(1.f), F::all(0.f)};
+      const Map<V> *o = maps + static_cast<long long>(z.line) * chunks * L + lc;
+      const int from = z.index * sub / P::U, to = z.index * (sub + 1) / P::U;
+#pragma unroll 8
+      for (int i = from; i < to; ++i) m = after(m, o[i * L]);
+      meet<V, L>(m, s_map);
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < W; ++i) carry = fma(s_map[i * L + lc].a, carry, s_map[i * L + lc].b);
+      __syncthreads();
+    }
+  }
+
+  for (int tl = 0; tl < tiles; ++tl) {
+    const int stage = tl & 1;
+    if (tl + 1 < tiles) ring.issue(tl + 1, stage ^ 1);  // over the tile before, which this warp has read
+    copy_commit();
+    copy_wait<1>();
     __syncwarp();
     // the map of the thread's steps: rates of zero behind the end change nothing
     F d[R], w[R];
@@ -298,74 +405,44 @@ __global__ void __launch_bounds__(32 * kWarps, 4) recur_walk_kernel(const RecurA
     Map<V> m = {F::all(1.f), F::all(0.f)};
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      decay<V>(word(stage, 0, i).get(), d[i], w[i]);
+      decay<V>(ring.word(stage, 0, i).get(), d[i], w[i]);
       if (BWD) {
-        g[i] = word(stage, 1, i);
-        h[i] = word(stage, 2, i);
-        if (MEAN) v[i] = word(stage, P::IN - 1, i);
+        g[i] = ring.word(stage, 1, i);
+        h[i] = ring.word(stage, 2 % P::IN, i);
+        if (MEAN) v[i] = ring.word(stage, P::IN - 1, i);
         m.b = d[i] * (g[i].get() + m.b);
       } else {
-        v[i] = word(stage, 1, i);
+        v[i] = ring.word(stage, 1, i);
         if (MEAN) w[i] = w[i] * v[i].get();
         m.b = fma(d[i], m.b, MEAN ? w[i] : v[i].get());
       }
       m.a = m.a * d[i];
     }
-    // with those of the threads before it in the warp
-#pragma unroll
-    for (int o = 1; o < G; o *= 2) {
-      const Map<V> before = shift_up(m, o * L);
-      if (inner >= o) m = after(before, m);
-    }
-    if (inner == G - 1) s_map[(buf * W + warp) * L + lc] = m;
+    meet<V, L>(m, s_map + stage * W * L);
     __syncthreads();
-    F x = carry;
-    if (ctas > 1) {
-      if (warp == W - 1 && inner == G - 1) {  // the CTA's map, to every CTA
-        Map<V> all = s_map[buf * W * L + lc];
-#pragma unroll
-        for (int i = 1; i < W; ++i) all = after(all, s_map[(buf * W + i) * L + lc]);
-        const uint32_t to = smem_u32(s_cta + (buf * ctas + rank) * L + lc);
-#pragma unroll 4
-        for (int r = 0; r < ctas; ++r) send(in_cta(to, r), in_cta(bars + 8 * buf, r), all);
-      }
-      if (threadIdx.x == 0) mbar_arrive_expect_tx(bars + 8 * buf, ctas * L * sizeof(Map<V>));
-      if (!mbar_wait(bars + 8 * buf, (tl >> 1) & 1, a.err, kErrWaitTma)) {
-        copy_wait<0>();
-        cg::this_cluster().sync();  // no CTA leaves while another may send to it
-        return;
-      }
-      const Map<V> *o = s_cta + buf * ctas * L + lc;
-#pragma unroll 4
-      for (int r = 0; r < rank; ++r, o += L) x = fma(o->a, x, o->b);
-      carry = x;
-#pragma unroll 4
-      for (int r = rank; r < ctas; ++r, o += L) carry = fma(o->a, carry, o->b);
-    } else if (tl > 0) {
-      x = s_carry[(buf ^ 1) * L + lc];
-    }
+    F x = tl == 0 ? carry : s_carry[(stage ^ 1) * L + lc];
     {
-      const Map<V> *o = s_map + buf * W * L + lc;
+      const Map<V> *o = s_map + stage * W * L + lc;
 #pragma unroll 4
       for (int i = 0; i < warp; ++i, o += L) x = fma(o->a, x, o->b);
     }
-    if (ctas == 1 && warp == W - 1 && inner == G - 1) {  // read behind the next tile's barrier
+    if (end) {  // read behind the next tile's barrier
       carry = fma(m.a, x, m.b);
-      s_carry[buf * L + lc] = carry;
+      s_carry[stage * L + lc] = carry;
     }
     if (G > 1) {
       const Map<V> before = shift_up(m, L);
       if (inner > 0) x = fma(before.a, x, before.b);
     }
     // the thread's steps, over the first inputs, which its warp has read, and from there in whole lines
-    char *out_p = ring_p + stage * P::IN * P::PART;
-    const long long k0 = tl * tile + static_cast<long long>(rank) * P::TR;
-    auto put = [&](int slot, int i, F y) { *reinterpret_cast<Wd *>(out_p + slot * P::PART + i * P::LINE + lane * P::WORD) = Wd::of(y); };
+    char *out_p = ring.part + stage * P::IN * Rg::PART;
+    const long long k0 = static_cast<long long>(tl) * P::TR;
+    auto put = [&](int slot, int i, F y) { *reinterpret_cast<Wd *>(out_p + slot * Rg::PART + i * Rg::LINE + lane * Rg::WORD) = Wd::of(y); };
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       if (BWD) {
         F before = h[i].get();
-        if (a.h0 && on && k0 + sub * R + i == n - 1) before = load_state<V>(a.h0, static_cast<long long>(q) * a.C + c);
+        if (a.h0 && on && z.k0 + k0 + sub * R + i == z.all - 1) before = load_state<V>(a.h0, static_cast<long long>(z.q) * a.C + c);
         const F total = g[i].get() + x;
         x = d[i] * total;
         put(0, i, MEAN ? x * fma(before, F::all(-1.f), v[i].get()) : x * (before * F::all(-1.f)));
@@ -380,48 +457,25 @@ __global__ void __launch_bounds__(32 * kWarps, 4) recur_walk_kernel(const RecurA
     for (int o = 0; o < P::OUT; ++o) {
       const long long st = o ? a.du_st : a.out_st;
 #pragma unroll
-      for (int j = 0; j < PIECES; ++j) {
-        const char *from = out_p + o * P::PART + (lane + 32 * j) * GRAIN;
-        char *to = dst[o] + WAY * STEP * j * st;
-        if (tl < whole || (k0 + copy_k + STEP * j < n && copy_bytes == GRAIN)) {
+      for (int j = 0; j < Rg::PIECES; ++j) {
+        const char *from = out_p + o * Rg::PART + (lane + 32 * j) * GRAIN;
+        char *to = dst[o] + Rg::WAY * Rg::STEP * j * st;
+        const bool there = tl < ring.whole || k0 + ring.k + Rg::STEP * j < z.n;
+        if (there && (tl < ring.whole || ring.bytes == GRAIN)) {
           if (GRAIN == 16) *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(from);
           else if (GRAIN == 4) *reinterpret_cast<uint32_t *>(to) = *reinterpret_cast<const uint32_t *>(from);
           else *reinterpret_cast<uint16_t *>(to) = *reinterpret_cast<const uint16_t *>(from);
-        } else if (k0 + copy_k + STEP * j < n) {
-          for (int e = 0; e < copy_bytes; e += sizeof(T)) *reinterpret_cast<T *>(to + e) = *reinterpret_cast<const T *>(from + e);
+        } else if (there) {
+          for (int e = 0; e < ring.bytes; e += sizeof(T)) *reinterpret_cast<T *>(to + e) = *reinterpret_cast<const T *>(from + e);
         }
       }
-      dst[o] += WAY * tile * st;
+      dst[o] += Rg::WAY * P::TR * st;
     }
-    stage = stage == S - 1 ? 0 : stage + 1;
     __syncwarp();
   }
-  if (rank == 0 && warp == W - 1 && inner == G - 1 && on && a.last && row >= 0)
+  if (z.index == z.count - 1 && end && on && a.last && z.row >= 0)
 #pragma unroll
     for (int i = 0; i < V; ++i) a.last[state_at + i] = carry.get(i);
-}
-
-template <typename T, int V, int L, bool MEAN, bool BWD, int GRAIN>
-cudaError_t launch_walk(const RecurArgs &a, int ctas, cudaStream_t stream) {
-  using P = Walk<T, V, L, MEAN, BWD>;
-  auto *kernel = recur_walk_kernel<T, V, L, MEAN, BWD, GRAIN>;
-  const int groups = (a.C + P::CH - 1) / P::CH;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(a.S) * groups * ctas);
-  cfg.blockDim = dim3(32 * P::W);
-  cfg.dynamicSmemBytes = P::bytes(ctas);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = ctas;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = ctas > 1 ? 1 : 0;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, P::bytes(kMostCtas));
-  if (e == cudaSuccess && ctas > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-  if (e != cudaSuccess) return e;
-  return cudaLaunchKernelEx(&cfg, kernel, a, groups, ctas);
 }
 
 // Sequences of few steps: a thread walks V channels of one, four steps' loads under way.
@@ -490,18 +544,65 @@ cudaError_t launch_few(const RecurArgs &a, cudaStream_t stream) {
   return cudaGetLastError();
 }
 
-template <typename T, int V, bool MEAN, bool BWD, int GRAIN>
-cudaError_t launch_rule(const RecurArgs &a, int num_sms, cudaStream_t stream) {
-  if (a.T <= kFewSteps) return launch_few<T, V, MEAN, BWD>(a, stream);
-  auto lines = [&](int lanes) { return static_cast<long long>(a.S) * ((a.C + lanes * V - 1) / (lanes * V)); };
+// How a call's lines are shared out: `lanes` to a line's channels, CTAs of `warps`, chunks of `per` steps.  No lanes: few
+// steps, a thread to a line.
+struct Split {
+  int lanes, warps, chunks, per;
+};
+
+// A line to a CTA where that fills the GPU, 16 warps an SM, to three fifths in its last round (64 or 32 bytes of channels
+// a row where there are no more), in CTAs of 8 warps if those fill it better; otherwise chunks, three to four CTAs an SM.
+// Eight sequences of 8192 steps of 2048 channels of bf16, 256 lines: forward 140 us in CTAs of 8 warps, 163 of 4, 207 in
+// chunks; backward 253, 303, 336.  One of 131072 steps of 256 channels, 4 lines: forward 68 us in 128 chunks, 78 in 64,
+// 74 in 160; backward 88, 107, 103.
+Split split_of(const RecurArgs &a, int V, bool bwd, int num_sms) {
+  if (a.T <= kFewSteps) return {0, 0, 0, 0};
   int lanes = 32;
-  while (lanes > 8 && lines(lanes) * kMostCtas < 2 * num_sms) lanes /= 2;
-  const long long rows = 32 / lanes * kWarps * (BWD ? 8 : 16);  // of a CTA in a tile
-  const long long want = (BWD ? 4 : 7) * num_sms / lines(lanes), most = (a.T + rows - 1) / rows;
-  const int ctas = static_cast<int>(std::max(1ll, std::min({want, most, static_cast<long long>(kMostCtas)})));
-  if (lanes == 32) return launch_walk<T, V, 32, MEAN, BWD, GRAIN>(a, ctas, stream);
-  if (lanes == 16) return launch_walk<T, V, 16, MEAN, BWD, GRAIN>(a, ctas, stream);
-  return launch_walk<T, V, 8, MEAN, BWD, GRAIN>(a, ctas, stream);
+  while (lanes > 8 && a.C <= lanes * V / 2) lanes /= 2;
+  const long long lines = static_cast<long long>(a.S) * ((a.C + lanes * V - 1) / (lanes * V));
+  auto fill = [&](int warps) {
+    const long long round = 16ll / warps * num_sms;
+    return static_cast<double>(lines) / static_cast<double>((lines + round - 1) / round * round);
+  };
+  const int tile = 32 / lanes * kWarps * (bwd ? 8 : 16);
+  const long long chunks = std::min(7ll * num_sms / 2 / lines, (a.T + 2ll * tile - 1) / (2 * tile));
+  const double four = fill(4), eight = lanes == 32 ? fill(8) : 0;
+  if (std::max(four, eight) >= 0.6 || chunks < 2) return {lanes, eight > four + 0.05 ? 8 : 4, 1, 0};
+  const long long per = ((a.T + chunks - 1) / chunks + tile - 1) / tile * tile;
+  return {lanes, kWarps, static_cast<int>((a.T + per - 1) / per), static_cast<int>(per)};
+}
+
+template <typename T, int V, int L, int W, bool MEAN, bool BWD, int GRAIN>
+cudaError_t launch_walk(const RecurArgs &a, const Split &sp, void *ws, cudaStream_t stream) {
+  using P = Walk<T, V, L, W, MEAN, BWD, GRAIN>;
+  auto *kernel = recur_walk_kernel<T, V, L, W, MEAN, BWD, GRAIN>;
+  const int groups = (a.C + L * V - 1) / (L * V), chunks = sp.chunks;
+  const unsigned blocks = static_cast<unsigned>(a.S) * groups * chunks;
+  Map<V> *maps = static_cast<Map<V> *>(ws);
+  int per_sm = 0;
+  cudaError_t e = resident_blocks<Tag<T, V, L, W, MEAN, BWD, GRAIN>>(kernel, 32 * W, P::BYTES, &per_sm);
+  if constexpr (W == kWarps) {
+    if (e == cudaSuccess && chunks > 1) {
+      constexpr int ring = W * Ring<T, V, L, 8, 2, 3, BWD, GRAIN>::BYTES;
+      static_assert(ring <= 40 * 1024, "no leave to ask for");
+      recur_maps_kernel<T, V, L, MEAN, BWD, GRAIN><<<blocks, 32 * W, ring, stream>>>(a, groups, chunks, sp.per, maps);
+      e = cudaGetLastError();
+    }
+  }
+  if (e != cudaSuccess) return e;
+  return launch_kernel(kernel, dim3(blocks), dim3(32 * W), P::BYTES, stream, chunks > 1, a, groups, chunks,
+                       chunks > 1 ? sp.per : 0x7fffff00, static_cast<const Map<V> *>(maps));
+}
+
+template <typename T, int V, bool MEAN, bool BWD, int GRAIN>
+cudaError_t launch_lanes(const RecurArgs &a, int num_sms, void *ws, cudaStream_t stream) {
+  const Split sp = split_of(a, V, BWD, num_sms);
+  if (sp.lanes == 0) return launch_few<T, V, MEAN, BWD>(a, stream);
+  if (sp.lanes == 32)
+    return sp.warps == 8 ? launch_walk<T, V, 32, 8, MEAN, BWD, GRAIN>(a, sp, ws, stream)
+                         : launch_walk<T, V, 32, 4, MEAN, BWD, GRAIN>(a, sp, ws, stream);
+  if (sp.lanes == 16) return launch_walk<T, V, 16, 4, MEAN, BWD, GRAIN>(a, sp, ws, stream);
+  return launch_walk<T, V, 8, 4, MEAN, BWD, GRAIN>(a, sp, ws, stream);
 }
 
 // Whether every row starts on a multiple of `bytes`.
@@ -513,28 +614,35 @@ bool starts_at(const RecurArgs &a, int bytes, int size) {
   return ok;
 }
 
+// Channels to a lane: two of bf16 where every row starts on a multiple of them.
+int channels(const RecurArgs &a, int type) { return type != kTypeF32 && a.C % 2 == 0 && starts_at(a, 4, 2) ? 2 : 1; }
+
 template <bool MEAN, bool BWD>
-cudaError_t launch_mean(const RecurArgs &a, int type, int num_sms, cudaStream_t stream) {
+cudaError_t launch_mean(const RecurArgs &a, int type, int num_sms, void *ws, cudaStream_t stream) {
   if (type == kTypeF32)
-    return starts_at(a, 16, 4) ? launch_rule<float, 1, MEAN, BWD, 16>(a, num_sms, stream)
-                               : launch_rule<float, 1, MEAN, BWD, 4>(a, num_sms, stream);
-  if (a.C % 2 == 0 && starts_at(a, 16, 2)) return launch_rule<__nv_bfloat16, 2, MEAN, BWD, 16>(a, num_sms, stream);
-  if (a.C % 2 == 0 && starts_at(a, 4, 2)) return launch_rule<__nv_bfloat16, 2, MEAN, BWD, 4>(a, num_sms, stream);
-  return launch_rule<__nv_bfloat16, 1, MEAN, BWD, 2>(a, num_sms, stream);
+    return starts_at(a, 16, 4) ? launch_lanes<float, 1, MEAN, BWD, 16>(a, num_sms, ws, stream)
+                               : launch_lanes<float, 1, MEAN, BWD, 4>(a, num_sms, ws, stream);
+  if (channels(a, type) == 1) return launch_lanes<__nv_bfloat16, 1, MEAN, BWD, 2>(a, num_sms, ws, stream);
+  return starts_at(a, 16, 2) ? launch_lanes<__nv_bfloat16, 2, MEAN, BWD, 16>(a, num_sms, ws, stream)
+                             : launch_lanes<__nv_bfloat16, 2, MEAN, BWD, 4>(a, num_sms, ws, stream);
 }
 
 template <bool BWD>
-cudaError_t launch(const RecurArgs &a, int type, bool mean, int num_sms, cudaStream_t stream) {
-  return mean ? launch_mean<true, BWD>(a, type, num_sms, stream) : launch_mean<false, BWD>(a, type, num_sms, stream);
+size_t workspace(const RecurArgs &a, int type, int num_sms) {
+  const int V = channels(a, type);
+  const Split sp = split_of(a, V, BWD, num_sms);
+  if (sp.chunks <= 1) return 0;
+  return static_cast<size_t>(a.S) * ((a.C + sp.lanes * V - 1) / (sp.lanes * V)) * sp.chunks * sp.lanes * V * 8;
 }
 
 }  // namespace
 
-cudaError_t launch_recur_fwd(const RecurArgs &a, int type, bool mean, int num_sms, cudaStream_t stream) {
-  return launch<false>(a, type, mean, num_sms, stream);
+size_t recur_workspace_bytes(const RecurArgs &a, int type, bool bwd, int num_sms) {
+  return bwd ? workspace<true>(a, type, num_sms) : workspace<false>(a, type, num_sms);
 }
-cudaError_t launch_recur_bwd(const RecurArgs &a, int type, bool mean, int num_sms, cudaStream_t stream) {
-  return launch<true>(a, type, mean, num_sms, stream);
+cudaError_t launch_recur(const RecurArgs &a, int type, bool mean, bool bwd, int num_sms, void *ws, cudaStream_t stream) {
+  if (bwd) return mean ? launch_mean<true, true>(a, type, num_sms, ws, stream) : launch_mean<false, true>(a, type, num_sms, ws, stream);
+  return mean ? launch_mean<true, false>(a, type, num_sms, ws, stream) : launch_mean<false, false>(a, type, num_sms, ws, stream);
 }
 
 }  // namespace fem
