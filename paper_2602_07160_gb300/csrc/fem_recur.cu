@@ -18,6 +18,7 @@
 // pass is the same walk from the last step to the first: with m_t = a_t (dh_t + m_(t+1)) the cotangent that step t sends
 // to the state before it, the map of a step is x -> a x + a dh.
 #include <algorithm>
+#include <cmath>
 
 #include "fem_launch.h"
 #include "fem_layer.cuh"
@@ -71,6 +72,12 @@ struct Word<float, 1> {
   __device__ __forceinline__ Vec<1> get() const { return {w}; }
   __device__ __forceinline__ static Word of(Vec<1> v) { return {v.x}; }
 };
+template <>
+struct Word<float, 2> {
+  float2 w;
+  __device__ __forceinline__ Vec<2> get() const { return {w}; }
+  __device__ __forceinline__ static Word of(Vec<2> v) { return {v.x}; }
+};
 
 // a = e^(-s) and w = 1 - a.  For s in [0, 1/8) w = s p(s), p the cubic with p(0) = 1 that is off least over the interval
 // (by 8e-8 of w; coefficients by linear programming on the condition itself), and a is 1 - w, off by 2^-25 and little
@@ -119,11 +126,12 @@ __device__ __forceinline__ bool state_row(const RecurArgs &a, int q, int &row) {
   return false;
 }
 
+// `there` of V channels of a state; the others are 0.
 template <int V>
-__device__ __forceinline__ Vec<V> load_state(const float *p, long long at) {
+__device__ __forceinline__ Vec<V> load_state(const float *p, long long at, int there) {
   Vec<V> x;
 #pragma unroll
-  for (int i = 0; i < V; ++i) x.set(i, p[at + i]);
+  for (int i = 0; i < V; ++i) x.set(i, i < there ? p[at + i] : 0.f);
   return x;
 }
 
@@ -156,6 +164,11 @@ __device__ __forceinline__ Map<V> after(const Map<V> &first, const Map<V> &then)
 }
 
 constexpr int kWarps = 4;  // of a CTA that has a chunk
+// Steps of a thread in a tile: what registers allow, and in fp32 as many bytes of shared memory.
+template <typename T, bool BWD>
+constexpr int kSteps = (BWD ? 8 : 16) * 2 / static_cast<int>(sizeof(T));
+template <typename T>
+constexpr int kMapSteps = 16 / static_cast<int>(sizeof(T));
 
 template <typename T, int V, int L, int W, bool MEAN, bool BWD, int GRAIN>
 struct Tag;
@@ -197,32 +210,40 @@ __device__ __forceinline__ Chunk chunk_of(const RecurArgs &a, int groups, int ch
 template <typename T, int V, int L, int R, int IN, int STAGES, bool BWD, int GRAIN>
 struct Ring {
   static constexpr int G = 32 / L, WORD = V * sizeof(T), LINE = 32 * WORD, PART = R * LINE, BYTES = STAGES * IN * PART;
-  static constexpr int PIECES = PART / (32 * GRAIN), PER_LINE = LINE / GRAIN, STEP = 32 / PER_LINE;  // lines between a lane's pieces
+  // A lane has PIECES copies of an array and tile: SPLIT in a line, where that is longer than 32, then STEP lines on
+  static constexpr int PIECES = PART / (32 * GRAIN), PER_LINE = LINE / GRAIN, SPLIT = PER_LINE > 32 ? PER_LINE / 32 : 1, STEP = 32 * SPLIT / PER_LINE;
   static constexpr int WAY = BWD ? -static_cast<int>(sizeof(T)) : static_cast<int>(sizeof(T));
-  char *part;            // the warp's
-  uint32_t to;           // this lane's first piece
-  const char *src[IN];   // where it comes from, tile after tile
+  char *part;                    // the warp's
+  uint32_t to;                   // this lane's first piece
+  const char *src[IN][SPLIT];    // where it comes from, tile after tile
   long long st[IN], most[IN];
-  const void *safe;      // an address to name where nothing is read
-  long long k, hop;      // the piece's step, steps between tiles
-  int c, bytes, whole;   // its byte among the channels, bytes that there are, tiles that need no look
+  const void *safe;              // an address to name where nothing is read
+  long long k[SPLIT], hop;       // the pieces' steps; steps between tiles
+  int c[SPLIT], bytes[SPLIT], whole;  // their byte among the channels, bytes that there are; tiles that need no look
 
   // sub: steps between the G threads' first ones; hop: between tiles
   __device__ __forceinline__ void start(char *smem, const RecurArgs &a, const Chunk &z, int first_sub, long long sub, long long hop_) {
-    const int lane = threadIdx.x & 31, in_line = lane % PER_LINE * GRAIN;
+    const int lane = threadIdx.x & 31;
     part = smem;
     to = smem_u32(smem) + lane * GRAIN;
-    c = in_line % (L * WORD);
-    k = (first_sub + in_line / (L * WORD)) * sub + lane / PER_LINE;
     hop = hop_;
-    bytes = max(0, min(GRAIN, (a.C - z.c0) * static_cast<int>(sizeof(T)) - c));
+#pragma unroll
+    for (int p = 0; p < SPLIT; ++p) {
+      const int in_line = (lane + 32 * p) % PER_LINE * GRAIN;
+      c[p] = in_line % (L * WORD);
+      k[p] = (first_sub + in_line / (L * WORD)) * sub + lane / PER_LINE;
+      bytes[p] = max(0, min(GRAIN, (a.C - z.c0) * static_cast<int>(sizeof(T)) - c[p]));
+    }
     safe = a.s;
     whole = 0;
   }
+  // the row of the chunk's step k
+  __device__ __forceinline__ static long long row(const Chunk &z, long long k) { return BWD ? z.hi - 1 - (z.k0 + k) : z.lo + z.k0 + k; }
   // array i, whose row lags `back` behind the step's; its steps from `most` on (of the chunk) are not there
   __device__ __forceinline__ void array(int i, const void *base, long long stride, int back, const Chunk &z, long long most_) {
-    const long long r = (BWD ? z.hi - 1 - (z.k0 + k) : z.lo + z.k0 + k) - back;
-    src[i] = static_cast<const char *>(base) + (r * stride + z.c0) * static_cast<int>(sizeof(T)) + c;
+#pragma unroll
+    for (int p = 0; p < SPLIT; ++p)
+      src[i][p] = static_cast<const char *>(base) + ((row(z, k[p]) - back) * stride + z.c0) * static_cast<int>(sizeof(T)) + c[p];
     st[i] = stride;
     most[i] = most_;
   }
@@ -237,21 +258,24 @@ struct Ring {
       for (int s = 0; s < IN; ++s)
 #pragma unroll
         for (int j = 0; j < PIECES; ++j)
-          if constexpr (GRAIN >= 4) copy_async<GRAIN>(to + (stage * IN + s) * PART + 32 * j * GRAIN, src[s] + WAY * STEP * j * st[s], GRAIN);
+          if constexpr (GRAIN >= 4)
+            copy_async<GRAIN>(to + (stage * IN + s) * PART + 32 * j * GRAIN, src[s][j % SPLIT] + WAY * STEP * (j / SPLIT) * st[s], GRAIN);
     } else {
 #pragma unroll
       for (int s = 0; s < IN; ++s)
 #pragma unroll
         for (int j = 0; j < PIECES; ++j) {
-          const char *from = src[s] + WAY * STEP * j * st[s];
-          const int there = k + tl * hop + STEP * j < most[s] ? bytes : 0;
+          const char *from = src[s][j % SPLIT] + WAY * STEP * (j / SPLIT) * st[s];
+          const int there = k[j % SPLIT] + tl * hop + STEP * (j / SPLIT) < most[s] ? bytes[j % SPLIT] : 0;
           const int at = (stage * IN + s) * PART + 32 * j * GRAIN;
           if constexpr (GRAIN >= 4) copy_async<GRAIN>(to + at, there ? from : static_cast<const char *>(safe), there);
           else *reinterpret_cast<uint16_t *>(part + at + (threadIdx.x & 31) * GRAIN) = there ? *reinterpret_cast<const uint16_t *>(from) : uint16_t(0);
         }
     }
 #pragma unroll
-    for (int s = 0; s < IN; ++s) src[s] += WAY * hop * st[s];
+    for (int s = 0; s < IN; ++s)
+#pragma unroll
+      for (int p = 0; p < SPLIT; ++p) src[s][p] += WAY * hop * st[s];
   }
   __device__ __forceinline__ Word<T, V> word(int stage, int slot, int i) const {
     return *reinterpret_cast<const Word<T, V> *>(part + (stage * IN + slot) * PART + i * LINE + (threadIdx.x & 31) * WORD);
@@ -275,13 +299,13 @@ __device__ __forceinline__ void meet(Map<V> &m, Map<V> *s_map) {
 // its own.
 template <typename T, int V, int L, bool MEAN, bool BWD, int GRAIN>
 __global__ void __launch_bounds__(32 * kWarps, 6) recur_maps_kernel(const RecurArgs a, int groups, int chunks, int per, Map<V> *maps) {
-  constexpr int W = kWarps, R = 8, U = 32 / L * W, S = 3;
+  constexpr int W = kWarps, R = kMapSteps<T>, U = 32 / L * W, S = 3;
   using F = Vec<V>;
   using Rg = Ring<T, V, L, R, 2, S, BWD, GRAIN>;
   extern __shared__ __align__(16) char smem[];
   __shared__ Map<V> s_map[W * L];
   grid_dep_launch_dependents();
-  const Chunk z = chunk_of<BWD, L * V, (BWD ? 8 : 16) * U>(a, groups, chunks, per);
+  const Chunk z = chunk_of<BWD, L * V, kSteps<T, BWD> * U>(a, groups, chunks, per);
   if (!z.ok || z.index == z.count - 1) return;  // such a chunk has a multiple of R U steps
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long each = z.n / U;
@@ -327,7 +351,7 @@ __global__ void __launch_bounds__(32 * kWarps, 6) recur_maps_kernel(const RecurA
 // behind each other R steps each.
 template <typename T, int V, int L, int W, bool MEAN, bool BWD, int GRAIN>
 struct Walk {
-  static constexpr int R = BWD ? 8 : 16, G = 32 / L, U = G * W, TR = U * R;
+  static constexpr int R = kSteps<T, BWD>, G = 32 / L, U = G * W, TR = U * R;
   static constexpr int IN = BWD ? (MEAN ? 4 : 3) : 2, OUT = BWD ? 2 : 1;  // arrays read and written
   using Rg = Ring<T, V, L, R, IN, 2, BWD, GRAIN>;
   static constexpr int kMaps = 2 * W * L * sizeof(Map<V>), BYTES = W * Rg::BYTES + kMaps + 2 * L * sizeof(Vec<V>);
@@ -352,7 +376,8 @@ __global__ void __launch_bounds__(32 * W, 16 / W)
   }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, lc = lane % L, inner = lane / L, sub = warp * G + inner;
   const int c = z.c0 + lc * V;
-  const bool on = c < a.C, end = warp == W - 1 && inner == G - 1;
+  const int there = min(V, a.C - c);  // of the thread's channels, 0 and less: none
+  const bool end = warp == W - 1 && inner == G - 1;
   const long long state_at = static_cast<long long>(z.row) * a.C + c;
   const int tiles = static_cast<int>((z.n + P::TR - 1) / P::TR);
 
@@ -367,16 +392,17 @@ __global__ void __launch_bounds__(32 * W, 16 / W)
     ring.array(1, a.u, a.u_st, 0, z, z.n);
   }
   ring.full(a, z, P::TR, BWD ? min(z.n, z.all - 1 - z.k0) : z.n);
-  char *dst[2];
-  {
-    const long long r = BWD ? z.hi - 1 - (z.k0 + ring.k) : z.lo + z.k0 + ring.k;
-    dst[0] = static_cast<char *>(a.out) + (r * a.out_st + z.c0) * static_cast<int>(sizeof(T)) + ring.c;
-    dst[1] = static_cast<char *>(a.du) + (r * a.du_st + z.c0) * static_cast<int>(sizeof(T)) + ring.c;
+  char *dst[2][Rg::SPLIT];
+#pragma unroll
+  for (int p = 0; p < Rg::SPLIT; ++p) {
+    const long long r = Rg::row(z, ring.k[p]);
+    dst[0][p] = static_cast<char *>(a.out) + (r * a.out_st + z.c0) * static_cast<int>(sizeof(T)) + ring.c[p];
+    dst[1][p] = static_cast<char *>(a.du) + (r * a.du_st + z.c0) * static_cast<int>(sizeof(T)) + ring.c[p];
   }
   if (tiles > 0) ring.issue(0, 0);
   copy_commit();
 
-  F carry = a.first && z.row >= 0 && on ? load_state<V>(a.first, state_at) : F::all(0.f);
+  F carry = a.first && z.row >= 0 ? load_state<V>(a.first, state_at, there) : F::all(0.f);
   if (chunks > 1) {
     grid_dep_wait();  // the maps, and whatever ran before them
     if (z.index > 0) {  // the chunks before this one, a stretch of them a thread
@@ -442,7 +468,7 @@ __global__ void __launch_bounds__(32 * W, 16 / W)
     for (int i = 0; i < R; ++i) {
       if (BWD) {
         F before = h[i].get();
-        if (a.h0 && on && z.k0 + k0 + sub * R + i == z.all - 1) before = load_state<V>(a.h0, static_cast<long long>(z.q) * a.C + c);
+        if (a.h0 && z.k0 + k0 + sub * R + i == z.all - 1) before = load_state<V>(a.h0, static_cast<long long>(z.q) * a.C + c, there);
         const F total = g[i].get() + x;
         x = d[i] * total;
         put(0, i, MEAN ? x * fma(before, F::all(-1.f), v[i].get()) : x * (before * F::all(-1.f)));
@@ -459,23 +485,26 @@ __global__ void __launch_bounds__(32 * W, 16 / W)
 #pragma unroll
       for (int j = 0; j < Rg::PIECES; ++j) {
         const char *from = out_p + o * Rg::PART + (lane + 32 * j) * GRAIN;
-        char *to = dst[o] + Rg::WAY * Rg::STEP * j * st;
-        const bool there = tl < ring.whole || k0 + ring.k + Rg::STEP * j < z.n;
-        if (there && (tl < ring.whole || ring.bytes == GRAIN)) {
+        constexpr int SPLIT = Rg::SPLIT;
+        char *to = dst[o][j % SPLIT] + Rg::WAY * Rg::STEP * (j / SPLIT) * st;
+        const bool has = tl < ring.whole || k0 + ring.k[j % SPLIT] + Rg::STEP * (j / SPLIT) < z.n;
+        if (has && (tl < ring.whole || ring.bytes[j % SPLIT] == GRAIN)) {
           if (GRAIN == 16) *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(from);
           else if (GRAIN == 4) *reinterpret_cast<uint32_t *>(to) = *reinterpret_cast<const uint32_t *>(from);
           else *reinterpret_cast<uint16_t *>(to) = *reinterpret_cast<const uint16_t *>(from);
-        } else if (there) {
-          for (int e = 0; e < ring.bytes; e += sizeof(T)) *reinterpret_cast<T *>(to + e) = *reinterpret_cast<const T *>(from + e);
+        } else if (has) {
+          for (int e = 0; e < ring.bytes[j % SPLIT]; e += sizeof(T)) *reinterpret_cast<T *>(to + e) = *reinterpret_cast<const T *>(from + e);
         }
       }
-      dst[o] += Rg::WAY * P::TR * st;
+#pragma unroll
+      for (int p = 0; p < Rg::SPLIT; ++p) dst[o][p] += Rg::WAY * P::TR * st;
     }
     __syncwarp();
   }
-  if (z.index == z.count - 1 && end && on && a.last && z.row >= 0)
+  if (z.index == z.count - 1 && end && a.last && z.row >= 0)
 #pragma unroll
-    for (int i = 0; i < V; ++i) a.last[state_at + i] = carry.get(i);
+    for (int i = 0; i < V; ++i)
+      if (i < there) a.last[state_at + i] = carry.get(i);
 }
 
 // Sequences of few steps: a thread walks V channels of one, four steps' loads under way.
@@ -498,7 +527,7 @@ __global__ void __launch_bounds__(128) recur_few_kernel(const RecurArgs a, int b
   auto at = [&](const void *p, long long st, long long k) {  // step k of the walk
     return reinterpret_cast<const Wd *>(static_cast<const T *>(p) + (BWD ? hi - 1 - k : lo + k) * st + c);
   };
-  F x = a.first && row >= 0 ? load_state<V>(a.first, state_at) : F::all(0.f);
+  F x = a.first && row >= 0 ? load_state<V>(a.first, state_at, V) : F::all(0.f);
   constexpr int N = 4;
   for (long long k0 = 0; k0 < n; k0 += N) {
     Wd s[N], u[N], g[N], h[N];
@@ -521,7 +550,7 @@ __global__ void __launch_bounds__(128) recur_few_kernel(const RecurArgs a, int b
       if (BWD) {
         F before = F::all(0.f);
         if (k0 + i + 1 < n) before = h[i].get();
-        else if (a.h0) before = load_state<V>(a.h0, static_cast<long long>(q) * a.C + c);
+        else if (a.h0) before = load_state<V>(a.h0, static_cast<long long>(q) * a.C + c, V);
         const F total = g[i].get() + x;
         x = d * total;
         *out = Wd::of(MEAN ? x * fma(before, F::all(-1.f), u[i].get()) : x * (before * F::all(-1.f)));
@@ -551,24 +580,24 @@ struct Split {
 };
 
 // A line to a CTA where that fills the GPU, 16 warps an SM, to three fifths in its last round (64 or 32 bytes of channels
-// a row where there are no more), in CTAs of 8 warps if those fill it better; otherwise chunks, three to four CTAs an SM.
+// a row where there are no more), in CTAs of 8 warps if those fill it better (tiles' last rows counted); otherwise chunks, three to four CTAs an SM.
 // Eight sequences of 8192 steps of 2048 channels of bf16, 256 lines: forward 140 us in CTAs of 8 warps, 163 of 4, 207 in
 // chunks; backward 253, 303, 336.  One of 131072 steps of 256 channels, 4 lines: forward 68 us in 128 chunks, 78 in 64,
 // 74 in 160; backward 88, 107, 103.
-Split split_of(const RecurArgs &a, int V, bool bwd, int num_sms) {
+Split split_of(const RecurArgs &a, int V, int steps, int num_sms) {
   if (a.T <= kFewSteps) return {0, 0, 0, 0};
   int lanes = 32;
   while (lanes > 8 && a.C <= lanes * V / 2) lanes /= 2;
-  const long long lines = static_cast<long long>(a.S) * ((a.C + lanes * V - 1) / (lanes * V));
+  // lines of the full length that there is work for: sequences may be shorter
+  const double groups = (a.C + lanes * V - 1) / (lanes * V), lines = std::min<double>(a.S, std::max(1.0, static_cast<double>(a.N) / a.T)) * groups;
+  const int tile = 32 / lanes * kWarps * steps;  // rows
   auto fill = [&](int warps) {
-    const long long round = 16ll / warps * num_sms;
-    return static_cast<double>(lines) / static_cast<double>((lines + round - 1) / round * round);
+    const double round = 16.0 / warps * num_sms, rows = tile / kWarps * warps;
+    return lines / (std::ceil(lines / round) * round) * a.T / (std::ceil(a.T / rows) * rows);
   };
-  const int tile = 32 / lanes * kWarps * (bwd ? 8 : 16);
-  const long long chunks = std::min(7ll * num_sms / 2 / lines, (a.T + 2ll * tile - 1) / (2 * tile));
   const double four = fill(4), eight = lanes == 32 ? fill(8) : 0;
-  if (std::max(four, eight) >= 0.6 || chunks < 2) return {lanes, eight > four + 0.05 ? 8 : 4, 1, 0};
-  const long long per = ((a.T + chunks - 1) / chunks + tile - 1) / tile * tile;
+  const long long per = std::max<long long>(2, static_cast<long long>(std::ceil(lines * a.T / (3.5 * num_sms * tile)))) * tile;
+  if (std::max(four, eight) >= 0.6 || per >= a.T) return {lanes, eight > four + 0.05 ? 8 : 4, 1, 0};
   return {lanes, kWarps, static_cast<int>((a.T + per - 1) / per), static_cast<int>(per)};
 }
 
@@ -583,8 +612,8 @@ cudaError_t launch_walk(const RecurArgs &a, const Split &sp, void *ws, cudaStrea
   cudaError_t e = resident_blocks<Tag<T, V, L, W, MEAN, BWD, GRAIN>>(kernel, 32 * W, P::BYTES, &per_sm);
   if constexpr (W == kWarps) {
     if (e == cudaSuccess && chunks > 1) {
-      constexpr int ring = W * Ring<T, V, L, 8, 2, 3, BWD, GRAIN>::BYTES;
-      static_assert(ring <= 40 * 1024, "no leave to ask for");
+      constexpr int ring = W * Ring<T, V, L, kMapSteps<T>, 2, 3, BWD, GRAIN>::BYTES;
+      static_assert(ring <= 48 * 1024 - W * L * static_cast<int>(sizeof(Map<V>)), "no leave to ask for");
       recur_maps_kernel<T, V, L, MEAN, BWD, GRAIN><<<blocks, 32 * W, ring, stream>>>(a, groups, chunks, sp.per, maps);
       e = cudaGetLastError();
     }
@@ -596,8 +625,8 @@ cudaError_t launch_walk(const RecurArgs &a, const Split &sp, void *ws, cudaStrea
 
 template <typename T, int V, bool MEAN, bool BWD, int GRAIN>
 cudaError_t launch_lanes(const RecurArgs &a, int num_sms, void *ws, cudaStream_t stream) {
-  const Split sp = split_of(a, V, BWD, num_sms);
-  if (sp.lanes == 0) return launch_few<T, V, MEAN, BWD>(a, stream);
+  const Split sp = split_of(a, V, kSteps<T, BWD>, num_sms);
+  if (sp.lanes == 0) return launch_few<T, sizeof(T) == 4 ? 1 : V, MEAN, BWD>(a, stream);
   if (sp.lanes == 32)
     return sp.warps == 8 ? launch_walk<T, V, 32, 8, MEAN, BWD, GRAIN>(a, sp, ws, stream)
                          : launch_walk<T, V, 32, 4, MEAN, BWD, GRAIN>(a, sp, ws, stream);
@@ -614,14 +643,14 @@ bool starts_at(const RecurArgs &a, int bytes, int size) {
   return ok;
 }
 
-// Channels to a lane: two of bf16 where every row starts on a multiple of them.
-int channels(const RecurArgs &a, int type) { return type != kTypeF32 && a.C % 2 == 0 && starts_at(a, 4, 2) ? 2 : 1; }
+// Channels to a lane: two, but of bf16 one where not every row starts on a multiple of two.
+int channels(const RecurArgs &a, int type) { return type == kTypeF32 || (a.C % 2 == 0 && starts_at(a, 4, 2)) ? 2 : 1; }
 
 template <bool MEAN, bool BWD>
 cudaError_t launch_mean(const RecurArgs &a, int type, int num_sms, void *ws, cudaStream_t stream) {
   if (type == kTypeF32)
-    return starts_at(a, 16, 4) ? launch_lanes<float, 1, MEAN, BWD, 16>(a, num_sms, ws, stream)
-                               : launch_lanes<float, 1, MEAN, BWD, 4>(a, num_sms, ws, stream);
+    return starts_at(a, 16, 4) ? launch_lanes<float, 2, MEAN, BWD, 16>(a, num_sms, ws, stream)
+                               : launch_lanes<float, 2, MEAN, BWD, 4>(a, num_sms, ws, stream);
   if (channels(a, type) == 1) return launch_lanes<__nv_bfloat16, 1, MEAN, BWD, 2>(a, num_sms, ws, stream);
   return starts_at(a, 16, 2) ? launch_lanes<__nv_bfloat16, 2, MEAN, BWD, 16>(a, num_sms, ws, stream)
                              : launch_lanes<__nv_bfloat16, 2, MEAN, BWD, 4>(a, num_sms, ws, stream);
@@ -630,7 +659,7 @@ cudaError_t launch_mean(const RecurArgs &a, int type, int num_sms, void *ws, cud
 template <bool BWD>
 size_t workspace(const RecurArgs &a, int type, int num_sms) {
   const int V = channels(a, type);
-  const Split sp = split_of(a, V, BWD, num_sms);
+  const Split sp = split_of(a, V, type == kTypeF32 ? kSteps<float, BWD> : kSteps<__nv_bfloat16, BWD>, num_sms);
   if (sp.chunks <= 1) return 0;
   return static_cast<size_t>(a.S) * ((a.C + sp.lanes * V - 1) / (sp.lanes * V)) * sp.chunks * sp.lanes * V * 8;
 }

@@ -43,7 +43,8 @@ def offsets_of(lens, first=0):
 
 
 CASES = [([1], 1), ([1] * 65, 64), ([5], 3), ([16, 17], 130), ([31, 33, 0, 1, 2], 64), ([127], 66), ([128, 129], 32),
-         ([500, 3], 100), ([0, 0, 7], 8), ([1000], 257), ([2500, 40, 0, 700], 72), ([4100], 33)]
+         ([500, 3], 100), ([0, 0, 7], 8), ([1000], 257), ([2500, 40, 0, 700], 72), ([4100], 33), ([2000, 30], 8), ([1300, 30], 24),
+         ([150] * 70 + [600, 0], 256), ([90] * 20, 2000)]
 
 
 @pytest.mark.parametrize("lens,c", CASES)
