@@ -24,8 +24,6 @@ constexpr int kSmem = rows_smem<S>(kRow<S, TX, TY>, kWeights<S, BIAS>, kBlocks<S
 
 template <typename S, typename TX, typename TY, bool BIAS>
 __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_fwd_kernel(const NormArgs a) {
-  using CX = Copied<S, TX>;
-  using CY = Copied<S, TY>;
   extern __shared__ __align__(16) char smem[];
   __shared__ float s_red[2 * kRowRed];
   int turn = 0;
@@ -36,8 +34,9 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_fwd_kernel(const 
   // x, then y, then the gate in a stage
   constexpr bool HOLD = keeps_weights<S>(kRow<S, TX, TY>, kWeights<S, BIAS>);
   constexpr int kept = HOLD ? kWeights<S, BIAS> : 0;  // weights, ahead of the stages
-  const int stage_bytes = CX::BYTES + (branch ? CY::BYTES : 0) + (gated ? CY::BYTES : 0);
-  const int stages = S::VEC ? min(4, (kSmem<S, TX, TY, BIAS> - kept) / stage_bytes) : 1;
+  const int part_x = stage_part<S, TX>(D), part_y = stage_part<S, TY>(D);
+  const int stage_bytes = part_x + (branch ? part_y : 0) + (gated ? part_y : 0);
+  const int stages = S::COPIED ? min(4, (kSmem<S, TX, TY, BIAS> - kept) / stage_bytes) : 1;  // staged: 2 at least
   int y_off[S::RUNS], g_off[S::RUNS];
   if (S::VEC && branch)
 #pragma unroll
@@ -67,13 +66,13 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_fwd_kernel(const 
     const bool there = n < a.N;
     const int m = there ? n : 0, b = there ? ahead.b : 0, t = there ? ahead.t : 0;
     const uint32_t to = smem_u32(smem) + kept + stage * stage_bytes;
-    CX::issue(to, static_cast<const TX *>(a.x) + static_cast<long long>(m) * D, nullptr, lane, mine, there);
-    if (branch) CY::issue(to + CX::BYTES, heads_row(a.y, b, t), y_off, lane, mine, there);
-    if (gated) CY::issue(to + CX::BYTES + CY::BYTES, heads_row(a.gate, b, t), g_off, lane, mine, there);
+    issue_row<S>(to, static_cast<const TX *>(a.x) + static_cast<long long>(m) * D, nullptr, D, lane, mine, there);
+    if (branch) issue_row<S>(to + part_x, heads_row(a.y, b, t), y_off, D, lane, mine, there);
+    if (gated) issue_row<S>(to + part_x + part_y, heads_row(a.gate, b, t), g_off, D, lane, mine, there);
     ahead.go(step, a.T);
   };
-  if constexpr (S::VEC) {
-    clear_smem<S>(smem + kept, stages * stage_bytes);
+  if constexpr (S::COPIED) {
+    if (S::VEC) clear_smem<S>(smem + kept, stages * stage_bytes);
     for (int k = 0; k < stages - 1; ++k) {
       if (k == 0 || first < a.N - k * step) issue(n + k * step, k);
       copy_commit();
@@ -82,20 +81,21 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_fwd_kernel(const 
   for (; first < a.N; first += step, n += step, here.go(step, a.T)) {
     const int Dn = n < a.N ? D : 0;  // a row past the end has no elements, and its threads meet the others
     const char *slot = smem + kept + stage * stage_bytes;
-    if constexpr (S::VEC) {
+    if constexpr (S::COPIED) {
+      if (S::STAGED) {  // the row's threads have all copied it, and have all done with the one before
+        rows_wait(stages - 1);
+        row_barrier<S>();
+      }
       if (first < a.N - (stages - 1) * step) issue(n + (stages - 1) * step, stage == 0 ? stages - 1 : stage - 1);
       copy_commit();
-      rows_wait(stages);
+      if (S::VEC) rows_wait(stages);
       stage = stage == stages - 1 ? 0 : stage + 1;
     }
     const long long at = static_cast<long long>(n) * D;
     const int b = here.b, t = here.t;
     Piece r[S::K];
 #pragma unroll
-    for (int i = 0; i < S::K; ++i) {
-      if constexpr (S::VEC) r[i] = CX::read(slot, i);
-      else r[i] = load_single<S, TX>(static_cast<const TX *>(a.x) + at, nullptr, 0, Dn, lane, i);
-    }
+    for (int i = 0; i < S::K; ++i) r[i] = get_piece<S>(slot, static_cast<const TX *>(a.x) + at, nullptr, 0, D, Dn, lane, i);
     auto factor = [&](Piece (&x)[S::K], int kind) {  // 1 / the norm; a layer norm's mean is taken off x
       float sum[1];
       float2 s = both(0.f);
@@ -117,19 +117,14 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_fwd_kernel(const 
     if (branch) {
       Piece y[S::K];
 #pragma unroll
-      for (int i = 0; i < S::K; ++i) {
-        if constexpr (S::VEC) y[i] = CY::read(slot + CX::BYTES, i);
-        else y[i] = load_single<S, TY>(heads_row(a.y, b, t), &a.y, a.d, Dn, lane, i);
-      }
+      for (int i = 0; i < S::K; ++i) y[i] = get_piece<S>(slot + part_x, heads_row(a.y, b, t), &a.y, a.d, D, Dn, lane, i);
       const float inv = a.post != 0 ? factor(y, a.post) : 1.f;
 #pragma unroll
       for (int i = 0; i < S::K; ++i) {
         Piece v = weighted(times(y[i], inv), weight(0, i), weight(2, i));
         if (gated) {
-          Piece g, value, slope;
-          if constexpr (S::VEC) g = CY::read(slot + CX::BYTES + CY::BYTES, i);
-          else g = load_single<S, TY>(heads_row(a.gate, b, t), &a.gate, a.d, Dn, lane, i);
-          gate_piece(g, a.act, value, slope);
+          Piece value, slope;
+          gate_piece(get_piece<S>(slot + part_x + part_y, heads_row(a.gate, b, t), &a.gate, a.d, D, Dn, lane, i), a.act, value, slope);
           v = times(v, value);
         }
         FEM_EACH_PAIR r[i].v[j] = __ffma2_rn(v.v[j], both(a.scale), r[i].v[j]);
@@ -169,9 +164,10 @@ struct Launch {
 template <typename TX, typename TY>
 cudaError_t launch_types(const NormArgs &a, int num_sms, cudaStream_t stream) {
   constexpr int RUN = sizeof(TX) == 4 ? 4 : 8;
-  const bool pieces = norm_pieces(a, sizeof(TY), RUN);
-  return a.b_post || a.b_pre ? with_shape<RUN, false, 1, Launch<TX, TY, true>::template With>(a.D, pieces, a, num_sms, stream)
-                             : with_shape<RUN, false, 1, Launch<TX, TY, false>::template With>(a.D, pieces, a, num_sms, stream);
+  const bool bias = a.b_post || a.b_pre;
+  const Way way = way_of(a, norm_pieces(a, sizeof(TY), RUN), staged_row<TX>(a.D) + 2 * staged_row<TY>(a.D), bias ? 4 : 2, 3);
+  return bias ? with_shape<RUN, false, 1, Launch<TX, TY, true>::template With>(a.D, way, a, num_sms, stream)
+              : with_shape<RUN, false, 1, Launch<TX, TY, false>::template With>(a.D, way, a, num_sms, stream);
 }
 
 }  // namespace

@@ -14,12 +14,13 @@
 namespace fem {
 
 // A piece is made of runs of RUN elements that lie together: 8 where all is bf16, 4 with fp32 (16 bytes of it, so that a
-// warp's accesses have no gaps), 1 where single elements are read.
+// warp's accesses have no gaps), 1 where single elements are read.  Rows that lie together but start anywhere are STAGED
+// (RUN_ 0): copied whole, in 16-byte pieces around them, and read as single elements.
 template <int TPR_, int K_, int RUN_, int MOST_ = 256>
 struct RowShape {
-  static constexpr int TPR = TPR_, K = K_, RUN = RUN_, ROWS = TPR_ < MOST_ ? MOST_ / TPR_ : 1, THREADS = TPR_ * ROWS;
-  static constexpr bool VEC = RUN_ > 1;
-  static constexpr int RUNS = VEC ? K_ * 8 / RUN_ : 1;  // of a thread, places to keep
+  static constexpr int TPR = TPR_, K = K_, RUN = RUN_ > 0 ? RUN_ : 1, ROWS = TPR_ < MOST_ ? MOST_ / TPR_ : 1, THREADS = TPR_ * ROWS;
+  static constexpr bool VEC = RUN_ > 1, STAGED = RUN_ == 0, COPIED = VEC || STAGED;
+  static constexpr int RUNS = VEC ? K_ * 8 / RUN : 1;  // of a thread, places to keep
   static constexpr int WARPS = TPR_ / 32;               // of a row
   static constexpr int WEIGHT = THREADS * K * 32;       // bytes of a vector of weights
 
@@ -209,11 +210,11 @@ struct Copied {
 // has `row` bytes: an SM's share of a block where `blocks` are to be on it.  As many rows as fit are under way, up to four.
 constexpr int kMostSmem = 224 * 1024;
 template <typename S>
-constexpr bool keeps_weights(int row, int weights) { return S::VEC && row + weights <= kMostSmem; }
+constexpr bool keeps_weights(int row, int weights) { return S::STAGED ? S::THREADS < 1024 : S::VEC && row + weights <= kMostSmem; }
 template <typename S>
 constexpr int rows_smem(int row, int weights, int blocks) {
   const int share = kMostSmem / blocks - (blocks > 1 ? 2048 : 0), least = row + (keeps_weights<S>(row, weights) ? weights : 0);
-  return !S::VEC ? 0 : share > least ? share : least;
+  return !S::COPIED ? 0 : S::STAGED || share > least ? share : least;
 }
 // Zeros in the first `bytes` of shared memory behind `from`, 16 a thread.
 template <typename S>
@@ -228,6 +229,30 @@ __device__ __forceinline__ void rows_wait(int stages) {
   else copy_wait<0>();
 }
 
+// Bytes of a staged row with what its pieces hold around it, and of an array in a stage.
+template <typename T>
+__host__ __device__ constexpr int staged_row(int D) { return (D * static_cast<int>(sizeof(T)) + 31) / 16 * 16; }
+template <typename S, typename T>
+__device__ __forceinline__ int stage_part(int D) {
+  return S::VEC ? Copied<S, T>::BYTES : S::ROWS * staged_row<T>(D);
+}
+// Copies a row of D elements at p with the rest of its first 16 bytes, which are the same allocation's, and none of what
+// follows its last.
+template <typename S, typename T>
+__device__ __forceinline__ void stage_issue(uint32_t slot, const T *p, int D, int lane) {
+  const uintptr_t start = reinterpret_cast<uintptr_t>(p);
+  const char *from = reinterpret_cast<const char *>(start & ~static_cast<uintptr_t>(15));
+  const int bytes = static_cast<int>(start & 15) + D * static_cast<int>(sizeof(T));
+  const uint32_t to = slot + threadIdx.x / S::TPR * staged_row<T>(D);
+  for (int at = lane * 16; at < bytes; at += S::TPR * 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + at), "l"(from + at), "r"(min(16, bytes - at)) : "memory");
+}
+// Where the row at p is in shared memory.
+template <typename S, typename T>
+__device__ __forceinline__ const T *staged(const char *slot, const T *p, int D) {
+  return reinterpret_cast<const T *>(slot + threadIdx.x / S::TPR * staged_row<T>(D) + (reinterpret_cast<uintptr_t>(p) & 15));
+}
+
 // Piece i of a row, element by element; what is past its end is 0.
 template <typename S, typename T>
 __device__ __forceinline__ Piece load_single(const T *row, const HeadsView *v, int d, int Dn, int lane, int i) {
@@ -239,6 +264,25 @@ __device__ __forceinline__ Piece load_single(const T *row, const HeadsView *v, i
   }
   return {make_float2(f[0], f[1]), make_float2(f[2], f[3]), make_float2(f[4], f[5]), make_float2(f[6], f[7])};
 }
+// Piece i of the row at p, whichever way it comes; `slot` where its array's copies are.
+template <typename S, typename T>
+__device__ __forceinline__ Piece get_piece(const char *slot, const T *p, const HeadsView *v, int d, int D, int Dn, int lane, int i) {
+  if constexpr (S::VEC) return Copied<S, T>::read(slot, i);
+  else if constexpr (S::STAGED) return load_single<S, T>(staged<S, T>(slot, p, D), nullptr, 0, Dn, lane, i);
+  else return load_single<S, T>(p, v, d, Dn, lane, i);
+}
+// Starts the copies of the row at p.
+template <typename S, typename T>
+__device__ __forceinline__ void issue_row(uint32_t slot, const T *p, const int *off, int D, int lane, const Mine<S> &mine, bool there) {
+  if constexpr (S::VEC) Copied<S, T>::issue(slot, p, off, lane, mine, there);
+  else if (there) stage_issue<S, T>(slot, p, D, lane);
+}
+template <typename S>
+__device__ __forceinline__ void row_barrier() {
+  if (S::TPR == 32) __syncwarp();
+  else bar_sync(1 + static_cast<int>(threadIdx.x) / S::TPR, S::TPR);
+}
+
 // Writes piece i of a row; `off` as above (VEC), `v` the array of heads or null.
 template <typename S, typename T>
 __device__ __forceinline__ void store_piece(T *row, const HeadsView *v, const int *off, int d, int Dn, int lane,
@@ -332,17 +376,25 @@ __device__ __forceinline__ void gate_piece(const Piece &g, int act, Piece &value
   }
 }
 
-// The shape for rows of D elements; `pieces`: whether the arrays allow copies of runs of RUN elements.  A thread has one
-// piece, or two with TWO, in blocks of 128 threads, where no threads are idle for it; WIDE of them in rows of more than
-// 4096 elements.
+// How rows are read: runs that the arrays allow to copy, rows copied whole, single elements.
+enum Way { SINGLE, STAGED, PIECES };
+
+// The shape for rows of D elements.  A thread has one piece, or two with TWO, in blocks of 128 threads, where no threads
+// are idle for it; WIDE of them in rows of more than 4096 elements.
 template <int RUN, bool TWO, int WIDE, template <typename> class F, typename... Args>
-cudaError_t with_shape(int D, bool pieces, Args &&...args) {
+cudaError_t with_shape(int D, Way way, Args &&...args) {
   constexpr int K = TWO ? 2 : 1, MOST = TWO ? 128 : 256;
-  if (!pieces) {
+  if (way == SINGLE) {
     if (D <= 1024) return F<RowShape<128, 1, 1>>::call(args...);
     if (D <= 4096) return F<RowShape<512, 1, 1>>::call(args...);
-    if (D <= 8192) return F<RowShape<1024, 1, 1>>::call(args...);
     return F<RowShape<1024, 2, 1>>::call(args...);
+  }
+  if (way == STAGED) {
+    if (D <= 256) return F<RowShape<32, 1, 0>>::call(args...);
+    if (D <= 1024) return F<RowShape<128, 1, 0>>::call(args...);
+    if (D <= 2048) return F<RowShape<256, 1, 0>>::call(args...);
+    if (D <= 5120) return F<RowShape<640, 1, 0>>::call(args...);
+    return F<RowShape<1024, 1, 0>>::call(args...);
   }
   if (D <= 256) return F<RowShape<32, 1, RUN>>::call(args...);
   if (D <= 512) return F<RowShape<64 / K, K, RUN, MOST>>::call(args...);
@@ -353,6 +405,19 @@ cudaError_t with_shape(int D, bool pieces, Args &&...args) {
   if (D <= 4096) return F<RowShape<512, 1, RUN>>::call(args...);
   if (D <= 8192) return F<RowShape<1024 / WIDE, WIDE, RUN>>::call(args...);
   return F<RowShape<1024, 2, RUN>>::call(args...);
+}
+
+// The way for a call whose rows of all arrays, staged, take `row` bytes: two of them have to fit beside the weights, in
+// blocks of 256 threads of which `blocks` are on an SM.
+inline Way way_of(const NormArgs &a, bool pieces, int row, int vectors, int blocks) {
+  if (pieces) return PIECES;
+  for (const HeadsView *v : {&a.y, &a.gate})
+    if (v->p && a.H > 1 && v->sh != a.d) return SINGLE;
+  if (a.D > 8192) return SINGLE;
+  // least shared memory of a block that has a row of such a length, in the shapes above, and the rows it has at a time
+  const int threads = a.D <= 2048 ? 256 : a.D <= 5120 ? 640 : 1024, rows = a.D <= 256 ? 8 : a.D <= 1024 ? 2 : 1;
+  const int smem = threads == 256 ? kMostSmem / blocks - 2048 : kMostSmem, kept = threads < 1024 ? vectors * threads * 32 : 0;
+  return 2 * rows * row + kept <= smem ? STAGED : SINGLE;
 }
 
 // Whether every array allows 16-byte pieces of eight elements.

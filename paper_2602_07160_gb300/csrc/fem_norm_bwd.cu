@@ -32,8 +32,6 @@ constexpr int kSmem = rows_smem<S>(kRow<S, TX, TY>, kWeights<S, BIAS>, kBlocks<S
 
 template <typename S, typename TX, typename TY, bool BIAS>
 __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_bwd_kernel(const NormArgs a) {
-  using CX = Copied<S, TX>;
-  using CY = Copied<S, TY>;
   constexpr int SUMS = BIAS ? 4 : 2;
   extern __shared__ __align__(16) char smem[];
   __shared__ float s_red[2 * kRowRed];
@@ -61,9 +59,10 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_bwd_kernel(const 
 #pragma unroll
       for (int i = 0; i < S::K; ++i) keep_weights<S>(smem + k * S::WEIGHT, weights(k, i), i);
   // r, dr, dz, y and the gate in a stage, those that there are
-  const int at_dr = normed ? CX::BYTES : 0, at_dz = at_dr + (a.dr ? CX::BYTES : 0), at_y = at_dz + (normed ? CY::BYTES : 0);
-  const int at_gate = at_y + (branch ? CY::BYTES : 0), stage_bytes = at_gate + (gated ? CY::BYTES : 0);
-  const int stages = S::VEC ? min(4, (kSmem<S, TX, TY, BIAS> - kept) / stage_bytes) : 1;
+  const int part_x = stage_part<S, TX>(D), part_y = stage_part<S, TY>(D);
+  const int at_dr = normed ? part_x : 0, at_dz = at_dr + (a.dr ? part_x : 0), at_y = at_dz + (normed ? part_y : 0);
+  const int at_gate = at_y + (branch ? part_y : 0), stage_bytes = at_gate + (gated ? part_y : 0);
+  const int stages = S::COPIED ? min(4, (kSmem<S, TX, TY, BIAS> - kept) / stage_bytes) : 1;  // staged: 2 at least
   // places of the pieces in the heads' arrays
   int off[4][S::RUNS];
   if (S::VEC && branch)
@@ -85,16 +84,16 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_bwd_kernel(const 
     const long long at = static_cast<long long>(there ? n : 0) * D;
     const uint32_t to = smem_u32(smem) + kept + stage * stage_bytes;
     if (normed) {
-      CX::issue(to, static_cast<const TX *>(a.x) + at, nullptr, lane, mine, there);
-      CY::issue(to + at_dz, static_cast<const TY *>(a.dz) + at, nullptr, lane, mine, there);
+      issue_row<S>(to, static_cast<const TX *>(a.x) + at, nullptr, D, lane, mine, there);
+      issue_row<S>(to + at_dz, static_cast<const TY *>(a.dz) + at, nullptr, D, lane, mine, there);
     }
-    if (a.dr) CX::issue(to + at_dr, static_cast<const TX *>(a.dr) + at, nullptr, lane, mine, there);
-    if (branch) CY::issue(to + at_y, heads_row(a.y, b, t), off[0], lane, mine, there);
-    if (gated) CY::issue(to + at_gate, heads_row(a.gate, b, t), off[1], lane, mine, there);
+    if (a.dr) issue_row<S>(to + at_dr, static_cast<const TX *>(a.dr) + at, nullptr, D, lane, mine, there);
+    if (branch) issue_row<S>(to + at_y, static_cast<const TY *>(heads_row(a.y, b, t)), off[0], D, lane, mine, there);
+    if (gated) issue_row<S>(to + at_gate, static_cast<const TY *>(heads_row(a.gate, b, t)), off[1], D, lane, mine, there);
     ahead.go(step, a.T);
   };
-  if constexpr (S::VEC) {
-    clear_smem<S>(smem + kept, stages * stage_bytes);
+  if constexpr (S::COPIED) {
+    if (S::VEC) clear_smem<S>(smem + kept, stages * stage_bytes);
     for (int k = 0; k < stages - 1; ++k) {
       if (k == 0 || first < a.N - k * step) issue(n + k * step, k);
       copy_commit();
@@ -104,30 +103,25 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_bwd_kernel(const 
   for (; first < a.N; first += step, n += step, here.go(step, a.T)) {
     const int Dn = n < a.N ? D : 0;  // a row past the end has no elements, and its threads meet the others
     const char *slot = smem + kept + stage * stage_bytes;
-    if constexpr (S::VEC) {
+    if constexpr (S::COPIED) {
+      if (S::STAGED) {  // the row's threads have all copied it, and have all done with the one before
+        rows_wait(stages - 1);
+        row_barrier<S>();
+      }
       if (first < a.N - (stages - 1) * step) issue(n + (stages - 1) * step, stage == 0 ? stages - 1 : stage - 1);
       copy_commit();
-      rows_wait(stages);
+      if (S::VEC) rows_wait(stages);
       stage = stage == stages - 1 ? 0 : stage + 1;
     }
     const long long at = static_cast<long long>(n) * D;
     const int b = here.b, t = here.t;
     // r and y stay in registers; dz, dr and the gate are read where they are used
-    auto get_dz = [&](int i) {
-      if constexpr (S::VEC) return CY::read(slot + at_dz, i);
-      else return load_single<S, TY>(static_cast<const TY *>(a.dz) + at, nullptr, 0, Dn, lane, i);
-    };
+    auto get_dz = [&](int i) { return get_piece<S>(slot + at_dz, static_cast<const TY *>(a.dz) + at, nullptr, 0, D, Dn, lane, i); };
     Piece r[S::K], y[S::K], dx[S::K];
 #pragma unroll
     for (int i = 0; i < S::K; ++i) {
-      if (normed) {
-        if constexpr (S::VEC) r[i] = CX::read(slot, i);
-        else r[i] = load_single<S, TX>(static_cast<const TX *>(a.x) + at, nullptr, 0, Dn, lane, i);
-      }
-      if (branch) {
-        if constexpr (S::VEC) y[i] = CY::read(slot + at_y, i);
-        else y[i] = load_single<S, TY>(heads_row(a.y, b, t), &a.y, a.d, Dn, lane, i);
-      }
+      if (normed) r[i] = get_piece<S>(slot, static_cast<const TX *>(a.x) + at, nullptr, 0, D, Dn, lane, i);
+      if (branch) y[i] = get_piece<S>(slot + at_y, static_cast<const TY *>(heads_row(a.y, b, t)), &a.y, a.d, D, Dn, lane, i);
     }
     // means for layer norms, f being w_pre dz
     float mean_f = 0.f;
@@ -173,8 +167,7 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_bwd_kernel(const 
 #pragma unroll
     for (int i = 0; i < S::K; ++i) {
       if (a.dr) {
-        if constexpr (S::VEC) dx[i] = CX::read(slot + at_dr, i);
-        else dx[i] = load_single<S, TX>(static_cast<const TX *>(a.dr) + at, nullptr, 0, Dn, lane, i);
+        dx[i] = get_piece<S>(slot + at_dr, static_cast<const TX *>(a.dr) + at, nullptr, 0, D, Dn, lane, i);
       } else {
         FEM_EACH_PAIR dx[i].v[j] = both(0.f);
       }
@@ -194,10 +187,8 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_bwd_kernel(const 
       y[i] = times(y[i], sigma);
       Piece value, slope;
       if (gated) {
-        Piece g;
-        if constexpr (S::VEC) g = CY::read(slot + at_gate, i);
-        else g = load_single<S, TY>(heads_row(a.gate, b, t), &a.gate, a.d, Dn, lane, i);
-        gate_piece(g, a.act, value, slope);
+        gate_piece(get_piece<S>(slot + at_gate, static_cast<const TY *>(heads_row(a.gate, b, t)), &a.gate, a.d, D, Dn, lane, i), a.act,
+                   value, slope);
         store_piece<S, TY>(heads_row(a.dgate, b, t), &a.dgate, off[3], a.d, Dn, lane, mine, i,
                            times(times(weighted(y[i], weight(0, i), weight(2, i)), slope), e));
         e = times(e, value);
@@ -294,11 +285,12 @@ struct Launch {
 template <typename TX, typename TY>
 cudaError_t types(const NormArgs &a, int num_sms, int *blocks, cudaStream_t stream) {
   constexpr int RUN = sizeof(TX) == 4 ? 4 : 8;
-  // a row of all arrays that does not fit in shared memory is read element by element
+  // a row of all arrays that does not fit in shared memory is not copied
   const bool pieces = norm_pieces(a, sizeof(TY), RUN) && (a.D <= 8192 || (2 * sizeof(TX) + 3 * sizeof(TY)) * 16384 <= kMostSmem);
-  return a.dw[1] || a.dw[3] || a.b_post
-             ? with_shape<RUN, RUN == 8, 2, Launch<TX, TY, true>::template With>(a.D, pieces, a, num_sms, blocks, stream)
-             : with_shape<RUN, RUN == 8, 2, Launch<TX, TY, false>::template With>(a.D, pieces, a, num_sms, blocks, stream);
+  const bool bias = a.dw[1] || a.dw[3] || a.b_post;
+  const Way way = way_of(a, pieces, 2 * staged_row<TX>(a.D) + 3 * staged_row<TY>(a.D), bias ? 3 : 2, 2);
+  return bias ? with_shape<RUN, RUN == 8, 2, Launch<TX, TY, true>::template With>(a.D, way, a, num_sms, blocks, stream)
+              : with_shape<RUN, RUN == 8, 2, Launch<TX, TY, false>::template With>(a.D, way, a, num_sms, blocks, stream);
 }
 
 cudaError_t dispatch(const NormArgs &a, int x_type, int y_type, int num_sms, int *blocks, cudaStream_t stream) {
