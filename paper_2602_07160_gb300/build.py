@@ -23,7 +23,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libfem.so")
 SOURCES = ["fem_api.cu", "fem_tc.cu", "fem_bank.cu", "fem_fixup.cu", "fem_simt.cu", "fem_decode.cu", "fem_gla.cu", "fem_gla_tc.cu", "fem_tdc.cu", "fem_bwd.cu", "fem_cache.cu",
            "fem_paged.cu", "fem_paged_token.cu", "fem_paged_chunk.cu", "fem_rope.cu", "fem_recur.cu", "fem_norm.cu",
-           "fem_norm_bwd.cu"]
+           "fem_norm_bwd.cu", "fem_norm_bwd_f32.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
