@@ -415,8 +415,8 @@ int fem_rope_turns(int rotary, double base, int scaling, double factor, double c
  *   q_out, k_out : as q and k; the same pointer and strides rotate in place
  *   turns        : device, uint64 [rotary/2] (fem_rope_turns); amplitude A
  *   positions    : device, int32 [B, T], any sign, or NULL: 0 .. T - 1 in every b
- * d up to 1024, rotary even and 2 .. d.  Angles are exact to fp32 rounding, the
- * rotation is fp32 arithmetic rounded once.  B = 0 or T = 0 does nothing.
+ * d up to 1024, rotary even and 2 .. d.  Angles are exact to fp32 rounding for
+ * positions up to 2^28, the rotation is fp32 arithmetic rounded once.  B = 0 or T = 0 does nothing.
  */
 int fem_rope(const fem_heads *q, const fem_heads *q_out, int Hq, const fem_heads *k, const fem_heads *k_out, int Hk,
              int B, int T, int d, int type, const uint64_t *turns, int rotary, int interleaved, float amplitude,
@@ -444,8 +444,10 @@ int fem_rope(const fem_heads *q, const fem_heads *q_out, int Hq, const fem_heads
  * Rows of no sequence are not written.  A sequence of length zero hands its state
  * on.  States, decays and sums are fp32; the same inputs give the same bits.  An
  * offset or state row outside its array is left out and recorded
- * (fem_check_device_error returns FEM_ERR_INVALID_ARG).  S = 0 does nothing.  No
- * workspace.
+ * (fem_check_device_error returns FEM_ERR_INVALID_ARG).  S = 0 does nothing.  Row
+ * strides and C below 2^20 (else FEM_ERR_UNSUPPORTED).  One launch, or two with a
+ * workspace from the library's stream-ordered pool where sequences times channels
+ * are too few for the GPU and sequences are cut into chunks.
  */
 int fem_recur_fwd(const void *s, const void *u, int64_t s_stride, int64_t u_stride, const int *offsets, int S, int T,
                   int N, int C, int type, int mean, const float *h0, float *h_last, const int *state_rows,

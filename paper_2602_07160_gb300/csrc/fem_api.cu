@@ -1072,11 +1072,11 @@ int fem_recur_bwd(const void *s, const void *u, const void *h, const void *dh, i
   DeviceState *ds = nullptr;
   if ((rc = device_state(&ds)) != FEM_OK) return rc;
   a.s = s;
-  a.u = mean ? u : nullptr;
+  a.u = mean ? u : nullptr;  // not looked at otherwise, nor its stride
   a.h = h;
   a.dh = dh;
   a.s_st = s_stride;
-  a.u_st = u_stride;
+  a.u_st = mean ? u_stride : 0;
   a.h_st = h_stride;
   a.dh_st = dh_stride;
   a.out = ds_out;

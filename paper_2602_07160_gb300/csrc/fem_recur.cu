@@ -597,8 +597,12 @@ Split split_of(const RecurArgs &a, int V, int steps, int num_sms) {
   };
   const double four = fill(4), eight = lanes == 32 ? fill(8) : 0;
   const long long per = std::max<long long>(2, static_cast<long long>(std::ceil(lines * a.T / (3.5 * num_sms * tile)))) * tile;
-  if (std::max(four, eight) >= 0.6 || per >= a.T) return {lanes, eight > four + 0.05 ? 8 : 4, 1, 0};
-  return {lanes, kWarps, static_cast<int>((a.T + per - 1) / per), static_cast<int>(per)};
+  // a CTA for every chunk that a sequence of the full length would have: not where many sequences are short
+  const double most = 262144.0 / (a.S * groups);
+  const long long chunks = std::min<long long>((a.T + per - 1) / per, static_cast<long long>(most));
+  if (std::max(four, eight) >= 0.6 || chunks < 2) return {lanes, eight > four + 0.05 ? 8 : 4, 1, 0};
+  const long long each = std::max(per, ((a.T + chunks - 1) / chunks + tile - 1) / tile * tile);
+  return {lanes, kWarps, static_cast<int>((a.T + each - 1) / each), static_cast<int>(each)};
 }
 
 template <typename T, int V, int L, int W, bool MEAN, bool BWD, int GRAIN>

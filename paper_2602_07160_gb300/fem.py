@@ -725,12 +725,16 @@ def fem_recur_fwd(s, u, offsets=None, max_len=None, h0=None, state_rows=None, me
 
 def fem_recur_bwd(s, u, h, dh, offsets=None, max_len=None, h0=None, dstate=None, mean: bool = False, stream=None):
     """Gradients of ``fem_recur_fwd`` from its outputs h and their cotangents dh, and the last states' dstate
-    (float32 [S, C] or None).  h0: float32 [S, C] or None, as the forward had it.  u is read where ``mean`` only.
+    (float32 [S, C] or None).  h0: float32 [S, C] or None, as the forward had it.  u is read where ``mean`` only, and
+    may be None elsewhere.
 
     Returns (ds, du, dh0), dh0 None where h0 is."""
     shape, dtype, index, off, S, T, N, C = _recur_sizes(s, offsets, max_len)
-    (s_ptr, s_st), (u_ptr, u_st), (h_ptr, h_st), (g_ptr, g_st) = (
-        _recur_rows(name, t, shape, dtype, index) for name, t in (("s", s), ("u", u), ("h", h), ("dh", dh)))
+    (s_ptr, s_st), (h_ptr, h_st), (g_ptr, g_st) = (
+        _recur_rows(name, t, shape, dtype, index) for name, t in (("s", s), ("h", h), ("dh", dh)))
+    if u is None and mean:
+        raise ValueError("the mean's gradients need u")
+    u_ptr, u_st = _recur_rows("u", u, shape, dtype, index) if u is not None else (None, 0)
     ds, du = _new(s, shape, dtype, stream), _new(s, shape, dtype, stream)
     dh0 = None if h0 is None else _new(s, (S, C), torch.float32, stream)
     rc = load().fem_recur_bwd(s_ptr, u_ptr, h_ptr, g_ptr, s_st, u_st, h_st, g_st, off, S, T, N, C, _TYPES[dtype], 1 if mean else 0,

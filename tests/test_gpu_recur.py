@@ -267,6 +267,26 @@ def test_streams_and_graphs():
     assert all(torch.equal(a, b) for a, b in zip(grads[:2], grads2[:2]))
 
 
+def test_many_short_sequences_beside_a_long_one():
+    """The chunks are counted by the long one's length, the others have none of them to do."""
+    lens, c = [1] * 3000 + [2000] + [0] * 500, 64
+    n = sum(lens)
+    s, u, dh = make(n, c, torch.bfloat16, 14)
+    off = offsets_of(lens)
+    h, last = fem.fem_recur_fwd(s, u, offsets=off, max_len=2000)
+    assert torch.equal(h[:3000], u[:3000])  # a first step has nothing to decay
+    want, want_last, hm, lm = ref.recur(s[3000:].cpu(), u[3000:].cpu(), [2000])
+    ref.check(h[3000:], want, hm, UNITS)
+    ref.check(last[3000:3001], want_last, lm, UNITS)
+    assert not last[3001:].any() and torch.equal(last[:3000], u[:3000].float())
+    ds, du, _ = fem.fem_recur_bwd(s, None, h, dh, offsets=off, max_len=2000)
+    assert torch.equal(du[:3000], dh[:3000]) and not ds[:3000].any()
+    grads, sizes = ref.recur_grads(s[3000:].cpu(), u[3000:].cpu(), h[3000:].cpu(), dh[3000:].cpu(), [2000])
+    ref.check(ds[3000:], grads[0], sizes[0], UNITS)
+    ref.check(du[3000:], grads[1], sizes[1], UNITS)
+    fem.check_device_error()
+
+
 def test_arrays_past_32_bits():
     """More than 2^32 elements: the last rows against a call on them alone, from the state before."""
     n, c, tail = 131200, 32768, 40
@@ -309,3 +329,5 @@ def test_refusals():
         fem.fem_recur_fwd(x.transpose(0, 1), x.transpose(0, 1))  # rows that are not evenly spaced
     with pytest.raises(ValueError):
         fem.fem_recur_bwd(s, u, s, dh, offsets=off, h0=h0, dstate=h0[:1])
+    with pytest.raises(ValueError):
+        fem.fem_recur_bwd(s, None, s, dh, offsets=off, mean=True)
