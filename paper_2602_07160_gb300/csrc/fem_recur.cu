@@ -295,8 +295,9 @@ __device__ __forceinline__ void meet(Map<V> &m, Map<V> *s_map) {
   if (inner == G - 1) s_map[(threadIdx.x >> 5) * L + lane % L] = m;
 }
 
-// The maps of the chunks but the last of each line, [line][chunks][L].  No thread waits for another: each walks a stretch of
-// its own.
+// The maps of the chunks but the last of each line, [line][chunks][L]; in the last one's place the state before the first
+// step, since the walk of the last chunk may write the new one over it before the others have begun.  No thread waits for
+// another: each walks a stretch of its own.
 template <typename T, int V, int L, bool MEAN, bool BWD, int GRAIN>
 __global__ void __launch_bounds__(32 * kWarps, 6) recur_maps_kernel(const RecurArgs a, int groups, int chunks, int per, Map<V> *maps) {
   constexpr int W = kWarps, R = kMapSteps<T>, U = 32 / L * W, S = 3;
@@ -308,6 +309,11 @@ __global__ void __launch_bounds__(32 * kWarps, 6) recur_maps_kernel(const RecurA
   const Chunk z = chunk_of<BWD, L * V, kSteps<T, BWD> * U>(a, groups, chunks, per);
   if (!z.ok || z.index == z.count - 1) return;  // such a chunk has a multiple of R U steps
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (z.index == 0 && a.first && threadIdx.x < L) {
+    const int c = z.c0 + lane * V;
+    const F x = z.row >= 0 ? load_state<V>(a.first, static_cast<long long>(z.row) * a.C + c, min(V, a.C - c)) : F::all(0.f);
+    maps[(static_cast<long long>(z.line) * chunks + z.count - 1) * L + lane] = {x, x};
+  }
   const long long each = z.n / U;
   Rg ring;
   ring.start(smem + warp * Rg::BYTES, a, z, warp * (32 / L), each, R);
@@ -402,9 +408,10 @@ __global__ void __launch_bounds__(32 * W, 16 / W)
   if (tiles > 0) ring.issue(0, 0);
   copy_commit();
 
-  F carry = a.first && z.row >= 0 ? load_state<V>(a.first, state_at, there) : F::all(0.f);
+  F carry = a.first && z.row >= 0 && z.count == 1 ? load_state<V>(a.first, state_at, there) : F::all(0.f);
   if (chunks > 1) {
     grid_dep_wait();  // the maps, and whatever ran before them
+    if (a.first && z.count > 1) carry = maps[(static_cast<long long>(z.line) * chunks + z.count - 1) * L + lc].a;
     if (z.index > 0) {  // the chunks before this one, a stretch of them a thread
       Map<V> m = {F::all(1.f), F::all(0.f)};
       const Map<V> *o = maps + static_cast<long long>(z.line) * chunks * L + lc;
