@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_fwd_kernel(const 
   auto weights = [&](int k, int i) {
     const float *p = k == 0 ? a.w_post : k == 1 ? a.w_pre : k == 2 ? a.b_post : a.b_pre;
     if (k >= 2 && !BIAS) p = nullptr;
-    return load_weights<S>(p, k < 2 ? 1.f : 0.f, D, lane, i);
+    return load_weights<S>(p, k < 2 ? 1.f : 0.f, D, lane, i, mine);
   };
   auto weight = [&](int k, int i) {
     if (HOLD && (BIAS || k < 2)) return kept_weights<S>(smem + k * S::WEIGHT, i);
@@ -129,7 +129,6 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_fwd_kernel(const 
         }
         FEM_EACH_PAIR r[i].v[j] = __ffma2_rn(v.v[j], both(a.scale), r[i].v[j]);
         store_piece<S, TX>(static_cast<TX *>(a.r) + at, nullptr, nullptr, 0, Dn, lane, mine, i, r[i]);
-        if (BIAS) FEM_EACH_PAIR r[i].v[j] = __fmul2_rn(r[i].v[j], mine.pair(1.f, i, j));  // a bias is not the row's behind its end
       }
     }
     if (a.pre != 0) {

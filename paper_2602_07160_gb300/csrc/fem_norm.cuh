@@ -306,17 +306,17 @@ __device__ __forceinline__ void store_piece(T *row, const HeadsView *v, const in
   }
 }
 
-// A weight vector's elements of a piece, `none` where there is no vector.
+// A weight vector's elements of a piece, `none` where there is no vector; 0 past the row's end.
 template <typename S>
-__device__ __forceinline__ Piece load_weights(const float *w, float none, int D, int lane, int i) {
+__device__ __forceinline__ Piece load_weights(const float *w, float none, int D, int lane, int i, const Mine<S> &mine) {
   Piece f;
   if (!w) {
-    FEM_EACH_PAIR f.v[j] = both(none);
+    FEM_EACH_PAIR f.v[j] = mine.pair(none, i, j);
   } else if constexpr (S::VEC) {
-    // past the end: any, nothing there counts
+    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
     const int e0 = S::at(lane, i, 0), e1 = S::at(lane, i, 4);
-    const float4 p = __ldg(reinterpret_cast<const float4 *>(w + (e0 < D ? e0 : 0)));
-    const float4 q = __ldg(reinterpret_cast<const float4 *>(w + (e1 < D ? e1 : 0)));
+    const float4 p = e0 < D ? __ldg(reinterpret_cast<const float4 *>(w + e0)) : zero;
+    const float4 q = e1 < D ? __ldg(reinterpret_cast<const float4 *>(w + e1)) : zero;
     f = {make_float2(p.x, p.y), make_float2(p.z, p.w), make_float2(q.x, q.y), make_float2(q.z, q.w)};
   } else {
 #pragma unroll

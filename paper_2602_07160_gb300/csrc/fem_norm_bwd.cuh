@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_bwd_kernel(const 
   constexpr bool HOLD = keeps_weights<S>(kRow<S, TX, TY>, kWeights<S, BIAS>);
   constexpr int kept = HOLD ? kWeights<S, BIAS> : 0;  // weights, ahead of the stages
   auto weights = [&](int k, int i) {
-    return load_weights<S>(k == 0 ? a.w_post : k == 1 ? a.w_pre : BIAS ? a.b_post : nullptr, k < 2 ? 1.f : 0.f, D, lane, i);
+    return load_weights<S>(k == 0 ? a.w_post : k == 1 ? a.w_pre : BIAS ? a.b_post : nullptr, k < 2 ? 1.f : 0.f, D, lane, i, mine);
   };
   auto weight = [&](int k, int i) {
     if (HOLD && (BIAS || k < 2)) return kept_weights<S>(smem + k * S::WEIGHT, i);
@@ -189,8 +189,7 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_bwd_kernel(const 
       }
       store_piece<S, TX>(static_cast<TX *>(a.dx) + at, nullptr, nullptr, 0, Dn, lane, mine, i, dx[i]);
       if (!branch) continue;
-      Piece e;  // nothing behind the row's end, where a mean has been taken off
-      FEM_EACH_PAIR e.v[j] = __fmul2_rn(dx[i].v[j], mine.pair(a.scale, i, j));
+      Piece e = times(dx[i], a.scale);  // behind the row's end the weights are 0, and what e is does not count
       y[i] = times(y[i], sigma);
       Piece value, slope;
       if (gated) {

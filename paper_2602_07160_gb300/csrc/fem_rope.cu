@@ -227,7 +227,7 @@ cudaError_t launch_rope_t(const RopeArgs &a, int num_sms, cudaStream_t stream) {
   for (int i = 0; i < (a.heads[1] ? 2 : 1); ++i)
     vec = vec && whole_pieces(a.in[i], sizeof(T)) && whole_pieces(a.out[i], sizeof(T));
   const Way way = !vec ? SINGLE : (INTER ? a.rotary : pairs) % PER == 0 ? WHOLE : SHIFTED;
-  const int pieces = way == SINGLE ? std::min(pairs, 128) : way == WHOLE && !INTER ? pairs / PER + (a.d - a.rotary) / PER : a.d / PER;
+  const int pieces = way == SINGLE ? std::min(std::max(pairs, (a.d - a.rotary) / 2), 128) : way == WHOLE && !INTER ? pairs / PER + (a.d - a.rotary) / PER : a.d / PER;
   const int lanes = 256 / pieces;  // at least 2
   // As few heads to a thread as the GPU has room for, up to eight; then tokens to a block, so that the fewest lanes idle.
   const long long room = 4ll * num_sms * lanes;

@@ -587,7 +587,7 @@ class Rope:
             raise FemError("fem_rope_turns", rc)
         signed = [v - (1 << 64) if v >> 63 else v for v in table]
         self.turns = torch.tensor(signed, dtype=torch.int64).to(device)
-        self.table, self.index = self.turns.data_ptr(), self.turns.get_device()
+        self.index = self.turns.get_device()
         self.rotary_dim, self.interleaved, self.amplitude = rotary_dim, int(bool(interleaved)), float(amplitude)
 
 
@@ -635,7 +635,7 @@ def fem_rope(rope: Rope, q, k=None, positions=None, inverse: bool = False, out=N
     pos = None
     if positions is not None:
         pos = _optional("positions", positions, (T,) if len(shape) == 3 else (B, T), torch.int32, index)
-    rc = load().fem_rope(qv, qo, Hq, kv, ko, Hk, B, T, d, _TYPES[dtype], rope.table, rope.rotary_dim, rope.interleaved,
+    rc = load().fem_rope(qv, qo, Hq, kv, ko, Hk, B, T, d, _TYPES[dtype], rope.turns.data_ptr(), rope.rotary_dim, rope.interleaved,
                          rope.amplitude, pos, 1 if inverse else 0, _stream_number(stream, index))
     if rc != 0:
         raise FemError("fem_rope", rc)
@@ -763,6 +763,8 @@ class BlockNorm:
 
     def __init__(self, width: int, post: str = "rms", pre: str = "rms", gate: str = "none", w_post=None, b_post=None,
                  w_pre=None, b_pre=None, scale: float = 1.0, eps: float = 1e-6):
+        if width < 1:
+            raise ValueError("width must be positive")
         if post not in self.KINDS or pre not in self.KINDS or gate not in self.ACTS:
             raise ValueError(f"post and pre are one of {list(self.KINDS)}, gate one of {list(self.ACTS)}")
         self.width, self.post, self.pre, self.gate, self.scale, self.eps = width, post, pre, gate, float(scale), float(eps)
@@ -776,8 +778,8 @@ class BlockNorm:
             if self.index not in (None, t.get_device()):
                 raise ValueError("the weights must be on one device")
             self.index = t.get_device()
-        self._fixed = (self.KINDS[post], self.KINDS[pre], self.ACTS[gate], self.scale, self.eps,
-                       *(0 if t is None else t.data_ptr() for t in (w_post, b_post, w_pre, b_pre)))
+        self._fixed = (self.KINDS[post], self.KINDS[pre], self.ACTS[gate], self.scale, self.eps)
+        self._addresses = [int if t is None else t.data_ptr for t in (w_post, b_post, w_pre, b_pre)]  # int() is 0
 
     def _call(self, name, x, y, gate):
         """((B, T, H, d), x's shape, x's and the branch's type, device) of a call; checks x, y and the gate."""
@@ -808,7 +810,8 @@ class BlockNorm:
         return (B, T, H, d), shape, dtype, y_type, index
 
     def _describe(self, sizes, x_type, y_type):
-        return _norm_bytes(*sizes, _TYPES[x_type], _TYPES[y_type], *self._fixed)
+        p, q, r, s = self._addresses
+        return _norm_bytes(*sizes, _TYPES[x_type], _TYPES[y_type], *self._fixed, p(), q(), r(), s())
 
 
 def _branch(name, t, x_shape, shape, dtype, index):

@@ -330,6 +330,35 @@ def test_rows_past_32_bits():
     assert torch.equal(back[0][-7:], want[0]) and torch.equal(back[1][-7:], want[1])
 
 
+def test_weights_are_read_at_each_call():
+    """Changed in place, and replaced behind the tensor."""
+    block, t = make(40, 64, "bf16", "rms", "rms", "none", 18)
+    before, _ = fem.fem_norm_fwd(block, t["x"], t["y"])
+    for change in (lambda w: w.mul_(2), lambda w: setattr(w, "data", torch.full((64,), 3.0, device="cuda"))):
+        change(block.weights["w_post"])
+        same = fem.BlockNorm(64, scale=0.7, eps=1e-5, **{n: None if w is None else w.clone() for n, w in block.weights.items()})
+        got, want = (fem.fem_norm_fwd(b, t["x"], t["y"]) for b in (block, same))
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and not torch.equal(got[0], before)
+
+
+@pytest.mark.parametrize("D", [1000, 1001, 200])
+def test_an_infinite_weight_stays_in_its_channel(D):
+    """Threads with no channel have no weight either."""
+    block, t = make(5, D, "f32", "rms", "none", "none", 19, weights=True)
+    fine, _ = fem.fem_norm_fwd(block, t["x"], t["y"])
+    fine_grads = fem.fem_norm_bwd(block, fine, t["y"], None, t["dr"])
+    block.weights["w_post"][0] = math.inf
+    r, _ = fem.fem_norm_fwd(block, t["x"], t["y"])
+    assert torch.equal(r[:, 1:], fine[:, 1:]) and torch.isinf(r[:, 0]).all()
+    dx, dy, _, dw, *_ = fem.fem_norm_bwd(block, r, t["y"], None, t["dr"])
+    assert torch.equal(dx, fine_grads[0]) and torch.equal(dw, fine_grads[3])
+    pre, t = make(5, D, "f32", "none", "rms", "none", 20)
+    _, z0 = fem.fem_norm_fwd(pre, t["x"])
+    pre.weights["w_pre"][0] = math.inf
+    _, z = fem.fem_norm_fwd(pre, t["x"])
+    assert torch.equal(z[:, 1:], z0[:, 1:])
+
+
 def test_refusals():
     block, t = make(6, 64, "bf16", "rms", "rms", "silu", 17)
     x, y, g = t["x"], t["y"], t["gate"]

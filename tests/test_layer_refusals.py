@@ -133,6 +133,8 @@ def test_the_binding_checks_its_tensors():
     with pytest.raises(ValueError):
         fem.BlockNorm(64, post="batch")
     with pytest.raises(ValueError):
+        fem.BlockNorm(0)
+    with pytest.raises(ValueError):
         fem.BlockNorm(64, w_post=x[0])  # not on a GPU
     with pytest.raises(ValueError):
         fem.Rope(16, scaling="other", device="cpu")
