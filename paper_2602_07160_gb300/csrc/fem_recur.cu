@@ -141,11 +141,9 @@ struct __align__(8 * V) Map {
   Vec<V> a, b;
 };
 
-// 16 or 4 bytes from global to shared memory, of which `bytes` are read and the rest is zero.
-template <int SIZE>
+// 16 bytes from global to shared memory, of which `bytes` are read and the rest is zero.
 __device__ __forceinline__ void copy_async(uint32_t dst, const void *src, int bytes) {
-  if (SIZE == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-  else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 
 template <int V>
@@ -182,11 +180,14 @@ struct Chunk {
 };
 
 // per: steps of a chunk, at least; more where a sequence is longer than the bound that the chunks were counted by.
+// First all lines' first chunks: those that short sequences lack come last, when the GPU is filled evenly (seven sequences
+// of 50 to 5000 steps of 1001 channels of fp32: 53 us, line after line 57).
 template <bool BWD, int CH, int TR>
 __device__ __forceinline__ Chunk chunk_of(const RecurArgs &a, int groups, int chunks, int per) {
   Chunk k;
-  k.line = blockIdx.x / chunks;
-  k.index = blockIdx.x % chunks;
+  const int lines = a.S * groups;
+  k.line = blockIdx.x % lines;
+  k.index = blockIdx.x / lines;
   k.q = k.line / groups;
   k.c0 = k.line % groups * CH;
   k.ok = sequence(a, k.q, k.lo, k.hi);
@@ -206,44 +207,59 @@ __device__ __forceinline__ Chunk chunk_of(const RecurArgs &a, int groups, int ch
 }
 
 // A warp's copies of IN arrays into its part of shared memory: of every array a line of L V channels for each of R steps of
-// its G threads, GRAIN bytes a copy.
+// its G threads, 16 bytes a copy.  Where lines do not start on 16 bytes (GRAIN 4 or 2, what they all start on) they are
+// copied with the rest of their first 16 bytes, which are the same allocation's, and nothing past their end, and lie as
+// far off 16 bytes in shared memory.  (Five sequences of 5000 steps of 1001 channels of fp32: 113 us, in copies of 4 bytes
+// 132; eight of 2048 of bf16: 44, in single loads 52.)  Results leave in words of GRAIN bytes.
 template <typename T, int V, int L, int R, int IN, int STAGES, bool BWD, int GRAIN>
 struct Ring {
-  static constexpr int G = 32 / L, WORD = V * sizeof(T), LINE = 32 * WORD, PART = R * LINE, BYTES = STAGES * IN * PART;
-  // A lane has PIECES copies of an array and tile: SPLIT in a line, where that is longer than 32, then STEP lines on
-  static constexpr int PIECES = PART / (32 * GRAIN), PER_LINE = LINE / GRAIN, SPLIT = PER_LINE > 32 ? PER_LINE / 32 : 1, STEP = 32 * SPLIT / PER_LINE;
-  static constexpr int WAY = BWD ? -static_cast<int>(sizeof(T)) : static_cast<int>(sizeof(T));
-  char *part;                    // the warp's
-  uint32_t to;                   // this lane's first piece
-  const char *src[IN][SPLIT];    // where it comes from, tile after tile
+  static constexpr bool AROUND = GRAIN < 16;
+  static constexpr int SIZE = sizeof(T), G = 32 / L, WORD = V * SIZE, LINE = 32 * WORD;
+  static constexpr int SPAN = L * WORD, PITCH = SPAN + (AROUND ? 16 : 0), PART = R * G * PITCH, BYTES = STAGES * IN * PART;
+  // A lane has PIECES words of GRAIN bytes of an array and tile: SPLIT in a line, where that is longer than 32, then STEP lines on
+  static constexpr int PIECES = R * LINE / (32 * GRAIN), PER_LINE = LINE / GRAIN, SPLIT = PER_LINE > 32 ? PER_LINE / 32 : 1, STEP = 32 * SPLIT / PER_LINE;
+  static constexpr int AROUNDS = SPAN / 16 + 1;  // copies of a line that starts anywhere
+  static constexpr int WAY = BWD ? -SIZE : SIZE;
+  char *part;                          // the warp's
+  uint32_t to;                         // and as an address in shared memory
+  const char *src[IN][AROUND ? 1 : SPLIT];  // where this lane's first copy comes from, tile after tile; AROUND: the warp's first line
   long long st[IN], most[IN];
-  const void *safe;              // an address to name where nothing is read
-  long long k[SPLIT], hop;       // the pieces' steps; steps between tiles
-  int c[SPLIT], bytes[SPLIT], whole;  // their byte among the channels, bytes that there are; tiles that need no look
+  uint32_t phase[IN];                  // AROUND: of this thread's first line, tile after tile
+  const char *safe;                    // an address to name where nothing is read
+  long long k[SPLIT], first, sub, hop; // the words' steps; the warp's first step, steps between its threads, between tiles
+  int c[SPLIT], bytes[SPLIT], whole, span;  // the words' byte among the channels, bytes that there are; tiles that need no look; bytes of a line
 
-  // sub: steps between the G threads' first ones; hop: between tiles
-  __device__ __forceinline__ void start(char *smem, const RecurArgs &a, const Chunk &z, int first_sub, long long sub, long long hop_) {
+  // first_sub: of the G threads; sub: steps between their first ones; hop: between tiles
+  __device__ __forceinline__ void start(char *smem, const RecurArgs &a, const Chunk &z, int first_sub, long long sub_, long long hop_) {
     const int lane = threadIdx.x & 31;
     part = smem;
-    to = smem_u32(smem) + lane * GRAIN;
+    to = smem_u32(smem);
+    sub = sub_;
     hop = hop_;
+    first = first_sub * sub;
+    span = min(SPAN, (a.C - z.c0) * SIZE);
 #pragma unroll
     for (int p = 0; p < SPLIT; ++p) {
       const int in_line = (lane + 32 * p) % PER_LINE * GRAIN;
-      c[p] = in_line % (L * WORD);
-      k[p] = (first_sub + in_line / (L * WORD)) * sub + lane / PER_LINE;
-      bytes[p] = max(0, min(GRAIN, (a.C - z.c0) * static_cast<int>(sizeof(T)) - c[p]));
+      c[p] = in_line % SPAN;
+      k[p] = first + in_line / SPAN * sub + lane / PER_LINE;
+      bytes[p] = max(0, min(GRAIN, span - c[p]));
     }
-    safe = a.s;
+    safe = reinterpret_cast<const char *>(reinterpret_cast<uintptr_t>(a.s) & ~static_cast<uintptr_t>(15));
     whole = 0;
   }
   // the row of the chunk's step k
   __device__ __forceinline__ static long long row(const Chunk &z, long long k) { return BWD ? z.hi - 1 - (z.k0 + k) : z.lo + z.k0 + k; }
   // array i, whose row lags `back` behind the step's; its steps from `most` on (of the chunk) are not there
   __device__ __forceinline__ void array(int i, const void *base, long long stride, int back, const Chunk &z, long long most_) {
+    const char *from = static_cast<const char *>(base) + z.c0 * SIZE;
+    if constexpr (AROUND) {
+      src[i][0] = from + (row(z, first) - back) * stride * SIZE;
+      phase[i] = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(src[i][0]) + (threadIdx.x & 31) / L * sub * WAY * stride);
+    } else {
 #pragma unroll
-    for (int p = 0; p < SPLIT; ++p)
-      src[i][p] = static_cast<const char *>(base) + ((row(z, k[p]) - back) * stride + z.c0) * static_cast<int>(sizeof(T)) + c[p];
+      for (int p = 0; p < SPLIT; ++p) src[i][p] = from + (row(z, k[p]) - back) * stride * SIZE + c[p];
+    }
     st[i] = stride;
     most[i] = most_;
   }
@@ -253,13 +269,28 @@ struct Ring {
     whole = GRAIN == 2 || z.c0 + L * V > a.C || left < 0 ? 0 : static_cast<int>(left / hop) + 1;
   }
   __device__ __forceinline__ void issue(int tl, int stage) {
-    if (tl < whole) {
+    const int lane = threadIdx.x & 31;
+    if constexpr (AROUND) {
+#pragma unroll
+      for (int s = 0; s < IN; ++s) {
+        const long long left = most[s] - first - tl * hop;  // steps that there are, from the warp's first one on
+#pragma unroll
+        for (int j = 0; j < (R * G * AROUNDS + 31) / 32; ++j) {
+          const int p = lane + 32 * j, line = p / AROUNDS, piece = p % AROUNDS * 16;
+          const int step = line % G * static_cast<int>(sub) + line / G;
+          if (R * G * AROUNDS % 32 != 0 && line >= R * G) break;
+          const char *at = src[s][0] + static_cast<long long>(step) * (WAY * static_cast<int>(st[s]));
+          const int off = static_cast<int>(reinterpret_cast<uintptr_t>(at) & 15);
+          const int there = step < left ? max(0, min(16, span + off - piece)) : 0;
+          copy_async(to + (stage * IN + s) * PART + line * PITCH + piece, there ? at - off + piece : safe, there);
+        }
+      }
+    } else if (tl < whole) {
 #pragma unroll
       for (int s = 0; s < IN; ++s)
 #pragma unroll
         for (int j = 0; j < PIECES; ++j)
-          if constexpr (GRAIN >= 4)
-            copy_async<GRAIN>(to + (stage * IN + s) * PART + 32 * j * GRAIN, src[s][j % SPLIT] + WAY * STEP * (j / SPLIT) * st[s], GRAIN);
+          copy_async(to + (stage * IN + s) * PART + (32 * j + lane) * 16, src[s][j % SPLIT] + WAY * STEP * (j / SPLIT) * st[s], 16);
     } else {
 #pragma unroll
       for (int s = 0; s < IN; ++s)
@@ -267,18 +298,32 @@ struct Ring {
         for (int j = 0; j < PIECES; ++j) {
           const char *from = src[s][j % SPLIT] + WAY * STEP * (j / SPLIT) * st[s];
           const int there = k[j % SPLIT] + tl * hop + STEP * (j / SPLIT) < most[s] ? bytes[j % SPLIT] : 0;
-          const int at = (stage * IN + s) * PART + 32 * j * GRAIN;
-          if constexpr (GRAIN >= 4) copy_async<GRAIN>(to + at, there ? from : static_cast<const char *>(safe), there);
-          else *reinterpret_cast<uint16_t *>(part + at + (threadIdx.x & 31) * GRAIN) = there ? *reinterpret_cast<const uint16_t *>(from) : uint16_t(0);
+          copy_async(to + (stage * IN + s) * PART + (32 * j + lane) * 16, there ? from : safe, there);
         }
     }
 #pragma unroll
     for (int s = 0; s < IN; ++s)
 #pragma unroll
-      for (int p = 0; p < SPLIT; ++p) src[s][p] += WAY * hop * st[s];
+      for (int p = 0; p < (AROUND ? 1 : SPLIT); ++p) src[s][p] += WAY * hop * st[s];
   }
+  // this thread's channels of array `slot` at its step i
   __device__ __forceinline__ Word<T, V> word(int stage, int slot, int i) const {
-    return *reinterpret_cast<const Word<T, V> *>(part + (stage * IN + slot) * PART + i * LINE + (threadIdx.x & 31) * WORD);
+    const int lane = threadIdx.x & 31;
+    const char *line = part + (stage * IN + slot) * PART + (i * G + lane / L) * PITCH + lane % L * WORD;
+    if constexpr (AROUND) {
+      line += (phase[slot] + static_cast<uint32_t>(i * WAY * static_cast<int>(st[slot]))) & 15;
+      if constexpr (WORD == 8) {  // on 4 bytes
+        const float *p = reinterpret_cast<const float *>(line);
+        return Word<T, V>::of({make_float2(p[0], p[1])});
+      }
+    }
+    return *reinterpret_cast<const Word<T, V> *>(line);
+  }
+  // after a tile's words
+  __device__ __forceinline__ void next() {
+    if constexpr (AROUND)
+#pragma unroll
+      for (int s = 0; s < IN; ++s) phase[s] += static_cast<uint32_t>(WAY * hop * st[s]);
   }
 };
 
@@ -342,6 +387,7 @@ __global__ void __launch_bounds__(32 * kWarps, 6) recur_maps_kernel(const RecurA
       m.a = m.a * d;
     }
     stage = stage == S - 1 ? 0 : stage + 1;
+    ring.next();
     __syncwarp();
   }
   meet<V, L>(m, s_map);
@@ -451,6 +497,7 @@ __global__ void __launch_bounds__(32 * W, 16 / W)
       }
       m.a = m.a * d[i];
     }
+    ring.next();
     meet<V, L>(m, s_map + stage * W * L);
     __syncthreads();
     F x = tl == 0 ? carry : s_carry[(stage ^ 1) * L + lc];
