@@ -1177,6 +1177,7 @@ int fem_norm_bwd(const fem_norm *norm, const void *r, const fem_heads *y, const 
   int blocks = 0;
   cudaError_t e = norm_bwd_blocks(a, norm->x_type, norm->y_type, ds->num_sms, &blocks);
   if (e != cudaSuccess) return map_cuda(e);
+  if (!dw_post && !db_post && !dw_pre && !db_pre) return map_cuda(launch_norm_bwd(a, norm->x_type, norm->y_type, blocks, s));
   e = ws_alloc(ds, reinterpret_cast<void **>(&a.part), static_cast<size_t>(blocks) * 4 * a.D * sizeof(float), s);
   if (e != cudaSuccess) return map_cuda(e);
   e = launch_norm_bwd(a, norm->x_type, norm->y_type, blocks, s);

@@ -56,7 +56,7 @@ struct NormArgs {
   void *dx;
   HeadsView dy, dgate;
   float *dw[4];        // dw_post, db_post, dw_pre, db_pre, or NULL
-  float *part;         // [blocks, 4, D] at most
+  float *part;         // [blocks, 4, D] at most, or NULL: no sums
 };
 cudaError_t launch_norm_fwd(const NormArgs &a, int x_type, int y_type, int num_sms, cudaStream_t stream);
 // `blocks` of norm_bwd_blocks, each of which leaves a row of partial sums of the weights' gradients.

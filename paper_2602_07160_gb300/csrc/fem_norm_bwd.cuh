@@ -220,6 +220,7 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_bwd_kernel(const 
     for (int i = 0; i < S::K; ++i) store_piece<S, TY>(heads_row(a.dy, b, t), &a.dy, off[2], a.d, Dn, lane, mine, i, dx[i]);
   }
 
+  if (!a.part) return;  // no weights' gradients wanted
   grid_dep_launch_dependents();
   // the block's sums: its rows' groups one after the other into row blockIdx.x of the partial sums
   float *part = a.part + static_cast<long long>(blockIdx.x) * SUMS * D;

@@ -907,8 +907,7 @@ def fem_norm_bwd(norm: BlockNorm, r, y=None, gate=None, dr=None, dz=None, stream
             dgv = _fresh_branch(dgate, shape, y_shape)
     pre, weights = norm.pre != "none", norm.weights
     wanted = (y is not None, y is not None and weights["b_post"] is not None, pre, pre and weights["b_pre"] is not None)
-    rows = iter(_new(r, (sum(wanted), norm.width), torch.float32, stream).unbind(0)) if any(wanted) else None
-    sums = [next(rows) if on else None for on in wanted]
+    sums = [_new(r, (norm.width,), torch.float32, stream) if on else None for on in wanted]
     rc = load().fem_norm_bwd(norm._describe(sizes, dtype, y_type), r.data_ptr(), yv, gv, dr_ptr, dz_ptr, dx.data_ptr(), dyv, dgv,
                              *(None if t is None else t.data_ptr() for t in sums), _stream_number(stream, index))
     if rc != 0:

@@ -359,6 +359,25 @@ def test_an_infinite_weight_stays_in_its_channel(D):
     assert torch.equal(z[:, 1:], z0[:, 1:])
 
 
+def test_some_of_the_weights_gradients():
+    """At the C entry each of them may be left out, and all."""
+    rows, D = 300, 256
+    block, t = make(rows, D, "f32", "layer", "layer", "silu", 21)
+    x, y, g, dr, dz = (t[n] for n in ("x", "y", "gate", "dr", "dz"))
+    want = fem.fem_norm_bwd(block, x, y, g, dr, dz)
+    describe = block._describe((1, rows, 1, D), torch.float32, torch.float32)
+    heads = lambda v: fem._heads_bytes(v.data_ptr(), 0, D, 0)
+    for keep in ((), (0,), (1,), (2,), (3,), (0, 2), (1, 3)):
+        got = [torch.empty_like(x) for _ in range(3)]
+        sums = [torch.empty(D, device="cuda") if i in keep else None for i in range(4)]
+        rc = fem.load().fem_norm_bwd(describe, x.data_ptr(), heads(y), heads(g), dr.data_ptr(), dz.data_ptr(), got[0].data_ptr(),
+                                     heads(got[1]), heads(got[2]), *(None if s is None else s.data_ptr() for s in sums),
+                                     torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        assert rc == 0 and all(torch.equal(a, b) for a, b in zip(got, want))
+        assert all(s is None or torch.equal(s, b) for s, b in zip(sums, want[3:]))
+
+
 def test_refusals():
     block, t = make(6, 64, "bf16", "rms", "rms", "silu", 17)
     x, y, g = t["x"], t["y"], t["gate"]
