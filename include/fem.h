@@ -416,7 +416,10 @@ int fem_rope_turns(int rotary, double base, int scaling, double factor, double c
  *   turns        : device, uint64 [rotary/2] (fem_rope_turns); amplitude A
  *   positions    : device, int32 [B, T], any sign, or NULL: 0 .. T - 1 in every b
  * d up to 1024, rotary even and 2 .. d.  Angles are exact to fp32 rounding for
- * positions up to 2^28, the rotation is fp32 arithmetic rounded once.  B = 0 or T = 0 does nothing.
+ * positions up to 2^28 in magnitude (beyond, to the rates' 2^-64 of a turn times
+ * the position); the rotation is fp32 arithmetic rounded once.  An output overlaps
+ * no input but its own in place.  B T and heads below 2^31 - 256 and 2^30, else
+ * FEM_ERR_UNSUPPORTED.  B = 0 or T = 0 does nothing.
  */
 int fem_rope(const fem_heads *q, const fem_heads *q_out, int Hq, const fem_heads *k, const fem_heads *k_out, int Hk,
              int B, int T, int d, int type, const uint64_t *turns, int rotary, int interleaved, float amplitude,
@@ -439,13 +442,16 @@ int fem_rope(const fem_heads *q, const fem_heads *q_out, int Hq, const fem_heads
  *                 and after the last, or NULL: zero, not kept.  The same array
  *                 updates states in place.
  *   state_rows  : device, int32 [S]: each sequence's row of them, or NULL: row s.
- *                 Negative: that sequence starts from zero and is not kept.  Which
- *                 of two sequences with one row stays is not defined.
+ *                 Negative: that sequence starts from zero and is not kept.  Two
+ *                 sequences must not share a row that is written: which of them
+ *                 stays, and what the other starts from, is not defined.
  * Rows of no sequence are not written.  A sequence of length zero hands its state
  * on.  States, decays and sums are fp32; the same inputs give the same bits.  An
  * offset or state row outside its array is left out and recorded
  * (fem_check_device_error returns FEM_ERR_INVALID_ARG).  S = 0 does nothing.  Row
- * strides and C below 2^20 (else FEM_ERR_UNSUPPORTED).  One launch, or two with a
+ * strides and C below 2^20, and S ceil(C / 32) below 2^27 (else
+ * FEM_ERR_UNSUPPORTED).  Outputs overlap no input but states in place.  Rows that
+ * do not start on 16 bytes are read with the rest of their first 16.  One launch, or two with a
  * workspace from the library's stream-ordered pool where sequences times channels
  * are too few for the GPU and sequences are cut into chunks.
  */
@@ -497,8 +503,11 @@ typedef struct {
  *   y, gate : device, heads; gate NULL: none.  y NULL: no block before (r = x is
  *             not written, gate must be NULL)
  *   z       : device, [N, D] contiguous; NULL if and only if pre is NONE
- * D up to 16384.  Sums and statistics in fp32; r rounded once, z formed from r
- * before its rounding.  N = 0 does nothing.  No workspace.
+ * D up to 16384, N below 2^31 - 2^20 (else FEM_ERR_UNSUPPORTED; so is a bf16 stream
+ * of a float32 branch).  Sums and statistics in fp32; r rounded once, z formed from
+ * r before its rounding.  Outputs overlap no input but r in place of x.  Rows that
+ * do not start on 16 bytes may be read with the rest of their first 16.  N = 0 does
+ * nothing.  No workspace.
  */
 int fem_norm_fwd(const fem_norm *norm, const void *x, const fem_heads *y, const fem_heads *gate, void *r, void *z,
                  void *stream);

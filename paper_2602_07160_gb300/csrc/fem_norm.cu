@@ -12,7 +12,7 @@ namespace fem {
 
 namespace {
 
-// Blocks on an SM that registers allow for: 80 a thread, 64 from 512 threads on.
+// Blocks on an SM that registers allow for: 80 a thread, 64 with 1024 threads.
 template <typename S>
 constexpr int kBlocks = S::THREADS > 512 ? 1 : S::THREADS > 256 ? 2 : 768 / S::THREADS;
 template <typename S, typename TX, typename TY>
@@ -51,16 +51,19 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_fwd_kernel(const 
     return load_weights<S>(p, k < 2 ? 1.f : 0.f, D, lane, i, mine);
   };
   auto weight = [&](int k, int i) {
-    if (HOLD && (BIAS || k < 2)) return kept_weights<S>(smem + k * S::WEIGHT, i);
+    if (HOLD && (BIAS || k < 2)) return kept_weights<S>(smem + k * S::WEIGHT, lane, i);
     return weights(k, i);
   };
-  if (HOLD)
-    for (int k = 0; k < (BIAS ? 4 : 2); ++k)
+  if (HOLD) {
+    if (threadIdx.x < S::TPR)
+      for (int k = 0; k < (BIAS ? 4 : 2); ++k)
 #pragma unroll
-      for (int i = 0; i < S::K; ++i) keep_weights<S>(smem + k * S::WEIGHT, weights(k, i), i);
-  const int step = gridDim.x * S::ROWS;
+        for (int i = 0; i < S::K; ++i) keep_weights<S>(smem + k * S::WEIGHT, weights(k, i), lane, i);
+    __syncthreads();
+  }
+  const int rows = blockDim.x / S::TPR, step = gridDim.x * rows;  // at a time: of the block, of the grid
   auto heads_row = [&](const HeadsView &v, int b, int t) { return static_cast<const TY *>(v.p) + heads_start<S>(v, b, t); };
-  int first = blockIdx.x * S::ROWS, n = first + threadIdx.x / S::TPR, stage = 0;  // the block's rows at a time, the thread's
+  int first = blockIdx.x * rows, n = first + threadIdx.x / S::TPR, stage = 0;  // the block's rows at a time, the thread's
   RowAt here(n, a.T), ahead = here;
   auto issue = [&](int n, int stage) {
     const bool there = n < a.N;
@@ -72,7 +75,7 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_fwd_kernel(const 
     ahead.go(step, a.T);
   };
   if constexpr (S::COPIED) {
-    if (S::VEC) clear_smem<S>(smem + kept, stages * stage_bytes);
+    if (S::VEC) clear_smem<S>(smem + kept, stages * stage_bytes, D);
     for (int k = 0; k < stages - 1; ++k) {
       if (k == 0 || first < a.N - k * step) issue(n + k * step, k);
       copy_commit();
@@ -153,8 +156,8 @@ struct Launch {
       int per_sm = 0;
       const cudaError_t e = resident_blocks<Tag<S, TX, TY, BIAS>>(kernel, S::THREADS, kSmem<S, TX, TY, BIAS>, &per_sm);
       if (e != cudaSuccess) return e;
-      const int groups = (a.N + S::ROWS - 1) / S::ROWS;
-      kernel<<<std::min(groups, per_sm * num_sms), S::THREADS, kSmem<S, TX, TY, BIAS>, stream>>>(a);
+      const int blocks = blocks_of(a.N, S::ROWS, per_sm, num_sms);
+      kernel<<<blocks, S::TPR * rows_of(a.N, S::ROWS, blocks), kSmem<S, TX, TY, BIAS>, stream>>>(a);
       return cudaGetLastError();
     }
   };
@@ -165,8 +168,8 @@ cudaError_t launch_types(const NormArgs &a, int num_sms, cudaStream_t stream) {
   constexpr int RUN = sizeof(TX) == 4 ? 4 : 8;
   const bool bias = a.b_post || a.b_pre;
   const Way way = way_of(a, norm_pieces(a, sizeof(TY), RUN), staged_row<TX>(a.D) + 2 * staged_row<TY>(a.D), bias ? 4 : 2, 3);
-  return bias ? with_shape<RUN, false, 1, Launch<TX, TY, true>::template With>(a.D, way, a, num_sms, stream)
-              : with_shape<RUN, false, 1, Launch<TX, TY, false>::template With>(a.D, way, a, num_sms, stream);
+  return bias ? with_shape<RUN, false, 1, 768, 768, 0, 1024, Launch<TX, TY, true>::template With>(a.D, way, a, num_sms, stream)
+              : with_shape<RUN, false, 1, 768, 768, 0, 1024, Launch<TX, TY, false>::template With>(a.D, way, a, num_sms, stream);
 }
 
 }  // namespace

@@ -7,6 +7,7 @@
 // neighbouring threads have neighbouring elements and read them when they need them.
 #pragma once
 
+#include <algorithm>
 #include <type_traits>
 
 #include "fem_layer.cuh"
@@ -22,7 +23,7 @@ struct RowShape {
   static constexpr bool VEC = RUN_ > 1, STAGED = RUN_ == 0, COPIED = VEC || STAGED;
   static constexpr int RUNS = VEC ? K_ * 8 / RUN : 1;  // of a thread, places to keep
   static constexpr int WARPS = TPR_ / 32;               // of a row
-  static constexpr int WEIGHT = THREADS * K * 32;       // bytes of a vector of weights
+  static constexpr int WEIGHT = TPR_ * K * 32;          // bytes of a vector of weights
 
   // element j of piece i of thread `lane` of the row
   __device__ static __forceinline__ int at(int lane, int i, int j) { return (lane + (i * (8 / RUN) + j / RUN) * TPR) * RUN + j % RUN; }
@@ -216,10 +217,11 @@ constexpr int rows_smem(int row, int weights, int blocks) {
   const int share = kMostSmem / blocks - (blocks > 1 ? 2048 : 0), least = row + (keeps_weights<S>(row, weights) ? weights : 0);
   return !S::COPIED ? 0 : S::STAGED || share > least ? share : least;
 }
-// Zeros in the first `bytes` of shared memory behind `from`, 16 a thread.
+// Zeros in the first `bytes` of shared memory behind `from`, 16 a thread, where rows leave some of it unwritten.
 template <typename S>
-__device__ __forceinline__ void clear_smem(char *from, int bytes) {
-  for (int i = threadIdx.x * 16; i < bytes; i += S::THREADS * 16) *reinterpret_cast<uint4 *>(from + i) = make_uint4(0, 0, 0, 0);
+__device__ __forceinline__ void clear_smem(char *from, int bytes, int D) {
+  if (D == S::TPR * 8 * S::K) return;
+  for (int i = threadIdx.x * 16; i < bytes; i += blockDim.x * 16) *reinterpret_cast<uint4 *>(from + i) = make_uint4(0, 0, 0, 0);
   __syncthreads();
 }
 __device__ __forceinline__ void rows_wait(int stages) {
@@ -327,18 +329,18 @@ __device__ __forceinline__ Piece load_weights(const float *w, float none, int D,
   }
   return f;
 }
-// The same out of shared memory, where each thread keeps its own: registers are short, and beside so much shared memory
-// the L1 cache is too small for what is read row after row.
+// The same out of shared memory, in which all rows of a block share them: registers are short, and beside so much shared
+// memory the L1 cache is too small for what is read row after row.
 template <typename S>
-__device__ __forceinline__ void keep_weights(char *slot, const Piece &f, int i) {
-  float4 *p = reinterpret_cast<float4 *>(slot) + 2 * i * S::THREADS + threadIdx.x;
+__device__ __forceinline__ void keep_weights(char *slot, const Piece &f, int lane, int i) {
+  float4 *p = reinterpret_cast<float4 *>(slot) + 2 * i * S::TPR + lane;
   p[0] = make_float4(f.v[0].x, f.v[0].y, f.v[1].x, f.v[1].y);
-  p[S::THREADS] = make_float4(f.v[2].x, f.v[2].y, f.v[3].x, f.v[3].y);
+  p[S::TPR] = make_float4(f.v[2].x, f.v[2].y, f.v[3].x, f.v[3].y);
 }
 template <typename S>
-__device__ __forceinline__ Piece kept_weights(const char *slot, int i) {
-  const float4 *s = reinterpret_cast<const float4 *>(slot) + 2 * i * S::THREADS + threadIdx.x;
-  const float4 p = s[0], q = s[S::THREADS];
+__device__ __forceinline__ Piece kept_weights(const char *slot, int lane, int i) {
+  const float4 *s = reinterpret_cast<const float4 *>(slot) + 2 * i * S::TPR + lane;
+  const float4 p = s[0], q = s[S::TPR];
   return {make_float2(p.x, p.y), make_float2(p.z, p.w), make_float2(q.x, q.y), make_float2(q.z, q.w)};
 }
 __device__ __forceinline__ Piece weighted(const Piece &x, const Piece &w, const Piece &b) {
@@ -379,13 +381,14 @@ __device__ __forceinline__ void gate_piece(const Piece &g, int act, Piece &value
 // How rows are read: runs that the arrays allow to copy, rows copied whole, single elements.
 enum Way { SINGLE, STAGED, PIECES };
 
-// The shape for rows of D elements.  A thread has one piece, or two with TWO, in blocks of 128 threads, where no threads
-// are idle for it; WIDE of them in rows of more than 4096 elements.
-template <int RUN, bool TWO, int WIDE, template <typename> class F, typename... Args>
+// The shape for rows of D elements.  A thread has one piece, or two with TWO, where no threads are idle for it; WIDE of them
+// in rows of more than 4096 elements.  Where runs are copied a block is all that an SM has: ONE threads with one piece, or
+// NARROW where a row's do not divide them, PAIR with two, FOUR in rows of 2048 to 4096 elements.
+template <int RUN, bool TWO, int WIDE, int ONE, int NARROW, int PAIR, int FOUR, template <typename> class F, typename... Args>
 cudaError_t with_shape(int D, Way way, Args &&...args) {
-  constexpr int K = TWO ? 2 : 1, MOST = TWO ? 128 : 256;
+  constexpr int K = TWO ? 2 : 1, MOST = TWO ? PAIR : ONE;
   if (way == SINGLE) {
-    if (D <= 1024) return F<RowShape<128, 1, 1>>::call(args...);
+    if (D <= 1024) return F<RowShape<128, 1, 1, 128>>::call(args...);
     if (D <= 4096) return F<RowShape<512, 1, 1>>::call(args...);
     return F<RowShape<1024, 2, 1>>::call(args...);
   }
@@ -396,13 +399,13 @@ cudaError_t with_shape(int D, Way way, Args &&...args) {
     if (D <= 5120) return F<RowShape<640, 1, 0>>::call(args...);
     return F<RowShape<1024, 1, 0>>::call(args...);
   }
-  if (D <= 256) return F<RowShape<32, 1, RUN>>::call(args...);
+  if (D <= 256) return F<RowShape<32, 1, RUN, ONE>>::call(args...);
   if (D <= 512) return F<RowShape<64 / K, K, RUN, MOST>>::call(args...);
-  if (D <= 768) return F<RowShape<96, 1, RUN>>::call(args...);
+  if (D <= 768) return F<RowShape<96, 1, RUN, NARROW>>::call(args...);
   if (D <= 1024) return F<RowShape<128 / K, K, RUN, MOST>>::call(args...);
-  if (D <= 1536) return F<RowShape<192 / K, K, RUN, MOST>>::call(args...);
+  if (D <= 1536) return F<RowShape<192 / K, K, RUN, TWO ? PAIR : NARROW>>::call(args...);
   if (D <= 2048) return F<RowShape<256 / K, K, RUN, MOST>>::call(args...);
-  if (D <= 4096) return F<RowShape<512, 1, RUN>>::call(args...);
+  if (D <= 4096) return F<RowShape<512, 1, RUN, FOUR>>::call(args...);
   if (D <= 8192) return F<RowShape<1024 / WIDE, WIDE, RUN>>::call(args...);
   return F<RowShape<1024, 2, RUN>>::call(args...);
 }
@@ -419,6 +422,14 @@ inline Way way_of(const NormArgs &a, bool pieces, int row, int vectors, int bloc
   const int smem = threads == 256 ? kMostSmem / blocks - 2048 : kMostSmem, kept = threads < 1024 ? vectors * threads * 32 : 0;
   return 2 * rows * row + kept <= smem ? STAGED : SINGLE;
 }
+
+// Blocks for N rows in a shape of `rows` at a time, of which an SM holds `per_sm`: as many as there are SMs where each then
+// has fewer rows at a time.  (100 rows of 2048, gradients: 17 us, 21 in blocks of three rows.)
+inline int blocks_of(int N, int rows, int per_sm, int num_sms) {
+  const int few = (N + num_sms - 1) / num_sms;
+  return few < rows ? (N + few - 1) / few : std::min((N + rows - 1) / rows, per_sm * num_sms);
+}
+inline int rows_of(int N, int rows, int blocks) { return std::min(rows, (N + blocks - 1) / blocks); }
 
 // Whether every array allows 16-byte pieces of eight elements.
 inline bool norm_pieces(const NormArgs &a, int y_size, int run) {

@@ -29,7 +29,7 @@ namespace {
 // Blocks on an SM that registers allow for: 170 a thread with two pieces, 112 to 128 with one.  (Spilled ones cost more than
 // fewer warps do: beside so much shared memory the L1 cache is small.)
 template <typename S>
-constexpr int kBlocks = S::THREADS > 256 ? 1 : S::THREADS <= 128 ? 384 / S::THREADS : S::THREADS < 256 ? 576 / S::THREADS : 2;
+constexpr int kBlocks = S::THREADS > 256 ? 1 : 512 / S::THREADS;
 template <typename S, typename TX, typename TY>
 constexpr int kRow = 2 * Copied<S, TX>::BYTES + 3 * Copied<S, TY>::BYTES;
 template <typename S, bool BIAS>
@@ -58,13 +58,16 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_bwd_kernel(const 
     return load_weights<S>(k == 0 ? a.w_post : k == 1 ? a.w_pre : BIAS ? a.b_post : nullptr, k < 2 ? 1.f : 0.f, D, lane, i, mine);
   };
   auto weight = [&](int k, int i) {
-    if (HOLD && (BIAS || k < 2)) return kept_weights<S>(smem + k * S::WEIGHT, i);
+    if (HOLD && (BIAS || k < 2)) return kept_weights<S>(smem + k * S::WEIGHT, lane, i);
     return weights(k, i);
   };
-  if (HOLD)
-    for (int k = 0; k < (BIAS ? 3 : 2); ++k)
+  if (HOLD) {
+    if (threadIdx.x < S::TPR)
+      for (int k = 0; k < (BIAS ? 3 : 2); ++k)
 #pragma unroll
-      for (int i = 0; i < S::K; ++i) keep_weights<S>(smem + k * S::WEIGHT, weights(k, i), i);
+        for (int i = 0; i < S::K; ++i) keep_weights<S>(smem + k * S::WEIGHT, weights(k, i), lane, i);
+    __syncthreads();
+  }
   // r, dr, dz, y and the gate in a stage, those that there are
   const int part_x = stage_part<S, TX>(D), part_y = stage_part<S, TY>(D);
   const int at_dr = normed ? part_x : 0, at_dz = at_dr + (a.dr ? part_x : 0), at_y = at_dz + (normed ? part_y : 0);
@@ -81,9 +84,9 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_bwd_kernel(const 
       off[2][k] = static_cast<int>(head_offset(a.dy, a.d, e));
       off[3][k] = static_cast<int>(head_offset(a.dgate, a.d, e));
     }
-  const int step = gridDim.x * S::ROWS;
+  const int rows = blockDim.x / S::TPR, step = gridDim.x * rows;  // at a time: of the block, of the grid
   auto heads_row = [&](const HeadsView &v, int b, int t) { return static_cast<TY *>(v.p) + heads_start<S>(v, b, t); };
-  int first = blockIdx.x * S::ROWS, n = first + threadIdx.x / S::TPR, stage = 0;  // the block's rows at a time, the thread's
+  int first = blockIdx.x * rows, n = first + threadIdx.x / S::TPR, stage = 0;  // the block's rows at a time, the thread's
   RowAt here(n, a.T), ahead = here;
   auto issue = [&](int n, int stage) {
     const bool there = n < a.N;
@@ -100,7 +103,7 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_bwd_kernel(const 
     ahead.go(step, a.T);
   };
   if constexpr (S::COPIED) {
-    if (S::VEC) clear_smem<S>(smem + kept, stages * stage_bytes);
+    if (S::VEC) clear_smem<S>(smem + kept, stages * stage_bytes, D);
     for (int k = 0; k < stages - 1; ++k) {
       if (k == 0 || first < a.N - k * step) issue(n + k * step, k);
       copy_commit();
@@ -222,21 +225,30 @@ __global__ void __launch_bounds__(S::THREADS, kBlocks<S>) norm_bwd_kernel(const 
 
   if (!a.part) return;  // no weights' gradients wanted
   grid_dep_launch_dependents();
-  // the block's sums: its rows' groups one after the other into row blockIdx.x of the partial sums
-  float *part = a.part + static_cast<long long>(blockIdx.x) * SUMS * D;
-  for (int g = 0; g < S::ROWS; ++g) {
-    if (S::ROWS > 1) __syncthreads();
-    if (static_cast<int>(threadIdx.x) / S::TPR != g) continue;
+  // the block's sums into row blockIdx.x of the partial sums: those of its rows meet in shared memory (where a row's copies
+  // had 10 bytes an element and array or more, and now have 4 a sum), in order
+  float *part = a.part + static_cast<long long>(blockIdx.x) * SUMS * D, *to = part;
+  if constexpr (S::ROWS > 1) {
+    to = reinterpret_cast<float *>(smem) + threadIdx.x / S::TPR * SUMS * D;
+    __syncthreads();
+  }
 #pragma unroll
-    for (int k = 0; k < SUMS; ++k)
+  for (int k = 0; k < SUMS; ++k)
 #pragma unroll
-      for (int i = 0; i < S::K; ++i)
+    for (int i = 0; i < S::K; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int e = S::at(lane, i, j);
-          const float x = j % 2 ? acc[k][i].v[j / 2].y : acc[k][i].v[j / 2].x;
-          if (e < D) part[k * D + e] = g == 0 ? x : part[k * D + e] + x;
-        }
+      for (int j = 0; j < 8; ++j) {
+        const int e = S::at(lane, i, j);
+        if (e < D) to[k * D + e] = j % 2 ? acc[k][i].v[j / 2].y : acc[k][i].v[j / 2].x;
+      }
+  if constexpr (S::ROWS > 1) {
+    static_assert(S::COPIED, "shared memory to meet in");
+    __syncthreads();
+    for (int e = threadIdx.x; e < SUMS * D; e += blockDim.x) {
+      float x = 0.f;
+      for (int g = 0; g < rows; ++g) x += reinterpret_cast<const float *>(smem)[g * SUMS * D + e];
+      part[e] = x;
+    }
   }
 }
 
@@ -254,10 +266,10 @@ struct Launch {
       if (num_sms > 0) {
         int per_sm = 0;
         const cudaError_t e = resident_blocks<Tag<S, TX, TY, BIAS>>(kernel, S::THREADS, smem, &per_sm);
-        *blocks = std::min((a.N + S::ROWS - 1) / S::ROWS, per_sm * num_sms);
+        *blocks = e == cudaSuccess ? blocks_of(a.N, S::ROWS, per_sm, num_sms) : 0;
         return e;
       }
-      kernel<<<*blocks, S::THREADS, smem, stream>>>(a);
+      kernel<<<*blocks, S::TPR * rows_of(a.N, S::ROWS, *blocks), smem, stream>>>(a);
       const cudaError_t e = cudaGetLastError();
       if (e != cudaSuccess || !(a.dw[0] || a.dw[1] || a.dw[2] || a.dw[3])) return e;
       return launch_norm_sums(a, *blocks, BIAS ? 4 : 2, stream);
@@ -272,8 +284,8 @@ cudaError_t types(const NormArgs &a, int num_sms, int *blocks, cudaStream_t stre
   const bool pieces = norm_pieces(a, sizeof(TY), RUN) && (a.D <= 8192 || (2 * sizeof(TX) + 3 * sizeof(TY)) * 16384 <= kMostSmem);
   const bool bias = a.dw[1] || a.dw[3] || a.b_post;
   const Way way = way_of(a, pieces, 2 * staged_row<TX>(a.D) + 3 * staged_row<TY>(a.D), bias ? 3 : 2, 2);
-  return bias ? with_shape<RUN, RUN == 8, 2, Launch<TX, TY, true>::template With>(a.D, way, a, num_sms, blocks, stream)
-              : with_shape<RUN, RUN == 8, 2, Launch<TX, TY, false>::template With>(a.D, way, a, num_sms, blocks, stream);
+  return bias ? with_shape<RUN, RUN == 8, 2, 512, 576, 384, 512, Launch<TX, TY, true>::template With>(a.D, way, a, num_sms, blocks, stream)
+              : with_shape<RUN, RUN == 8, 2, 512, 576, 384, 512, Launch<TX, TY, false>::template With>(a.D, way, a, num_sms, blocks, stream);
 }
 
 }  // namespace
