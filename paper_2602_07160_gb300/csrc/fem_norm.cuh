@@ -381,12 +381,13 @@ __device__ __forceinline__ void gate_piece(const Piece &g, int act, Piece &value
 // How rows are read: runs that the arrays allow to copy, rows copied whole, single elements.
 enum Way { SINGLE, STAGED, PIECES };
 
-// The shape for rows of D elements.  A thread has one piece, or two with TWO, where no threads are idle for it; WIDE of them
-// in rows of more than 4096 elements.  Where runs are copied a block is all that an SM has: ONE threads with one piece, or
-// NARROW where a row's do not divide them, PAIR with two, FOUR in rows of 2048 to 4096 elements.
-template <int RUN, bool TWO, int WIDE, int ONE, int NARROW, int PAIR, int FOUR, template <typename> class F, typename... Args>
+// The shape for rows of D elements.  A thread has one piece, or two in rows up to 1024 elements with TWO, up to 2048 with
+// LONG_TWO, where no threads are idle for it; WIDE of them in rows of more than 4096.  Where runs are copied a block is all
+// that an SM has: ONE threads with one piece, or NARROW where a row's do not divide them, PAIR with two, FOUR in rows of
+// 2048 to 4096 elements.
+template <int RUN, bool TWO, bool LONG_TWO, int WIDE, int ONE, int NARROW, int PAIR, int FOUR, template <typename> class F, typename... Args>
 cudaError_t with_shape(int D, Way way, Args &&...args) {
-  constexpr int K = TWO ? 2 : 1, MOST = TWO ? PAIR : ONE;
+  constexpr int K = TWO ? 2 : 1, MOST = TWO ? PAIR : ONE, KL = LONG_TWO ? 2 : 1;
   if (way == SINGLE) {
     if (D <= 1024) return F<RowShape<128, 1, 1, 128>>::call(args...);
     if (D <= 4096) return F<RowShape<512, 1, 1>>::call(args...);
@@ -403,8 +404,8 @@ cudaError_t with_shape(int D, Way way, Args &&...args) {
   if (D <= 512) return F<RowShape<64 / K, K, RUN, MOST>>::call(args...);
   if (D <= 768) return F<RowShape<96, 1, RUN, NARROW>>::call(args...);
   if (D <= 1024) return F<RowShape<128 / K, K, RUN, MOST>>::call(args...);
-  if (D <= 1536) return F<RowShape<192 / K, K, RUN, TWO ? PAIR : NARROW>>::call(args...);
-  if (D <= 2048) return F<RowShape<256 / K, K, RUN, MOST>>::call(args...);
+  if (D <= 1536) return F<RowShape<192 / KL, KL, RUN, LONG_TWO ? PAIR : NARROW>>::call(args...);
+  if (D <= 2048) return F<RowShape<256 / KL, KL, RUN, LONG_TWO ? PAIR : ONE>>::call(args...);
   if (D <= 4096) return F<RowShape<512, 1, RUN, FOUR>>::call(args...);
   if (D <= 8192) return F<RowShape<1024 / WIDE, WIDE, RUN>>::call(args...);
   return F<RowShape<1024, 2, RUN>>::call(args...);

@@ -284,8 +284,10 @@ cudaError_t types(const NormArgs &a, int num_sms, int *blocks, cudaStream_t stre
   const bool pieces = norm_pieces(a, sizeof(TY), RUN) && (a.D <= 8192 || (2 * sizeof(TX) + 3 * sizeof(TY)) * 16384 <= kMostSmem);
   const bool bias = a.dw[1] || a.dw[3] || a.b_post;
   const Way way = way_of(a, pieces, 2 * staged_row<TX>(a.D) + 3 * staged_row<TY>(a.D), bias ? 3 : 2, 2);
-  return bias ? with_shape<RUN, RUN == 8, 2, 512, 576, 384, 512, Launch<TX, TY, true>::template With>(a.D, way, a, num_sms, blocks, stream)
-              : with_shape<RUN, RUN == 8, 2, 512, 576, 384, 512, Launch<TX, TY, false>::template With>(a.D, way, a, num_sms, blocks, stream);
+  // 32768 rows of 2048 of bf16: 199 us with two pieces, 224 with one; of fp32 two leave registers short
+  constexpr bool TWO = RUN == 8;
+  return bias ? with_shape<RUN, TWO, TWO, 2, 512, 576, 384, 512, Launch<TX, TY, true>::template With>(a.D, way, a, num_sms, blocks, stream)
+              : with_shape<RUN, TWO, TWO, 2, 512, 576, 384, 512, Launch<TX, TY, false>::template With>(a.D, way, a, num_sms, blocks, stream);
 }
 
 }  // namespace

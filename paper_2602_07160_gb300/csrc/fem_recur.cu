@@ -562,8 +562,6 @@ __global__ void __launch_bounds__(32 * W, 16 / W)
 }
 
 // Sequences of few steps: a thread walks V channels of one, four steps' loads under way.
-constexpr int kFewSteps = 16;
-
 template <typename T, int V, bool MEAN, bool BWD>
 __global__ void __launch_bounds__(128) recur_few_kernel(const RecurArgs a, int blocks_c) {
   using F = Vec<V>;
@@ -638,8 +636,14 @@ struct Split {
 // Eight sequences of 8192 steps of 2048 channels of bf16, 256 lines: forward 140 us in CTAs of 8 warps, 163 of 4, 207 in
 // chunks; backward 253, 303, 336.  One of 131072 steps of 256 channels, 4 lines: forward 68 us in 128 chunks, 78 in 64,
 // 74 in 160; backward 88, 107, 103.
+//
+// Few steps fill no tile: a thread walks them alone, 0.13 us a step, where the GPU is not filled four times over, and each
+// such filling costs a walk by tiles some 2.4 us.  2048 channels of bf16, forward, by threads alone and by tiles: 8
+// sequences of 8 steps 3.1 and 3.6 us, of 16 4.2 and 3.6; 64 of 32 7.5 and 11.3, of 64 13.0 and 12.4; 512 of 16 19 and 79,
+// of 64 67 and 88.
 Split split_of(const RecurArgs &a, int V, int steps, int num_sms) {
-  if (a.T <= kFewSteps) return {0, 0, 0, 0};
+  const double rounds = static_cast<double>(a.S) * a.C / (32 * V) / (4 * num_sms);
+  if (a.T <= std::min(64.0, 8 + 13 * rounds)) return {0, 0, 0, 0};
   int lanes = 32;
   while (lanes > 8 && a.C <= lanes * V / 2) lanes /= 2;
   // lines of the full length that there is work for: sequences may be shorter

@@ -267,6 +267,24 @@ def test_streams_and_graphs():
     assert all(torch.equal(a, b) for a, b in zip(grads[:2], grads2[:2]))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_many_sequences_of_some_steps(dtype):
+    """So many that a thread walks each channel of one alone, and a longer one than was said."""
+    lens, c = [40] * 255 + [131, 0, 1], 512
+    n = sum(lens)
+    s, u, dh = make(n, c, dtype, 15)
+    h0, dlast = states(len(lens), c, 16)
+    off = offsets_of(lens)
+    h, last = fem.fem_recur_fwd(s, u, offsets=off, max_len=40, h0=h0, mean=True)
+    want, want_last, hm, lm = ref.recur(s.cpu(), u.cpu(), lens, h0.cpu(), True)
+    ref.check(h, want, hm, UNITS)
+    ref.check(last, want_last, lm, UNITS)
+    got = fem.fem_recur_bwd(s, u, h, dh, offsets=off, max_len=40, h0=h0, dstate=dlast, mean=True)
+    grads, sizes = ref.recur_grads(s.cpu(), u.cpu(), h.cpu(), dh.cpu(), lens, h0.cpu(), dlast.cpu(), True)
+    for g, w, m in zip(got, grads, sizes):
+        ref.check(g, w, m, UNITS)
+
+
 def test_many_short_sequences_beside_a_long_one():
     """The chunks are counted by the long one's length, the others have none of them to do."""
     lens, c = [1] * 3000 + [2000] + [0] * 500, 64
