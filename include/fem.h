@@ -416,8 +416,8 @@ int fem_rope_turns(int rotary, double base, int scaling, double factor, double c
  *   turns        : device, uint64 [rotary/2] (fem_rope_turns); amplitude A
  *   positions    : device, int32 [B, T], any sign, or NULL: 0 .. T - 1 in every b
  * d up to 1024, rotary even and 2 .. d.  Angles are exact to fp32 rounding for
- * positions up to 2^28 in magnitude (beyond, to the rates' 2^-64 of a turn times
- * the position); the rotation is fp32 arithmetic rounded once.  An output overlaps
+ * positions up to 2^28 in magnitude (beyond, off by 2^-56 of a turn a position at
+ * most: the rates are formed in double); the rotation is fp32 arithmetic rounded once.  An output overlaps
  * no input but its own in place.  B T and heads below 2^31 - 256 and 2^30, else
  * FEM_ERR_UNSUPPORTED.  B = 0 or T = 0 does nothing.
  */

@@ -1,10 +1,11 @@
 // What the forward and backward kernels of the norms share (include/fem.h, fem_norm): a row's elements in registers.
 //
-// TPR threads take a row, K pieces of eight elements each; a block goes through rows, as many at a time as 256 (128)
-// threads have room for.  Where the row's length, alignment and strides allow (VEC) a piece is one or two 16-byte
+// TPR threads take a row, K pieces of eight elements each; a block goes through rows, as many at a time as it has threads
+// for.  Where the row's length, alignment and strides allow (VEC) a piece is one or two 16-byte
 // copies and neighbouring threads have neighbouring pieces; the next row's copies into shared memory are under way while
 // a row is worked on, and as a thread reads back only what it copied itself, no barrier stands between.  Elsewhere
-// neighbouring threads have neighbouring elements and read them when they need them.
+// neighbouring threads have neighbouring elements and read them when they need them: 32768 rows of 2048 of bf16, forward,
+// take 108 us in pieces, 157 copied whole and read singly (a way for rows that start anywhere), 770 without copies.
 #pragma once
 
 #include <algorithm>
@@ -411,6 +412,9 @@ cudaError_t with_shape(int D, Way way, Args &&...args) {
   return F<RowShape<1024, 2, RUN>>::call(args...);
 }
 
+// Rows that start anywhere take three times an aligned one's time copied whole (16384 rows of 4097 of bf16: forward 143 us,
+// gradients 360) and ten times without (540, 1260).
+//
 // The way for a call whose rows of all arrays, staged, take `row` bytes: two of them have to fit beside the weights, in
 // blocks of 256 threads of which `blocks` are on an SM.
 inline Way way_of(const NormArgs &a, bool pieces, int row, int vectors, int blocks) {

@@ -7,6 +7,9 @@
 //
 // Bound by memory: every element is read once and written once, and a token's cosines and sines are formed once for
 // all its heads, in shared memory.
+//
+// Measured: 16383 tokens of 32 + 8 heads of 128, bf16, 56 us, 6.0 TB/s; 8192 of 16 + 16 heads of 64, half of each, fp32
+// pairs of neighbours 23 us, 5.8 TB/s.
 #include <algorithm>
 
 #include "fem_layer.cuh"
@@ -64,7 +67,8 @@ constexpr int kHeads = 4;  // of a thread under way
 
 // How a head is shared out.  WHOLE: a thread has 16 bytes of each half, 16 bytes of neighbours, or 16 bytes to copy, whose
 // cosines and sines stay in registers from head to head.  SHIFTED: where the halves do not end on 16 bytes a thread has
-// any 16 bytes of the head and finds their other halves in shared memory.  SINGLE: every pieces-th pair.
+// any 16 bytes of the head and finds their other halves in shared memory.  SINGLE: every pieces-th pair.  (16383 tokens of
+// 32 + 8 heads of 128, bf16: WHOLE 56 us, SHIFTED 132, SINGLE 465; 8192 of heads of 80, 74 turned: SHIFTED 42, SINGLE 85.)
 enum Way { SINGLE, WHOLE, SHIFTED };
 
 template <typename T, bool INTER, Way WAY>

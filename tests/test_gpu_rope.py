@@ -1,6 +1,6 @@
 """Rotary positions on the GPU against their 64-bit form (needs a GB300).
 
-Tolerance: the output's half step, and 10 roundings of fp32 of A (|a| + |b|): cosine and sine are off by 2 ulp (4 units)
+Tolerance: the output's half step, and 10 roundings of fp32 of A (|a| + |b|): cosine and sine are off by 4 units at most
 and by what the remainder of the turn is rounded (pi/4 units), then come the amplitude (1), each product (1) and their
 sum (1); the rates' and positions' part is under a unit for positions below 2^24.
 """
