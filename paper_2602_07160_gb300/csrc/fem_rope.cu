@@ -121,6 +121,16 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a, int tokens,
     // every thread goes round as often as the one with the most heads: the others wait for it
     const int rounds = (all + kHeads * step - 1) / (kHeads * step);
     uint4 *buf = reinterpret_cast<uint4 *>(s_cs);
+    float2 w[PER];  // what an element and its other half are taken by
+    int other[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = min(at + i, a.rotary - 1);
+      const bool second = INTER ? e & 1 : e >= pairs;
+      w[i] = cs[INTER ? e / 2 : second ? e - pairs : e];
+      if (!second) w[i].y = -w[i].y;
+      other[i] = INTER ? e ^ 1 : second ? e - pairs : e + pairs;
+    }
     for (int it = 0; it < rounds; ++it) {
       const int from = h0 + it * kHeads * step;
       if (it > 0) load(from);
@@ -137,12 +147,8 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a, int tokens,
         x[u].get(f);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-          const int e = at + i;
-          if (e >= a.rotary) break;
-          const bool second = INTER ? i & 1 : e >= pairs;
-          const float2 w = cs[INTER ? e / 2 : second ? e - pairs : e];
-          const float other = to_f32(head[INTER ? e ^ 1 : second ? e - pairs : e + pairs]);
-          f[i] = second ? f[i] * w.x + other * w.y : f[i] * w.x - other * w.y;
+          const float turned = f[i] * w[i].x + to_f32(head[other[i]]) * w[i].y;
+          f[i] = at + i < a.rotary ? turned : f[i];
         }
         x[u].put(f);
         x[u].store(place(a.out, h) + at);
