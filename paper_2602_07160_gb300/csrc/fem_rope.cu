@@ -65,17 +65,18 @@ struct Chunk {
 
 constexpr int kHeads = 4;  // of a thread under way
 
-// How a head is shared out.  WHOLE: a thread has 16 bytes of each half, 16 bytes of neighbours, or 16 bytes to copy, whose
-// cosines and sines stay in registers from head to head.  SHIFTED: where the halves do not end on 16 bytes a thread has
+// How a head is shared out.  WHOLE: a thread has 16 bytes of each half, twice 16 bytes of neighbours, or twice 16 bytes to
+// copy, whose cosines and sines stay in registers from head to head (twice: 16383 tokens of 32 + 8 heads of 128 in
+// neighbours 57 us, once 67; of 16 + 4 heads of 256, half turned, 57 and 79).  SHIFTED: where the halves do not end on 16 bytes a thread has
 // any 16 bytes of the head and finds their other halves in shared memory.  SINGLE: every pieces-th pair.  (16383 tokens of
-// 32 + 8 heads of 128, bf16: WHOLE 56 us, SHIFTED 132, SINGLE 465; 8192 of heads of 80, 74 turned: SHIFTED 42, SINGLE 85.)
+// 32 + 8 heads of 128, bf16: WHOLE 56 us, SHIFTED 132, SINGLE 465; 8192 of heads of 80, 74 turned: SHIFTED 32, SINGLE 85.)
 enum Way { SINGLE, WHOLE, SHIFTED };
 
 template <typename T, bool INTER, Way WAY>
 __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a, int tokens, int pieces, int hl) {
   extern __shared__ __align__(16) float2 s_cs[];  // [tokens][rotary / 2], SHIFTED behind [kHeads][256] pieces
   constexpr bool VEC = WAY == WHOLE;
-  constexpr int PER = Chunk<T>::PER, TURNS = INTER ? PER / 2 : PER;
+  constexpr int PER = Chunk<T>::PER;
   const int pairs = a.rotary / 2, first = blockIdx.x * tokens, rows = a.B * a.T, all = a.heads[0] + a.heads[1];
   const int piece = threadIdx.x % pieces, lane = threadIdx.x / pieces, tok = lane / hl, n = first + tok;
   const int turned = INTER ? a.rotary / PER : pairs / PER;  // pieces of the rotated part
@@ -85,7 +86,11 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a, int tokens,
     const int which = h >= a.heads[0];
     return static_cast<T *>(v[which].p) + b * v[which].sb + t * v[which].st + (which ? h - a.heads[0] : h) * v[which].sh;
   };
-  const int at = WAY == SINGLE ? 0 : WAY == SHIFTED ? piece * PER : piece >= turned ? a.rotary + (piece - turned) * PER : piece * PER;
+  // VEC: a thread's first 16 bytes, the second ones `gap` behind them if there are `two`
+  const bool copies = VEC && !INTER && piece >= turned;
+  const int at = WAY == SINGLE ? 0 : copies ? a.rotary + (piece - turned) * PER : piece * PER;
+  const int gap = INTER ? pieces * PER : copies ? (pieces - turned) * PER : pairs;
+  const bool two = VEC && (INTER || copies ? at + gap < a.d : true);
   Chunk<T> x[kHeads], y[kHeads];
   auto load = [&](int from) {
 #pragma unroll
@@ -94,7 +99,7 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a, int tokens,
       if (!on || h >= all) break;
       const T *src = place(a.in, h) + at;
       x[u].load(src);
-      if (VEC && !INTER && piece < turned) y[u].load(src + pairs);
+      if (two) y[u].load(src + gap);
     }
   };
   if (WAY != SINGLE) load(h0);  // under way while the angles are formed
@@ -159,10 +164,25 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a, int tokens,
   }
   if (!on) return;
   if constexpr (VEC) {
-    float2 c[TURNS];
-    if (piece < turned)
+    float2 c[PER];  // neighbours: the first pairs' and the second ones'
+    const bool turns = piece < turned, turns_too = INTER && piece + pieces < turned;
 #pragma unroll
-      for (int i = 0; i < TURNS; ++i) c[i] = cs[piece * TURNS + i];
+    for (int i = 0; i < PER; ++i) {
+      const bool second = INTER && i >= PER / 2;
+      if (second ? turns_too : turns) c[i] = cs[INTER ? (piece + (second ? pieces : 0)) * (PER / 2) + i % (PER / 2) : piece * PER + i];
+    }
+    auto turn_neighbours = [&](Chunk<T> &v, int from) {
+      float f[PER];
+      v.get(f);
+#pragma unroll
+      for (int i = 0; i < PER; i += 2) {
+        const float2 w = c[(from + i / 2) % PER];
+        const float p = f[i] * w.x - f[i + 1] * w.y;
+        f[i + 1] = f[i + 1] * w.x + f[i] * w.y;
+        f[i] = p;
+      }
+      v.put(f);
+    };
     for (int from = h0; from < all; from += kHeads * step) {
       if (from != h0) load(from);
 #pragma unroll
@@ -170,30 +190,23 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a, int tokens,
         const int h = from + u * step;
         if (h >= all) break;
         T *dst = place(a.out, h) + at;
-        if (piece < turned) {
+        if constexpr (INTER) {
+          if (turns) turn_neighbours(x[u], 0);
+          if (turns_too) turn_neighbours(y[u], PER / 2);
+        } else if (turns) {
           float f[PER], g[PER];
           x[u].get(f);
-          if (INTER) {
+          y[u].get(g);
 #pragma unroll
-            for (int i = 0; i < PER; i += 2) {
-              const float p = f[i] * c[i / 2].x - f[i + 1] * c[i / 2].y;
-              f[i + 1] = f[i + 1] * c[i / 2].x + f[i] * c[i / 2].y;
-              f[i] = p;
-            }
-          } else {
-            y[u].get(g);
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-              const float2 w = c[i % TURNS];
-              const float p = f[i] * w.x - g[i] * w.y;
-              g[i] = g[i] * w.x + f[i] * w.y;
-              f[i] = p;
-            }
-            y[u].put(g);
-            y[u].store(dst + pairs);
+          for (int i = 0; i < PER; ++i) {
+            const float p = f[i] * c[i].x - g[i] * c[i].y;
+            g[i] = g[i] * c[i].x + f[i] * c[i].y;
+            f[i] = p;
           }
           x[u].put(f);
+          y[u].put(g);
         }
+        if (two) y[u].store(dst + gap);
         x[u].store(dst);
       }
     }
@@ -237,7 +250,7 @@ cudaError_t launch_rope_t(const RopeArgs &a, int num_sms, cudaStream_t stream) {
   for (int i = 0; i < (a.heads[1] ? 2 : 1); ++i)
     vec = vec && whole_pieces(a.in[i], sizeof(T)) && whole_pieces(a.out[i], sizeof(T));
   const Way way = !vec ? SINGLE : (INTER ? a.rotary : pairs) % PER == 0 ? WHOLE : SHIFTED;
-  const int pieces = way == SINGLE ? std::min(std::max(pairs, (a.d - a.rotary) / 2), 128) : way == WHOLE && !INTER ? pairs / PER + (a.d - a.rotary) / PER : a.d / PER;
+  const int pieces = way == SINGLE ? std::min(std::max(pairs, (a.d - a.rotary) / 2), 128) : way == SHIFTED ? a.d / PER : INTER ? (a.d / PER + 1) / 2 : pairs / PER + ((a.d - a.rotary) / PER + 1) / 2;
   const int lanes = 256 / pieces;  // at least 2
   // As few heads to a thread as the GPU has room for, up to eight; then tokens to a block, so that the fewest lanes idle.
   const long long room = 4ll * num_sms * lanes;
