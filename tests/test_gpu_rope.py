@@ -38,7 +38,8 @@ def compare(got, x, pos, rates, plan, inverse=False):
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("N,Hq,Hk,d,r", [(1, 1, 1, 16, 16), (3, 4, 1, 64, 32), (37, 12, 3, 128, 128), (5, 5, 2, 80, 74),
                                          (9, 3, 3, 2, 2), (2, 7, 1, 33, 18), (130, 2, 1, 256, 64), (4, 1, 1, 1024, 1024),
-                                         (3, 2, 1, 1023, 1022), (700, 33, 9, 64, 64)])
+                                         (3, 2, 1, 1023, 1022), (700, 33, 9, 64, 64), (6, 3, 2, 8, 8), (6, 3, 1, 24, 24),
+                                         (7, 3, 1, 24, 16), (7, 3, 1, 40, 16), (6, 2, 2, 24, 8)])
 def test_rows(N, Hq, Hk, d, r, interleaved, dtype):
     """Queries and keys as views of one projection's output, positions in any order."""
     qkv = make((N, Hq + 2 * Hk, d), dtype, N + d)
