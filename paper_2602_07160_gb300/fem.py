@@ -756,7 +756,7 @@ class BlockNorm:
 
     ``post`` and ``pre`` name P and Q: "none", "rms" or "layer" (``pre`` "none": there is no z); ``gate`` the gate's act:
     "none" (no gate), "identity", "sigmoid" or "silu".  The weights are float32 [width] CUDA tensors or None (1 and 0); the object
-    keeps them and reads them at each call."""
+    keeps them, and looks at and reads them at each call."""
 
     KINDS = {"none": 0, "rms": 1, "layer": 2}
     ACTS = {"none": 0, "identity": 0, "sigmoid": 1, "silu": 2}
@@ -773,13 +773,27 @@ class BlockNorm:
         for name, t in self.weights.items():
             if t is None:
                 continue
-            if t.dtype != torch.float32 or t.shape != (width,) or not t.is_contiguous() or t.device.type != "cuda":
+            if t.device.type != "cuda":
                 raise ValueError(f"{name} must be a contiguous float32 CUDA tensor of shape ({width},)")
             if self.index not in (None, t.get_device()):
                 raise ValueError("the weights must be on one device")
             self.index = t.get_device()
         self._fixed = (self.KINDS[post], self.KINDS[pre], self.ACTS[gate], self.scale, self.eps)
-        self._addresses = [int if t is None else t.data_ptr for t in (w_post, b_post, w_pre, b_pre)]  # int() is 0
+        self._vector = torch.Size((width,))
+        self._addresses()
+
+    def _addresses(self):
+        """The weights' addresses for a call, each looked at again: a module that changes its type or device replaces
+        what is behind a parameter."""
+        got = []
+        for name, t in self.weights.items():
+            if t is None:
+                got.append(0)
+                continue
+            if t.dtype is not torch.float32 or t.shape != self._vector or t.get_device() != self.index or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous float32 CUDA tensor of shape ({self.width},) on the device it came from")
+            got.append(t.data_ptr())
+        return got
 
     def _call(self, name, x, y, gate):
         """((B, T, H, d), x's shape, x's and the branch's type, device) of a call; checks x, y and the gate."""
@@ -810,8 +824,7 @@ class BlockNorm:
         return (B, T, H, d), shape, dtype, y_type, index
 
     def _describe(self, sizes, x_type, y_type):
-        p, q, r, s = self._addresses
-        return _norm_bytes(*sizes, _TYPES[x_type], _TYPES[y_type], *self._fixed, p(), q(), r(), s())
+        return _norm_bytes(*sizes, _TYPES[x_type], _TYPES[y_type], *self._fixed, *self._addresses())
 
 
 def _branch(name, t, x_shape, shape, dtype, index):

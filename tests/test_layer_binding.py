@@ -1,0 +1,69 @@
+"""The binding of the operators around the read against a stand-in library and stand-in devices (CPU only)."""
+import types
+
+import pytest
+import torch
+
+from paper_2602_07160_gb300 import fem
+
+D = 64
+
+
+class Library:
+    """Takes every call and does nothing."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append(name)
+            return 0
+        return call
+
+
+@pytest.fixture
+def library(monkeypatch):
+    """Host tensors, whose device index is -1, pass for those of the current device."""
+    lib = Library()
+    monkeypatch.setattr(fem, "load", lambda: lib)
+    monkeypatch.setattr(fem, "_current", lambda index: None)
+    monkeypatch.setattr(fem, "_stream_number", lambda stream, index: 0)
+    return lib
+
+
+class Weight:
+    """What BlockNorm looks at of a CUDA parameter; `data` is what a module replaces when it changes type or device."""
+
+    def __init__(self, data, index=-1):
+        self.data, self.index = data, index
+
+    device = types.SimpleNamespace(type="cuda")
+    dtype = property(lambda self: self.data.dtype)
+    shape = property(lambda self: self.data.shape)
+    get_device = lambda self: self.index  # noqa: E731
+    is_contiguous = lambda self: self.data.is_contiguous()  # noqa: E731
+    data_ptr = lambda self: self.data.data_ptr()  # noqa: E731
+
+
+CHANGES = {"bf16": lambda w: setattr(w, "data", w.data.bfloat16()), "shorter": lambda w: setattr(w, "data", w.data[:D - 1].clone()),
+           "longer": lambda w: setattr(w, "data", torch.ones(D + 1)), "of two axes": lambda w: setattr(w, "data", w.data.view(1, D)),
+           "strided": lambda w: setattr(w, "data", torch.ones(2 * D)[::2]), "elsewhere": lambda w: setattr(w, "index", 0)}
+
+
+@pytest.mark.parametrize("name", ["w_post", "b_post", "w_pre", "b_pre"])
+@pytest.mark.parametrize("change", list(CHANGES))
+def test_a_weight_that_changed_is_refused(library, name, change):
+    """`module.bfloat16()` and `module.cpu()` replace what is behind a parameter that the object keeps."""
+    weights = {n: Weight(torch.ones(D)) for n in ("w_post", "b_post", "w_pre", "b_pre")}
+    block = fem.BlockNorm(D, **weights)
+    x = torch.zeros((3, D))
+    calls = (lambda: fem.fem_norm_fwd(block, x, x), lambda: fem.fem_norm_bwd(block, x, x, dz=x))
+    for call in calls:
+        call()
+    assert library.calls == ["fem_norm_fwd", "fem_norm_bwd"]
+    CHANGES[change](weights[name])
+    for call in calls:
+        with pytest.raises(ValueError, match=name):
+            call()
+    assert library.calls == ["fem_norm_fwd", "fem_norm_bwd"]
