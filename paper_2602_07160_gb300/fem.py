@@ -12,6 +12,7 @@ import ctypes
 import os
 import struct
 import threading
+import types
 
 import torch
 
@@ -566,6 +567,18 @@ def _fresh_heads(t, shape):
     return _heads_bytes(t.data_ptr(), shape[1] * shape[2] * shape[3], shape[3], shape[2] * shape[3])
 
 
+class _Settled:
+    """Its attributes stay as the constructor leaves them, which ends with `_settle`: the calls take what it made of them."""
+
+    def _settle(self):
+        self.__dict__["_settled"] = True
+
+    def __setattr__(self, name, value):
+        if "_settled" in self.__dict__:
+            raise AttributeError(f"a {type(self).__name__}'s {name} cannot be changed: make another one")
+        object.__setattr__(self, name, value)
+
+
 class Rope:
     """The rates of rotary positions, for ``fem_rope``: of every head the first ``rotary_dim`` elements turn in pairs,
     elements i and i + rotary_dim/2, or 2 i and 2 i + 1 where ``interleaved``, by pos * base^(-2 i / rotary_dim).
@@ -749,14 +762,14 @@ def fem_recur_bwd(s, u, h, dh, offsets=None, max_len=None, h0=None, dstate=None,
 _norm_bytes = struct.Struct("@9i2f4P").pack  # fem_norm of include/fem.h
 
 
-class BlockNorm:
+class BlockNorm(_Settled):
     """A block's end and the next one's start, for ``fem_norm_fwd`` and ``fem_norm_bwd``:
 
         r = x + scale act(gate) (w_post P(y) + b_post),    z = w_pre Q(r) + b_pre
 
     ``post`` and ``pre`` name P and Q: "none", "rms" or "layer" (``pre`` "none": there is no z); ``gate`` the gate's act:
     "none" (no gate), "identity", "sigmoid" or "silu".  The weights are float32 [width] CUDA tensors or None (1 and 0); the object
-    keeps them, and looks at and reads them at each call."""
+    keeps them, and looks at and reads them at each call.  Its attributes cannot be assigned to."""
 
     KINDS = {"none": 0, "rms": 1, "layer": 2}
     ACTS = {"none": 0, "identity": 0, "sigmoid": 1, "silu": 2}
@@ -768,9 +781,9 @@ class BlockNorm:
         if post not in self.KINDS or pre not in self.KINDS or gate not in self.ACTS:
             raise ValueError(f"post and pre are one of {list(self.KINDS)}, gate one of {list(self.ACTS)}")
         self.width, self.post, self.pre, self.gate, self.scale, self.eps = width, post, pre, gate, float(scale), float(eps)
-        self.weights = {"w_post": w_post, "b_post": b_post, "w_pre": w_pre, "b_pre": b_pre}
+        self._weights = {"w_post": w_post, "b_post": b_post, "w_pre": w_pre, "b_pre": b_pre}
         self.index = None  # of the weights' device
-        for name, t in self.weights.items():
+        for name, t in self._weights.items():
             if t is None:
                 continue
             if t.device.type != "cuda":
@@ -780,13 +793,19 @@ class BlockNorm:
             self.index = t.get_device()
         self._fixed = (self.KINDS[post], self.KINDS[pre], self.ACTS[gate], self.scale, self.eps)
         self._vector = torch.Size((width,))
+        self._settle()
         self._addresses()
+
+    @property
+    def weights(self):
+        """The weights by name, to be read: what they hold may change, which there are may not."""
+        return types.MappingProxyType(self._weights)
 
     def _addresses(self):
         """The weights' addresses for a call, each looked at again: a module that changes its type or device replaces
         what is behind a parameter."""
         got = []
-        for name, t in self.weights.items():
+        for name, t in self._weights.items():
             if t is None:
                 got.append(0)
                 continue
@@ -918,7 +937,7 @@ def fem_norm_bwd(norm: BlockNorm, r, y=None, gate=None, dr=None, dz=None, stream
             gv = _branch("gate", gate, shape, y_shape, y_type, index)
             dgate = _new(r, y_shape, y_type, stream)
             dgv = _fresh_branch(dgate, shape, y_shape)
-    pre, weights = norm.pre != "none", norm.weights
+    pre, weights = norm.pre != "none", norm._weights
     wanted = (y is not None, y is not None and weights["b_post"] is not None, pre, pre and weights["b_pre"] is not None)
     sums = [_new(r, (norm.width,), torch.float32, stream) if on else None for on in wanted]
     rc = load().fem_norm_bwd(norm._describe(sizes, dtype, y_type), r.data_ptr(), yv, gv, dr_ptr, dz_ptr, dx.data_ptr(), dyv, dgv,

@@ -1,4 +1,5 @@
 """The binding of the operators around the read against a stand-in library and stand-in devices (CPU only)."""
+import copy
 import types
 
 import pytest
@@ -67,3 +68,23 @@ def test_a_weight_that_changed_is_refused(library, name, change):
         with pytest.raises(ValueError, match=name):
             call()
     assert library.calls == ["fem_norm_fwd", "fem_norm_bwd"]
+
+
+@pytest.mark.parametrize("name,value", [("width", 32), ("post", "layer"), ("pre", "none"), ("gate", "silu"), ("scale", 2.0), ("eps", 1e-3),
+                                        ("index", 0), ("weights", {})])
+def test_a_norm_stays_as_it_was_made(name, value):
+    """Its calls take what the constructor made of these: a later assignment would be half seen."""
+    block = fem.BlockNorm(D, w_post=Weight(torch.ones(D)))
+    before = getattr(block, name)
+    with pytest.raises(AttributeError):
+        setattr(block, name, value)
+    assert getattr(block, name) == before
+    with pytest.raises(TypeError):
+        block.weights["b_pre"] = Weight(torch.ones(D))
+
+
+def test_a_copied_norm_reads_its_own_weights(library):
+    block = fem.BlockNorm(D, w_post=Weight(torch.ones(D)))
+    twin = copy.deepcopy(block)
+    assert twin.weights["w_post"] is not block.weights["w_post"]
+    assert twin._addresses() == [twin.weights["w_post"].data_ptr(), 0, 0, 0] != block._addresses()
