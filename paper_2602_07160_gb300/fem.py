@@ -579,14 +579,14 @@ class _Settled:
         object.__setattr__(self, name, value)
 
 
-class Rope:
+class Rope(_Settled):
     """The rates of rotary positions, for ``fem_rope``: of every head the first ``rotary_dim`` elements turn in pairs,
     elements i and i + rotary_dim/2, or 2 i and 2 i + 1 where ``interleaved``, by pos * base^(-2 i / rotary_dim).
 
     ``scaling`` stretches the rates for contexts ``factor`` times as long: "linear" all of them, "base" by a larger
     base, "parts" those that turn less than ``low`` times over ``context`` positions, those that turn more than
     ``high`` times not, and those between in part.  ``amplitude`` multiplies the rotated part.  The table lives on
-    ``device``."""
+    ``device``; the attributes cannot be assigned to."""
 
     SCALINGS = {None: 0, "linear": 1, "base": 2, "parts": 3}
 
@@ -602,6 +602,7 @@ class Rope:
         self.turns = torch.tensor(signed, dtype=torch.int64).to(device)
         self.index = self.turns.get_device()
         self.rotary_dim, self.interleaved, self.amplitude = rotary_dim, int(bool(interleaved)), float(amplitude)
+        self._settle()
 
 
 def fem_rope(rope: Rope, q, k=None, positions=None, inverse: bool = False, out=None, stream=None):

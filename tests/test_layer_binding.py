@@ -88,3 +88,13 @@ def test_a_copied_norm_reads_its_own_weights(library):
     twin = copy.deepcopy(block)
     assert twin.weights["w_post"] is not block.weights["w_post"]
     assert twin._addresses() == [twin.weights["w_post"].data_ptr(), 0, 0, 0] != block._addresses()
+
+
+@pytest.mark.parametrize("name,value", [("rotary_dim", 128), ("interleaved", 1), ("amplitude", 2.0), ("turns", None), ("index", 0)])
+def test_a_rope_stays_as_it_was_made(name, value):
+    """Its table has a rate for each of the pairs that it was made for, and the kernel reads one for each that a call names."""
+    rope = fem.Rope(16, device="cpu")
+    before = getattr(rope, name)
+    with pytest.raises(AttributeError):
+        setattr(rope, name, value)
+    assert getattr(rope, name) is before
