@@ -530,6 +530,15 @@ def _current(index):
         raise ValueError("the tensors' device must be a CUDA device and the current one")
 
 
+_UNSUPPORTED = 2  # of STATUS
+
+
+def _sizes(entry, *sizes):
+    """The entries take sizes of 32 bits, and ctypes would pass on the low ones of a larger number."""
+    if max(sizes) > 0x7fffffff:
+        raise FemError(entry, _UNSUPPORTED)
+
+
 def _stream_number(stream, index):
     return torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
 
@@ -594,7 +603,8 @@ class Rope(_Settled):
                  context: float = 4096.0, low: float = 1.0, high: float = 32.0, amplitude: float = 1.0, device="cuda"):
         if scaling not in self.SCALINGS:
             raise ValueError(f"scaling must be one of {list(self.SCALINGS)}")
-        table = (ctypes.c_uint64 * max(1, rotary_dim // 2))()
+        _sizes("fem_rope_turns", rotary_dim)
+        table = (ctypes.c_uint64 * max(1, min(rotary_dim, 1024) // 2))()  # longer ones are refused
         rc = load().fem_rope_turns(rotary_dim, base, self.SCALINGS[scaling], factor, context, low, high, table)
         if rc != 0:
             raise FemError("fem_rope_turns", rc)
@@ -621,6 +631,7 @@ def fem_rope(rope: Rope, q, k=None, positions=None, inverse: bool = False, out=N
     if dtype not in _TYPES:
         raise ValueError(f"q has dtype {dtype}")
     _current(index)
+    _sizes("fem_rope", B, T, Hq, *(() if k is None else k.shape))
     if rope.index != index:
         raise ValueError("the rope's table must be on q's device")
     q_out, k_out = out if out is not None else (None, None)

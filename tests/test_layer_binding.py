@@ -98,3 +98,28 @@ def test_a_rope_stays_as_it_was_made(name, value):
     with pytest.raises(AttributeError):
         setattr(rope, name, value)
     assert getattr(rope, name) is before
+
+
+M = 1 << 32
+BF16 = torch.bfloat16
+
+
+def far(*shape, dtype=BF16):
+    """A tensor of any size, without its memory."""
+    return torch.empty(shape, dtype=dtype, device="meta")
+
+
+ROPE_SIZES = [((M, 1, 16), None), ((1, M, 16), None), ((M + 3, 2, 16), (M + 3, 1, 16)), ((3, 2, 16), (3, M + 1, 16)), ((M, 1, 3, 16), None),
+              ((1, 2, M + 3, 16), None), ((1, 2, 3, M + 16), None)]
+
+
+@pytest.mark.parametrize("q,k", ROPE_SIZES)
+def test_rope_sizes_past_32_bits_are_refused(library, q, k):
+    """The C entry takes 32 bits of each: what a call had beyond them was left out without an error."""
+    rope = fem.Rope.__new__(fem.Rope)
+    rope.__dict__.update(turns=far(8, dtype=torch.int64), index=-1, rotary_dim=16, interleaved=0, amplitude=1.0)
+    with pytest.raises(fem.FemError) as error:
+        fem.fem_rope(rope, far(*q), None if k is None else far(*k))
+    assert error.value.status == 2 and library.calls == []
+    with pytest.raises(fem.FemError):
+        fem.Rope(M + 16, device="cpu")
