@@ -631,7 +631,7 @@ def fem_rope(rope: Rope, q, k=None, positions=None, inverse: bool = False, out=N
     if dtype not in _TYPES:
         raise ValueError(f"q has dtype {dtype}")
     _current(index)
-    _sizes("fem_rope", B, T, Hq, *(() if k is None else k.shape))
+    _sizes("fem_rope", B, T, Hq, d, *(() if k is None else k.shape))
     if rope.index != index:
         raise ValueError("the rope's table must be on q's device")
     q_out, k_out = out if out is not None else (None, None)
