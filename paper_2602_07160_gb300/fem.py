@@ -685,7 +685,7 @@ def _recur_rows(name, t, shape, dtype, index):
     return t.data_ptr(), row
 
 
-def _recur_sizes(s, offsets, max_len):
+def _recur_sizes(entry, s, offsets, max_len):
     """(shape, dtype, device, address of the offsets, S, T, N, C) of a call; checks s and the offsets."""
     shape, dtype, index = s.shape, s.dtype, s.get_device()
     if dtype not in _TYPES:
@@ -695,12 +695,14 @@ def _recur_sizes(s, offsets, max_len):
         raise ValueError("s must be [B, T, C], or [N, C] with offsets")
     if offsets is None:
         B, T, C = shape
+        _sizes(entry, B, T, B * T, C)
         return shape, dtype, index, None, B, T, B * T, C
     if offsets.dim() != 1 or offsets.shape[0] < 1:
         raise ValueError("offsets must be int32 [S + 1]")
     S, (N, C) = offsets.shape[0] - 1, shape
+    _sizes(entry, S, N, C)
     off = _optional("offsets", offsets, (S + 1,), torch.int32, index)
-    return shape, dtype, index, off, S, N if max_len is None else int(max_len), N, C
+    return shape, dtype, index, off, S, N if max_len is None else min(int(max_len), 0x7fffffff), N, C
 
 
 def fem_recur_fwd(s, u, offsets=None, max_len=None, h0=None, state_rows=None, mean: bool = False, out=None,
@@ -712,7 +714,7 @@ def fem_recur_fwd(s, u, offsets=None, max_len=None, h0=None, state_rows=None, me
     h0: float32 states before the first step, [S, C], or [num_states, C] with state_rows int32 [S] (negative: none).
     state_out: where the states after the last step go, shaped like h0: None allocates [S, C], or with state_rows
     updates h0 in place; False skips them.  Returns (h, states)."""
-    shape, dtype, index, off, S, T, N, C = _recur_sizes(s, offsets, max_len)
+    shape, dtype, index, off, S, T, N, C = _recur_sizes("fem_recur_fwd", s, offsets, max_len)
     if state_out is None and state_rows is not None and h0 is not None:
         state_out = h0
     kept = state_out is not None and state_out is not False
@@ -722,6 +724,7 @@ def fem_recur_fwd(s, u, offsets=None, max_len=None, h0=None, state_rows=None, me
         num = S
     else:
         num = (state_out if h0 is None else h0).shape[0]
+        _sizes("fem_recur_fwd", num)
         if state_rows is None and num != S:
             raise ValueError("h0 and state_out must have a row for each sequence, or state_rows")
     h0_ptr = _optional("h0", h0, (num, C), torch.float32, index)
@@ -754,7 +757,7 @@ def fem_recur_bwd(s, u, h, dh, offsets=None, max_len=None, h0=None, dstate=None,
     may be None elsewhere.
 
     Returns (ds, du, dh0), dh0 None where h0 is."""
-    shape, dtype, index, off, S, T, N, C = _recur_sizes(s, offsets, max_len)
+    shape, dtype, index, off, S, T, N, C = _recur_sizes("fem_recur_bwd", s, offsets, max_len)
     (s_ptr, s_st), (h_ptr, h_st), (g_ptr, g_st) = (
         _recur_rows(name, t, shape, dtype, index) for name, t in (("s", s), ("h", h), ("dh", dh)))
     if u is None and mean:

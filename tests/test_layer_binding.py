@@ -123,3 +123,38 @@ def test_rope_sizes_past_32_bits_are_refused(library, q, k):
     assert error.value.status == 2 and library.calls == []
     with pytest.raises(fem.FemError):
         fem.Rope(M + 16, device="cpu")
+
+
+RECUR_SIZES = [((1, M, 16), None), ((M + 3, 1, 16), None), ((3, 2, M + 16), None), ((M + 40, 16), 3), ((40, M + 16), 3),
+               ((1 << 16, 1 << 16, 16), None)]
+
+
+@pytest.mark.parametrize("shape,seqs", RECUR_SIZES)
+def test_recurrence_sizes_past_32_bits_are_refused(library, shape, seqs):
+    s = far(*shape)
+    offsets = None if seqs is None else far(seqs + 1, dtype=torch.int32)
+    for call in (lambda: fem.fem_recur_fwd(s, s, offsets=offsets, state_out=False), lambda: fem.fem_recur_bwd(s, s, s, s, offsets=offsets)):
+        with pytest.raises(fem.FemError) as error:
+            call()
+        assert error.value.status == 2 and library.calls == []
+
+
+def test_more_states_or_sequences_than_32_bits_are_refused(library):
+    s, offsets = far(40, 16), far(4, dtype=torch.int32)
+    pool, rows = far(M + 5, 16, dtype=torch.float32), far(3, dtype=torch.int32)
+    for call in (lambda: fem.fem_recur_fwd(s, s, offsets=offsets, h0=pool, state_rows=rows),
+                 lambda: fem.fem_recur_fwd(s, s, offsets=offsets, state_rows=rows, state_out=pool),
+                 lambda: fem.fem_recur_fwd(s, s, offsets=far(M + 3, dtype=torch.int32))):
+        with pytest.raises(fem.FemError) as error:
+            call()
+        assert error.value.status == 2 and library.calls == []
+
+
+def test_a_bound_past_32_bits_is_still_a_bound(library, monkeypatch):
+    """max_len bounds the lengths from above: more than there can be is no more than that."""
+    s, offsets = far(40, 16), far(4, dtype=torch.int32)
+    seen = []
+    monkeypatch.setattr(library, "fem_recur_fwd", lambda *a: seen.append(a[6]) or 0, raising=False)
+    for bound in (40, (1 << 31) - 1, M + 8):
+        fem.fem_recur_fwd(s, s, offsets=offsets, max_len=bound)
+    assert seen == [40, (1 << 31) - 1, (1 << 31) - 1]
