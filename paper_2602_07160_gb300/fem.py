@@ -829,7 +829,7 @@ class BlockNorm(_Settled):
             got.append(t.data_ptr())
         return got
 
-    def _call(self, name, x, y, gate):
+    def _call(self, entry, name, x, y, gate):
         """((B, T, H, d), x's shape, x's and the branch's type, device) of a call; checks x, y and the gate."""
         shape, dtype, index = x.shape, x.dtype, x.get_device()
         if dtype not in _TYPES or not shape or shape[-1] != self.width or not x.is_contiguous():
@@ -852,6 +852,7 @@ class BlockNorm(_Settled):
                 raise ValueError("y must have x's shape or be [N, H, d] or [B, H, T, d]")
             if B * T != rows or H * d != self.width or (len(shape) == 3 and len(y_shape) == 4 and (B, T) != shape[:2]):
                 raise ValueError("y must have x's rows, and heads of its width together")
+        _sizes(entry, B, T, H, d)
         y_type = dtype if y is None else y.dtype
         if y_type not in _TYPES:
             raise ValueError(f"y has dtype {y_type}")
@@ -893,7 +894,7 @@ def fem_norm_fwd(norm: BlockNorm, x, y=None, gate=None, out=None, z_out=None, st
     x: contiguous [..., width], bf16 or float32; y and gate: x's shape, or heads [N, H, d] or [B, H, T, d] (the read's
     outputs as they are), bf16, or float32 with a float32 x; without y there is no block before and r is x.  ``out`` may
     be x itself.  Returns (r, z), z of y's type (without y of z_out's, or x's)."""
-    sizes, shape, dtype, y_type, index = norm._call("x", x, y, gate)
+    sizes, shape, dtype, y_type, index = norm._call("fem_norm_fwd", "x", x, y, gate)
     yv = gv = r_ptr = z_ptr = None
     if y is not None:
         y_shape = y.shape
@@ -932,7 +933,7 @@ def fem_norm_bwd(norm: BlockNorm, r, y=None, gate=None, dr=None, dz=None, stream
 
     Returns (dx, dy, dgate, dw_post, db_post, dw_pre, db_pre): dy and dgate of y's shape, contiguous; the weights'
     float32 [width], summed over all rows; None for what is not there (biases' where the norm has none)."""
-    sizes, shape, dtype, y_type, index = norm._call("r", r, y, gate)
+    sizes, shape, dtype, y_type, index = norm._call("fem_norm_bwd", "r", r, y, gate)
     if (norm.pre != "none") != (dz is not None):
         raise ValueError("dz goes with a pre norm")
     if y is None and dz is not None:

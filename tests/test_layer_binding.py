@@ -158,3 +158,14 @@ def test_a_bound_past_32_bits_is_still_a_bound(library, monkeypatch):
     for bound in (40, (1 << 31) - 1, M + 8):
         fem.fem_recur_fwd(s, s, offsets=offsets, max_len=bound)
     assert seen == [40, (1 << 31) - 1, (1 << 31) - 1]
+
+
+@pytest.mark.parametrize("shape,y", [((M, 16), None), ((2, M // 2, 16), (2, 4, M // 2, 4)), ((M, 16), (M, 4, 4)), ((3, M + 16), None)])
+def test_norm_sizes_past_32_bits_are_refused(library, shape, y):
+    block = fem.BlockNorm(shape[-1])
+    x = far(*shape)
+    y = x if y is None else far(*y)
+    for call in (lambda: fem.fem_norm_fwd(block, x, y), lambda: fem.fem_norm_bwd(block, x, y, dz=x)):
+        with pytest.raises(fem.FemError) as error:
+            call()
+        assert error.value.status == 2 and library.calls == []
