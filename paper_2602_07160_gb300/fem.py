@@ -271,6 +271,7 @@ def fem_tdc_conv(s, u, out=None, stream=None):
         if t.dtype != torch.float32 or not t.is_contiguous() or t.device.type != "cuda" or t.device != s.device:
             raise ValueError(f"{name} must be a contiguous float32 CUDA tensor on s's device")
     B, T, Hc = s.shape
+    _sizes("fem_tdc_conv", B, T, Hc)
     if out is None:
         out = torch.empty_like(s)
     rc = load().fem_tdc_conv(_ptr(s), _ptr(u), _ptr(out), B, T, Hc, _stream(stream, s.device))

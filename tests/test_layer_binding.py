@@ -169,3 +169,13 @@ def test_norm_sizes_past_32_bits_are_refused(library, shape, y):
         with pytest.raises(fem.FemError) as error:
             call()
         assert error.value.status == 2 and library.calls == []
+
+
+@pytest.mark.parametrize("shape", [(1, M, 1), (M + 2, 3, 1), (2, 3, M + 1)])
+def test_conditioner_sizes_past_32_bits_are_refused(library, monkeypatch, shape):
+    """The dense convolution of the recurrence's kind, through the same 32 bits."""
+    monkeypatch.setattr(torch.Tensor, "device", types.SimpleNamespace(type="cuda"))
+    s = far(*shape, dtype=torch.float32)
+    with pytest.raises(fem.FemError) as error:
+        fem.fem_tdc_conv(s, s, out=s, stream=types.SimpleNamespace(cuda_stream=0))
+    assert error.value.status == 2 and library.calls == []
