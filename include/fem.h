@@ -483,7 +483,8 @@ int fem_recur_bwd(const void *s, const void *u, const void *h, const void *dh, i
  *   z = w_pre Q(r) + b_pre                            what the next block reads
  *
  * P and Q are no norm, v / sqrt(mean v^2 + eps) or (v - mean v) / sqrt(var v + eps),
- * act nothing, the sigmoid or g sigmoid(g).  Without a norm w_post is a scale of the
+ * act nothing, the sigmoid or g sigmoid(g): below 2^-126 the sigmoid is 0, and so is g times it
+ * for the lowest finite g (of -infinity it is NaN).  Without a norm w_post is a scale of the
  * branch's channels.
  */
 typedef enum { FEM_NORM_NONE = 0, FEM_NORM_RMS = 1, FEM_NORM_LAYER = 2 } fem_norm_kind;

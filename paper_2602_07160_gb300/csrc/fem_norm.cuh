@@ -350,12 +350,13 @@ __device__ __forceinline__ Piece weighted(const Piece &x, const Piece &w, const 
   return z;
 }
 
-// The sigmoid p of g and q = 1 - p = e p, e = e^(-g): no cancellation, and with e at most 2^126 no overflow (a NaN stays
-// one).  The approximated exponential and reciprocal are off by 2 ulp and 1, the rounded exponent by |g| units of 2^-24,
+// The sigmoid p of g and q = 1 - p = e p, e = e^(-g): no cancellation, and with e at most 2^127 no overflow (a NaN stays
+// one).  Above 2^126, a gate below -87, p is flushed to 0 and with it p g and the slopes, whose limits these are: the type's
+// lowest number times a p of 2^-126 would be -4.  The approximated exponential and reciprocal are off by 2 ulp and 1, the rounded exponent by |g| units of 2^-24,
 // of what e is beside 1.
 __device__ __forceinline__ void sigmoid(float g, float &p, float &q) {
   float t;
-  asm("min.NaN.f32 %0, %1, %2;" : "=f"(t) : "f"(g * -kLog2e), "f"(126.f));
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(t) : "f"(g * -kLog2e), "f"(127.f));
   const float e = ex2_approx(t);
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(p) : "f"(1.f + e));
   q = e * p;
