@@ -446,7 +446,12 @@ int fem_rope(const fem_heads *q, const fem_heads *q_out, int Hq, const fem_heads
  *                 sequences must not share a row that is written: which of them
  *                 stays, and what the other starts from, is not defined.
  * Rows of no sequence are not written.  A sequence of length zero hands its state
- * on.  States, decays and sums are fp32; the same inputs give the same bits.  An
+ * on.  States, decays and sums are fp32; the same inputs give the same bits.  So a
+ * slow rate counts as its decay in fp32 does, 2^-25 of 1 off at a step, and a state
+ * of a horizon of 1/s steps may be off by 5 2^-25 / s of its terms, with their
+ * roundings: 1.5e-3 at s = 1e-4, and from s = 2^-25 down nothing decays.  A state that
+ * is infinite or NaN is one or the other from there on, which of them goes by how
+ * the sequence is cut; no rate, infinity included, ends that.  An
  * offset or state row outside its array is left out and recorded
  * (fem_check_device_error returns FEM_ERR_INVALID_ARG).  S = 0 does nothing.  Row
  * strides and C below 2^20, and S ceil(C / 32) below 2^27 (else

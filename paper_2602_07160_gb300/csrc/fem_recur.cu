@@ -80,8 +80,9 @@ struct Word<float, 2> {
 };
 
 // a = e^(-s) and w = 1 - a.  For s in [0, 1/8) w = s p(s), p the cubic with p(0) = 1 that is off least over the interval
-// (by 8e-8 of w; coefficients by linear programming on the condition itself), and a is 1 - w, off by 2^-25 and little
-// more: the error of a decay counts as often as its horizon has steps.  Elsewhere a is 2^(-s log2 e), off by 2 ulp and,
+// (by 8e-8 of w; coefficients by linear programming on the condition itself), and a is 1 - w, off by 0.5 units of 2^-24 for
+// slow rates and 0.75 near 1/8: the error of a decay counts as often as its horizon has steps, which is what limits slow
+// ones (a constant input's mean is 2e-4 low at s = 1e-4, 1.3e-2 at 1e-6).  Elsewhere a is 2^(-s log2 e), off by 2 ulp and,
 // by its rounded exponent, s units of 2^-24.
 template <int V>
 __device__ __forceinline__ void decay(Vec<V> s, Vec<V> &a, Vec<V> &w) {
