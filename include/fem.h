@@ -397,6 +397,8 @@ typedef struct {
  *                    (high - low) clamped to [0, 1], c_i = context theta_i /
  *                    (2 pi) the pair's turns over the original context
  * rotary even, 2 .. 1024; base, factor > 0, context > 0 and low < high finite.
+ * The rates are formed in double: off by up to (7 + |ln base| + 4 |ln factor|) 2^-53
+ * of themselves (PARTS: where 0 < g < 1 also by what c_i's roundings change g).
  */
 typedef enum { FEM_ROPE_PLAIN = 0, FEM_ROPE_LINEAR = 1, FEM_ROPE_BASE = 2, FEM_ROPE_PARTS = 3 } fem_rope_scaling;
 int fem_rope_turns(int rotary, double base, int scaling, double factor, double context, double low, double high,
@@ -415,9 +417,10 @@ int fem_rope_turns(int rotary, double base, int scaling, double factor, double c
  *   q_out, k_out : as q and k; the same pointer and strides rotate in place
  *   turns        : device, uint64 [rotary/2] (fem_rope_turns); amplitude A
  *   positions    : device, int32 [B, T], any sign, or NULL: 0 .. T - 1 in every b
- * d up to 1024, rotary even and 2 .. d.  Angles are exact to fp32 rounding for
- * positions up to 2^28 in magnitude (beyond, off by 2^-56 of a turn a position at
- * most: the rates are formed in double); the rotation is fp32 arithmetic rounded once.  An output overlaps
+ * d up to 1024, rotary even and 2 .. d.  An angle is the product of position and
+ * rate, exact modulo a turn: what a rate is off by counts |pos| times (plain rates of
+ * a base of at least 1: under 3 2^-53 rad a position, less than fp32's rounding to
+ * positions of 2^27).  The rotation is fp32 arithmetic rounded once.  An output overlaps
  * no input but its own in place.  B T and heads below 2^31 - 256 and 2^30, else
  * FEM_ERR_UNSUPPORTED.  B = 0 or T = 0 does nothing.
  */
