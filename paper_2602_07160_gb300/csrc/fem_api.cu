@@ -1001,7 +1001,7 @@ static int recur_common(RecurArgs &a, const int *offsets, int S, int T, int N, i
   a.C = C;
   return FEM_OK;
 }
-// The kernels reach a tile of rows by 32-bit offsets.
+// A thread's steps of a row are formed in 32 bits, tiles of them in 64.
 static bool strides_long(std::initializer_list<int64_t> strides, int C) {
   for (int64_t st : strides)
     if (st >= kRecurMostStride) return true;
@@ -1091,7 +1091,7 @@ int fem_recur_bwd(const void *s, const void *u, const void *h, const void *dh, i
   return recur_run(a, type, mean != 0, true, ds, static_cast<cudaStream_t>(stream));
 }
 
-// What both passes of the norms check; `back`: the gradients' arrays are looked at as well.
+// What both passes of the norms check.
 static int norm_common(NormArgs &a, const fem_norm *n, const void *x, const fem_heads *y, const fem_heads *gate) {
   if (!n || n->B < 0 || n->T < 0 || n->H <= 0 || n->d <= 0 || !known_type(n->x_type) || !known_type(n->y_type))
     return FEM_ERR_INVALID_ARG;

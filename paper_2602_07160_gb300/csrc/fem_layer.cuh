@@ -1,5 +1,5 @@
 // Shared by the operators around the read (rotary positions, the gated recurrence, norms with gate and residual):
-// their arguments as the kernels take them, and rows in pieces of eight elements.
+// their arguments as the kernels take them, and elements as they lie in memory.
 #pragma once
 
 #include <atomic>
@@ -27,7 +27,7 @@ struct RopeArgs {
 };
 cudaError_t launch_rope(const RopeArgs &a, int type, bool interleaved, int num_sms, cudaStream_t stream);
 
-constexpr long long kRecurMostStride = 1ll << 20;  // elements between rows: a tile of at most 1024 rows stays under 2^32 bytes
+constexpr long long kRecurMostStride = 1ll << 20;  // elements between rows: a thread's 16 steps of them are products of 32 bits
 struct RecurArgs {
   const void *s, *u, *h, *dh;  // h is read by the backward pass only
   long long s_st, u_st, h_st, dh_st;
@@ -83,9 +83,6 @@ __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_gr
 template <int LEFT>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-// ---------------------------------------------------------------------------
-// Eight elements of a row as they lie in memory, and in fp32.
-// ---------------------------------------------------------------------------
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 __device__ __forceinline__ uint32_t bf16_pack(float lo, float hi) {
@@ -93,41 +90,16 @@ __device__ __forceinline__ uint32_t bf16_pack(float lo, float hi) {
   return *reinterpret_cast<const uint32_t *>(&v);
 }
 
+// Eight elements of a row as they lie in memory.
 template <typename T>
 struct Eight;
 template <>
 struct Eight<__nv_bfloat16> {
   uint4 a;
-  __device__ __forceinline__ void load(const __nv_bfloat16 *p) { a = __ldcs(reinterpret_cast<const uint4 *>(p)); }
-  __device__ __forceinline__ void store(__nv_bfloat16 *p) const { *reinterpret_cast<uint4 *>(p) = a; }
-  __device__ __forceinline__ void zero() { a = make_uint4(0, 0, 0, 0); }
-  __device__ __forceinline__ void get(float (&f)[8]) const {
-    f[0] = bf16_lo(a.x), f[1] = bf16_hi(a.x), f[2] = bf16_lo(a.y), f[3] = bf16_hi(a.y);
-    f[4] = bf16_lo(a.z), f[5] = bf16_hi(a.z), f[6] = bf16_lo(a.w), f[7] = bf16_hi(a.w);
-  }
-  __device__ __forceinline__ void put(const float (&f)[8]) {
-    a = make_uint4(bf16_pack(f[0], f[1]), bf16_pack(f[2], f[3]), bf16_pack(f[4], f[5]), bf16_pack(f[6], f[7]));
-  }
 };
 template <>
 struct Eight<float> {
   float4 a, b;
-  __device__ __forceinline__ void load(const float *p) {
-    a = __ldcs(reinterpret_cast<const float4 *>(p));
-    b = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
-  }
-  __device__ __forceinline__ void store(float *p) const {
-    *reinterpret_cast<float4 *>(p) = a;
-    *(reinterpret_cast<float4 *>(p) + 1) = b;
-  }
-  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
-  __device__ __forceinline__ void get(float (&f)[8]) const {
-    f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
-  }
-  __device__ __forceinline__ void put(const float (&f)[8]) {
-    a = make_float4(f[0], f[1], f[2], f[3]);
-    b = make_float4(f[4], f[5], f[6], f[7]);
-  }
 };
 
 __device__ __forceinline__ float to_f32(float x) { return x; }
