@@ -513,7 +513,8 @@ typedef struct {
  *             not written, gate must be NULL)
  *   z       : device, [N, D] contiguous; NULL if and only if pre is NONE
  * D up to 16384, N below 2^31 - 2^20 (else FEM_ERR_UNSUPPORTED; so is a bf16 stream
- * of a float32 branch).  Sums and statistics in fp32; r rounded once, z formed from
+ * of a float32 branch).  Sums and statistics in fp32 (a row whose squares' sum passes
+ * its range normalises to 0); r rounded once, z formed from
  * r before its rounding.  Outputs overlap no input but r in place of x.  Rows that
  * do not start on 16 bytes may be read with the rest of their first 16.  N = 0 does
  * nothing.  No workspace.

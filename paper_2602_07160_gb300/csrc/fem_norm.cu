@@ -5,8 +5,8 @@
 // the first load to the last store; the sums for a norm are a butterfly in each warp and one meeting of a row's warps,
 // and the variance of a layer norm is taken about its mean, which costs a second one but no cancellation.
 //
-// Measured (32768 rows of 2048): rms, rms, a silu gate, bf16 108 us, 6.2 TB/s of its five arrays; rms, layer, a gate and
-// biases over an fp32 stream 157 us, 6.0 TB/s.
+// Measured (32768 rows of 2048): rms, rms, a silu gate, bf16 112 us, 6.0 TB/s of its five arrays; rms, layer, a gate and
+// biases over an fp32 stream 159 us, 5.9 TB/s.
 #include <algorithm>
 
 #include "fem_norm.cuh"

@@ -5,7 +5,7 @@
 // copies and neighbouring threads have neighbouring pieces; the next row's copies into shared memory are under way while
 // a row is worked on, and as a thread reads back only what it copied itself, no barrier stands between.  Elsewhere
 // neighbouring threads have neighbouring elements and read them when they need them: 32768 rows of 2048 of bf16, forward,
-// take 108 us in pieces, 157 copied whole and read singly (a way for rows that start anywhere), 770 without copies.
+// take 112 us in pieces, 172 copied whole and read singly (a way for rows that start anywhere), 810 without copies.
 #pragma once
 
 #include <algorithm>
@@ -352,8 +352,8 @@ __device__ __forceinline__ Piece weighted(const Piece &x, const Piece &w, const 
 
 // The sigmoid p of g and q = 1 - p = e p, e = e^(-g): no cancellation, and with e at most 2^127 no overflow (a NaN stays
 // one).  Above 2^126, a gate below -87, p is flushed to 0 and with it p g and the slopes, whose limits these are: the type's
-// lowest number times a p of 2^-126 would be -4.  The approximated exponential and reciprocal are off by 2 ulp and 1, the rounded exponent by |g| units of 2^-24,
-// of what e is beside 1.
+// lowest number times a p of 2^-126 would be -4.  The approximated exponential and reciprocal are off by 2 ulp and 1, the
+// rounded exponent by |g| units of 2^-24, of what e is beside 1.
 __device__ __forceinline__ void sigmoid(float g, float &p, float &q) {
   float t;
   asm("min.NaN.f32 %0, %1, %2;" : "=f"(t) : "f"(g * -kLog2e), "f"(127.f));
@@ -413,8 +413,8 @@ cudaError_t with_shape(int D, Way way, Args &&...args) {
   return F<RowShape<1024, 2, RUN>>::call(args...);
 }
 
-// Rows that start anywhere take three times an aligned one's time copied whole (16384 rows of 4097 of bf16: forward 143 us,
-// gradients 360) and ten times without (540, 1260).
+// Rows that start anywhere, copied whole, take two to three times an aligned one's time (8192 rows of 4097 of bf16: forward
+// 130 us, gradients 366, of 4096 aligned 56 and 124) and nine to ten times without (522, 1265).
 //
 // The way for a call whose rows of all arrays, staged, take `row` bytes: two of them have to fit beside the weights, in
 // blocks of 256 threads of which `blocks` are on an SM.
@@ -430,7 +430,8 @@ inline Way way_of(const NormArgs &a, bool pieces, int row, int vectors, int bloc
 }
 
 // Blocks for N rows in a shape of `rows` at a time, of which an SM holds `per_sm`: as many as there are SMs where each then
-// has fewer rows at a time.  (100 rows of 2048, gradients: 17 us, 21 in blocks of three rows.)
+// has fewer rows at a time.  (100 rows of 2048: forward 3.1 us, gradients 8.8; in blocks of three rows 4.1 and
+// 9.9.)
 inline int blocks_of(int N, int rows, int per_sm, int num_sms) {
   const int few = (N + num_sms - 1) / num_sms;
   return few < rows ? (N + few - 1) / few : std::min((N + rows - 1) / rows, per_sm * num_sms);

@@ -210,8 +210,8 @@ __device__ __forceinline__ Chunk chunk_of(const RecurArgs &a, int groups, int ch
 // A warp's copies of IN arrays into its part of shared memory: of every array a line of L V channels for each of R steps of
 // its G threads, 16 bytes a copy.  Where lines do not start on 16 bytes (GRAIN 4 or 2, what they all start on) they are
 // copied with the rest of their first 16 bytes, which are the same allocation's, and nothing past their end, and lie as
-// far off 16 bytes in shared memory.  (Five sequences of 5000 steps of 1001 channels of fp32: 113 us, in copies of 4 bytes
-// 132; eight of 2048 of bf16: 44, in single loads 52.)  Results leave in words of GRAIN bytes.
+// far off 16 bytes in shared memory.  (Five sequences of 5000 steps of 1001 channels of fp32 105 us, eight of 2048 of bf16 38;
+// in copies of 4 bytes, and in single loads, a sixth more.)  Results leave in words of GRAIN bytes.
 template <typename T, int V, int L, int R, int IN, int STAGES, bool BWD, int GRAIN>
 struct Ring {
   static constexpr bool AROUND = GRAIN < 16;
@@ -634,14 +634,16 @@ struct Split {
 
 // A line to a CTA where that fills the GPU, 16 warps an SM, to three fifths in its last round (64 or 32 bytes of channels
 // a row where there are no more), in CTAs of 8 warps if those fill it better (tiles' last rows counted); otherwise chunks, three to four CTAs an SM.
-// Eight sequences of 8192 steps of 2048 channels of bf16, 256 lines: forward 140 us in CTAs of 8 warps, 163 of 4, 207 in
-// chunks; backward 253, 303, 336.  One of 131072 steps of 256 channels, 4 lines: forward 68 us in 128 chunks, 78 in 64,
-// 74 in 160; backward 88, 107, 103.
+// Eight sequences of 8192 steps of 2048 channels of bf16, 256 lines: forward 134 us in CTAs of 8 warps, 158 of 4, 195 in
+// chunks; backward 243, 303, 317.  One of 131072 steps of 256 channels, 4 lines: forward 60 us in 128 chunks, 71 in 64,
+// 69 in 160; backward 82, 102, 99.  By the rule and the best of the others: 4 x 8192 x 768 45 us in chunks and 76, 64 x 1024 x
+// 64 11 in chunks and 12, 16 x 4096 x 1024 67 and 80, 8 x 4096 x 4096 130 and 128.  It loses where lines fill a little less than
+// three fifths: 32 x 2048 x 333 73 in chunks and 55, 20 x 1030 x 1000 39 and 32.
 //
-// Few steps fill no tile: a thread walks them alone, 0.13 us a step, where the GPU is not filled four times over, and each
-// such filling costs a walk by tiles some 2.4 us.  2048 channels of bf16, forward, by threads alone and by tiles: 8
-// sequences of 8 steps 3.1 and 3.6 us, of 16 4.2 and 3.6; 64 of 32 7.5 and 11.3, of 64 13.0 and 12.4; 512 of 16 19 and 79,
-// of 64 67 and 88.
+// Few steps fill no tile: a thread walks them alone, 0.2 us a step, where the GPU is not filled four times over, and each
+// such filling costs a walk by tiles some 2.4 us.  Forward, bf16, by threads alone and by tiles: 256 channels, 64 sequences of
+// 32 steps 5.0 and 3.0 us, 512 of 16 6.5 and 11.8, of 64 19 and 15; 2048 channels, 8 of 8 2.5 and 3.0, of 16 3.3 and 3.0; 64 of 32
+// 11 and 13, of 64 20 and 15; 512 of 16 19 and 79, of 64 68 and 90; 4096 channels, 64 of 16 8 and 22, 512 of 64 127 and 174.
 Split split_of(const RecurArgs &a, int V, int steps, int num_sms) {
   const double rounds = static_cast<double>(a.S) * a.C / (32 * V) / (4 * num_sms);
   if (a.T <= std::min(64.0, 8 + 13 * rounds)) return {0, 0, 0, 0};

@@ -8,8 +8,8 @@
 // Bound by memory: every element is read once and written once, and a token's cosines and sines are formed once for
 // all its heads, in shared memory.
 //
-// Measured: 16383 tokens of 32 + 8 heads of 128, bf16, 56 us, 6.0 TB/s; 8192 of 16 + 16 heads of 64, half of each, fp32
-// pairs of neighbours 20 us, 6.7 TB/s with what L2 keeps.
+// Measured: 16383 tokens of 32 + 8 heads of 128, bf16, 60 us, 5.6 TB/s; 8192 of 16 + 16 heads of 64, half of each, fp32
+// pairs of neighbours 25 us, 5.3 TB/s.
 #include <algorithm>
 
 #include "fem_layer.cuh"
